@@ -540,6 +540,79 @@ uint64_t tda_launch_count(void);
 tda_status tda_set_sm_budget(int32_t n_sms);
 int32_t tda_get_sm_budget(void);
 
+/* ===========================================================================
+ * The training step around the attributed linears. The paper takes the factors
+ * (a, g) of Eq. 1 from a model's forward and backward pass; the calls below are
+ * the parts of such a pass that the linear layers sit in, so that a job can make
+ * its factors with this library and attribute the update that was applied.
+ * They share the conventions above (device pointers, caller-owned buffers and
+ * scratch, asynchronous on `stream`, arguments validated before any launch) and
+ * allow CUDA-graph capture. dtype is TDA_BF16 or TDA_F32; strides are in elements.
+ * ========================================================================= */
+typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
+
+/* ---------------------------------------------------------------------------
+ * tda_embedding_forward -- out[i][:] = scale * E[tokens[i]][:] for n tokens.
+ *   E       device, V rows of d values, row stride ld_e >= d.
+ *   tokens  device, n ids of type `it`. A negative id is a padded token and gives
+ *           a zero row; an id >= V gives a row of NaN (visible, as tda_mask_gather).
+ *   out     device, n rows of d values of E's type, row stride ld_out >= d; may
+ *           not overlap E.
+ * Any d, stride and element alignment; rows aligned to 16 bytes are copied in
+ * 16-byte vectors. scale must be finite. V, n < 2^31.
+ * ------------------------------------------------------------------------- */
+tda_status tda_embedding_forward(tda_dtype dtype, const void* E, int64_t ld_e, int64_t V, int64_t d,
+                                 tda_index_type it, const void* tokens, int64_t n, float scale, void* out,
+                                 int64_t ld_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tda_embedding_backward -- the gradient of the table E:
+ *   dE[v][:] = beta * dE[v][:] + scale * sum_{i : tokens[i] = v} dout[i][:],  0 <= v < V.
+ * Ids outside [0, V) contribute nothing. The tokens are sorted by (id, position)
+ * on the GPU and a row's sum runs in that order in fp32, split at fixed places,
+ * so results do not depend on timing; one rounding to grad_dtype at the end.
+ *   dout        device, n rows of d values, row stride ld_d >= d.
+ *   grad_dtype  TDA_F32, or TDA_BF16 for bf16 dout (TDA_ERR_UNSUPPORTED for fp32 dout).
+ *   dE          device, V rows of d values of grad_dtype, row stride ld_e >= d. With
+ *               beta 0 every row is overwritten (zeros where no token names it);
+ *               with beta 1 only the named rows are touched.
+ *   ws          >= tda_embedding_workspace_size(V, d, n) bytes, 256-byte aligned.
+ * ------------------------------------------------------------------------- */
+size_t tda_embedding_workspace_size(int64_t V, int64_t d, int64_t n);
+tda_status tda_embedding_backward(tda_dtype dtype, const void* dout, int64_t ld_d, int64_t V, int64_t d,
+                                  tda_index_type it, const void* tokens, int64_t n, float scale,
+                                  tda_dtype grad_dtype, void* dE, int64_t ld_e, float beta, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tda_grad_clip -- the global norm of a list of gradient tensors and their clipping:
+ *   norm = sqrt(sum over all tensors and elements g^2),
+ *   out  = c * g,  c = 1 if norm <= max_norm, else max_norm / norm.
+ *   list      HOST array of n_tensors entries (read during the call only); the
+ *             tensors it names are on the device, each contiguous, of any size,
+ *             type TDA_F32 or TDA_BF16 (mixed lists are fine). out == in clips in place
+ *             (nothing is written when c = 1), out == NULL leaves the tensor
+ *             unclipped (it counts in the norm). No other overlap.
+ *   max_norm  > 0; +inf: c = 1.
+ *   norm      device fp32, the norm before clipping.
+ *   ws        >= tda_grad_clip_workspace_size(list, n_tensors) bytes, 16-byte aligned.
+ * The sum of squares is held in more than 32 bits and covers the whole range of
+ * fp32 values (no overflow below a norm of 3e38, no underflow). An infinite norm
+ * gives c = 0 (an infinite element then becomes NaN); a NaN element makes the norm
+ * and every output NaN.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t n;      /* elements */
+    int32_t dtype;  /* tda_dtype */
+    int32_t pad;    /* 0 */
+} tda_tensor_ref;
+
+size_t tda_grad_clip_workspace_size(const tda_tensor_ref* list, int64_t n_tensors);
+tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, void* ws,
+                         size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

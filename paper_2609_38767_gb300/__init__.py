@@ -24,6 +24,8 @@ __all__ = [
     "tda_precondition_info", "tda_score", "tda_score_engine", "tda_similarity_gram_engine", "tda_topk", "tda_route", "tda_route_calibrate",
     "tda_route_set_model", "tda_device_status", "tda_selftest_bounded_wait", "tda_last_error", "tda_version", "tda_launch_count",
     "tda_set_sm_budget", "tda_get_sm_budget",
+    "TensorRef", "tensor_list", "tda_embedding_forward", "tda_embedding_workspace_size", "tda_embedding_backward",
+    "tda_grad_clip_workspace_size", "tda_grad_clip",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -40,6 +42,7 @@ TDA_OP_PROJECT, TDA_OP_SIMILARITY_PROJECTED, TDA_OP_SIMILARITY_EXACT = 0, 1, 2
 TDA_OP_NORM_PROJECTED, TDA_OP_NORM_EXACT = 3, 4
 TDA_PC_RESET, TDA_PC_FIT_ACCUM, TDA_PC_FACTOR, TDA_PC_APPLY, TDA_PC_FACTOR_APPLY = 0, 1, 2, 3, 4
 TDA_KFAC, TDA_EKFAC = 0, 1
+TDA_I32, TDA_I64 = 0, 1
 TDA_CALIBRATE_WS_BYTES = 768 << 20
 _STATUS = {0: "TDA_OK", 1: "TDA_ERR_INVALID_ARG", 2: "TDA_ERR_UNSUPPORTED", 3: "TDA_ERR_WORKSPACE",
            4: "TDA_ERR_CUDA", 5: "TDA_ERR_NOT_SPD", 6: "TDA_ERR_TIMEOUT"}
@@ -53,6 +56,12 @@ class LayerDesc(ctypes.Structure):
 
     def __init__(self, d_in, d_out, T, k_in, k_out, seed=0, layer=0, kind=TDA_PROJ_RADEMACHER):
         super().__init__(d_in, d_out, T, k_in, k_out, seed, layer, kind)
+
+
+class TensorRef(ctypes.Structure):
+    """tda_tensor_ref."""
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("pad", ctypes.c_int32)]
 
 
 class TdaError(RuntimeError):
@@ -119,6 +128,11 @@ def load() -> ctypes.CDLL:
             "tda_launch_count": (U64, []),
             "tda_set_sm_budget": (I32, [I32]),
             "tda_get_sm_budget": (I32, []),
+            "tda_embedding_forward": (I32, [I32, P, I64, I64, I64, I32, P, I64, F, P, I64, P]),
+            "tda_embedding_workspace_size": (SZ, [I64, I64, I64]),
+            "tda_embedding_backward": (I32, [I32, P, I64, I64, I64, I32, P, I64, F, I32, P, I64, F, P, SZ, P]),
+            "tda_grad_clip_workspace_size": (SZ, [ctypes.POINTER(TensorRef), I64]),
+            "tda_grad_clip": (I32, [ctypes.POINTER(TensorRef), I64, F, P, P, SZ, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(lib, name)
@@ -337,3 +351,45 @@ def tda_selftest_bounded_wait(timeout_ns, stream=None) -> None:
 
 def tda_device_status(stream=None) -> None:
     _check(load().tda_device_status(_stream(stream)))
+
+
+def tda_embedding_forward(dtype, E, ld_e, V, d, it, tokens, n, scale, out, ld_out, stream=None):
+    _check(load().tda_embedding_forward(dtype, _ptr(E), ld_e, V, d, it, _ptr(tokens), n, scale, _ptr(out), ld_out,
+                                        _stream(stream)))
+
+
+def tda_embedding_workspace_size(V, d, n) -> int:
+    return int(load().tda_embedding_workspace_size(V, d, n))
+
+
+def tda_embedding_backward(dtype, dout, ld_d, V, d, it, tokens, n, scale, grad_dtype, dE, ld_e, beta=0.0, ws=None,
+                           ws_bytes=0, stream=None):
+    _check(load().tda_embedding_backward(dtype, _ptr(dout), ld_d, V, d, it, _ptr(tokens), n, scale, grad_dtype,
+                                         _ptr(dE), ld_e, beta, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def tensor_list(tensors, outs=None):
+    """The host array of tda_tensor_ref that tda_grad_clip takes: contiguous bf16 or fp32 tensors,
+    clipped into `outs` (same sizes and types; None entries are left unclipped), or in place
+    (outs None). The array holds addresses only: keep the tensors alive."""
+    import torch
+    kinds = {torch.float32: TDA_F32, torch.bfloat16: TDA_BF16}
+    outs = list(tensors) if outs is None else list(outs)
+    if len(outs) != len(tensors):
+        raise ValueError("tensor_list: one output per tensor")
+    refs = (TensorRef * max(len(outs), 1))()
+    for r, t, o in zip(refs, tensors, outs):
+        if not t.is_contiguous() or t.dtype not in kinds:
+            raise ValueError("tensor_list: tensors must be contiguous bf16 or fp32")
+        if o is not None and (not o.is_contiguous() or o.dtype != t.dtype or o.numel() != t.numel()):
+            raise ValueError("tensor_list: an output must have its tensor's size and type and be contiguous")
+        r.in_, r.out, r.n, r.dtype = t.data_ptr(), o.data_ptr() if o is not None else None, t.numel(), kinds[t.dtype]
+    return refs
+
+
+def tda_grad_clip_workspace_size(refs, n_tensors) -> int:
+    return int(load().tda_grad_clip_workspace_size(refs, n_tensors))
+
+
+def tda_grad_clip(refs, n_tensors, max_norm, norm, ws, ws_bytes, stream=None):
+    _check(load().tda_grad_clip(refs, n_tensors, max_norm, _ptr(norm), _ptr(ws), ws_bytes, _stream(stream)))

@@ -22,6 +22,8 @@ tda_status fail(tda_status st, const char* fmt, ...) {
     return st;
 }
 
+void clear_message() { g_msg[0] = 0; }
+
 tda_status cuda_check(cudaError_t e, const char* what) {
     if (e == cudaSuccess) return TDA_OK;
     return fail(TDA_ERR_CUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));

@@ -1,0 +1,294 @@
+// k_clip.cu -- the global norm of many gradient tensors and their clipping:
+//   norm = sqrt(sum over tensors and elements of g^2),
+//   out  = c g,  c = max_norm / norm if norm > max_norm, else 1.
+//
+// Two launches: the sums of squares (one partial per CTA, in a fixed order),
+// then the scaling, whose CTAs each add the few hundred partials up in the same
+// fixed order (no counter to clear, no atomics: the result does not depend on
+// timing). Both are bound by HBM. The bytes that must move are one read and one
+// write of every element, plus a second read of what the L2 has dropped since
+// the first; the scaling walks the tensors backwards, so it starts with what the
+// sums read last, while that is still in the L2.
+//
+// Sums: a thread adds the squares of one chunk's elements (at most 32) in fp32,
+// and the chunks' sums as an fp32 pair (the rounding error of each addition kept
+// beside it); the pairs are added across the CTA in fp64. A thread whose
+// chunk sum has left the range in which fp32 squares are exact enough (elements
+// above about 1e14, or only such below 1e-14) squares that chunk again in fp64.
+#include <cuda_bf16.h>
+
+#include "tda_internal.cuh"
+
+namespace tda {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 8192;  // elements per unit of work: 16 or 32 KiB
+constexpr int kMaxTensors = 512;  // tensors of one launch: their table travels in the kernel's parameters (16 KiB)
+
+struct ClipTensor {
+    const void* in;
+    void* out;
+    int64_t n;
+    int64_t first;  // index of its first chunk, with bit 62 set for bf16
+};
+constexpr int64_t kBf16Bit = (int64_t)1 << 62;
+
+struct ClipTable {
+    ClipTensor t[kMaxTensors];
+    int32_t count;
+    int64_t chunks;
+};
+
+__device__ __forceinline__ float2 two_sum(float a, float b) {
+    const float s = __fadd_rn(a, b), bb = __fsub_rn(s, a);
+    return make_float2(s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, bb)), __fsub_rn(b, bb)));
+}
+
+// The tensor that holds chunk c: the last one whose first chunk is <= c.
+__device__ __forceinline__ int find_tensor(const ClipTable& T, int64_t c) {
+    int lo = 0, hi = T.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((T.t[mid].first & ~kBf16Bit) <= c)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
+}
+
+struct Sum {
+    float hi = 0.f, lo = 0.f;  // sum of squares of the ordinary chunks
+    double wide = 0.0;         // of the chunks whose squares leave fp32's range
+};
+
+// Adds the squares of v[0..N): one chunk's elements of this thread.
+template <int N>
+__device__ __forceinline__ void add_squares(Sum& s, const float* v) {
+    float q = 0.f, top = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        q = fmaf(v[i], v[i], q);
+        top = fmaxf(top, fabsf(v[i]));
+    }
+    if (q < 1e30f && (q > 1e-28f || top == 0.f)) {
+        const float2 r = two_sum(s.hi, q);
+        s.hi = r.x;
+        s.lo += r.y;
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < N; ++i) s.wide = fma((double)v[i], (double)v[i], s.wide);
+    }
+}
+
+__device__ __forceinline__ void unpack(const uint4& r, float* v, const float*) {
+    v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y), v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ void unpack(const uint4& r, float* v, const __nv_bfloat16*) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack(const float* v, const float*) {
+    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint4 pack(const float* v, const __nv_bfloat16*) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_f(float x, float* p) { *p = x; }
+__device__ __forceinline__ void from_f(float x, __nv_bfloat16* p) { *p = __float2bfloat16_rn(x); }
+
+template <typename T>
+__device__ __forceinline__ void chunk_squares(Sum& s, const T* g, int n) {
+    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, U = 4;
+    if (n == kChunk && ((uintptr_t)g & 15) == 0) {
+#pragma unroll
+        for (int j = 0; j < kVecs / kThreads; j += U) {
+            uint4 r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = __ldg((const uint4*)g + (j + u) * kThreads + threadIdx.x);
+            float v[U * E];
+#pragma unroll
+            for (int u = 0; u < U; ++u) unpack(r[u], v + u * E, g);
+            add_squares<U * E>(s, v);
+        }
+        return;
+    }
+    for (int i = threadIdx.x; i < n; i += 8 * kThreads) {  // a tensor's ragged end, or an unaligned one
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + u * kThreads < n ? to_f(g[i + u * kThreads]) : 0.f;
+        add_squares<8>(s, v);
+    }
+}
+
+// CTA b owns chunks [chunks b / grid, chunks (b+1) / grid).
+__global__ void __launch_bounds__(kThreads) clip_squares_kernel(const __grid_constant__ ClipTable T, double* part) {
+    const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
+    Sum s;
+    int t = find_tensor(T, c0);
+    for (int64_t c = c0; c < c1; ++c) {
+        while (t + 1 < T.count && (T.t[t + 1].first & ~kBf16Bit) <= c) ++t;
+        const int64_t off = (c - (T.t[t].first & ~kBf16Bit)) * kChunk, left = T.t[t].n - off;
+        const int n = left < kChunk ? (int)left : kChunk;
+        if (T.t[t].first & kBf16Bit)
+            chunk_squares(s, (const __nv_bfloat16*)T.t[t].in + off, n);
+        else
+            chunk_squares(s, (const float*)T.t[t].in + off, n);
+    }
+    double d = (double)s.hi + (double)s.lo + s.wide;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    __shared__ double w[kThreads / 32];
+    if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = d;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kThreads / 32; ++i) d += w[i];
+        part[blockIdx.x] = d;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const T* g, T* out, int n, float c) {
+    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, U = 4;
+    if (n == kChunk && (((uintptr_t)g | (uintptr_t)out) & 15) == 0) {
+#pragma unroll
+        for (int j = 0; j < kVecs / kThreads; j += U) {
+            uint4 r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = __ldcs((const uint4*)g + (j + u) * kThreads + threadIdx.x);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[E];
+                unpack(r[u], v, g);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] *= c;
+                __stcs((uint4*)out + (j + u) * kThreads + threadIdx.x, pack(v, g));
+            }
+        }
+        return;
+    }
+    for (int i = threadIdx.x; i < n; i += 8 * kThreads) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = i + u * kThreads < n ? to_f(g[i + u * kThreads]) : 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (i + u * kThreads < n) from_f(v[u] * c, out + i + u * kThreads);
+    }
+}
+
+// n_part partials of all launches of clip_squares_kernel. norm_out is written by the last table's first CTA.
+__global__ void __launch_bounds__(kThreads)
+clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n_part, float max_norm, float* norm_out) {
+    double d = 0.0;
+    for (int i = threadIdx.x; i < n_part; i += kThreads) d += part[i];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    __shared__ double w[kThreads / 32];
+    __shared__ float coef;
+    if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = d;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kThreads / 32; ++i) d += w[i];
+        const double norm = sqrt(d);
+        // a NaN norm is not <= max_norm and passes into every output
+        coef = norm <= (double)max_norm ? 1.f : (float)((double)max_norm / norm);
+        if (norm_out && blockIdx.x == 0) *norm_out = (float)norm;
+    }
+    __syncthreads();
+    const float c = coef;
+    const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
+    if (c1 <= c0) return;
+    int t = find_tensor(T, c1 - 1);
+    for (int64_t k = c1 - 1; k >= c0; --k) {
+        while ((T.t[t].first & ~kBf16Bit) > k) --t;
+        if (!T.t[t].out || (c == 1.f && T.t[t].out == T.t[t].in)) continue;  // norm only, or nothing changes in place
+        const int64_t off = (k - (T.t[t].first & ~kBf16Bit)) * kChunk, left = T.t[t].n - off;
+        const int n = left < kChunk ? (int)left : kChunk;
+        if (T.t[t].first & kBf16Bit)
+            chunk_scale((const __nv_bfloat16*)T.t[t].in + off, (__nv_bfloat16*)T.t[t].out + off, n, c);
+        else
+            chunk_scale((const float*)T.t[t].in + off, (float*)T.t[t].out + off, n, c);
+    }
+}
+
+int sm_count() {
+    static std::atomic<int> sms{0};
+    int v = sms.load(std::memory_order_relaxed);
+    if (!v) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0)
+            v = 152;
+        sms.store(v, std::memory_order_relaxed);
+    }
+    return v;
+}
+
+// Fills the table with tensors from *i on (empty ones left out); false when there is nothing left.
+bool next_table(const tda_tensor_ref* list, int64_t n_tensors, int64_t* i, ClipTable* T) {
+    T->count = 0;
+    T->chunks = 0;
+    for (; *i < n_tensors && T->count < kMaxTensors; ++*i) {
+        const tda_tensor_ref& r = list[*i];
+        if (r.n == 0) continue;
+        ClipTensor& t = T->t[T->count++];
+        t.in = r.in;
+        t.out = r.out;
+        t.n = r.n;
+        t.first = T->chunks | (r.dtype == TDA_BF16 ? kBf16Bit : 0);
+        T->chunks += (r.n + kChunk - 1) / kChunk;
+    }
+    return T->count > 0;
+}
+
+}  // namespace
+
+// CTAs of one table's launches: enough to fill the SMs, at most one per chunk.
+constexpr int kClipCtasPerSm = 8;
+constexpr int64_t kClipMaxGrid = 4096;  // bounds the partials of one launch (any GPU up to 512 SMs)
+
+size_t clip_workspace_bytes(int64_t n_tensors) {
+    const int64_t tables = (n_tensors + kMaxTensors - 1) / kMaxTensors;
+    return sizeof(double) * (size_t)(kClipMaxGrid * (tables > 1 ? tables : 1));
+}
+
+cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, double* part,
+                             cudaStream_t s) {
+    const int64_t most = (int64_t)sm_count() * kClipCtasPerSm < kClipMaxGrid ? (int64_t)sm_count() * kClipCtasPerSm
+                                                                             : kClipMaxGrid;
+    ClipTable T;
+    int n_part = 0;
+    for (int64_t i = 0; next_table(list, n_tensors, &i, &T);) {
+        const int64_t grid = T.chunks < most ? T.chunks : most;
+        note_launches(1);
+        clip_squares_kernel<<<(unsigned)grid, kThreads, 0, s>>>(T, part + n_part);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        n_part += (int)grid;
+    }
+    bool first = true;
+    for (int64_t i = 0; next_table(list, n_tensors, &i, &T) || first; first = false) {
+        const int64_t grid = T.chunks < 1 ? 1 : T.chunks < most ? T.chunks : most;
+        note_launches(1);
+        clip_scale_kernel<<<(unsigned)grid, kThreads, 0, s>>>(T, part, n_part, max_norm, first ? norm : nullptr);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace tda

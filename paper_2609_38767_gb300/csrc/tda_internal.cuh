@@ -59,6 +59,7 @@ unsigned int* device_error_word();
 
 // Thread-local error message helpers (api.cu).
 tda_status fail(tda_status st, const char* fmt, ...);
+void clear_message();
 tda_status cuda_check(cudaError_t e, const char* what);
 
 // ---------------------------------------------------------------------------
@@ -220,6 +221,19 @@ cudaError_t launch_score_splitk(const float* Q, int64_t n_q, int64_t ld_q, const
                                 float* part, bool tc, cudaStream_t s);
 cudaError_t launch_topk(const float* S, int64_t n_q, int64_t n_t, int64_t ld_S, int32_t k,
                         int32_t* idx, float* val, cudaStream_t s);
+
+// The training step's operators: embedding lookup and gradient (k_embedding.cu), gradient norm and
+// clipping (k_clip.cu).
+size_t embedding_workspace_bytes(int64_t d, int64_t n);
+cudaError_t launch_embedding_forward(tda_dtype dt, const void* E, int64_t ld_e, int64_t V, int64_t d,
+                                     tda_index_type it, const void* tok, int64_t n, float scale, void* out,
+                                     int64_t ld_out, cudaStream_t s);
+cudaError_t launch_embedding_backward(tda_dtype dt, const void* dout, int64_t ld_d, int64_t V, int64_t d,
+                                      tda_index_type it, const void* tok, int64_t n, float scale, tda_dtype gt,
+                                      void* dE, int64_t ld_e, float beta, void* ws, cudaStream_t s);
+size_t clip_workspace_bytes(int64_t n_tensors);
+cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, double* part,
+                             cudaStream_t s);
 
 // State header layout of the preconditioner (doubles).
 enum { kPcLambda = 0, kPcMeanEig = 1, kPcFailedPivot = 2, kPcNTotal = 3, kPcHeaderDoubles = 8 };
