@@ -552,6 +552,70 @@ int32_t tda_get_sm_budget(void);
 typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
 
 /* ---------------------------------------------------------------------------
+ * tda_linear_forward -- one linear layer over M tokens (rows), z = W a + b:
+ *   Z = X W^T + bias,   Y = act(Z) + R.
+ *   X     [M][d_in], the layer's input: the factor A of Eq. 1 (ld_x >= d_in).
+ *   W     [d_out][d_in] (ld_w >= d_in).
+ *   bias  [d_out], or NULL.   R  [M][d_out] residual, or NULL (ld_r >= d_out).
+ *   Y     [M][d_out] (ld_y >= d_out). Y may be R (same pointer and stride).
+ *   Z     [M][d_out] pre-activation for tda_linear_backward, or NULL (ld_z >= d_out).
+ * Every tensor is of type L->dtype. Sums are fp32 (bf16: products of bf16 values,
+ * exact; fp32: every product to 2^-24), one rounding per output; act is applied to
+ * the unrounded sum. Activations: TDA_ACT_GELU is z Phi(z) (the normal
+ * distribution function), TDA_ACT_GELU_TANH its tanh approximation,
+ * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.
+ *
+ * tda_linear_backward -- the layer's gradients, given dY (the gradient of the loss
+ * by Y) and the Z that the forward pass kept:
+ *   B  = dY * act'(Z)            the factor B of Eq. 1: with A = X it is what
+ *                                tda_project and the other calls above take;
+ *   dX = B W,   dW = beta dW + B^T X,   db = beta db + sum of B's rows.
+ * dY is also the gradient of R. B is rounded to L->dtype where it is stored, and the
+ * two products read it as stored (bf16: one rounding of at most 2^-8 per element, of
+ * the size of the outputs' own); db sums the unrounded values in fp32.
+ *   Z    NULL allowed for TDA_ACT_NONE, whose factor is dY itself.
+ *   B    [M][d_out]; NULL allowed for TDA_ACT_NONE. May be dY (same pointer, stride).
+ *   dX, dW, db   NULL: not computed (X, W are then not read).
+ *   grad_dtype   type of dW and db: TDA_F32, or TDA_BF16 for bf16 layers
+ *                (TDA_ERR_UNSUPPORTED for fp32 layers).  beta 0 overwrites.
+ *
+ * A padded token is a zero row of dY. M may be 0 (dW and db become beta times
+ * themselves). ws: scratch, 256-byte aligned. tda_linear_workspace_size(op, L, M)
+ * bytes are enough when every tensor starts on 16 bytes and every stride is its
+ * row length, or any multiple of 8 elements that is no shorter; for any other
+ * pointers or strides add TDA_LINEAR_ANY_STRIDE to op. Runs on sm_103 only.
+ * An infinite or NaN element of X or W makes the outputs that it enters
+ * non-finite (for fp32 layers NaN).
+ * ------------------------------------------------------------------------- */
+typedef enum {
+    TDA_ACT_NONE = 0,
+    TDA_ACT_RELU = 1,
+    TDA_ACT_GELU = 2,
+    TDA_ACT_GELU_TANH = 3,
+    TDA_ACT_SILU = 4
+} tda_activation;
+
+typedef struct {
+    int64_t d_in;
+    int64_t d_out;
+    int32_t act;   /* tda_activation */
+    int32_t dtype; /* tda_dtype: TDA_BF16 or TDA_F32 */
+} tda_linear_desc;
+
+#define TDA_LINEAR_FORWARD 0
+#define TDA_LINEAR_BACKWARD 1
+#define TDA_LINEAR_ANY_STRIDE 256
+
+tda_status tda_linear_workspace_size(int32_t op, const tda_linear_desc* L, int64_t M, size_t* bytes);
+tda_status tda_linear_forward(const tda_linear_desc* L, const void* X, int64_t ld_x, int64_t M, const void* W,
+                              int64_t ld_w, const void* bias, const void* R, int64_t ld_r, void* Y, int64_t ld_y,
+                              void* Z, int64_t ld_z, void* ws, size_t ws_bytes, void* stream);
+tda_status tda_linear_backward(const tda_linear_desc* L, const void* dY, int64_t ld_dy, const void* Z, int64_t ld_z,
+                               int64_t M, const void* X, int64_t ld_x, const void* W, int64_t ld_w, void* B,
+                               int64_t ld_b, void* dX, int64_t ld_dx, void* dW, int64_t ld_dw, void* db,
+                               tda_dtype grad_dtype, float beta, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * tda_embedding_forward -- out[i][:] = scale * E[tokens[i]][:] for n tokens.
  *   E       device, V rows of d values, row stride ld_e >= d.
  *   tokens  device, n ids of type `it`. A negative id is a padded token and gives

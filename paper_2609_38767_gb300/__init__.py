@@ -26,6 +26,7 @@ __all__ = [
     "tda_set_sm_budget", "tda_get_sm_budget",
     "TensorRef", "tensor_list", "tda_embedding_forward", "tda_embedding_workspace_size", "tda_embedding_backward",
     "tda_grad_clip_workspace_size", "tda_grad_clip",
+    "LinearDesc", "tda_linear_workspace_size", "tda_linear_forward", "tda_linear_backward",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -43,6 +44,8 @@ TDA_OP_NORM_PROJECTED, TDA_OP_NORM_EXACT = 3, 4
 TDA_PC_RESET, TDA_PC_FIT_ACCUM, TDA_PC_FACTOR, TDA_PC_APPLY, TDA_PC_FACTOR_APPLY = 0, 1, 2, 3, 4
 TDA_KFAC, TDA_EKFAC = 0, 1
 TDA_I32, TDA_I64 = 0, 1
+TDA_ACT_NONE, TDA_ACT_RELU, TDA_ACT_GELU, TDA_ACT_GELU_TANH, TDA_ACT_SILU = 0, 1, 2, 3, 4
+TDA_LINEAR_FORWARD, TDA_LINEAR_BACKWARD, TDA_LINEAR_ANY_STRIDE = 0, 1, 256
 TDA_CALIBRATE_WS_BYTES = 768 << 20
 _STATUS = {0: "TDA_OK", 1: "TDA_ERR_INVALID_ARG", 2: "TDA_ERR_UNSUPPORTED", 3: "TDA_ERR_WORKSPACE",
            4: "TDA_ERR_CUDA", 5: "TDA_ERR_NOT_SPD", 6: "TDA_ERR_TIMEOUT"}
@@ -56,6 +59,14 @@ class LayerDesc(ctypes.Structure):
 
     def __init__(self, d_in, d_out, T, k_in, k_out, seed=0, layer=0, kind=TDA_PROJ_RADEMACHER):
         super().__init__(d_in, d_out, T, k_in, k_out, seed, layer, kind)
+
+
+class LinearDesc(ctypes.Structure):
+    """tda_linear_desc."""
+    _fields_ = [("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64), ("act", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+    def __init__(self, d_in, d_out, act=TDA_ACT_NONE, dtype=TDA_BF16):
+        super().__init__(d_in, d_out, act, dtype)
 
 
 class TensorRef(ctypes.Structure):
@@ -128,6 +139,11 @@ def load() -> ctypes.CDLL:
             "tda_launch_count": (U64, []),
             "tda_set_sm_budget": (I32, [I32]),
             "tda_get_sm_budget": (I32, []),
+            "tda_linear_workspace_size": (I32, [I32, ctypes.POINTER(LinearDesc), I64, ctypes.POINTER(SZ)]),
+            "tda_linear_forward": (I32, [ctypes.POINTER(LinearDesc), P, I64, I64, P, I64, P, P, I64, P, I64, P, I64, P,
+                                         SZ, P]),
+            "tda_linear_backward": (I32, [ctypes.POINTER(LinearDesc), P, I64, P, I64, I64, P, I64, P, I64, P, I64, P,
+                                          I64, P, I64, P, I32, F, P, SZ, P]),
             "tda_embedding_forward": (I32, [I32, P, I64, I64, I64, I32, P, I64, F, P, I64, P]),
             "tda_embedding_workspace_size": (SZ, [I64, I64, I64]),
             "tda_embedding_backward": (I32, [I32, P, I64, I64, I64, I32, P, I64, F, I32, P, I64, F, P, SZ, P]),
@@ -351,6 +367,25 @@ def tda_selftest_bounded_wait(timeout_ns, stream=None) -> None:
 
 def tda_device_status(stream=None) -> None:
     _check(load().tda_device_status(_stream(stream)))
+
+
+def tda_linear_workspace_size(op, L, M) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().tda_linear_workspace_size(op, ctypes.byref(L), M, ctypes.byref(b)))
+    return int(b.value)
+
+
+def tda_linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z=None, ld_z=0, ws=None, ws_bytes=0,
+                       stream=None):
+    _check(load().tda_linear_forward(ctypes.byref(L), _ptr(X), ld_x, M, _ptr(W), ld_w, _ptr(bias), _ptr(R), ld_r,
+                                     _ptr(Y), ld_y, _ptr(Z), ld_z, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def tda_linear_backward(L, dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B, ld_b, dX, ld_dx, dW, ld_dw, db,
+                        grad_dtype=TDA_F32, beta=0.0, ws=None, ws_bytes=0, stream=None):
+    _check(load().tda_linear_backward(ctypes.byref(L), _ptr(dY), ld_dy, _ptr(Z), ld_z, M, _ptr(X), ld_x, _ptr(W), ld_w,
+                                      _ptr(B), ld_b, _ptr(dX), ld_dx, _ptr(dW), ld_dw, _ptr(db), grad_dtype, beta,
+                                      _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def tda_embedding_forward(dtype, E, ld_e, V, d, it, tokens, n, scale, out, ld_out, stream=None):

@@ -2,7 +2,7 @@
 // (include/tda.h): host-side argument validation and kernel dispatch.
 #include <cmath>
 
-#include "tda_internal.cuh"
+#include "linear.cuh"
 
 using namespace tda;
 
@@ -26,9 +26,123 @@ tda_status check_table(tda_dtype dtype, int64_t V, int64_t d, int32_t it, const 
     return TDA_OK;
 }
 
+tda_status check_linear(const tda_linear_desc* L, int64_t M, const char* who) {
+    if (!L) return fail(TDA_ERR_INVALID_ARG, "%s: layer descriptor is NULL", who);
+    if (L->d_in < 1 || L->d_out < 1 || L->d_in > kMaxCount || L->d_out > kMaxCount || M < 0 || M > kMaxCount)
+        return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes d_in=%lld d_out=%lld M=%lld", who, (long long)L->d_in,
+                    (long long)L->d_out, (long long)M);
+    if (L->act < TDA_ACT_NONE || L->act > TDA_ACT_SILU) return fail(TDA_ERR_INVALID_ARG, "%s: bad activation %d", who, L->act);
+    if (!float_type(L->dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
+    return TDA_OK;
+}
+
+// A tensor argument of `cols` values a row: present unless optional, aligned to its type, rows not overlapping.
+// Row strides stay below 2^39 bytes, the tensor maps' limit.
+tda_status check_rows(const void* p, int64_t ld, int64_t cols, int32_t dt, bool optional, const char* name) {
+    if (!p) return optional ? TDA_OK : fail(TDA_ERR_INVALID_ARG, "%s is NULL", name);
+    if (!aligned_to(p, el_size(dt))) return fail(TDA_ERR_INVALID_ARG, "%s is misaligned", name);
+    if (ld < cols || ld > (1LL << 37)) return fail(TDA_ERR_INVALID_ARG, "%s: row stride %lld for %lld columns", name,
+                                                   (long long)ld, (long long)cols);
+    return TDA_OK;
+}
+
+tda_status linear_device(unsigned int** err) {
+    if (!linear_tc_available()) return fail(TDA_ERR_UNSUPPORTED, "the linear layer needs an sm_103 device");
+    *err = device_error_word();
+    if (!*err) return fail(TDA_ERR_CUDA, "cannot resolve the device error word");
+    return TDA_OK;
+}
+
+tda_status check_ws(const void* ws, size_t ws_bytes, size_t need, const char* who) {
+    if (need && (!ws || ws_bytes < need))
+        return fail(TDA_ERR_WORKSPACE, "%s needs >= %zu bytes of ws, got %zu", who, need, ws ? ws_bytes : 0);
+    if (need && !aligned_to(ws, 256)) return fail(TDA_ERR_INVALID_ARG, "ws must be 256-byte aligned");
+    return TDA_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+tda_status tda_linear_workspace_size(int32_t op, const tda_linear_desc* L, int64_t M, size_t* bytes) {
+    clear_message();
+    if (!bytes) return fail(TDA_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = 0;
+    tda_status st = check_linear(L, M, "tda_linear_workspace_size");
+    if (st) return st;
+    const int32_t pass = op & ~TDA_LINEAR_ANY_STRIDE;
+    if (pass != TDA_LINEAR_FORWARD && pass != TDA_LINEAR_BACKWARD) return fail(TDA_ERR_INVALID_ARG, "bad linear op %d", op);
+    *bytes = M == 0 ? 0
+                    : linear_ws_bound(pass == TDA_LINEAR_BACKWARD, M, L->d_in, L->d_out, (tda_dtype)L->dtype,
+                                      (op & TDA_LINEAR_ANY_STRIDE) != 0);
+    return TDA_OK;
+}
+
+tda_status tda_linear_forward(const tda_linear_desc* L, const void* X, int64_t ld_x, int64_t M, const void* W,
+                              int64_t ld_w, const void* bias, const void* R, int64_t ld_r, void* Y, int64_t ld_y,
+                              void* Z, int64_t ld_z, void* ws, size_t ws_bytes, void* stream) {
+    clear_message();
+    tda_status st = check_linear(L, M, "tda_linear_forward");
+    if (st) return st;
+    if (M == 0) return TDA_OK;
+    if ((st = check_rows(X, ld_x, L->d_in, L->dtype, false, "X")) ||
+        (st = check_rows(W, ld_w, L->d_in, L->dtype, false, "W")) ||
+        (st = check_rows(bias, L->d_out, L->d_out, L->dtype, true, "bias")) ||
+        (st = check_rows(R, ld_r, L->d_out, L->dtype, true, "R")) ||
+        (st = check_rows(Y, ld_y, L->d_out, L->dtype, false, "Y")) ||
+        (st = check_rows(Z, ld_z, L->d_out, L->dtype, true, "Z")))
+        return st;
+    LinearForward f;
+    f.M = M, f.d_in = L->d_in, f.d_out = L->d_out, f.act = L->act, f.dt = (tda_dtype)L->dtype;
+    f.X = X, f.W = W, f.bias = bias, f.R = R, f.Y = Y, f.Z = Z;
+    f.ld_x = ld_x, f.ld_w = ld_w, f.ld_r = ld_r, f.ld_y = ld_y, f.ld_z = ld_z;
+    if ((st = check_ws(ws, ws_bytes, linear_forward_ws(f), "tda_linear_forward"))) return st;
+    unsigned int* err = nullptr;
+    if ((st = linear_device(&err))) return st;
+    return cuda_check(launch_linear_forward(f, ws, err, (cudaStream_t)stream), "linear forward");
+}
+
+tda_status tda_linear_backward(const tda_linear_desc* L, const void* dY, int64_t ld_dy, const void* Z, int64_t ld_z,
+                               int64_t M, const void* X, int64_t ld_x, const void* W, int64_t ld_w, void* B,
+                               int64_t ld_b, void* dX, int64_t ld_dx, void* dW, int64_t ld_dw, void* db,
+                               tda_dtype grad_dtype, float beta, void* ws, size_t ws_bytes, void* stream) {
+    clear_message();
+    tda_status st = check_linear(L, M, "tda_linear_backward");
+    if (st) return st;
+    if (!float_type(grad_dtype)) return fail(TDA_ERR_INVALID_ARG, "tda_linear_backward: grad_dtype must be TDA_F32 or TDA_BF16");
+    if (!std::isfinite(beta)) return fail(TDA_ERR_INVALID_ARG, "tda_linear_backward: beta must be finite");
+    if (L->dtype == TDA_F32 && grad_dtype == TDA_BF16)
+        return fail(TDA_ERR_UNSUPPORTED, "tda_linear_backward: bf16 gradients need a bf16 layer");
+    const bool act = L->act != TDA_ACT_NONE;
+    if ((st = check_rows(dW, ld_dw, L->d_in, grad_dtype, true, "dW")) ||
+        (st = check_rows(db, L->d_out, L->d_out, grad_dtype, true, "db")))
+        return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (M == 0) {
+        if (dW && beta != 1.f &&
+            (st = cuda_check(launch_scale_matrix(grad_dtype, dW, L->d_out, L->d_in, ld_dw, beta, s), "scale dW")))
+            return st;
+        if (db && beta != 1.f)
+            return cuda_check(launch_scale_matrix(grad_dtype, db, 1, L->d_out, L->d_out, beta, s), "scale db");
+        return TDA_OK;
+    }
+    if ((st = check_rows(dY, ld_dy, L->d_out, L->dtype, false, "dY")) ||
+        (st = check_rows(Z, ld_z, L->d_out, L->dtype, !act, "Z")) ||
+        (st = check_rows(B, ld_b, L->d_out, L->dtype, !act, "B")) ||
+        (st = check_rows(X, ld_x, L->d_in, L->dtype, !dW, "X")) ||
+        (st = check_rows(W, ld_w, L->d_in, L->dtype, !dX, "W")) ||
+        (st = check_rows(dX, ld_dx, L->d_in, L->dtype, true, "dX")))
+        return st;
+    LinearBackward b;
+    b.M = M, b.d_in = L->d_in, b.d_out = L->d_out, b.act = L->act, b.dt = (tda_dtype)L->dtype, b.gt = grad_dtype;
+    b.beta = beta;
+    b.dY = dY, b.Z = Z, b.X = X, b.W = W, b.B = B, b.dX = dX, b.dW = dW, b.db = db;
+    b.ld_dy = ld_dy, b.ld_z = ld_z, b.ld_x = ld_x, b.ld_w = ld_w, b.ld_b = ld_b, b.ld_dx = ld_dx, b.ld_dw = ld_dw;
+    if ((st = check_ws(ws, ws_bytes, linear_backward_ws(b), "tda_linear_backward"))) return st;
+    unsigned int* err = nullptr;
+    if ((st = linear_device(&err))) return st;
+    return cuda_check(launch_linear_backward(b, ws, err, s), "linear backward");
+}
 
 tda_status tda_embedding_forward(tda_dtype dtype, const void* E, int64_t ld_e, int64_t V, int64_t d,
                                  tda_index_type it, const void* tokens, int64_t n, float scale, void* out,

@@ -1,0 +1,111 @@
+// linear.cuh -- what the translation units of the linear layer share: the
+// activations with their derivatives, the operands and the epilogue of the
+// tensor-core product. Internal.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "tda_internal.cuh"
+
+namespace tda {
+
+// ------------------------------------------------------------------ activations
+// Values in forms without cancellation or overflow: gelu through erfc, the tanh form as
+// z sigmoid(2u) (tanh(u) = 2 sigmoid(2u) - 1). exp of a large argument gives 0 or inf,
+// and 1 / (1 + inf) = 0, so finite z of any size give finite results.
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if (ACT == TDA_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
+    if (ACT == TDA_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+    if (ACT == TDA_ACT_GELU_TANH) return z * sigmoid(1.5957691216057308f * fmaf(0.044715f * z * z, z, z));
+    if (ACT == TDA_ACT_SILU) return z * sigmoid(z);
+    return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if (ACT == TDA_ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
+    if (ACT == TDA_ACT_GELU) {
+        const float phi = 0.39894228040143268f * expf(-0.5f * z * z);
+        return fmaf(z, phi, 0.5f * erfcf(-0.70710678118654752f * z));
+    }
+    if (ACT == TDA_ACT_GELU_TANH) {
+        // past |z| = 10 the slope is 0 or 1 to fp32, while z^2 or the exponential could overflow;
+        // 1 - s = e s without the cancellation
+        const float c = fminf(fmaxf(z, -10.f), 10.f);
+        const float e = expf(-1.5957691216057308f * fmaf(0.044715f * c * c, c, c)), s = 1.f / (1.f + e);
+        const float r = fmaf(c * s * (e * s), 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f), s);
+        return z != z ? z : r;
+    }
+    if (ACT == TDA_ACT_SILU) {
+        const float c = fmaxf(z, -88.f), e = expf(-c), s = 1.f / (1.f + e);  // 1 - s = e s; e stays finite
+        const float r = s * fmaf(c, e * s, 1.f);
+        return z != z ? z : r;
+    }
+    return 1.f;
+}
+
+// ------------------------------------------------------------------ the tensor-core product
+// D[i][j] = sum_k P[i][k] Q[j][k]. An operand is a matrix in memory of `rows` rows of `cols`
+// contiguous bf16 values, K-major (rows are i or j, columns k) or MN-major (mn: rows are k),
+// with 16-byte aligned rows. planes = 3: three such matrices whose sum is an fp32 operand.
+struct LinearOperand {
+    const void* p;
+    int64_t rows, cols, ld;
+    int64_t plane_stride;  // elements
+    int planes;
+    bool mn;
+    int64_t extent() const { return mn ? cols : rows; }
+    int64_t depth() const { return mn ? rows : cols; }
+};
+
+// The epilogue: z = D + bias[n]; Z = z; Y = act(z) + r_scale R. All of the output's type.
+struct LinearEpilogue {
+    int64_t M, N;  // output rows and columns
+    const void* bias;
+    const void* R;
+    int64_t ld_r;
+    float r_scale;
+    void* Y;
+    int64_t ld_y;
+    void* Z;
+    int64_t ld_z;
+    int act;
+    int vec;  // all of bias, R, Y, Z may be moved four values at a time
+};
+
+// ------------------------------------------------------------------ the two passes (k_linear.cu)
+struct LinearForward {
+    int64_t M, d_in, d_out;
+    int act;
+    tda_dtype dt;
+    const void *X, *W, *bias, *R;
+    void *Y, *Z;
+    int64_t ld_x, ld_w, ld_r, ld_y, ld_z;
+};
+struct LinearBackward {
+    int64_t M, d_in, d_out;
+    int act;
+    tda_dtype dt, gt;
+    float beta;
+    const void *dY, *Z, *X, *W;
+    void *B, *dX, *dW, *db;
+    int64_t ld_dy, ld_z, ld_x, ld_w, ld_b, ld_dx, ld_dw;
+};
+size_t linear_forward_ws(const LinearForward& f);
+size_t linear_backward_ws(const LinearBackward& b);
+// The same from the sizes alone: packed = every operand needs planes of its own.
+size_t linear_ws_bound(bool backward, int64_t M, int64_t d_in, int64_t d_out, tda_dtype dt, bool packed);
+cudaError_t launch_linear_forward(const LinearForward& f, void* ws, unsigned int* err, cudaStream_t s);
+cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned int* err, cudaStream_t s);
+cudaError_t launch_scale_matrix(tda_dtype dt, void* x, int64_t rows, int64_t cols, int64_t ld, float beta,
+                                cudaStream_t s);
+
+bool linear_tc_available();
+// One product with its epilogue; out: type of bias, R, Y, Z.
+cudaError_t launch_linear_product(const LinearOperand& P, const LinearOperand& Q, LinearEpilogue ep, tda_dtype out,
+                                  unsigned int* err, cudaStream_t s);
+
+}  // namespace tda

@@ -80,3 +80,53 @@ def test_tensor_list_refusals():
             tda.tensor_list(ts, outs)
     refs = tda.tensor_list([a, a.bfloat16()], [None, None])
     assert refs[0].n == 24 and refs[0].out is None and refs[1].dtype == tda.TDA_BF16
+
+
+def layer(d_in=64, d_out=32, act=0, dtype=tda.TDA_BF16):
+    return tda.LinearDesc(d_in, d_out, act, dtype)
+
+
+def test_linear_descriptor_and_workspace():
+    assert ctypes.sizeof(tda.LinearDesc) == 24
+    F, B, ANY = tda.TDA_LINEAR_FORWARD, tda.TDA_LINEAR_BACKWARD, tda.TDA_LINEAR_ANY_STRIDE
+    size = tda.tda_linear_workspace_size
+    assert size(F, layer(), 10) == 0 and size(F, layer(), 0) == 0
+    assert size(F | ANY, layer(), 10) >= 2 * 64 * (10 + 32)
+    assert size(F, layer(d_in=65), 10) >= 2 * 72 * (10 + 32)  # rows of 65 values need aligned copies
+    assert size(F, layer(dtype=tda.TDA_F32), 10) >= 6 * 64 * (10 + 32)
+    assert size(B, layer(), 10) >= 4 * 32
+    for bad in (lambda: size(7, layer(), 1), lambda: size(F, layer(d_in=0), 1), lambda: size(F, layer(), -1),
+                lambda: size(F, layer(act=5), 1), lambda: size(F, layer(dtype=tda.TDA_F64), 1)):
+        with pytest.raises(tda.TdaError):
+            bad()
+
+
+def test_linear_forward_refusals():
+    def fwd(L=None, X=256, ld_x=64, M=4, W=256, ld_w=64, bias=None, R=None, ld_r=32, Y=256, ld_y=32, Z=None, ld_z=32,
+            ws=None, wsb=0):
+        return err(tda.tda_linear_forward, L or layer(), X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, wsb)
+
+    for k in (dict(L=layer(d_out=0)), dict(L=layer(act=-1)), dict(L=layer(dtype=2)), dict(M=-1), dict(M=1 << 31),
+              dict(X=None), dict(X=257), dict(ld_x=63), dict(W=None), dict(ld_w=63), dict(bias=257), dict(R=257),
+              dict(R=256, ld_r=31), dict(Y=None), dict(Y=255), dict(ld_y=31), dict(Z=255), dict(Z=256, ld_z=31),
+              dict(ld_x=1 << 40)):
+        assert fwd(**k) == BAD, k
+    f32 = layer(dtype=tda.TDA_F32)
+    need = tda.tda_linear_workspace_size(tda.TDA_LINEAR_FORWARD, f32, 4)
+    assert fwd(L=f32, ws=256, wsb=need - 1) == WORKSPACE and fwd(L=f32) == WORKSPACE
+    assert fwd(L=f32, ws=264, wsb=need) == BAD
+    assert fwd(ld_x=65) == WORKSPACE  # rows off 16 bytes need a copy
+
+
+def test_linear_backward_refusals():
+    def bwd(L=None, dY=256, ld_dy=32, Z=256, ld_z=32, M=4, X=256, ld_x=64, W=256, ld_w=64, B=256, ld_b=32, dX=256,
+            ld_dx=64, dW=256, ld_dw=64, db=256, gt=tda.TDA_F32, beta=0.0, ws=256, wsb=1 << 20):
+        return err(tda.tda_linear_backward, L or layer(act=tda.TDA_ACT_SILU), dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B,
+                   ld_b, dX, ld_dx, dW, ld_dw, db, gt, beta, ws, wsb)
+
+    for k in (dict(dY=None), dict(dY=257), dict(ld_dy=31), dict(Z=None), dict(ld_z=31), dict(B=None), dict(B=257),
+              dict(ld_b=31), dict(X=None), dict(W=None), dict(ld_w=63), dict(dX=257), dict(ld_dx=63), dict(dW=258),
+              dict(ld_dw=63), dict(db=257), dict(gt=tda.TDA_F64), dict(beta=float("inf")), dict(M=-1), dict(ws=264)):
+        assert bwd(**k) == BAD, k
+    assert bwd(L=layer(act=1, dtype=tda.TDA_F32), gt=tda.TDA_BF16) == UNSUPPORTED
+    assert bwd(wsb=100) == WORKSPACE and bwd(ws=None) == WORKSPACE
