@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kFacThreads) factor_kernel(const __grid_consta
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     float v = to_f(g[u].v[i]);
-                    if (ACT != TDA_ACT_NONE) v *= act_slope<ACT>(to_f(z[u].v[i]));
+                    if (ACT != TDA_ACT_NONE) v *= act_slope<ACT, sizeof(T) == 2>(to_f(z[u].v[i]));
                     sum[i] += v;
                     set_f(&b.v[i], v);
                 }
@@ -265,10 +265,21 @@ struct Planner {
     }
 };
 
+// How far the epilogue's tensors are aligned.
+void align_epilogue(LinearEpilogue* e, tda_dtype out) {
+    const size_t el = out == TDA_BF16 ? 2 : 4;
+    auto all = [&](size_t bytes) {
+        return rows_by(e->Y, e->ld_y, bytes, el) && rows_by(e->Z, e->ld_z, bytes, el) &&
+               rows_by(e->R, e->ld_r, bytes < 16 ? bytes : 16, el) && rows_by(e->bias, 0, bytes < 16 ? bytes : 16, el);
+    };
+    e->vec = all(4 * el);
+    e->wide = all(32) ? 32 : all(16) ? 16 : 0;
+}
+
 LinearEpilogue plain_epilogue(int64_t M, int64_t N, void* Y, int64_t ld_y, tda_dtype out) {
     LinearEpilogue e = {};
     e.M = M, e.N = N, e.Y = Y, e.ld_y = ld_y, e.act = TDA_ACT_NONE;
-    e.vec = rows_by(Y, ld_y, out == TDA_BF16 ? 8 : 16, out == TDA_BF16 ? 2 : 4);
+    align_epilogue(&e, out);
     return e;
 }
 
@@ -315,14 +326,14 @@ cudaError_t launch_linear_forward(const LinearForward& f, void* ws, unsigned int
     const LinearOperand X = pl.add(f.X, f.M, f.d_in, f.ld_x), W = pl.add(f.W, f.d_out, f.d_in, f.ld_w);
     cudaError_t e = pl.run(s);
     if (e != cudaSuccess) return e;
-    const size_t el = f.dt == TDA_BF16 ? 2 : 4, four = 4 * el;
     LinearEpilogue ep = plain_epilogue(f.M, f.d_out, f.Y, f.ld_y, f.dt);
     ep.bias = f.bias;
     ep.R = f.R, ep.ld_r = f.ld_r, ep.r_scale = 1.f;
     ep.Z = f.Z, ep.ld_z = f.ld_z;
     ep.act = f.act;
-    ep.vec = ep.vec && rows_by(f.bias, 0, four, el) && rows_by(f.R, f.ld_r, four, el) && rows_by(f.Z, f.ld_z, four, el);
-    return launch_linear_product(X, W, ep, f.dt, err, s);
+    align_epilogue(&ep, f.dt);
+    const LinearProduct pr = {X, W, ep, f.dt};
+    return launch_linear_products(&pr, 1, err, s);
 }
 
 cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned int* err, cudaStream_t s) {
@@ -359,20 +370,21 @@ cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned i
     if (b.dX) W = pl.add(b.W, b.d_out, b.d_in, b.ld_w);
     if (b.dW) X = pl.add(b.X, b.M, b.d_in, b.ld_x);
     if ((e = pl.run(s)) != cudaSuccess) return e;
+    LinearProduct pr[2];
+    int count = 0;
     if (b.dX) {
         W.mn = true;  // the contraction runs over W's rows
-        if ((e = launch_linear_product(G, W, plain_epilogue(b.M, b.d_in, b.dX, b.ld_dx, b.dt), b.dt, err, s)) !=
-            cudaSuccess)
-            return e;
+        pr[count++] = {G, W, plain_epilogue(b.M, b.d_in, b.dX, b.ld_dx, b.dt), b.dt};
     }
     if (b.dW) {
         LinearOperand Gt = G;
         Gt.mn = X.mn = true;  // over the tokens
         LinearEpilogue ep = plain_epilogue(b.d_out, b.d_in, b.dW, b.ld_dw, b.gt);
         if (b.beta != 0.f) ep.R = b.dW, ep.ld_r = b.ld_dw, ep.r_scale = b.beta;
-        if ((e = launch_linear_product(Gt, X, ep, b.gt, err, s)) != cudaSuccess) return e;
+        align_epilogue(&ep, b.gt);
+        pr[count++] = {Gt, X, ep, b.gt};
     }
-    return cudaSuccess;
+    return launch_linear_products(pr, count, err, s);
 }
 
 // beta x for an empty batch.

@@ -11,6 +11,11 @@
 // fp32 accumulators with truncation, so for these a run of kWindow chunks is
 // drained and added up in registers with rounding.
 //
+// linear_pair_kernel, for products with a tile for most SM pairs: two CTAs of a
+// cluster hold one 256 x BN tile (cta_group::2), each staging 128 rows of P and half
+// of Q, so an operand byte that reaches an SM feeds twice the MMAs; persistent, the
+// epilogue of a tile beside the next tile's MMAs.
+//
 // linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a decoded token, a
 // short batch) swap the operands, so the long side fills the 128 rows of a tile,
 // and split the K loop over the CTAs of a cluster, whose fp32 tiles are added in
@@ -22,6 +27,7 @@
 #include <cuda.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "linear.cuh"
 
@@ -59,6 +65,22 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, bool mn) {
 // 16 values of k further: 32 bytes along a K-major row, two 8-row groups of an MN-major box.
 __device__ __forceinline__ uint64_t desc_step(bool mn) { return mn ? 2048 >> 4 : 32 >> 4; }
 
+// 32 lanes x 32 consecutive fp32 columns of TMEM into registers.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
 template <typename T>
 __device__ __forceinline__ float ld1(const T* p);
 template <>
@@ -89,60 +111,149 @@ __device__ __forceinline__ void st4(__nv_bfloat16* p, const float* v) {
         make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-template <int ACT>
-__device__ __forceinline__ void act4(float* v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = act_value<ACT>(v[i]);
-}
-
-// Four sums of output row m, columns n .. n + 3, through the epilogue and out.
-template <typename T>
-__device__ __forceinline__ void finish4(const LinearEpilogue& e, int64_t m, int64_t n, float* v) {
-    const bool vec = e.vec && n + 4 <= e.N;
-    const T* bias = (const T*)e.bias + n;
-    const T* R = (const T*)e.R + m * e.ld_r + n;
-    T* Y = (T*)e.Y + m * e.ld_y + n;
-    T* Z = (T*)e.Z + m * e.ld_z + n;
-    const int have = vec ? 4 : (int)(e.N - n < 4 ? e.N - n : 4);
-    float r[4];
-    if (e.R) {
-        if (vec)
-            ld4(R, r);
-        else
-            for (int i = 0; i < have; ++i) r[i] = ld1(R + i);
-    }
-    if (e.bias) {
-        float b[4];
-        if (vec) {
-            ld4(bias, b);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += b[i];
-        } else {
-            for (int i = 0; i < have; ++i) v[i] += ld1(bias + i);
-        }
-    }
-    if (e.Z) {
-        if (vec)
-            st4(Z, v);
-        else
-            for (int i = 0; i < have; ++i) st1(Z + i, v[i]);
-    }
-    switch (e.act) {
-        case TDA_ACT_RELU: act4<TDA_ACT_RELU>(v); break;
-        case TDA_ACT_GELU: act4<TDA_ACT_GELU>(v); break;
-        case TDA_ACT_GELU_TANH: act4<TDA_ACT_GELU_TANH>(v); break;
-        case TDA_ACT_SILU: act4<TDA_ACT_SILU>(v); break;
+// act of U x 4 values, the choice made once for all.
+template <typename T, int U>
+__device__ __forceinline__ void activate(int act, float (*v)[4]) {
+    constexpr bool FAST = sizeof(T) == 2;
+#define TDA_ACT_CASE(A)                                                          \
+    case A:                                                                      \
+        _Pragma("unroll") for (int u = 0; u < U; ++u)                            \
+            _Pragma("unroll") for (int i = 0; i < 4; ++i) v[u][i] = act_value<A, FAST>(v[u][i]); \
+        break
+    switch (act) {
+        TDA_ACT_CASE(TDA_ACT_RELU);
+        TDA_ACT_CASE(TDA_ACT_GELU);
+        TDA_ACT_CASE(TDA_ACT_GELU_TANH);
+        TDA_ACT_CASE(TDA_ACT_SILU);
         default: break;
     }
-    if (e.R) {
+#undef TDA_ACT_CASE
+}
+
+// Four sums of output row m, columns n .. n + 3, a value at a time: edges and unaligned outputs.
+template <typename T>
+__device__ __noinline__ void finish_edge(const LinearEpilogue& e, int64_t m, int64_t n, float x0, float x1, float x2,
+                                         float x3) {
+    float v[1][4] = {{x0, x1, x2, x3}};
+    const int have = (int)(e.N - n < 4 ? e.N - n : 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < have) v[i] = fmaf(e.r_scale, r[i], v[i]);
+    for (int i = 0; i < 4; ++i) {
+        if (e.bias && i < have) v[0][i] += ld1((const T*)e.bias + n + i);
+        if (e.Z && i < have) st1((T*)e.Z + m * e.ld_z + n + i, v[0][i]);
     }
-    if (vec)
-        st4(Y, v);
-    else
-        for (int i = 0; i < have; ++i) st1(Y + i, v[i]);
+    activate<T, 1>(e.act, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= have) break;
+        if (e.R) v[0][i] = fmaf(e.r_scale, ld1((const T*)e.R + m * e.ld_r + n + i), v[0][i]);
+        st1((T*)e.Y + m * e.ld_y + n + i, v[0][i]);
+    }
+}
+
+// U groups of four sums through the epilogue and out: group u is output row m[u], columns n[u] .. + 3
+// (SAME_N: one column group for all), inside the output where ok[u]. All loads come before the first store.
+template <typename T, int U, bool SAME_N>
+__device__ __forceinline__ void finish(const LinearEpilogue& e, const int64_t* m, const int64_t* n, const bool* ok,
+                                       float (*v)[4]) {
+    bool whole[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        whole[u] = ok[u] && e.vec && n[u] + 4 <= e.N;
+        if (ok[u] && !whole[u]) finish_edge<T>(e, m[u], n[u], v[u][0], v[u][1], v[u][2], v[u][3]);
+    }
+    float r[U][4], b[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (e.R && whole[u]) ld4((const T*)e.R + m[u] * e.ld_r + n[u], r[u]);
+        if (e.bias && (SAME_N ? u == 0 && n[0] + 4 <= e.N && e.vec : whole[u])) ld4((const T*)e.bias + n[u], b[u]);
+    }
+    if (e.bias)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[u][i] += b[SAME_N ? 0 : u][i];
+    if (e.Z)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (whole[u]) st4((T*)e.Z + m[u] * e.ld_z + n[u], v[u]);
+    activate<T, U>(e.act, v);
+    if (e.R)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[u][i] = fmaf(e.r_scale, r[u][i], v[u][i]);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (whole[u]) st4((T*)e.Y + m[u] * e.ld_y + n[u], v[u]);
+}
+
+// 32 values of one row of a tensor, as they are in memory.
+template <typename T>
+struct Row32 {
+    using Type = T;
+    static constexpr int kVecs = sizeof(T) * 32 / 16;
+    uint4 q[kVecs];
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) q[i] = *reinterpret_cast<const uint4*>(p + i * (16 / sizeof(T)));
+    }
+    __device__ __forceinline__ float get(int i) const {  // i known at compile time
+        const uint4& x = q[i * sizeof(T) / 16];
+        const int w = sizeof(T) == 4 ? i & 3 : (i >> 1) & 3;
+        const uint32_t b = w == 0 ? x.x : w == 1 ? x.y : w == 2 ? x.z : x.w;
+        return __uint_as_float(sizeof(T) == 4 ? b : i & 1 ? b & 0xFFFF0000u : b << 16);
+    }
+};
+__device__ __forceinline__ void st_32b(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+// One sector of a row (16 bf16 or 8 fp32 values from v on): a whole 32-byte store, or two of 16 bytes where rows
+// start between sectors.
+template <typename T>
+__device__ __forceinline__ void store_sector(T* p, const float* v, bool sectors) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            w[j] = __float_as_uint(v[j]);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+    if (sectors) {
+        st_32b(p, w);
+    } else {
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(p + 16 / sizeof(T)) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
+// A row of 32 sums through the epilogue and out, a sector at a time. PLAIN: no bias, Z or activation.
+template <typename T, bool PLAIN>
+__device__ __forceinline__ void finish_row32(const LinearEpilogue& e, int64_t m, int64_t n, float* v,
+                                             const Row32<T>& r) {
+    constexpr int kPer = 32 / sizeof(T);
+    if (!PLAIN && e.bias) {
+        Row32<T> b;  // the same addresses in every lane
+        b.load((const T*)e.bias + n);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += b.get(i);
+    }
+#pragma unroll
+    for (int i = 0; i < 32; i += kPer) {
+        if (!PLAIN) {
+            if (e.Z && m < e.M) store_sector((T*)e.Z + m * e.ld_z + n + i, v + i, e.wide == 32);
+#pragma unroll
+            for (int j = 0; j < kPer; j += 8) activate<T, 2>(e.act, reinterpret_cast<float(*)[4]>(v + i + j));
+        }
+        if (e.R)
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[i + j] = fmaf(e.r_scale, r.get(i + j), v[i + j]);
+        if (m < e.M) store_sector((T*)e.Y + m * e.ld_y + n + i, v + i, e.wide == 32);
+    }
 }
 
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
@@ -360,17 +471,25 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
         const int groups = kTM * BN / 4, g0 = groups * rank / p.split, g1 = groups * (rank + 1) / p.split;
         const int64_t m0 = p.swap ? j0 : i0, n0 = p.swap ? i0 : j0;
         const uint32_t base = smem_u32(smem);
-        for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
-            const int o = g * 4 / inner, c = g * 4 % inner;
-            const int64_t m = m0 + o, n = n0 + c;
-            if (m >= p.ep.M || n >= p.ep.N) continue;
-            const uint32_t at = base + (uint32_t)(o * stride + c) * 4;
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int r = 0; r < p.split; ++r) {
-                const float4 x = ld_cluster_f4(map_rank(at, r));
-                v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        constexpr int U = ROUND ? 4 : 2;
+        for (int g = g0 + threadIdx.x; g < g1; g += U * kThreads) {
+            int64_t m[U], n[U];
+            bool ok[U];
+            float v[U][4];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int gu = g + u * kThreads, o = gu * 4 / inner, c = gu * 4 % inner;
+                m[u] = m0 + o, n[u] = n0 + c;
+                ok[u] = gu < g1 && m[u] < p.ep.M && n[u] < p.ep.N;
+                v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0.f;
+                if (!ok[u]) continue;
+                const uint32_t at = base + (uint32_t)(o * stride + c) * 4;
+                for (int r = 0; r < p.split; ++r) {
+                    const float4 x = ld_cluster_f4(map_rank(at, r));
+                    v[u][0] += x.x, v[u][1] += x.y, v[u][2] += x.z, v[u][3] += x.w;
+                }
             }
-            finish4<T>(p.ep, m, n, v);
+            finish<T, U, false>(p.ep, m, n, ok, v);
         }
     }
     __syncwarp();
@@ -381,6 +500,350 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, S::kCols);
+    }
+}
+
+// ------------------------------------------------------------------ one tile per CTA pair, persistent
+__device__ __forceinline__ void pair_alloc(uint32_t dst, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void pair_relinquish() {
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void pair_dealloc(uint32_t taddr, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Arrives on the barrier at this offset in both CTAs once the MMAs so far are done.
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+}
+// A box into this CTA's shared memory whose bytes count on a barrier of either CTA of the pair.
+__device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* tm, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+        "%4}], [%5];" ::"r"(dst),
+        "l"((uint64_t)tm), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+
+template <int BN>
+struct PairShape {
+    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN / 2 * kTK * 2, kStage = kP + kQ;
+    static constexpr int kStages = BN == 256 ? 6 : 7;
+    static constexpr uint32_t kBlockLd = 20;  // floats of a staged row: 16 + 4, conflict-free 16-byte accesses
+    static constexpr uint32_t kBlock = 32 * kBlockLd * 4;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kEpiWarps * kBlock + 8 * (2 * kStages + 5) + 16;
+    static constexpr uint32_t kCols = 512;  // the SM's whole TMEM: both CTAs' columns start at the same place
+    static_assert(kSmem <= 232448, "shared memory per CTA");
+};
+
+// One or two products (dX and dW of a layer) in one launch: their tiles form one list, those with the longer
+// K loop first, so that the short ones fill the last round.
+struct PairParams {
+    TileParams g[2];
+    CUtensorMap tmP[2], tmQ[2];
+    int64_t tiles[2];  // tiles[1] = 0: one product
+    unsigned int* err;
+};
+
+template <int BN, bool ROUND>
+__global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ PairParams pp) {
+    using S = PairShape<BN>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* blocks = smem + (size_t)S::kStages * S::kStage;
+    uint64_t* bars = (uint64_t*)(blocks + kEpiWarps * S::kBlock);
+    uint64_t* full = bars;                    // leader's: both CTAs' bytes landed
+    uint64_t* empty = bars + S::kStages;      // each CTA's own: MMAs done with the stage
+    uint64_t* tfull = bars + 2 * S::kStages;  // [2] each CTA's own: accumulator ready
+    uint64_t* tempty = tfull + 2;             // [2] leader's: accumulator drained by both CTAs' warps
+    uint64_t* mma_done = tempty + 2;
+    uint32_t* tmem_slot = (uint32_t*)(mma_done + 1);
+    volatile int* abort = (volatile int*)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&tfull[b]), 1);
+            mbar_init(smem_u32(&tempty[b]), 2 * kEpiWarps);
+        }
+        mbar_init(smem_u32(mma_done), 1);
+        *abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        pair_alloc(smem_u32(tmem_slot), S::kCols);
+        pair_relinquish();
+    }
+    tc_fence_before();
+    cluster_sync();  // both CTAs' barriers exist before either signals the other's
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    const int64_t units = pp.tiles[0] + pp.tiles[1], u0 = blockIdx.x >> 1, du = gridDim.x >> 1;
+    // A product's tiles go in bands of 8 tile rows, down each column of a band: the
+    // pairs at work share operand rows in L2.
+    // Each role runs its loop once per product, with that product's parameters at fixed places of the constant
+    // bank: reading them through an index made the loops a fifth slower.
+    auto place = [](const TileParams& p, int64_t u, int64_t* i0, int64_t* j0) {
+        const int64_t band = u / (8 * p.tiles_q), in = u % (8 * p.tiles_q);
+        const int64_t h = p.tiles_p - band * 8 < 8 ? p.tiles_p - band * 8 : 8;
+        *i0 = (band * 8 + in % h) * (2 * kTM);
+        *j0 = (in / h) * BN;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---------------- TMA producer of this CTA's halves
+            uint32_t ring = 0, last_par[S::kStages];
+            bool issued[S::kStages], ok = true;
+            for (int s = 0; s < S::kStages; ++s) issued[s] = false;
+            int64_t u = u0;
+            auto feed = [&](auto G) {
+              constexpr int g = decltype(G)::value;
+              const TileParams& p = pp.g[g];
+              const CUtensorMap *tmP = &pp.tmP[g], *tmQ = &pp.tmQ[g];
+              const int total = p.nk * p.pairs;
+              const int64_t end = g ? units : pp.tiles[0], base = g ? pp.tiles[0] : 0;
+              for (; ok && u < end; u += du) {
+                int64_t i0, j0;
+                place(p, u - base, &i0, &j0);
+                const int pr = (int)i0 + (int)rank * kTM, qr = (int)j0 + (int)rank * (BN / 2);
+                int pair = 0, kc = 0;
+                for (int t = 0; t < total; ++t, ++ring) {
+                    const int s = ring % S::kStages;
+                    const uint32_t ph = (ring / S::kStages) & 1u;
+                    if (!wait_bounded(smem_u32(&empty[s]), ph ^ 1u, abort, pp.err)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t st = smem_u32(smem + (size_t)s * S::kStage), bar = smem_u32(&full[s]);
+                    const uint32_t lead = map_rank(bar, 0);
+                    const int vp = pair_p(p.pairs, pair), vq = pair_q(p.pairs, pair), k0 = kc * kTK;
+                    if (rank == 0) mbar_arrive_tx(bar, 2 * S::kStage);
+                    if (p.p_mn) {
+                        for (int j = 0; j < kTM / 64; ++j) pair_load_3d(st + j * kBox, tmP, pr + 64 * j, k0, vp, lead);
+                    } else {
+                        pair_load_3d(st, tmP, k0, pr, vp, lead);
+                    }
+                    if (p.q_mn) {
+                        for (int j = 0; j < BN / 128; ++j)
+                            pair_load_3d(st + S::kP + j * kBox, tmQ, qr + 64 * j, k0, vq, lead);
+                    } else {
+                        pair_load_3d(st + S::kP, tmQ, k0, qr, vq, lead);
+                    }
+                    issued[s] = true;
+                    last_par[s] = ph;
+                    if (++kc == p.nk) kc = 0, ++pair;
+                }
+              }
+            };
+            feed(std::integral_constant<int, 0>());
+            feed(std::integral_constant<int, 1>());
+            // copies still in flight when the MMA side stopped early land before the pair exits
+            if (rank == 0)
+                for (int s = 0; s < S::kStages; ++s)
+                    if (issued[s]) {
+                        const uint64_t since = global_ns();
+                        while (!mbar_try_wait(smem_u32(&full[s]), last_par[s]))
+                            if (global_ns() - since > kTimeoutNs) {
+                                atomicOr(pp.err, kErrTimeout);
+                                break;
+                            }
+                    }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            // ---------------- MMA issuer of the pair
+            uint32_t ring = 0, use = 0;
+            bool ok = true;
+            int64_t u = u0;
+            auto issue = [&](auto G) {
+              constexpr int g = decltype(G)::value;
+              const TileParams& p = pp.g[g];
+              const bool p_mn = p.p_mn, q_mn = p.q_mn;
+              const uint32_t idesc = idesc_bf16(2 * kTM, BN) | (p_mn ? 1u << 15 : 0u) | (q_mn ? 1u << 16 : 0u);
+              const uint64_t sp = desc_step(p_mn), sq = desc_step(q_mn);
+              const int total = p.nk * p.pairs, window = p.window, windows = (total + window - 1) / window;
+              const int64_t last = g ? units : pp.tiles[0];
+              for (; ok && u < last; u += du) {
+                int t = 0;
+                for (int w = 0; ok && w < windows; ++w, ++use) {
+                    const uint32_t b = use & 1u;
+                    if (!wait_bounded_cluster(smem_u32(&tempty[b]), ((use >> 1) & 1u) ^ 1u, abort, pp.err)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const int end = t + window < total ? t + window : total;
+                    for (bool first = true; t < end; ++t, ++ring) {
+                        const int s = ring % S::kStages;
+                        const uint32_t ph = (ring / S::kStages) & 1u;
+                        if (!wait_bounded(smem_u32(&full[s]), ph, abort, pp.err)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t st = smem_u32(smem + (size_t)s * S::kStage);
+                        const uint64_t dp = desc_of(st, p_mn), dq = desc_of(st + S::kP, q_mn);
+#pragma unroll
+                        for (int k = 0; k < kTK / 16; ++k) {
+                            pair_mma(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
+                            first = false;
+                        }
+                        pair_commit(smem_u32(&empty[s]));
+                    }
+                    if (ok) pair_commit(smem_u32(&tfull[b]));
+                }
+              }
+            };
+            issue(std::integral_constant<int, 0>());
+            issue(std::integral_constant<int, 1>());
+            pair_commit(smem_u32(mma_done));
+            const uint64_t since = global_ns();
+            while (!mbar_try_wait(smem_u32(mma_done), 0))
+                if (global_ns() - since > kTimeoutNs) {
+                    atomicOr(pp.err, kErrTimeout);
+                    break;
+                }
+        }
+    } else {
+        // ---------------- epilogue of this CTA's 128 rows: 32 x 32 blocks through shared memory
+        const int half = (warp - 2) >> 2, q = warp & 3;
+        constexpr int kC = BN / 2;  // columns of this warp
+        float* blk = reinterpret_cast<float*>(blocks + (warp - 2) * S::kBlock);
+        const uint32_t tb = tmem + ((uint32_t)(q * 32) << 16) + half * kC;
+        uint32_t use = 0;
+        auto wait_for = [&]() {
+            bool got = true;
+            if (lane == 0) got = wait_bounded(smem_u32(&tfull[use & 1u]), (use >> 1) & 1u, abort, pp.err);
+            got = __shfl_sync(0xffffffffu, got, 0);
+            tc_fence_after();
+            return got;
+        };
+        auto release = [&]() {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(smem_u32(&tempty[use & 1u]), 0);
+            ++use;
+        };
+        // 16 columns of this warp's 32 rows, held a row a lane, through shared memory: edges and rows that are not
+        // aligned go out a few values at a time, neighbours by neighbouring lanes
+        auto out = [&](const LinearEpilogue& ep, const float* v, int64_t m0, int64_t n0) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(blk + lane * S::kBlockLd + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            __syncwarp();
+#pragma unroll 1
+            for (int r = lane >> 2; r < 32; r += 8) {
+                int64_t m[1] = {m0 + r}, n[1] = {n0 + (lane & 3) * 4};
+                const bool ok[1] = {m[0] < ep.M && n[0] < ep.N};
+                const float4 x = *reinterpret_cast<const float4*>(blk + r * S::kBlockLd + (lane & 3) * 4);
+                float y[1][4] = {{x.x, x.y, x.z, x.w}};
+                if (ROUND || ep.f32)
+                    finish<float, 1, true>(ep, m, n, ok, y);
+                else
+                    finish<__nv_bfloat16, 1, true>(ep, m, n, ok, y);
+            }
+        };
+        // 32 columns, a row a lane, straight from registers; r: the residual's row, loaded ahead
+        auto load_r = [&](auto& r, const LinearEpilogue& ep, int64_t m, int64_t n) {
+            using T = typename std::remove_reference<decltype(r)>::type::Type;
+            if (ep.R && m < ep.M && n + 32 <= ep.N) r.load((const T*)ep.R + m * ep.ld_r + n);
+        };
+        bool got = true;
+        int64_t u = u0;
+        auto drain = [&](auto G) {
+          constexpr int g = decltype(G)::value;
+          const TileParams& p = pp.g[g];
+          const int64_t end = g ? units : pp.tiles[0], base = g ? pp.tiles[0] : 0;
+          for (; got && u < end; u += du) {
+            int64_t i0, j0;
+            place(p, u - base, &i0, &j0);
+            const int64_t m0 = i0 + rank * kTM + q * 32, n0 = j0 + half * kC;
+            // 32 columns from n0 + c on, read by `get` into v[8][4]
+            auto column_blocks = [&](auto zero, auto get) {
+                using T = decltype(zero);
+                const int64_t m = m0 + lane;
+                Row32<T> r;
+                if (p.ep.wide) load_r(r, p.ep, m, n0);
+                if (!ROUND && !(got = wait_for())) return;
+                // fp32 outputs of bf16 products are gradients: nothing but beta times themselves is added
+                constexpr bool kPlain = g == 1 || (!ROUND && sizeof(T) == 4);
+                auto block = [&](int c) {
+                    const int64_t n = n0 + c;
+                    float v[32];
+                    get(c, v);
+                    if (p.ep.wide && n + 32 <= p.ep.N) {
+                        finish_row32<T, kPlain>(p.ep, m, n, v, r);
+                        if (c + 32 < kC) load_r(r, p.ep, m, n + 32);
+                    } else {
+                        out(p.ep, v, m0, n);
+                        out(p.ep, v + 16, m0, n + 16);
+                    }
+                };
+                if (ROUND) {
+#pragma unroll
+                    for (int c = 0; c < kC; c += 32) block(c);  // the sums are registers
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < kC; c += 32) block(c);
+                    release();
+                }
+            };
+            if (!ROUND) {
+                auto get = [&](int c, float* v) { tmem_ld32(tb + (use & 1u) * BN + c, v); };
+                if (p.ep.f32)
+                    column_blocks(float(), get);
+                else
+                    column_blocks(__nv_bfloat16(), get);
+            } else {
+                float acc[kC];
+#pragma unroll
+                for (int i = 0; i < kC; ++i) acc[i] = 0.f;
+                const int windows = (p.nk * p.pairs + p.window - 1) / p.window;
+                for (int w = 0; w < windows; ++w) {
+                    if (!(got = wait_for())) break;
+#pragma unroll
+                    for (int c = 0; c < kC; c += 16) {
+                        float v[16];
+                        tmem_ld16(tb + (use & 1u) * BN + c, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[c + i] += v[i];
+                    }
+                    release();
+                }
+                if (!got) break;
+                column_blocks(float(), [&](int c, float* v) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = acc[c + i];
+                });
+            }
+          }
+        };
+        drain(std::integral_constant<int, 0>());
+        drain(std::integral_constant<int, 1>());
+    }
+    __syncwarp();
+    tc_fence_before();
+    cluster_sync();  // neither CTA leaves while the pair's MMAs, copies or signals may touch it
+    if (warp == 1) {
+        tc_fence_after();
+        pair_dealloc(tmem, S::kCols);
     }
 }
 
@@ -460,6 +923,51 @@ cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams&
     return cudaLaunchKernelEx(&cfg, linear_tile_kernel<T, BN, ROUND>, mP, mQ, p);
 }
 
+struct Product {
+    LinearOperand P, Q;
+    TileParams p;
+    tda_dtype out;
+};
+
+template <int BN, bool ROUND>
+cudaError_t run_pair(const Product* const* pr, int count, cudaStream_t s) {
+    using S = PairShape<BN>;
+    PairParams pp;
+    pp.tiles[0] = pp.tiles[1] = 0;
+    for (int i = 0; i < count; ++i) {
+        const Product& x = *pr[i];
+        if (!make_map(&pp.tmP[i], x.P, x.P.mn ? kTK : kTM) || !make_map(&pp.tmQ[i], x.Q, x.Q.mn ? kTK : BN / 2))
+            return cudaErrorInvalidValue;
+        pp.g[i] = x.p;
+        pp.g[i].tiles_p = (x.P.extent() + 2 * kTM - 1) / (2 * kTM);
+        pp.g[i].tiles_q = (x.Q.extent() + BN - 1) / BN;
+        pp.tiles[i] = pp.g[i].tiles_p * pp.g[i].tiles_q;
+    }
+    if (count == 1) {
+        pp.g[1] = pp.g[0];
+        pp.tmP[1] = pp.tmP[0], pp.tmQ[1] = pp.tmQ[0];
+    }
+    pp.err = pr[0]->p.err;
+    cudaError_t e = smem_attr_once<linear_pair_kernel<BN, ROUND>>((int)S::kSmem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(2);
+    const int64_t most = max_clusters_once<linear_pair_kernel<BN, ROUND>>(cfg, 2, sm_count() / 2);
+    const int64_t tiles = pp.tiles[0] + pp.tiles[1];
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < most ? tiles : most)));
+    note_launches(1);
+    return cudaLaunchKernelEx(&cfg, linear_pair_kernel<BN, ROUND>, pp);
+}
+
 template <typename T, bool ROUND>
 cudaError_t pick_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, cudaStream_t s) {
     const int64_t q = Q.extent();
@@ -482,22 +990,59 @@ bool linear_tc_available() {
     return sm103 && encode_fn();
 }
 
-cudaError_t launch_linear_product(const LinearOperand& P0, const LinearOperand& Q0, LinearEpilogue ep, tda_dtype out,
-                                  unsigned int* err, cudaStream_t s) {
-    TileParams p;
+static Product make_product(const LinearProduct& x, unsigned int* err) {
+    Product r;
     // a short side takes the narrow dimension of the tile
-    p.swap = P0.extent() <= 64 && Q0.extent() > P0.extent();
-    const LinearOperand &P = p.swap ? Q0 : P0, &Q = p.swap ? P0 : Q0;
-    p.ep = ep;
-    p.nk = (int)((P.depth() + kTK - 1) / kTK);
-    p.pairs = P.planes == 3 ? 6 : 1;
-    p.window = P.planes == 3 ? kWindow : p.nk;
-    p.p_mn = P.mn;
-    p.q_mn = Q.mn;
-    p.err = err;
-    const bool round = p.pairs > 1;
-    if (out == TDA_BF16) return round ? cudaErrorInvalidValue : pick_tile<__nv_bfloat16, false>(P, Q, p, s);
-    return round ? pick_tile<float, true>(P, Q, p, s) : pick_tile<float, false>(P, Q, p, s);
+    r.p.swap = x.P.extent() <= 64 && x.Q.extent() > x.P.extent();
+    r.P = r.p.swap ? x.Q : x.P;
+    r.Q = r.p.swap ? x.P : x.Q;
+    r.out = x.out;
+    r.p.ep = x.ep;
+    r.p.ep.f32 = x.out == TDA_F32;
+    r.p.nk = (int)((r.P.depth() + kTK - 1) / kTK);
+    r.p.pairs = r.P.planes == 3 ? 6 : 1;
+    r.p.window = r.P.planes == 3 ? kWindow : r.p.nk;
+    r.p.split = 1;
+    r.p.p_mn = r.P.mn;
+    r.p.q_mn = r.Q.mn;
+    r.p.err = err;
+    return r;
+}
+
+static int64_t pair_tiles(const Product& x) {
+    const int64_t bn = x.p.pairs > 1 ? 128 : 256;
+    return x.p.swap ? 0 : ((x.P.extent() + 2 * kTM - 1) / (2 * kTM)) * ((x.Q.extent() + bn - 1) / bn);
+}
+
+cudaError_t launch_linear_products(const LinearProduct* x, int count, unsigned int* err, cudaStream_t s) {
+    Product r[2];
+    const Product* order[2];
+    int64_t tiles = 0;
+    for (int i = 0; i < count; ++i) {
+        r[i] = make_product(x[i], err);
+        const int64_t t = pair_tiles(r[i]);
+        tiles = i > 0 && (t == 0 || tiles == 0) ? 0 : tiles + t;
+        order[i] = &r[i];
+    }
+    const bool round = r[0].p.pairs > 1;
+    // a pair's tile for at least half of the SM pairs
+    if (tiles * 4 >= sm_count()) {
+        if (count == 2 && r[1].p.nk > r[0].p.nk) order[0] = &r[1], order[1] = &r[0];
+        return round ? run_pair<128, true>(order, count, s) : run_pair<256, false>(order, count, s);
+    }
+    for (int i = 0; i < count; ++i) {
+        if (count == 2 && pair_tiles(r[i]) * 4 >= sm_count()) {  // the other one has a short side
+            const Product* one = &r[i];
+            cudaError_t e = round ? run_pair<128, true>(&one, 1, s) : run_pair<256, false>(&one, 1, s);
+            if (e != cudaSuccess) return e;
+            continue;
+        }
+        cudaError_t e = r[i].out == TDA_BF16 ? pick_tile<__nv_bfloat16, false>(r[i].P, r[i].Q, r[i].p, s)
+                        : round              ? pick_tile<float, true>(r[i].P, r[i].Q, r[i].p, s)
+                                             : pick_tile<float, false>(r[i].P, r[i].Q, r[i].p, s);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace tda

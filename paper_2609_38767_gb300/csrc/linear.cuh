@@ -10,37 +10,67 @@
 namespace tda {
 
 // ------------------------------------------------------------------ activations
-// Values in forms without cancellation or overflow: gelu through erfc, the tanh form as
+// Values in forms without cancellation or overflow: gelu through the normal tail, the tanh form as
 // z sigmoid(2u) (tanh(u) = 2 sigmoid(2u) - 1). exp of a large argument gives 0 or inf,
 // and 1 / (1 + inf) = 0, so finite z of any size give finite results.
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+// FAST (bf16 results): the exponential and the quotient by the approximate instructions, good to
+// 2^-21 |x| and 2^-22, far below bf16's 2^-8.
+template <bool FAST>
+__device__ __forceinline__ float sigmoid(float x) {
+    return FAST ? __fdividef(1.f, 1.f + __expf(-x)) : 1.f / (1.f + expf(-x));
+}
 
-template <int ACT>
+// q = Phi(-|z|) and e = exp(-z^2/2). FAST: erfc by formula 7.1.26 of Abramowitz and Stegun, Handbook of
+// Mathematical Functions (absolute error 1.5e-7).
+template <bool FAST>
+__device__ __forceinline__ float normal_tail(float z, float* e) {
+    const float a = fabsf(z);
+    if (!FAST) {
+        *e = expf(-0.5f * z * z);
+        return 0.5f * erfcf(0.70710678118654752f * a);
+    }
+    *e = __expf(-0.5f * z * z);
+    const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678118654752f, a, 1.f));
+    float s = fmaf(t, 1.061405429f, -1.453152027f);
+    s = fmaf(t, s, 1.421413741f);
+    s = fmaf(t, s, -0.284496736f);
+    s = fmaf(t, s, 0.254829592f);
+    return 0.5f * t * s * *e;
+}
+
+template <int ACT, bool FAST>
 __device__ __forceinline__ float act_value(float z) {
     if (ACT == TDA_ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
-    if (ACT == TDA_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    if (ACT == TDA_ACT_GELU_TANH) return z * sigmoid(1.5957691216057308f * fmaf(0.044715f * z * z, z, z));
-    if (ACT == TDA_ACT_SILU) return z * sigmoid(z);
+    if (ACT == TDA_ACT_GELU) {
+        float e;
+        const float q = normal_tail<FAST>(z, &e);
+        return z > 0.f ? fmaf(-z, q, z) : z * q;
+    }
+    if (ACT == TDA_ACT_GELU_TANH) return z * sigmoid<FAST>(1.5957691216057308f * fmaf(0.044715f * z * z, z, z));
+    if (ACT == TDA_ACT_SILU) return z * sigmoid<FAST>(z);
     return z;
 }
 
-template <int ACT>
+template <int ACT, bool FAST>
 __device__ __forceinline__ float act_slope(float z) {
     if (ACT == TDA_ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
     if (ACT == TDA_ACT_GELU) {
-        const float phi = 0.39894228040143268f * expf(-0.5f * z * z);
-        return fmaf(z, phi, 0.5f * erfcf(-0.70710678118654752f * z));
+        float e;
+        const float q = normal_tail<FAST>(z, &e);
+        return fmaf(0.39894228040143268f * z, e, z > 0.f ? 1.f - q : q);
     }
     if (ACT == TDA_ACT_GELU_TANH) {
-        // past |z| = 10 the slope is 0 or 1 to fp32, while z^2 or the exponential could overflow;
+        // past |z| = 9.9 the slope is 0 or 1 to fp32, while z^2 or the exponential could overflow;
         // 1 - s = e s without the cancellation
-        const float c = fminf(fmaxf(z, -10.f), 10.f);
-        const float e = expf(-1.5957691216057308f * fmaf(0.044715f * c * c, c, c)), s = 1.f / (1.f + e);
+        const float c = fminf(fmaxf(z, -9.9f), 9.9f);
+        const float x = -1.5957691216057308f * fmaf(0.044715f * c * c, c, c), e = FAST ? __expf(x) : expf(x);
+        const float s = FAST ? __fdividef(1.f, 1.f + e) : 1.f / (1.f + e);
         const float r = fmaf(c * s * (e * s), 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f), s);
         return z != z ? z : r;
     }
     if (ACT == TDA_ACT_SILU) {
-        const float c = fmaxf(z, -88.f), e = expf(-c), s = 1.f / (1.f + e);  // 1 - s = e s; e stays finite
+        const float c = fmaxf(z, -86.f), e = FAST ? __expf(-c) : expf(-c);  // 1 - s = e s; e stays below 2^126
+        const float s = FAST ? __fdividef(1.f, 1.f + e) : 1.f / (1.f + e);
         const float r = s * fmaf(c, e * s, 1.f);
         return z != z ? z : r;
     }
@@ -74,6 +104,8 @@ struct LinearEpilogue {
     int64_t ld_z;
     int act;
     int vec;  // all of bias, R, Y, Z may be moved four values at a time
+    int wide; // all of them by 16 bytes (16), Y and Z also by 32-byte sectors (32); else 0
+    int f32;  // type of bias, R, Y, Z (set by the launch)
 };
 
 // ------------------------------------------------------------------ the two passes (k_linear.cu)
@@ -104,8 +136,12 @@ cudaError_t launch_scale_matrix(tda_dtype dt, void* x, int64_t rows, int64_t col
                                 cudaStream_t s);
 
 bool linear_tc_available();
-// One product with its epilogue; out: type of bias, R, Y, Z.
-cudaError_t launch_linear_product(const LinearOperand& P, const LinearOperand& Q, LinearEpilogue ep, tda_dtype out,
-                                  unsigned int* err, cudaStream_t s);
+// One product, or two that do not read each other's output, each with its epilogue; out: type of bias, R, Y, Z.
+struct LinearProduct {
+    LinearOperand P, Q;
+    LinearEpilogue ep;
+    tda_dtype out;
+};
+cudaError_t launch_linear_products(const LinearProduct* x, int count, unsigned int* err, cudaStream_t s);
 
 }  // namespace tda
