@@ -6,10 +6,10 @@
 // nothing is transposed in memory.
 //
 // fp32 operands arrive as three bf16 planes x = x0 + x1 + x2 (each the rounding of
-// what the ones before leave, exact to 2^-24): the K loop then runs over the six
-// plane pairs whose products matter, smallest first. The tensor pipe adds into its
-// fp32 accumulators with truncation, so for these a run of kWindow chunks is
-// drained and added up in registers with rounding.
+// what the ones before leave, exact to 2^-24). A stage holds all planes of a chunk
+// of k, read once, and feeds the six plane pairs whose products matter, smallest
+// first. The tensor pipe adds into its fp32 accumulators with truncation, so for
+// these every chunk's sum is drained and added up in registers with rounding.
 //
 // linear_pair_kernel, for products with a tile for most SM pairs: two CTAs of a
 // cluster hold one 256 x BN tile (cta_group::2), each staging 128 rows of P and half
@@ -39,22 +39,20 @@ namespace {
 constexpr int kThreads = 320, kEpiWarps = 8;
 constexpr int kTM = 128, kTK = 64;
 constexpr uint32_t kBox = 64 * kTK * 2;  // one 64 x 64 MN-major box: 8 KiB
-constexpr int kWindow = 4;               // chunks accumulated in TMEM before rounding, fp32 operands
 
 struct TileParams {
     LinearEpilogue ep;
     int64_t tiles_p, tiles_q;
-    int nk, pairs;      // K chunks of one plane pair, plane pairs
-    int window;         // chunks per accumulator
+    int nk;             // chunks of kTK along K
     int split;          // CTAs of a cluster along K
     bool p_mn, q_mn;
     bool swap;          // tile rows are output columns
     unsigned int* err;
 };
 
-// Planes of P and Q of the t-th pair of fp32 operands.
-__device__ __forceinline__ int pair_p(int pairs, int t) { return pairs == 1 ? 0 : (0x001102 >> (4 * t)) & 15; }
-__device__ __forceinline__ int pair_q(int pairs, int t) { return pairs == 1 ? 0 : (0x010120 >> (4 * t)) & 15; }
+// Planes of P and Q of the t-th product of fp32 operands.
+__device__ __forceinline__ constexpr int plane_p(int t) { return (0x001102 >> (4 * t)) & 15; }
+__device__ __forceinline__ constexpr int plane_q(int t) { return (0x010120 >> (4 * t)) & 15; }
 
 // Descriptor fields beside the address: K-major tiles have 8-row groups 1 KiB apart; MN-major
 // tiles 64-element atoms one box apart (LBO) and 8-row K groups 1 KiB apart (SBO).
@@ -268,10 +266,11 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
 // ------------------------------------------------------------------ one tile per CTA
 template <int BN, bool ROUND>
 struct TileShape {
-    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN * kTK * 2, kStage = kP + kQ;
+    static constexpr int kPlanes = ROUND ? 3 : 1;
+    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN * kTK * 2, kStage = kPlanes * (kP + kQ);
     // two CTAs share an SM (96 to 100 KiB of stages each); the rounding variant keeps its sums in
     // registers and takes an SM alone
-    static constexpr int kStages = ROUND ? 5 : BN == 128 ? 3 : BN == 64 ? 4 : 5;
+    static constexpr int kStages = ROUND ? (BN == 128 ? 2 : 3) : BN == 128 ? 3 : BN == 64 ? 4 : 5;
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 8 * (2 * kStages + 5) + 16;
     static constexpr uint32_t kCols = 2 * BN;  // two accumulators
     static_assert((BN + 4) * kTM * 4 <= kStages * kStage, "the fp32 tile reuses the stages");
@@ -318,9 +317,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
     const int64_t tile = blockIdx.x / p.split;
     const int rank = blockIdx.x % p.split;
     const int64_t i0 = (tile / p.tiles_q) * kTM, j0 = (tile % p.tiles_q) * BN;
-    const int total = p.nk * p.pairs;
-    const int t0 = (int)((int64_t)total * rank / p.split), t1 = (int)((int64_t)total * (rank + 1) / p.split);
-    const int windows = (t1 - t0 + p.window - 1) / p.window;
+    const int t0 = (int)((int64_t)p.nk * rank / p.split), t1 = (int)((int64_t)p.nk * (rank + 1) / p.split);
+    const int windows = ROUND ? t1 - t0 : 1;  // accumulator fills
 
     if (warp == 0) {
         if (lane == 0) {
@@ -328,28 +326,31 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
             uint32_t last_par[S::kStages];
             bool issued[S::kStages];
             for (int s = 0; s < S::kStages; ++s) issued[s] = false;
-            int pair = t0 / p.nk, kc = t0 % p.nk;
             for (int t = t0, ring = 0; t < t1; ++t, ++ring) {
                 const int s = ring % S::kStages;
                 const uint32_t ph = (ring / S::kStages) & 1u;
                 if (!wait_bounded(smem_u32(&empty[s]), ph ^ 1u, abort, p.err)) break;
                 const uint32_t st = smem_u32(smem + (size_t)s * S::kStage), bar = smem_u32(&full[s]);
-                const int pp = pair_p(p.pairs, pair), pq = pair_q(p.pairs, pair), k0 = kc * kTK;
+                const int k0 = t * kTK;
                 mbar_arrive_tx(bar, S::kStage);
-                if (p.p_mn) {
-                    for (int j = 0; j < kTM / 64; ++j) tma_load_3d(st + j * kBox, &tmP, (int)i0 + 64 * j, k0, pp, bar);
-                } else {
-                    tma_load_3d(st, &tmP, k0, (int)i0, pp, bar);
-                }
-                if (BN >= 64 && p.q_mn) {
-                    for (int j = 0; j < BN / 64; ++j)
-                        tma_load_3d(st + S::kP + j * kBox, &tmQ, (int)j0 + 64 * j, k0, pq, bar);
-                } else {
-                    tma_load_3d(st + S::kP, &tmQ, k0, (int)j0, pq, bar);
+#pragma unroll 1
+                for (int pl = 0; pl < S::kPlanes; ++pl) {
+                    const uint32_t dp = st + pl * S::kP, dq = st + S::kPlanes * S::kP + pl * S::kQ;
+                    if (p.p_mn) {
+                        for (int j = 0; j < kTM / 64; ++j)
+                            tma_load_3d(dp + j * kBox, &tmP, (int)i0 + 64 * j, k0, pl, bar);
+                    } else {
+                        tma_load_3d(dp, &tmP, k0, (int)i0, pl, bar);
+                    }
+                    if (BN >= 64 && p.q_mn) {
+                        for (int j = 0; j < BN / 64; ++j)
+                            tma_load_3d(dq + j * kBox, &tmQ, (int)j0 + 64 * j, k0, pl, bar);
+                    } else {
+                        tma_load_3d(dq, &tmQ, k0, (int)j0, pl, bar);
+                    }
                 }
                 issued[s] = true;
                 last_par[s] = ph;
-                if (++kc == p.nk) kc = 0, ++pair;
             }
             // copies still in flight when the MMA side stopped early land before the CTA exits
             for (int s = 0; s < S::kStages; ++s)
@@ -373,7 +374,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
                 const uint32_t b = w & 1u, use = w >> 1;
                 if (!wait_bounded(smem_u32(&tempty[b]), (use & 1u) ^ 1u, abort, p.err)) break;
                 tc_fence_after();
-                const int end = t + p.window < t1 ? t + p.window : t1;
+                const int end = ROUND ? t + 1 : t1;
                 for (bool first = true; t < end; ++t, ++ring) {
                     const int s = ring % S::kStages;
                     const uint32_t ph = (ring / S::kStages) & 1u;
@@ -383,11 +384,16 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
                     }
                     tc_fence_after();
                     const uint32_t st = smem_u32(smem + (size_t)s * S::kStage);
-                    const uint64_t dp = desc_of(st, p.p_mn), dq = desc_of(st + S::kP, p.q_mn);
 #pragma unroll
-                    for (int k = 0; k < kTK / 16; ++k) {
-                        mma_bf16(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
-                        first = false;
+                    for (int x = 0; x < (ROUND ? 6 : 1); ++x) {
+                        const int vp = ROUND ? plane_p(x) : 0, vq = ROUND ? plane_q(x) : 0;
+                        const uint64_t dp = desc_of(st + vp * S::kP, p.p_mn);
+                        const uint64_t dq = desc_of(st + S::kPlanes * S::kP + vq * S::kQ, p.q_mn);
+#pragma unroll
+                        for (int k = 0; k < kTK / 16; ++k) {
+                            mma_bf16(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
+                            first = false;
+                        }
                     }
                     mma_commit(smem_u32(&empty[s]));
                 }
@@ -535,10 +541,11 @@ __device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* tm
         : "memory");
 }
 
-template <int BN>
+template <int BN, bool ROUND>
 struct PairShape {
-    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN / 2 * kTK * 2, kStage = kP + kQ;
-    static constexpr int kStages = BN == 256 ? 6 : 7;
+    static constexpr int kPlanes = ROUND ? 3 : 1;
+    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN / 2 * kTK * 2, kStage = kPlanes * (kP + kQ);
+    static constexpr int kStages = ROUND ? 2 : 6;
     static constexpr uint32_t kBlockLd = 20;  // floats of a staged row: 16 + 4, conflict-free 16-byte accesses
     static constexpr uint32_t kBlock = 32 * kBlockLd * 4;
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kEpiWarps * kBlock + 8 * (2 * kStages + 5) + 16;
@@ -557,7 +564,7 @@ struct PairParams {
 
 template <int BN, bool ROUND>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ PairParams pp) {
-    using S = PairShape<BN>;
+    using S = PairShape<BN, ROUND>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* blocks = smem + (size_t)S::kStages * S::kStage;
@@ -616,13 +623,12 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
               constexpr int g = decltype(G)::value;
               const TileParams& p = pp.g[g];
               const CUtensorMap *tmP = &pp.tmP[g], *tmQ = &pp.tmQ[g];
-              const int total = p.nk * p.pairs;
+              const int total = p.nk;
               const int64_t end = g ? units : pp.tiles[0], base = g ? pp.tiles[0] : 0;
               for (; ok && u < end; u += du) {
                 int64_t i0, j0;
                 place(p, u - base, &i0, &j0);
                 const int pr = (int)i0 + (int)rank * kTM, qr = (int)j0 + (int)rank * (BN / 2);
-                int pair = 0, kc = 0;
                 for (int t = 0; t < total; ++t, ++ring) {
                     const int s = ring % S::kStages;
                     const uint32_t ph = (ring / S::kStages) & 1u;
@@ -632,22 +638,24 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     }
                     const uint32_t st = smem_u32(smem + (size_t)s * S::kStage), bar = smem_u32(&full[s]);
                     const uint32_t lead = map_rank(bar, 0);
-                    const int vp = pair_p(p.pairs, pair), vq = pair_q(p.pairs, pair), k0 = kc * kTK;
+                    const int k0 = t * kTK;
                     if (rank == 0) mbar_arrive_tx(bar, 2 * S::kStage);
-                    if (p.p_mn) {
-                        for (int j = 0; j < kTM / 64; ++j) pair_load_3d(st + j * kBox, tmP, pr + 64 * j, k0, vp, lead);
-                    } else {
-                        pair_load_3d(st, tmP, k0, pr, vp, lead);
-                    }
-                    if (p.q_mn) {
-                        for (int j = 0; j < BN / 128; ++j)
-                            pair_load_3d(st + S::kP + j * kBox, tmQ, qr + 64 * j, k0, vq, lead);
-                    } else {
-                        pair_load_3d(st + S::kP, tmQ, k0, qr, vq, lead);
+#pragma unroll 1
+                    for (int pl = 0; pl < S::kPlanes; ++pl) {
+                        const uint32_t dp = st + pl * S::kP, dq = st + S::kPlanes * S::kP + pl * S::kQ;
+                        if (p.p_mn) {
+                            for (int j = 0; j < kTM / 64; ++j) pair_load_3d(dp + j * kBox, tmP, pr + 64 * j, k0, pl, lead);
+                        } else {
+                            pair_load_3d(dp, tmP, k0, pr, pl, lead);
+                        }
+                        if (p.q_mn) {
+                            for (int j = 0; j < BN / 128; ++j) pair_load_3d(dq + j * kBox, tmQ, qr + 64 * j, k0, pl, lead);
+                        } else {
+                            pair_load_3d(dq, tmQ, k0, qr, pl, lead);
+                        }
                     }
                     issued[s] = true;
                     last_par[s] = ph;
-                    if (++kc == p.nk) kc = 0, ++pair;
                 }
               }
             };
@@ -677,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
               const bool p_mn = p.p_mn, q_mn = p.q_mn;
               const uint32_t idesc = idesc_bf16(2 * kTM, BN) | (p_mn ? 1u << 15 : 0u) | (q_mn ? 1u << 16 : 0u);
               const uint64_t sp = desc_step(p_mn), sq = desc_step(q_mn);
-              const int total = p.nk * p.pairs, window = p.window, windows = (total + window - 1) / window;
+              const int total = p.nk, windows = ROUND ? total : 1;  // accumulator fills of a tile
               const int64_t last = g ? units : pp.tiles[0];
               for (; ok && u < last; u += du) {
                 int t = 0;
@@ -688,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         break;
                     }
                     tc_fence_after();
-                    const int end = t + window < total ? t + window : total;
+                    const int end = ROUND ? t + 1 : total;
                     for (bool first = true; t < end; ++t, ++ring) {
                         const int s = ring % S::kStages;
                         const uint32_t ph = (ring / S::kStages) & 1u;
@@ -698,11 +706,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         }
                         tc_fence_after();
                         const uint32_t st = smem_u32(smem + (size_t)s * S::kStage);
-                        const uint64_t dp = desc_of(st, p_mn), dq = desc_of(st + S::kP, q_mn);
 #pragma unroll
-                        for (int k = 0; k < kTK / 16; ++k) {
-                            pair_mma(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
-                            first = false;
+                        for (int x = 0; x < (ROUND ? 6 : 1); ++x) {
+                            const int vp = ROUND ? plane_p(x) : 0, vq = ROUND ? plane_q(x) : 0;
+                            const uint64_t dp = desc_of(st + vp * S::kP, p_mn);
+                            const uint64_t dq = desc_of(st + S::kPlanes * S::kP + vq * S::kQ, q_mn);
+#pragma unroll
+                            for (int k = 0; k < kTK / 16; ++k) {
+                                pair_mma(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
+                                first = false;
+                            }
                         }
                         pair_commit(smem_u32(&empty[s]));
                     }
@@ -815,7 +828,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 float acc[kC];
 #pragma unroll
                 for (int i = 0; i < kC; ++i) acc[i] = 0.f;
-                const int windows = (p.nk * p.pairs + p.window - 1) / p.window;
+                const int windows = p.nk;
                 for (int w = 0; w < windows; ++w) {
                     if (!(got = wait_for())) break;
 #pragma unroll
@@ -901,10 +914,11 @@ cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams&
     p.tiles_p = (P.extent() + kTM - 1) / kTM;
     p.tiles_q = (Q.extent() + BN - 1) / BN;
     const int64_t tiles = p.tiles_p * p.tiles_q;
-    // split the K loop while the CTAs still fit the GPU at once and each keeps four chunks
+    // split the K loop while the CTAs still fit the GPU at once and each keeps four chunks' worth of MMAs
+    const int least = ROUND ? 1 : 4;
     const int64_t slots = (int64_t)sm_count() * (ROUND ? 1 : 2);
     p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= slots && p.nk * p.pairs >= 8 * p.split) p.split *= 2;
+    while (p.split < 8 && tiles * p.split * 2 <= slots && p.nk >= 2 * least * p.split) p.split *= 2;
     if (tiles * p.split > 2147483647LL) return cudaErrorInvalidConfiguration;
     cudaError_t e = smem_attr_once<linear_tile_kernel<T, BN, ROUND>>((int)S::kSmem);
     if (e != cudaSuccess) return e;
@@ -931,7 +945,7 @@ struct Product {
 
 template <int BN, bool ROUND>
 cudaError_t run_pair(const Product* const* pr, int count, cudaStream_t s) {
-    using S = PairShape<BN>;
+    using S = PairShape<BN, ROUND>;
     PairParams pp;
     pp.tiles[0] = pp.tiles[1] = 0;
     for (int i = 0; i < count; ++i) {
@@ -1000,8 +1014,6 @@ static Product make_product(const LinearProduct& x, unsigned int* err) {
     r.p.ep = x.ep;
     r.p.ep.f32 = x.out == TDA_F32;
     r.p.nk = (int)((r.P.depth() + kTK - 1) / kTK);
-    r.p.pairs = r.P.planes == 3 ? 6 : 1;
-    r.p.window = r.P.planes == 3 ? kWindow : r.p.nk;
     r.p.split = 1;
     r.p.p_mn = r.P.mn;
     r.p.q_mn = r.Q.mn;
@@ -1010,7 +1022,7 @@ static Product make_product(const LinearProduct& x, unsigned int* err) {
 }
 
 static int64_t pair_tiles(const Product& x) {
-    const int64_t bn = x.p.pairs > 1 ? 128 : 256;
+    const int64_t bn = x.P.planes == 3 ? 128 : 256;
     return x.p.swap ? 0 : ((x.P.extent() + 2 * kTM - 1) / (2 * kTM)) * ((x.Q.extent() + bn - 1) / bn);
 }
 
@@ -1024,7 +1036,7 @@ cudaError_t launch_linear_products(const LinearProduct* x, int count, unsigned i
         tiles = i > 0 && (t == 0 || tiles == 0) ? 0 : tiles + t;
         order[i] = &r[i];
     }
-    const bool round = r[0].p.pairs > 1;
+    const bool round = r[0].P.planes == 3;
     // a pair's tile for at least half of the SM pairs
     if (tiles * 4 >= sm_count()) {
         if (count == 2 && r[1].p.nk > r[0].p.nk) order[0] = &r[1], order[1] = &r[0];
