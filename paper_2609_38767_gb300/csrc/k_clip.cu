@@ -34,28 +34,17 @@ struct ClipTensor {
 };
 constexpr int64_t kBf16Bit = (int64_t)1 << 62;
 
+constexpr int kMaxGrid = 2048;    // CTAs of one launch
 struct ClipTable {
     ClipTensor t[kMaxTensors];
     int32_t count;
     int64_t chunks;
+    uint16_t first_of[kMaxGrid + 1];  // tensor that holds CTA b's first chunk; [b + 1]: about its last
 };
 
 __device__ __forceinline__ float2 two_sum(float a, float b) {
     const float s = __fadd_rn(a, b), bb = __fsub_rn(s, a);
     return make_float2(s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, bb)), __fsub_rn(b, bb)));
-}
-
-// The tensor that holds chunk c: the last one whose first chunk is <= c.
-__device__ __forceinline__ int find_tensor(const ClipTable& T, int64_t c) {
-    int lo = 0, hi = T.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if ((T.t[mid].first & ~kBf16Bit) <= c)
-            lo = mid;
-        else
-            hi = mid - 1;
-    }
-    return lo;
 }
 
 struct Sum {
@@ -77,7 +66,7 @@ __device__ __forceinline__ void add_squares(Sum& s, const float* v) {
         s.hi = r.x;
         s.lo += r.y;
     } else {
-#pragma unroll 1
+#pragma unroll
         for (int i = 0; i < N; ++i) s.wide = fma((double)v[i], (double)v[i], s.wide);
     }
 }
@@ -112,10 +101,10 @@ __device__ __forceinline__ void from_f(float x, __nv_bfloat16* p) { *p = __float
 
 template <typename T>
 __device__ __forceinline__ void chunk_squares(Sum& s, const T* g, int n) {
-    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, U = 4;
+    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, kPer = kVecs / kThreads, U = kPer;
     if (n == kChunk && ((uintptr_t)g & 15) == 0) {
 #pragma unroll
-        for (int j = 0; j < kVecs / kThreads; j += U) {
+        for (int j = 0; j < kPer; j += U) {
             uint4 r[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) r[u] = __ldg((const uint4*)g + (j + u) * kThreads + threadIdx.x);
@@ -136,9 +125,11 @@ __device__ __forceinline__ void chunk_squares(Sum& s, const T* g, int n) {
 
 // CTA b owns chunks [chunks b / grid, chunks (b+1) / grid).
 __global__ void __launch_bounds__(kThreads) clip_squares_kernel(const __grid_constant__ ClipTable T, double* part) {
+    chain_wait();
+    chain_next();
     const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
     Sum s;
-    int t = find_tensor(T, c0);
+    int t = T.first_of[blockIdx.x];
     for (int64_t c = c0; c < c1; ++c) {
         while (t + 1 < T.count && (T.t[t + 1].first & ~kBf16Bit) <= c) ++t;
         const int64_t off = (c - (T.t[t].first & ~kBf16Bit)) * kChunk, left = T.t[t].n - off;
@@ -162,10 +153,10 @@ __global__ void __launch_bounds__(kThreads) clip_squares_kernel(const __grid_con
 
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T* g, T* out, int n, float c) {
-    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, U = 4;
+    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, kPer = kVecs / kThreads, U = kPer;
     if (n == kChunk && (((uintptr_t)g | (uintptr_t)out) & 15) == 0) {
 #pragma unroll
-        for (int j = 0; j < kVecs / kThreads; j += U) {
+        for (int j = 0; j < kPer; j += U) {
             uint4 r[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) r[u] = __ldcs((const uint4*)g + (j + u) * kThreads + threadIdx.x);
@@ -193,6 +184,8 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* out, int n, float c) 
 // n_part partials of all launches of clip_squares_kernel. norm_out is written by the last table's first CTA.
 __global__ void __launch_bounds__(kThreads)
 clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n_part, float max_norm, float* norm_out) {
+    chain_wait();
+    chain_next();
     double d = 0.0;
     for (int i = threadIdx.x; i < n_part; i += kThreads) d += part[i];
 #pragma unroll
@@ -212,7 +205,7 @@ clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n
     const float c = coef;
     const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
     if (c1 <= c0) return;
-    int t = find_tensor(T, c1 - 1);
+    int t = T.first_of[blockIdx.x + 1];  // the next CTA's first tensor: this CTA's last one or the one after it
     for (int64_t k = c1 - 1; k >= c0; --k) {
         while ((T.t[t].first & ~kBf16Bit) > k) --t;
         if (!T.t[t].out || (c == 1.f && T.t[t].out == T.t[t].in)) continue;  // norm only, or nothing changes in place
@@ -238,8 +231,8 @@ int sm_count() {
     return v;
 }
 
-// Fills the table with tensors from *i on (empty ones left out); false when there is nothing left.
-bool next_table(const tda_tensor_ref* list, int64_t n_tensors, int64_t* i, ClipTable* T) {
+// Fills the table with tensors from *i on (empty ones left out) for at most `most` CTAs; false when none is left.
+bool next_table(const tda_tensor_ref* list, int64_t n_tensors, int64_t* i, int64_t most, ClipTable* T, int64_t* grid) {
     T->count = 0;
     T->chunks = 0;
     for (; *i < n_tensors && T->count < kMaxTensors; ++*i) {
@@ -252,40 +245,42 @@ bool next_table(const tda_tensor_ref* list, int64_t n_tensors, int64_t* i, ClipT
         t.first = T->chunks | (r.dtype == TDA_BF16 ? kBf16Bit : 0);
         T->chunks += (r.n + kChunk - 1) / kChunk;
     }
+    *grid = T->chunks < 1 ? 1 : T->chunks < most ? T->chunks : most;
+    int t = 0;
+    for (int64_t b = 0; b <= *grid; ++b) {
+        const int64_t c = T->chunks * b / *grid;
+        while (t + 1 < T->count && (T->t[t + 1].first & ~kBf16Bit) <= c) ++t;
+        T->first_of[b] = (uint16_t)t;
+    }
     return T->count > 0;
 }
 
 }  // namespace
 
-// CTAs of one table's launches: enough to fill the SMs, at most one per chunk.
-constexpr int kClipCtasPerSm = 8;
-constexpr int64_t kClipMaxGrid = 4096;  // bounds the partials of one launch (any GPU up to 512 SMs)
+constexpr int kClipCtasPerSm = 8;  // enough to fill an SM
 
 size_t clip_workspace_bytes(int64_t n_tensors) {
     const int64_t tables = (n_tensors + kMaxTensors - 1) / kMaxTensors;
-    return sizeof(double) * (size_t)(kClipMaxGrid * (tables > 1 ? tables : 1));
+    return sizeof(double) * (size_t)(kMaxGrid * (tables > 1 ? tables : 1));
 }
 
 cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, double* part,
                              cudaStream_t s) {
-    const int64_t most = (int64_t)sm_count() * kClipCtasPerSm < kClipMaxGrid ? (int64_t)sm_count() * kClipCtasPerSm
-                                                                             : kClipMaxGrid;
+    int64_t most = (int64_t)sm_count() * kClipCtasPerSm, grid;
+    if (most > kMaxGrid) most = kMaxGrid;
     ClipTable T;
     int n_part = 0;
-    for (int64_t i = 0; next_table(list, n_tensors, &i, &T);) {
-        const int64_t grid = T.chunks < most ? T.chunks : most;
-        note_launches(1);
-        clip_squares_kernel<<<(unsigned)grid, kThreads, 0, s>>>(T, part + n_part);
-        cudaError_t e = cudaGetLastError();
+    bool chained = false;
+    for (int64_t i = 0; next_table(list, n_tensors, &i, most, &T, &grid); chained = true) {
+        cudaError_t e = launch_chained(chained, clip_squares_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T,
+                                       part + n_part);
         if (e != cudaSuccess) return e;
         n_part += (int)grid;
     }
     bool first = true;
-    for (int64_t i = 0; next_table(list, n_tensors, &i, &T) || first; first = false) {
-        const int64_t grid = T.chunks < 1 ? 1 : T.chunks < most ? T.chunks : most;
-        note_launches(1);
-        clip_scale_kernel<<<(unsigned)grid, kThreads, 0, s>>>(T, part, n_part, max_norm, first ? norm : nullptr);
-        cudaError_t e = cudaGetLastError();
+    for (int64_t i = 0; next_table(list, n_tensors, &i, most, &T, &grid) || first; first = false, chained = true) {
+        cudaError_t e = launch_chained(chained, clip_scale_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T, part,
+                                       n_part, max_norm, first ? norm : nullptr);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

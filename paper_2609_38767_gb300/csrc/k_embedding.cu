@@ -77,13 +77,33 @@ lookup_kernel(const T* __restrict__ E, int64_t ld_e, int64_t V, int64_t d, const
 // #{j < i : k_j <= k_i} + #{j > i : k_j < k_i}, counted directly: one launch, n^2 comparisons over all SMs.
 constexpr int kRankMax = 8192, kRankThreads = 256;
 
+//
+// With `clear` set the launch also zeroes the gradient's rows, all of them, beside the counting: the few
+// that tokens name are written twice, but no row waits for the sorted list.
+struct ClearParams {
+    uint4* p;          // NULL: nothing to clear; rows 16-byte aligned, whole 16-byte vectors
+    int64_t rows, vecs, ld;  // vectors of a row, row stride in vectors
+};
+constexpr int kClearRows = 16;
+
 template <typename I>
 __global__ void __launch_bounds__(kRankThreads)
-rank_kernel(const I* __restrict__ tok, int n, uint32_t V, uint32_t* __restrict__ skey, int32_t* __restrict__ order) {
+rank_kernel(const I* __restrict__ tok, int n, uint32_t V, uint32_t* __restrict__ skey, int32_t* __restrict__ order,
+            int ctas, const ClearParams clear) {
+    if ((int)blockIdx.x >= ctas) {
+        chain_next();
+        const int64_t r0 = (int64_t)((int)blockIdx.x - ctas) * kClearRows;
+        for (int64_t r = r0; r < r0 + kClearRows && r < clear.rows; ++r)
+            for (int64_t c = threadIdx.x; c < clear.vecs; c += kRankThreads)
+                clear.p[r * clear.ld + c] = make_uint4(0, 0, 0, 0);
+        return;
+    }
     __shared__ alignas(16) uint32_t key[kRankMax];
     __shared__ int cnt[kRankThreads / 32][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int np = (n + 31) & ~31;
+    chain_next();
+#pragma unroll 8
     for (int j = threadIdx.x; j < np; j += kRankThreads) key[j] = j < n ? sort_key(tok, j, V) : 0xFFFFFFFFu;
     __syncthreads();
     const int i0 = blockIdx.x * 32, i = i0 + lane;
@@ -121,13 +141,15 @@ rank_kernel(const I* __restrict__ tok, int n, uint32_t V, uint32_t* __restrict__
 
 // More tokens: a stable radix sort from the low digit up, digits of at most 9 bits (2 passes up to 2^18 ids),
 // three launches a pass: digit counts per tile, their scan per digit, the scatter.
-constexpr int kTile = 4096, kSortThreads = 256, kBins = 512, kRounds = kTile / kSortThreads;
+constexpr int kTile = 1024, kSortThreads = 256, kBins = 512, kRounds = kTile / kSortThreads;
 
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
 digit_count_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key, int n, uint32_t V, int shift,
                    uint32_t mask, uint32_t* __restrict__ hist) {
     __shared__ uint32_t h[kBins];
+    chain_wait();
+    chain_next();
     for (int b = threadIdx.x; b < kBins; b += kSortThreads) h[b] = 0;
     __syncthreads();
     const int64_t base = (int64_t)blockIdx.x * kTile;
@@ -144,6 +166,8 @@ digit_count_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key, 
 __global__ void __launch_bounds__(kSortThreads) digit_scan_kernel(uint32_t* __restrict__ hist, int tiles,
                                                                   uint32_t* __restrict__ total) {
     __shared__ uint32_t w[kSortThreads / 32];
+    chain_wait();
+    chain_next();
     uint32_t* h = hist + (int64_t)blockIdx.x * tiles;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t before = 0;
@@ -181,6 +205,8 @@ digit_scatter_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key
     __shared__ uint32_t pos[W][kBins];  // counts of each warp's run, then the next place of each digit
     __shared__ uint32_t start[kBins];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    chain_wait();
+    chain_next();
     for (int b = threadIdx.x; b < W * kBins; b += kSortThreads) (&pos[0][0])[b] = 0;
     // first place of each digit: scan of the totals (warp 0, 16 digits a lane)
     if (warp == 0) {
@@ -252,6 +278,7 @@ struct GradParams {
     int64_t n, d, ld_d, V, ld_e, dp;  // dp: row length of the partials
     int64_t chunks, col_blocks;
     int C;
+    int quads;  // rows of dE may be moved four values at a time
     float scale, beta;
     const uint32_t* skey;
     const int32_t* order;
@@ -274,8 +301,10 @@ __device__ __forceinline__ void store_row(TO* p, const float* acc, float scale, 
 }
 
 template <typename TI, typename TO, int N>
-__global__ void __launch_bounds__(kSumThreads)
+__global__ void __launch_bounds__(kSumThreads, 8)
 grad_sum_kernel(const TI* __restrict__ dout, TO* __restrict__ dE, const GradParams p) {
+    chain_wait();
+    chain_next();
     const int64_t sums = p.chunks * p.col_blocks;
     if ((int64_t)blockIdx.x >= sums) {
         // rows of E that no token names
@@ -297,115 +326,175 @@ grad_sum_kernel(const TI* __restrict__ dout, TO* __restrict__ dE, const GradPara
         for (int r = 0; r < kZeroRows; ++r) {
             if (named[r]) continue;
             TO* row = dE + (v0 + r) * p.ld_e;
-            for (int64_t c = (int64_t)threadIdx.x * N; c < p.d; c += kSumThreads * N) {
-                const float zero[N] = {};
-                store_row<TO, N>(row + c, zero, 0.f, p.beta);
+            constexpr int kZ = N == 1 ? 1 : N == 2 ? 2 : 16 / sizeof(TO);  // 16 bytes, neighbours side by side
+            for (int64_t c = (int64_t)threadIdx.x * kZ; c < p.d; c += kSumThreads * kZ) {
+                const float zero[kZ] = {};
+                store_row<TO, kZ>(row + c, zero, 0.f, p.beta);
             }
         }
         return;
     }
-    extern __shared__ uint32_t sm[];
-    uint32_t* key = sm;                     // [C]
-    int32_t* pos = (int32_t*)(sm + p.C);    // [C]
+    // For each position of the chunk: where its row is, and, if a run ends there, where the sum goes: a row of
+    // dE or a row of partials (byte offsets).
+    extern __shared__ int64_t sm[];
+    int64_t* dst = sm;                             // [C]
+    int32_t* pos = (int32_t*)(sm + p.C);           // [C]
+    uint32_t* key = (uint32_t*)(pos + p.C);        // [C]
+    uint8_t* end = (uint8_t*)(key + p.C);          // [C]: 0 the run goes on, 1 ends in dE, 2 in partials
     const int64_t ch = (int64_t)blockIdx.x / p.col_blocks, i0 = ch * p.C;
     const int64_t col = ((int64_t)blockIdx.x % p.col_blocks) * kSumThreads * N + (int64_t)threadIdx.x * N;
-    const int have = p.n - i0 < p.C ? (int)(p.n - i0) : p.C;
-    for (int i = threadIdx.x; i < have; i += kSumThreads) {
+    const int in = p.n - i0 < p.C ? (int)(p.n - i0) : p.C;
+    const uint32_t none = (uint32_t)p.V;
+    const uint32_t prev = i0 > 0 ? p.skey[i0 - 1] : none, next = i0 + p.C < p.n ? p.skey[i0 + p.C] : none;
+    for (int i = threadIdx.x; i < in; i += kSumThreads) {
         key[i] = p.skey[i0 + i];
         pos[i] = p.order[i0 + i];
     }
-    const uint32_t none = (uint32_t)p.V;
-    const uint32_t prev = i0 > 0 ? p.skey[i0 - 1] : none, next = i0 + p.C < p.n ? p.skey[i0 + p.C] : none;
     __syncthreads();
+    int live = 0;
+    for (int i = threadIdx.x; i < in; i += kSumThreads) {
+        const uint32_t k = key[i];
+        const bool last = i + 1 == in || key[i + 1] != k;
+        end[i] = 0;
+        if (last) {
+            // the first run of the chunk may have begun before it, the last one may go on after it
+            const bool head = key[0] == k && k == prev, tail = i + 1 == p.C && k == next;
+            end[i] = head || tail ? 2 : 1;
+            dst[i] = head ? 2 * ch * p.dp : tail ? (2 * ch + 1) * p.dp : (int64_t)k * p.ld_e;
+        }
+        live += k != none;
+    }
+    const int have = [&] {  // ids outside the table come last and are left out
+        int c = live;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
+        __shared__ int w[kSumThreads / 32];
+        if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int i = 0; i < kSumThreads / 32; ++i) c += w[i];
+        return c;
+    }();
     if (col >= p.d) return;
     float acc[N] = {};
-    int from = 0;  // where the current run starts in this chunk
-    uint32_t cur = key[0];
-    auto flush = [&](int to) {
-        if (from == 0 && cur == prev)
-            store_row<float, N>(p.part + (2 * ch) * p.dp + col, acc, 1.f, 0.f);
-        else if (to == p.C && cur == next)
-            store_row<float, N>(p.part + (2 * ch + 1) * p.dp + col, acc, 1.f, 0.f);
-        else
-            store_row<TO, N>(dE + (int64_t)cur * p.ld_e + col, acc, p.scale, p.beta);
-    };
     const TI* src = dout + col;
-    for (int i = 0; i < have && cur != none; i += kBatch) {
+    TO* out = dE + col;
+    float* part = p.part + col;
+    for (int i = 0; i < have; i += kBatch) {
         Vec<TI, N> x[kBatch];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
-            if (i + u < have && key[i + u] != none)
-                x[u] = *reinterpret_cast<const Vec<TI, N>*>(src + (int64_t)pos[i + u] * p.ld_d);
+            if (i + u < have) x[u] = *reinterpret_cast<const Vec<TI, N>*>(src + (int64_t)pos[i + u] * p.ld_d);
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (i + u >= have) break;
-            if (key[i + u] != cur) {
-                flush(i + u);
-                cur = key[i + u];
-                from = i + u;
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += to_f(x[u].v[e]);
+            if (const int f = end[i + u]) {
+                if (f == 1)
+                    store_row<TO, N>(out + dst[i + u], acc, p.scale, p.beta);
+                else
+                    store_row<float, N>(part + dst[i + u], acc, 1.f, 0.f);
 #pragma unroll
                 for (int e = 0; e < N; ++e) acc[e] = 0.f;
             }
-            if (cur == none) break;
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += to_f(x[u].v[e]);
         }
     }
-    if (cur != none) flush(have);
 }
 
 // A run that crosses chunk edges: the CTA of the chunk where it starts adds its partials in order.
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
+// Four columns of a finished sum to dE.
+template <typename TO>
+__device__ __forceinline__ void store_join(const GradParams& p, TO* dE, uint32_t k, int64_t col, const float4& a) {
+    const float v[4] = {a.x, a.y, a.z, a.w};
+    TO* q = dE + (int64_t)k * p.ld_e + col;
+    if (p.quads && col + 4 <= p.d) {
+        store_row<TO, 4>(q, v, p.scale, p.beta);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < p.d) store_row<TO, 1>(q + i, v + i, p.scale, p.beta);
+    }
+}
+
+// CTA (x, y): the runs that start in kJoinChunks chunks, 128 columns of them (4 a lane). A warp looks through
+// each chunk; then each warp takes a run of its own, or all of them share a long one.
+constexpr int kJoinChunks = kJoinWarps;
+
 template <typename TO>
 __global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(TO* __restrict__ dE, const GradParams p) {
-    const int64_t ch = blockIdx.x, i0 = ch * p.C, i1 = i0 + p.C;  // i1 < n: the last chunk starts no such run
-    const uint32_t k = p.skey[i1 - 1], none = (uint32_t)p.V;
-    if (k == none || p.skey[i1] != k) return;
-    if (i0 > 0 && p.skey[i0 - 1] == k) return;  // the run started earlier
-    int64_t lo = ch + 1, hi = p.chunks - 1;     // last chunk whose first key is k
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (p.skey[mid * p.C] == k)
-            lo = mid;
-        else
-            hi = mid - 1;
-    }
-    const int64_t parts = lo - ch + 1;
+    chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // partial 0: the tail of chunk ch; partial j: the head of chunk ch + j. Unrolled loads, ordered additions.
-    auto add = [&](int64_t j0, int64_t j1, int64_t col) {
-        float a = 0.f;
-        for (int64_t j = j0; j < j1; j += 8) {
-            float x[8];
+    const uint32_t none = (uint32_t)p.V;
+    __shared__ int parts_of[kJoinChunks];  // 0: no run starts in the chunk and leaves it
+    __shared__ uint32_t key_of[kJoinChunks];
+    const int64_t ch0 = (int64_t)blockIdx.x * kJoinChunks;
+    if (const int64_t ch = ch0 + warp; warp < kJoinChunks) {
+        const int64_t i0 = ch * p.C, i1 = i0 + p.C;
+        int parts = 0;
+        uint32_t k = none;
+        if (ch + 1 < p.chunks) {
+            k = p.skey[i1 - 1];
+            const uint32_t after = p.skey[i1], before = i0 > 0 ? p.skey[i0 - 1] : none;
+            if (k != none && after == k && before != k) {
+                // the chunks after ch whose first key is k, 32 at a time
+                parts = 1;
+                for (int64_t c = ch + 1;; c += 32) {
+                    const uint32_t other = ~__ballot_sync(0xffffffffu, c + lane < p.chunks && p.skey[(c + lane) * p.C] == k);
+                    parts += other ? __ffs(other) - 1 : 32;
+                    if (other) break;
+                }
+            }
+        }
+        if (lane == 0) {
+            parts_of[warp] = parts;
+            key_of[warp] = k;
+        }
+    }
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.y * 128 + lane * 4;
+    // partial 0 of a run is the tail of its first chunk, partial j the head of the j-th after it; rows of partials
+    // are padded to a multiple of 8 columns. Eight loads ahead, additions in order.
+    auto add = [&](int64_t ch, int j0, int j1) {
+        const float* base = p.part + 2 * ch * p.dp + col;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (col >= p.d) return a;
+        for (int j = j0; j < j1; j += 8) {
+            float4 x[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                x[u] = j + u < j1 ? p.part[(2 * (ch + j + u) + (j + u == 0)) * p.dp + col] : 0.f;
+            for (int u = 0; u < 8; ++u) {
+                x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (j + u < j1) x[u] = *reinterpret_cast<const float4*>(base + (2 * (int64_t)(j + u) + (j + u == 0)) * p.dp);
+            }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) a += x[u];
+            for (int u = 0; u < 8; ++u) a.x += x[u].x, a.y += x[u].y, a.z += x[u].z, a.w += x[u].w;
         }
         return a;
     };
-    __shared__ float sh[kJoinWarps][32];
-    if (parts < 4 * kJoinWarps) {  // a thread adds all partials of a column
-        for (int64_t col = (int64_t)blockIdx.y * kJoinThreads + threadIdx.x; col < p.d;
-             col += (int64_t)gridDim.y * kJoinThreads) {
-            const float a = add(0, parts, col);
-            store_row<TO, 1>(dE + (int64_t)k * p.ld_e + col, &a, p.scale, p.beta);
-        }
-        return;
+    constexpr int kLong = 4 * kJoinWarps;
+    int seen = 0;
+    for (int c = 0; c < kJoinChunks; ++c) {
+        const int parts = parts_of[c];
+        if (parts == 0 || parts >= kLong) continue;
+        if (seen++ % kJoinWarps != warp) continue;
+        const float4 a = add(ch0 + c, 0, parts);
+        if (col < p.d) store_join(p, dE, key_of[c], col, a);
     }
-    // a long run: each warp adds an eighth of the partials, then the eighths in order
-    for (int64_t c0 = (int64_t)blockIdx.y * 32; c0 < p.d; c0 += (int64_t)gridDim.y * 32) {
-        const int64_t col = c0 + lane;
-        float a = 0.f;
-        if (col < p.d) a = add(parts * warp / kJoinWarps, parts * (warp + 1) / kJoinWarps, col);
+    __shared__ float4 sh[kJoinWarps][32];
+    for (int c = 0; c < kJoinChunks; ++c) {
+        const int parts = parts_of[c];
+        if (parts < kLong) continue;
+        float4 a = add(ch0 + c, (int)((int64_t)parts * warp / kJoinWarps), (int)((int64_t)parts * (warp + 1) / kJoinWarps));
         sh[warp][lane] = a;
         __syncthreads();
         if (warp == 0 && col < p.d) {
 #pragma unroll
-            for (int w = 1; w < kJoinWarps; ++w) a += sh[w][lane];
-            store_row<TO, 1>(dE + (int64_t)k * p.ld_e + col, &a, p.scale, p.beta);
+            for (int w = 1; w < kJoinWarps; ++w)
+                a.x += sh[w][lane].x, a.y += sh[w][lane].y, a.z += sh[w][lane].z, a.w += sh[w][lane].w;
+            store_join(p, dE, key_of[c], col, a);
         }
         __syncthreads();
     }
@@ -428,7 +517,7 @@ struct GradLayout {
 // leave few partials (2 rows of fp32 per chunk against C rows read).
 GradLayout grad_layout(int64_t d, int64_t n) {
     GradLayout g;
-    g.C = n <= 16384 ? 32 : n <= 131072 ? 64 : 256;
+    g.C = n <= 8192 ? 16 : n <= 16384 ? 32 : n <= 131072 ? 64 : 256;
     g.chunks = (n + g.C - 1) / g.C;
     g.dp = (d + 7) & ~(int64_t)7;
     g.tiles = (n + kTile - 1) / kTile;
@@ -487,13 +576,14 @@ cudaError_t lookup(const T* E, int64_t ld_e, int64_t V, int64_t d, const I* tok,
 }
 
 template <typename I>
-cudaError_t sort_tokens(const I* tok, int64_t n, int64_t V, const GradLayout& g, char* ws, cudaStream_t s) {
+cudaError_t sort_tokens(const I* tok, int64_t n, int64_t V, const GradLayout& g, const ClearParams& clear, char* ws,
+                        cudaStream_t s) {
     uint32_t* skey = (uint32_t*)(ws + g.skey);
     int32_t* order = (int32_t*)(ws + g.order);
     if (n <= kRankMax) {
-        note_launches(1);
-        rank_kernel<I><<<(unsigned)((n + 31) / 32), kRankThreads, 0, s>>>(tok, (int)n, (uint32_t)V, skey, order);
-        return cudaGetLastError();
+        const int64_t ctas = (n + 31) / 32, more = clear.p ? (clear.rows + kClearRows - 1) / kClearRows : 0;
+        return launch_chained(false, rank_kernel<I>, dim3((unsigned)(ctas + more)), dim3(kRankThreads), 0, s, tok, (int)n,
+                              (uint32_t)V, skey, order, (int)ctas, clear);
     }
     int bits = 1;  // of the keys 0 .. V
     while (V >> bits) ++bits;
@@ -507,13 +597,14 @@ cudaError_t sort_tokens(const I* tok, int64_t n, int64_t V, const GradLayout& g,
         uint32_t* ko = here ? skey : (uint32_t*)(ws + g.key2);
         int32_t* vo = here ? order : (int32_t*)(ws + g.val2);
         const uint32_t mask = (1u << width) - 1;
-        note_launches(3);
-        digit_count_kernel<I><<<(unsigned)g.tiles, kSortThreads, 0, s>>>(tok, kin, (int)n, (uint32_t)V, p * width, mask,
-                                                                        hist);
-        digit_scan_kernel<<<mask + 1, kSortThreads, 0, s>>>(hist, (int)g.tiles, total);
-        digit_scatter_kernel<I><<<(unsigned)g.tiles, kSortThreads, 0, s>>>(tok, kin, vin, (int)n, (uint32_t)V,
-                                                                          p * width, mask, hist, total, ko, vo);
-        cudaError_t e = cudaGetLastError();
+        const dim3 tiles((unsigned)g.tiles), block(kSortThreads);
+        cudaError_t e = launch_chained(p > 0, digit_count_kernel<I>, tiles, block, 0, s, tok, kin, (int)n, (uint32_t)V,
+                                       p * width, mask, hist);
+        if (e != cudaSuccess) return e;
+        e = launch_chained(true, digit_scan_kernel, dim3(mask + 1), block, 0, s, hist, (int)g.tiles, total);
+        if (e != cudaSuccess) return e;
+        e = launch_chained(true, digit_scatter_kernel<I>, tiles, block, 0, s, tok, kin, vin, (int)n, (uint32_t)V, p * width,
+                           mask, hist, total, ko, vo);
         if (e != cudaSuccess) return e;
         kin = ko;
         vin = vo;
@@ -523,7 +614,7 @@ cudaError_t sort_tokens(const I* tok, int64_t n, int64_t V, const GradLayout& g,
 
 template <typename TI, typename TO>
 cudaError_t sums(const TI* dout, int64_t ld_d, int64_t V, int64_t d, int64_t n, float scale, TO* dE, int64_t ld_e,
-                 float beta, const GradLayout& g, char* ws, cudaStream_t s) {
+                 float beta, bool cleared, const GradLayout& g, char* ws, cudaStream_t s) {
     GradParams p;
     p.n = n, p.d = d, p.ld_d = ld_d, p.V = V, p.ld_e = ld_e, p.dp = g.dp;
     p.chunks = g.chunks, p.C = g.C, p.scale = scale, p.beta = beta;
@@ -533,28 +624,23 @@ cudaError_t sums(const TI* dout, int64_t ld_d, int64_t V, int64_t d, int64_t n, 
     const int ai = row_align(dout, ld_d, sizeof(TI)) / (int)sizeof(TI), ao = row_align(dE, ld_e, sizeof(TO));
     constexpr int kFull = 16 / sizeof(TI);
     auto fits = [&](int N) { return d % N == 0 && ai >= N && (size_t)ao >= (N * sizeof(TO) < 16 ? N * sizeof(TO) : 16); };
+    p.quads = ao >= (int)(4 * sizeof(TO));
     const int N = fits(kFull) ? kFull : fits(2) ? 2 : 1;
     p.col_blocks = (d + (int64_t)kSumThreads * N - 1) / ((int64_t)kSumThreads * N);
-    const int64_t zero = beta == 1.f ? 0 : (V + kZeroRows - 1) / kZeroRows;
+    const int64_t zero = beta == 1.f || cleared ? 0 : (V + kZeroRows - 1) / kZeroRows;
     const int64_t grid = p.chunks * p.col_blocks + zero;
     if (grid > 0) {
         if (grid > 2147483647LL) return cudaErrorInvalidConfiguration;
-        const size_t sm = 8 * (size_t)g.C;
-        note_launches(1);
-        if (N == kFull)
-            grad_sum_kernel<TI, TO, kFull><<<(unsigned)grid, kSumThreads, sm, s>>>(dout, dE, p);
-        else if (N == 2)
-            grad_sum_kernel<TI, TO, 2><<<(unsigned)grid, kSumThreads, sm, s>>>(dout, dE, p);
-        else
-            grad_sum_kernel<TI, TO, 1><<<(unsigned)grid, kSumThreads, sm, s>>>(dout, dE, p);
-        cudaError_t e = cudaGetLastError();
+        const auto kernel = N == kFull ? grad_sum_kernel<TI, TO, kFull>
+                            : N == 2   ? grad_sum_kernel<TI, TO, 2>
+                                       : grad_sum_kernel<TI, TO, 1>;
+        cudaError_t e = launch_chained(n > 0, kernel, dim3((unsigned)grid), dim3(kSumThreads), 17 * (size_t)g.C, s, dout,
+                                       dE, p);
         if (e != cudaSuccess) return e;
     }
     if (p.chunks < 2) return cudaSuccess;
-    int64_t cols = (d + kJoinThreads - 1) / kJoinThreads;
-    note_launches(1);
-    grad_join_kernel<TO><<<dim3((unsigned)(p.chunks - 1), (unsigned)(cols < 8 ? cols : 8)), kJoinThreads, 0, s>>>(dE, p);
-    return cudaGetLastError();
+    const dim3 grid2((unsigned)((p.chunks - 1 + kJoinChunks - 1) / kJoinChunks), (unsigned)((d + 127) / 128));
+    return launch_chained(true, grad_join_kernel<TO>, grid2, dim3(kJoinThreads), 0, s, dE, p);
 }
 
 }  // namespace
@@ -573,17 +659,24 @@ cudaError_t launch_embedding_forward(tda_dtype dt, const void* E, int64_t ld_e, 
 cudaError_t launch_embedding_backward(tda_dtype dt, const void* dout, int64_t ld_d, int64_t V, int64_t d,
                                       tda_index_type it, const void* tok, int64_t n, float scale, tda_dtype gt,
                                       void* dE, int64_t ld_e, float beta, void* ws, cudaStream_t s) {
-    GradLayout g;
+    GradLayout g = {};
+    g.C = 32;
+    ClearParams clear = {};
     if (n > 0) {
         g = grad_layout(d, n);
-        cudaError_t e = it == TDA_I64 ? sort_tokens((const int64_t*)tok, n, V, g, (char*)ws, s)
-                                      : sort_tokens((const int32_t*)tok, n, V, g, (char*)ws, s);
+        const size_t el = gt == TDA_BF16 ? 2 : 4;
+        if (beta == 0.f && n <= kRankMax && d * el % 16 == 0 && row_align(dE, ld_e, el) == 16) {
+            clear.p = (uint4*)dE;
+            clear.rows = V;
+            clear.vecs = d * (int64_t)el / 16;
+            clear.ld = ld_e * (int64_t)el / 16;
+        }
+        cudaError_t e = it == TDA_I64 ? sort_tokens((const int64_t*)tok, n, V, g, clear, (char*)ws, s)
+                                      : sort_tokens((const int32_t*)tok, n, V, g, clear, (char*)ws, s);
         if (e != cudaSuccess) return e;
-    } else {  // no token: every row is cleared or scaled
-        g = GradLayout{};
-        g.C = 32;
     }
-#define TDA_CALL(TI, TO) sums((const TI*)dout, ld_d, V, d, n, scale, (TO*)dE, ld_e, beta, g, (char*)ws, s)
+#define TDA_CALL(TI, TO) \
+    sums((const TI*)dout, ld_d, V, d, n, scale, (TO*)dE, ld_e, beta, clear.p != nullptr, g, (char*)ws, s)
     if (dt == TDA_BF16) return gt == TDA_BF16 ? TDA_CALL(__nv_bfloat16, __nv_bfloat16) : TDA_CALL(__nv_bfloat16, float);
     return TDA_CALL(float, float);
 #undef TDA_CALL

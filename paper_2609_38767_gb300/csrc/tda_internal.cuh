@@ -254,6 +254,30 @@ cudaError_t smem_attr_once(int bytes) {
     return e;
 }
 
+// Programmatic dependent launch for the chains of short kernels inside one call: kernel i + 1 is put on the
+// SMs while kernel i still runs and waits (chain_wait) until i has finished and its writes are visible. Every
+// thread of a chained kernel waits before it touches memory, so completion carries along the chain; the first
+// kernel of a call is launched plainly. chain_next lets the next kernel come as soon as all CTAs have started.
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... Params, typename... Args>
+cudaError_t launch_chained(bool chained, void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                           Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = chained ? 1 : 0;
+    note_launches(1);
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
 template <auto Kernel>
 int max_clusters_once(const cudaLaunchConfig_t& cfg, int cs, int fallback) {
     static std::atomic<int> cache[64][3];  // 0 = not yet queried; cs 1, 2, 4
