@@ -585,7 +585,7 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  * row length, or any multiple of 8 elements that is no shorter; for any other
  * pointers or strides add TDA_LINEAR_ANY_STRIDE to op. Runs on sm_103 only.
  * An infinite or NaN element of X or W makes the outputs that it enters
- * non-finite (for fp32 layers NaN).
+ * non-finite (for fp32 layers NaN may stand where infinity would).
  * ------------------------------------------------------------------------- */
 typedef enum {
     TDA_ACT_NONE = 0,
@@ -623,7 +623,7 @@ tda_status tda_linear_backward(const tda_linear_desc* L, const void* dY, int64_t
  *   out     device, n rows of d values of E's type, row stride ld_out >= d; may
  *           not overlap E.
  * Any d, stride and element alignment; rows aligned to 16 bytes are copied in
- * 16-byte vectors. scale must be finite. V, n < 2^31.
+ * 16-byte vectors. scale must be finite. V, n < 2^31, d <= 2^22.
  * ------------------------------------------------------------------------- */
 tda_status tda_embedding_forward(tda_dtype dtype, const void* E, int64_t ld_e, int64_t V, int64_t d,
                                  tda_index_type it, const void* tokens, int64_t n, float scale, void* out,

@@ -88,6 +88,8 @@ def lib_path(name: str = "libtda.so") -> str:
 def load() -> ctypes.CDLL:
     """Load libtda.so (built by ``build.build()``); raises if it is absent."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
@@ -167,10 +169,26 @@ def _ptr(x):
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
+def _current_stream():
+    """torch's current stream on the current device, without making a Stream object where torch offers that."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        c = torch._C
+        if hasattr(c, "_cuda_getCurrentRawStream") and hasattr(c, "_cuda_getDevice"):
+            torch.cuda.current_stream()  # initialises CUDA
+            _raw_stream = lambda: c._cuda_getCurrentRawStream(c._cuda_getDevice())  # noqa: E731
+        else:
+            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    return _raw_stream()
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -26,7 +26,8 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxe
 LIBS = {
     "libtda.so": ["api.cu", "calibrate.cu", "k_project_simt.cu", "k_project_tc.cu", "k_routes.cu",
                   "k_precond.cu", "k_score.cu", "stream_host.cu", "noalloc.cu", "selftest.cu", "k_gemm_tc.cu", "k_gram_tc.cu", "k_kfac.cu", "k_tokens.cu", "k_tokens_tc.cu", "k_materialize_tc.cu",
-                  "api_train.cu", "k_embedding.cu", "k_clip.cu", "k_linear.cu", "k_linear_tc.cu"],
+                  "api_train.cu", "k_embedding.cu", "k_clip.cu", "k_linear.cu", "k_linear_tc.cu",
+                  "k_linear_rows.cu"],
     "libtda_synth.so": ["synth.cu"],
 }
 

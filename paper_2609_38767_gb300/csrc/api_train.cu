@@ -17,7 +17,7 @@ tda_status check_table(tda_dtype dtype, int64_t V, int64_t d, int32_t it, const 
                        const char* who) {
     if (!float_type(dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
     if (it != TDA_I32 && it != TDA_I64) return fail(TDA_ERR_INVALID_ARG, "%s: index type must be TDA_I32 or TDA_I64", who);
-    if (V < 1 || V > kMaxCount || d < 1 || n < 0 || n > kMaxCount)
+    if (V < 1 || V > kMaxCount || d < 1 || d > (1 << 22) || n < 0 || n > kMaxCount)
         return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes V=%lld d=%lld n=%lld", who, (long long)V, (long long)d,
                     (long long)n);
     if (!std::isfinite(scale)) return fail(TDA_ERR_INVALID_ARG, "%s: scale must be finite", who);

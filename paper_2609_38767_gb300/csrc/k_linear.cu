@@ -43,6 +43,8 @@ __device__ __forceinline__ void load8(const PackJob& j, int64_t r, int64_t c, T*
 
 template <typename T>
 __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constant__ PackJobs jobs) {
+    chain_wait();
+    chain_next();
     const PackJob& j = jobs.j[blockIdx.y];
     const int64_t per = j.ld_dst / 8, total = j.rows * per;
     for (int64_t i = (int64_t)blockIdx.x * kPackThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kPackThreads) {
@@ -103,8 +105,9 @@ __device__ __forceinline__ void set_f(float* p, float x) { *p = x; }
 __device__ __forceinline__ void set_f(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
 template <typename T, int ACT, int N>
-__global__ void __launch_bounds__(kFacThreads) factor_kernel(const __grid_constant__ FactorParams p) {
-    constexpr int U = 4;  // rows in flight
+__global__ void __launch_bounds__(kFacThreads, 4) factor_kernel(const __grid_constant__ FactorParams p) {
+    constexpr int U = 2;  // rows in flight
+    chain_next();
     const int64_t col = ((int64_t)blockIdx.x * kColLanes + threadIdx.x % kColLanes) * N;
     const int rl = threadIdx.x / kColLanes;
     const int64_t r0 = (int64_t)blockIdx.y * p.run, r1 = r0 + p.run < p.M ? r0 + p.run : p.M;
@@ -153,6 +156,8 @@ __global__ void __launch_bounds__(kFacThreads) factor_kernel(const __grid_consta
 // db[n] = beta db[n] + sum of the runs' sums, in order.
 template <typename TG>
 __global__ void bias_grad_kernel(const float* __restrict__ sums, int64_t runs, int64_t N, float beta, TG* db) {
+    chain_wait();
+    chain_next();
     const int64_t n = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (n >= N) return;
     float s = 0.f;
@@ -248,7 +253,7 @@ struct Planner {
         o.p = j.dst, o.ld = j.ld_dst, o.plane_stride = j.plane, o.planes = dt == TDA_F32 ? 3 : 1;
         return o;
     }
-    cudaError_t run(cudaStream_t s) {
+    cudaError_t run(bool chained, cudaStream_t s) {
         if (!count) return cudaSuccess;
         int64_t most = 0;
         for (int i = 0; i < count; ++i) {
@@ -256,12 +261,8 @@ struct Planner {
             if (t > most) most = t;
         }
         const dim3 grid((unsigned)(most < 152 * 16 ? most : 152 * 16), (unsigned)count);
-        note_launches(1);
-        if (dt == TDA_F32)
-            pack_kernel<float><<<grid, kPackThreads, 0, s>>>(jobs);
-        else
-            pack_kernel<__nv_bfloat16><<<grid, kPackThreads, 0, s>>>(jobs);
-        return cudaGetLastError();
+        return launch_chained(chained, dt == TDA_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, grid,
+                              dim3(kPackThreads), 0, s, jobs);
     }
 };
 
@@ -270,10 +271,10 @@ void align_epilogue(LinearEpilogue* e, tda_dtype out) {
     const size_t el = out == TDA_BF16 ? 2 : 4;
     auto all = [&](size_t bytes) {
         return rows_by(e->Y, e->ld_y, bytes, el) && rows_by(e->Z, e->ld_z, bytes, el) &&
-               rows_by(e->R, e->ld_r, bytes < 16 ? bytes : 16, el) && rows_by(e->bias, 0, bytes < 16 ? bytes : 16, el);
+               rows_by(e->R, e->ld_r, bytes, el) && rows_by(e->bias, 0, bytes, el);
     };
     e->vec = all(4 * el);
-    e->wide = all(32) ? 32 : all(16) ? 16 : 0;
+    e->wide = all(16);
 }
 
 LinearEpilogue plain_epilogue(int64_t M, int64_t N, void* Y, int64_t ld_y, tda_dtype out) {
@@ -289,8 +290,13 @@ LinearEpilogue plain_epilogue(int64_t M, int64_t N, void* Y, int64_t ld_y, tda_d
 // Scratch of a forward: planes of X and W where they need them.
 static bool needs_planes(tda_dtype dt, const void* p, int64_t ld) { return dt == TDA_F32 || !rows16(p, ld, 2); }
 
+// Rows up to which dW is written by plain rank-M updates.
+constexpr int64_t kOuterMost = 16;
+static bool few_cols(const LinearBackward& b) { return b.dt == TDA_F32 && linear_rows_preferred(b.M, b.dt); }
+
 size_t linear_forward_ws(const LinearForward& f) {
     size_t b = 0;
+    if (linear_rows_preferred(f.M, f.dt)) return 0;
     if (needs_planes(f.dt, f.X, f.ld_x)) b += plane_bytes(f.M, f.d_in, f.dt);
     if (needs_planes(f.dt, f.W, f.ld_w)) b += plane_bytes(f.d_out, f.d_in, f.dt);
     return b;
@@ -300,9 +306,10 @@ size_t linear_backward_ws(const LinearBackward& b) {
     size_t n = 0;
     const void* G = b.B ? b.B : b.dY;
     const int64_t ld_g = b.B ? b.ld_b : b.ld_dy;
-    if ((b.dX || b.dW) && needs_planes(b.dt, G, ld_g)) n += plane_bytes(b.M, b.d_out, b.dt);
-    if (b.dX && needs_planes(b.dt, b.W, b.ld_w)) n += plane_bytes(b.d_out, b.d_in, b.dt);
-    if (b.dW && needs_planes(b.dt, b.X, b.ld_x)) n += plane_bytes(b.M, b.d_in, b.dt);
+    const bool dX = b.dX && !few_cols(b), dW = b.dW && b.M > kOuterMost;
+    if ((dX || dW) && needs_planes(b.dt, G, ld_g)) n += plane_bytes(b.M, b.d_out, b.dt);
+    if (dX && needs_planes(b.dt, b.W, b.ld_w)) n += plane_bytes(b.d_out, b.d_in, b.dt);
+    if (dW && needs_planes(b.dt, b.X, b.ld_x)) n += plane_bytes(b.M, b.d_in, b.dt);
     if (b.db) {
         const int64_t run = factor_run(b.M, b.d_out);
         n += up256(sizeof(float) * (size_t)((b.M + run - 1) / run) * (size_t)b.d_out);
@@ -320,20 +327,21 @@ size_t linear_ws_bound(bool backward, int64_t M, int64_t d_in, int64_t d_out, td
 }
 
 cudaError_t launch_linear_forward(const LinearForward& f, void* ws, unsigned int* err, cudaStream_t s) {
-    Planner pl;
-    pl.dt = f.dt;
-    pl.ws = (char*)ws;
-    const LinearOperand X = pl.add(f.X, f.M, f.d_in, f.ld_x), W = pl.add(f.W, f.d_out, f.d_in, f.ld_w);
-    cudaError_t e = pl.run(s);
-    if (e != cudaSuccess) return e;
     LinearEpilogue ep = plain_epilogue(f.M, f.d_out, f.Y, f.ld_y, f.dt);
     ep.bias = f.bias;
     ep.R = f.R, ep.ld_r = f.ld_r, ep.r_scale = 1.f;
     ep.Z = f.Z, ep.ld_z = f.ld_z;
     ep.act = f.act;
     align_epilogue(&ep, f.dt);
+    if (linear_rows_preferred(f.M, f.dt)) return launch_linear_rows(f.X, f.ld_x, f.W, f.ld_w, f.d_in, ep, f.dt, s);
+    Planner pl;
+    pl.dt = f.dt;
+    pl.ws = (char*)ws;
+    const LinearOperand X = pl.add(f.X, f.M, f.d_in, f.ld_x), W = pl.add(f.W, f.d_out, f.d_in, f.ld_w);
+    cudaError_t e = pl.run(false, s);
+    if (e != cudaSuccess) return e;
     const LinearProduct pr = {X, W, ep, f.dt};
-    return launch_linear_products(&pr, 1, err, s);
+    return launch_linear_products(&pr, 1, pl.count > 0, err, s);
 }
 
 cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned int* err, cudaStream_t s) {
@@ -354,29 +362,45 @@ cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned i
         e = b.dt == TDA_BF16 ? launch_factor<__nv_bfloat16>(b.act, p, s) : launch_factor<float>(b.act, p, s);
         if (e != cudaSuccess) return e;
     }
+    bool chained = b.B || b.db;
     if (b.db) {
-        const unsigned grid = (unsigned)((b.d_out + 127) / 128);
-        note_launches(1);
-        if (b.gt == TDA_BF16)
-            bias_grad_kernel<<<grid, 128, 0, s>>>(sums, runs, b.d_out, b.beta, (__nv_bfloat16*)b.db);
-        else
-            bias_grad_kernel<<<grid, 128, 0, s>>>(sums, runs, b.d_out, b.beta, (float*)b.db);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        const dim3 grid((unsigned)((b.d_out + 127) / 128));
+        e = b.gt == TDA_BF16 ? launch_chained(true, bias_grad_kernel<__nv_bfloat16>, grid, dim3(128), 0, s,
+                                              (const float*)sums, runs, b.d_out, b.beta, (__nv_bfloat16*)b.db)
+                             : launch_chained(true, bias_grad_kernel<float>, grid, dim3(128), 0, s, (const float*)sums,
+                                              runs, b.d_out, b.beta, (float*)b.db);
+        if (e != cudaSuccess) return e;
     }
-    if (!b.dX && !b.dW) return cudaSuccess;
+    // few rows: dW (and dX of fp32 layers) read their operands as they are
+    const void* F = b.B ? b.B : b.dY;
+    const int64_t ld_f = b.B ? b.ld_b : b.ld_dy;
+    const bool outer = b.dW && b.M <= kOuterMost, few = b.dX && few_cols(b);
+    if (few) {
+        e = launch_linear_cols((const float*)F, ld_f, (const float*)b.W, b.ld_w, (float*)b.dX, b.ld_dx, b.M, b.d_out, b.d_in,
+                               chained, s);
+        if (e != cudaSuccess) return e;
+        chained = true;
+    }
+    if (outer) {
+        e = launch_linear_outer(F, ld_f, b.X, b.ld_x, b.M, b.d_out, b.d_in, b.dt, b.dW, b.ld_dw, b.gt, b.beta, chained, s);
+        if (e != cudaSuccess) return e;
+        chained = true;
+    }
+    const bool dX = b.dX && !few, dW = b.dW && !outer;
+    if (!dX && !dW) return cudaSuccess;
     // the products read the factor as it is stored: B, or dY itself without an activation
     const LinearOperand G = b.B ? pl.add(b.B, b.M, b.d_out, b.ld_b) : pl.add(b.dY, b.M, b.d_out, b.ld_dy);
     LinearOperand W = {}, X = {};
-    if (b.dX) W = pl.add(b.W, b.d_out, b.d_in, b.ld_w);
-    if (b.dW) X = pl.add(b.X, b.M, b.d_in, b.ld_x);
-    if ((e = pl.run(s)) != cudaSuccess) return e;
+    if (dX) W = pl.add(b.W, b.d_out, b.d_in, b.ld_w);
+    if (dW) X = pl.add(b.X, b.M, b.d_in, b.ld_x);
+    if ((e = pl.run(chained, s)) != cudaSuccess) return e;
     LinearProduct pr[2];
     int count = 0;
-    if (b.dX) {
+    if (dX) {
         W.mn = true;  // the contraction runs over W's rows
         pr[count++] = {G, W, plain_epilogue(b.M, b.d_in, b.dX, b.ld_dx, b.dt), b.dt};
     }
-    if (b.dW) {
+    if (dW) {
         LinearOperand Gt = G;
         Gt.mn = X.mn = true;  // over the tokens
         LinearEpilogue ep = plain_epilogue(b.d_out, b.d_in, b.dW, b.ld_dw, b.gt);
@@ -384,7 +408,7 @@ cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned i
         align_epilogue(&ep, b.gt);
         pr[count++] = {Gt, X, ep, b.gt};
     }
-    return launch_linear_products(pr, count, err, s);
+    return launch_linear_products(pr, count, chained || pl.count > 0, err, s);
 }
 
 // beta x for an empty batch.

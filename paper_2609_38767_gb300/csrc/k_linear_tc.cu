@@ -14,7 +14,7 @@
 // linear_pair_kernel, for products with a tile for most SM pairs: two CTAs of a
 // cluster hold one 256 x BN tile (cta_group::2), each staging 128 rows of P and half
 // of Q, so an operand byte that reaches an SM feeds twice the MMAs; persistent, the
-// epilogue of a tile beside the next tile's MMAs.
+// epilogue of a tile beside the next tile's MMAs, its outputs by TMA.
 //
 // linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a decoded token, a
 // short batch) swap the operands, so the long side fills the 128 rows of a tile,
@@ -185,35 +185,46 @@ __device__ __forceinline__ void finish(const LinearEpilogue& e, const int64_t* m
         if (whole[u]) st4((T*)e.Y + m[u] * e.ld_y + n[u], v[u]);
 }
 
-// 32 values of one row of a tensor, as they are in memory.
-template <typename T>
-struct Row32 {
-    using Type = T;
-    static constexpr int kVecs = sizeof(T) * 32 / 16;
-    uint4 q[kVecs];
-    __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) q[i] = *reinterpret_cast<const uint4*>(p + i * (16 / sizeof(T)));
-    }
-    __device__ __forceinline__ float get(int i) const {  // i known at compile time
-        const uint4& x = q[i * sizeof(T) / 16];
-        const int w = sizeof(T) == 4 ? i & 3 : (i >> 1) & 3;
-        const uint32_t b = w == 0 ? x.x : w == 1 ? x.y : w == 2 ? x.z : x.w;
-        return __uint_as_float(sizeof(T) == 4 ? b : i & 1 ? b & 0xFFFF0000u : b << 16);
-    }
-};
-__device__ __forceinline__ void st_32b(void* p, const uint32_t* w) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+// ---- units of 32 rows x 64 bytes, the grain of the pair kernel's outputs
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* tm, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"((uint64_t)tm),
+                 "r"(c0), "r"(c1), "r"(src)
                  : "memory");
 }
-// One sector of a row (16 bf16 or 8 fp32 values from v on): a whole 32-byte store, or two of 16 bytes where rows
-// start between sectors.
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// 16-byte piece j of row r in a unit's shared memory: the 64-byte swizzle, conflict-free by rows and by pieces.
+__device__ __forceinline__ uint32_t unit_at(int r, int j) { return (uint32_t)(r * 64 + ((j ^ ((r >> 1) & 3)) << 4)); }
+
+// Piece of 16 bytes of a row, n its first column: whole, or value by value at the matrix's edge.
 template <typename T>
-__device__ __forceinline__ void store_sector(T* p, const float* v, bool sectors) {
-    uint32_t w[8];
+__device__ __forceinline__ uint4 load_piece(const T* row, int64_t n, int64_t N) {
+    constexpr int E = 16 / sizeof(T);
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (n + E <= N) {
+        q = *reinterpret_cast<const uint4*>(row + n);
+    } else if (n < N) {
+        T x[E];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+        for (int i = 0; i < E; ++i) x[i] = n + i < N ? row[n + i] : T(0.f);
+        q = *reinterpret_cast<const uint4*>(x);
+    }
+    return q;
+}
+template <typename T>
+__device__ __forceinline__ float piece_get(const uint4& x, int i) {  // i known at compile time
+    const int w = sizeof(T) == 4 ? i : i >> 1;
+    const uint32_t b = w == 0 ? x.x : w == 1 ? x.y : w == 2 ? x.z : x.w;
+    return __uint_as_float(sizeof(T) == 4 ? b : i & 1 ? b & 0xFFFF0000u : b << 16);
+}
+template <typename T>
+__device__ __forceinline__ uint4 piece_of(const float* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
         if constexpr (sizeof(T) == 4) {
             w[j] = __float_as_uint(v[j]);
         } else {
@@ -221,37 +232,7 @@ __device__ __forceinline__ void store_sector(T* p, const float* v, bool sectors)
             w[j] = *reinterpret_cast<const uint32_t*>(&h);
         }
     }
-    if (sectors) {
-        st_32b(p, w);
-    } else {
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        *reinterpret_cast<uint4*>(p + 16 / sizeof(T)) = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-}
-
-// A row of 32 sums through the epilogue and out, a sector at a time. PLAIN: no bias, Z or activation.
-template <typename T, bool PLAIN>
-__device__ __forceinline__ void finish_row32(const LinearEpilogue& e, int64_t m, int64_t n, float* v,
-                                             const Row32<T>& r) {
-    constexpr int kPer = 32 / sizeof(T);
-    if (!PLAIN && e.bias) {
-        Row32<T> b;  // the same addresses in every lane
-        b.load((const T*)e.bias + n);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] += b.get(i);
-    }
-#pragma unroll
-    for (int i = 0; i < 32; i += kPer) {
-        if (!PLAIN) {
-            if (e.Z && m < e.M) store_sector((T*)e.Z + m * e.ld_z + n + i, v + i, e.wide == 32);
-#pragma unroll
-            for (int j = 0; j < kPer; j += 8) activate<T, 2>(e.act, reinterpret_cast<float(*)[4]>(v + i + j));
-        }
-        if (e.R)
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) v[i + j] = fmaf(e.r_scale, r.get(i + j), v[i + j]);
-        if (m < e.M) store_sector((T*)e.Y + m * e.ld_y + n + i, v + i, e.wide == 32);
-    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
@@ -313,6 +294,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    chain_wait();
+    chain_next();
 
     const int64_t tile = blockIdx.x / p.split;
     const int rank = blockIdx.x % p.split;
@@ -546,21 +529,38 @@ struct PairShape {
     static constexpr int kPlanes = ROUND ? 3 : 1;
     static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN / 2 * kTK * 2, kStage = kPlanes * (kP + kQ);
     static constexpr int kStages = ROUND ? 2 : 6;
-    static constexpr uint32_t kBlockLd = 20;  // floats of a staged row: 16 + 4, conflict-free 16-byte accesses
-    static constexpr uint32_t kBlock = 32 * kBlockLd * 4;
+    static constexpr uint32_t kUnit = 32 * 64;       // one output unit
+    static constexpr uint32_t kBlock = 2 * kUnit;    // two per epilogue warp
+    static constexpr uint32_t kBlockLd = 20;         // floats of a row staged for edges: 16 + 4
+    static_assert(32 * kBlockLd * 4 <= kBlock, "edge staging");
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kEpiWarps * kBlock + 8 * (2 * kStages + 5) + 16;
     static constexpr uint32_t kCols = 512;  // the SM's whole TMEM: both CTAs' columns start at the same place
     static_assert(kSmem <= 232448, "shared memory per CTA");
 };
 
-// One or two products (dX and dW of a layer) in one launch: their tiles form one list, those with the longer
-// K loop first, so that the short ones fill the last round.
+// One or two products (dX and dW of a layer) in one launch, the one with the longer K loop first. Its tiles go
+// round the pairs; where the last round is short, the pairs left out take `extra` tiles of the second product
+// each (about as long as one of the first) before the rest of those goes round all pairs.
 struct PairParams {
     TileParams g[2];
     CUtensorMap tmP[2], tmQ[2];
+    CUtensorMap tmY[2], tmZ;  // outputs with 16-byte aligned rows; tmZ: of product 0
     int64_t tiles[2];  // tiles[1] = 0: one product
+    int extra;
     unsigned int* err;
 };
+
+// The j-th tile of product g for pair i of n; >= pp.tiles[g]: there is none.
+template <int g>
+__device__ __forceinline__ int64_t pair_tile(const PairParams& pp, int64_t i, int64_t n, int64_t j) {
+    if (g == 0) return i + j * n;
+    const int64_t rem = pp.tiles[0] % n, idle = n - rem;  // pairs rem .. n - 1 have one tile less of product 0
+    if (i >= rem) {
+        if (j < pp.extra) return i - rem + j * idle;
+        j -= pp.extra;
+    }
+    return pp.extra * idle + (i >= rem ? i - rem : i + idle) + j * n;
+}
 
 template <int BN, bool ROUND>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ PairParams pp) {
@@ -599,8 +599,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     cluster_sync();  // both CTAs' barriers exist before either signals the other's
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    chain_wait();
+    chain_next();
 
-    const int64_t units = pp.tiles[0] + pp.tiles[1], u0 = blockIdx.x >> 1, du = gridDim.x >> 1;
+    const int64_t me = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     // A product's tiles go in bands of 8 tile rows, down each column of a band: the
     // pairs at work share operand rows in L2.
     // Each role runs its loop once per product, with that product's parameters at fixed places of the constant
@@ -618,16 +620,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             uint32_t ring = 0, last_par[S::kStages];
             bool issued[S::kStages], ok = true;
             for (int s = 0; s < S::kStages; ++s) issued[s] = false;
-            int64_t u = u0;
             auto feed = [&](auto G) {
               constexpr int g = decltype(G)::value;
               const TileParams& p = pp.g[g];
               const CUtensorMap *tmP = &pp.tmP[g], *tmQ = &pp.tmQ[g];
               const int total = p.nk;
-              const int64_t end = g ? units : pp.tiles[0], base = g ? pp.tiles[0] : 0;
-              for (; ok && u < end; u += du) {
+              for (int64_t j = 0, u; ok && (u = pair_tile<g>(pp, me, pairs, j)) < pp.tiles[g]; ++j) {
                 int64_t i0, j0;
-                place(p, u - base, &i0, &j0);
+                place(p, u, &i0, &j0);
                 const int pr = (int)i0 + (int)rank * kTM, qr = (int)j0 + (int)rank * (BN / 2);
                 for (int t = 0; t < total; ++t, ++ring) {
                     const int s = ring % S::kStages;
@@ -678,7 +678,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             // ---------------- MMA issuer of the pair
             uint32_t ring = 0, use = 0;
             bool ok = true;
-            int64_t u = u0;
             auto issue = [&](auto G) {
               constexpr int g = decltype(G)::value;
               const TileParams& p = pp.g[g];
@@ -686,8 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
               const uint32_t idesc = idesc_bf16(2 * kTM, BN) | (p_mn ? 1u << 15 : 0u) | (q_mn ? 1u << 16 : 0u);
               const uint64_t sp = desc_step(p_mn), sq = desc_step(q_mn);
               const int total = p.nk, windows = ROUND ? total : 1;  // accumulator fills of a tile
-              const int64_t last = g ? units : pp.tiles[0];
-              for (; ok && u < last; u += du) {
+              for (int64_t j = 0; ok && pair_tile<g>(pp, me, pairs, j) < pp.tiles[g]; ++j) {
                 int t = 0;
                 for (int w = 0; ok && w < windows; ++w, ++use) {
                     const uint32_t b = use & 1u;
@@ -756,6 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         // 16 columns of this warp's 32 rows, held a row a lane, through shared memory: edges and rows that are not
         // aligned go out a few values at a time, neighbours by neighbouring lanes
         auto out = [&](const LinearEpilogue& ep, const float* v, int64_t m0, int64_t n0) {
+            if (lane == 0) bulk_wait_read0();
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
@@ -773,57 +772,109 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     finish<__nv_bfloat16, 1, true>(ep, m, n, ok, y);
             }
         };
-        // 32 columns, a row a lane, straight from registers; r: the residual's row, loaded ahead
-        auto load_r = [&](auto& r, const LinearEpilogue& ep, int64_t m, int64_t n) {
-            using T = typename std::remove_reference<decltype(r)>::type::Type;
-            if (ep.R && m < ep.M && n + 32 <= ep.N) r.load((const T*)ep.R + m * ep.ld_r + n);
-        };
         bool got = true;
-        int64_t u = u0;
         auto drain = [&](auto G) {
           constexpr int g = decltype(G)::value;
           const TileParams& p = pp.g[g];
-          const int64_t end = g ? units : pp.tiles[0], base = g ? pp.tiles[0] : 0;
-          for (; got && u < end; u += du) {
+          for (int64_t j = 0, u; got && (u = pair_tile<g>(pp, me, pairs, j)) < pp.tiles[g]; ++j) {
             int64_t i0, j0;
-            place(p, u - base, &i0, &j0);
+            place(p, u, &i0, &j0);
             const int64_t m0 = i0 + rank * kTM + q * 32, n0 = j0 + half * kC;
-            // 32 columns from n0 + c on, read by `get` into v[8][4]
-            auto column_blocks = [&](auto zero, auto get) {
+            // This warp's rows and columns, a unit at a time: the row in registers (from `get`) through the epilogue
+            // into shared memory, and out by TMA, which clips it at the matrix's edges. The residual's unit is
+            // loaded 8 rows an access, one unit ahead, and handed to the rows' lanes through shared memory.
+            auto column_units = [&](auto zero, auto get) {
                 using T = decltype(zero);
-                const int64_t m = m0 + lane;
-                Row32<T> r;
-                if (p.ep.wide) load_r(r, p.ep, m, n0);
-                if (!ROUND && !(got = wait_for())) return;
+                constexpr int kU = 64 / sizeof(T), E = 16 / sizeof(T);
                 // fp32 outputs of bf16 products are gradients: nothing but beta times themselves is added
                 constexpr bool kPlain = g == 1 || (!ROUND && sizeof(T) == 4);
-                auto block = [&](int c) {
-                    const int64_t n = n0 + c;
-                    float v[32];
-                    get(c, v);
-                    if (p.ep.wide && n + 32 <= p.ep.N) {
-                        finish_row32<T, kPlain>(p.ep, m, n, v, r);
-                        if (c + 32 < kC) load_r(r, p.ep, m, n + 32);
-                    } else {
-                        out(p.ep, v, m0, n);
-                        out(p.ep, v + 16, m0, n + 16);
+                const bool has_r = p.ep.R != nullptr && p.ep.wide;
+                uint4 r[4];
+                auto load_r = [&](int64_t n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t m = m0 + i * 8 + (lane >> 2);
+                        if (m < p.ep.M) r[i] = load_piece((const T*)p.ep.R + m * p.ep.ld_r, n + (lane & 3) * E, p.ep.N);
                     }
                 };
-                if (ROUND) {
+                uint32_t which = 0;
+                // a unit that may be written: all but the last store have read theirs
+                auto take = [&]() {
+                    if (lane == 0) bulk_wait_read1();
+                    __syncwarp();
+                    which ^= 1;
+                    return blocks + (warp - 2) * S::kBlock + which * S::kUnit;
+                };
+                auto send = [&](const CUtensorMap* tm, uint8_t* unit, const float* v, int64_t n) {
 #pragma unroll
-                    for (int c = 0; c < kC; c += 32) block(c);  // the sums are registers
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<uint4*>(unit + unit_at(lane, j)) = piece_of<T>(v + j * E);
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (m0 < p.ep.M && n < p.ep.N) tma_store_2d(tm, smem_u32(unit), (int)n, (int)m0);
+                        bulk_commit();
+                    }
+                };
+                auto unit = [&](int c) {
+                    const int64_t n = n0 + c;
+                    float v[kU];
+                    get(c, v);
+                    if (!kPlain && p.ep.bias) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {  // the same addresses in every lane
+                            const uint4 b = load_piece((const T*)p.ep.bias, n + j * E, p.ep.N);
+#pragma unroll
+                            for (int i = 0; i < E; ++i) v[j * E + i] += piece_get<T>(b, i);
+                        }
+                    }
+                    if (!kPlain && p.ep.Z) send(&pp.tmZ, take(), v, n);
+                    uint8_t* y = take();
+                    if (!kPlain)
+#pragma unroll
+                        for (int j = 0; j < kU; j += 8) activate<T, 2>(p.ep.act, reinterpret_cast<float(*)[4]>(v + j));
+                    if (has_r) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<uint4*>(y + unit_at(i * 8 + (lane >> 2), lane & 3)) = r[i];
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(y + unit_at(lane, j));
+#pragma unroll
+                            for (int i = 0; i < E; ++i)
+                                v[j * E + i] = fmaf(p.ep.r_scale, piece_get<T>(x, i), v[j * E + i]);
+                        }
+                        if (c + kU < kC) load_r(n + kU);
+                        __syncwarp();  // every row has been read before its lane's outputs take the place
+                    }
+                    send(&pp.tmY[g], y, v, n);
+                };
+                if (has_r) load_r(n0);
+                if (!ROUND && !(got = wait_for())) return;
+                if (!p.ep.wide) {
+#pragma unroll
+                    for (int c = 0; c < kC; c += kU) {
+                        float v[kU];
+                        get(c, v);
+#pragma unroll
+                        for (int i = 0; i < kU; i += 16) out(p.ep, v + i, m0, n0 + c + i);
+                    }
+                } else if (ROUND) {
+#pragma unroll
+                    for (int c = 0; c < kC; c += kU) unit(c);  // the sums are registers
                 } else {
 #pragma unroll 1
-                    for (int c = 0; c < kC; c += 32) block(c);
-                    release();
+                    for (int c = 0; c < kC; c += kU) unit(c);
                 }
+                if (!ROUND) release();
             };
             if (!ROUND) {
-                auto get = [&](int c, float* v) { tmem_ld32(tb + (use & 1u) * BN + c, v); };
+                const uint32_t at = tb + (use & 1u) * BN;
                 if (p.ep.f32)
-                    column_blocks(float(), get);
+                    column_units(float(), [&](int c, float* v) { tmem_ld16(at + c, v); });
                 else
-                    column_blocks(__nv_bfloat16(), get);
+                    column_units(__nv_bfloat16(), [&](int c, float* v) { tmem_ld32(at + c, v); });
             } else {
                 float acc[kC];
 #pragma unroll
@@ -841,15 +892,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     release();
                 }
                 if (!got) break;
-                column_blocks(float(), [&](int c, float* v) {
+                column_units(float(), [&](int c, float* v) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = acc[c + i];
+                    for (int i = 0; i < 16; ++i) v[i] = acc[c + i];
                 });
             }
           }
         };
         drain(std::integral_constant<int, 0>());
         drain(std::integral_constant<int, 1>());
+        if (lane == 0) bulk_wait_all();  // the outputs are written before the CTA exits
     }
     __syncwarp();
     tc_fence_before();
@@ -893,6 +945,20 @@ bool make_map(CUtensorMap* tm, const LinearOperand& o, int box_rows) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 2-D map over an output's rows: boxes of 64 bytes x 32 rows, 64-byte swizzle.
+bool make_out_map(CUtensorMap* tm, void* p, int64_t rows, int64_t cols, int64_t ld, bool f32) {
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    const int el = f32 ? 4 : 2;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)(ld * el)};
+    cuuint32_t box[2] = {(cuuint32_t)(64 / el), 32};
+    cuuint32_t estr[2] = {1, 1};
+    return enc(tm, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, box,
+               estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int sm_count() {
     static std::atomic<int> sms{0};
     int v = sms.load(std::memory_order_relaxed);
@@ -906,8 +972,17 @@ int sm_count() {
     return v;
 }
 
+// The cluster's size, and (second) a chained launch.
+void cluster_attributes(cudaLaunchAttribute* at, int size) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)size;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+}
+
 template <typename T, int BN, bool ROUND>
-cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, cudaStream_t s) {
+cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, bool chained, cudaStream_t s) {
     using S = TileShape<BN, ROUND>;
     CUtensorMap mP, mQ;
     if (!make_map(&mP, P, P.mn ? kTK : kTM) || !make_map(&mQ, Q, Q.mn ? kTK : BN)) return cudaErrorInvalidValue;
@@ -927,12 +1002,10 @@ cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams&
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)p.split;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    cluster_attributes(at, p.split);
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = chained ? 2 : 1;
     note_launches(1);
     return cudaLaunchKernelEx(&cfg, linear_tile_kernel<T, BN, ROUND>, mP, mQ, p);
 }
@@ -944,13 +1017,17 @@ struct Product {
 };
 
 template <int BN, bool ROUND>
-cudaError_t run_pair(const Product* const* pr, int count, cudaStream_t s) {
+cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStream_t s) {
     using S = PairShape<BN, ROUND>;
-    PairParams pp;
+    PairParams pp = {};
     pp.tiles[0] = pp.tiles[1] = 0;
     for (int i = 0; i < count; ++i) {
         const Product& x = *pr[i];
         if (!make_map(&pp.tmP[i], x.P, x.P.mn ? kTK : kTM) || !make_map(&pp.tmQ[i], x.Q, x.Q.mn ? kTK : BN / 2))
+            return cudaErrorInvalidValue;
+        const LinearEpilogue& e = x.p.ep;
+        if (e.wide && (!make_out_map(&pp.tmY[i], e.Y, e.M, e.N, e.ld_y, e.f32) ||
+                       (e.Z && !make_out_map(&pp.tmZ, e.Z, e.M, e.N, e.ld_z, e.f32))))
             return cudaErrorInvalidValue;
         pp.g[i] = x.p;
         pp.g[i].tiles_p = (x.P.extent() + 2 * kTM - 1) / (2 * kTM);
@@ -962,32 +1039,33 @@ cudaError_t run_pair(const Product* const* pr, int count, cudaStream_t s) {
         pp.tmP[1] = pp.tmP[0], pp.tmQ[1] = pp.tmQ[0];
     }
     pp.err = pr[0]->p.err;
+    // a tile costs its K loop and about two chunks of set-up
+    pp.extra = count == 2 ? (pp.g[0].nk + 2 + (pp.g[1].nk + 2) / 2) / (pp.g[1].nk + 2) : 0;
     cudaError_t e = smem_attr_once<linear_pair_kernel<BN, ROUND>>((int)S::kSmem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    cluster_attributes(at, 2);
     cfg.attrs = at;
     cfg.numAttrs = 1;
     cfg.gridDim = dim3(2);
     const int64_t most = max_clusters_once<linear_pair_kernel<BN, ROUND>>(cfg, 2, sm_count() / 2);
     const int64_t tiles = pp.tiles[0] + pp.tiles[1];
     cfg.gridDim = dim3((unsigned)(2 * (tiles < most ? tiles : most)));
+    cfg.numAttrs = chained ? 2 : 1;
     note_launches(1);
     return cudaLaunchKernelEx(&cfg, linear_pair_kernel<BN, ROUND>, pp);
 }
 
 template <typename T, bool ROUND>
-cudaError_t pick_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, cudaStream_t s) {
+cudaError_t pick_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, bool chained, cudaStream_t s) {
     const int64_t q = Q.extent();
-    if (q <= 32 && !Q.mn) return run_tile<T, 32, ROUND>(P, Q, p, s);
-    if (q <= 64) return run_tile<T, 64, ROUND>(P, Q, p, s);
-    return run_tile<T, 128, ROUND>(P, Q, p, s);
+    if (q <= 32 && !Q.mn) return run_tile<T, 32, ROUND>(P, Q, p, chained, s);
+    if (q <= 64) return run_tile<T, 64, ROUND>(P, Q, p, chained, s);
+    return run_tile<T, 128, ROUND>(P, Q, p, chained, s);
 }
 
 }  // namespace
@@ -1026,7 +1104,8 @@ static int64_t pair_tiles(const Product& x) {
     return x.p.swap ? 0 : ((x.P.extent() + 2 * kTM - 1) / (2 * kTM)) * ((x.Q.extent() + bn - 1) / bn);
 }
 
-cudaError_t launch_linear_products(const LinearProduct* x, int count, unsigned int* err, cudaStream_t s) {
+cudaError_t launch_linear_products(const LinearProduct* x, int count, bool chained, unsigned int* err,
+                                   cudaStream_t s) {
     Product r[2];
     const Product* order[2];
     int64_t tiles = 0;
@@ -1040,18 +1119,18 @@ cudaError_t launch_linear_products(const LinearProduct* x, int count, unsigned i
     // a pair's tile for at least half of the SM pairs
     if (tiles * 4 >= sm_count()) {
         if (count == 2 && r[1].p.nk > r[0].p.nk) order[0] = &r[1], order[1] = &r[0];
-        return round ? run_pair<128, true>(order, count, s) : run_pair<256, false>(order, count, s);
+        return round ? run_pair<128, true>(order, count, chained, s) : run_pair<256, false>(order, count, chained, s);
     }
-    for (int i = 0; i < count; ++i) {
+    for (int i = 0; i < count; ++i, chained = true) {
         if (count == 2 && pair_tiles(r[i]) * 4 >= sm_count()) {  // the other one has a short side
             const Product* one = &r[i];
-            cudaError_t e = round ? run_pair<128, true>(&one, 1, s) : run_pair<256, false>(&one, 1, s);
+            cudaError_t e = round ? run_pair<128, true>(&one, 1, chained, s) : run_pair<256, false>(&one, 1, chained, s);
             if (e != cudaSuccess) return e;
             continue;
         }
-        cudaError_t e = r[i].out == TDA_BF16 ? pick_tile<__nv_bfloat16, false>(r[i].P, r[i].Q, r[i].p, s)
-                        : round              ? pick_tile<float, true>(r[i].P, r[i].Q, r[i].p, s)
-                                             : pick_tile<float, false>(r[i].P, r[i].Q, r[i].p, s);
+        cudaError_t e = r[i].out == TDA_BF16 ? pick_tile<__nv_bfloat16, false>(r[i].P, r[i].Q, r[i].p, chained, s)
+                        : round              ? pick_tile<float, true>(r[i].P, r[i].Q, r[i].p, chained, s)
+                                             : pick_tile<float, false>(r[i].P, r[i].Q, r[i].p, chained, s);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

@@ -104,7 +104,7 @@ struct LinearEpilogue {
     int64_t ld_z;
     int act;
     int vec;  // all of bias, R, Y, Z may be moved four values at a time
-    int wide; // all of them by 16 bytes (16), Y and Z also by 32-byte sectors (32); else 0
+    int wide; // rows of all of them start on 16 bytes
     int f32;  // type of bias, R, Y, Z (set by the launch)
 };
 
@@ -142,6 +142,18 @@ struct LinearProduct {
     LinearEpilogue ep;
     tda_dtype out;
 };
-cudaError_t launch_linear_products(const LinearProduct* x, int count, unsigned int* err, cudaStream_t s);
+// A few rows on the CUDA cores (k_linear_rows.cu): the forward product with its epilogue, and dX of fp32 layers.
+bool linear_rows_preferred(int64_t M, tda_dtype dt);
+cudaError_t launch_linear_rows(const void* X, int64_t ld_x, const void* W, int64_t ld_w, int64_t K,
+                               const LinearEpilogue& ep, tda_dtype dt, cudaStream_t s);
+cudaError_t launch_linear_cols(const float* B, int64_t ld_b, const float* W, int64_t ld_w, float* dX, int64_t ld_dx,
+                               int64_t M, int64_t N, int64_t K, bool chained, cudaStream_t s);
+// chained: after another kernel of the same call.
+// dW of a few rows: rank-M updates on the CUDA cores.
+cudaError_t launch_linear_outer(const void* B, int64_t ld_b, const void* X, int64_t ld_x, int64_t M, int64_t N, int64_t K,
+                                tda_dtype dt, void* dW, int64_t ld_dw, tda_dtype gt, float beta, bool chained,
+                                cudaStream_t s);
+cudaError_t launch_linear_products(const LinearProduct* x, int count, bool chained, unsigned int* err,
+                                   cudaStream_t s);
 
 }  // namespace tda

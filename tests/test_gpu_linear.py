@@ -88,7 +88,9 @@ SHAPES = [
     (33, 72, 1001, 3, 2), (64, 1024, 640, 0, 0), (65, 136, 65, 0, 0), (127, 129, 131, 0, 0), (128, 256, 128, 0, 0),
     (129, 264, 264, 24, 0), (200, 1000, 1363, 0, 0), (256, 4096, 512, 0, 0), (257, 4096, 64, 0, 0),
     (300, 5, 3, 0, 0), (513, 640, 1, 0, 0), (1000, 1, 700, 0, 0), (1024, 520, 776, 1, 0), (2047, 256, 256, 0, 0),
-    (2500, 384, 2056, 64, 8), (1500, 1800, 2104, 8, 8), (1601, 1803, 2101, 3, 1),
+    (2500, 384, 2056, 64, 8), (4, 4104, 520, 8, 8), (4, 131, 600, 1, 1), (5, 264, 1000, 0, 0),
+    (12, 1003, 301, 2, 0), (16, 4100, 3000, 4, 4), (2, 5000, 64, 0, 0),
+    (1500, 1800, 2104, 8, 8), (1601, 1803, 2101, 3, 1),
 ]
 
 

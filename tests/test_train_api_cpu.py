@@ -102,7 +102,7 @@ def test_linear_descriptor_and_workspace():
 
 
 def test_linear_forward_refusals():
-    def fwd(L=None, X=256, ld_x=64, M=4, W=256, ld_w=64, bias=None, R=None, ld_r=32, Y=256, ld_y=32, Z=None, ld_z=32,
+    def fwd(L=None, X=256, ld_x=64, M=40, W=256, ld_w=64, bias=None, R=None, ld_r=32, Y=256, ld_y=32, Z=None, ld_z=32,
             ws=None, wsb=0):
         return err(tda.tda_linear_forward, L or layer(), X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, wsb)
 
@@ -112,7 +112,7 @@ def test_linear_forward_refusals():
               dict(ld_x=1 << 40)):
         assert fwd(**k) == BAD, k
     f32 = layer(dtype=tda.TDA_F32)
-    need = tda.tda_linear_workspace_size(tda.TDA_LINEAR_FORWARD, f32, 4)
+    need = tda.tda_linear_workspace_size(tda.TDA_LINEAR_FORWARD, f32, 40)
     assert fwd(L=f32, ws=256, wsb=need - 1) == WORKSPACE and fwd(L=f32) == WORKSPACE
     assert fwd(L=f32, ws=264, wsb=need) == BAD
     assert fwd(ld_x=65) == WORKSPACE  # rows off 16 bytes need a copy
