@@ -830,9 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     }
                     if (!kPlain && p.ep.Z) send(&pp.tmZ, take(), v, n);
                     uint8_t* y = take();
-                    if (!kPlain)
-#pragma unroll
-                        for (int j = 0; j < kU; j += 8) activate<T, 2>(p.ep.act, reinterpret_cast<float(*)[4]>(v + j));
+                    if (!kPlain) activate<T, kU / 4>(p.ep.act, reinterpret_cast<float(*)[4]>(v));
                     if (has_r) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
