@@ -37,8 +37,14 @@ namespace {
 #include "tc_ptx.cuh"
 
 constexpr int kThreads = 320, kEpiWarps = 8;
-constexpr int kTM = 128, kTK = 64;
-constexpr uint32_t kBox = 64 * kTK * 2;  // one 64 x 64 MN-major box: 8 KiB
+constexpr int kTM = 128;
+constexpr int kTK = 64;                  // values of k per chunk
+constexpr uint32_t kBox = 64 * kTK * 2;  // one MN-major box of 64 values: 8 KiB
+
+// Accumulators in TMEM. Handing one to the epilogue and back takes about 1.6 us, several times the MMAs of a
+// stage of fp32 planes, each of which fills one.
+template <bool ROUND>
+constexpr int kAcc = ROUND ? 4 : 2;
 
 struct TileParams {
     LinearEpilogue ep;
@@ -50,12 +56,16 @@ struct TileParams {
     unsigned int* err;
 };
 
-// Planes of P and Q of the t-th product of fp32 operands.
-__device__ __forceinline__ constexpr int plane_p(int t) { return (0x001102 >> (4 * t)) & 15; }
-__device__ __forceinline__ constexpr int plane_q(int t) { return (0x010120 >> (4 * t)) & 15; }
+// fp32 operands: each plane of a chunk is a stage of its own, loaded in the order 0, 2, 1. The products
+// P2 Q0, P0 Q2 free plane 2's stage, then P1 Q1, P1 Q0, P0 Q1 plane 1's, then P0 Q0: smallest first, and the
+// next chunk's loads run through all of them. (Stages of all three planes left room for two, which did
+// not cover the loads: 1.43 us a chunk of 256 x 128 tiles against the figure below.)
+__device__ __forceinline__ constexpr int plane_of(int i) { return i == 0 ? 0 : i == 1 ? 2 : 1; }
 
-// Descriptor fields beside the address: K-major tiles have 8-row groups 1 KiB apart; MN-major
-// tiles 64-element atoms one box apart (LBO) and 8-row K groups 1 KiB apart (SBO).
+// Shared-memory descriptors, 128-byte swizzle. K-major tiles: 8-row groups 1 KiB apart. MN-major tiles: 64-value
+// atoms one box apart (LBO), 8-row groups of k 1 KiB apart (SBO). The low word holds the address (which alone
+// changes) and the LBO, the high word the rest. One thread issues all MMAs of an SM pair, a chunk's in about 300
+// cycles, so its loop is kept short: running stage numbers, 32-bit additions, no division.
 __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, bool mn) {
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(mn ? kBox >> 4 : 1) << 16) |
            ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
@@ -63,20 +73,118 @@ __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, bool mn) {
 // 16 values of k further: 32 bytes along a K-major row, two 8-row groups of an MN-major box.
 __device__ __forceinline__ uint64_t desc_step(bool mn) { return mn ? 2048 >> 4 : 32 >> 4; }
 
-// 32 lanes x 32 consecutive fp32 columns of TMEM into registers.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+    return r;
+}
+// Issued by the elected lane of a converged warp, so that the operands stay in uniform registers.
+template <bool PAIR>
+__device__ __forceinline__ void mma_one(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+            " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+            " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+            : "memory");
+}
+// Arrives on `bar` (in both CTAs of a pair) once the MMAs so far are done.
+template <bool PAIR>
+__device__ __forceinline__ void commit_one(uint32_t lead, uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n"
+            " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(bar),
+            "h"((uint16_t)3), "r"(lead)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+            " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar),
+            "r"(lead)
+            : "memory");
+}
+// The products of a chunk's four steps along k.
+template <bool PAIR>
+__device__ __forceinline__ void mma_chunk(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint64_t sa, uint64_t sb,
+                                          uint32_t idesc, bool first) {
+#pragma unroll
+    for (int k = 0; k < kTK / 16; ++k) mma_one<PAIR>(lead, d, a + k * sa, b + k * sb, idesc, first && k == 0 ? 0u : 1u);
+}
+
+// A wait that the whole warp made, its outcome the same in all lanes.
+__device__ __forceinline__ bool all_waited(bool ok) { return __all_sync(0xffffffffu, ok); }
+
+// The stage in turn and its phase.
+template <int STAGES>
+struct Ring {
+    uint32_t s = 0, ph = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == STAGES) s = 0, ph ^= 1u;
+    }
+};
+
+// 32 lanes x N consecutive fp32 columns of TMEM into registers, one instruction and one wait.
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float* v);
+template <>
+__device__ __forceinline__ void tmem_load<16>(uint32_t taddr, float* v) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15"
+        "}, [%16];\n tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <>
+__device__ __forceinline__ void tmem_load<32>(uint32_t taddr, float* v) {
     uint32_t r[32];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%2"
+        "6,%27,%28,%29,%30,%31"
+        "}, [%32];\n tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr)
         : "memory");
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <>
+__device__ __forceinline__ void tmem_load<64>(uint32_t taddr, float* v) {
+    uint32_t r[64];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%2"
+        "6,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%5"
+        "0,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
+        "}, [%64];\n tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 template <typename T>
@@ -247,13 +355,13 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
 // ------------------------------------------------------------------ one tile per CTA
 template <int BN, bool ROUND>
 struct TileShape {
-    static constexpr int kPlanes = ROUND ? 3 : 1;
-    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN * kTK * 2, kStage = kPlanes * (kP + kQ);
+    static constexpr int kPlanes = ROUND ? 3 : 1;  // stages of a chunk
+    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN * kTK * 2, kStage = kP + kQ;
     // two CTAs share an SM (96 to 100 KiB of stages each); the rounding variant keeps its sums in
     // registers and takes an SM alone
-    static constexpr int kStages = ROUND ? (BN == 128 ? 2 : 3) : BN == 128 ? 3 : BN == 64 ? 4 : 5;
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 8 * (2 * kStages + 5) + 16;
-    static constexpr uint32_t kCols = 2 * BN;  // two accumulators
+    static constexpr int kStages = ROUND ? (BN == 128 ? 6 : 8) : BN == 128 ? 3 : BN == 64 ? 4 : 5;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 8 * (2 * kStages + 2 * kAcc<ROUND> + 1) + 16;
+    static constexpr uint32_t kCols = kAcc<ROUND> * BN;
     static_assert((BN + 4) * kTM * 4 <= kStages * kStage, "the fp32 tile reuses the stages");
 };
 
@@ -267,9 +375,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
     uint64_t* bars = (uint64_t*)(smem + (size_t)S::kStages * S::kStage);
     uint64_t* full = bars;                    // TMA bytes landed
     uint64_t* empty = bars + S::kStages;      // MMAs done with the stage
-    uint64_t* tfull = bars + 2 * S::kStages;  // [2] accumulator ready
-    uint64_t* tempty = tfull + 2;             // [2] accumulator drained
-    uint64_t* mma_done = tempty + 2;
+    uint64_t* tfull = bars + 2 * S::kStages;  // accumulator ready
+    uint64_t* tempty = tfull + kAcc<ROUND>;   // accumulator drained
+    uint64_t* mma_done = tempty + kAcc<ROUND>;
     uint32_t* tmem_slot = (uint32_t*)(mma_done + 1);
     volatile int* abort = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -278,7 +386,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
             mbar_init(smem_u32(&full[s]), 1);
             mbar_init(smem_u32(&empty[s]), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kAcc<ROUND>; ++b) {
             mbar_init(smem_u32(&tfull[b]), 1);
             mbar_init(smem_u32(&tempty[b]), kEpiWarps);
         }
@@ -309,28 +417,23 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
             uint32_t last_par[S::kStages];
             bool issued[S::kStages];
             for (int s = 0; s < S::kStages; ++s) issued[s] = false;
-            for (int t = t0, ring = 0; t < t1; ++t, ++ring) {
-                const int s = ring % S::kStages;
-                const uint32_t ph = (ring / S::kStages) & 1u;
-                if (!wait_bounded(smem_u32(&empty[s]), ph ^ 1u, abort, p.err)) break;
-                const uint32_t st = smem_u32(smem + (size_t)s * S::kStage), bar = smem_u32(&full[s]);
-                const int k0 = t * kTK;
+            bool ok = true;
+            Ring<S::kStages> ring;
+            for (int i = t0 * S::kPlanes; ok && i < t1 * S::kPlanes; ++i, ring.next()) {
+                const int k0 = i / S::kPlanes * kTK, pl = plane_of(i % S::kPlanes);
+                const uint32_t s = ring.s, ph = ring.ph;
+                if (!(ok = wait_bounded(smem_u32(&empty[s]), ph ^ 1u, abort, p.err))) break;
+                const uint32_t dp = smem_u32(smem + (size_t)s * S::kStage), dq = dp + S::kP, bar = smem_u32(&full[s]);
                 mbar_arrive_tx(bar, S::kStage);
-#pragma unroll 1
-                for (int pl = 0; pl < S::kPlanes; ++pl) {
-                    const uint32_t dp = st + pl * S::kP, dq = st + S::kPlanes * S::kP + pl * S::kQ;
-                    if (p.p_mn) {
-                        for (int j = 0; j < kTM / 64; ++j)
-                            tma_load_3d(dp + j * kBox, &tmP, (int)i0 + 64 * j, k0, pl, bar);
-                    } else {
-                        tma_load_3d(dp, &tmP, k0, (int)i0, pl, bar);
-                    }
-                    if (BN >= 64 && p.q_mn) {
-                        for (int j = 0; j < BN / 64; ++j)
-                            tma_load_3d(dq + j * kBox, &tmQ, (int)j0 + 64 * j, k0, pl, bar);
-                    } else {
-                        tma_load_3d(dq, &tmQ, k0, (int)j0, pl, bar);
-                    }
+                if (p.p_mn) {
+                    for (int j = 0; j < kTM / 64; ++j) tma_load_3d(dp + j * kBox, &tmP, (int)i0 + 64 * j, k0, pl, bar);
+                } else {
+                    tma_load_3d(dp, &tmP, k0, (int)i0, pl, bar);
+                }
+                if (BN >= 64 && p.q_mn) {
+                    for (int j = 0; j < BN / 64; ++j) tma_load_3d(dq + j * kBox, &tmQ, (int)j0 + 64 * j, k0, pl, bar);
+                } else {
+                    tma_load_3d(dq, &tmQ, k0, (int)j0, pl, bar);
                 }
                 issued[s] = true;
                 last_par[s] = ph;
@@ -347,42 +450,59 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
                 }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            // ---------------- MMA issuer
+        {
+            // ---------------- MMA issuer: the whole warp runs the loop, one lane issues
+            const uint32_t lead = elect_one();
             const uint32_t idesc = idesc_bf16(kTM, BN) | (p.p_mn ? 1u << 15 : 0u) | (p.q_mn ? 1u << 16 : 0u);
             const uint64_t sp = desc_step(p.p_mn), sq = desc_step(p.q_mn);
+            const uint32_t bar_full = smem_u32(full), bar_empty = smem_u32(empty);
+            const uint64_t low_p = desc_of(smem_u32(smem), p.p_mn), low_q = desc_of(smem_u32(smem) + S::kP, p.q_mn);
             bool ok = true;
-            int t = t0, ring = 0;
+            int t = t0;
+            Ring<S::kStages> ring;
             for (int w = 0; ok && w < windows; ++w) {
-                const uint32_t b = w & 1u, use = w >> 1;
-                if (!wait_bounded(smem_u32(&tempty[b]), (use & 1u) ^ 1u, abort, p.err)) break;
+                const uint32_t b = w % kAcc<ROUND>, use = w / kAcc<ROUND>;
+                if (!all_waited(wait_bounded(smem_u32(&tempty[b]), (use & 1u) ^ 1u, abort, p.err))) break;
                 tc_fence_after();
-                const int end = ROUND ? t + 1 : t1;
-                for (bool first = true; t < end; ++t, ++ring) {
-                    const int s = ring % S::kStages;
-                    const uint32_t ph = (ring / S::kStages) & 1u;
-                    if (!wait_bounded(smem_u32(&full[s]), ph, abort, p.err)) {
-                        ok = false;
-                        break;
-                    }
+                const uint32_t d = tmem + b * BN;
+                auto await = [&](const Ring<S::kStages>& r) {
+                    if (ok) ok = all_waited(wait_bounded(bar_full + 8 * r.s, r.ph, abort, p.err));
                     tc_fence_after();
-                    const uint32_t st = smem_u32(smem + (size_t)s * S::kStage);
-#pragma unroll
-                    for (int x = 0; x < (ROUND ? 6 : 1); ++x) {
-                        const int vp = ROUND ? plane_p(x) : 0, vq = ROUND ? plane_q(x) : 0;
-                        const uint64_t dp = desc_of(st + vp * S::kP, p.p_mn);
-                        const uint64_t dq = desc_of(st + S::kPlanes * S::kP + vq * S::kQ, p.q_mn);
-#pragma unroll
-                        for (int k = 0; k < kTK / 16; ++k) {
-                            mma_bf16(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
-                            first = false;
-                        }
+                    return r.s * (S::kStage >> 4);
+                };
+                if (ROUND) {
+                    const uint32_t s0 = ring.s, o0 = await(ring);
+                    ring.next();
+                    const uint32_t s2 = ring.s, o2 = await(ring);
+                    ring.next();
+                    if (ok) {
+                        mma_chunk<false>(lead, d, low_p + o2, low_q + o0, sp, sq, idesc, true);
+                        mma_chunk<false>(lead, d, low_p + o0, low_q + o2, sp, sq, idesc, false);
+                        commit_one<false>(lead, bar_empty + 8 * s2);
                     }
-                    mma_commit(smem_u32(&empty[s]));
+                    const uint32_t s1 = ring.s, o1 = await(ring);
+                    ring.next();
+                    if (ok) {
+                        mma_chunk<false>(lead, d, low_p + o1, low_q + o1, sp, sq, idesc, false);
+                        mma_chunk<false>(lead, d, low_p + o1, low_q + o0, sp, sq, idesc, false);
+                        mma_chunk<false>(lead, d, low_p + o0, low_q + o1, sp, sq, idesc, false);
+                        commit_one<false>(lead, bar_empty + 8 * s1);
+                        mma_chunk<false>(lead, d, low_p + o0, low_q + o0, sp, sq, idesc, false);
+                        commit_one<false>(lead, bar_empty + 8 * s0);
+                    }
+                    ++t;
+                } else {
+                    for (bool first = true; ok && t < t1; ++t, first = false) {
+                        const uint32_t s = ring.s, o = await(ring);
+                        ring.next();
+                        if (!ok) break;
+                        mma_chunk<false>(lead, d, low_p + o, low_q + o, sp, sq, idesc, first);
+                        commit_one<false>(lead, bar_empty + 8 * s);
+                    }
                 }
-                if (ok) mma_commit(smem_u32(&tfull[b]));
+                if (ok) commit_one<false>(lead, smem_u32(&tfull[b]));
             }
-            mma_commit(smem_u32(mma_done));
+            commit_one<false>(lead, smem_u32(mma_done));
             const uint64_t since = global_ns();
             while (!mbar_try_wait(smem_u32(mma_done), 0))
                 if (global_ns() - since > kTimeoutNs) {
@@ -410,12 +530,13 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
         };
         auto wait_for = [&](int w) {
             bool got = true;
-            if (lane == 0) got = wait_bounded(smem_u32(&tfull[w & 1]), (uint32_t)(w >> 1) & 1u, abort, p.err);
+            if (lane == 0)
+                got = wait_bounded(smem_u32(&tfull[w % kAcc<ROUND>]), (uint32_t)(w / kAcc<ROUND>) & 1u, abort, p.err);
             got = __shfl_sync(0xffffffffu, got, 0);
             tc_fence_after();
             return got;
         };
-        if (!ROUND) {
+        if constexpr (!ROUND) {
             if (wait_for(0)) {
 #pragma unroll
                 for (int c = 0; c < kC; c += 16) {
@@ -431,16 +552,13 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
             bool got = true;
             for (int w = 0; got && w < windows; ++w) {
                 if (!(got = wait_for(w))) break;
-#pragma unroll
-                for (int c = 0; c < kC; c += 16) {
-                    float v[16];
-                    tmem_ld16(tb + (w & 1) * BN + c, v);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[c + i] += v[i];
-                }
+                float v[kC];
+                tmem_load<kC>(tb + (w % kAcc<ROUND>) * BN, v);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&tempty[w & 1]));
+                if (lane == 0) mbar_arrive(smem_u32(&tempty[w % kAcc<ROUND>]));
+#pragma unroll
+                for (int i = 0; i < kC; ++i) acc[i] += v[i];
             }
             // the last window's MMAs have read every stage: the tile may take their place
             if (got)
@@ -502,19 +620,6 @@ __device__ __forceinline__ void pair_relinquish() {
 __device__ __forceinline__ void pair_dealloc(uint32_t taddr, uint32_t cols) {
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
 }
-__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-// Arrives on the barrier at this offset in both CTAs once the MMAs so far are done.
-__device__ __forceinline__ void pair_commit(uint32_t bar) {
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-        "h"((uint16_t)3)
-        : "memory");
-}
 // A box into this CTA's shared memory whose bytes count on a barrier of either CTA of the pair.
 __device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* tm, int c0, int c1, int c2, uint32_t bar) {
     asm volatile(
@@ -524,16 +629,22 @@ __device__ __forceinline__ void pair_load_3d(uint32_t dst, const CUtensorMap* tm
         : "memory");
 }
 
+// Arrive on the leader's barrier: orders what the thread has read from TMEM (before a tcgen05 fence), no memory
+// is handed over, so nothing wider than the default scope is waited for.
+__device__ __forceinline__ void pair_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
+}
+
 template <int BN, bool ROUND>
 struct PairShape {
-    static constexpr int kPlanes = ROUND ? 3 : 1;
-    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN / 2 * kTK * 2, kStage = kPlanes * (kP + kQ);
-    static constexpr int kStages = ROUND ? 2 : 6;
+    static constexpr int kPlanes = ROUND ? 3 : 1;  // stages of a chunk
+    static constexpr uint32_t kP = kTM * kTK * 2, kQ = BN / 2 * kTK * 2, kStage = kP + kQ;
+    static constexpr int kStages = ROUND ? 8 : 6;
     static constexpr uint32_t kUnit = 32 * 64;       // one output unit
     static constexpr uint32_t kBlock = 2 * kUnit;    // two per epilogue warp
     static constexpr uint32_t kBlockLd = 20;         // floats of a row staged for edges: 16 + 4
     static_assert(32 * kBlockLd * 4 <= kBlock, "edge staging");
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kEpiWarps * kBlock + 8 * (2 * kStages + 5) + 16;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kEpiWarps * kBlock + 8 * (2 * kStages + 2 * kAcc<ROUND> + 1) + 16;
     static constexpr uint32_t kCols = 512;  // the SM's whole TMEM: both CTAs' columns start at the same place
     static_assert(kSmem <= 232448, "shared memory per CTA");
 };
@@ -571,9 +682,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     uint64_t* bars = (uint64_t*)(blocks + kEpiWarps * S::kBlock);
     uint64_t* full = bars;                    // leader's: both CTAs' bytes landed
     uint64_t* empty = bars + S::kStages;      // each CTA's own: MMAs done with the stage
-    uint64_t* tfull = bars + 2 * S::kStages;  // [2] each CTA's own: accumulator ready
-    uint64_t* tempty = tfull + 2;             // [2] leader's: accumulator drained by both CTAs' warps
-    uint64_t* mma_done = tempty + 2;
+    uint64_t* tfull = bars + 2 * S::kStages;  // each CTA's own: accumulator ready
+    uint64_t* tempty = tfull + kAcc<ROUND>;   // leader's: accumulator drained by both CTAs' warps
+    uint64_t* mma_done = tempty + kAcc<ROUND>;
     uint32_t* tmem_slot = (uint32_t*)(mma_done + 1);
     volatile int* abort = (volatile int*)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -583,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             mbar_init(smem_u32(&full[s]), 1);
             mbar_init(smem_u32(&empty[s]), 1);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kAcc<ROUND>; ++b) {
             mbar_init(smem_u32(&tfull[b]), 1);
             mbar_init(smem_u32(&tempty[b]), 2 * kEpiWarps);
         }
@@ -617,7 +728,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     if (warp == 0) {
         if (lane == 0) {
             // ---------------- TMA producer of this CTA's halves
-            uint32_t ring = 0, last_par[S::kStages];
+            Ring<S::kStages> ring;
+            uint32_t last_par[S::kStages];
             bool issued[S::kStages], ok = true;
             for (int s = 0; s < S::kStages; ++s) issued[s] = false;
             auto feed = [&](auto G) {
@@ -629,30 +741,25 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 int64_t i0, j0;
                 place(p, u, &i0, &j0);
                 const int pr = (int)i0 + (int)rank * kTM, qr = (int)j0 + (int)rank * (BN / 2);
-                for (int t = 0; t < total; ++t, ++ring) {
-                    const int s = ring % S::kStages;
-                    const uint32_t ph = (ring / S::kStages) & 1u;
+                for (int i = 0; i < total * S::kPlanes; ++i, ring.next()) {
+                    const int k0 = i / S::kPlanes * kTK, pl = plane_of(i % S::kPlanes);
+                    const uint32_t s = ring.s, ph = ring.ph;
                     if (!wait_bounded(smem_u32(&empty[s]), ph ^ 1u, abort, pp.err)) {
                         ok = false;
                         break;
                     }
-                    const uint32_t st = smem_u32(smem + (size_t)s * S::kStage), bar = smem_u32(&full[s]);
+                    const uint32_t dp = smem_u32(smem + (size_t)s * S::kStage), dq = dp + S::kP, bar = smem_u32(&full[s]);
                     const uint32_t lead = map_rank(bar, 0);
-                    const int k0 = t * kTK;
                     if (rank == 0) mbar_arrive_tx(bar, 2 * S::kStage);
-#pragma unroll 1
-                    for (int pl = 0; pl < S::kPlanes; ++pl) {
-                        const uint32_t dp = st + pl * S::kP, dq = st + S::kPlanes * S::kP + pl * S::kQ;
-                        if (p.p_mn) {
-                            for (int j = 0; j < kTM / 64; ++j) pair_load_3d(dp + j * kBox, tmP, pr + 64 * j, k0, pl, lead);
-                        } else {
-                            pair_load_3d(dp, tmP, k0, pr, pl, lead);
-                        }
-                        if (p.q_mn) {
-                            for (int j = 0; j < BN / 128; ++j) pair_load_3d(dq + j * kBox, tmQ, qr + 64 * j, k0, pl, lead);
-                        } else {
-                            pair_load_3d(dq, tmQ, k0, qr, pl, lead);
-                        }
+                    if (p.p_mn) {
+                        for (int j = 0; j < kTM / 64; ++j) pair_load_3d(dp + j * kBox, tmP, pr + 64 * j, k0, pl, lead);
+                    } else {
+                        pair_load_3d(dp, tmP, k0, pr, pl, lead);
+                    }
+                    if (p.q_mn) {
+                        for (int j = 0; j < BN / 128; ++j) pair_load_3d(dq + j * kBox, tmQ, qr + 64 * j, k0, pl, lead);
+                    } else {
+                        pair_load_3d(dq, tmQ, k0, qr, pl, lead);
                     }
                     issued[s] = true;
                     last_par[s] = ph;
@@ -674,9 +781,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            // ---------------- MMA issuer of the pair
-            uint32_t ring = 0, use = 0;
+        if (rank == 0) {
+            // ---------------- MMA issuer of the pair: the whole warp runs the loop, one lane issues
+            const uint32_t lead = elect_one();
+            Ring<S::kStages> ring;
+            Ring<kAcc<ROUND>> acc;
             bool ok = true;
             auto issue = [&](auto G) {
               constexpr int g = decltype(G)::value;
@@ -684,46 +793,61 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
               const bool p_mn = p.p_mn, q_mn = p.q_mn;
               const uint32_t idesc = idesc_bf16(2 * kTM, BN) | (p_mn ? 1u << 15 : 0u) | (q_mn ? 1u << 16 : 0u);
               const uint64_t sp = desc_step(p_mn), sq = desc_step(q_mn);
+              const uint32_t bar_full = smem_u32(full), bar_empty = smem_u32(empty);
+              const uint64_t low_p = desc_of(smem_u32(smem), p_mn), low_q = desc_of(smem_u32(smem) + S::kP, q_mn);
               const int total = p.nk, windows = ROUND ? total : 1;  // accumulator fills of a tile
               for (int64_t j = 0; ok && pair_tile<g>(pp, me, pairs, j) < pp.tiles[g]; ++j) {
                 int t = 0;
-                for (int w = 0; ok && w < windows; ++w, ++use) {
-                    const uint32_t b = use & 1u;
-                    if (!wait_bounded_cluster(smem_u32(&tempty[b]), ((use >> 1) & 1u) ^ 1u, abort, pp.err)) {
+                for (int w = 0; ok && w < windows; ++w, acc.next()) {
+                    const uint32_t b = acc.s;
+                    if (!all_waited(wait_bounded(smem_u32(&tempty[b]), acc.ph ^ 1u, abort, pp.err))) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const int end = ROUND ? t + 1 : total;
-                    for (bool first = true; t < end; ++t, ++ring) {
-                        const int s = ring % S::kStages;
-                        const uint32_t ph = (ring / S::kStages) & 1u;
-                        if (!wait_bounded(smem_u32(&full[s]), ph, abort, pp.err)) {
-                            ok = false;
-                            break;
-                        }
+                    const uint32_t d = tmem + b * BN;
+                    auto await = [&](const Ring<S::kStages>& r) {
+                        if (ok) ok = all_waited(wait_bounded(bar_full + 8 * r.s, r.ph, abort, pp.err));
                         tc_fence_after();
-                        const uint32_t st = smem_u32(smem + (size_t)s * S::kStage);
-#pragma unroll
-                        for (int x = 0; x < (ROUND ? 6 : 1); ++x) {
-                            const int vp = ROUND ? plane_p(x) : 0, vq = ROUND ? plane_q(x) : 0;
-                            const uint64_t dp = desc_of(st + vp * S::kP, p_mn);
-                            const uint64_t dq = desc_of(st + S::kPlanes * S::kP + vq * S::kQ, q_mn);
-#pragma unroll
-                            for (int k = 0; k < kTK / 16; ++k) {
-                                pair_mma(tmem + b * BN, dp + k * sp, dq + k * sq, idesc, first ? 0u : 1u);
-                                first = false;
-                            }
+                        return r.s * (S::kStage >> 4);
+                    };
+                    if (ROUND) {
+                        const uint32_t s0 = ring.s, o0 = await(ring);
+                        ring.next();
+                        const uint32_t s2 = ring.s, o2 = await(ring);
+                        ring.next();
+                        if (ok) {
+                            mma_chunk<true>(lead, d, low_p + o2, low_q + o0, sp, sq, idesc, true);
+                            mma_chunk<true>(lead, d, low_p + o0, low_q + o2, sp, sq, idesc, false);
+                            commit_one<true>(lead, bar_empty + 8 * s2);
                         }
-                        pair_commit(smem_u32(&empty[s]));
+                        const uint32_t s1 = ring.s, o1 = await(ring);
+                        ring.next();
+                        if (ok) {
+                            mma_chunk<true>(lead, d, low_p + o1, low_q + o1, sp, sq, idesc, false);
+                            mma_chunk<true>(lead, d, low_p + o1, low_q + o0, sp, sq, idesc, false);
+                            mma_chunk<true>(lead, d, low_p + o0, low_q + o1, sp, sq, idesc, false);
+                            commit_one<true>(lead, bar_empty + 8 * s1);
+                            mma_chunk<true>(lead, d, low_p + o0, low_q + o0, sp, sq, idesc, false);
+                            commit_one<true>(lead, bar_empty + 8 * s0);
+                        }
+                        ++t;
+                    } else {
+                        for (bool first = true; ok && t < total; ++t, first = false) {
+                            const uint32_t s = ring.s, o = await(ring);
+                            ring.next();
+                            if (!ok) break;
+                            mma_chunk<true>(lead, d, low_p + o, low_q + o, sp, sq, idesc, first);
+                            commit_one<true>(lead, bar_empty + 8 * s);
+                        }
                     }
-                    if (ok) pair_commit(smem_u32(&tfull[b]));
+                    if (ok) commit_one<true>(lead, smem_u32(&tfull[b]));
                 }
               }
             };
             issue(std::integral_constant<int, 0>());
             issue(std::integral_constant<int, 1>());
-            pair_commit(smem_u32(mma_done));
+            commit_one<true>(lead, smem_u32(mma_done));
             const uint64_t since = global_ns();
             while (!mbar_try_wait(smem_u32(mma_done), 0))
                 if (global_ns() - since > kTimeoutNs) {
@@ -740,7 +864,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         uint32_t use = 0;
         auto wait_for = [&]() {
             bool got = true;
-            if (lane == 0) got = wait_bounded(smem_u32(&tfull[use & 1u]), (use >> 1) & 1u, abort, pp.err);
+            if (lane == 0)
+                got = wait_bounded(smem_u32(&tfull[use % kAcc<ROUND>]), (use / kAcc<ROUND>) & 1u, abort, pp.err);
             got = __shfl_sync(0xffffffffu, got, 0);
             tc_fence_after();
             return got;
@@ -748,7 +873,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         auto release = [&]() {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_remote(smem_u32(&tempty[use & 1u]), 0);
+            if (lane == 0) pair_arrive(smem_u32(&tempty[use % kAcc<ROUND>]));
             ++use;
         };
         // 16 columns of this warp's 32 rows, held a row a lane, through shared memory: edges and rows that are not
@@ -867,12 +992,12 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 }
                 if (!ROUND) release();
             };
-            if (!ROUND) {
+            if constexpr (!ROUND) {
                 const uint32_t at = tb + (use & 1u) * BN;
                 if (p.ep.f32)
                     column_units(float(), [&](int c, float* v) { tmem_ld16(at + c, v); });
                 else
-                    column_units(__nv_bfloat16(), [&](int c, float* v) { tmem_ld32(at + c, v); });
+                    column_units(__nv_bfloat16(), [&](int c, float* v) { tmem_load<32>(at + c, v); });
             } else {
                 float acc[kC];
 #pragma unroll
@@ -880,14 +1005,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 const int windows = p.nk;
                 for (int w = 0; w < windows; ++w) {
                     if (!(got = wait_for())) break;
-#pragma unroll
-                    for (int c = 0; c < kC; c += 16) {
-                        float v[16];
-                        tmem_ld16(tb + (use & 1u) * BN + c, v);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[c + i] += v[i];
-                    }
+                    float v[kC];
+                    tmem_load<kC>(tb + (use % kAcc<ROUND>) * BN, v);
                     release();
+#pragma unroll
+                    for (int i = 0; i < kC; ++i) acc[i] += v[i];
                 }
                 if (!got) break;
                 column_units(float(), [&](int c, float* v) {
@@ -943,6 +1065,9 @@ bool make_map(CUtensorMap* tm, const LinearOperand& o, int box_rows) {
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The map of an operand whose tile has `extent` values along MN.
+bool operand_map(CUtensorMap* tm, const LinearOperand& o, int extent) { return make_map(tm, o, o.mn ? kTK : extent); }
+
 // 2-D map over an output's rows: boxes of 64 bytes x 32 rows, 64-byte swizzle.
 bool make_out_map(CUtensorMap* tm, void* p, int64_t rows, int64_t cols, int64_t ld, bool f32) {
     EncodeTiledFn enc = encode_fn();
@@ -983,11 +1108,11 @@ template <typename T, int BN, bool ROUND>
 cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, bool chained, cudaStream_t s) {
     using S = TileShape<BN, ROUND>;
     CUtensorMap mP, mQ;
-    if (!make_map(&mP, P, P.mn ? kTK : kTM) || !make_map(&mQ, Q, Q.mn ? kTK : BN)) return cudaErrorInvalidValue;
+    if (!operand_map(&mP, P, kTM) || !operand_map(&mQ, Q, BN)) return cudaErrorInvalidValue;
     p.tiles_p = (P.extent() + kTM - 1) / kTM;
     p.tiles_q = (Q.extent() + BN - 1) / BN;
     const int64_t tiles = p.tiles_p * p.tiles_q;
-    // split the K loop while the CTAs still fit the GPU at once and each keeps four chunks' worth of MMAs
+    // split the K loop while the CTAs still fit the GPU at once and each keeps a few chunks
     const int least = ROUND ? 1 : 4;
     const int64_t slots = (int64_t)sm_count() * (ROUND ? 1 : 2);
     p.split = 1;
@@ -1021,7 +1146,7 @@ cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStre
     pp.tiles[0] = pp.tiles[1] = 0;
     for (int i = 0; i < count; ++i) {
         const Product& x = *pr[i];
-        if (!make_map(&pp.tmP[i], x.P, x.P.mn ? kTK : kTM) || !make_map(&pp.tmQ[i], x.Q, x.Q.mn ? kTK : BN / 2))
+        if (!operand_map(&pp.tmP[i], x.P, kTM) || !operand_map(&pp.tmQ[i], x.Q, BN / 2))
             return cudaErrorInvalidValue;
         const LinearEpilogue& e = x.p.ep;
         if (e.wide && (!make_out_map(&pp.tmY[i], e.Y, e.M, e.N, e.ld_y, e.f32) ||
@@ -1116,7 +1241,7 @@ cudaError_t launch_linear_products(const LinearProduct* x, int count, bool chain
     const bool round = r[0].P.planes == 3;
     // a pair's tile for at least half of the SM pairs
     if (tiles * 4 >= sm_count()) {
-        if (count == 2 && r[1].p.nk > r[0].p.nk) order[0] = &r[1], order[1] = &r[0];
+        if (count == 2 && r[1].P.depth() > r[0].P.depth()) order[0] = &r[1], order[1] = &r[0];
         return round ? run_pair<128, true>(order, count, chained, s) : run_pair<256, false>(order, count, chained, s);
     }
     for (int i = 0; i < count; ++i, chained = true) {
