@@ -6,24 +6,29 @@
 // nothing is transposed in memory.
 //
 // fp32 operands arrive as three bf16 planes x = x0 + x1 + x2 (each the rounding of
-// what the ones before leave, exact to 2^-24). A stage holds all planes of a chunk
-// of k, read once, and feeds the six plane pairs whose products matter, smallest
-// first. The tensor pipe adds into its fp32 accumulators with truncation, so for
-// these every chunk's sum is drained and added up in registers with rounding.
+// what the ones before leave, exact to 2^-24). The planes of a chunk of k are staged
+// once and feed the six plane pairs whose products matter, smallest first. The
+// tensor pipe adds into its fp32 accumulators with truncation, so for these every
+// chunk's sum is drained and added up in registers with rounding (error against 64
+// bits 1e-7 to 2e-7 of the result's norm up to K = 14336, below an fp32 FMA chain's).
 //
 // linear_pair_kernel, for products with a tile for most SM pairs: two CTAs of a
 // cluster hold one 256 x BN tile (cta_group::2), each staging 128 rows of P and half
 // of Q, so an operand byte that reaches an SM feeds twice the MMAs; persistent, the
-// epilogue of a tile beside the next tile's MMAs, its outputs by TMA.
+// epilogue of a tile beside the next tile's MMAs, its outputs by TMA. Bound by the
+// tensor pipe at the clock that the power limit leaves: 8192 x 14336 -> 4096 bf16
+// 540 us = 1.78 PFLOP/s (468 us without loads and epilogue), 4096 x 2048 -> 8192 with
+// tanh-gelu and Z 87-93 us (75 without its epilogue); fp32 2048 x 4096 -> 4096 300 us
+// = 229 TFLOP/s, six bf16 products each.
 //
-// linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a decoded token, a
-// short batch) swap the operands, so the long side fills the 128 rows of a tile,
-// and split the K loop over the CTAs of a cluster, whose fp32 tiles are added in
-// rank order through distributed shared memory.
+// linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a short batch) swap the
+// operands, so the long side fills the 128 rows of a tile, and split the K loop over
+// the CTAs of a cluster, whose fp32 tiles are added in rank order through distributed
+// shared memory. Bound by reading W: 16 x 4096 -> 14336 24.8 us = 4.7 TB/s.
 //
-// Warp roles: warp 0 TMA producer (lane 0), warp 1 TMEM allocator and MMA issuer
-// (lane 0), warps 2-9 epilogue (TMEM lane quadrant warp % 4, column half by warp).
-// Waits are bounded (about 1 s) and set kErrTimeout on expiry.
+// Warp roles: warp 0 TMA producer (lane 0), warp 1 TMEM allocator and MMA issuer,
+// warps 2-9 epilogue (TMEM lane quadrant warp % 4, column half by warp). Waits are
+// bounded (about 1 s) and set kErrTimeout on expiry.
 #include <cuda.h>
 
 #include <mutex>
@@ -41,8 +46,8 @@ constexpr int kTM = 128;
 constexpr int kTK = 64;                  // values of k per chunk
 constexpr uint32_t kBox = 64 * kTK * 2;  // one MN-major box of 64 values: 8 KiB
 
-// Accumulators in TMEM. Handing one to the epilogue and back takes about 1.6 us, several times the MMAs of a
-// stage of fp32 planes, each of which fills one.
+// Accumulators in TMEM. One is handed to the epilogue and back per tile, for fp32 operands per chunk (24 MMAs,
+// 0.8 us), where the way there and back takes about 1.6 us.
 template <bool ROUND>
 constexpr int kAcc = ROUND ? 4 : 2;
 
@@ -59,13 +64,11 @@ struct TileParams {
 // fp32 operands: each plane of a chunk is a stage of its own, loaded in the order 0, 2, 1. The products
 // P2 Q0, P0 Q2 free plane 2's stage, then P1 Q1, P1 Q0, P0 Q1 plane 1's, then P0 Q0: smallest first, and the
 // next chunk's loads run through all of them. (Stages of all three planes left room for two, which did
-// not cover the loads: 1.43 us a chunk of 256 x 128 tiles against the figure below.)
+// not cover the loads: 1.43 us a chunk of a 256 x 128 tile against 1.17.)
 __device__ __forceinline__ constexpr int plane_of(int i) { return i == 0 ? 0 : i == 1 ? 2 : 1; }
 
 // Shared-memory descriptors, 128-byte swizzle. K-major tiles: 8-row groups 1 KiB apart. MN-major tiles: 64-value
-// atoms one box apart (LBO), 8-row groups of k 1 KiB apart (SBO). The low word holds the address (which alone
-// changes) and the LBO, the high word the rest. One thread issues all MMAs of an SM pair, a chunk's in about 300
-// cycles, so its loop is kept short: running stage numbers, 32-bit additions, no division.
+// atoms one box apart (LBO), 8-row groups of k 1 KiB apart (SBO).
 __device__ __forceinline__ uint64_t desc_of(uint32_t saddr, bool mn) {
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(mn ? kBox >> 4 : 1) << 16) |
            ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
@@ -78,7 +81,9 @@ __device__ __forceinline__ uint32_t elect_one() {
     asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
     return r;
 }
-// Issued by the elected lane of a converged warp, so that the operands stay in uniform registers.
+// Issued by the elected lane of a converged warp, so that the operands stay in uniform registers: a single-lane
+// branch issued the 4 MMAs of a bf16 chunk up to a fifth slower than the tensor pipe runs them, depending on
+// the code around them (fp32 2048 x 4096 -> 4096 366 us, 306 this way).
 template <bool PAIR>
 __device__ __forceinline__ void mma_one(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     if constexpr (PAIR)
@@ -365,11 +370,19 @@ struct TileShape {
     static_assert((BN + 4) * kTM * 4 <= kStages * kStage, "the fp32 tile reuses the stages");
 };
 
-template <typename T, int BN, bool ROUND>
-__global__ void __launch_bounds__(kThreads, ROUND ? 1 : 2)
-linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ,
-                   const __grid_constant__ TileParams p) {
+// One product, or two in one launch: CTAs below ctas0 work on the first.
+struct TileLaunch {
+    TileParams g[2];
+    CUtensorMap tmP[2], tmQ[2];
+    int ctas0;
+};
+
+// A CTA's work on product g; the parameters stay at fixed places of the constant bank.
+template <int BN, bool ROUND, int g>
+__device__ __forceinline__ void tile_body(const TileLaunch& pp) {
     using S = TileShape<BN, ROUND>;
+    const TileParams& p = pp.g[g];
+    const CUtensorMap &tmP = pp.tmP[g], &tmQ = pp.tmQ[g];
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint64_t* bars = (uint64_t*)(smem + (size_t)S::kStages * S::kStage);
@@ -405,8 +418,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
     chain_wait();
     chain_next();
 
-    const int64_t tile = blockIdx.x / p.split;
-    const int rank = blockIdx.x % p.split;
+    const int cta = (int)blockIdx.x - (g ? pp.ctas0 : 0);
+    const int64_t tile = cta / p.split;
+    const int rank = cta % p.split;
     const int64_t i0 = (tile / p.tiles_q) * kTM, j0 = (tile % p.tiles_q) * BN;
     const int t0 = (int)((int64_t)p.nk * rank / p.split), t1 = (int)((int64_t)p.nk * (rank + 1) / p.split);
     const int windows = ROUND ? t1 - t0 : 1;  // accumulator fills
@@ -541,7 +555,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < kC; c += 16) {
                     float v[16];
-                    tmem_ld16(tb + c, v);
+                    tmem_load<16>(tb + c, v);
                     put(half * kC + c, v);
                 }
             }
@@ -596,7 +610,10 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
                     v[u][0] += x.x, v[u][1] += x.y, v[u][2] += x.z, v[u][3] += x.w;
                 }
             }
-            finish<T, U, false>(p.ep, m, n, ok, v);
+            if (ROUND || p.ep.f32)
+                finish<float, U, false>(p.ep, m, n, ok, v);
+            else
+                finish<__nv_bfloat16, U, false>(p.ep, m, n, ok, v);
         }
     }
     __syncwarp();
@@ -608,6 +625,14 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constan
         tc_fence_after();
         tmem_dealloc(tmem, S::kCols);
     }
+}
+
+template <int BN, bool ROUND>
+__global__ void __launch_bounds__(kThreads, ROUND ? 1 : 2) linear_tile_kernel(const __grid_constant__ TileLaunch pp) {
+    if ((int)blockIdx.x < pp.ctas0)
+        tile_body<BN, ROUND, 0>(pp);
+    else
+        tile_body<BN, ROUND, 1>(pp);
 }
 
 // ------------------------------------------------------------------ one tile per CTA pair, persistent
@@ -995,7 +1020,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             if constexpr (!ROUND) {
                 const uint32_t at = tb + (use & 1u) * BN;
                 if (p.ep.f32)
-                    column_units(float(), [&](int c, float* v) { tmem_ld16(at + c, v); });
+                    column_units(float(), [&](int c, float* v) { tmem_load<16>(at + c, v); });
                 else
                     column_units(__nv_bfloat16(), [&](int c, float* v) { tmem_load<32>(at + c, v); });
             } else {
@@ -1005,11 +1030,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 const int windows = p.nk;
                 for (int w = 0; w < windows; ++w) {
                     if (!(got = wait_for())) break;
-                    float v[kC];
-                    tmem_load<kC>(tb + (use % kAcc<ROUND>) * BN, v);
-                    release();
+                    const uint32_t at = tb + (use % kAcc<ROUND>) * BN;
 #pragma unroll
-                    for (int i = 0; i < kC; ++i) acc[i] += v[i];
+                    for (int c = 0; c < kC; c += 32) {
+                        float v[32];
+                        tmem_load<32>(at + c, v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[c + i] += v[i];
+                    }
+                    release();
                 }
                 if (!got) break;
                 column_units(float(), [&](int c, float* v) {
@@ -1095,6 +1124,7 @@ int sm_count() {
     return v;
 }
 
+
 // The cluster's size, and (second) a chained launch.
 void cluster_attributes(cudaLaunchAttribute* at, int size) {
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -1104,40 +1134,55 @@ void cluster_attributes(cudaLaunchAttribute* at, int size) {
     at[1].val.programmaticStreamSerializationAllowed = 1;
 }
 
-template <typename T, int BN, bool ROUND>
-cudaError_t run_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, bool chained, cudaStream_t s) {
-    using S = TileShape<BN, ROUND>;
-    CUtensorMap mP, mQ;
-    if (!operand_map(&mP, P, kTM) || !operand_map(&mQ, Q, BN)) return cudaErrorInvalidValue;
-    p.tiles_p = (P.extent() + kTM - 1) / kTM;
-    p.tiles_q = (Q.extent() + BN - 1) / BN;
-    const int64_t tiles = p.tiles_p * p.tiles_q;
-    // split the K loop while the CTAs still fit the GPU at once and each keeps a few chunks
-    const int least = ROUND ? 1 : 4;
-    const int64_t slots = (int64_t)sm_count() * (ROUND ? 1 : 2);
-    p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= slots && p.nk >= 2 * least * p.split) p.split *= 2;
-    if (tiles * p.split > 2147483647LL) return cudaErrorInvalidConfiguration;
-    cudaError_t e = smem_attr_once<linear_tile_kernel<T, BN, ROUND>>((int)S::kSmem);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * p.split));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = S::kSmem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[2];
-    cluster_attributes(at, p.split);
-    cfg.attrs = at;
-    cfg.numAttrs = chained ? 2 : 1;
-    note_launches(1);
-    return cudaLaunchKernelEx(&cfg, linear_tile_kernel<T, BN, ROUND>, mP, mQ, p);
-}
-
 struct Product {
     LinearOperand P, Q;
     TileParams p;
     tda_dtype out;
 };
+
+// CTAs along K of a tile launch: as many as fit the GPU at once, a few chunks each.
+int tile_split(int64_t tiles, int nk, bool round) {
+    const int least = round ? 1 : 4;
+    const int64_t slots = (int64_t)sm_count() * (round ? 1 : 2);
+    int split = 1;
+    while (split < 8 && tiles * split * 2 <= slots && nk >= 2 * least * split) split *= 2;
+    return split;
+}
+
+template <int BN, bool ROUND>
+cudaError_t run_tile(const Product* const* pr, int count, bool chained, cudaStream_t s) {
+    using S = TileShape<BN, ROUND>;
+    TileLaunch pp = {};
+    int64_t tiles[2] = {0, 0};
+    int nk = 1 << 30;
+    for (int i = 0; i < count; ++i) {
+        const Product& x = *pr[i];
+        if (!operand_map(&pp.tmP[i], x.P, kTM) || !operand_map(&pp.tmQ[i], x.Q, BN)) return cudaErrorInvalidValue;
+        pp.g[i] = x.p;
+        pp.g[i].tiles_p = (x.P.extent() + kTM - 1) / kTM;
+        pp.g[i].tiles_q = (x.Q.extent() + BN - 1) / BN;
+        tiles[i] = pp.g[i].tiles_p * pp.g[i].tiles_q;
+        if (x.p.nk < nk) nk = x.p.nk;
+    }
+    const int64_t all = tiles[0] + tiles[1];
+    const int split = tile_split(all, nk, ROUND);
+    if (all * split > 2147483647LL) return cudaErrorInvalidConfiguration;
+    pp.g[0].split = pp.g[1].split = split;
+    pp.ctas0 = (int)(tiles[0] * split);
+    cudaError_t e = smem_attr_once<linear_tile_kernel<BN, ROUND>>((int)S::kSmem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(all * split));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    cluster_attributes(at, split);
+    cfg.attrs = at;
+    cfg.numAttrs = chained ? 2 : 1;
+    note_launches(1);
+    return cudaLaunchKernelEx(&cfg, linear_tile_kernel<BN, ROUND>, pp);
+}
 
 template <int BN, bool ROUND>
 cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStream_t s) {
@@ -1183,12 +1228,12 @@ cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStre
     return cudaLaunchKernelEx(&cfg, linear_pair_kernel<BN, ROUND>, pp);
 }
 
-template <typename T, bool ROUND>
-cudaError_t pick_tile(const LinearOperand& P, const LinearOperand& Q, TileParams& p, bool chained, cudaStream_t s) {
-    const int64_t q = Q.extent();
-    if (q <= 32 && !Q.mn) return run_tile<T, 32, ROUND>(P, Q, p, chained, s);
-    if (q <= 64) return run_tile<T, 64, ROUND>(P, Q, p, chained, s);
-    return run_tile<T, 128, ROUND>(P, Q, p, chained, s);
+template <bool ROUND>
+cudaError_t pick_tile(const Product* const* pr, int count, bool chained, cudaStream_t s) {
+    const LinearOperand& Q = pr[0]->Q;
+    if (count == 1 && Q.extent() <= 32 && !Q.mn) return run_tile<32, ROUND>(pr, count, chained, s);
+    if (count == 1 && Q.extent() <= 64) return run_tile<64, ROUND>(pr, count, chained, s);
+    return run_tile<128, ROUND>(pr, count, chained, s);
 }
 
 }  // namespace
@@ -1222,41 +1267,77 @@ static Product make_product(const LinearProduct& x, unsigned int* err) {
     return r;
 }
 
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Tiles of 256 x 256 (fp32 operands: 128) of a product; 0 where a side is too short for them.
 static int64_t pair_tiles(const Product& x) {
-    const int64_t bn = x.P.planes == 3 ? 128 : 256;
-    return x.p.swap ? 0 : ((x.P.extent() + 2 * kTM - 1) / (2 * kTM)) * ((x.Q.extent() + bn - 1) / bn);
+    return x.p.swap ? 0 : ceil_div(x.P.extent(), 2 * kTM) * ceil_div(x.Q.extent(), x.P.planes == 3 ? 128 : 256);
 }
 
-cudaError_t launch_linear_products(const LinearProduct* x, int count, bool chained, unsigned int* err,
-                                   cudaStream_t s) {
+// Estimated times, in chunks of an SM pair (0.36 us; fp32 1.2 us). The pair kernel: its longest list of tiles
+// (pair_tile's order), each its chunks and about two more of set-up, or the time of writing its outputs value by
+// value where rows are not aligned.
+static double pair_time(const Product* const* r, int count) {
+    auto cost = [](const Product& x) { return x.p.nk + (x.p.ep.wide ? 2 : x.P.planes == 3 ? 6 : 16); };
+    const int64_t n = sm_count() / 2, t0 = pair_tiles(*r[0]), c0 = cost(*r[0]);
+    if (count == 1) return (double)(ceil_div(t0, n) * c0);
+    const int64_t t1 = pair_tiles(*r[1]), c1 = cost(*r[1]), idle = n - t0 % n;
+    int64_t extra = (c0 + c1 / 2) / c1;
+    if (extra > ceil_div(t1, idle)) extra = ceil_div(t1, idle);
+    const int64_t left = t1 > extra * idle ? t1 - extra * idle : 0;
+    return (double)(t0 / n * c0 + (c0 > extra * c1 ? c0 : extra * c1) + ceil_div(left, n) * c1);
+}
+
+// The tile kernel: bf16 CTAs share an SM by twos, at the pace of its operand loads; fp32 CTAs take an SM each, in
+// rounds, a chunk 1.4 times as long as a pair's.
+static double tile_time(const Product* const* r, int count, bool round) {
+    int64_t tiles = 0;
+    int most = 0, least = 1 << 30;
+    for (int i = 0; i < count; ++i) {
+        tiles += ceil_div(r[i]->P.extent(), kTM) * ceil_div(r[i]->Q.extent(), 128);
+        if (r[i]->p.nk > most) most = r[i]->p.nk;
+        if (r[i]->p.nk < least) least = r[i]->p.nk;
+    }
+    const int split = tile_split(tiles, least, round);
+    const double chunks = (double)ceil_div(most, split), fill = (double)(tiles * split) / sm_count();
+    if (round) return (double)ceil_div(tiles * split, sm_count()) * (1.4 * chunks + 4);
+    return (fill > 1 ? fill : 1) * chunks + 4;
+}
+
+// Which kernel, by these estimates. Whole passes (us, pair / tile): fp32 forward 2048 x 2048 -> 2048 84 / 109,
+// 1024 x 2048 -> 1024 45 / 35, backward of 1021 x 1000 -> 1363 58 / 56; bf16 forward 2048 x 2048 -> 2048 17 / 24,
+// 700 x 4096 -> 2000 24 / 22, 1024 x 2048 -> 1024 15 / 13. Two products share a launch unless one has few tiles and a
+// long K loop, which alone is split over more SMs (backward of 128 x 512 -> 8192, together / apart: bf16 49 / 18,
+// fp32 148 / 51).
+cudaError_t launch_linear_products(const LinearProduct* x, int count, bool chained, unsigned int* err, cudaStream_t s) {
     Product r[2];
     const Product* order[2];
-    int64_t tiles = 0;
+    bool wide = true;  // both products have whole tiles
     for (int i = 0; i < count; ++i) {
         r[i] = make_product(x[i], err);
-        const int64_t t = pair_tiles(r[i]);
-        tiles = i > 0 && (t == 0 || tiles == 0) ? 0 : tiles + t;
         order[i] = &r[i];
+        wide = wide && pair_tiles(r[i]) > 0;
     }
     const bool round = r[0].P.planes == 3;
-    // a pair's tile for at least half of the SM pairs
-    if (tiles * 4 >= sm_count()) {
-        if (count == 2 && r[1].P.depth() > r[0].P.depth()) order[0] = &r[1], order[1] = &r[0];
-        return round ? run_pair<128, true>(order, count, chained, s) : run_pair<256, false>(order, count, chained, s);
-    }
-    for (int i = 0; i < count; ++i, chained = true) {
-        if (count == 2 && pair_tiles(r[i]) * 4 >= sm_count()) {  // the other one has a short side
-            const Product* one = &r[i];
-            cudaError_t e = round ? run_pair<128, true>(&one, 1, chained, s) : run_pair<256, false>(&one, 1, chained, s);
-            if (e != cudaSuccess) return e;
-            continue;
+    if (count == 2 && r[1].P.depth() > r[0].P.depth()) order[0] = &r[1], order[1] = &r[0];
+    const double never = 1e30, pair = wide ? pair_time(order, count) : never;
+    const double tile = wide || count == 1 ? tile_time(order, count, round) : never;
+    if (count == 2) {
+        double apart = round ? 3 : 10;  // the second launch
+        for (int i = 0; i < 2; ++i) {
+            const double a = pair_tiles(*order[i]) > 0 ? pair_time(order + i, 1) : never, b = tile_time(order + i, 1, round);
+            apart += a < b ? a : b;
         }
-        cudaError_t e = r[i].out == TDA_BF16 ? pick_tile<__nv_bfloat16, false>(r[i].P, r[i].Q, r[i].p, chained, s)
-                        : round              ? pick_tile<float, true>(r[i].P, r[i].Q, r[i].p, chained, s)
-                                             : pick_tile<float, false>(r[i].P, r[i].Q, r[i].p, chained, s);
-        if (e != cudaSuccess) return e;
+        if (apart < pair && apart < tile) {
+            for (int i = 0; i < 2; ++i, chained = true) {
+                cudaError_t e = launch_linear_products(x + i, 1, chained, err, s);
+                if (e != cudaSuccess) return e;
+            }
+            return cudaSuccess;
+        }
     }
-    return cudaSuccess;
+    if (pair <= tile) return round ? run_pair<128, true>(order, count, chained, s) : run_pair<256, false>(order, count, chained, s);
+    return round ? pick_tile<true>(order, count, chained, s) : pick_tile<false>(order, count, chained, s);
 }
 
 }  // namespace tda

@@ -182,7 +182,8 @@ def test_linear_backward(dev, case, dtype, gt):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_linear_backward_parts(dev, dtype):
-    """Each output alone gives what it gives with the others; an empty batch scales what is there."""
+    """Each output alone gives what it gives with the others, up to the order of its sums (which may depend on what
+    shares the launch); an empty batch scales what is there."""
     M, di, do = 150, 264, 392
     gen = torch.Generator(device=dev).manual_seed(3)
     mk = lambda *s: torch.randn(s, generator=gen, device=dev).to(dtype)
@@ -200,16 +201,21 @@ def test_linear_backward_parts(dev, dtype):
         return o
 
     full = call(("dX", "dW", "db"))
+    Bd = full["B"].to(F64).abs()
+    bound = {"dX": 2 * product_bound(do, dtype) * (Bd @ W.to(F64).abs()) + 2 * HALF_ULP[dtype] * full["dX"].to(F64).abs(),
+             "dW": 2 * product_bound(M, dtype) * (Bd.t() @ X.to(F64).abs()) + 2 * U * full["dW"].to(F64).abs(),
+             "db": 0 * full["db"].to(F64)}
     for want in (("dX",), ("dW",), ("db",), ()):
         o = call(want)
         assert torch.equal(o["B"], full["B"])
         for w in want:
-            assert torch.equal(o[w], full[w])
+            close(o[w], full[w].to(F64), bound[w])
     # the factor in dY's place
     g = dY.clone()
     dX = torch.empty_like(X)
     tda.tda_linear_backward(L, g, do, Z, do, M, None, 0, W, di, g, do, dX, di, None, 0, None, tda.TDA_F32, 0.0, ws, wsb)
-    assert torch.equal(g, full["B"]) and torch.equal(dX, full["dX"])
+    assert torch.equal(g, full["B"])
+    close(dX, full["dX"].to(F64), bound["dX"])
     # no tokens
     dW, db = full["dW"].clone(), full["db"].clone()
     tda.tda_linear_backward(L, None, do, None, do, 0, None, di, None, di, None, do, None, di, dW, di, db, tda.TDA_F32,
