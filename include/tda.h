@@ -8,7 +8,9 @@
  * and operation between factored, materialised and Gram forms (dattri-LLM
  * paper, Sec. 3.2 and App. A.2, A.4, B.2, B.3). It also computes routed
  * per-example gradient norms and cosine scores, token-level score
- * decompositions and random-mask reductions from the same factors.
+ * decompositions and random-mask reductions from the same factors, and runs the
+ * parts of a training step that make them (linear layers with their backward pass,
+ * embedding, gradient clipping; last section).
  *
  * Notation. A linear layer z = W a has W in R^{N_o x N_i}. For one example with
  * T token positions the paper's factors are a in R^{N_i x T} and g = Dz in
@@ -561,7 +563,7 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  *   Z     [M][d_out] pre-activation for tda_linear_backward, or NULL (ld_z >= d_out).
  * Every tensor is of type L->dtype. Sums are fp32 (bf16: products of bf16 values,
  * exact; fp32: every product to 2^-24), one rounding per output; act is applied to
- * the unrounded sum. Activations: TDA_ACT_GELU is z Phi(z) (the normal
+ * the unrounded sum, for bf16 layers with functions good to about 2^-20. Activations: TDA_ACT_GELU is z Phi(z) (the normal
  * distribution function), TDA_ACT_GELU_TANH its tanh approximation,
  * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.
  *
