@@ -563,8 +563,9 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  *   Z     [M][d_out] pre-activation for tda_linear_backward, or NULL (ld_z >= d_out).
  * Every tensor is of type L->dtype. Sums are fp32 (bf16: products of bf16 values,
  * exact; fp32: every product to 2^-24), one rounding per output; act is applied to
- * the unrounded sum, for bf16 layers with functions good to about 2^-20. Activations: TDA_ACT_GELU is z Phi(z) (the normal
- * distribution function), TDA_ACT_GELU_TANH its tanh approximation,
+ * the unrounded sum, for bf16 layers with functions good to about 2^-20.
+ * Activations: TDA_ACT_GELU is z Phi(z) (the normal distribution function),
+ * TDA_ACT_GELU_TANH its tanh approximation,
  * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.
  *
  * tda_linear_backward -- the layer's gradients, given dY (the gradient of the loss
@@ -581,7 +582,8 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  *   grad_dtype   type of dW and db: TDA_F32, or TDA_BF16 for bf16 layers
  *                (TDA_ERR_UNSUPPORTED for fp32 layers).  beta 0 overwrites.
  *
- * A padded token is a zero row of dY. M may be 0 (dW and db become beta times
+ * A padded token is a zero row of dY: B is zero where dY is, whatever Z holds there
+ * (its row of X must be finite, as a zero times NaN is NaN in dW). M may be 0 (dW and db become beta times
  * themselves). ws: scratch, 256-byte aligned. tda_linear_workspace_size(op, L, M)
  * bytes are enough when every tensor starts on 16 bytes and every stride is its
  * row length, or any multiple of 8 elements that is no shorter; for any other

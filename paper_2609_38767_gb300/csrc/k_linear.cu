@@ -130,7 +130,8 @@ __global__ void __launch_bounds__(kFacThreads, 4) factor_kernel(const __grid_con
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     float v = to_f(g[u].v[i]);
-                    if (ACT != TDA_ACT_NONE) v *= act_slope<ACT, sizeof(T) == 2>(to_f(z[u].v[i]));
+                    // a padded token (a zero of dY) has a zero factor whatever its Z holds
+                    if (ACT != TDA_ACT_NONE && v != 0.f) v *= act_slope<ACT, sizeof(T) == 2>(to_f(z[u].v[i]));
                     sum[i] += v;
                     set_f(&b.v[i], v);
                 }

@@ -383,3 +383,46 @@ def test_linear_in_a_graph(dev):
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(t, w) for t, w in zip((Y, Z, B, dX, dW, db), want))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_linear_padded_rows_with_non_finite_z(dev, act, dtype):
+    """A padded token's pre-activation may hold anything: its factor is zero, and so is its share of dX, dW, db."""
+    M, di, do = 90, 136, 200
+    mk = lambda *s: torch.randn(s, device=dev).to(dtype)
+    dY, Z, X, W = mk(M, do), mk(M, do), mk(M, di), mk(do, di)
+    dY[7::9] = 0
+    clean = Z.clone()
+    Z[7], Z[16], Z[25] = float("nan"), float("inf"), float("-inf")
+    L = tda.LinearDesc(di, do, ACTS.index(act), KIND[dtype])
+    ws, wsb = ws_for(tda.TDA_LINEAR_BACKWARD, L, M, dev, False)
+    got = []
+    for z in (Z, clean):
+        B, dX, dW, db = torch.empty_like(dY), torch.empty_like(X), torch.empty(do, di, device=dev), torch.empty(do, device=dev)
+        tda.tda_linear_backward(L, dY, do, z, do, M, X, di, W, di, B, do, dX, di, dW, di, db, tda.TDA_F32, 0.0, ws, wsb)
+        got.append((B, dX, dW, db))
+    assert bool((got[0][0][7::9] == 0).all())
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_linear_offsets_past_32_bits(dev):
+    """Tall views in wide rows: elements more than 2^31 from the tensors' starts, both passes."""
+    M, di, do, ld = 270_000, 64, 40, 8192
+    gen = torch.Generator(device=dev).manual_seed(1)
+    wide = lambda n: torch.empty((M, ld), dtype=torch.bfloat16, device=dev)[:, :n]
+    X, Y, dX = wide(di), wide(do), wide(di)
+    X.copy_(torch.randn((M, di), generator=gen, device=dev))
+    W = (torch.randn((do, di), generator=gen, device=dev) / 8).bfloat16()
+    L = tda.LinearDesc(di, do, tda.TDA_ACT_NONE, tda.TDA_BF16)
+    tda.tda_linear_forward(L, X, ld, M, W, di, None, None, 0, Y, ld)
+    tda.tda_device_status()
+    ref = X.to(F64) @ W.to(F64).t()
+    close(Y, ref, product_bound(di, torch.bfloat16) * (X.to(F64).abs() @ W.to(F64).abs().t()) + 1.01 * 2.0 ** -8 * ref.abs()
+          + 1e-4, 2.4e-3)
+    ws, wsb = ws_for(tda.TDA_LINEAR_BACKWARD, L, M, dev, False)
+    tda.tda_linear_backward(L, Y, ld, None, 0, M, None, 0, W, di, None, 0, dX, ld, None, 0, None, tda.TDA_F32, 0.0, ws, wsb)
+    tda.tda_device_status()
+    ref = Y.to(F64) @ W.to(F64)
+    close(dX, ref, product_bound(do, torch.bfloat16) * (Y.to(F64).abs() @ W.to(F64).abs()) + 1.01 * 2.0 ** -8 * ref.abs()
+          + 1e-4, 2.4e-3)
