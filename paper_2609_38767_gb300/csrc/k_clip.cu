@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 8192;  // elements per unit of work: 16 or 32 KiB
-constexpr int kMaxTensors = 512;  // tensors of one launch: their table travels in the kernel's parameters (16 KiB)
+constexpr int kMaxTensors = 256;  // tensors of one launch: their table travels in the kernel's parameters (8 KiB)
 
 struct ClipTensor {
     const void* in;
@@ -36,7 +36,7 @@ struct ClipTensor {
 };
 constexpr int64_t kBf16Bit = (int64_t)1 << 62;
 
-constexpr int kMaxGrid = 2048;    // CTAs of one launch
+constexpr int kMaxGrid = 1280;    // CTAs of one launch: eight per SM of 160
 struct ClipTable {
     ClipTensor t[kMaxTensors];
     int32_t count;
@@ -153,26 +153,30 @@ __global__ void __launch_bounds__(kThreads) clip_squares_kernel(const __grid_con
     }
 }
 
+// A whole, aligned chunk's share of a thread: 4 (bf16) or 8 accesses of 16 bytes.
+template <typename T>
+constexpr int kPieces = kChunk * (int)sizeof(T) / 16 / kThreads;
+
+template <typename T>
+__device__ __forceinline__ void chunk_load(const T* g, uint4* r) {
+#pragma unroll
+    for (int u = 0; u < kPieces<T>; ++u) r[u] = __ldcs((const uint4*)g + u * kThreads + threadIdx.x);
+}
+template <typename T>
+__device__ __forceinline__ void chunk_store(T* out, const uint4* r, float c) {
+    constexpr int E = 16 / sizeof(T);
+#pragma unroll
+    for (int u = 0; u < kPieces<T>; ++u) {
+        float v[E];
+        unpack(r[u], v, out);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] *= c;
+        __stcs((uint4*)out + u * kThreads + threadIdx.x, pack(v, out));
+    }
+}
+// A ragged end, or a tensor that is not aligned.
 template <typename T>
 __device__ __forceinline__ void chunk_scale(const T* g, T* out, int n, float c) {
-    constexpr int E = 16 / sizeof(T), kVecs = kChunk / E, kPer = kVecs / kThreads, U = kPer;
-    if (n == kChunk && (((uintptr_t)g | (uintptr_t)out) & 15) == 0) {
-#pragma unroll
-        for (int j = 0; j < kPer; j += U) {
-            uint4 r[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) r[u] = __ldcs((const uint4*)g + (j + u) * kThreads + threadIdx.x);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                float v[E];
-                unpack(r[u], v, g);
-#pragma unroll
-                for (int e = 0; e < E; ++e) v[e] *= c;
-                __stcs((uint4*)out + (j + u) * kThreads + threadIdx.x, pack(v, g));
-            }
-        }
-        return;
-    }
     for (int i = threadIdx.x; i < n; i += 8 * kThreads) {
         float v[8];
 #pragma unroll
@@ -186,6 +190,31 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* out, int n, float c) 
 // n_part partials of all launches of clip_squares_kernel. norm_out is written by the last table's first CTA.
 __global__ void __launch_bounds__(kThreads)
 clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n_part, float max_norm, float* norm_out) {
+    const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
+    int t = T.first_of[blockIdx.x + 1];  // the next CTA's first tensor: this CTA's last one or the one after it
+    // chunk k: its tensor, elements, and whether it goes by whole accesses
+    auto find = [&](int64_t k, const ClipTensor** x, int64_t* off, int* n) {
+        while (t > 0 && (T.t[t].first & ~kBf16Bit) > k) --t;
+        *x = &T.t[t];
+        *off = (k - (T.t[t].first & ~kBf16Bit)) * kChunk;
+        const int64_t left = T.t[t].n - *off;
+        *n = left < kChunk ? (int)left : kChunk;
+        return *n == kChunk && (((uintptr_t)T.t[t].in | (uintptr_t)T.t[t].out) & 15) == 0;
+    };
+    const ClipTensor* x = nullptr;
+    int64_t off = 0;
+    int n = 0;
+    uint4 r[kPieces<float>];
+    auto load = [&]() {
+        if (x->first & kBf16Bit)
+            chunk_load((const __nv_bfloat16*)x->in + off, r);
+        else
+            chunk_load((const float*)x->in + off, r);
+    };
+    // The first chunk is read while the sums are still being taken, which write none of it (nor does any CTA here
+    // write another's chunks).
+    bool whole = false;
+    if (c1 > c0 && (whole = find(c1 - 1, &x, &off, &n))) load();
     chain_wait();
     chain_next();
     double d = 0.0;
@@ -198,25 +227,35 @@ clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < kThreads / 32; ++i) d += w[i];
-        const double norm = sqrt(d);
+        // fp32 where the sum is an fp32 number (an fp64 root and quotient take a microsecond on these SMs);
         // a NaN norm is not <= max_norm and passes into every output
-        coef = norm <= (double)max_norm ? 1.f : (float)((double)max_norm / norm);
-        if (norm_out && blockIdx.x == 0) *norm_out = (float)norm;
+        float norm;
+        if (d > 1e-30 && d < 1e30) {
+            norm = sqrtf((float)d);
+            coef = norm <= max_norm ? 1.f : max_norm / norm;
+        } else {
+            const double exact = sqrt(d);
+            norm = (float)exact;
+            coef = exact <= (double)max_norm ? 1.f : (float)((double)max_norm / exact);
+        }
+        if (norm_out && blockIdx.x == 0) *norm_out = norm;
     }
     __syncthreads();
     const float c = coef;
-    const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
-    if (c1 <= c0) return;
-    int t = T.first_of[blockIdx.x + 1];  // the next CTA's first tensor: this CTA's last one or the one after it
     for (int64_t k = c1 - 1; k >= c0; --k) {
-        while ((T.t[t].first & ~kBf16Bit) > k) --t;
-        if (!T.t[t].out || (c == 1.f && T.t[t].out == T.t[t].in)) continue;  // norm only, or nothing changes in place
-        const int64_t off = (k - (T.t[t].first & ~kBf16Bit)) * kChunk, left = T.t[t].n - off;
-        const int n = left < kChunk ? (int)left : kChunk;
-        if (T.t[t].first & kBf16Bit)
-            chunk_scale((const __nv_bfloat16*)T.t[t].in + off, (__nv_bfloat16*)T.t[t].out + off, n, c);
-        else
-            chunk_scale((const float*)T.t[t].in + off, (float*)T.t[t].out + off, n, c);
+        if (k < c1 - 1) whole = find(k, &x, &off, &n);
+        if (!x->out || (c == 1.f && x->out == x->in)) continue;  // norm only, or nothing changes in place
+        if (whole) {
+            if (k < c1 - 1) load();
+            if (x->first & kBf16Bit)
+                chunk_store((__nv_bfloat16*)x->out + off, r, c);
+            else
+                chunk_store((float*)x->out + off, r, c);
+        } else if (x->first & kBf16Bit) {
+            chunk_scale((const __nv_bfloat16*)x->in + off, (__nv_bfloat16*)x->out + off, n, c);
+        } else {
+            chunk_scale((const float*)x->in + off, (float*)x->out + off, n, c);
+        }
     }
 }
 
@@ -248,9 +287,11 @@ bool next_table(const tda_tensor_ref* list, int64_t n_tensors, int64_t* i, int64
         T->chunks += (r.n + kChunk - 1) / kChunk;
     }
     *grid = T->chunks < 1 ? 1 : T->chunks < most ? T->chunks : most;
+    // CTA b starts at chunk floor(chunks b / grid)
+    const int64_t step = T->chunks / *grid, rem = T->chunks % *grid;
     int t = 0;
-    for (int64_t b = 0; b <= *grid; ++b) {
-        const int64_t c = T->chunks * b / *grid;
+    for (int64_t b = 0, c = 0, over = 0; b <= *grid; ++b, c += step, over += rem) {
+        if (over >= *grid) over -= *grid, ++c;
         while (t + 1 < T->count && (T->t[t + 1].first & ~kBf16Bit) <= c) ++t;
         T->first_of[b] = (uint16_t)t;
     }
@@ -271,18 +312,22 @@ cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, floa
     int64_t most = (int64_t)sm_count() * kClipCtasPerSm, grid;
     if (most > kMaxGrid) most = kMaxGrid;
     ClipTable T;
-    int n_part = 0;
-    bool chained = false;
-    for (int64_t i = 0; next_table(list, n_tensors, &i, most, &T, &grid); chained = true) {
-        cudaError_t e = launch_chained(chained, clip_squares_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T,
+    int n_part = 0, tables = 0;
+    for (int64_t i = 0; next_table(list, n_tensors, &i, most, &T, &grid); ++tables) {
+        cudaError_t e = launch_chained(tables > 0, clip_squares_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T,
                                        part + n_part);
         if (e != cudaSuccess) return e;
         n_part += (int)grid;
+        if (i == n_tensors && tables == 0) {  // one table: it serves the scaling as well
+            return launch_chained(true, clip_scale_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T, part, n_part,
+                                  max_norm, norm);
+        }
     }
-    bool first = true;
-    for (int64_t i = 0; next_table(list, n_tensors, &i, most, &T, &grid) || first; first = false, chained = true) {
-        cudaError_t e = launch_chained(chained, clip_scale_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T, part,
-                                       n_part, max_norm, first ? norm : nullptr);
+    int64_t i = 0;
+    for (int k = 0; k < tables || k == 0; ++k) {  // without a tensor: one CTA, for the norm
+        next_table(list, n_tensors, &i, most, &T, &grid);
+        cudaError_t e = launch_chained(tables > 0, clip_scale_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T, part,
+                                       n_part, max_norm, k == 0 ? norm : nullptr);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

@@ -313,3 +313,31 @@ def test_train_ops_capture_in_a_graph(dev):
     g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(x, w) for x, w in zip((out, dE, clipped, norm), want))
+
+
+def test_grad_clip_many_tables(dev):
+    """More tensors than one launch holds, empty ones among them, some left unclipped."""
+    gen = torch.Generator(device=dev).manual_seed(9)
+    ts = [torch.randn(0 if i % 7 == 3 else 1 + 37 * (i % 50), generator=gen, device=dev) for i in range(900)]
+    outs = [None if i % 11 == 5 else torch.full_like(t, 9.0) for i, t in enumerate(ts)]
+    want = ref_norm(ts)
+    norm = clip(ts, 2.0, outs, dev)
+    assert abs(float(norm) - want) <= 20 * U * want
+    c = 2.0 / want
+    for t, o in zip(ts, outs):
+        if o is not None:
+            assert bool(((o.double() - c * t.double()).abs() <= 24 * U * (c * t.double()).abs()).all())
+
+
+def test_embedding_backward_long_table(dev):
+    """Gradient rows more than 2^31 elements from the table's start, short and long lists of tokens."""
+    V, d = 540_000, 4096
+    dE = torch.empty((V, d), dtype=torch.bfloat16, device=dev)
+    gen = torch.Generator(device=dev).manual_seed(4)
+    for n in (600, 9000):
+        tok = torch.randint(V - 50, V, (n,), generator=gen, device=dev)
+        dout = torch.randn((n, d), generator=gen, device=dev).bfloat16()
+        dE.fill_(3.0)
+        run_grad(dout, V, tok, 1.0, torch.bfloat16, dE, 0.0)
+        assert bool((dE[: V - 50] == 0).all())
+        check_grad(dout, 50, tok - (V - 50), 1.0, torch.bfloat16, dE[V - 50:], 0.0, torch.zeros((50, d), device=dev))
