@@ -10,6 +10,7 @@ so there is no silent CPU path.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 import threading
 
@@ -393,22 +394,45 @@ def tda_linear_workspace_size(op, L, M) -> int:
     return int(b.value)
 
 
+_calls = None
+
+
+def _train():
+    """The extension module that calls the training step's entry points (csrc/fastcall.c), bound to libtda.so."""
+    global _calls
+    if _calls is None:
+        lib = load()
+        try:
+            mod = importlib.import_module("paper_2609_38767_gb300._fast")
+        except ImportError as e:
+            raise ImportError(f"_fast.so is missing: run paper_2609_38767_gb300.build.build() first ({e})") from e
+        addr = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
+        mod.bind(_current_stream, addr(lib.tda_linear_forward), addr(lib.tda_linear_backward),
+                 addr(lib.tda_embedding_forward), addr(lib.tda_embedding_backward), addr(lib.tda_grad_clip))
+        _calls = mod
+    return _calls
+
+
 def tda_linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z=None, ld_z=0, ws=None, ws_bytes=0,
                        stream=None):
-    _check(load().tda_linear_forward(ctypes.byref(L), _ptr(X), ld_x, M, _ptr(W), ld_w, _ptr(bias), _ptr(R), ld_r,
-                                     _ptr(Y), ld_y, _ptr(Z), ld_z, _ptr(ws), ws_bytes, _stream(stream)))
+    st = (_calls or _train()).linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, ws_bytes,
+                                            stream)
+    if st:
+        _check(st)
 
 
 def tda_linear_backward(L, dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B, ld_b, dX, ld_dx, dW, ld_dw, db,
                         grad_dtype=TDA_F32, beta=0.0, ws=None, ws_bytes=0, stream=None):
-    _check(load().tda_linear_backward(ctypes.byref(L), _ptr(dY), ld_dy, _ptr(Z), ld_z, M, _ptr(X), ld_x, _ptr(W), ld_w,
-                                      _ptr(B), ld_b, _ptr(dX), ld_dx, _ptr(dW), ld_dw, _ptr(db), grad_dtype, beta,
-                                      _ptr(ws), ws_bytes, _stream(stream)))
+    st = (_calls or _train()).linear_backward(L, dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B, ld_b, dX, ld_dx, dW, ld_dw,
+                                             db, grad_dtype, beta, ws, ws_bytes, stream)
+    if st:
+        _check(st)
 
 
 def tda_embedding_forward(dtype, E, ld_e, V, d, it, tokens, n, scale, out, ld_out, stream=None):
-    _check(load().tda_embedding_forward(dtype, _ptr(E), ld_e, V, d, it, _ptr(tokens), n, scale, _ptr(out), ld_out,
-                                        _stream(stream)))
+    st = (_calls or _train()).embedding_forward(dtype, E, ld_e, V, d, it, tokens, n, scale, out, ld_out, stream)
+    if st:
+        _check(st)
 
 
 def tda_embedding_workspace_size(V, d, n) -> int:
@@ -417,8 +441,10 @@ def tda_embedding_workspace_size(V, d, n) -> int:
 
 def tda_embedding_backward(dtype, dout, ld_d, V, d, it, tokens, n, scale, grad_dtype, dE, ld_e, beta=0.0, ws=None,
                            ws_bytes=0, stream=None):
-    _check(load().tda_embedding_backward(dtype, _ptr(dout), ld_d, V, d, it, _ptr(tokens), n, scale, grad_dtype,
-                                         _ptr(dE), ld_e, beta, _ptr(ws), ws_bytes, _stream(stream)))
+    st = (_calls or _train()).embedding_backward(dtype, dout, ld_d, V, d, it, tokens, n, scale, grad_dtype, dE, ld_e,
+                                                beta, ws, ws_bytes, stream)
+    if st:
+        _check(st)
 
 
 def tensor_list(tensors, outs=None):
@@ -445,4 +471,6 @@ def tda_grad_clip_workspace_size(refs, n_tensors) -> int:
 
 
 def tda_grad_clip(refs, n_tensors, max_norm, norm, ws, ws_bytes, stream=None):
-    _check(load().tda_grad_clip(refs, n_tensors, max_norm, _ptr(norm), _ptr(ws), ws_bytes, _stream(stream)))
+    st = (_calls or _train()).grad_clip(refs, n_tensors, max_norm, norm, ws, ws_bytes, stream)
+    if st:
+        _check(st)

@@ -2,6 +2,7 @@
 
 libtda.so        -- the attribution hot path (include/tda.h)
 libtda_synth.so  -- the seeded synthetic-factor generator (include/tda_synth.h)
+_fast.so         -- the extension module that calls the training step's entry points
 
 Translation units compile in parallel into ``_build/`` and are linked with
 ``nvcc -shared`` next to this file. A library is rebuilt when any of its
@@ -13,6 +14,7 @@ import concurrent.futures as cf
 import glob
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -72,6 +74,20 @@ def build_synth_cpu() -> str:
     return target
 
 
+def build_fast() -> str:
+    """gcc build of the extension module _fast (csrc/fastcall.c)."""
+    src = os.path.join(CSRC, "fastcall.c")
+    target = lib_path("_fast.so")
+    if _stale(target, [src] + _headers()):
+        cmd = ["gcc", "-O2", "-std=gnu11", "-fPIC", "-shared", "-Wall", f"-I{sysconfig.get_paths()['include']}",
+               "-o", target + ".tmp", src]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"gcc failed for {src}:\n{r.stderr}")
+        os.replace(target + ".tmp", target)
+    return target
+
+
 def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, str]:
     """Build every library that is out of date; returns {name: path}."""
     os.makedirs(BUILD, exist_ok=True)
@@ -93,6 +109,7 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
                     print("built", target)
             out[name] = target
     out["libtda_synth_cpu.so"] = build_synth_cpu()
+    out["_fast.so"] = build_fast()
     return out
 
 

@@ -130,3 +130,18 @@ def test_linear_backward_refusals():
         assert bwd(**k) == BAD, k
     assert bwd(L=layer(act=1, dtype=tda.TDA_F32), gt=tda.TDA_BF16) == UNSUPPORTED
     assert bwd(wsb=100) == WORKSPACE and bwd(ws=None) == WORKSPACE
+
+
+def test_calls_with_arguments_of_the_wrong_kind():
+    """The binding converts before it calls: a Python error, and nothing reaches the library."""
+    for bad in (dict(E="x"), dict(ld_e=1.5), dict(n=None), dict(scale="a"), dict(tok=object()), dict(V=1 << 70)):
+        k = dict(dtype=tda.TDA_BF16, E=256, ld_e=8, V=4, d=8, it=tda.TDA_I32, tok=256, n=3, scale=1.0, out=256, ld_out=8)
+        k.update(bad)
+        with pytest.raises((TypeError, AttributeError, OverflowError)):
+            tda.tda_embedding_forward(*k.values(), stream=0)
+    with pytest.raises(TypeError):
+        tda.tda_linear_forward(3, 256, 64, 1, 256, 64, None, None, 0, 256, 32, stream=0)
+    with pytest.raises(ValueError):  # more tensors than the list holds
+        tda.tda_grad_clip(ref(), 2, 1.0, 256, 256, 1 << 20, stream=0)
+    with pytest.raises(tda.TdaError):  # no descriptor: the library's own refusal
+        tda.tda_linear_forward(None, 256, 64, 1, 256, 64, None, None, 0, 256, 32, stream=0)
