@@ -16,9 +16,8 @@
 // in order. Rows of E that no token names are cleared (or scaled by beta) by
 // further CTAs: of the sums' launch, or, for short lists, of the sort's. Bound by
 // HBM: n rows read, V rows written. Sums are fp32, rounded once to dE's type.
-// 65536 rows into 131072 x 4096 bf16 (1.6 GB): 313 us = 5.1 TB/s, of which the
-// sums and the clearing take 265 (6.1 TB/s); 4096 rows into 32000 x 2048 fp32
-// (279 MB): 60 us = 4.6 TB/s, the clearing alone 38.
+// 65536 rows into 131072 x 4096 bf16 (1.6 GB): 273 us = 5.9 TB/s; 4096 rows into
+// 32000 x 2048 fp32 (279 MB): 54 us = 5.2 TB/s, the clearing alone 38.
 #include <cuda_bf16.h>
 
 #include "tda_internal.cuh"
@@ -279,8 +278,11 @@ digit_scatter_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key
 }
 
 // ------------------------------------------------------------------ sums over the sorted list
-// kZeroRows: rows that a clearing CTA looks up and clears (8, 16, 32: the large case above 318, 323, 335 us).
-constexpr int kSumThreads = 128, kBatch = 8, kZeroRows = 8;
+// kZeroRows: rows that a clearing CTA looks up and clears (8, 16, 32: 318, 323, 335 us for the large case above, then).
+// kBatch: rows whose loads are in flight per thread, kSumCtas: CTAs meant for an SM, which caps the registers. Eight
+// rows in 64 registers spilled (313 us); four rows and nine CTAs run without (274; 8 CTAs 277, 12 331; three rows
+// and ten CTAs 275, two rows and twelve 283).
+constexpr int kSumThreads = 128, kBatch = 4, kZeroRows = 8, kSumCtas = 9;
 
 struct GradParams {
     int64_t n, d, ld_d, V, ld_e, dp;  // dp: row length of the partials
@@ -309,7 +311,7 @@ __device__ __forceinline__ void store_row(TO* p, const float* acc, float scale, 
 }
 
 template <typename TI, typename TO, int N>
-__global__ void __launch_bounds__(kSumThreads, 8)
+__global__ void __launch_bounds__(kSumThreads, kSumCtas)
 grad_sum_kernel(const TI* __restrict__ dout, TO* __restrict__ dE, const GradParams p) {
     chain_wait();
     chain_next();
@@ -482,7 +484,7 @@ __global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(TO* __restrict_
         }
         return a;
     };
-    constexpr int kLong = 4 * kJoinWarps;
+    constexpr int kLong = 2 * kJoinWarps;  // partials from which a run is shared (4 x: 275 us, 2 x: 273)
     int seen = 0;
     for (int c = 0; c < kJoinChunks; ++c) {
         const int parts = parts_of[c];
