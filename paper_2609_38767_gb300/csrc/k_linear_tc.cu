@@ -255,7 +255,7 @@ __device__ __forceinline__ void activate(int act, float (*v)[4]) {
 #undef TDA_ACT_CASE
 }
 
-// Four sums of output row m, columns n .. n + 3, a value at a time: edges and unaligned outputs.
+// Four sums of output row m, columns n .. n + 3, a value at a time: the last columns of aligned rows.
 template <typename T>
 __device__ __noinline__ void finish_edge(const LinearEpilogue& e, int64_t m, int64_t n, float x0, float x1, float x2,
                                          float x3) {
@@ -275,28 +275,28 @@ __device__ __noinline__ void finish_edge(const LinearEpilogue& e, int64_t m, int
     }
 }
 
-// U groups of four sums through the epilogue and out: group u is output row m[u], columns n[u] .. + 3
-// (SAME_N: one column group for all), inside the output where ok[u]. All loads come before the first store.
-template <typename T, int U, bool SAME_N>
+// U groups of four sums through the epilogue and out: group u is output row m[u], columns n[u] .. + 3, inside the
+// output where ok[u]. All loads come before the first store.
+template <typename T, int U>
 __device__ __forceinline__ void finish(const LinearEpilogue& e, const int64_t* m, const int64_t* n, const bool* ok,
                                        float (*v)[4]) {
     bool whole[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        whole[u] = ok[u] && e.vec && n[u] + 4 <= e.N;
+        whole[u] = ok[u] && n[u] + 4 <= e.N;
         if (ok[u] && !whole[u]) finish_edge<T>(e, m[u], n[u], v[u][0], v[u][1], v[u][2], v[u][3]);
     }
     float r[U][4], b[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (e.R && whole[u]) ld4((const T*)e.R + m[u] * e.ld_r + n[u], r[u]);
-        if (e.bias && (SAME_N ? u == 0 && n[0] + 4 <= e.N && e.vec : whole[u])) ld4((const T*)e.bias + n[u], b[u]);
+        if (e.bias && whole[u]) ld4((const T*)e.bias + n[u], b[u]);
     }
     if (e.bias)
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[u][i] += b[SAME_N ? 0 : u][i];
+            for (int i = 0; i < 4; ++i) v[u][i] += b[u][i];
     if (e.Z)
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -310,6 +310,32 @@ __device__ __forceinline__ void finish(const LinearEpilogue& e, const int64_t* m
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (whole[u]) st4((T*)e.Y + m[u] * e.ld_y + n[u], v[u]);
+}
+
+// U sums through the epilogue and out a value at a time, for rows that do not start on an aligned place: sum u is
+// output row m[u], column n[u], inside the output where ok[u]. Neighbouring lanes hold
+// neighbouring columns. All loads come before the first store.
+template <typename T, int U>
+__device__ __forceinline__ void finish_values(const LinearEpilogue& e, const int64_t* m, const int64_t* n, const bool* ok,
+                                              float (*v)[4]) {
+    float r[U], b[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        r[u] = e.R && ok[u] ? ld1((const T*)e.R + m[u] * e.ld_r + n[u]) : 0.f;
+        b[u] = e.bias && n[u] < e.N ? ld1((const T*)e.bias + n[u]) : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        v[u / 4][u % 4] += b[u];
+        if (e.Z && ok[u]) st1((T*)e.Z + m[u] * e.ld_z + n[u], v[u / 4][u % 4]);
+    }
+    activate<T, U / 4>(e.act, v);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (ok[u]) {
+            const float y = v[u / 4][u % 4];
+            st1((T*)e.Y + m[u] * e.ld_y + n[u], e.R ? fmaf(e.r_scale, r[u], y) : y);
+        }
 }
 
 // ---- units of 32 rows x 64 bytes, the grain of the pair kernel's outputs
@@ -596,28 +622,63 @@ __device__ __forceinline__ void tile_body(const TileLaunch& pp) {
         const int groups = kTM * BN / 4, g0 = groups * rank / p.split, g1 = groups * (rank + 1) / p.split;
         const int64_t m0 = p.swap ? j0 : i0, n0 = p.swap ? i0 : j0;
         const uint32_t base = smem_u32(smem);
-        constexpr int U = ROUND ? 4 : 2;
-        for (int g = g0 + threadIdx.x; g < g1; g += U * kThreads) {
-            int64_t m[U], n[U];
-            bool ok[U];
-            float v[U][4];
+        if (p.ep.vec) {
+            constexpr int U = ROUND ? 4 : 2;
+            for (int g = g0 + threadIdx.x; g < g1; g += U * kThreads) {
+                int64_t m[U], n[U];
+                bool ok[U];
+                float v[U][4];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int gu = g + u * kThreads, o = gu * 4 / inner, c = gu * 4 % inner;
-                m[u] = m0 + o, n[u] = n0 + c;
-                ok[u] = gu < g1 && m[u] < p.ep.M && n[u] < p.ep.N;
-                v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0.f;
-                if (!ok[u]) continue;
-                const uint32_t at = base + (uint32_t)(o * stride + c) * 4;
-                for (int r = 0; r < p.split; ++r) {
-                    const float4 x = ld_cluster_f4(map_rank(at, r));
-                    v[u][0] += x.x, v[u][1] += x.y, v[u][2] += x.z, v[u][3] += x.w;
+                for (int u = 0; u < U; ++u) {
+                    const int gu = g + u * kThreads, o = gu * 4 / inner, c = gu * 4 % inner;
+                    m[u] = m0 + o, n[u] = n0 + c;
+                    ok[u] = gu < g1 && m[u] < p.ep.M && n[u] < p.ep.N;
+                    v[u][0] = v[u][1] = v[u][2] = v[u][3] = 0.f;
+                    if (!ok[u]) continue;
+                    const uint32_t at = base + (uint32_t)(o * stride + c) * 4;
+                    for (int r = 0; r < p.split; ++r) {
+                        const float4 x = ld_cluster_f4(map_rank(at, r));
+                        v[u][0] += x.x, v[u][1] += x.y, v[u][2] += x.z, v[u][3] += x.w;
+                    }
                 }
+                if (ROUND || p.ep.f32)
+                    finish<float, U>(p.ep, m, n, ok, v);
+                else
+                    finish<__nv_bfloat16, U>(p.ep, m, n, ok, v);
             }
-            if (ROUND || p.ep.f32)
-                finish<float, U, false>(p.ep, m, n, ok, v);
-            else
-                finish<__nv_bfloat16, U, false>(p.ep, m, n, ok, v);
+        } else {
+            // the sums to this CTA's own tile, whose share of the rows no other CTA reads, and out a value a lane
+            const float* ft = reinterpret_cast<const float*>(smem);
+            if (p.split > 1) {
+                for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
+                    const uint32_t off = (uint32_t)(g * 4 / inner * stride + g * 4 % inner) * 4;
+                    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int r = 0; r < p.split; ++r) {
+                        const float4 x = ld_cluster_f4(map_rank(base + off, r));
+                        t.x += x.x, t.y += x.y, t.z += x.z, t.w += x.w;
+                    }
+                    *reinterpret_cast<float4*>(smem + off) = t;
+                }
+                __syncthreads();
+            }
+            const int lg = p.swap ? 7 : BN == 128 ? 7 : BN == 64 ? 6 : 5;
+            constexpr int U = 8;
+            for (int g = g0 * 4 + threadIdx.x; g < g1 * 4; g += U * kThreads) {
+                int64_t m[U], n[U];
+                bool ok[U];
+                float v[U / 4][4];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int gu = g + u * kThreads, o = gu >> lg, c = gu & ((1 << lg) - 1);
+                    m[u] = m0 + o, n[u] = n0 + c;
+                    ok[u] = gu < g1 * 4 && m[u] < p.ep.M && n[u] < p.ep.N;
+                    v[u / 4][u % 4] = ok[u] ? ft[o * stride + c] : 0.f;
+                }
+                if (ROUND || p.ep.f32)
+                    finish_values<float, U>(p.ep, m, n, ok, v);
+                else
+                    finish_values<__nv_bfloat16, U>(p.ep, m, n, ok, v);
+            }
         }
     }
     __syncwarp();
@@ -671,8 +732,7 @@ struct PairShape {
     static constexpr int kStages = ROUND ? 8 : 6;
     static constexpr uint32_t kUnit = 32 * 64;       // one output unit
     static constexpr uint32_t kBlock = 2 * kUnit;    // two per epilogue warp
-    static constexpr uint32_t kBlockLd = 20;         // floats of a row staged for edges: 16 + 4
-    static_assert(32 * kBlockLd * 4 <= kBlock, "edge staging");
+    static_assert(32 * 32 * 4 <= kBlock, "a unit in fp32");
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kEpiWarps * kBlock + 8 * (2 * kStages + 2 * kAcc<ROUND> + 1) + 16;
     static constexpr uint32_t kCols = 512;  // the SM's whole TMEM: both CTAs' columns start at the same place
     static_assert(kSmem <= 232448, "shared memory per CTA");
@@ -895,27 +955,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             if (lane == 0) pair_arrive(smem_u32(&tempty[use % kAcc<ROUND>]));
             ++use;
         };
-        // 16 columns of this warp's 32 rows, held a row a lane, through shared memory: edges and rows that are not
-        // aligned go out a few values at a time, neighbours by neighbouring lanes
-        auto out = [&](const LinearEpilogue& ep, const float* v, int64_t m0, int64_t n0) {
-            if (lane == 0) bulk_wait_read0();
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4*>(blk + lane * S::kBlockLd + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-            __syncwarp();
-#pragma unroll 1
-            for (int r = lane >> 2; r < 32; r += 8) {
-                int64_t m[1] = {m0 + r}, n[1] = {n0 + (lane & 3) * 4};
-                const bool ok[1] = {m[0] < ep.M && n[0] < ep.N};
-                const float4 x = *reinterpret_cast<const float4*>(blk + r * S::kBlockLd + (lane & 3) * 4);
-                float y[1][4] = {{x.x, x.y, x.z, x.w}};
-                if (ROUND || ep.f32)
-                    finish<float, 1, true>(ep, m, n, ok, y);
-                else
-                    finish<__nv_bfloat16, 1, true>(ep, m, n, ok, y);
-            }
-        };
         bool got = true;
         auto drain = [&](auto G) {
           constexpr int g = decltype(G)::value;
@@ -992,15 +1031,61 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     }
                     send(&pp.tmY[g], y, v, n);
                 };
+                // The same for rows that TMA cannot write: turned by way of shared memory (a row a lane in, columns over
+                // lanes out; 16-byte pieces at places that leave no bank conflict either way) and stored a value a lane:
+                // 4096 x 2048 -> 8191 bf16 89 us (four values a lane, one after the other: 386).
+                auto values = [&](int c) {
+                    constexpr int kPer = 32 / kU, kMask = kU / 4 - 1;  // rows in 128 bytes; pieces of a row, less one
+                    float v[kU];
+                    get(c, v);
+                    auto piece = [](int r, int j) { return r * kU + ((j ^ (r / kPer & kMask)) << 2); };
+                    __syncwarp();  // the unit before has been read
+#pragma unroll
+                    for (int j = 0; j <= kMask; ++j)
+                        *reinterpret_cast<float4*>(blk + piece(lane, j)) =
+                            make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                    __syncwarp();
+                    constexpr int U = ROUND ? 4 : 8;  // accesses in flight, of kPer rows each
+                    const int sub = lane / kU, col = lane % kU;
+                    const int64_t n = n0 + c + col, left = p.ep.M - m0;
+                    const int rows = n < p.ep.N ? (int)(left < 32 ? left : 32) : 0;
+                    const float bias = !kPlain && p.ep.bias && rows > 0 ? ld1((const T*)p.ep.bias + n) : 0.f;
+                    const T* rp = (const T*)p.ep.R + (m0 + sub) * p.ep.ld_r + n;
+                    T *y = (T*)p.ep.Y + (m0 + sub) * p.ep.ld_y + n, *z = (T*)p.ep.Z + (m0 + sub) * p.ep.ld_z + n;
+#pragma unroll 1
+                    for (int r0 = 0; r0 < rows; r0 += U * kPer) {
+                        float x[U / 4][4], r[U];
+                        const int have = (rows - r0 - sub + kPer - 1) / kPer;  // accesses inside the output
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            x[u / 4][u % 4] = blk[(r0 + u * kPer + sub) * kU + (col ^ ((u & kMask) << 2))] + bias;
+                        if (p.ep.R)
+#pragma unroll
+                            for (int u = 0; u < U; ++u) r[u] = u < have ? ld1(rp + u * kPer * p.ep.ld_r) : 0.f;
+                        if (!kPlain && p.ep.Z)
+#pragma unroll
+                            for (int u = 0; u < U; ++u)
+                                if (u < have) st1(z + u * kPer * p.ep.ld_z, x[u / 4][u % 4]);
+                        if (!kPlain) activate<T, U / 4>(p.ep.act, x);
+                        if (p.ep.R)
+#pragma unroll
+                            for (int u = 0; u < U; ++u) x[u / 4][u % 4] = fmaf(p.ep.r_scale, r[u], x[u / 4][u % 4]);
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            if (u < have) st1(y + u * kPer * p.ep.ld_y, x[u / 4][u % 4]);
+                        rp += U * kPer * p.ep.ld_r, y += U * kPer * p.ep.ld_y, z += U * kPer * p.ep.ld_z;
+                    }
+                };
                 if (has_r) load_r(n0);
                 if (!ROUND && !(got = wait_for())) return;
                 if (!p.ep.wide) {
+                    if (lane == 0) bulk_wait_read0();
+                    if (ROUND) {
 #pragma unroll
-                    for (int c = 0; c < kC; c += kU) {
-                        float v[kU];
-                        get(c, v);
-#pragma unroll
-                        for (int i = 0; i < kU; i += 16) out(p.ep, v + i, m0, n0 + c + i);
+                        for (int c = 0; c < kC; c += kU) values(c);
+                    } else {
+#pragma unroll 1
+                        for (int c = 0; c < kC; c += kU) values(c);
                     }
                 } else if (ROUND) {
 #pragma unroll
@@ -1272,13 +1357,13 @@ static int64_t pair_tiles(const Product& x) {
 }
 
 // Estimated times, in chunks of an SM pair (0.36 us; fp32 1.2 us). The pair kernel: its longest list of tiles
-// (pair_tile's order), each its chunks and about two more of set-up, or the time of writing its outputs value by
-// value where rows are not aligned.
+// (pair_tile's order), each its chunks and about two more of set-up. Rows that are not aligned cost little more
+// (4096 x 2048 -> 8191 89 us, -> 8192 81; taken for 8 or 16 chunks more, the tile kernel was chosen where it is
+// slower: 406 x 768 -> 12485 39 us, 28 this way).
 static double pair_time(const Product* const* r, int count) {
-    auto cost = [](const Product& x) { return x.p.nk + (x.p.ep.wide ? 2 : x.P.planes == 3 ? 6 : 16); };
-    const int64_t n = sm_count() / 2, t0 = pair_tiles(*r[0]), c0 = cost(*r[0]);
+    const int64_t n = sm_count() / 2, t0 = pair_tiles(*r[0]), c0 = r[0]->p.nk + 2;
     if (count == 1) return (double)(ceil_div(t0, n) * c0);
-    const int64_t t1 = pair_tiles(*r[1]), c1 = cost(*r[1]), idle = n - t0 % n;
+    const int64_t t1 = pair_tiles(*r[1]), c1 = r[1]->p.nk + 2, idle = n - t0 % n;
     int64_t extra = (c0 + c1 / 2) / c1;
     if (extra > ceil_div(t1, idle)) extra = ceil_div(t1, idle);
     const int64_t left = t1 > extra * idle ? t1 - extra * idle : 0;

@@ -91,6 +91,7 @@ SHAPES = [
     (2500, 384, 2056, 64, 8), (4, 4104, 520, 8, 8), (4, 131, 600, 1, 1), (5, 264, 1000, 0, 0),
     (12, 1003, 301, 2, 0), (16, 4100, 3000, 4, 4), (2, 5000, 64, 0, 0),
     (1500, 1800, 2104, 8, 8), (1601, 1803, 2101, 3, 1),
+    (600, 200, 1363, 0, 0), (2100, 264, 4097, 0, 1), (150, 256, 217, 24, 0), (401, 768, 5001, 0, 0), (1030, 513, 2044, 0, 4),
 ]
 
 
