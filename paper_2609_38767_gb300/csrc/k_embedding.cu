@@ -3,7 +3,8 @@
 // Lookup: out[i] = scale E[t_i]; a padded token (t_i < 0) gives a zero row, an
 // id outside the table (t_i >= V) a NaN row, so that it is seen. Bound by HBM:
 // the rows read plus the rows written. A group of lanes copies up to four
-// vectors per lane of one row, all loads before the first store. 32768 rows of
+// 16-byte vectors per lane of one row (more of the narrower ones that rows of
+// other alignments take), all loads before the first store. 32768 rows of
 // 4096 bf16 values from a table of 131072 (365 MB in all): 62 us = 5.9 TB/s (in
 // CTAs of 256 threads 64, of 512 with half the vectors 73).
 //
@@ -17,7 +18,7 @@
 // further CTAs: of the sums' launch, or, for short lists, of the sort's. Bound by
 // HBM: n rows read, V rows written. Sums are fp32, rounded once to dE's type.
 // 65536 rows into 131072 x 4096 bf16 (1.6 GB): 273 us = 5.9 TB/s; 4096 rows into
-// 32000 x 2048 fp32 (279 MB): 54 us = 5.2 TB/s, the clearing alone 38.
+// 32000 x 2048 fp32 (279 MB): 52 us = 5.4 TB/s, the clearing alone 38.
 #include <cuda_bf16.h>
 
 #include "tda_internal.cuh"
@@ -44,30 +45,34 @@ __device__ __forceinline__ uint32_t sort_key(const I* tok, int64_t i, uint32_t V
 }
 
 // ------------------------------------------------------------------ lookup
-constexpr int kLookThreads = 128, kLookVecs = 4;
+constexpr int kLookThreads = 128;
+// Vectors of `bytes` each that a lane moves: enough bytes in flight for rows of any alignment (20000 rows of 1001 bf16
+// values: 4 vectors 36 us, 8 26, 16 22; of 1001 fp32 values 36, 26, 22; 30000 of 3004 bf16 values 56, 53, 80).
+constexpr int look_vecs(int bytes) { return bytes == 16 ? 4 : bytes == 8 ? 8 : 16; }
 
-// lanes (a power of two <= 32) copy one segment of lanes * kLookVecs vectors of a row.
+// lanes (a power of two <= 32) copy one segment of lanes * kVecs vectors of a row.
 template <typename T, typename I, int N>
 __global__ void __launch_bounds__(kLookThreads)
 lookup_kernel(const T* __restrict__ E, int64_t ld_e, int64_t V, int64_t d, const I* __restrict__ tok, int64_t n,
               float scale, T* __restrict__ out, int64_t ld_out, int lanes, int64_t segs) {
+    constexpr int kVecs = look_vecs(N * (int)sizeof(T));
     const int64_t g = ((int64_t)blockIdx.x * kLookThreads + threadIdx.x) / lanes;
     const int64_t row = g / segs;
     if (row >= n) return;
-    const int64_t v0 = (g % segs) * lanes * kLookVecs + threadIdx.x % lanes, nv = d / N;
+    const int64_t v0 = (g % segs) * lanes * kVecs + threadIdx.x % lanes, nv = d / N;
     const I t = tok[row];
     const bool in = t >= 0 && (uint64_t)t < (uint64_t)V;
-    Vec<T, N> x[kLookVecs];
+    Vec<T, N> x[kVecs];
     if (in) {
         const Vec<T, N>* src = reinterpret_cast<const Vec<T, N>*>(E + (int64_t)t * ld_e);
 #pragma unroll
-        for (int j = 0; j < kLookVecs; ++j)
+        for (int j = 0; j < kVecs; ++j)
             if (v0 + j * lanes < nv) x[j] = src[v0 + j * lanes];
     }
     Vec<T, N>* dst = reinterpret_cast<Vec<T, N>*>(out + row * ld_out);
     const float fill = t < 0 ? 0.f : __int_as_float(0x7fc00000);
 #pragma unroll
-    for (int j = 0; j < kLookVecs; ++j) {
+    for (int j = 0; j < kVecs; ++j) {
         if (v0 + j * lanes >= nv) break;
         Vec<T, N> y;
 #pragma unroll
@@ -84,10 +89,12 @@ constexpr int kRankMax = 8192, kRankThreads = 256;
 
 //
 // With `clear` set the launch also zeroes the gradient's rows, all of them, beside the counting: the few
-// that tokens name are written twice, but no row waits for the sorted list.
+// that tokens name are written twice, but no row waits for the sorted list (85 tokens of 69041 x 256 fp32 19 us; 24
+// with a whole CTA at each row).
 struct ClearParams {
     uint4* p;          // NULL: nothing to clear; rows 16-byte aligned, whole 16-byte vectors
     int64_t rows, vecs, ld;  // vectors of a row, row stride in vectors
+    int log_lanes;           // threads of a row, as a power of two: short rows are cleared several at a time
 };
 constexpr int kClearRows = 16;
 
@@ -98,8 +105,9 @@ rank_kernel(const I* __restrict__ tok, int n, uint32_t V, uint32_t* __restrict__
     if ((int)blockIdx.x >= ctas) {
         chain_next();
         const int64_t r0 = (int64_t)((int)blockIdx.x - ctas) * kClearRows;
-        for (int64_t r = r0; r < r0 + kClearRows && r < clear.rows; ++r)
-            for (int64_t c = threadIdx.x; c < clear.vecs; c += kRankThreads)
+        const int ll = clear.log_lanes, lanes = 1 << ll;
+        for (int64_t r = r0 + (threadIdx.x >> ll); r < r0 + kClearRows && r < clear.rows; r += kRankThreads >> ll)
+            for (int64_t c = threadIdx.x & (lanes - 1); c < clear.vecs; c += lanes)
                 clear.p[r * clear.ld + c] = make_uint4(0, 0, 0, 0);
         return;
     }
@@ -558,9 +566,10 @@ cudaError_t lookup(const T* E, int64_t ld_e, int64_t V, int64_t d, const I* tok,
     int N = (int)((al < bl ? al : bl) / sizeof(T));
     while (d % N) N >>= 1;
     const int64_t nv = d / N;
+    const int vecs = look_vecs(N * (int)sizeof(T));
     int lanes = 1;
-    while (lanes < 32 && (int64_t)lanes * kLookVecs < nv) lanes <<= 1;
-    const int64_t segs = (nv + lanes * kLookVecs - 1) / (lanes * kLookVecs);
+    while (lanes < 32 && (int64_t)lanes * vecs < nv) lanes <<= 1;
+    const int64_t segs = (nv + lanes * vecs - 1) / (lanes * vecs);
     const int64_t per = kLookThreads / lanes;
     // at most 2^31 - 1 CTAs a launch: rows in pieces
     const int64_t most = (((int64_t)1 << 31) - 1) / segs * per;
@@ -680,6 +689,8 @@ cudaError_t launch_embedding_backward(tda_dtype dt, const void* dout, int64_t ld
             clear.rows = V;
             clear.vecs = d * (int64_t)el / 16;
             clear.ld = ld_e * (int64_t)el / 16;
+            clear.log_lanes = 0;
+            while ((1 << clear.log_lanes) < kRankThreads && (1 << clear.log_lanes) < clear.vecs) ++clear.log_lanes;
         }
         cudaError_t e = it == TDA_I64 ? sort_tokens((const int64_t*)tok, n, V, g, clear, (char*)ws, s)
                                       : sort_tokens((const int32_t*)tok, n, V, g, clear, (char*)ws, s);
