@@ -82,8 +82,9 @@ __global__ void __launch_bounds__(kPackThreads) pack_kernel(const __grid_constan
 }
 
 // ------------------------------------------------------------------ factor and bias gradient
-// CTA (x, y): columns of one block x rows of one run. A thread owns N columns and every
-// kRowLanes-th row of the run; the column sums of the rows are added over the row lanes in shared memory.
+// CTA (x, y): columns of one block x rows of one run. A thread owns N columns (side by side and moved at once, or, where
+// rows are not aligned, kColLanes apart and moved one by one: 4096 x 4095 bf16 25 us, with one column a thread 52) and
+// every kRowLanes-th row of the run; the column sums of the rows are added over the row lanes in shared memory.
 constexpr int kFacThreads = 256, kColLanes = 32, kRowLanes = kFacThreads / kColLanes;
 
 struct FactorParams {
@@ -104,12 +105,34 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float
 __device__ __forceinline__ void set_f(float* p, float x) { *p = x; }
 __device__ __forceinline__ void set_f(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-template <typename T, int ACT, int N>
+// have: a thread's columns inside the matrix.
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ Vec<T, N> load_cols(const T* p, int have) {
+    if (VEC) return *reinterpret_cast<const Vec<T, N>*>(p);
+    Vec<T, N> x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x.v[i] = i < have ? p[i * kColLanes] : T(0.f);
+    return x;
+}
+template <typename T, int N, bool VEC>
+__device__ __forceinline__ void store_cols(T* p, const Vec<T, N>& x, int have) {
+    if (VEC) {
+        *reinterpret_cast<Vec<T, N>*>(p) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < have) p[i * kColLanes] = x.v[i];
+    }
+}
+
+template <typename T, int ACT, int N, bool VEC>
 __global__ void __launch_bounds__(kFacThreads, 4) factor_kernel(const __grid_constant__ FactorParams p) {
     constexpr int U = 2;  // rows in flight
     chain_next();
-    const int64_t col = ((int64_t)blockIdx.x * kColLanes + threadIdx.x % kColLanes) * N;
-    const int rl = threadIdx.x / kColLanes;
+    const int lane = threadIdx.x % kColLanes, rl = threadIdx.x / kColLanes;
+    const int64_t col = (int64_t)blockIdx.x * kColLanes * N + lane * (VEC ? N : 1);
+    const int64_t left = (p.N - col + kColLanes - 1) / kColLanes;
+    const int have = VEC ? N : (int)(left < N ? left : N);
     const int64_t r0 = (int64_t)blockIdx.y * p.run, r1 = r0 + p.run < p.M ? r0 + p.run : p.M;
     float sum[N] = {};
     if (col < p.N) {
@@ -119,8 +142,8 @@ __global__ void __launch_bounds__(kFacThreads, 4) factor_kernel(const __grid_con
             for (int u = 0; u < U; ++u) {
                 const int64_t m = r + u * kRowLanes;
                 if (m >= r1) break;
-                g[u] = *reinterpret_cast<const Vec<T, N>*>((const T*)p.dY + m * p.ld_dy + col);
-                if (ACT != TDA_ACT_NONE) z[u] = *reinterpret_cast<const Vec<T, N>*>((const T*)p.Z + m * p.ld_z + col);
+                g[u] = load_cols<T, N, VEC>((const T*)p.dY + m * p.ld_dy + col, have);
+                if (ACT != TDA_ACT_NONE) z[u] = load_cols<T, N, VEC>((const T*)p.Z + m * p.ld_z + col, have);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -135,14 +158,14 @@ __global__ void __launch_bounds__(kFacThreads, 4) factor_kernel(const __grid_con
                     sum[i] += v;
                     set_f(&b.v[i], v);
                 }
-                if (p.B) *reinterpret_cast<Vec<T, N>*>((T*)p.B + m * p.ld_b + col) = b;
+                if (p.B) store_cols<T, N, VEC>((T*)p.B + m * p.ld_b + col, b, have);
             }
         }
     }
     if (!p.sums) return;
     __shared__ float sh[kRowLanes][kColLanes * N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) sh[rl][(threadIdx.x % kColLanes) * N + i] = sum[i];
+    for (int i = 0; i < N; ++i) sh[rl][VEC ? lane * N + i : i * kColLanes + lane] = sum[i];
     __syncthreads();
     for (int c = threadIdx.x; c < kColLanes * N; c += kFacThreads) {
         const int64_t n = (int64_t)blockIdx.x * kColLanes * N + c;
@@ -203,14 +226,14 @@ int64_t factor_run(int64_t M, int64_t N) {
     return run < 32 ? 32 : run;
 }
 
-template <typename T, int N>
+template <typename T, int N, bool VEC>
 void factor_act(int act, const FactorParams& p, dim3 grid, cudaStream_t s) {
     switch (act) {
-        case TDA_ACT_RELU: factor_kernel<T, TDA_ACT_RELU, N><<<grid, kFacThreads, 0, s>>>(p); break;
-        case TDA_ACT_GELU: factor_kernel<T, TDA_ACT_GELU, N><<<grid, kFacThreads, 0, s>>>(p); break;
-        case TDA_ACT_GELU_TANH: factor_kernel<T, TDA_ACT_GELU_TANH, N><<<grid, kFacThreads, 0, s>>>(p); break;
-        case TDA_ACT_SILU: factor_kernel<T, TDA_ACT_SILU, N><<<grid, kFacThreads, 0, s>>>(p); break;
-        default: factor_kernel<T, TDA_ACT_NONE, N><<<grid, kFacThreads, 0, s>>>(p); break;
+        case TDA_ACT_RELU: factor_kernel<T, TDA_ACT_RELU, N, VEC><<<grid, kFacThreads, 0, s>>>(p); break;
+        case TDA_ACT_GELU: factor_kernel<T, TDA_ACT_GELU, N, VEC><<<grid, kFacThreads, 0, s>>>(p); break;
+        case TDA_ACT_GELU_TANH: factor_kernel<T, TDA_ACT_GELU_TANH, N, VEC><<<grid, kFacThreads, 0, s>>>(p); break;
+        case TDA_ACT_SILU: factor_kernel<T, TDA_ACT_SILU, N, VEC><<<grid, kFacThreads, 0, s>>>(p); break;
+        default: factor_kernel<T, TDA_ACT_NONE, N, VEC><<<grid, kFacThreads, 0, s>>>(p); break;
     }
 }
 
@@ -220,13 +243,13 @@ cudaError_t launch_factor(int act, FactorParams p, cudaStream_t s) {
     const bool vec = p.N % kVec == 0 && rows16(p.dY, p.ld_dy, sizeof(T)) &&
                      (act == TDA_ACT_NONE || rows16(p.Z, p.ld_z, sizeof(T))) &&
                      (!p.B || rows16(p.B, p.ld_b, sizeof(T)));
-    const int64_t w = (int64_t)kColLanes * (vec ? kVec : 1);
+    const int64_t w = (int64_t)kColLanes * kVec;
     const dim3 grid((unsigned)((p.N + w - 1) / w), (unsigned)((p.M + p.run - 1) / p.run));
     note_launches(1);
     if (vec)
-        factor_act<T, kVec>(act, p, grid, s);
+        factor_act<T, kVec, true>(act, p, grid, s);
     else
-        factor_act<T, 1>(act, p, grid, s);
+        factor_act<T, kVec, false>(act, p, grid, s);
     return cudaGetLastError();
 }
 
