@@ -8,9 +8,9 @@
 // timing). Both are bound by HBM. The bytes that must move are one read and one
 // write of every element, plus a second read of what the L2 has dropped since
 // the first; the scaling walks the tensors backwards, so it starts with what the
-// sums read last, while that is still in the L2. 537M bf16 values (1.07 GB): 508 us,
-// the sums 158 (6.8 TB/s), the scaling 332 (6.5 TB/s read and written); 2.6M fp32
-// values, which stay in the L2: 10.9 us for both launches.
+// sums read last, while that is still in the L2. 537M bf16 values (1.07 GB): 500 us,
+// the sums 161 (6.7 TB/s), the scaling 325 (6.5 TB/s read and written); 2.6M fp32
+// values, which stay in the L2: 10.4 us for both launches.
 //
 // Sums: a thread adds the squares of one chunk's elements (at most 32) in fp32,
 // and the chunks' sums as an fp32 pair (the rounding error of each addition kept

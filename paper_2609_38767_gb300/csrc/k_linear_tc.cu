@@ -17,8 +17,8 @@
 // of Q, so an operand byte that reaches an SM feeds twice the MMAs; persistent, the
 // epilogue of a tile beside the next tile's MMAs, its outputs by TMA. Bound by the
 // tensor pipe at the clock that the power limit leaves: 8192 x 14336 -> 4096 bf16
-// 540 us = 1.78 PFLOP/s (468 us without loads and epilogue), 4096 x 2048 -> 8192 with
-// tanh-gelu and Z 87-93 us (75 without its epilogue); fp32 2048 x 4096 -> 4096 300 us
+// 515-540 us = 1.78-1.87 PFLOP/s (468 us without loads and epilogue), 4096 x 2048 -> 8192 with
+// tanh-gelu and Z 86-88 us (75 without its epilogue); fp32 2048 x 4096 -> 4096 300 us
 // = 229 TFLOP/s, six bf16 products each.
 //
 // linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a short batch) swap the
