@@ -15,11 +15,11 @@
 // linear_pair_kernel, for products with a tile for most SM pairs: two CTAs of a
 // cluster hold one 256 x BN tile (cta_group::2), each staging 128 rows of P and half
 // of Q, so an operand byte that reaches an SM feeds twice the MMAs; persistent, the
-// epilogue of a tile beside the next tile's MMAs, its outputs by TMA. Bound by the
+// epilogue of a tile beside the next tile's MMAs, bf16 outputs by TMA. Bound by the
 // tensor pipe at the clock that the power limit leaves: 8192 x 14336 -> 4096 bf16
 // 515-540 us = 1.78-1.87 PFLOP/s (468 us without loads and epilogue), 4096 x 2048 -> 8192 with
-// tanh-gelu and Z 86-88 us (75 without its epilogue); fp32 2048 x 4096 -> 4096 300 us
-// = 229 TFLOP/s, six bf16 products each.
+// tanh-gelu and Z 86-88 us (75 without its epilogue); fp32 2048 x 4096 -> 4096 297 us
+// = 231 TFLOP/s, six bf16 products each.
 //
 // linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a short batch) swap the
 // operands, so the long side fills the 128 rows of a tile, and split the K loop over
@@ -744,7 +744,7 @@ struct PairShape {
 struct PairParams {
     TileParams g[2];
     CUtensorMap tmP[2], tmQ[2];
-    CUtensorMap tmY[2], tmZ;  // outputs with 16-byte aligned rows; tmZ: of product 0
+    CUtensorMap tmY[2], tmZ;  // outputs with 16-byte aligned rows, of bf16 operands; tmZ: of product 0
     int64_t tiles[2];  // tiles[1] = 0: one product
     int extra;
     unsigned int* err;
@@ -971,7 +971,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 constexpr int kU = 64 / sizeof(T), E = 16 / sizeof(T);
                 // fp32 outputs of bf16 products are gradients: nothing but beta times themselves is added
                 constexpr bool kPlain = g == 1 || (!ROUND && sizeof(T) == 4);
-                const bool has_r = p.ep.R != nullptr && p.ep.wide;
+                const bool has_r = !ROUND && p.ep.R != nullptr && p.ep.wide;
                 uint4 r[4];
                 auto load_r = [&](int64_t n) {
 #pragma unroll
@@ -1031,9 +1031,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     }
                     send(&pp.tmY[g], y, v, n);
                 };
-                // The same for rows that TMA cannot write: turned by way of shared memory (a row a lane in, columns over
-                // lanes out; 16-byte pieces at places that leave no bank conflict either way) and stored a value a lane:
-                // 4096 x 2048 -> 8191 bf16 89 us (four values a lane, one after the other: 386).
+                // The same without TMA, for rows that it cannot write and for the sums of fp32 operands, which are registers
+                // (4096 x 512 -> 4096 with Z 113 us, by units 136; with a residual 132 / 150): turned by way of shared
+                // memory (a row a lane in, columns over lanes out; 16-byte pieces at places that leave no bank conflict
+                // either way) and stored a value a lane: 4096 x 2048 -> 8191 bf16 89 us (four values a lane, one after
+                // the other: 386).
                 auto values = [&](int c) {
                     constexpr int kPer = 32 / kU, kMask = kU / 4 - 1;  // rows in 128 bytes; pieces of a row, less one
                     float v[kU];
@@ -1045,7 +1047,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         *reinterpret_cast<float4*>(blk + piece(lane, j)) =
                             make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                     __syncwarp();
-                    constexpr int U = ROUND ? 4 : 8;  // accesses in flight, of kPer rows each
+                    constexpr int U = 8;  // accesses in flight, of kPer rows each
                     const int sub = lane / kU, col = lane % kU;
                     const int64_t n = n0 + c + col, left = p.ep.M - m0;
                     const int rows = n < p.ep.N ? (int)(left < 32 ? left : 32) : 0;
@@ -1078,18 +1080,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 };
                 if (has_r) load_r(n0);
                 if (!ROUND && !(got = wait_for())) return;
-                if (!p.ep.wide) {
+                if (ROUND || !p.ep.wide) {
                     if (lane == 0) bulk_wait_read0();
                     if (ROUND) {
 #pragma unroll
-                        for (int c = 0; c < kC; c += kU) values(c);
+                        for (int c = 0; c < kC; c += kU) values(c);  // the sums are registers
                     } else {
 #pragma unroll 1
                         for (int c = 0; c < kC; c += kU) values(c);
                     }
-                } else if (ROUND) {
-#pragma unroll
-                    for (int c = 0; c < kC; c += kU) unit(c);  // the sums are registers
                 } else {
 #pragma unroll 1
                     for (int c = 0; c < kC; c += kU) unit(c);
@@ -1276,8 +1275,9 @@ cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStre
         if (!operand_map(&pp.tmP[i], x.P, kTM) || !operand_map(&pp.tmQ[i], x.Q, BN / 2))
             return cudaErrorInvalidValue;
         const LinearEpilogue& e = x.p.ep;
-        if (e.wide && (!make_out_map(&pp.tmY[i], e.Y, e.M, e.N, e.ld_y, e.f32) ||
-                       (e.Z && !make_out_map(&pp.tmZ, e.Z, e.M, e.N, e.ld_z, e.f32))))
+        if (!ROUND && e.wide &&
+            (!make_out_map(&pp.tmY[i], e.Y, e.M, e.N, e.ld_y, e.f32) ||
+             (e.Z && !make_out_map(&pp.tmZ, e.Z, e.M, e.N, e.ld_z, e.f32))))
             return cudaErrorInvalidValue;
         pp.g[i] = x.p;
         pp.g[i].tiles_p = (x.P.extent() + 2 * kTM - 1) / (2 * kTM);
