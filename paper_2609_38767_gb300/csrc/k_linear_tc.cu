@@ -863,6 +863,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     if (issued[s]) {
                         wait_settled(smem_u32(&full[s]), last_par[s], pp.err);
                     }
+            // and so do the last signals that the pair's MMAs send to this CTA's stages; a signal sent means that both
+            // CTAs' copies into the stage have landed
+            for (int s = 0; s < S::kStages; ++s)
+                if (issued[s]) wait_bounded(smem_u32(&empty[s]), last_par[s], abort, pp.err);
         }
     } else if (warp == 1) {
         if (rank == 0) {
@@ -1129,6 +1133,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         drain(std::integral_constant<int, 0>());
         drain(std::integral_constant<int, 1>());
         if (lane == 0) bulk_wait_all();  // the outputs are written before the CTA exits
+        // The leader's last signal comes to the other CTA too: waited for here, where the last tile is done, as a wait
+        // from the kernel's start would run into its limit in a long launch.
+        if (rank != 0 && warp == 2) wait_settled(smem_u32(mma_done), 0, pp.err);
     }
     __syncwarp();
     tc_fence_before();

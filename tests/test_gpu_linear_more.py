@@ -1,0 +1,61 @@
+"""The linear layer, further: launches that follow each other closely, values at the edges of the activations, long sums,
+several threads. Plain fp64 implementations as in test_gpu_linear.py, whose derived bounds hold here too."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_38767_gb300 as tda
+from paper_2609_38767_gb300 import build as tbuild
+
+pytestmark = pytest.mark.gpu
+
+F64 = torch.float64
+KIND = {torch.float32: tda.TDA_F32, torch.bfloat16: tda.TDA_BF16}
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    tbuild.build()
+    tda.load()
+    return torch.device("cuda:0")
+
+
+def workspace(op, L, M, dev):
+    wsb = tda.tda_linear_workspace_size(op, L, M)
+    return torch.full((max(wsb, 1),), 0x7F, dtype=torch.uint8, device=dev), wsb
+
+
+def test_launches_close_together_repeat_bit_for_bit(dev):
+    """Calls of one or a few tiles per SM pair queued without a pause: each CTA starts where another has just left, so a
+    signal or a copy that outlives its CTA would land in the next one's shared memory."""
+    gen = torch.Generator(device=dev).manual_seed(21)
+    jobs = []
+    for M, di, do, dtype in ((512, 256, 1024, torch.bfloat16), (2048, 128, 2304, torch.bfloat16),
+                             (1024, 192, 1280, torch.float32), (4096, 64, 5120, torch.bfloat16)):
+        mk = lambda *s: torch.randn(s, generator=gen, device=dev).to(dtype)
+        L = tda.LinearDesc(di, do, tda.TDA_ACT_NONE, KIND[dtype])
+        ws, wsb = workspace(tda.TDA_LINEAR_BACKWARD, L, M, dev)
+        jobs.append((L, M, di, do, mk(M, di), mk(do, di), mk(M, do), ws, wsb))
+
+    def run(j):
+        L, M, di, do, X, W, dY, ws, wsb = j
+        Y, dX, dW = torch.empty_like(dY), torch.empty_like(X), torch.empty((do, di), device=dev)
+        tda.tda_linear_forward(L, X, di, M, W, di, None, None, 0, Y, do, None, 0, ws, wsb)
+        tda.tda_linear_backward(L, dY, do, None, 0, M, X, di, W, di, None, 0, dX, di, dW, di, None, tda.TDA_F32, 0.0, ws, wsb)
+        return Y, dX, dW
+
+    first = [run(j) for j in jobs]
+    wrong = torch.zeros(1, dtype=torch.int64, device=dev)
+    for _ in range(40):
+        got = [run(j) for j in jobs]
+        for a, b in zip(first, got):
+            for x, y in zip(a, b):
+                wrong += (x != y).sum()
+    tda.tda_device_status()
+    assert int(wrong) == 0
+    for (L, M, di, do, X, W, *_), (Y, _, _) in zip(jobs, first):
+        ref = X.to(F64) @ W.to(F64).t()
+        assert float((Y.to(F64) - ref).norm() / ref.norm()) <= (2.4e-3 if X.dtype == torch.bfloat16 else 1e-6)

@@ -1,0 +1,61 @@
+"""Rules of the asynchronous kernels that no run can show reliably, held on their source text: what a CTA waits for
+before it exits, and which arguments a kernel may call read-only."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_38767_gb300", "csrc")
+
+
+def source(name):
+    """A file's code without comments."""
+    text = open(os.path.join(CSRC, name)).read()
+    return re.sub(r"/\*.*?\*/", " ", re.sub(r"//[^\n]*", "", text), flags=re.S)
+
+
+def block(text, at):
+    """The text from the first brace after `at` to its partner, and the place after it."""
+    i = text.index("{", at)
+    depth = 0
+    for j in range(i, len(text)):
+        depth += {"{": 1, "}": -1}.get(text[j], 0)
+        if depth == 0:
+            return text[i + 1:j], j + 1
+    raise AssertionError("unbalanced braces")
+
+
+def run_by(body, rank):
+    """What the CTA of `rank` runs of a pair kernel's body: `if (rank == 0)` blocks and `if (rank != 0 ...)`
+    statements resolved."""
+    out, at = "", 0
+    for m in re.finditer(r"if \(rank (==|!=) 0( && [^)]*)?\) ?", body):
+        if m.start() < at:
+            continue
+        out += body[at:m.start()]
+        taken = (rank == 0) == (m.group(1) == "==")
+        if body[m.end()] == "{":
+            inner, at = block(body, m.start())
+        else:  # one statement, itself perhaps with a block
+            semi, brace = body.index(";", m.end()), body.find("{", m.end())
+            at = block(body, m.end())[1] if 0 <= brace < semi else semi + 1
+            if body[m.end():].startswith("for"):
+                at = max(at, block(body, m.end())[1])
+            inner = body[m.end():at]
+        if taken:
+            out += run_by(inner, rank)
+    return out + body[at:]
+
+
+def test_both_ctas_of_a_pair_wait_for_the_signals_sent_to_them():
+    """linear_pair_kernel: the leader's commits arrive on barriers in both CTAs' shared memory (multicast mask 3), so
+    either CTA has to see the last one on `mma_done`, and the last one on each stage's `empty`, before it exits."""
+    text = source("k_linear_tc.cu")
+    assert re.search(r"commit\.cta_group::2[^;]*multicast::cluster", text) and '"h"((uint16_t)3)' in text
+    body, _ = block(text, text.index("linear_pair_kernel("))
+    assert "commit_one<true>(lead, smem_u32(mma_done))" in body
+    end = body.rindex("cluster_sync()")
+    for rank in (0, 1):
+        mine = run_by(body[:end], rank)
+        assert re.search(r"wait_settled\(smem_u32\(mma_done\), 0,", mine), f"rank {rank} leaves mma_done unseen"
+        after = mine[mine.index("feed(std::integral_constant<int, 1>())"):]
+        producer = after[:after.index("} else if (warp == 1)")]
+        assert re.search(r"wait_\w+\(smem_u32\(&empty\[s\]\), last_par\[s\]", producer), f"rank {rank}: empty unseen"
