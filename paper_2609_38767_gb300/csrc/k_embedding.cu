@@ -152,6 +152,9 @@ rank_kernel(const I* __restrict__ tok, int n, uint32_t V, uint32_t* __restrict__
     }
 }
 
+// The kernels from here on start while the launch before them still runs (chain_wait): nothing that it writes may be
+// __restrict__ in them, which would let the compiler read it ahead of the wait. The call's own inputs may be.
+//
 // More tokens: a stable radix sort from the low digit up, digits of at most 9 bits (2 passes up to 2^18 ids),
 // three launches a pass: digit counts per tile, their scan per digit, the scatter.
 // Tiles are small, so that a list of some ten thousand tokens still spreads over the SMs.
@@ -159,8 +162,8 @@ constexpr int kTile = 512, kSortThreads = 256, kBins = 512, kRounds = kTile / kS
 
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
-digit_count_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key, int n, uint32_t V, int shift,
-                   uint32_t mask, uint32_t* __restrict__ hist) {
+digit_count_kernel(const I* __restrict__ tok, const uint32_t* key, int n, uint32_t V, int shift,
+                   uint32_t mask, uint32_t* hist) {
     __shared__ uint32_t h[kBins];
     chain_wait();
     chain_next();
@@ -177,8 +180,7 @@ digit_count_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key, 
 }
 
 // CTA b: exclusive scan of digit b's counts over the tiles, and their total.
-__global__ void __launch_bounds__(kSortThreads) digit_scan_kernel(uint32_t* __restrict__ hist, int tiles,
-                                                                  uint32_t* __restrict__ total) {
+__global__ void __launch_bounds__(kSortThreads) digit_scan_kernel(uint32_t* hist, int tiles, uint32_t* total) {
     __shared__ uint32_t w[kSortThreads / 32];
     chain_wait();
     chain_next();
@@ -211,10 +213,8 @@ __global__ void __launch_bounds__(kSortThreads) digit_scan_kernel(uint32_t* __re
 
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
-digit_scatter_kernel(const I* __restrict__ tok, const uint32_t* __restrict__ key, const int32_t* __restrict__ val,
-                     int n, uint32_t V, int shift, uint32_t mask, const uint32_t* __restrict__ hist,
-                     const uint32_t* __restrict__ total, uint32_t* __restrict__ key_out,
-                     int32_t* __restrict__ val_out) {
+digit_scatter_kernel(const I* __restrict__ tok, const uint32_t* key, const int32_t* val, int n, uint32_t V, int shift,
+                     uint32_t mask, const uint32_t* hist, const uint32_t* total, uint32_t* key_out, int32_t* val_out) {
     constexpr int W = kSortThreads / 32, kPer = kTile / W / 32;
     __shared__ uint32_t pos[W][kBins];  // counts of each warp's run, then the next place of each digit
     __shared__ uint32_t start[kBins];
@@ -320,7 +320,7 @@ __device__ __forceinline__ void store_row(TO* p, const float* acc, float scale, 
 
 template <typename TI, typename TO, int N>
 __global__ void __launch_bounds__(kSumThreads, kSumCtas)
-grad_sum_kernel(const TI* __restrict__ dout, TO* __restrict__ dE, const GradParams p) {
+grad_sum_kernel(const TI* __restrict__ dout, TO* dE, const GradParams p) {
     chain_wait();
     chain_next();
     const int64_t sums = p.chunks * p.col_blocks;
@@ -443,7 +443,7 @@ __device__ __forceinline__ void store_join(const GradParams& p, TO* dE, uint32_t
 constexpr int kJoinChunks = kJoinWarps;
 
 template <typename TO>
-__global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(TO* __restrict__ dE, const GradParams p) {
+__global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(TO* dE, const GradParams p) {
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t none = (uint32_t)p.V;

@@ -177,9 +177,10 @@ __global__ void __launch_bounds__(kFacThreads, 4) factor_kernel(const __grid_con
     }
 }
 
-// db[n] = beta db[n] + sum of the runs' sums, in order.
+// db[n] = beta db[n] + sum of the runs' sums, in order. The factor's launch still writes the sums when this one starts:
+// they are not __restrict__.
 template <typename TG>
-__global__ void bias_grad_kernel(const float* __restrict__ sums, int64_t runs, int64_t N, float beta, TG* db) {
+__global__ void bias_grad_kernel(const float* sums, int64_t runs, int64_t N, float beta, TG* db) {
     chain_wait();
     chain_next();
     const int64_t n = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;

@@ -257,7 +257,8 @@ cudaError_t smem_attr_once(int bytes) {
 // Programmatic dependent launch for the chains of short kernels inside one call: kernel i + 1 is put on the
 // SMs while kernel i still runs and waits (chain_wait) until i has finished and its writes are visible. Every
 // thread of a chained kernel waits before it touches memory, so completion carries along the chain; the first
-// kernel of a call is launched plainly. chain_next lets the next kernel come as soon as all CTAs have started.
+// kernel of a call is launched plainly. What the kernel before writes is not __restrict__ in a chained kernel's
+// arguments, as that would promise that it does not change while the kernel runs. chain_next lets the next kernel come as soon as all CTAs have started.
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -59,3 +59,27 @@ def test_both_ctas_of_a_pair_wait_for_the_signals_sent_to_them():
         after = mine[mine.index("feed(std::integral_constant<int, 1>())"):]
         producer = after[:after.index("} else if (warp == 1)")]
         assert re.search(r"wait_\w+\(smem_u32\(&empty\[s\]\), last_par\[s\]", producer), f"rank {rank}: empty unseen"
+
+
+# What a chained kernel may declare __restrict__: the inputs of the call, which nothing of the call writes.
+INPUTS_OF_CALL = {"digit_count_kernel": {"tok"}, "digit_scatter_kernel": {"tok"}, "grad_sum_kernel": {"dout"}}
+
+
+def test_chained_kernels_promise_nothing_about_the_launch_before():
+    """A kernel that calls chain_wait() is on the SMs while its predecessor still writes. `const __restrict__` would say
+    that the memory does not change during the kernel and allow loads ahead of the wait, and __restrict__ alone that
+    the wait does not concern it."""
+    chained = set()
+    for name in sorted(os.listdir(CSRC)):
+        if not name.endswith((".cu", ".cuh")):
+            continue
+        text = source(name)
+        for m in re.finditer(r"__global__", text):
+            head = text[m.start():text.index("{", m.start())]
+            kernel = re.search(r"(\w+_kernel)\s*\(", head)
+            if not kernel or "chain_wait()" not in block(text, m.start())[0]:
+                continue
+            chained.add(kernel.group(1))
+            promised = set(re.findall(r"__restrict__\s+(\w+)", head))
+            assert promised <= INPUTS_OF_CALL.get(kernel.group(1), set()), (name, kernel.group(1), promised)
+    assert {"bias_grad_kernel", "digit_scan_kernel", "grad_join_kernel", "clip_scale_kernel"} <= chained
