@@ -589,7 +589,9 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  * row length, or any multiple of 8 elements that is no shorter; for any other
  * pointers or strides add TDA_LINEAR_ANY_STRIDE to op. Runs on sm_103 only.
  * An infinite or NaN element of X or W makes the outputs that it enters
- * non-finite (for fp32 layers NaN may stand where infinity would).
+ * non-finite (for fp32 layers NaN may stand where infinity would; relu of -inf is
+ * 0). act(+inf) is +inf, act(-inf) NaN but for relu; act'(Z) of an infinite Z is the
+ * limit, 1 or 0.
  * ------------------------------------------------------------------------- */
 typedef enum {
     TDA_ACT_NONE = 0,

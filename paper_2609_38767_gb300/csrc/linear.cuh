@@ -12,7 +12,8 @@ namespace tda {
 // ------------------------------------------------------------------ activations
 // Values in forms without cancellation or overflow: gelu through the normal tail, the tanh form as
 // z sigmoid(2u) (tanh(u) = 2 sigmoid(2u) - 1). exp of a large argument gives 0 or inf,
-// and 1 / (1 + inf) = 0, so finite z of any size give finite results.
+// and 1 / (1 + inf) = 0, so finite z of any size give finite results. Slopes of an infinite z are their limits,
+// the value of +inf is +inf; the value of -inf is NaN (-inf times 0) but for relu.
 // FAST (bf16 results): the exponential and the reciprocal by the approximate instructions, good to
 // 2^-21 |x| and 2^-22, far below bf16's 2^-8.
 template <bool FAST>
@@ -58,7 +59,7 @@ __device__ __forceinline__ float act_value(float z) {
     if (ACT == TDA_ACT_GELU) {
         float e;
         const float q = normal_tail<FAST>(z, &e);
-        return z > 0.f ? fmaf(-z, q, z) : z * q;
+        return z * (z > 0.f ? 1.f - q : q);  // +inf stays +inf
     }
     if (ACT == TDA_ACT_GELU_TANH) return z * sigmoid<FAST>(1.5957691216057308f * fmaf(0.044715f * z * z, z, z));
     if (ACT == TDA_ACT_SILU) return z * sigmoid<FAST>(z);
@@ -71,7 +72,8 @@ __device__ __forceinline__ float act_slope(float z) {
     if (ACT == TDA_ACT_GELU) {
         float e;
         const float q = normal_tail<FAST>(z, &e);
-        return fmaf(0.39894228040143268f * z, e, z > 0.f ? 1.f - q : q);
+        // past |z| = 20 e is 0: an infinite z has the slope's limit, 0 or 1 (a NaN is one in q)
+        return fmaf(0.39894228040143268f * fminf(fmaxf(z, -20.f), 20.f), e, z > 0.f ? 1.f - q : q);
     }
     if (ACT == TDA_ACT_GELU_TANH) {
         // past |z| = 9.9 the slope is 0 or 1 to fp32, while z^2 or the exponential could overflow;
@@ -83,7 +85,8 @@ __device__ __forceinline__ float act_slope(float z) {
         return z != z ? z : r;
     }
     if (ACT == TDA_ACT_SILU) {
-        const float c = fmaxf(z, -86.f), e = exp_of<FAST>(-c);  // 1 - s = e s; e stays below 2^126
+        // 1 - s = e s; e stays below 2^126, and past z = 86 it is 0 beside 1
+        const float c = fminf(fmaxf(z, -86.f), 86.f), e = exp_of<FAST>(-c);
         const float s = reciprocal<FAST>(1.f + e);
         const float r = s * fmaf(c, e * s, 1.f);
         return z != z ? z : r;

@@ -59,3 +59,37 @@ def test_launches_close_together_repeat_bit_for_bit(dev):
     for (L, M, di, do, X, W, *_), (Y, _, _) in zip(jobs, first):
         ref = X.to(F64) @ W.to(F64).t()
         assert float((Y.to(F64) - ref).norm() / ref.norm()) <= (2.4e-3 if X.dtype == torch.bfloat16 else 1e-6)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M", [1, 40, 2048])
+def test_infinite_pre_activations(dev, M, act, dtype):
+    """Infinities that enter by the bias, through each kernel: +inf passes every activation, -inf leaves relu as 0 and the
+    others not finite; the slopes are the limits 1 and 0 (below 2^-20, the functions' own error)."""
+    di, do = 64, 1024
+    gen = torch.Generator(device=dev).manual_seed(31)
+    mk = lambda *s: torch.randn(s, generator=gen, device=dev).to(dtype)
+    X, W, b, dY = mk(M, di), mk(do, di), mk(do), mk(M, do)
+    up, down = torch.arange(3, do, 29, device=dev), torch.arange(5, do, 31, device=dev)
+    up = up[~torch.isin(up, down)]
+    rest = torch.ones(do, dtype=torch.bool, device=dev)
+    rest[up] = rest[down] = False
+    b[up], b[down] = float("inf"), float("-inf")
+    L = tda.LinearDesc(di, do, ACTS.index(act), KIND[dtype])
+    ws, wsb = workspace(tda.TDA_LINEAR_BACKWARD, L, M, dev)
+    Y, Z, B = torch.empty_like(dY), torch.empty_like(dY), torch.empty_like(dY)
+    tda.tda_linear_forward(L, X, di, M, W, di, b, None, 0, Y, do, Z, do, ws, wsb)
+    tda.tda_linear_backward(L, dY, do, Z, do, M, None, 0, None, 0, B, do, None, 0, None, 0, None, tda.TDA_F32, 0.0, ws, wsb)
+    tda.tda_device_status()
+    inf = float("inf")
+    assert bool((Z[:, up] == inf).all()) and bool((Z[:, down] == -inf).all())
+    assert bool((Y[:, up] == inf).all())
+    assert bool((Y[:, down] == 0).all() if act == "relu" else ~torch.isfinite(Y[:, down]).any())
+    assert bool(torch.isfinite(Y[:, rest]).all()) and bool(torch.isfinite(B).all())
+    limit = dY.clone()
+    if act != "none":
+        limit[:, down] = 0
+    off = (B - limit).to(F64).abs()
+    for cols in (up, down):
+        assert bool((off[:, cols] <= 2.0 ** -20 * dY[:, cols].to(F64).abs()).all())
