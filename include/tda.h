@@ -563,7 +563,9 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  *   Z     [M][d_out] pre-activation for tda_linear_backward, or NULL (ld_z >= d_out).
  * Every tensor is of type L->dtype. Sums are fp32 (bf16: products of bf16 values,
  * exact; fp32: every product to 2^-24), one rounding per output; act is applied to
- * the unrounded sum, for bf16 layers with functions good to about 2^-20.
+ * the unrounded sum, for bf16 layers with functions good to about 2^-20 of max(|z|, 1)
+ * and, where the value itself is small (the tails of gelu and silu), to 2^-11 of it
+ * down to 1e-36.
  * Activations: TDA_ACT_GELU is z Phi(z) (the normal distribution function),
  * TDA_ACT_GELU_TANH its tanh approximation,
  * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.

@@ -15,7 +15,7 @@ namespace tda {
 // and 1 / (1 + inf) = 0, so finite z of any size give finite results. Slopes of an infinite z are their limits,
 // the value of +inf is +inf; the value of -inf is NaN (-inf times 0) but for relu.
 // FAST (bf16 results): the exponential and the reciprocal by the approximate instructions, good to
-// 2^-21 |x| and 2^-22, far below bf16's 2^-8.
+// 2^-21 |x| and 2^-22 of their value, far below bf16's 2^-8 (4096 x 2048 -> 8192 with tanh-gelu and Z 94 -> 93 us).
 template <bool FAST>
 __device__ __forceinline__ float exp_of(float x) {
     if (!FAST) return expf(x);
@@ -35,22 +35,21 @@ __device__ __forceinline__ float sigmoid(float x) {
     return reciprocal<FAST>(1.f + exp_of<FAST>(-x));
 }
 
-// q = Phi(-|z|) and e = exp(-z^2/2). FAST: erfc by formula 7.1.26 of Abramowitz and Stegun, Handbook of
-// Mathematical Functions (absolute error 1.5e-7).
+// q = Phi(-|z|) and e = exp(-z^2/2). FAST: q = e t P(t), t = 1 / (1 + 0.2895 |z|), whose form has the tail's 1 / |z|; P of
+// degree 5 fitted for |z| <= 13.3, past which e is 0, to a relative error of 1.1e-4 (2^-13, below bf16's rounding) in
+// the far tail and an absolute one of 2e-7, fp32's roundings included.
 template <bool FAST>
 __device__ __forceinline__ float normal_tail(float z, float* e) {
     const float a = fabsf(z);
-    if (!FAST) {
-        *e = expf(-0.5f * z * z);
-        return 0.5f * erfcf(0.70710678118654752f * a);
-    }
     *e = exp_of<FAST>(-0.5f * z * z);
-    const float t = reciprocal<FAST>(fmaf(0.3275911f * 0.70710678118654752f, a, 1.f));
-    float s = fmaf(t, 1.061405429f, -1.453152027f);
-    s = fmaf(t, s, 1.421413741f);
-    s = fmaf(t, s, -0.284496736f);
-    s = fmaf(t, s, 0.254829592f);
-    return 0.5f * t * s * *e;
+    if (!FAST) return 0.5f * erfcf(0.70710678118654752f * a);
+    const float t = reciprocal<FAST>(fmaf(0.28948054575753167f, a, 1.f));
+    float s = fmaf(t, -0.0903595890286826f, 0.2922750212769822f);
+    s = fmaf(t, s, -0.10288718530166549f);
+    s = fmaf(t, s, 0.1853646140376046f);
+    s = fmaf(t, s, 0.09875243697672076f);
+    s = fmaf(t, s, 0.11685465736958278f);
+    return t * s * *e;
 }
 
 template <int ACT, bool FAST>

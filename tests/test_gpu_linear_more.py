@@ -93,3 +93,31 @@ def test_infinite_pre_activations(dev, M, act, dtype):
     off = (B - limit).to(F64).abs()
     for cols in (up, down):
         assert bool((off[:, cols] <= 2.0 ** -20 * dY[:, cols].to(F64).abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("M", [1, 24, 1024])
+def test_activation_tails_are_right_in_proportion(dev, M, act, dtype):
+    """W = I, z from -1 down to where the value leaves the normal numbers. bf16: 2^-11 for the functions and half an ulp
+    (2^-8); fp32: the exponential's argument (up to 88) is rounded a few times, 4 * 88 * 2^-24 < 2^-15 of the value."""
+    d = 512
+    z = torch.linspace(-1, -88 if act == "silu" else -13, M * d, dtype=F64).view(M, d).to(device=dev).to(dtype)
+    L = tda.LinearDesc(d, d, ACTS.index(act), KIND[dtype])
+    ws, wsb = workspace(tda.TDA_LINEAR_FORWARD, L, M, dev)
+    Y, Z = torch.empty_like(z), torch.empty_like(z)
+    tda.tda_linear_forward(L, z, d, M, torch.eye(d, device=dev).to(dtype), d, None, None, 0, Y, d, Z, d, ws, wsb)
+    tda.tda_device_status()
+    assert torch.equal(Z, z) or dtype == torch.float32
+    x = Z.to(F64)
+    if act == "gelu":
+        # z Phi(z) by the scaled function, which keeps the tail's digits
+        ref = x * 0.5 * torch.special.erfcx(-x / math.sqrt(2)) * torch.exp(-0.5 * x * x)
+    elif act == "gelu_tanh":
+        ref = x / (1 + torch.exp(-2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3)))
+    else:
+        ref = x / (1 + torch.exp(-x))
+    held = ref.abs() >= 1e-36
+    off = ((Y.to(F64) - ref).abs() / ref.abs())[held]
+    assert int(held.sum()) > 0.6 * held.numel()
+    assert float(off.max()) <= (2.0 ** -8 + 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -15), float(off.max())
