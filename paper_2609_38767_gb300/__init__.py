@@ -407,7 +407,7 @@ def _train():
         except ImportError as e:
             raise ImportError(f"_fast.so is missing: run paper_2609_38767_gb300.build.build() first ({e})") from e
         addr = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
-        mod.bind(_current_stream, addr(lib.tda_linear_forward), addr(lib.tda_linear_backward),
+        mod.bind(_current_stream, LinearDesc, addr(lib.tda_linear_forward), addr(lib.tda_linear_backward),
                  addr(lib.tda_embedding_forward), addr(lib.tda_embedding_backward), addr(lib.tda_grad_clip))
         _calls = mod
     return _calls

@@ -13,7 +13,7 @@
 
 #include "../../include/tda.h"
 
-static PyObject *str_data_ptr, *str_cuda_stream, *current_stream;
+static PyObject *str_data_ptr, *str_cuda_stream, *current_stream, *linear_desc;
 
 static __typeof__(&tda_linear_forward) f_linear_forward;
 static __typeof__(&tda_linear_backward) f_linear_backward;
@@ -52,6 +52,17 @@ static void *as_struct(PyObject *o, Py_buffer *b) {
     return b->buf;
 }
 
+/* A layer's descriptor: a LinearDesc, nothing else that happens to have a buffer. */
+static const tda_linear_desc *as_desc(PyObject *o, Py_buffer *b) {
+    if (o != Py_None && !PyObject_TypeCheck(o, (PyTypeObject *)linear_desc)) {
+        PyErr_Format(PyExc_TypeError, "the layer is a LinearDesc, not %.100s", Py_TYPE(o)->tp_name);
+        return NULL;
+    }
+    const tda_linear_desc *L = (const tda_linear_desc *)as_struct(o, b);
+    if (L && b->len < (Py_ssize_t)sizeof *L) PyErr_SetString(PyExc_TypeError, "the LinearDesc is too short");
+    return L;
+}
+
 #define ENTRY(name, count)                                                                       \
     static PyObject *name(PyObject *self, PyObject *const *a, Py_ssize_t n) {                    \
         (void)self;                                                                              \
@@ -83,7 +94,7 @@ ENTRY(embedding_backward, 16)
 
 ENTRY(linear_forward, 16)
     Py_buffer b = {0};
-    const tda_linear_desc *L = (const tda_linear_desc *)as_struct(a[0], &b);
+    const tda_linear_desc *L = as_desc(a[0], &b);
     const void *X = P(1), *W = P(4), *bias = P(6), *R = P(7);
     const long long ld_x = I(2), M = I(3), ld_w = I(5), ld_r = I(8), ld_y = I(10), ld_z = I(12), wsb = I(14);
     void *Y = P(9), *Z = P(11), *ws = P(13), *s = as_stream(a[15]);
@@ -96,7 +107,7 @@ ENTRY(linear_forward, 16)
 
 ENTRY(linear_backward, 22)
     Py_buffer b = {0};
-    const tda_linear_desc *L = (const tda_linear_desc *)as_struct(a[0], &b);
+    const tda_linear_desc *L = as_desc(a[0], &b);
     const void *dY = P(1), *Z = P(3), *X = P(6), *W = P(8);
     const long long ld_dy = I(2), ld_z = I(4), M = I(5), ld_x = I(7), ld_w = I(9), ld_b = I(11), ld_dx = I(13),
                     ld_dw = I(15), wsb = I(20);
@@ -130,15 +141,18 @@ ENTRY(grad_clip, 7)
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);
 }
 
-/* bind(current_stream, linear_forward, linear_backward, embedding_forward, embedding_backward, grad_clip) */
+/* bind(current_stream, LinearDesc, linear_forward, linear_backward, embedding_forward, embedding_backward, grad_clip) */
 static PyObject *bind(PyObject *self, PyObject *const *a, Py_ssize_t n) {
     (void)self;
-    if (n != 6) return PyErr_Format(PyExc_TypeError, "bind takes 6 arguments, got %zd", n);
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "bind takes 7 arguments, got %zd", n);
+    if (!PyType_Check(a[1])) return PyErr_Format(PyExc_TypeError, "bind: LinearDesc is not a type");
     void *f[5];
-    for (int i = 0; i < 5; ++i) f[i] = as_address(a[i + 1]);
+    for (int i = 0; i < 5; ++i) f[i] = as_address(a[i + 2]);
     if (PyErr_Occurred()) return NULL;
     Py_INCREF(a[0]);
     Py_XSETREF(current_stream, a[0]);
+    Py_INCREF(a[1]);
+    Py_XSETREF(linear_desc, a[1]);
     f_linear_forward = (__typeof__(f_linear_forward))f[0];
     f_linear_backward = (__typeof__(f_linear_backward))f[1];
     f_embedding_forward = (__typeof__(f_embedding_forward))f[2];

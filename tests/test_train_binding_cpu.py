@@ -1,0 +1,34 @@
+"""The extension module that calls the training step's entry points: what it refuses before the library sees it
+(no GPU; a refused call launches nothing)."""
+import ctypes
+
+import pytest
+
+import paper_2609_38767_gb300 as tda
+from paper_2609_38767_gb300 import build as tbuild
+
+
+@pytest.fixture(scope="module", autouse=True)
+def libs():
+    return tbuild.build()
+
+
+def forward(L, ws=None, wsb=0):
+    tda.tda_linear_forward(L, 256, 64, 4, 256, 64, None, None, 0, 256, 32, None, 0, ws, wsb, stream=0)
+
+
+def backward(L, ws=256, wsb=1 << 20):
+    tda.tda_linear_backward(L, 256, 32, 256, 32, 4, 256, 64, 256, 64, 256, 32, 256, 64, 256, 64, 256, tda.TDA_F32, 0.0, ws,
+                            wsb, stream=0)
+
+
+@pytest.mark.parametrize("call", [forward, backward])
+def test_the_layer_is_a_linear_descriptor(call):
+    """Any other object with a buffer would be read by the descriptor's layout, past its end where it is short."""
+    good = tda.LinearDesc(64, 32, tda.TDA_ACT_SILU, tda.TDA_F64)
+    with pytest.raises(tda.TdaError):  # reaches the library, which refuses the type
+        call(good)
+    for other in (b"", b"short", bytes(good), bytearray(24), tda.LayerDesc(64, 32, 8, 4, 4), memoryview(good),
+                  (ctypes.c_int64 * 3)(64, 32, 0), tda.TensorRef()):
+        with pytest.raises(TypeError):
+            call(other)
