@@ -23,6 +23,11 @@ static __typeof__(&tda_grad_clip) f_grad_clip;
 
 /* An argument that does not convert leaves a Python error set; the caller looks once, before the call. */
 static long long as_int(PyObject *o) { return PyLong_AsLongLong(o); }
+static size_t as_size(PyObject *o) {
+    const long long v = as_int(o);
+    if (v < 0 && !PyErr_Occurred()) PyErr_SetString(PyExc_OverflowError, "a workspace size is not negative");
+    return (size_t)v;
+}
 static double as_float(PyObject *o) { return PyFloat_AsDouble(o); }
 static void *as_address(PyObject *o) { return PyLong_AsVoidPtr(o); }
 
@@ -70,6 +75,7 @@ static const tda_linear_desc *as_desc(PyObject *o, Py_buffer *b) {
         if (n != count) return PyErr_Format(PyExc_TypeError, #name " takes %d arguments, got %zd", count, n);
 #define I(k) as_int(a[k])
 #define P(k) as_ptr(a[k])
+#define N(k) as_size(a[k])
 
 ENTRY(embedding_forward, 12)
     const int dt = (int)I(0), it = (int)I(5);
@@ -84,23 +90,25 @@ ENTRY(embedding_forward, 12)
 ENTRY(embedding_backward, 16)
     const int dt = (int)I(0), it = (int)I(5), gt = (int)I(9);
     const void *dout = P(1), *tok = P(6);
-    const long long ld_d = I(2), V = I(3), d = I(4), cnt = I(7), ld_e = I(11), wsb = I(14);
+    const long long ld_d = I(2), V = I(3), d = I(4), cnt = I(7), ld_e = I(11);
+    const size_t wsb = N(14);
     const float scale = (float)as_float(a[8]), beta = (float)as_float(a[12]);
     void *dE = P(10), *ws = P(13), *s = as_stream(a[15]);
     if (PyErr_Occurred()) return NULL;
     return PyLong_FromLong(f_embedding_backward((tda_dtype)dt, dout, ld_d, V, d, (tda_index_type)it, tok, cnt, scale,
-                                                (tda_dtype)gt, dE, ld_e, beta, ws, (size_t)wsb, s));
+                                                (tda_dtype)gt, dE, ld_e, beta, ws, wsb, s));
 }
 
 ENTRY(linear_forward, 16)
     Py_buffer b = {0};
     const tda_linear_desc *L = as_desc(a[0], &b);
     const void *X = P(1), *W = P(4), *bias = P(6), *R = P(7);
-    const long long ld_x = I(2), M = I(3), ld_w = I(5), ld_r = I(8), ld_y = I(10), ld_z = I(12), wsb = I(14);
+    const long long ld_x = I(2), M = I(3), ld_w = I(5), ld_r = I(8), ld_y = I(10), ld_z = I(12);
+    const size_t wsb = N(14);
     void *Y = P(9), *Z = P(11), *ws = P(13), *s = as_stream(a[15]);
     int st = 0;
     if (!PyErr_Occurred())
-        st = f_linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, (size_t)wsb, s);
+        st = f_linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, wsb, s);
     if (b.obj) PyBuffer_Release(&b);
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);
 }
@@ -110,14 +118,15 @@ ENTRY(linear_backward, 22)
     const tda_linear_desc *L = as_desc(a[0], &b);
     const void *dY = P(1), *Z = P(3), *X = P(6), *W = P(8);
     const long long ld_dy = I(2), ld_z = I(4), M = I(5), ld_x = I(7), ld_w = I(9), ld_b = I(11), ld_dx = I(13),
-                    ld_dw = I(15), wsb = I(20);
+                    ld_dw = I(15);
+    const size_t wsb = N(20);
     void *B = P(10), *dX = P(12), *dW = P(14), *db = P(16), *ws = P(19), *s = as_stream(a[21]);
     const int gt = (int)I(17);
     const float beta = (float)as_float(a[18]);
     int st = 0;
     if (!PyErr_Occurred())
         st = f_linear_backward(L, dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B, ld_b, dX, ld_dx, dW, ld_dw, db,
-                               (tda_dtype)gt, beta, ws, (size_t)wsb, s);
+                               (tda_dtype)gt, beta, ws, wsb, s);
     if (b.obj) PyBuffer_Release(&b);
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);
 }
@@ -125,7 +134,8 @@ ENTRY(linear_backward, 22)
 ENTRY(grad_clip, 7)
     Py_buffer b = {0};
     const tda_tensor_ref *list = (const tda_tensor_ref *)as_struct(a[0], &b);
-    const long long count = I(1), wsb = I(5);
+    const long long count = I(1);
+    const size_t wsb = N(5);
     const float most = (float)as_float(a[2]);
     float *norm = (float *)P(3);
     void *ws = P(4), *s = as_stream(a[6]);
@@ -135,7 +145,7 @@ ENTRY(grad_clip, 7)
         if (list && count <= (1LL << 20) && count > (long long)(b.len / (Py_ssize_t)sizeof(tda_tensor_ref)))
             PyErr_SetString(PyExc_ValueError, "grad_clip: more tensors than the list has entries");
         else
-            st = f_grad_clip(list, count, most, norm, ws, (size_t)wsb, s);
+            st = f_grad_clip(list, count, most, norm, ws, wsb, s);
     }
     if (b.obj) PyBuffer_Release(&b);
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);

@@ -32,3 +32,18 @@ def test_the_layer_is_a_linear_descriptor(call):
                   (ctypes.c_int64 * 3)(64, 32, 0), tda.TensorRef()):
         with pytest.raises(TypeError):
             call(other)
+
+
+def test_workspace_sizes_are_not_negative():
+    """-1 would reach the library as the largest size there is and pass its check of the workspace."""
+    L = tda.LinearDesc(64, 32, tda.TDA_ACT_SILU, tda.TDA_F64)  # refused by the library if it gets there
+    refs = (tda.TensorRef * 1)(tda.TensorRef(256, 256, 4, tda.TDA_F64, 0))
+    for call in (lambda b: forward(L, 256, b), lambda b: backward(L, 256, b),
+                 lambda b: tda.tda_embedding_backward(tda.TDA_F64, 256, 8, 4, 8, tda.TDA_I32, 256, 3, 1.0, tda.TDA_F32, 256,
+                                                      8, 0.0, 256, b, stream=0),
+                 lambda b: tda.tda_grad_clip(refs, 1, 1.0, 256, 256, b, stream=0)):
+        for b in (-1, -(1 << 40)):
+            with pytest.raises(OverflowError):
+                call(b)
+        with pytest.raises(tda.TdaError):
+            call(1 << 20)
