@@ -1,5 +1,6 @@
 // api.cu -- the extern "C" entry points of libtda.so (include/tda.h):
 // host-side argument validation, route selection and kernel dispatch.
+#include <cuda.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -37,6 +38,21 @@ int sm_budget() { return g_sm_budget.load(std::memory_order_relaxed); }
 
 // The device error word: bounded waits that expire OR bits into it.
 __device__ unsigned int g_error_word;
+
+void bind_thread_context() {
+    static thread_local bool bound = false;
+    if (bound) return;
+    bound = true;
+    typedef CUresult (*CtxGetCurrentFn)(CUcontext*);
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    CUcontext c = nullptr;
+    int dev = 0;
+    if (cudaGetDriverEntryPointByVersion("cuCtxGetCurrent", &f, 4000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess || ((CtxGetCurrentFn)f)(&c) != CUDA_SUCCESS || c)
+        return;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaSetDevice(dev);
+}
 
 unsigned int* device_error_word() {
     static std::mutex mu;

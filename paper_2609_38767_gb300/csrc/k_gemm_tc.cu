@@ -934,6 +934,7 @@ EncodeTiledFn encode_fn() {
             q == cudaDriverEntryPointSuccess)
             fn = (EncodeTiledFn)f;
     });
+    bind_thread_context();
     return fn;
 }
 

@@ -286,6 +286,7 @@ EncodeTiledFn encode_fn() {
             q == cudaDriverEntryPointSuccess)
             fn = (EncodeTiledFn)f;
     });
+    bind_thread_context();
     return fn;
 }
 

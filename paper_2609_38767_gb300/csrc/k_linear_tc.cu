@@ -1162,6 +1162,7 @@ EncodeTiledFn encode_fn() {
             q == cudaDriverEntryPointSuccess)
             fn = (EncodeTiledFn)f;
     });
+    bind_thread_context();
     return fn;
 }
 

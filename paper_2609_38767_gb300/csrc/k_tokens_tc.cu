@@ -331,6 +331,7 @@ EncodeTiledFn encode_fn() {
             q == cudaDriverEntryPointSuccess)
             fn = (EncodeTiledFn)f;
     });
+    bind_thread_context();
     return fn;
 }
 

@@ -57,6 +57,10 @@ int sm_budget();
 // Device address of the library's error word on the current device.
 unsigned int* device_error_word();
 
+// Makes the current device's context the calling thread's, if the thread has none yet (api.cu). The tensor-map
+// encoder is a driver call and refuses a thread whose first CUDA work it is; the runtime's launches bind by themselves.
+void bind_thread_context();
+
 // Thread-local error message helpers (api.cu).
 tda_status fail(tda_status st, const char* fmt, ...);
 void clear_message();

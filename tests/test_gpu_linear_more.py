@@ -121,3 +121,47 @@ def test_activation_tails_are_right_in_proportion(dev, M, act, dtype):
     off = ((Y.to(F64) - ref).abs() / ref.abs())[held]
     assert int(held.sum()) > 0.6 * held.numel()
     assert float(off.max()) <= (2.0 ** -8 + 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -15), float(off.max())
+
+
+def test_first_call_of_a_host_thread(dev):
+    """A thread that has done no CUDA work yet calls the library: its tensor maps need a context too. Every buffer is made
+    beforehand, so that the call is the thread's first."""
+    import threading
+
+    mk = lambda *s: torch.randn(s, device=dev).bfloat16()
+    s = torch.cuda.current_stream().cuda_stream
+    calls = []
+    for M, di, do in ((2048, 256, 2304), (300, 256, 520)):
+        L = tda.LinearDesc(di, do, tda.TDA_ACT_NONE, tda.TDA_BF16)
+        X, W, Y, dX, dW = mk(M, di), mk(do, di), mk(M, do), mk(M, di), torch.zeros((do, di), device=dev)
+        calls.append((lambda L=L, M=M, di=di, do=do, X=X, W=W, Y=Y: tda.tda_linear_forward(
+            L, X, di, M, W, di, None, None, 0, Y, do, stream=s), Y))
+        dY = mk(M, do)
+        calls.append((lambda L=L, M=M, di=di, do=do, X=X, W=W, dY=dY, dX=dX, dW=dW: tda.tda_linear_backward(
+            L, dY, do, None, 0, M, X, di, W, di, None, 0, dX, di, dW, di, None, tda.TDA_F32, 0.0, None, 0, stream=s), dW))
+    N, T, d, k = 8, 128, 256, 32
+    A, B, phi = mk(N, T, d), mk(N, T, d), torch.zeros((N, k * k), device=dev)
+    P = tda.LayerDesc(d, d, T, k, k)
+    calls.append((lambda: tda.tda_project(P, tda.TDA_BF16, A, B, N, phi, k * k, tda.TDA_ROUTE_FACTORED, stream=s), phi))
+    Q, F, S = torch.randn(64, 1024, device=dev), torch.randn(256, 1024, device=dev), torch.zeros(64, 256, device=dev)
+    calls.append((lambda: tda.tda_score(Q, tda.TDA_F32, 64, 1024, F, 256, 1024, 1024, S, 256, stream=s), S))
+    for call, out in calls:
+        call()
+        want = out.clone()
+        out.zero_()
+        torch.cuda.synchronize()
+        failed = []
+
+        def first(call=call, failed=failed):
+            try:
+                call()
+            except Exception as e:  # noqa: BLE001
+                failed.append(e)
+
+        t = threading.Thread(target=first)
+        t.start()
+        t.join()
+        assert not failed, failed
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    tda.tda_device_status()
