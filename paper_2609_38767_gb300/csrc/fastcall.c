@@ -75,6 +75,12 @@ static const tda_linear_desc *as_desc(PyObject *o, Py_buffer *b) {
         if (n != count) return PyErr_Format(PyExc_TypeError, #name " takes %d arguments, got %zd", count, n);
 #define I(k) as_int(a[k])
 #define P(k) as_ptr(a[k])
+/* The library's call, with other threads free to run: it waits where the launch queue is full. */
+#define CALL(expr)                              \
+    do {                                        \
+        Py_BEGIN_ALLOW_THREADS st = (int)(expr); \
+        Py_END_ALLOW_THREADS                    \
+    } while (0)
 #define N(k) as_size(a[k])
 
 ENTRY(embedding_forward, 12)
@@ -84,7 +90,9 @@ ENTRY(embedding_forward, 12)
     const float scale = (float)as_float(a[8]);
     void *out = P(9), *s = as_stream(a[11]);
     if (PyErr_Occurred()) return NULL;
-    return PyLong_FromLong(f_embedding_forward((tda_dtype)dt, E, ld_e, V, d, (tda_index_type)it, tok, cnt, scale, out, ld_o, s));
+    int st;
+    CALL(f_embedding_forward((tda_dtype)dt, E, ld_e, V, d, (tda_index_type)it, tok, cnt, scale, out, ld_o, s));
+    return PyLong_FromLong(st);
 }
 
 ENTRY(embedding_backward, 16)
@@ -95,8 +103,10 @@ ENTRY(embedding_backward, 16)
     const float scale = (float)as_float(a[8]), beta = (float)as_float(a[12]);
     void *dE = P(10), *ws = P(13), *s = as_stream(a[15]);
     if (PyErr_Occurred()) return NULL;
-    return PyLong_FromLong(f_embedding_backward((tda_dtype)dt, dout, ld_d, V, d, (tda_index_type)it, tok, cnt, scale,
-                                                (tda_dtype)gt, dE, ld_e, beta, ws, wsb, s));
+    int st;
+    CALL(f_embedding_backward((tda_dtype)dt, dout, ld_d, V, d, (tda_index_type)it, tok, cnt, scale, (tda_dtype)gt, dE, ld_e,
+                              beta, ws, wsb, s));
+    return PyLong_FromLong(st);
 }
 
 ENTRY(linear_forward, 16)
@@ -108,7 +118,7 @@ ENTRY(linear_forward, 16)
     void *Y = P(9), *Z = P(11), *ws = P(13), *s = as_stream(a[15]);
     int st = 0;
     if (!PyErr_Occurred())
-        st = f_linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, wsb, s);
+        CALL(f_linear_forward(L, X, ld_x, M, W, ld_w, bias, R, ld_r, Y, ld_y, Z, ld_z, ws, wsb, s));
     if (b.obj) PyBuffer_Release(&b);
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);
 }
@@ -125,8 +135,8 @@ ENTRY(linear_backward, 22)
     const float beta = (float)as_float(a[18]);
     int st = 0;
     if (!PyErr_Occurred())
-        st = f_linear_backward(L, dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B, ld_b, dX, ld_dx, dW, ld_dw, db,
-                               (tda_dtype)gt, beta, ws, wsb, s);
+        CALL(f_linear_backward(L, dY, ld_dy, Z, ld_z, M, X, ld_x, W, ld_w, B, ld_b, dX, ld_dx, dW, ld_dw, db, (tda_dtype)gt,
+                               beta, ws, wsb, s));
     if (b.obj) PyBuffer_Release(&b);
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);
 }
@@ -145,7 +155,7 @@ ENTRY(grad_clip, 7)
         if (list && count <= (1LL << 20) && count > (long long)(b.len / (Py_ssize_t)sizeof(tda_tensor_ref)))
             PyErr_SetString(PyExc_ValueError, "grad_clip: more tensors than the list has entries");
         else
-            st = f_grad_clip(list, count, most, norm, ws, wsb, s);
+            CALL(f_grad_clip(list, count, most, norm, ws, wsb, s));
     }
     if (b.obj) PyBuffer_Release(&b);
     return PyErr_Occurred() ? NULL : PyLong_FromLong(st);

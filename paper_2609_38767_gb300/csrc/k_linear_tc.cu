@@ -1329,15 +1329,17 @@ cudaError_t pick_tile(const Product* const* pr, int count, bool chained, cudaStr
 }  // namespace
 
 bool linear_tc_available() {
-    static int sm103 = -1;
-    if (sm103 < 0) {
+    static std::atomic<int> sm103{-1};
+    int v = sm103.load(std::memory_order_relaxed);
+    if (v < 0) {
         int dev = 0, major = 0, minor = 0;
         cudaGetDevice(&dev);
         cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
         cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
-        sm103 = (major == 10 && minor == 3) ? 1 : 0;
+        v = (major == 10 && minor == 3) ? 1 : 0;
+        sm103.store(v, std::memory_order_relaxed);
     }
-    return sm103 && encode_fn();
+    return v && encode_fn();
 }
 
 static Product make_product(const LinearProduct& x, unsigned int* err) {

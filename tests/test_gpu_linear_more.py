@@ -165,3 +165,49 @@ def test_first_call_of_a_host_thread(dev):
         torch.cuda.synchronize()
         assert torch.equal(out, want)
     tda.tda_device_status()
+
+
+def test_threads_with_streams_and_workspaces_of_their_own(dev):
+    """Four host threads at once, each on its stream: the same bits as one after the other."""
+    import threading
+
+    jobs = []
+    for k, (M, di, do, dtype) in enumerate(((700, 264, 1000, torch.bfloat16), (2048, 512, 2304, torch.bfloat16),
+                                            (333, 130, 520, torch.float32), (9, 1024, 640, torch.float32))):
+        gen = torch.Generator(device=dev).manual_seed(50 + k)
+        mk = lambda *s: torch.randn(s, generator=gen, device=dev).to(dtype)
+        L = tda.LinearDesc(di, do, tda.TDA_ACT_GELU_TANH, KIND[dtype])
+        ws, wsb = workspace(tda.TDA_LINEAR_BACKWARD | tda.TDA_LINEAR_ANY_STRIDE, L, M, dev)
+        jobs.append((L, M, di, do, mk(M, di), mk(do, di), mk(do), mk(M, do), ws, wsb))
+
+    def run(j, stream):
+        L, M, di, do, X, W, b, dY, ws, wsb = j
+        with torch.cuda.stream(stream):
+            Y, Z, B, dX = torch.empty_like(dY), torch.empty_like(dY), torch.empty_like(dY), torch.empty_like(X)
+            dW, db = torch.empty((do, di), device=dev), torch.empty(do, device=dev)
+            tda.tda_linear_forward(L, X, di, M, W, di, b, None, 0, Y, do, Z, do, ws, wsb)
+            tda.tda_linear_backward(L, dY, do, Z, do, M, X, di, W, di, B, do, dX, di, dW, di, db, tda.TDA_F32, 0.0, ws, wsb)
+        return Y, Z, B, dX, dW, db
+
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    alone = [run(j, s) for j, s in zip(jobs, streams)]
+    torch.cuda.synchronize()
+    got, failed = [[] for _ in jobs], []
+
+    def work(i):
+        try:
+            got[i] += [run(jobs[i], streams[i]) for _ in range(25)]
+        except Exception as e:  # noqa: BLE001
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    tda.tda_device_status()
+    assert not failed
+    for a, runs in zip(alone, got):
+        assert len(runs) == 25 and all(torch.equal(x, y) for r in runs for x, y in zip(a, r))

@@ -47,3 +47,34 @@ def test_workspace_sizes_are_not_negative():
                 call(b)
         with pytest.raises(tda.TdaError):
             call(1 << 20)
+
+
+def test_other_threads_run_during_a_call():
+    """The calls give up Python's lock, as ctypes does. In the library's place stands libc's usleep, which takes the first
+    argument as microseconds."""
+    import threading
+    import time
+
+    mod = tda._train()
+    usleep = ctypes.cast(ctypes.CDLL(None).usleep, ctypes.c_void_p).value
+    ticks, stop = [], threading.Event()
+
+    def beat():
+        while not stop.is_set():
+            ticks.append(time.monotonic())
+            time.sleep(0.005)
+
+    try:
+        mod.bind(tda._current_stream, tda.LinearDesc, *[usleep] * 5)
+        t = threading.Thread(target=beat)
+        t.start()
+        t0 = time.monotonic()
+        st = mod.embedding_forward(300_000, 256, 8, 4, 8, tda.TDA_I32, 256, 3, 1.0, 256, 8, 0)
+        t1 = time.monotonic()
+        stop.set()
+        t.join()
+    finally:
+        tda._calls = None
+        tda._train()
+    assert st == 0 and t1 - t0 >= 0.25
+    assert sum(t0 + 0.02 < x < t1 - 0.02 for x in ticks) >= 5
