@@ -75,16 +75,24 @@ def build_synth_cpu() -> str:
 
 
 def build_fast() -> str:
-    """gcc build of the extension module _fast (csrc/fastcall.c)."""
+    """gcc build of the extension module _fast (csrc/fastcall.c), for the Python that runs this."""
     src = os.path.join(CSRC, "fastcall.c")
     target = lib_path("_fast.so")
-    if _stale(target, [src] + _headers()):
+    tag, abi = os.path.join(BUILD, "_fast.abi"), f"{sysconfig.get_config_var('SOABI')}\n"
+    try:
+        with open(tag) as f:
+            built_for = f.read()
+    except OSError:
+        built_for = ""
+    if built_for != abi or _stale(target, [src] + _headers()):
         cmd = ["gcc", "-O2", "-std=gnu11", "-fPIC", "-shared", "-Wall", f"-I{sysconfig.get_paths()['include']}",
                "-o", target + ".tmp", src]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"gcc failed for {src}:\n{r.stderr}")
         os.replace(target + ".tmp", target)
+        with open(tag, "w") as f:
+            f.write(abi)
     return target
 
 
