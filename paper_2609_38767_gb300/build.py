@@ -15,6 +15,7 @@ import glob
 import os
 import subprocess
 import sysconfig
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -74,10 +75,15 @@ def build_synth_cpu() -> str:
     return target
 
 
-def build_fast() -> str:
-    """gcc build of the extension module _fast (csrc/fastcall.c), for the Python that runs this."""
+def build_fast() -> str | None:
+    """gcc build of the extension module _fast (csrc/fastcall.c), for the Python that runs this. None, with a warning,
+    where Python's headers are not installed: only the training step's calls need the module."""
     src = os.path.join(CSRC, "fastcall.c")
     target = lib_path("_fast.so")
+    include = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        warnings.warn(f"no Python.h in {include}: _fast.so is not built and the training step's calls are missing")
+        return None
     tag, abi = os.path.join(BUILD, "_fast.abi"), f"{sysconfig.get_config_var('SOABI')}\n"
     try:
         with open(tag) as f:
@@ -85,7 +91,7 @@ def build_fast() -> str:
     except OSError:
         built_for = ""
     if built_for != abi or _stale(target, [src] + _headers()):
-        cmd = ["gcc", "-O2", "-std=gnu11", "-fPIC", "-shared", "-Wall", f"-I{sysconfig.get_paths()['include']}",
+        cmd = ["gcc", "-O2", "-std=gnu11", "-fPIC", "-shared", "-Wall", f"-I{include}",
                "-o", target + ".tmp", src]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
@@ -117,7 +123,9 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> dict[str, st
                     print("built", target)
             out[name] = target
     out["libtda_synth_cpu.so"] = build_synth_cpu()
-    out["_fast.so"] = build_fast()
+    fast = build_fast()
+    if fast:
+        out["_fast.so"] = fast
     return out
 
 

@@ -26,3 +26,14 @@ def test_the_extension_is_built_for_the_python_that_asks(folder, monkeypatch):
     assert second != first
     tbuild.build_fast()
     assert os.stat(target).st_mtime_ns == second
+
+
+def test_without_pythons_headers_the_rest_is_built(folder, monkeypatch):
+    """Attribution alone needs no extension module: its build goes through and says what is missing."""
+    monkeypatch.setattr(tbuild, "LIBS", {})
+    monkeypatch.setattr(tbuild, "build_synth_cpu", lambda: "synth")
+    paths = dict(sysconfig.get_paths(), include=str(folder / "none"))
+    monkeypatch.setattr(tbuild.sysconfig, "get_paths", lambda *a, **k: paths)
+    with pytest.warns(UserWarning, match="Python.h"):
+        out = tbuild.build()
+    assert out == {"libtda_synth_cpu.so": "synth"} and not (folder / "_fast.so").exists()
