@@ -22,6 +22,8 @@ import torch
 
 import paper_2609_38767_gb300 as tda
 
+_INDEX = {torch.int32: tda.TDA_I32, torch.int64: tda.TDA_I64}
+
 
 class _Linear:
     """Weights, gradients and the step's tensors of one linear over M tokens."""
@@ -78,9 +80,12 @@ class TokenModel:
         self.ws = torch.empty(need, dtype=torch.uint8, device=device)
 
     def forward(self, tokens):
-        """Logits [M][V] of tokens [N][T] (int32; a negative id is padding)."""
-        self.tokens = tokens.reshape(-1).contiguous()
-        tda.tda_embedding_forward(self.kind, self.E, self.d, self.V, self.d, tda.TDA_I32, self.tokens, self.M, self.scale,
+        """Logits [M][V] of tokens [N][T] (int32 or int64, on the model's device; a negative id is padding)."""
+        if tokens.dtype not in _INDEX or tokens.numel() != self.M or tokens.device != self.E.device:
+            raise ValueError(f"tokens are {self.N} x {self.T} int32 or int64 ids on {self.E.device}, not "
+                             f"{tuple(tokens.shape)} {tokens.dtype} on {tokens.device}")
+        self.tokens, self.index = tokens.reshape(-1).contiguous(), _INDEX[tokens.dtype]
+        tda.tda_embedding_forward(self.kind, self.E, self.d, self.V, self.d, self.index, self.tokens, self.M, self.scale,
                                   self.h0, self.d)
         h = self.h0
         for up, down in self.blocks:
@@ -88,7 +93,11 @@ class TokenModel:
         return self.head.forward(h, self.M, None, self.ws)
 
     def backward(self, dlogits):
-        """Gradients of every parameter and every linear's B, from dlogits [M][V] (zero rows for padding)."""
+        """Gradients of every parameter and every linear's B, from dlogits [M][V] of the model's type (zero rows for
+        padding)."""
+        if (tuple(dlogits.shape) != (self.M, self.V) or dlogits.dtype != self.dtype or dlogits.device != self.E.device
+                or not dlogits.is_contiguous()):
+            raise ValueError(f"dlogits are contiguous {self.M} x {self.V} {self.dtype} on {self.E.device}")
         dh, other = self.dh
         self.head.backward(dlogits, self.M, dh, self.ws)
         for up, down in reversed(self.blocks):
@@ -96,7 +105,7 @@ class TokenModel:
             up.backward(self.du, self.M, other, self.ws)
             other += dh  # the residual's share of the gradient
             dh, other = other, dh
-        tda.tda_embedding_backward(self.kind, dh, self.d, self.V, self.d, tda.TDA_I32, self.tokens, self.M, self.scale,
+        tda.tda_embedding_backward(self.kind, dh, self.d, self.V, self.d, self.index, self.tokens, self.M, self.scale,
                                    tda.TDA_F32, self.dE, self.d, 0.0, self.ws, self.ws.numel())
 
     def loss_gradient(self, logits, targets):
