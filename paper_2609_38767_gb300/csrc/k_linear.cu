@@ -215,11 +215,16 @@ bool rows_by(const void* p, int64_t ld, size_t bytes, size_t el) {
 int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Runs of rows of the factor kernel: as many as make at most one wave of four CTAs per SM, at least 32 rows each, at
-// most 256 runs. Rounded up instead, the few CTAs of a second wave cost a whole one: 8192 tokens of 14336 columns
-// (224 column blocks, 2 runs against 3) 227 us with their products, against 271.
-int64_t factor_run(int64_t M, int64_t N) {
-    const int64_t blocks = (N + kColLanes * 8 - 1) / (kColLanes * 8);
+// Columns of a CTA of the factor kernel.
+int64_t factor_width(tda_dtype dt) { return (int64_t)kColLanes * (dt == TDA_BF16 ? 8 : 4); }
+
+// Runs of rows of the factor kernel: as many as make at most one wave of four CTAs per SM (where one run of all rows
+// does not make more), at least 32 rows each, at most 256 runs. Rounded up instead, the few CTAs of a second wave cost
+// a whole one: 8192 tokens of 14336 bf16 columns (56 column blocks, 10 runs against 11) 227 us with their products,
+// against 271. fp32 columns, whose blocks are half as wide, factor and bias sums: 4096 x 2048 silu 19.1 us (two waves
+// 24.2), 2048 x 4096 tanh-gelu 19.8 (21.9), 8192 x 8192 silu 129.9 (128.4), 4096 x 8192 gelu 98.6 (92.4).
+int64_t factor_run(int64_t M, int64_t N, tda_dtype dt) {
+    const int64_t blocks = (N + factor_width(dt) - 1) / factor_width(dt);
     int64_t runs = 4 * 152 / blocks;
     if (runs < 1) runs = 1;
     if (runs > 256) runs = 256;
@@ -339,7 +344,7 @@ size_t linear_backward_ws(const LinearBackward& b) {
     if (dX && needs_planes(b.dt, b.W, b.ld_w)) n += plane_bytes(b.d_out, b.d_in, b.dt);
     if (dW && needs_planes(b.dt, b.X, b.ld_x)) n += plane_bytes(b.M, b.d_in, b.dt);
     if (b.db) {
-        const int64_t run = factor_run(b.M, b.d_out);
+        const int64_t run = factor_run(b.M, b.d_out, b.dt);
         n += up256(sizeof(float) * (size_t)((b.M + run - 1) / run) * (size_t)b.d_out);
     }
     return n;
@@ -350,7 +355,7 @@ size_t linear_ws_bound(bool backward, int64_t M, int64_t d_in, int64_t d_out, td
     size_t n = in ? plane_bytes(M, d_in, dt) + plane_bytes(d_out, d_in, dt) : 0;
     if (!backward) return n;
     if (out) n += plane_bytes(M, d_out, dt);
-    const int64_t run = factor_run(M, d_out);
+    const int64_t run = factor_run(M, d_out, dt);
     return n + up256(sizeof(float) * (size_t)((M + run - 1) / run) * (size_t)d_out);
 }
 
@@ -374,7 +379,7 @@ cudaError_t launch_linear_forward(const LinearForward& f, void* ws, unsigned int
 
 cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned int* err, cudaStream_t s) {
     cudaError_t e;
-    const int64_t run = factor_run(b.M, b.d_out), runs = (b.M + run - 1) / run;
+    const int64_t run = factor_run(b.M, b.d_out, b.dt), runs = (b.M + run - 1) / run;
     float* sums = nullptr;
     Planner pl;
     pl.dt = b.dt;

@@ -78,3 +78,21 @@ def test_other_threads_run_during_a_call():
         tda._train()
     assert st == 0 and t1 - t0 >= 0.25
     assert sum(t0 + 0.02 < x < t1 - 0.02 for x in ticks) >= 5
+
+
+@pytest.mark.parametrize("dtype,width", [(tda.TDA_F32, 128), (tda.TDA_BF16, 256)])
+def test_bias_gradient_scratch_is_one_wave_of_partial_sums(dtype, width):
+    """The factor's launch makes a row of partial sums per run of tokens, over blocks of 32 lanes x 16 bytes of columns: at
+    most four CTAs for each of 152 SMs in all, unless the columns alone make more."""
+    up256 = lambda x: (x + 255) // 256 * 256
+    for M, do in ((8192, 8192), (4096, 2048), (3000, 1000), (100000, 128), (8192, 80000), (33, 64)):
+        L = tda.LinearDesc(64, do, tda.TDA_ACT_SILU, dtype)
+        total = tda.tda_linear_workspace_size(tda.TDA_LINEAR_BACKWARD, L, M)
+        planes = sum(up256(6 * r * c) for r, c in ((M, 64), (do, 64), (M, do))) if dtype == tda.TDA_F32 else 0
+        blocks = -(-do // width)
+        runs = (total - planes) // (4 * do)
+        assert runs >= 1 and (runs == 1 or runs * blocks <= 4 * 152), (M, do, runs)
+        # and no fewer than that allows, down to 32 tokens a run
+        most = min(256, max(1, 4 * 152 // blocks))
+        run = max(32, -(-M // most))
+        assert up256(4 * -(-M // run) * do) == total - planes
