@@ -62,6 +62,19 @@ tda_status check_ws(const void* ws, size_t ws_bytes, size_t need, const char* wh
 
 }  // namespace
 
+int tda::train_sms() {
+    static std::atomic<int> sms{0};
+    int v = sms.load(std::memory_order_relaxed);
+    if (!v) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0)
+            v = 152;
+        sms.store(v, std::memory_order_relaxed);
+    }
+    return v;
+}
+
 extern "C" {
 
 tda_status tda_linear_workspace_size(int32_t op, const tda_linear_desc* L, int64_t M, size_t* bytes) {

@@ -259,19 +259,6 @@ clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n
     }
 }
 
-int sm_count() {
-    static std::atomic<int> sms{0};
-    int v = sms.load(std::memory_order_relaxed);
-    if (!v) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess ||
-            cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0)
-            v = 152;
-        sms.store(v, std::memory_order_relaxed);
-    }
-    return v;
-}
-
 // Fills the table with tensors from *i on (empty ones left out) for at most `most` CTAs; false when none is left.
 bool next_table(const tda_tensor_ref* list, int64_t n_tensors, int64_t* i, int64_t most, ClipTable* T, int64_t* grid) {
     T->count = 0;
@@ -309,7 +296,7 @@ size_t clip_workspace_bytes(int64_t n_tensors) {
 
 cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, double* part,
                              cudaStream_t s) {
-    int64_t most = (int64_t)sm_count() * kClipCtasPerSm, grid;
+    int64_t most = (int64_t)train_sms() * kClipCtasPerSm, grid;
     if (most > kMaxGrid) most = kMaxGrid;
     ClipTable T;
     int n_part = 0, tables = 0;

@@ -225,7 +225,7 @@ int64_t factor_width(tda_dtype dt) { return (int64_t)kColLanes * (dt == TDA_BF16
 // 24.2), 2048 x 4096 tanh-gelu 19.8 (21.9), 8192 x 8192 silu 129.9 (128.4), 4096 x 8192 gelu 98.6 (92.4).
 int64_t factor_run(int64_t M, int64_t N, tda_dtype dt) {
     const int64_t blocks = (N + factor_width(dt) - 1) / factor_width(dt);
-    int64_t runs = 4 * 152 / blocks;
+    int64_t runs = 4 * train_sms() / blocks;
     if (runs < 1) runs = 1;
     if (runs > 256) runs = 256;
     int64_t run = (M + runs - 1) / runs;
@@ -293,7 +293,8 @@ struct Planner {
             const int64_t t = (jobs.j[i].rows * (jobs.j[i].ld_dst / 8) + kPackThreads - 1) / kPackThreads;
             if (t > most) most = t;
         }
-        const dim3 grid((unsigned)(most < 152 * 16 ? most : 152 * 16), (unsigned)count);
+        const int64_t cap = train_sms() * 16;
+        const dim3 grid((unsigned)(most < cap ? most : cap), (unsigned)count);
         return launch_chained(chained, dt == TDA_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, grid,
                               dim3(kPackThreads), 0, s, jobs);
     }
@@ -447,8 +448,8 @@ cudaError_t launch_linear_backward(const LinearBackward& b, void* ws, unsigned i
 // beta x for an empty batch.
 cudaError_t launch_scale_matrix(tda_dtype dt, void* x, int64_t rows, int64_t cols, int64_t ld, float beta,
                                 cudaStream_t s) {
-    const int64_t blocks = (rows * cols + 255) / 256;
-    const unsigned grid = (unsigned)(blocks < 152 * 16 ? blocks : 152 * 16);
+    const int64_t blocks = (rows * cols + 255) / 256, cap = train_sms() * 16;
+    const unsigned grid = (unsigned)(blocks < cap ? blocks : cap);
     note_launches(1);
     if (dt == TDA_BF16)
         scale_kernel<<<grid, 256, 0, s>>>((__nv_bfloat16*)x, rows, cols, ld, beta);

@@ -164,7 +164,7 @@ cudaError_t rows(RowsParams p, cudaStream_t s) {
                        (uintptr_t)(p.ld_w * (int64_t)sizeof(T))) & 15) == 0;
     // about 16 warps per SM
     p.wk = 1;
-    while (p.wk < kRowWarps && (p.ep.N + kRows - 1) / kRows * p.wk < 152 * 16) p.wk *= 2;
+    while (p.wk < kRowWarps && (p.ep.N + kRows - 1) / kRows * p.wk < train_sms() * 16) p.wk *= 2;
     note_launches(1);
     if (p.ep.M == 1)
         run_rows<T, 1>(p, vec, s);

@@ -1197,19 +1197,6 @@ bool make_out_map(CUtensorMap* tm, void* p, int64_t rows, int64_t cols, int64_t 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int sm_count() {
-    static std::atomic<int> sms{0};
-    int v = sms.load(std::memory_order_relaxed);
-    if (!v) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess ||
-            cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0)
-            v = 152;
-        sms.store(v, std::memory_order_relaxed);
-    }
-    return v;
-}
-
 
 // The cluster's size, and (second) a chained launch.
 void cluster_attributes(cudaLaunchAttribute* at, int size) {
@@ -1229,7 +1216,7 @@ struct Product {
 // CTAs along K of a tile launch: as many as fit the GPU at once, a few chunks each.
 int tile_split(int64_t tiles, int nk, bool round) {
     const int least = round ? 1 : 4;
-    const int64_t slots = (int64_t)sm_count() * (round ? 1 : 2);
+    const int64_t slots = (int64_t)train_sms() * (round ? 1 : 2);
     int split = 1;
     while (split < 8 && tiles * split * 2 <= slots && nk >= 2 * least * split) split *= 2;
     // clusters of eight find room on three quarters of the SMs at best (fp32 500 x 512 -> 512: 16 clusters of eight
@@ -1310,7 +1297,7 @@ cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStre
     cfg.attrs = at;
     cfg.numAttrs = 1;
     cfg.gridDim = dim3(2);
-    const int64_t most = max_clusters_once<linear_pair_kernel<BN, ROUND>>(cfg, 2, sm_count() / 2);
+    const int64_t most = max_clusters_once<linear_pair_kernel<BN, ROUND>>(cfg, 2, train_sms() / 2);
     const int64_t tiles = pp.tiles[0] + pp.tiles[1];
     cfg.gridDim = dim3((unsigned)(2 * (tiles < most ? tiles : most)));
     cfg.numAttrs = chained ? 2 : 1;
@@ -1371,7 +1358,7 @@ static int64_t pair_tiles(const Product& x) {
 // (4096 x 2048 -> 8191 89 us, -> 8192 81; taken for 8 or 16 chunks more, the tile kernel was chosen where it is
 // slower: 406 x 768 -> 12485 39 us, 28 this way).
 static double pair_time(const Product* const* r, int count) {
-    const int64_t n = sm_count() / 2, t0 = pair_tiles(*r[0]), c0 = r[0]->p.nk + 2;
+    const int64_t n = train_sms() / 2, t0 = pair_tiles(*r[0]), c0 = r[0]->p.nk + 2;
     if (count == 1) return (double)(ceil_div(t0, n) * c0);
     const int64_t t1 = pair_tiles(*r[1]), c1 = r[1]->p.nk + 2, idle = n - t0 % n;
     int64_t extra = (c0 + c1 / 2) / c1;
@@ -1391,8 +1378,8 @@ static double tile_time(const Product* const* r, int count, bool round) {
         if (r[i]->p.nk < least) least = r[i]->p.nk;
     }
     const int split = tile_split(tiles, least, round);
-    const double chunks = (double)ceil_div(most, split), fill = (double)(tiles * split) / sm_count();
-    if (round) return (double)ceil_div(tiles * split, sm_count()) * (1.4 * chunks + 4);
+    const double chunks = (double)ceil_div(most, split), fill = (double)(tiles * split) / train_sms();
+    if (round) return (double)ceil_div(tiles * split, train_sms()) * (1.4 * chunks + 4);
     return (fill > 1 ? fill : 1) * chunks + 4;
 }
 

@@ -226,6 +226,9 @@ cudaError_t launch_score_splitk(const float* Q, int64_t n_q, int64_t ld_q, const
 cudaError_t launch_topk(const float* S, int64_t n_q, int64_t n_t, int64_t ld_S, int32_t k,
                         int32_t* idx, float* val, cudaStream_t s);
 
+// SMs of the device that the training step's first call finds, 152 where there is none (api_train.cu).
+int train_sms();
+
 // The training step's operators: embedding lookup and gradient (k_embedding.cu), gradient norm and
 // clipping (k_clip.cu).
 size_t embedding_workspace_bytes(int64_t d, int64_t n);

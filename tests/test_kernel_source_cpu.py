@@ -83,3 +83,10 @@ def test_chained_kernels_promise_nothing_about_the_launch_before():
             promised = set(re.findall(r"__restrict__\s+(\w+)", head))
             assert promised <= INPUTS_OF_CALL.get(kernel.group(1), set()), (name, kernel.group(1), promised)
     assert {"bias_grad_kernel", "digit_scan_kernel", "grad_join_kernel", "clip_scale_kernel"} <= chained
+
+
+def test_the_sm_count_is_the_devices():
+    """The training step's launches are sized by one function that asks the device; no file has the number of its own."""
+    for name in ("k_linear.cu", "k_linear_rows.cu", "k_linear_tc.cu", "k_clip.cu", "k_embedding.cu", "linear.cuh"):
+        text = source(name)
+        assert not re.search(r"\b152\b", text) and "cudaDevAttrMultiProcessorCount" not in text, name
