@@ -3,9 +3,11 @@
 //   out  = c g,  c = max_norm / norm if norm > max_norm, else 1.
 //
 // Two launches: the sums of squares (one partial per CTA, in a fixed order),
-// then the scaling, whose CTAs each add the few hundred partials up in the same
+// then the scaling, whose CTAs each add the partials (at most 1280) up in the same
 // fixed order (no counter to clear, no atomics: the result does not depend on
-// timing). Both are bound by HBM. The bytes that must move are one read and one
+// timing). A launch takes up to 256 tensors; longer lists take several of each kind, and one CTA between them
+// that adds all partials up once (else every scaling CTA of every launch would read them all: 65536
+// tensors of 100 fp32 values 11.2 ms that way, 2.0 this; 2000 of 10000 119 us and 81). Both are bound by HBM. The bytes that must move are one read and one
 // write of every element, plus a second read of what the L2 has dropped since
 // the first; the scaling walks the tensors backwards, so it starts with what the
 // sums read last, while that is still in the L2. 537M bf16 values (1.07 GB): 500 us,
@@ -26,7 +28,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 8192;  // elements per unit of work: 16 or 32 KiB
-constexpr int kMaxTensors = 256;  // tensors of one launch: their table travels in the kernel's parameters (8 KiB)
+constexpr int kMaxTensors = 256;  // tensors of one launch: their table travels in the kernel's parameters (10.8 KB)
 
 struct ClipTensor {
     const void* in;
@@ -153,6 +155,28 @@ __global__ void __launch_bounds__(kThreads) clip_squares_kernel(const __grid_con
     }
 }
 
+// The sum of the partials in a fixed order, complete in thread 0.
+__device__ __forceinline__ double sum_partials(const double* part, int n_part) {
+    double d = 0.0;
+    for (int i = threadIdx.x; i < n_part; i += kThreads) d += part[i];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    __shared__ double w[kThreads / 32];
+    if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = d;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 1; i < kThreads / 32; ++i) d += w[i];
+    return d;
+}
+
+// Several launches of clip_squares_kernel: all their partials added up into part[0].
+__global__ void __launch_bounds__(kThreads) clip_total_kernel(double* part, int n_part) {
+    chain_wait();
+    chain_next();
+    const double d = sum_partials(part, n_part);
+    if (threadIdx.x == 0) part[0] = d;
+}
+
 // A whole, aligned chunk's share of a thread: 4 (bf16) or 8 accesses of 16 bytes.
 template <typename T>
 constexpr int kPieces = kChunk * (int)sizeof(T) / 16 / kThreads;
@@ -187,7 +211,8 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* out, int n, float c) 
     }
 }
 
-// n_part partials of all launches of clip_squares_kernel. norm_out is written by the last table's first CTA.
+// n_part partials of one launch of clip_squares_kernel, or the one that clip_total_kernel left. norm_out, where it is
+// given (in the first of several launches), is written by the first CTA.
 __global__ void __launch_bounds__(kThreads)
 clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n_part, float max_norm, float* norm_out) {
     const int64_t c0 = T.chunks * blockIdx.x / gridDim.x, c1 = T.chunks * (blockIdx.x + 1) / gridDim.x;
@@ -217,16 +242,9 @@ clip_scale_kernel(const __grid_constant__ ClipTable T, const double* part, int n
     if (c1 > c0 && (whole = find(c1 - 1, &x, &off, &n))) load();
     chain_wait();
     chain_next();
-    double d = 0.0;
-    for (int i = threadIdx.x; i < n_part; i += kThreads) d += part[i];
-#pragma unroll
-    for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-    __shared__ double w[kThreads / 32];
+    const double d = sum_partials(part, n_part);
     __shared__ float coef;
-    if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = d;
-    __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < kThreads / 32; ++i) d += w[i];
         // fp32 where the sum is an fp32 number (an fp64 root and quotient take a microsecond on these SMs);
         // a NaN norm is not <= max_norm and passes into every output
         float norm;
@@ -309,6 +327,11 @@ cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, floa
             return launch_chained(true, clip_scale_kernel, dim3((unsigned)grid), dim3(kThreads), 0, s, T, part, n_part,
                                   max_norm, norm);
         }
+    }
+    if (tables > 1) {
+        const cudaError_t e = launch_chained(true, clip_total_kernel, dim3(1), dim3(kThreads), 0, s, part, n_part);
+        if (e != cudaSuccess) return e;
+        n_part = 1;
     }
     int64_t i = 0;
     for (int k = 0; k < tables || k == 0; ++k) {  // without a tensor: one CTA, for the norm
