@@ -562,7 +562,10 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  *   Y     [M][d_out] (ld_y >= d_out). Y may be R (same pointer and stride).
  *   Z     [M][d_out] pre-activation for tda_linear_backward, or NULL (ld_z >= d_out).
  * Every tensor is of type L->dtype. Sums are fp32 (bf16: products of bf16 values,
- * exact; fp32: every product to 2^-24), one rounding per output; act is applied to
+ * exact; fp32: every product to 2^-24), one rounding per output. The sums of bf16
+ * layers are truncated every 16 products, by at most 2^-22 of sum |products| each
+ * time, for as long as the sum is (d_in; d_out for dX; the tokens for bf16 dW), and for
+ * 4096 tokens at a time for fp32 dW: 2^-14 in all. act is applied to
  * the unrounded sum, for bf16 layers with functions good to about 2^-20 of max(|z|, 1)
  * and, where the value itself is small (the tails of gelu and silu), to 2^-11 of it
  * down to 1e-36.

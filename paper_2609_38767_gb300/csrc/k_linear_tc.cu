@@ -11,6 +11,7 @@
 // tensor pipe adds into its fp32 accumulators with truncation, so for these every
 // chunk's sum is drained and added up in registers with rounding (error against 64
 // bits 1e-7 to 2e-7 of the result's norm up to K = 14336, below an fp32 FMA chain's).
+// So are the sums of bf16 products whose output is fp32, every 64 chunks.
 //
 // linear_pair_kernel, for products with a tile for most SM pairs: two CTAs of a
 // cluster hold one 256 x BN tile (cta_group::2), each staging 128 rows of P and half
@@ -51,10 +52,18 @@ constexpr uint32_t kBox = 64 * kTK * 2;  // one MN-major box of 64 values: 8 KiB
 template <bool ROUND>
 constexpr int kAcc = ROUND ? 4 : 2;
 
+// The truncation is always towards zero, so a long sum of one sign drifts with its length: weight gradients of 8192
+// tokens of 2048 -> 2304 were 2.4e-5 short, of 262144 1.5e-3. fp32 outputs are therefore drained every this many chunks
+// and are 8e-6 short at any length. In the pair kernel that costs 2 to 8 % from 4097 tokens on (us without / with, dX
+// beside dW: 8192 tokens of 2048 -> 8192 338 / 344, of 4096 -> 4096 317 / 323; dW alone 189 / 198; every 16 chunks,
+// 8e-7, 13 %), in the tile kernel nothing.
+constexpr int kWindow = 64;
+
 struct TileParams {
     LinearEpilogue ep;
     int64_t tiles_p, tiles_q;
     int nk;             // chunks of kTK along K
+    bool drain;         // bf16 operands: a fill of the accumulator is kWindow chunks, not all
     int split;          // CTAs of a cluster along K
     bool p_mn, q_mn;
     bool swap;          // tile rows are output columns
@@ -463,7 +472,7 @@ __device__ __forceinline__ void tile_body(const TileLaunch& pp) {
     const int rank = cta % p.split;
     const int64_t i0 = (tile / p.tiles_q) * kTM, j0 = (tile % p.tiles_q) * BN;
     const int t0 = (int)((int64_t)p.nk * rank / p.split), t1 = (int)((int64_t)p.nk * (rank + 1) / p.split);
-    const int windows = ROUND ? t1 - t0 : 1;  // accumulator fills
+    const int windows = ROUND ? t1 - t0 : p.drain ? (t1 - t0 + kWindow - 1) / kWindow : 1;  // accumulator fills
 
     if (warp == 0) {
         if (lane == 0) {
@@ -541,7 +550,8 @@ __device__ __forceinline__ void tile_body(const TileLaunch& pp) {
                     }
                     ++t;
                 } else {
-                    for (bool first = true; ok && t < t1; ++t, first = false) {
+                    const int end = p.drain && t1 - t > kWindow ? t + kWindow : t1;
+                    for (bool first = true; ok && t < end; ++t, first = false) {
                         const uint32_t s = ring.s, o = await(ring);
                         ring.next();
                         if (!ok) break;
@@ -580,7 +590,7 @@ __device__ __forceinline__ void tile_body(const TileLaunch& pp) {
             tc_fence_after();
             return got;
         };
-        if constexpr (!ROUND) {
+        if (!ROUND && windows == 1) {
             if (wait_for(0)) {
 #pragma unroll
                 for (int c = 0; c < kC; c += 16) {
@@ -590,19 +600,25 @@ __device__ __forceinline__ void tile_body(const TileLaunch& pp) {
                 }
             }
         } else {
+            constexpr int kL = ROUND ? kC : 16;  // columns loaded at once
             float acc[kC];
 #pragma unroll
             for (int i = 0; i < kC; ++i) acc[i] = 0.f;
             bool got = true;
             for (int w = 0; got && w < windows; ++w) {
                 if (!(got = wait_for(w))) break;
-                float v[kC];
-                tmem_load<kC>(tb + (w % kAcc<ROUND>) * BN, v);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&tempty[w % kAcc<ROUND>]));
 #pragma unroll
-                for (int i = 0; i < kC; ++i) acc[i] += v[i];
+                for (int c = 0; c < kC; c += kL) {
+                    float v[kL];
+                    tmem_load<kL>(tb + (w % kAcc<ROUND>) * BN + c, v);
+                    if (c + kL == kC) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&tempty[w % kAcc<ROUND>]));
+                    }
+#pragma unroll
+                    for (int i = 0; i < kL; ++i) acc[c + i] += v[i];
+                }
             }
             // the last window's MMAs have read every stage: the tile may take their place
             if (got)
@@ -762,8 +778,11 @@ __device__ __forceinline__ int64_t pair_tile(const PairParams& pp, int64_t i, in
     return pp.extra * idle + (i >= rem ? i - rem : i + idle) + j * n;
 }
 
-template <int BN, bool ROUND>
+// DRAIN: a product has fp32 outputs of bf16 operands and more than a window of chunks. A variant of its own: its 128 sums
+// a thread do not all fit the registers (1.1 KB of spills outside the loop over chunks), which the others need not pay.
+template <int BN, bool ROUND, bool DRAIN>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ PairParams pp) {
+    static_assert(!ROUND || !DRAIN, "fp32 operands are always drained");
     using S = PairShape<BN, ROUND>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -883,7 +902,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
               const uint64_t sp = desc_step(p_mn), sq = desc_step(q_mn);
               const uint32_t bar_full = smem_u32(full), bar_empty = smem_u32(empty);
               const uint64_t low_p = desc_of(smem_u32(smem), p_mn), low_q = desc_of(smem_u32(smem) + S::kP, q_mn);
-              const int total = p.nk, windows = ROUND ? total : 1;  // accumulator fills of a tile
+              const int total = p.nk, windows = ROUND ? total : DRAIN && p.drain ? (total + kWindow - 1) / kWindow : 1;  // fills of a tile
               for (int64_t j = 0; ok && pair_tile<g>(pp, me, pairs, j) < pp.tiles[g]; ++j) {
                 int t = 0;
                 for (int w = 0; ok && w < windows; ++w, acc.next()) {
@@ -921,7 +940,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         }
                         ++t;
                     } else {
-                        for (bool first = true; ok && t < total; ++t, first = false) {
+                        const int end = DRAIN && p.drain && total - t > kWindow ? t + kWindow : total;
+                        for (bool first = true; ok && t < end; ++t, first = false) {
                             const uint32_t s = ring.s, o = await(ring);
                             ring.next();
                             if (!ok) break;
@@ -970,8 +990,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             // This warp's rows and columns, a unit at a time: the row in registers (from `get`) through the epilogue
             // into shared memory, and out by TMA, which clips it at the matrix's edges. The residual's unit is
             // loaded 8 rows an access, one unit ahead, and handed to the rows' lanes through shared memory.
-            auto column_units = [&](auto zero, auto get) {
+            // held: the sums are registers already (`get` with places known at compile time), not one accumulator.
+            auto column_units = [&](auto zero, auto held, auto get) {
                 using T = decltype(zero);
+                constexpr bool kHeld = decltype(held)::value;
                 constexpr int kU = 64 / sizeof(T), E = 16 / sizeof(T);
                 // fp32 outputs of bf16 products are gradients: nothing but beta times themselves is added
                 constexpr bool kPlain = g == 1 || (!ROUND && sizeof(T) == 4);
@@ -1083,33 +1105,45 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     }
                 };
                 if (has_r) load_r(n0);
-                if (!ROUND && !(got = wait_for())) return;
-                if (ROUND || !p.ep.wide) {
+                if constexpr (ROUND) {
                     if (lane == 0) bulk_wait_read0();
-                    if (ROUND) {
 #pragma unroll
-                        for (int c = 0; c < kC; c += kU) values(c);  // the sums are registers
-                    } else {
-#pragma unroll 1
+                    for (int c = 0; c < kC; c += kU) values(c);
+                } else if constexpr (kHeld) {
+                    if (!p.ep.wide) {
+                        if (lane == 0) bulk_wait_read0();
+#pragma unroll
                         for (int c = 0; c < kC; c += kU) values(c);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < kC; c += kU) unit(c);
                     }
                 } else {
+                    if (!(got = wait_for())) return;
+                    if (!p.ep.wide) {
+                        if (lane == 0) bulk_wait_read0();
 #pragma unroll 1
-                    for (int c = 0; c < kC; c += kU) unit(c);
+                        for (int c = 0; c < kC; c += kU) values(c);
+                    } else {
+#pragma unroll 1
+                        for (int c = 0; c < kC; c += kU) unit(c);
+                    }
+                    release();
                 }
-                if (!ROUND) release();
             };
-            if constexpr (!ROUND) {
-                const uint32_t at = tb + (use & 1u) * BN;
-                if (p.ep.f32)
-                    column_units(float(), [&](int c, float* v) { tmem_load<16>(at + c, v); });
-                else
-                    column_units(__nv_bfloat16(), [&](int c, float* v) { tmem_load<32>(at + c, v); });
-            } else {
+            if (!ROUND && !(DRAIN && p.drain)) {
+                if constexpr (!ROUND) {
+                    const uint32_t at = tb + (use & 1u) * BN;
+                    if (p.ep.f32)
+                        column_units(float(), std::false_type(), [&](int c, float* v) { tmem_load<16>(at + c, v); });
+                    else
+                        column_units(__nv_bfloat16(), std::false_type(), [&](int c, float* v) { tmem_load<32>(at + c, v); });
+                }
+            } else if constexpr (ROUND || DRAIN) {
                 float acc[kC];
 #pragma unroll
                 for (int i = 0; i < kC; ++i) acc[i] = 0.f;
-                const int windows = p.nk;
+                const int windows = ROUND ? p.nk : (p.nk + kWindow - 1) / kWindow;
                 for (int w = 0; w < windows; ++w) {
                     if (!(got = wait_for())) break;
                     const uint32_t at = tb + (use % kAcc<ROUND>) * BN;
@@ -1123,7 +1157,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     release();
                 }
                 if (!got) break;
-                column_units(float(), [&](int c, float* v) {
+                column_units(float(), std::true_type(), [&](int c, float* v) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = acc[c + i];
                 });
@@ -1260,7 +1294,7 @@ cudaError_t run_tile(const Product* const* pr, int count, bool chained, cudaStre
     return cudaLaunchKernelEx(&cfg, linear_tile_kernel<BN, ROUND>, pp);
 }
 
-template <int BN, bool ROUND>
+template <int BN, bool ROUND, bool DRAIN>
 cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStream_t s) {
     using S = PairShape<BN, ROUND>;
     PairParams pp = {};
@@ -1286,7 +1320,7 @@ cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStre
     pp.err = pr[0]->p.err;
     // a tile costs its K loop and about two chunks of set-up
     pp.extra = count == 2 ? (pp.g[0].nk + 2 + (pp.g[1].nk + 2) / 2) / (pp.g[1].nk + 2) : 0;
-    cudaError_t e = smem_attr_once<linear_pair_kernel<BN, ROUND>>((int)S::kSmem);
+    cudaError_t e = smem_attr_once<linear_pair_kernel<BN, ROUND, DRAIN>>((int)S::kSmem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kThreads);
@@ -1297,12 +1331,12 @@ cudaError_t run_pair(const Product* const* pr, int count, bool chained, cudaStre
     cfg.attrs = at;
     cfg.numAttrs = 1;
     cfg.gridDim = dim3(2);
-    const int64_t most = max_clusters_once<linear_pair_kernel<BN, ROUND>>(cfg, 2, train_sms() / 2);
+    const int64_t most = max_clusters_once<linear_pair_kernel<BN, ROUND, DRAIN>>(cfg, 2, train_sms() / 2);
     const int64_t tiles = pp.tiles[0] + pp.tiles[1];
     cfg.gridDim = dim3((unsigned)(2 * (tiles < most ? tiles : most)));
     cfg.numAttrs = chained ? 2 : 1;
     note_launches(1);
-    return cudaLaunchKernelEx(&cfg, linear_pair_kernel<BN, ROUND>, pp);
+    return cudaLaunchKernelEx(&cfg, linear_pair_kernel<BN, ROUND, DRAIN>, pp);
 }
 
 template <bool ROUND>
@@ -1339,6 +1373,7 @@ static Product make_product(const LinearProduct& x, unsigned int* err) {
     r.p.ep = x.ep;
     r.p.ep.f32 = x.out == TDA_F32;
     r.p.nk = (int)((r.P.depth() + kTK - 1) / kTK);
+    r.p.drain = x.out == TDA_F32 && r.P.planes == 1 && r.p.nk > kWindow;
     r.p.split = 1;
     r.p.p_mn = r.P.mn;
     r.p.q_mn = r.Q.mn;
@@ -1415,7 +1450,12 @@ cudaError_t launch_linear_products(const LinearProduct* x, int count, bool chain
             return cudaSuccess;
         }
     }
-    if (pair <= tile) return round ? run_pair<128, true>(order, count, chained, s) : run_pair<256, false>(order, count, chained, s);
+    if (pair <= tile) {
+        if (round) return run_pair<128, true, false>(order, count, chained, s);
+        const bool drain = order[0]->p.drain || (count == 2 && order[1]->p.drain);
+        return drain ? run_pair<256, false, true>(order, count, chained, s)
+                     : run_pair<256, false, false>(order, count, chained, s);
+    }
     return round ? pick_tile<true>(order, count, chained, s) : pick_tile<false>(order, count, chained, s);
 }
 

@@ -211,3 +211,35 @@ def test_threads_with_streams_and_workspaces_of_their_own(dev):
     assert not failed
     for a, runs in zip(alone, got):
         assert len(runs) == 25 and all(torch.equal(x, y) for r in runs for x, y in zip(a, r))
+
+
+@pytest.mark.parametrize("M", [4095, 4160, 20011, 70000])
+@pytest.mark.parametrize("di,do", [(64, 128), (264, 520), (2048, 2304)])
+def test_long_sums_of_one_sign_do_not_drift(dev, M, di, do):
+    """fp32 dW of bf16 layers from operands of one sign. The tensor pipe adds 16 products at a time with truncation, at most
+    2^-22 of the running sum, for 4096 tokens; what comes then is added with rounding, 2^-24 a time:
+    256 * 2^-22 + (M / 4096 + 2) * 2^-24. Truncation on average takes half of a step of a sum that is half as
+    large: no more than a quarter of the first term in the mean, which is what would grow with M."""
+    gen = torch.Generator(device=dev).manual_seed(M + di)
+    X = (torch.rand((M, di), generator=gen, device=dev) + 0.5).bfloat16()
+    dY = (torch.rand((M, do), generator=gen, device=dev) + 0.5).bfloat16()
+    W = torch.randn((do, di), generator=gen, device=dev).bfloat16()
+    old = torch.rand((do, di), generator=gen, device=dev) * M
+    L = tda.LinearDesc(di, do, tda.TDA_ACT_NONE, tda.TDA_BF16)
+    ws, wsb = workspace(tda.TDA_LINEAR_BACKWARD, L, M, dev)
+    ref = torch.zeros((do, di), dtype=F64, device=dev)
+    for m in range(0, M, 8192):
+        ref += dY[m:m + 8192].to(F64).t() @ X[m:m + 8192].to(F64)
+    pipe, rnd = 256 * 2.0 ** -22, (M / 4096 + 2) * 2.0 ** -24
+    for with_dx, beta in ((False, 0.0), (True, 0.0), (True, 1.0)):
+        dX, dW = torch.empty_like(X), old.clone()
+        tda.tda_linear_backward(L, dY, do, None, 0, M, X, di, W, di, None, 0, dX if with_dx else None, di, dW, di, None,
+                                tda.TDA_F32, beta, ws, wsb)
+        tda.tda_device_status()
+        want = ref + beta * old.to(F64)
+        off = (dW.to(F64) - want) / want
+        assert float(off.abs().max()) <= pipe + rnd, float(off.abs().max())
+        assert abs(float(off.mean())) <= pipe / 4 + rnd, float(off.mean())
+        if with_dx:
+            dx = dY.to(F64) @ W.to(F64)
+            assert float((dX.to(F64) - dx).norm() / dx.norm()) <= 2.4e-3
