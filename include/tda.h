@@ -592,7 +592,8 @@ typedef enum { TDA_I32 = 0, TDA_I64 = 1 } tda_index_type;
  * themselves). ws: scratch, 256-byte aligned. tda_linear_workspace_size(op, L, M)
  * bytes are enough when every tensor starts on 16 bytes and every stride is its
  * row length, or any multiple of 8 elements that is no shorter; for any other
- * pointers or strides add TDA_LINEAR_ANY_STRIDE to op. Runs on sm_103 only.
+ * pointers or strides add TDA_LINEAR_ANY_STRIDE to op. Sizes are below 2^31 - 1, a
+ * matrix has at most 2^47 elements. Runs on sm_103 only.
  * An infinite or NaN element of X or W makes the outputs that it enters
  * non-finite (for fp32 layers NaN may stand where infinity would; relu of -inf is
  * 0). act(+inf) is +inf, act(-inf) NaN but for relu; act'(Z) of an infinite Z is the
@@ -651,7 +652,8 @@ tda_status tda_embedding_forward(tda_dtype dtype, const void* E, int64_t ld_e, i
  *   dE          device, V rows of d values of grad_dtype, row stride ld_e >= d. With
  *               beta 0 every row is overwritten (zeros where no token names it);
  *               with beta 1 only the named rows are touched.
- *   ws          >= tda_embedding_workspace_size(V, d, n) bytes, 256-byte aligned.
+ *   ws          >= tda_embedding_workspace_size(V, d, n) bytes, 256-byte aligned
+ *               (0 for sizes that the call refuses).
  * ------------------------------------------------------------------------- */
 size_t tda_embedding_workspace_size(int64_t V, int64_t d, int64_t n);
 tda_status tda_embedding_backward(tda_dtype dtype, const void* dout, int64_t ld_d, int64_t V, int64_t d,
@@ -670,7 +672,8 @@ tda_status tda_embedding_backward(tda_dtype dtype, const void* dout, int64_t ld_
  *             unclipped (it counts in the norm). No other overlap.
  *   max_norm  > 0; +inf: c = 1.
  *   norm      device fp32, the norm before clipping.
- *   ws        >= tda_grad_clip_workspace_size(list, n_tensors) bytes, 16-byte aligned.
+ *   ws        >= tda_grad_clip_workspace_size(list, n_tensors) bytes, 16-byte aligned
+ *             (0 for an n_tensors that the call refuses: at most 2^20).
  * The sum of squares is held in more than 32 bits and covers the whole range of
  * fp32 values (no overflow below a norm of 3e38, no underflow). An infinite norm
  * gives c = 0 (an infinite element then becomes NaN); a NaN element makes the norm

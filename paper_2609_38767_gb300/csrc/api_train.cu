@@ -11,13 +11,14 @@ namespace {
 size_t el_size(int32_t dt) { return dt == TDA_BF16 ? 2 : 4; }
 bool float_type(int32_t dt) { return dt == TDA_BF16 || dt == TDA_F32; }
 bool aligned_to(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 2;
+constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 2, kMaxRow = 1 << 22, kMaxMatrix = (int64_t)1 << 47;
+constexpr int64_t kMaxTensors = 1 << 20;
 
 tda_status check_table(tda_dtype dtype, int64_t V, int64_t d, int32_t it, const void* tokens, int64_t n, float scale,
                        const char* who) {
     if (!float_type(dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
     if (it != TDA_I32 && it != TDA_I64) return fail(TDA_ERR_INVALID_ARG, "%s: index type must be TDA_I32 or TDA_I64", who);
-    if (V < 1 || V > kMaxCount || d < 1 || d > (1 << 22) || n < 0 || n > kMaxCount)
+    if (V < 1 || V > kMaxCount || d < 1 || d > kMaxRow || n < 0 || n > kMaxCount)
         return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes V=%lld d=%lld n=%lld", who, (long long)V, (long long)d,
                     (long long)n);
     if (!std::isfinite(scale)) return fail(TDA_ERR_INVALID_ARG, "%s: scale must be finite", who);
@@ -31,6 +32,11 @@ tda_status check_linear(const tda_linear_desc* L, int64_t M, const char* who) {
     if (L->d_in < 1 || L->d_out < 1 || L->d_in > kMaxCount || L->d_out > kMaxCount || M < 0 || M > kMaxCount)
         return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes d_in=%lld d_out=%lld M=%lld", who, (long long)L->d_in,
                     (long long)L->d_out, (long long)M);
+    // matrices past any memory, whose scratch would wrap a size_t
+    for (int64_t n : {M * L->d_in, M * L->d_out, L->d_in * L->d_out})
+        if (n > kMaxMatrix)
+            return fail(TDA_ERR_INVALID_ARG, "%s: a matrix of more than 2^47 elements (d_in=%lld d_out=%lld M=%lld)", who,
+                        (long long)L->d_in, (long long)L->d_out, (long long)M);
     if (L->act < TDA_ACT_NONE || L->act > TDA_ACT_SILU) return fail(TDA_ERR_INVALID_ARG, "%s: bad activation %d", who, L->act);
     if (!float_type(L->dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
     return TDA_OK;
@@ -173,7 +179,7 @@ tda_status tda_embedding_forward(tda_dtype dtype, const void* E, int64_t ld_e, i
 }
 
 size_t tda_embedding_workspace_size(int64_t V, int64_t d, int64_t n) {
-    if (V < 1 || d < 1 || n < 0 || n > kMaxCount) return 0;
+    if (V < 1 || V > kMaxCount || d < 1 || d > kMaxRow || n < 0 || n > kMaxCount) return 0;
     return embedding_workspace_bytes(d, n);
 }
 
@@ -207,14 +213,14 @@ tda_status tda_embedding_backward(tda_dtype dtype, const void* dout, int64_t ld_
 
 size_t tda_grad_clip_workspace_size(const tda_tensor_ref* list, int64_t n_tensors) {
     (void)list;
-    if (n_tensors < 0) return 0;
+    if (n_tensors < 0 || n_tensors > kMaxTensors) return 0;
     return clip_workspace_bytes(n_tensors);
 }
 
 tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, void* ws,
                          size_t ws_bytes, void* stream) {
     clear_message();
-    if (n_tensors < 0 || n_tensors > (1LL << 20) || (n_tensors > 0 && !list))
+    if (n_tensors < 0 || n_tensors > kMaxTensors || (n_tensors > 0 && !list))
         return fail(TDA_ERR_INVALID_ARG, "tda_grad_clip: list is NULL or n_tensors not in [0, 2^20]");
     if (!(max_norm > 0)) return fail(TDA_ERR_INVALID_ARG, "tda_grad_clip: max_norm must be > 0");
     if (!norm || !aligned_to(norm, 4)) return fail(TDA_ERR_INVALID_ARG, "tda_grad_clip: norm is NULL or misaligned");

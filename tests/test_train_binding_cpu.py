@@ -96,3 +96,21 @@ def test_bias_gradient_scratch_is_one_wave_of_partial_sums(dtype, width):
         most = min(256, max(1, 4 * 152 // blocks))
         run = max(32, -(-M // most))
         assert up256(4 * -(-M // run) * do) == total - planes
+
+
+def test_workspace_sizes_do_not_wrap():
+    """Sizes whose scratch passes 64 bits are refused, not answered with what is left of it."""
+    big = (1 << 31) - 8
+    for dtype in (tda.TDA_BF16, tda.TDA_F32):
+        for di, do, M in ((big, big, big), (big, 8, big), (1, big, big), (big, big, 1)):
+            for op in (tda.TDA_LINEAR_FORWARD, tda.TDA_LINEAR_BACKWARD, tda.TDA_LINEAR_BACKWARD | tda.TDA_LINEAR_ANY_STRIDE):
+                with pytest.raises(tda.TdaError) as e:
+                    tda.tda_linear_workspace_size(op, tda.LinearDesc(di, do, 0, dtype), M)
+                assert e.value.status == tda.TDA_ERR_INVALID_ARG
+        # the largest that fit: three planes of fp32, every matrix of 2^46 elements at most
+        L = tda.LinearDesc(1 << 23, 1 << 23, 0, dtype)
+        size = tda.tda_linear_workspace_size(tda.TDA_LINEAR_BACKWARD | tda.TDA_LINEAR_ANY_STRIDE, L, 1 << 23)
+        assert size >= 3 * (1 << 46) * (6 if dtype == tda.TDA_F32 else 2)
+    assert tda.tda_embedding_workspace_size(10, 1 << 62, 1000) == 0 and tda.tda_embedding_workspace_size(10, 1 << 23, 5) == 0
+    assert tda.tda_embedding_workspace_size(1 << 40, 8, 1000) == 0 and tda.tda_embedding_workspace_size(10, 1 << 22, 5) > 0
+    assert tda.tda_grad_clip_workspace_size(None, 1 << 62) == 0 and tda.tda_grad_clip_workspace_size(None, 1 << 20) > 0
