@@ -21,19 +21,21 @@ static __typeof__(&tda_embedding_forward) f_embedding_forward;
 static __typeof__(&tda_embedding_backward) f_embedding_backward;
 static __typeof__(&tda_grad_clip) f_grad_clip;
 
-/* An argument that does not convert leaves a Python error set; the caller looks once, before the call. */
-static long long as_int(PyObject *o) { return PyLong_AsLongLong(o); }
+/* An argument that does not convert leaves a Python error set; the caller looks once, before the call. Until then no
+ * Python code runs for the arguments after it, which would turn the error into a SystemError. */
+static long long as_int(PyObject *o) { return PyLong_Check(o) || !PyErr_Occurred() ? PyLong_AsLongLong(o) : 0; }
 static size_t as_size(PyObject *o) {
     const long long v = as_int(o);
     if (v < 0 && !PyErr_Occurred()) PyErr_SetString(PyExc_OverflowError, "a workspace size is not negative");
     return (size_t)v;
 }
-static double as_float(PyObject *o) { return PyFloat_AsDouble(o); }
+static double as_float(PyObject *o) { return PyFloat_Check(o) || !PyErr_Occurred() ? PyFloat_AsDouble(o) : 0; }
 static void *as_address(PyObject *o) { return PyLong_AsVoidPtr(o); }
 
 static void *as_ptr(PyObject *o) {
     if (o == Py_None) return NULL;
     if (PyLong_Check(o)) return as_address(o);
+    if (PyErr_Occurred()) return NULL;
     PyObject *a = PyObject_CallMethodNoArgs(o, str_data_ptr);
     if (!a) return NULL;
     void *p = as_address(a);
@@ -43,6 +45,7 @@ static void *as_ptr(PyObject *o) {
 
 static void *as_stream(PyObject *o) {
     if (PyLong_Check(o)) return as_address(o);
+    if (PyErr_Occurred()) return NULL;
     PyObject *a = o == Py_None ? PyObject_CallNoArgs(current_stream) : PyObject_GetAttr(o, str_cuda_stream);
     if (!a) return NULL;
     void *p = as_address(a);

@@ -114,3 +114,32 @@ def test_workspace_sizes_do_not_wrap():
     assert tda.tda_embedding_workspace_size(10, 1 << 62, 1000) == 0 and tda.tda_embedding_workspace_size(10, 1 << 23, 5) == 0
     assert tda.tda_embedding_workspace_size(1 << 40, 8, 1000) == 0 and tda.tda_embedding_workspace_size(10, 1 << 22, 5) > 0
     assert tda.tda_grad_clip_workspace_size(None, 1 << 62) == 0 and tda.tda_grad_clip_workspace_size(None, 1 << 20) > 0
+
+
+def test_the_first_bad_argument_is_the_error():
+    """Tensors after an argument that does not convert: its own error comes out, and none of their code runs before."""
+    import torch
+
+    t = torch.zeros(8)
+
+    class Touched:
+        def data_ptr(self):
+            raise AssertionError("called after an error")
+
+        __index__ = __float__ = data_ptr
+
+        @property
+        def cuda_stream(self):
+            raise AssertionError("read after an error")
+
+    def lookup(ld_e=8, E=t, out=t, n=3, scale=1.0, stream=0):
+        tda.tda_embedding_forward(tda.TDA_F64, E, ld_e, 4, 8, tda.TDA_I32, t, n, scale, out, 8, stream=stream)
+
+    for bad in (dict(ld_e=1.5), dict(ld_e="x"), dict(E="x"), dict(ld_e=1 << 70), dict(scale="a")):
+        for later in (dict(), dict(out=Touched()), dict(stream=Touched())) + ((dict(n=Touched()),) if "scale" not in bad else ()):
+            with pytest.raises((TypeError, AttributeError, OverflowError)):
+                lookup(**bad, **later)
+    with pytest.raises(TypeError):
+        tda.tda_linear_forward(b"short", t, 64, 1, t, 64, None, None, 0, t, 32, stream=0)
+    with pytest.raises(tda.TdaError):  # every argument converts: the library refuses the type
+        lookup()
