@@ -214,7 +214,7 @@ def test_threads_with_streams_and_workspaces_of_their_own(dev):
 
 
 @pytest.mark.parametrize("M", [4095, 4160, 20011, 70000])
-@pytest.mark.parametrize("di,do", [(64, 128), (264, 520), (2048, 2304)])
+@pytest.mark.parametrize("di,do", [(64, 128), (264, 520), (2048, 2304), (1801, 2563)])
 def test_long_sums_of_one_sign_do_not_drift(dev, M, di, do):
     """fp32 dW of bf16 layers from operands of one sign. The tensor pipe adds 16 products at a time with truncation, at most
     2^-22 of the running sum, for 4096 tokens; what comes then is added with rounding, 2^-24 a time:
@@ -243,3 +243,41 @@ def test_long_sums_of_one_sign_do_not_drift(dev, M, di, do):
         if with_dx:
             dx = dY.to(F64) @ W.to(F64)
             assert float((dX.to(F64) - dx).norm() / dx.norm()) <= 2.4e-3
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,di,do", [(1, 16384, 520), (4, 8192, 264), (16, 20001, 130), (33, 14336, 1000), (300, 16384, 392),
+                                     (1100, 8200, 2056)])
+def test_long_rows(dev, M, di, do, dtype):
+    """Sums over 8192 and more inputs, through each kernel, and dX over as many outputs. Bounds of test_gpu_linear.py: bf16
+    (K / 16 + 16) 2^-22 of the sum of |products|, fp32 24 * 2^-22 + (6 K / 256 + 8) 2^-24, few fp32 rows a chain
+    of K / 32 additions; then half an ulp."""
+    gen = torch.Generator(device=dev).manual_seed(di + M)
+    mk = lambda *s: torch.randn(s, generator=gen, device=dev).to(dtype)
+    X, W, b = mk(M, di), (mk(do, di).float() / math.sqrt(di)).to(dtype), mk(do)
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+
+    def bound(K):
+        if dtype == torch.bfloat16:
+            return (K / 16 + 16) * 2.0 ** -22
+        return max(24 * 2.0 ** -22 + (6 * K / 256 + 8) * 2.0 ** -24, (K / 32 + 8) * 2.0 ** -24)
+
+    def check(got, ref, size, K):
+        t = bound(K) * size + 2.0 ** -23 * size
+        off = (got.to(F64) - ref).abs()
+        assert bool((off <= t + half * (ref.abs() + t)).all()), float((off / size).max())
+        assert float(off.norm() / ref.norm()) <= (2.4e-3 if dtype == torch.bfloat16 else 1.5e-6)
+
+    L = tda.LinearDesc(di, do, tda.TDA_ACT_NONE, KIND[dtype])
+    ws, wsb = workspace(tda.TDA_LINEAR_BACKWARD, L, M, dev)
+    Y = torch.empty((M, do), dtype=dtype, device=dev)
+    tda.tda_linear_forward(L, X, di, M, W, di, b, None, 0, Y, do, None, 0, ws, wsb)
+    tda.tda_device_status()
+    check(Y, X.to(F64) @ W.to(F64).t() + b.to(F64), X.to(F64).abs() @ W.to(F64).abs().t() + b.to(F64).abs(), di)
+    # the transposed layer: di outputs, dX sums over them
+    Wt, T = W.t().contiguous(), tda.LinearDesc(do, di, tda.TDA_ACT_NONE, KIND[dtype])
+    ws, wsb = workspace(tda.TDA_LINEAR_BACKWARD, T, M, dev)
+    dX = torch.empty((M, do), dtype=dtype, device=dev)
+    tda.tda_linear_backward(T, X, di, None, 0, M, None, 0, Wt, do, None, 0, dX, do, None, 0, None, tda.TDA_F32, 0.0, ws, wsb)
+    tda.tda_device_status()
+    check(dX, X.to(F64) @ W.to(F64).t(), X.to(F64).abs() @ W.to(F64).abs().t(), di)
