@@ -546,7 +546,8 @@ int32_t tda_get_sm_budget(void);
  * The training step around the attributed linears. The paper takes the factors
  * (a, g) of Eq. 1 from a model's forward and backward pass; the calls below are
  * the parts of such a pass that the linear layers sit in, so that a job can make
- * its factors with this library and attribute the update that was applied.
+ * its factors with this library and take the step as well. (The factors are those
+ * of the gradient before clipping, which scales a whole step by one number.)
  * They share the conventions above (device pointers, caller-owned buffers and
  * scratch, asynchronous on `stream`, arguments validated before any launch) and
  * allow CUDA-graph capture. dtype is TDA_BF16 or TDA_F32; strides are in elements.

@@ -12,7 +12,9 @@ that the step left are projected as they lie, [N][T][d] (tda_project), and score
 
     python -m paper_2609_38767_gb300.capture     # a few steps, then the examples that moved a query
 
-Only the loss (a softmax over the vocabulary) and the update are torch operations.
+The features are those of the gradient before clipping: the clipping scales the step's whole gradient, and so all its
+examples' features, by one number. The loss (a softmax over the vocabulary), the sum of the two gradients that meet at
+a residual and the update are torch operations.
 """
 from __future__ import annotations
 

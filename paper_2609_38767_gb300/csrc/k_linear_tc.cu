@@ -18,14 +18,14 @@
 // of Q, so an operand byte that reaches an SM feeds twice the MMAs; persistent, the
 // epilogue of a tile beside the next tile's MMAs, bf16 outputs by TMA. Bound by the
 // tensor pipe at the clock that the power limit leaves: 8192 x 14336 -> 4096 bf16
-// 515-540 us = 1.78-1.87 PFLOP/s (468 us without loads and epilogue), 4096 x 2048 -> 8192 with
-// tanh-gelu and Z 86-88 us (75 without its epilogue); fp32 2048 x 4096 -> 4096 297 us
-// = 231 TFLOP/s, six bf16 products each.
+// 590-605 us = 1.59-1.63 PFLOP/s as calls on new inputs, 512-580 one launch after another (468 without loads and
+// epilogue), 4096 x 2048 -> 8192 with tanh-gelu and Z 99 us as calls, 86 launch after launch (75 without its
+// epilogue); fp32 2048 x 4096 -> 4096 300 us = 229 TFLOP/s, six bf16 products each.
 //
 // linear_tile_kernel: one 128 x BN tile per CTA. Few rows (a short batch) swap the
 // operands, so the long side fills the 128 rows of a tile, and split the K loop over
 // the CTAs of a cluster, whose fp32 tiles are added in rank order through distributed
-// shared memory. Bound by reading W: 16 x 4096 -> 14336 24.8 us = 4.7 TB/s.
+// shared memory. Bound by reading W: 16 x 4096 -> 14336 23-25 us = 4.7-5.1 TB/s.
 //
 // Warp roles: warp 0 TMA producer (lane 0), warp 1 TMEM allocator and MMA issuer,
 // warps 2-9 epilogue (TMEM lane quadrant warp % 4, column half by warp). Waits are
