@@ -255,6 +255,7 @@ __global__ void __launch_bounds__(kThreads) cols_kernel(const __grid_constant__ 
         for (int w = 1; w < kWarps; ++w) v += (&sh[w][0][0])[i];
         (&sum[0][0])[i] = v;
     }
+    __syncwarp();  // the barrier's aligned form is one instruction of the whole warp
     cluster_barrier();
     // each CTA adds a share of the columns over the cluster, in rank order
     constexpr int kOut = MT * 128 / kColsCluster;
@@ -266,6 +267,7 @@ __global__ void __launch_bounds__(kThreads) cols_kernel(const __grid_constant__ 
         const int64_t m = m0 + i / 128, k = (int64_t)(blockIdx.x / kColsCluster) * 128 + i % 128;
         if (m < p.M && k < p.K) p.dX[m * p.ld_dx + k] = v;
     }
+    __syncwarp();
     cluster_barrier();  // no CTA leaves while its sums are still read
 }
 

@@ -815,6 +815,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         pair_relinquish();
     }
     tc_fence_before();
+    __syncwarp();
     cluster_sync();  // both CTAs' barriers exist before either signals the other's
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;

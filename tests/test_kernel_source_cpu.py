@@ -90,3 +90,18 @@ def test_the_sm_count_is_the_devices():
     for name in ("k_linear.cu", "k_linear_rows.cu", "k_linear_tc.cu", "k_clip.cu", "k_embedding.cu", "linear.cuh"):
         text = source(name)
         assert not re.search(r"\b152\b", text) and "cudaDevAttrMultiProcessorCount" not in text, name
+
+
+def test_cluster_barriers_are_met_by_whole_warps():
+    """barrier.cluster's aligned form has to be one instruction of all 32 lanes: each use in the linear layer's kernels comes
+    after a __syncwarp() with no branch of single lanes between them."""
+    found = 0
+    for name in ("k_linear_tc.cu", "k_linear_rows.cu"):
+        text = source(name)
+        for m in re.finditer(r"\bcluster_(sync|barrier)\(\);", text):
+            found += 1
+            before = text[:m.start()].rstrip()
+            before = re.sub(r"if \(p\.split > 1\)$", "", before).rstrip()  # the same in every thread of the launch
+            before = re.sub(r"tc_fence_before\(\);$", "", before).rstrip()
+            assert before.endswith("__syncwarp();"), (name, text[m.start() - 120:m.end()])
+    assert found == 6
