@@ -10,7 +10,7 @@
  * per-example gradient norms and cosine scores, token-level score
  * decompositions and random-mask reductions from the same factors, and runs the
  * parts of a training step that make them (linear layers with their backward pass,
- * embedding, gradient clipping; last section).
+ * embedding, gradient clipping, attention, norm; last section).
  *
  * Notation. A linear layer z = W a has W in R^{N_o x N_i}. For one example with
  * T token positions the paper's factors are a in R^{N_i x T} and g = Dz in
@@ -691,6 +691,123 @@ typedef struct {
 size_t tda_grad_clip_workspace_size(const tda_tensor_ref* list, int64_t n_tensors);
 tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, void* ws,
                          size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tda_attention_forward -- masked attention of N examples of T tokens, heads of
+ * head_dim values; query head h reads key/value head h / (heads / kv_heads):
+ *   x_ij = scale q_i . k_j,   c_ij = cap tanh(x_ij / cap)   (cap 0: c = x),
+ *   s_ij = c_ij + table[bucket[i - j]][h] - slope[h] |i - j|,
+ *   O_i  = sum_j P_ij v_j,   P_ij = exp(s_ij - lse_i),   lse_i = log sum_j exp s_ij,
+ * the sums over the keys that token i sees: lo_i <= j < hi_i, of the same example.
+ *   Q, O   N*T rows (token t of example n is row n*T + t), row strides ld_q, ld_o >=
+ *          heads * head_dim; head h has columns [h*head_dim, (h+1)*head_dim).
+ *   K, V   the same with kv_heads heads. Q, K, V may be columns of one tensor.
+ *   range  [N][T][2] int32, lo and hi of each token (see tda_attention_ranges), clamped
+ *          to [0, T]; hi <= lo: the token sees nothing, its O is 0 and its lse -inf.
+ *          NULL: every key, or with causal keys up to the token itself (causal is not
+ *          read where a range is given).
+ *   bucket [2*max_distance + 1] int32: bucket of the distance i - j, clamped to
+ *          +-max_distance, at index max_distance + (i - j); an entry outside
+ *          [0, n_buckets) adds nothing. tda_position_buckets makes the usual map.
+ *   table  [n_buckets][heads] of L->dtype, the learned bias (n_buckets 0: none, neither
+ *          is read). slope: [heads] fp32, or NULL.
+ *   lse    [N][heads][T] fp32, natural logarithm, or NULL.
+ * Sums and statistics are fp32. bf16: products of bf16 values, P rounded to bf16 for the
+ * product with V (its sum is of the unrounded values); fp32: fp32 throughout.
+ * A bias of -inf hides a pair, and a row whose pairs are all hidden is one that sees
+ * nothing. What lies in a token that no token sees, or in the query of one that sees
+ * nothing, may be anything, NaN included. A NaN or infinity elsewhere may make other rows of
+ * its example and head non-finite.
+ * head_dim <= 128 (else TDA_ERR_UNSUPPORTED); any strides and element alignment; bf16 with
+ * head_dim a multiple of 8 and rows on 16 bytes runs on the tensor cores (sm_103), anything
+ * else on the CUDA cores. N or T may be 0. ws: tda_attention_workspace_size(op, L) bytes,
+ * 256-byte aligned.
+ *
+ * tda_attention_backward -- its gradients, given O and lse of the forward pass and dO:
+ *   dV_j = sum P_ij dO_i,   dP_ij = dO_i . v_j,   dS_ij = P_ij (dP_ij - dO_i . O_i),
+ *   dX_ij = scale dS_ij (1 - (c_ij/cap)^2),   dQ_i = sum_j dX_ij k_j,   dK_j = sum dX_ij q_i,
+ *   dtable[b][h] = beta dtable[b][h] + sum of dS_ij over the pairs of bucket b,
+ * dK and dV summed over the query heads that share them. dS of a token that sees a single
+ * key is 0. P and dX are rounded to bf16 for bf16 products; dO . O takes O as it was stored
+ * (bf16: an error of up to 2^-9 of |dO||O| in every dS of a row, in dtable too).
+ *   dQ, dK, dV  of L->dtype, overwritten; strides as Q, K, V. They overlap nothing else.
+ *   dtable      [n_buckets][heads] of grad_dtype (TDA_F32, or TDA_BF16 for bf16 inputs), or
+ *               NULL. slope has no gradient.
+ * Every sum has a fixed order: equal calls give equal bits.
+ *
+ * tda_attention_ranges -- the ranges of packed documents and prefixes:
+ *   doc     [N][T] int32: a document is a maximal run of equal ids, a negative id is
+ *           padding (sees nothing, seen by none). NULL: one document per example.
+ *   prefix  [N][T] int32, or NULL: a document's prefix is its leading run of non-zero
+ *           values; with causal every token of the document sees all of it.
+ *   causal  1: keys up to the token itself (and the prefix); 0: the whole document.
+ *   window  0, or w: of these only keys with |i - j| < w.
+ *
+ * tda_position_buckets -- host only: fills bucket[2*max_distance + 1] (host memory) so that
+ * with b buckets in a direction the distances 0 ... e - 1, e = b/2 rounded down, have one
+ * each and a longer distance d has e + floor((b - e) log(d/e) / log(max_distance/e)), at
+ * most b - 1. bidirectional: the second half of the buckets is for later keys (i < j); else
+ * later keys have bucket 0. n_buckets in [2, 1024] (bidirectional: even, >= 4), max_distance
+ * in (e, 2^20].
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int64_t N;            /* examples */
+    int64_t T;            /* tokens per example */
+    int32_t heads;        /* query heads */
+    int32_t kv_heads;     /* key/value heads, a divisor of heads */
+    int32_t head_dim;
+    int32_t dtype;        /* tda_dtype: TDA_BF16 or TDA_F32 */
+    float scale;          /* > 0 */
+    float cap;            /* >= 0 */
+    int32_t causal;       /* 0 or 1 */
+    int32_t n_buckets;    /* 0 ... 1024 */
+    int64_t max_distance; /* 0 ... 2^20 */
+} tda_attention_desc;
+
+#define TDA_ATTENTION_FORWARD 0
+#define TDA_ATTENTION_BACKWARD 1
+
+tda_status tda_attention_workspace_size(int32_t op, const tda_attention_desc* L, size_t* bytes);
+tda_status tda_attention_forward(const tda_attention_desc* L, const void* Q, int64_t ld_q, const void* K, int64_t ld_k,
+                                 const void* V, int64_t ld_v, const int32_t* range, const int32_t* bucket,
+                                 const void* table, const float* slope, void* O, int64_t ld_o, float* lse, void* ws,
+                                 size_t ws_bytes, void* stream);
+tda_status tda_attention_backward(const tda_attention_desc* L, const void* Q, int64_t ld_q, const void* K, int64_t ld_k,
+                                  const void* V, int64_t ld_v, const int32_t* range, const int32_t* bucket,
+                                  const void* table, const float* slope, const void* O, int64_t ld_o, const float* lse,
+                                  const void* dO, int64_t ld_do, void* dQ, int64_t ld_dq, void* dK, int64_t ld_dk,
+                                  void* dV, int64_t ld_dv, void* dtable, tda_dtype grad_dtype, float beta, void* ws,
+                                  size_t ws_bytes, void* stream);
+tda_status tda_attention_ranges(int64_t N, int64_t T, const int32_t* doc, const int32_t* prefix, int32_t causal,
+                                int64_t window, int32_t* range, void* stream);
+tda_status tda_position_buckets(int32_t n_buckets, int64_t max_distance, int32_t bidirectional, int32_t* bucket);
+
+/* ---------------------------------------------------------------------------
+ * tda_rmsnorm_forward -- root-mean-square norm of M rows with the residual's addition:
+ *   h = x + r,   rstd = 1 / sqrt(mean of h^2 + eps),   y = h rstd w.
+ * The norm reads h as it is stored (rounded to dtype). y is the factor A of the linear
+ * layer after it.
+ *   x, r, h, y  M rows of d values, strides >= d; r NULL: h = x; h NULL: not stored. h and y may be
+ *               x or r (same pointer and stride), but not one another.
+ *   w     [d].  rstd  [M] fp32, or NULL.  eps > 0.
+ * tda_rmsnorm_backward -- its gradients, n = h rstd, g = dy w:
+ *   dx = dres + rstd (g - n mean(g n)),   dw = beta dw + sum over rows of dy n.
+ *   dres  gradient of h from elsewhere (the residual stream), or NULL. dx is the gradient of
+ *         x and of r; it may be dy or dres (same pointer and stride).
+ *   dx, dw  NULL: not computed. grad_dtype: type of dw, TDA_F32, or TDA_BF16 for bf16 rows.
+ *   ws    >= tda_rmsnorm_workspace_size(M, d) bytes, 256-byte aligned (for dw only; 0 for sizes
+ *         that the call refuses).
+ * Sums are fp32, in a fixed order. d <= 32768 (else TDA_ERR_UNSUPPORTED), any strides and
+ * element alignment. A row of zeros (padding) gives zeros.
+ * ------------------------------------------------------------------------- */
+tda_status tda_rmsnorm_forward(tda_dtype dtype, const void* x, int64_t ld_x, const void* r, int64_t ld_r, int64_t M,
+                               int64_t d, const void* w, float eps, void* h, int64_t ld_h, void* y, int64_t ld_y,
+                               float* rstd, void* stream);
+size_t tda_rmsnorm_workspace_size(int64_t M, int64_t d);
+tda_status tda_rmsnorm_backward(tda_dtype dtype, const void* h, int64_t ld_h, const float* rstd, const void* w,
+                                const void* dy, int64_t ld_dy, const void* dres, int64_t ld_r, int64_t M, int64_t d,
+                                void* dx, int64_t ld_dx, void* dw, tda_dtype grad_dtype, float beta, void* ws,
+                                size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,8 @@ __all__ = [
     "TensorRef", "tensor_list", "tda_embedding_forward", "tda_embedding_workspace_size", "tda_embedding_backward",
     "tda_grad_clip_workspace_size", "tda_grad_clip",
     "LinearDesc", "tda_linear_workspace_size", "tda_linear_forward", "tda_linear_backward",
+    "AttentionDesc", "tda_attention_workspace_size", "tda_attention_ranges", "tda_position_buckets", "tda_attention_forward",
+    "tda_attention_backward", "tda_rmsnorm_forward", "tda_rmsnorm_workspace_size", "tda_rmsnorm_backward",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -47,6 +49,7 @@ TDA_KFAC, TDA_EKFAC = 0, 1
 TDA_I32, TDA_I64 = 0, 1
 TDA_ACT_NONE, TDA_ACT_RELU, TDA_ACT_GELU, TDA_ACT_GELU_TANH, TDA_ACT_SILU = 0, 1, 2, 3, 4
 TDA_LINEAR_FORWARD, TDA_LINEAR_BACKWARD, TDA_LINEAR_ANY_STRIDE = 0, 1, 256
+TDA_ATTENTION_FORWARD, TDA_ATTENTION_BACKWARD = 0, 1
 TDA_CALIBRATE_WS_BYTES = 768 << 20
 _STATUS = {0: "TDA_OK", 1: "TDA_ERR_INVALID_ARG", 2: "TDA_ERR_UNSUPPORTED", 3: "TDA_ERR_WORKSPACE",
            4: "TDA_ERR_CUDA", 5: "TDA_ERR_NOT_SPD", 6: "TDA_ERR_TIMEOUT"}
@@ -68,6 +71,18 @@ class LinearDesc(ctypes.Structure):
 
     def __init__(self, d_in, d_out, act=TDA_ACT_NONE, dtype=TDA_BF16):
         super().__init__(d_in, d_out, act, dtype)
+
+
+class AttentionDesc(ctypes.Structure):
+    """tda_attention_desc."""
+    _fields_ = [("N", ctypes.c_int64), ("T", ctypes.c_int64), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("causal", ctypes.c_int32), ("n_buckets", ctypes.c_int32), ("max_distance", ctypes.c_int64)]
+
+    def __init__(self, N, T, heads, kv_heads, head_dim, dtype=TDA_BF16, scale=None, cap=0.0, causal=True, n_buckets=0,
+                 max_distance=0):
+        super().__init__(N, T, heads, kv_heads, head_dim, dtype, scale if scale is not None else max(head_dim, 1) ** -0.5, cap,
+                         int(causal), n_buckets, max_distance)
 
 
 class TensorRef(ctypes.Structure):
@@ -147,6 +162,16 @@ def load() -> ctypes.CDLL:
                                          SZ, P]),
             "tda_linear_backward": (I32, [ctypes.POINTER(LinearDesc), P, I64, P, I64, I64, P, I64, P, I64, P, I64, P,
                                           I64, P, I64, P, I32, F, P, SZ, P]),
+            "tda_attention_workspace_size": (I32, [I32, ctypes.POINTER(AttentionDesc), ctypes.POINTER(SZ)]),
+            "tda_position_buckets": (I32, [I32, I64, I32, P]),
+            "tda_attention_ranges": (I32, [I64, I64, P, P, I32, I64, P, P]),
+            "tda_attention_forward": (I32, [ctypes.POINTER(AttentionDesc), P, I64, P, I64, P, I64, P, P, P, P, P, I64, P, P,
+                                            SZ, P]),
+            "tda_attention_backward": (I32, [ctypes.POINTER(AttentionDesc), P, I64, P, I64, P, I64, P, P, P, P, P, I64, P, P,
+                                             I64, P, I64, P, I64, P, I64, P, I32, F, P, SZ, P]),
+            "tda_rmsnorm_forward": (I32, [I32, P, I64, P, I64, I64, I64, P, F, P, I64, P, I64, P, P]),
+            "tda_rmsnorm_workspace_size": (SZ, [I64, I64]),
+            "tda_rmsnorm_backward": (I32, [I32, P, I64, P, P, P, I64, P, I64, I64, I64, P, I64, P, I32, F, P, SZ, P]),
             "tda_embedding_forward": (I32, [I32, P, I64, I64, I64, I32, P, I64, F, P, I64, P]),
             "tda_embedding_workspace_size": (SZ, [I64, I64, I64]),
             "tda_embedding_backward": (I32, [I32, P, I64, I64, I64, I32, P, I64, F, I32, P, I64, F, P, SZ, P]),
@@ -409,6 +434,8 @@ def _train():
         addr = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
         mod.bind(_current_stream, LinearDesc, addr(lib.tda_linear_forward), addr(lib.tda_linear_backward),
                  addr(lib.tda_embedding_forward), addr(lib.tda_embedding_backward), addr(lib.tda_grad_clip))
+        mod.bind_block(AttentionDesc, addr(lib.tda_attention_ranges), addr(lib.tda_attention_forward),
+                       addr(lib.tda_attention_backward), addr(lib.tda_rmsnorm_forward), addr(lib.tda_rmsnorm_backward))
         _calls = mod
     return _calls
 
@@ -472,5 +499,61 @@ def tda_grad_clip_workspace_size(refs, n_tensors) -> int:
 
 def tda_grad_clip(refs, n_tensors, max_norm, norm, ws, ws_bytes, stream=None):
     st = (_calls or _train()).grad_clip(refs, n_tensors, max_norm, norm, ws, ws_bytes, stream)
+    if st:
+        _check(st)
+
+
+def tda_attention_workspace_size(op, L) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load().tda_attention_workspace_size(op, ctypes.byref(L), ctypes.byref(b)))
+    return int(b.value)
+
+
+def tda_position_buckets(n_buckets, max_distance, bidirectional, bucket):
+    """bucket: a contiguous int32 CPU tensor of 2 * max_distance + 1 values (or the address of such memory)."""
+    if not isinstance(bucket, int) and bucket is not None:
+        import torch
+        if bucket.dtype != torch.int32 or bucket.is_cuda or not bucket.is_contiguous() or bucket.numel() < 2 * max_distance + 1:
+            raise ValueError("tda_position_buckets: bucket is a contiguous int32 CPU tensor of 2 * max_distance + 1 values")
+    _check(load().tda_position_buckets(n_buckets, max_distance, int(bidirectional), _ptr(bucket)))
+
+
+def tda_attention_ranges(N, T, doc, prefix, causal, window, range, stream=None):
+    st = (_calls or _train()).attention_ranges(N, T, doc, prefix, causal, window, range, stream)
+    if st:
+        _check(st)
+
+
+def tda_attention_forward(L, Q, ld_q, K, ld_k, V, ld_v, range, bucket, table, slope, O, ld_o, lse=None, ws=None, ws_bytes=0,
+                          stream=None):
+    st = (_calls or _train()).attention_forward(L, Q, ld_q, K, ld_k, V, ld_v, range, bucket, table, slope, O, ld_o, lse, ws,
+                                               ws_bytes, stream)
+    if st:
+        _check(st)
+
+
+def tda_attention_backward(L, Q, ld_q, K, ld_k, V, ld_v, range, bucket, table, slope, O, ld_o, lse, dO, ld_do, dQ, ld_dq, dK,
+                           ld_dk, dV, ld_dv, dtable=None, grad_dtype=TDA_F32, beta=0.0, ws=None, ws_bytes=0, stream=None):
+    st = (_calls or _train()).attention_backward(L, Q, ld_q, K, ld_k, V, ld_v, range, bucket, table, slope, O, ld_o, lse, dO,
+                                                ld_do, dQ, ld_dq, dK, ld_dk, dV, ld_dv, dtable, grad_dtype, beta, ws, ws_bytes,
+                                                stream)
+    if st:
+        _check(st)
+
+
+def tda_rmsnorm_forward(dtype, x, ld_x, r, ld_r, M, d, w, eps, h, ld_h, y, ld_y, rstd=None, stream=None):
+    st = (_calls or _train()).rmsnorm_forward(dtype, x, ld_x, r, ld_r, M, d, w, eps, h, ld_h, y, ld_y, rstd, stream)
+    if st:
+        _check(st)
+
+
+def tda_rmsnorm_workspace_size(M, d) -> int:
+    return int(load().tda_rmsnorm_workspace_size(M, d))
+
+
+def tda_rmsnorm_backward(dtype, h, ld_h, rstd, w, dy, ld_dy, dres, ld_r, M, d, dx, ld_dx, dw=None, grad_dtype=TDA_F32, beta=0.0,
+                         ws=None, ws_bytes=0, stream=None):
+    st = (_calls or _train()).rmsnorm_backward(dtype, h, ld_h, rstd, w, dy, ld_dy, dres, ld_r, M, d, dx, ld_dx, dw, grad_dtype,
+                                              beta, ws, ws_bytes, stream)
     if st:
         _check(st)

@@ -2,6 +2,7 @@
 // (include/tda.h): host-side argument validation and kernel dispatch.
 #include <cmath>
 
+#include "attention.cuh"
 #include "linear.cuh"
 
 using namespace tda;
@@ -63,6 +64,65 @@ tda_status check_ws(const void* ws, size_t ws_bytes, size_t need, const char* wh
     if (need && (!ws || ws_bytes < need))
         return fail(TDA_ERR_WORKSPACE, "%s needs >= %zu bytes of ws, got %zu", who, need, ws ? ws_bytes : 0);
     if (need && !aligned_to(ws, 256)) return fail(TDA_ERR_INVALID_ARG, "ws must be 256-byte aligned");
+    return TDA_OK;
+}
+
+constexpr int kMaxHeadDim = 128;
+constexpr int64_t kMaxReach = 1 << 20, kMaxBuckets = 1024;
+
+tda_status check_attention(const tda_attention_desc* L, const char* who) {
+    if (!L) return fail(TDA_ERR_INVALID_ARG, "%s: attention descriptor is NULL", who);
+    if (L->N < 0 || L->T < 0 || L->N > kMaxCount || L->T > kMaxCount || L->heads < 1 || L->heads > 65535 || L->kv_heads < 1 ||
+        L->head_dim < 1)
+        return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes N=%lld T=%lld heads=%d kv_heads=%d head_dim=%d", who, (long long)L->N,
+                    (long long)L->T, L->heads, L->kv_heads, L->head_dim);
+    if (L->heads % L->kv_heads)
+        return fail(TDA_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, L->kv_heads, L->heads);
+    if (L->head_dim > kMaxHeadDim) return fail(TDA_ERR_UNSUPPORTED, "%s: head_dim %d > %d", who, L->head_dim, kMaxHeadDim);
+    // one CTA per 64 queries of a head
+    if (L->N * L->T > kMaxCount || L->N * ((L->T + 63) / 64) > kMaxCount / L->heads || L->N * L->T > (kMaxCount / L->heads) * 8)
+        return fail(TDA_ERR_INVALID_ARG, "%s: too many tokens or heads (N=%lld T=%lld heads=%d)", who, (long long)L->N,
+                    (long long)L->T, L->heads);
+    if (!float_type(L->dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
+    if (!(L->scale > 0) || !std::isfinite(L->scale)) return fail(TDA_ERR_INVALID_ARG, "%s: scale must be finite and > 0", who);
+    if (!(L->cap >= 0) || !std::isfinite(L->cap)) return fail(TDA_ERR_INVALID_ARG, "%s: cap must be finite and >= 0", who);
+    if (L->causal != 0 && L->causal != 1) return fail(TDA_ERR_INVALID_ARG, "%s: causal must be 0 or 1", who);
+    if (L->n_buckets < 0 || L->n_buckets > kMaxBuckets || L->max_distance < 0 || L->max_distance > kMaxReach)
+        return fail(TDA_ERR_INVALID_ARG, "%s: n_buckets=%d not in [0, %lld] or max_distance=%lld not in [0, %lld]", who, L->n_buckets,
+                    (long long)kMaxBuckets, (long long)L->max_distance, (long long)kMaxReach);
+    return TDA_OK;
+}
+
+// The arguments that both passes share; the tensors of a batch without tokens are not looked at.
+tda_status check_attention_inputs(const tda_attention_desc* L, const void* Q, int64_t ld_q, const void* K, int64_t ld_k,
+                                  const void* V, int64_t ld_v, const int32_t* range, const int32_t* bucket, const void* table,
+                                  const float* slope) {
+    const int64_t q = (int64_t)L->heads * L->head_dim, kv = (int64_t)L->kv_heads * L->head_dim;
+    tda_status st;
+    if ((st = check_rows(Q, ld_q, q, L->dtype, false, "Q")) || (st = check_rows(K, ld_k, kv, L->dtype, false, "K")) ||
+        (st = check_rows(V, ld_v, kv, L->dtype, false, "V")))
+        return st;
+    if (!aligned_to(range, 8)) return fail(TDA_ERR_INVALID_ARG, "range is misaligned");
+    if (L->n_buckets) {
+        if (!bucket || !aligned_to(bucket, 4)) return fail(TDA_ERR_INVALID_ARG, "bucket is NULL or misaligned");
+        if (!table || !aligned_to(table, el_size(L->dtype))) return fail(TDA_ERR_INVALID_ARG, "table is NULL or misaligned");
+    }
+    if (!aligned_to(slope, 4)) return fail(TDA_ERR_INVALID_ARG, "slope is misaligned");
+    return TDA_OK;
+}
+
+Attention attention_of(const tda_attention_desc* L) {
+    Attention a = {};
+    a.N = L->N, a.T = L->T, a.H = L->heads, a.KV = L->kv_heads, a.hd = L->head_dim, a.dt = (tda_dtype)L->dtype;
+    a.scale = L->scale, a.cap = L->cap, a.causal = L->causal, a.n_buckets = L->n_buckets, a.reach = L->max_distance;
+    return a;
+}
+
+tda_status check_norm(tda_dtype dtype, int64_t M, int64_t d, const char* who) {
+    if (!float_type(dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
+    if (M < 0 || M > kMaxCount || d < 1 || d > kMaxCount)
+        return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes M=%lld d=%lld", who, (long long)M, (long long)d);
+    if (d > kNormMaxRow) return fail(TDA_ERR_UNSUPPORTED, "%s: rows of %lld > %lld values", who, (long long)d, (long long)kNormMaxRow);
     return TDA_OK;
 }
 
@@ -238,6 +298,157 @@ tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float ma
     if (!aligned_to(ws, 16)) return fail(TDA_ERR_INVALID_ARG, "ws must be 16-byte aligned");
     return cuda_check(launch_grad_clip(list, n_tensors, max_norm, norm, (double*)ws, (cudaStream_t)stream),
                       "gradient clip");
+}
+
+tda_status tda_attention_workspace_size(int32_t op, const tda_attention_desc* L, size_t* bytes) {
+    clear_message();
+    if (!bytes) return fail(TDA_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = 0;
+    tda_status st = check_attention(L, "tda_attention_workspace_size");
+    if (st) return st;
+    if (op != TDA_ATTENTION_FORWARD && op != TDA_ATTENTION_BACKWARD) return fail(TDA_ERR_INVALID_ARG, "bad attention op %d", op);
+    if (L->N && L->T) *bytes = attention_ws_bytes(attention_of(L), op == TDA_ATTENTION_BACKWARD);
+    return TDA_OK;
+}
+
+tda_status tda_attention_ranges(int64_t N, int64_t T, const int32_t* doc, const int32_t* prefix, int32_t causal, int64_t window,
+                                int32_t* range, void* stream) {
+    clear_message();
+    if (N < 0 || T < 0 || N > kMaxCount || T > kMaxCount || (N && T > kMaxCount / N))
+        return fail(TDA_ERR_INVALID_ARG, "tda_attention_ranges: bad sizes N=%lld T=%lld", (long long)N, (long long)T);
+    if (causal != 0 && causal != 1) return fail(TDA_ERR_INVALID_ARG, "tda_attention_ranges: causal must be 0 or 1");
+    if (window < 0 || window > kMaxCount) return fail(TDA_ERR_INVALID_ARG, "tda_attention_ranges: bad window %lld", (long long)window);
+    if (N == 0 || T == 0) return TDA_OK;
+    if (!aligned_to(doc, 4) || !aligned_to(prefix, 4)) return fail(TDA_ERR_INVALID_ARG, "doc or prefix is misaligned");
+    if (!range || !aligned_to(range, 8)) return fail(TDA_ERR_INVALID_ARG, "range is NULL or misaligned");
+    return cuda_check(launch_attention_ranges(N, T, doc, prefix, causal, window, (int2*)range, (cudaStream_t)stream),
+                      "attention ranges");
+}
+
+tda_status tda_position_buckets(int32_t n_buckets, int64_t max_distance, int32_t bidirectional, int32_t* bucket) {
+    clear_message();
+    if (!bucket) return fail(TDA_ERR_INVALID_ARG, "bucket is NULL");
+    if (bidirectional != 0 && bidirectional != 1) return fail(TDA_ERR_INVALID_ARG, "bidirectional must be 0 or 1");
+    if (n_buckets < (bidirectional ? 4 : 2) || n_buckets > kMaxBuckets || (bidirectional && n_buckets % 2))
+        return fail(TDA_ERR_INVALID_ARG, "tda_position_buckets: bad n_buckets %d", n_buckets);
+    const int32_t side = bidirectional ? n_buckets / 2 : n_buckets, single = side / 2;
+    if (max_distance <= single || max_distance > kMaxReach)
+        return fail(TDA_ERR_INVALID_ARG, "tda_position_buckets: max_distance %lld not in (%d, %lld]", (long long)max_distance, single,
+                    (long long)kMaxReach);
+    const double per = (side - single) / std::log((double)max_distance / single);
+    for (int64_t d = -max_distance; d <= max_distance; ++d) {
+        const int64_t a = d < 0 ? (bidirectional ? -d : 0) : d;
+        // the margin keeps distances on a border, whose logarithms are exact in the reals, in the bucket they begin
+        const int64_t far = a < single ? a : single + (int64_t)std::floor(std::log((double)a / single) * per + 1e-9);
+        bucket[d + max_distance] = (int32_t)(far < side ? far : side - 1) + (bidirectional && d < 0 ? side : 0);
+    }
+    return TDA_OK;
+}
+
+tda_status tda_attention_forward(const tda_attention_desc* L, const void* Q, int64_t ld_q, const void* K, int64_t ld_k, const void* V,
+                                 int64_t ld_v, const int32_t* range, const int32_t* bucket, const void* table, const float* slope,
+                                 void* O, int64_t ld_o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    clear_message();
+    tda_status st = check_attention(L, "tda_attention_forward");
+    if (st) return st;
+    if (L->N == 0 || L->T == 0) return TDA_OK;
+    if ((st = check_attention_inputs(L, Q, ld_q, K, ld_k, V, ld_v, range, bucket, table, slope)) ||
+        (st = check_rows(O, ld_o, (int64_t)L->heads * L->head_dim, L->dtype, false, "O")))
+        return st;
+    if (!aligned_to(lse, 4)) return fail(TDA_ERR_INVALID_ARG, "lse is misaligned");
+    Attention a = attention_of(L);
+    a.Q = Q, a.K = K, a.V = V, a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v;
+    a.range = (const int2*)range, a.bucket = bucket, a.table = table, a.slope = slope, a.O = O, a.ld_o = ld_o, a.lse = lse;
+    if ((st = check_ws(ws, ws_bytes, attention_ws_bytes(a, false), "tda_attention_forward"))) return st;
+    unsigned int* err = device_error_word();
+    if (!err) return fail(TDA_ERR_CUDA, "cannot resolve the device error word");
+    return cuda_check(launch_attention_forward(a, ws, err, (cudaStream_t)stream), "attention forward");
+}
+
+tda_status tda_attention_backward(const tda_attention_desc* L, const void* Q, int64_t ld_q, const void* K, int64_t ld_k, const void* V,
+                                  int64_t ld_v, const int32_t* range, const int32_t* bucket, const void* table, const float* slope,
+                                  const void* O, int64_t ld_o, const float* lse, const void* dO, int64_t ld_do, void* dQ, int64_t ld_dq,
+                                  void* dK, int64_t ld_dk, void* dV, int64_t ld_dv, void* dtable, tda_dtype grad_dtype, float beta,
+                                  void* ws, size_t ws_bytes, void* stream) {
+    clear_message();
+    tda_status st = check_attention(L, "tda_attention_backward");
+    if (st) return st;
+    if (!float_type(grad_dtype)) return fail(TDA_ERR_INVALID_ARG, "tda_attention_backward: grad_dtype must be TDA_F32 or TDA_BF16");
+    if (!std::isfinite(beta)) return fail(TDA_ERR_INVALID_ARG, "tda_attention_backward: beta must be finite");
+    if (L->dtype == TDA_F32 && grad_dtype == TDA_BF16)
+        return fail(TDA_ERR_UNSUPPORTED, "tda_attention_backward: a bf16 dtable needs bf16 inputs");
+    if (dtable && !L->n_buckets) return fail(TDA_ERR_INVALID_ARG, "tda_attention_backward: dtable without n_buckets");
+    if (!aligned_to(dtable, el_size(grad_dtype))) return fail(TDA_ERR_INVALID_ARG, "dtable is misaligned");
+    if (L->N == 0 || L->T == 0) {
+        if (!dtable || beta == 1.f) return TDA_OK;
+        return cuda_check(launch_scale_matrix(grad_dtype, dtable, L->n_buckets, L->heads, L->heads, beta, (cudaStream_t)stream),
+                          "scale dtable");
+    }
+    const int64_t q = (int64_t)L->heads * L->head_dim, kv = (int64_t)L->kv_heads * L->head_dim;
+    if ((st = check_attention_inputs(L, Q, ld_q, K, ld_k, V, ld_v, range, bucket, table, slope)) ||
+        (st = check_rows(O, ld_o, q, L->dtype, false, "O")) || (st = check_rows(dO, ld_do, q, L->dtype, false, "dO")) ||
+        (st = check_rows(dQ, ld_dq, q, L->dtype, false, "dQ")) || (st = check_rows(dK, ld_dk, kv, L->dtype, false, "dK")) ||
+        (st = check_rows(dV, ld_dv, kv, L->dtype, false, "dV")))
+        return st;
+    if (!lse || !aligned_to(lse, 4)) return fail(TDA_ERR_INVALID_ARG, "lse is NULL or misaligned");
+    Attention a = attention_of(L);
+    a.Q = Q, a.K = K, a.V = V, a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v;
+    a.range = (const int2*)range, a.bucket = bucket, a.table = table, a.slope = slope;
+    a.O = const_cast<void*>(O), a.ld_o = ld_o, a.lse = const_cast<float*>(lse), a.dO = dO, a.ld_do = ld_do;
+    a.dQ = dQ, a.dK = dK, a.dV = dV, a.ld_dq = ld_dq, a.ld_dk = ld_dk, a.ld_dv = ld_dv;
+    a.dtable = dtable, a.gt = grad_dtype, a.beta = beta;
+    if ((st = check_ws(ws, ws_bytes, attention_ws_bytes(a, true), "tda_attention_backward"))) return st;
+    unsigned int* err = device_error_word();
+    if (!err) return fail(TDA_ERR_CUDA, "cannot resolve the device error word");
+    return cuda_check(launch_attention_backward(a, ws, err, (cudaStream_t)stream), "attention backward");
+}
+
+tda_status tda_rmsnorm_forward(tda_dtype dtype, const void* x, int64_t ld_x, const void* r, int64_t ld_r, int64_t M, int64_t d,
+                               const void* w, float eps, void* h, int64_t ld_h, void* y, int64_t ld_y, float* rstd, void* stream) {
+    clear_message();
+    tda_status st = check_norm(dtype, M, d, "tda_rmsnorm_forward");
+    if (st) return st;
+    if (!(eps > 0) || !std::isfinite(eps)) return fail(TDA_ERR_INVALID_ARG, "tda_rmsnorm_forward: eps must be finite and > 0");
+    if (M == 0) return TDA_OK;
+    if ((st = check_rows(x, ld_x, d, dtype, false, "x")) || (st = check_rows(r, ld_r, d, dtype, true, "r")) ||
+        (st = check_rows(w, d, d, dtype, false, "w")) || (st = check_rows(h, ld_h, d, dtype, true, "h")) ||
+        (st = check_rows(y, ld_y, d, dtype, false, "y")))
+        return st;
+    if (!aligned_to(rstd, 4)) return fail(TDA_ERR_INVALID_ARG, "rstd is misaligned");
+    return cuda_check(launch_norm_forward(dtype, x, ld_x, r, ld_r, M, d, w, eps, h, ld_h, y, ld_y, rstd, (cudaStream_t)stream),
+                      "norm forward");
+}
+
+size_t tda_rmsnorm_workspace_size(int64_t M, int64_t d) {
+    if (M < 0 || M > kMaxCount || d < 1 || d > kNormMaxRow) return 0;
+    return norm_ws_bytes(M, d);
+}
+
+tda_status tda_rmsnorm_backward(tda_dtype dtype, const void* h, int64_t ld_h, const float* rstd, const void* w, const void* dy,
+                                int64_t ld_dy, const void* dres, int64_t ld_r, int64_t M, int64_t d, void* dx, int64_t ld_dx,
+                                void* dw, tda_dtype grad_dtype, float beta, void* ws, size_t ws_bytes, void* stream) {
+    clear_message();
+    tda_status st = check_norm(dtype, M, d, "tda_rmsnorm_backward");
+    if (st) return st;
+    if (!float_type(grad_dtype)) return fail(TDA_ERR_INVALID_ARG, "tda_rmsnorm_backward: grad_dtype must be TDA_F32 or TDA_BF16");
+    if (!std::isfinite(beta)) return fail(TDA_ERR_INVALID_ARG, "tda_rmsnorm_backward: beta must be finite");
+    if (dtype == TDA_F32 && grad_dtype == TDA_BF16)
+        return fail(TDA_ERR_UNSUPPORTED, "tda_rmsnorm_backward: bf16 gradients of w need bf16 rows");
+    if ((st = check_rows(dw, d, d, grad_dtype, true, "dw"))) return st;
+    if (M == 0) {
+        if (!dw || beta == 1.f) return TDA_OK;
+        return cuda_check(launch_scale_matrix(grad_dtype, dw, 1, d, d, beta, (cudaStream_t)stream), "scale dw");
+    }
+    if ((st = check_rows(h, ld_h, d, dtype, false, "h")) || (st = check_rows(w, d, d, dtype, false, "w")) ||
+        (st = check_rows(dy, ld_dy, d, dtype, false, "dy")) || (st = check_rows(dres, ld_r, d, dtype, true, "dres")) ||
+        (st = check_rows(dx, ld_dx, d, dtype, true, "dx")))
+        return st;
+    if (!rstd || !aligned_to(rstd, 4)) return fail(TDA_ERR_INVALID_ARG, "rstd is NULL or misaligned");
+    if (!dx && !dw) return TDA_OK;
+    if (dw && (st = check_ws(ws, ws_bytes, norm_ws_bytes(M, d), "tda_rmsnorm_backward"))) return st;
+    return cuda_check(launch_norm_backward(dtype, h, ld_h, rstd, w, dy, ld_dy, dres, ld_r, M, d, dx, ld_dx, dw, grad_dtype, beta,
+                                           (float*)ws, (cudaStream_t)stream),
+                      "norm backward");
 }
 
 }  // extern "C"

@@ -1,0 +1,69 @@
+// attention.cuh -- what the translation units of the attention share: the arguments of a
+// pass, a row's visible keys, the scores' cap and biases. Internal.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "tda_internal.cuh"
+
+namespace tda {
+
+// One call. Row i of example n is token n T + i; head h's values start at column h hd of its row.
+struct Attention {
+    int64_t N, T;
+    int H, KV, hd;
+    tda_dtype dt;
+    float scale, cap;
+    int causal, n_buckets;
+    int64_t reach;          // distances are held within +-reach for the table
+    const void *Q, *K, *V;
+    int64_t ld_q, ld_k, ld_v;
+    const int2* range;      // [N][T] keys [lo, hi), or NULL
+    const int32_t* bucket;  // [2 reach + 1]
+    const void* table;      // [n_buckets][H]
+    const float* slope;     // [H] or NULL
+    void* O;
+    int64_t ld_o;
+    float* lse;             // [N][H][T]
+    // backward pass
+    const void* dO;
+    void *dQ, *dK, *dV, *dtable;
+    int64_t ld_do, ld_dq, ld_dk, ld_dv;
+    tda_dtype gt;
+    float beta;
+};
+
+// Keys [x, y) that row i of an example sees; rows past T see none.
+__device__ __forceinline__ int2 visible(const int2* range, int causal, int T, int64_t row0, int i) {
+    if (i >= T) return make_int2(0, 0);
+    if (range) {
+        const int2 r = range[row0 + i];
+        return make_int2(max(r.x, 0), min(r.y, T));
+    }
+    return make_int2(0, causal ? i + 1 : T);
+}
+
+// What distance d = i - j adds to a score of head h.
+template <typename T>
+__device__ __forceinline__ float distance_bias(const int32_t* bucket, const T* table, const float* slope, int n_buckets,
+                                               int64_t reach, int H, int h, int64_t d) {
+    float v = 0.f;
+    if (n_buckets) {
+        const int64_t c = d < -reach ? -reach : d > reach ? reach : d;
+        const int b = bucket[c + reach];
+        if (b >= 0 && b < n_buckets) v = (float)table[(int64_t)b * H + h];
+    }
+    if (slope) v -= slope[h] * (float)(d < 0 ? -d : d);
+    return v;
+}
+
+// Workspace of a call, and its launches. The CUDA-core kernels (k_attention.cu) take every shape; the tensor-core ones
+// (k_attention_tc.cu, k_attention_grad_tc.cu) bf16 with aligned rows.
+size_t attention_ws_bytes(const Attention& a, bool backward);
+bool attention_tc_supported(const Attention& a, bool backward);
+cudaError_t launch_attention_forward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
+cudaError_t launch_attention_backward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
+cudaError_t launch_attention_ranges(int64_t N, int64_t T, const int32_t* doc, const int32_t* prefix, int causal,
+                                    int64_t window, int2* range, cudaStream_t s);
+
+}  // namespace tda

@@ -241,6 +241,15 @@ cudaError_t launch_embedding_backward(tda_dtype dt, const void* dout, int64_t ld
 size_t clip_workspace_bytes(int64_t n_tensors);
 cudaError_t launch_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float max_norm, float* norm, double* part,
                              cudaStream_t s);
+// Root-mean-square norm with the residual's addition (k_norm.cu); rows of at most kNormMaxRow values.
+constexpr int64_t kNormMaxRow = 32768;
+size_t norm_ws_bytes(int64_t M, int64_t d);
+cudaError_t launch_norm_forward(tda_dtype dt, const void* x, int64_t ld_x, const void* r, int64_t ld_r, int64_t M, int64_t d,
+                                const void* w, float eps, void* h, int64_t ld_h, void* y, int64_t ld_y, float* rstd,
+                                cudaStream_t s);
+cudaError_t launch_norm_backward(tda_dtype dt, const void* h, int64_t ld_h, const float* rstd, const void* w, const void* dy,
+                                 int64_t ld_dy, const void* dres, int64_t ld_r, int64_t M, int64_t d, void* dx, int64_t ld_dx,
+                                 void* dw, tda_dtype gt, float beta, float* part, cudaStream_t s);
 
 // State header layout of the preconditioner (doubles).
 enum { kPcLambda = 0, kPcMeanEig = 1, kPcFailedPivot = 2, kPcNTotal = 3, kPcHeaderDoubles = 8 };

@@ -1,0 +1,351 @@
+"""Attention and its backward pass against the definition in 64 bits, at the lengths, masks, strides and values where
+they can go wrong. The bounds are attention_reference.Bounds'."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_38767_gb300 as tda
+from attention_reference import Bounds, attention, bias_of, by_bucket, gradients, seen_by
+from paper_2609_38767_gb300 import build as tbuild
+
+pytestmark = pytest.mark.gpu
+
+KIND = {torch.float32: tda.TDA_F32, torch.bfloat16: tda.TDA_BF16}
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def dev():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    tbuild.build()
+    tda.load()
+    return torch.device("cuda:0")
+
+
+def wide(rows, cols, gap, shift, dtype, dev, gen, fill=None, sigma=1.0):
+    """rows x cols in rows of cols + gap, the first value `shift` values into its buffer."""
+    buf = torch.empty(rows * (cols + gap) + shift + 16, dtype=torch.float32, device=dev)
+    buf = (buf.normal_(0, sigma, generator=gen) if fill is None else buf.fill_(fill)).to(dtype)
+    return buf, buf[shift:shift + rows * (cols + gap)].view(rows, cols + gap)[:, :cols]
+
+
+def ranges_for(kind, N, T, gen, dev):
+    """Ranges of a kind; None for the plain masks."""
+    if kind in ("causal", "full"):
+        return None
+    at = torch.arange(T).expand(N, T)
+    g = torch.Generator().manual_seed(T)
+    if kind == "causal_range":
+        return torch.stack([torch.zeros_like(at), at + 1], 2).int().to(dev)
+    if kind == "window":
+        return torch.stack([at - 70, at + 1], 2).int().to(dev)  # negative starts are clamped
+    if kind == "any":  # nothing, one key, everything, the far end, past the end
+        lo, n = torch.randint(-3, T, (N, T), generator=g), torch.randint(0, T + 5, (N, T), generator=g)
+        n[torch.rand((N, T), generator=g) < 0.2] = 0
+        n[torch.rand((N, T), generator=g) < 0.1] = 1
+        return torch.stack([lo, lo + n], 2).int().to(dev)
+    if kind == "docs":
+        doc = (torch.rand((N, T), generator=g) < 3.5 / max(T, 4)).long().cumsum(1)
+        doc[torch.rand((N, T), generator=g) < 0.03] = -1
+        doc[:, T - T // 7:] = -1
+        pre = (torch.rand((N, T), generator=g) < 0.9).int().to(dev)
+        out = torch.empty((N, T, 2), dtype=torch.int32, device=dev)
+        tda.tda_attention_ranges(N, T, doc.int().to(dev), pre, True, 0, out)
+        return out
+    if kind == "none":
+        return torch.zeros((N, T, 2), dtype=torch.int32, device=dev)
+    raise KeyError(kind)
+
+
+class Problem:
+    def __init__(self, dev, N, T, H, KV, hd, dtype, mask, cap=0.0, buckets=0, reach=0, slope=False, layout="packed", seed=0,
+                 sigma=1.0, garbage=True):
+        self.gen = gen = torch.Generator(device=dev).manual_seed(1000 * T + 10 * H + hd + seed)
+        self.N, self.T, self.H, self.KV, self.hd, self.dtype, self.dev = N, T, H, KV, hd, dtype, dev
+        self.scale, self.cap, self.reach, self.buckets = 1.0 / math.sqrt(hd), cap, reach, buckets
+        M, a, b = N * T, H * hd, KV * hd
+        if layout == "packed":
+            self.buf, x = wide(M, a + 2 * b, 0, 0, dtype, dev, gen, sigma=sigma)
+            self.Q, self.K, self.V = x[:, :a], x[:, a:a + b], x[:, a + b:]
+        else:
+            gap, shift = layout
+            self.Q, self.K, self.V = (wide(M, c, gap, shift, dtype, dev, gen, sigma=sigma)[1] for c in (a, b, b))
+        self.range = ranges_for(mask, N, T, gen, dev)
+        self.seen = seen_by(self.range, T, N, mask == "causal", dev)
+        gap, shift = (0, 0) if layout == "packed" else layout
+        self.dO = wide(M, a, gap, shift, dtype, dev, gen)[1]
+        if garbage and self.range is not None:
+            dead = ~self.seen.any(1).reshape(-1)
+            idle = ~self.seen.any(2).reshape(-1)
+            self.K[dead], self.V[dead], self.Q[idle], self.dO[idle] = math.nan, math.inf, math.nan, math.nan
+        self.bucket = self.table = self.slope = None
+        if buckets:
+            self.bucket = torch.randint(-1, buckets, (2 * reach + 1,), generator=gen, device=dev).int()
+            self.table = torch.randn((buckets, H), generator=gen, device=dev).to(dtype)
+        if slope:
+            self.slope = torch.rand(H, generator=gen, device=dev) * 0.1
+        self.bias = bias_of(T, H, self.bucket, reach, self.table, self.slope, dev) if buckets or slope else None
+        self.L = tda.AttentionDesc(N, T, H, KV, hd, KIND[dtype], self.scale, cap, mask == "causal", buckets, reach)
+        self.gap, self.shift = gap, shift
+
+    def heads(self, x, n):
+        return x.reshape(self.N, self.T, n, self.hd).transpose(1, 2)
+
+    def exact(self):
+        return attention(self.heads(self.Q, self.H), self.heads(self.K, self.KV), self.heads(self.V, self.KV), self.seen, self.scale,
+                         self.cap, self.bias)
+
+    def forward(self, stream=None):
+        M, a = self.N * self.T, self.H * self.hd
+        obuf, self.O = wide(M, a, self.gap, self.shift, self.dtype, self.dev, self.gen, fill=7.0)
+        self.lse = torch.full((self.N, self.H, self.T), 7.0, device=self.dev)
+        wsb = tda.tda_attention_workspace_size(tda.TDA_ATTENTION_FORWARD, self.L)
+        ws = torch.full((max(wsb, 1),), 255, dtype=torch.uint8, device=self.dev)
+        tda.tda_attention_forward(self.L, self.Q, self.Q.stride(0), self.K, self.K.stride(0), self.V, self.V.stride(0), self.range,
+                                  self.bucket, self.table, self.slope, self.O, self.O.stride(0), self.lse, ws, wsb, stream)
+        return obuf
+
+    def backward(self, beta=0.0, grad=None, stream=None):
+        M, a, b = self.N * self.T, self.H * self.hd, self.KV * self.hd
+        made = [wide(M, c, self.gap, self.shift, self.dtype, self.dev, self.gen, fill=7.0) for c in (a, b, b)]
+        self.dQ, self.dK, self.dV = (x for _, x in made)
+        grad = grad or self.dtype
+        self.dtable = torch.full((self.buckets, self.H), 0.5, dtype=grad, device=self.dev) if self.buckets else None
+        wsb = tda.tda_attention_workspace_size(tda.TDA_ATTENTION_BACKWARD, self.L)
+        ws = torch.full((max(wsb, 1),), 255, dtype=torch.uint8, device=self.dev)
+        tda.tda_attention_backward(self.L, self.Q, self.Q.stride(0), self.K, self.K.stride(0), self.V, self.V.stride(0), self.range,
+                                   self.bucket, self.table, self.slope, self.O, self.O.stride(0), self.lse, self.dO,
+                                   self.dO.stride(0), self.dQ, self.dQ.stride(0), self.dK, self.dK.stride(0), self.dV,
+                                   self.dV.stride(0), self.dtable, KIND[grad], beta, ws, wsb, stream)
+        return [x for x, _ in made]
+
+
+def near(got, want, tol, what):
+    got = got.double()
+    fine = torch.isfinite(want)
+    bad = int((~torch.isfinite(got[fine])).sum())
+    assert not bad, f"{what}: {bad} of {want.numel()} values not finite"
+    same = torch.equal(got[~fine], want[~fine])
+    assert same, f"{what}: infinities"
+    off = (got - want)[fine].abs() / tol.expand_as(want)[fine]
+    most = float(off.max()) if off.numel() else 0.0
+    assert most <= 1.0, f"{what}: {most:.3g} of the bound, {int((off > 1).sum())} of {off.numel()} values"
+
+
+def untouched(buf, p, cols):
+    """What lies outside the rows of a wide() tensor still holds its filling."""
+    rows = p.N * p.T
+    assert (buf[:p.shift] == 7).all() and (buf[p.shift + rows * (cols + p.gap):] == 7).all()
+    assert (buf[p.shift:p.shift + rows * (cols + p.gap)].view(rows, cols + p.gap)[:, cols:] == 7).all()
+
+
+def check_forward(p):
+    buf = p.forward()
+    tda.tda_device_status()
+    f = p.exact()
+    b = Bounds(f, p.dtype, p.T, p.hd, p.cap, p.bias)
+    near(p.heads(p.O, p.H), f["o"], b.o(), "O")
+    near(p.lse, f["lse"], b.lse(), "lse")
+    untouched(buf, p, p.H * p.hd)
+    return f, b
+
+
+def check_backward(p, f, b, beta=0.0, grad=None):
+    bufs = p.backward(beta, grad)
+    tda.tda_device_status()
+    r = gradients(f, p.heads(p.dO, p.H), p.scale, p.KV, p.bucket, p.reach, p.buckets)
+    if p.buckets:
+        r["dtable"] = r["dtable"] + beta * 0.5
+    tol = b.grads(r, p.scale, p.KV, p.bucket, p.reach, p.buckets, {BF: 2.0 ** -8, F32: 2.0 ** -24}[grad or p.dtype])
+    near(p.heads(p.dQ, p.H), r["dQ"], tol["dQ"], "dQ")
+    near(p.heads(p.dK, p.KV), r["dK"], tol["dK"], "dK")
+    near(p.heads(p.dV, p.KV), r["dV"], tol["dV"], "dV")
+    if p.buckets:
+        near(p.dtable, r["dtable"], tol["dtable"], "dtable")
+    for x, c in zip(bufs, (p.H, p.KV, p.KV)):
+        untouched(x, p, c * p.hd)
+
+
+MASKS = ["causal", "full", "window", "any", "docs", "none"]
+SHAPES = [
+    # (N, T, H, KV, hd)
+    (1, 1, 1, 1, 64), (2, 2, 2, 1, 128), (1, 37, 4, 2, 64), (2, 64, 2, 2, 128), (1, 127, 3, 1, 96), (3, 128, 2, 1, 64),
+    (1, 129, 2, 2, 128), (1, 255, 4, 1, 80), (2, 257, 2, 2, 128), (1, 300, 2, 1, 8), (1, 513, 2, 1, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_attention(dev, shape, mask, dtype):
+    p = Problem(dev, *shape, dtype, mask)
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+
+
+RICH = [
+    # (shape, mask, cap, buckets, reach, slope)
+    ((1, 1, 1, 1, 64), "causal", 5.0, 4, 0, True), ((2, 67, 4, 2, 64), "docs", 3.0, 8, 20, False),
+    ((1, 200, 2, 1, 128), "causal", 0.0, 32, 128, False), ((2, 200, 2, 2, 64), "full", 0.0, 0, 0, True),
+    ((1, 385, 4, 2, 128), "any", 30.0, 40, 300, True), ((1, 640, 2, 1, 64), "causal", 50.0, 32, 128, False),
+    ((1, 640, 2, 2, 72), "docs", 0.0, 16, 1000, False), ((3, 130, 2, 1, 128), "full", 20.0, 3, 5, False),
+    ((1, 333, 1, 1, 64), "window", 0.0, 300, 150, True),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("shape,mask,cap,buckets,reach,slope", RICH)
+def test_caps_and_biases(dev, shape, mask, cap, buckets, reach, slope, dtype):
+    p = Problem(dev, *shape, dtype, mask, cap, buckets, reach, slope, sigma=2.0)
+    f, b = check_forward(p)
+    check_backward(p, f, b, beta=1.0 if buckets else 0.0)
+    if buckets and dtype == BF:
+        check_backward(p, f, b, beta=-0.5, grad=F32)
+
+
+@pytest.mark.parametrize("layout", [(8, 8), (3, 1), (0, 2), (24, 0)])
+@pytest.mark.parametrize("dtype,hd", [(BF, 64), (BF, 36), (BF, 33), (F32, 33), (F32, 128)])
+def test_strides_and_widths(dev, layout, dtype, hd):
+    p = Problem(dev, 2, 150, 4, 2, hd, dtype, "docs", layout=layout)
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_hidden_by_bias(dev, dtype):
+    """Biases of -inf hide pairs, rows of them see nothing; the type's lowest value does not."""
+    p = Problem(dev, 1, 140, 2, 1, 64, dtype, "causal", 0.0, 3, 139)
+    at = torch.arange(-139, 140, device=dev)
+    p.bucket = torch.where(at % 3 == 0, 0, torch.where(at % 3 == 1, 1, 2)).int()
+    p.table = torch.tensor([[-math.inf, torch.finfo(dtype).min], [0.5, 0.0], [-math.inf, torch.finfo(dtype).min]], device=dev).to(dtype)
+    p.bias = bias_of(140, 2, p.bucket, 139, p.table, None, dev)
+    p.forward()
+    tda.tda_device_status()
+    f = p.exact()
+    assert p.lse[0, 0, 0] == -math.inf and (p.O[0, :64] == 0).all()  # the first token's only key is hidden
+    b = Bounds(f, dtype, 140, 64, 0.0, torch.zeros((), dtype=torch.float64, device=dev))
+    near(p.heads(p.O, 2), f["o"], b.o(), "O")
+    p.backward()
+    tda.tda_device_status()
+    r = gradients(f, p.heads(p.dO, 2), p.scale, 1)
+    tol = b.grads(r, p.scale, 1)
+    for name in ("dQ", "dK", "dV"):
+        near(p.heads(getattr(p, name), 2 if name == "dQ" else 1), r[name], tol[name], name)
+
+
+def test_equal_calls_give_equal_bits(dev):
+    for dtype in (BF, F32):
+        p = Problem(dev, 2, 700, 8, 2, 64, dtype, "docs", 30.0, 32, 128)
+        got = []
+        for _ in range(3):
+            p.forward()
+            p.backward()
+            got.append([x.clone() for x in (p.O, p.lse, p.dQ, p.dK, p.dV, p.dtable)])
+        tda.tda_device_status()
+        for other in got[1:]:
+            assert all(torch.equal(x, y) for x, y in zip(got[0], other))
+
+
+def test_no_lse_and_empty_batches(dev):
+    p = Problem(dev, 1, 90, 2, 1, 64, BF, "causal")
+    p.forward()
+    with_lse = p.O.clone()
+    wsb = tda.tda_attention_workspace_size(tda.TDA_ATTENTION_FORWARD, p.L)
+    ws = torch.empty(max(wsb, 1), dtype=torch.uint8, device=dev)
+    tda.tda_attention_forward(p.L, p.Q, p.Q.stride(0), p.K, p.K.stride(0), p.V, p.V.stride(0), None, None, None, None, p.O,
+                              p.O.stride(0), None, ws, wsb)
+    assert torch.equal(p.O, with_lse)
+    for N, T in ((0, 5), (3, 0)):
+        L = tda.AttentionDesc(N, T, 2, 1, 64, n_buckets=4, max_distance=8)
+        table = torch.full((4, 2), 3.0, device=dev)
+        tda.tda_attention_forward(L, None, 128, None, 64, None, 64, None, None, None, None, None, 128)
+        tda.tda_attention_backward(L, None, 128, None, 64, None, 64, None, None, None, None, None, 128, None, None, 128, None, 128,
+                                   None, 64, None, 64, table, tda.TDA_F32, 0.5)
+        assert (table == 1.5).all()
+
+
+def test_streams_and_graphs(dev):
+    """On another stream than the current one, and captured with the backward pass and replayed on new inputs."""
+    p = Problem(dev, 2, 300, 4, 2, 64, BF, "docs", 20.0, 16, 64)
+    p.forward()
+    p.backward()
+    want = [x.clone() for x in (p.O, p.lse, p.dQ, p.dK, p.dV, p.dtable)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    p.forward(s)
+    p.backward(stream=s)
+    s.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(want, (p.O, p.lse, p.dQ, p.dK, p.dV, p.dtable)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.forward()
+        p.backward()
+    kept = (p.O, p.lse, p.dQ, p.dK, p.dV, p.dtable)
+    p.buf.copy_(torch.where(torch.isfinite(p.buf.float()), -p.buf, p.buf))  # other queries, keys, values
+    graph.replay()
+    tda.tda_device_status()
+    got = [x.clone() for x in kept]
+    p.forward()
+    p.backward()
+    assert all(torch.equal(x, y) for x, y in zip(got, (p.O, p.lse, p.dQ, p.dK, p.dV, p.dtable)))
+    assert not torch.equal(got[0], want[0])
+
+
+# ------------------------------------------------------------------ ranges
+def by_hand(doc, pre, causal, window):
+    N, T = doc.shape
+    out = torch.zeros((N, T, 2), dtype=torch.int32)
+    for n in range(N):
+        d, f = doc[n].tolist(), pre[n].tolist()
+        s = 0
+        while s < T:
+            e = s
+            while e < T and d[e] == d[s]:
+                e += 1
+            p = s
+            while p < e and f[p]:
+                p += 1
+            for i in range(s, e):
+                lo, hi = s, max(i + 1, p) if causal else e
+                if window:
+                    lo, hi = max(lo, i - window + 1), min(hi, i + window)
+                out[n, i] = torch.tensor([lo, hi]) if d[s] >= 0 else 0
+            s = e
+    return out
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("N,T,docs,window", [(1, 1, 1, 0), (3, 7, 2, 0), (2, 33, 5, 4), (1, 1000, 9, 0), (2, 8192, 30, 511),
+                                             (1, 8193, 3, 0), (2, 20001, 400, 0), (1, 30000, 2, 9000)])
+def test_ranges(dev, N, T, docs, window, causal):
+    gen = torch.Generator().manual_seed(T + docs)
+    doc = (torch.rand((N, T), generator=gen) < docs / T).int().cumsum(1).int()
+    doc[torch.rand((N, T), generator=gen) < 0.01] = -1
+    doc[:, T - T // 9:] = -5
+    pre = (torch.rand((N, T), generator=gen) < 0.97).int() * 3
+    out = torch.full((N * T + 1, 2), 7, dtype=torch.int32, device=dev)
+    none = torch.zeros_like(pre)
+    for d, p in ((doc, pre), (doc, None), (None, pre), (None, None)):
+        tda.tda_attention_ranges(N, T, None if d is None else d.to(dev), None if p is None else p.to(dev), causal, window, out)
+        want = by_hand(none if d is None else d, none if p is None else p, causal, window)
+        assert torch.equal(out[:N * T].cpu(), want.view(N * T, 2)) and (out[N * T] == 7).all()
+
+
+def test_bucket_gradient_is_a_difference(dev):
+    """dtable against central differences of the fp32 forward pass along a direction of the table."""
+    p = Problem(dev, 1, 96, 2, 1, 32, F32, "causal", 4.0, 6, 40)
+    p.forward()
+    p.backward()
+    got = p.dtable.double()
+    step = torch.randn(6, 2, device=dev, dtype=torch.float64)
+    table, h = p.table.double(), 1e-5
+    out = []
+    for sign in (1, -1):
+        b = bias_of(96, 2, p.bucket, 40, table + sign * h * step, None, dev)
+        out.append((attention(p.heads(p.Q, 2), p.heads(p.K, 1), p.heads(p.V, 1), p.seen, p.scale, 4.0, b)["o"]
+                    * p.heads(p.dO, 2).double()).sum())
+    want = (out[0] - out[1]) / (2 * h)
+    # third order of the difference h^2, 64-bit rounding 1e-16 / h; the kernel's fp32 sums 2^-24 (96 + 32) per term
+    size = by_bucket(gradients(p.exact(), p.heads(p.dO, 2), p.scale, 1)["ds"].abs(), p.bucket, 40, 6)
+    assert ((got * step).sum() - want).abs() <= 2.0 ** -15 * (size * step.abs()).sum() + 1e-6
