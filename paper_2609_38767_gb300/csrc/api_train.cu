@@ -80,7 +80,7 @@ tda_status check_attention(const tda_attention_desc* L, const char* who) {
         return fail(TDA_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, L->kv_heads, L->heads);
     if (L->head_dim > kMaxHeadDim) return fail(TDA_ERR_UNSUPPORTED, "%s: head_dim %d > %d", who, L->head_dim, kMaxHeadDim);
     // one CTA per 64 queries of a head
-    if (L->N * L->T > kMaxCount || L->N * ((L->T + 63) / 64) > kMaxCount / L->heads || L->N * L->T > (kMaxCount / L->heads) * 8)
+    if (L->N * L->T > kMaxCount || L->N * ((L->T + 63) / 64) > (kMaxCount - 65536) / L->heads || L->N * L->T > (kMaxCount / L->heads) * 8)
         return fail(TDA_ERR_INVALID_ARG, "%s: too many tokens or heads (N=%lld T=%lld heads=%d)", who, (long long)L->N,
                     (long long)L->T, L->heads);
     if (!float_type(L->dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);
@@ -307,7 +307,7 @@ tda_status tda_attention_workspace_size(int32_t op, const tda_attention_desc* L,
     tda_status st = check_attention(L, "tda_attention_workspace_size");
     if (st) return st;
     if (op != TDA_ATTENTION_FORWARD && op != TDA_ATTENTION_BACKWARD) return fail(TDA_ERR_INVALID_ARG, "bad attention op %d", op);
-    if (L->N && L->T) *bytes = attention_ws_bytes(attention_of(L), op == TDA_ATTENTION_BACKWARD);
+    if (L->N && L->T) *bytes = attention_ws_bytes(attention_of(L), op == TDA_ATTENTION_BACKWARD, true);
     return TDA_OK;
 }
 
@@ -359,7 +359,7 @@ tda_status tda_attention_forward(const tda_attention_desc* L, const void* Q, int
     Attention a = attention_of(L);
     a.Q = Q, a.K = K, a.V = V, a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v;
     a.range = (const int2*)range, a.bucket = bucket, a.table = table, a.slope = slope, a.O = O, a.ld_o = ld_o, a.lse = lse;
-    if ((st = check_ws(ws, ws_bytes, attention_ws_bytes(a, false), "tda_attention_forward"))) return st;
+    if ((st = check_ws(ws, ws_bytes, attention_ws_bytes(a, false, false), "tda_attention_forward"))) return st;
     unsigned int* err = device_error_word();
     if (!err) return fail(TDA_ERR_CUDA, "cannot resolve the device error word");
     return cuda_check(launch_attention_forward(a, ws, err, (cudaStream_t)stream), "attention forward");
@@ -397,7 +397,7 @@ tda_status tda_attention_backward(const tda_attention_desc* L, const void* Q, in
     a.O = const_cast<void*>(O), a.ld_o = ld_o, a.lse = const_cast<float*>(lse), a.dO = dO, a.ld_do = ld_do;
     a.dQ = dQ, a.dK = dK, a.dV = dV, a.ld_dq = ld_dq, a.ld_dk = ld_dk, a.ld_dv = ld_dv;
     a.dtable = dtable, a.gt = grad_dtype, a.beta = beta;
-    if ((st = check_ws(ws, ws_bytes, attention_ws_bytes(a, true), "tda_attention_backward"))) return st;
+    if ((st = check_ws(ws, ws_bytes, attention_ws_bytes(a, true, false), "tda_attention_backward"))) return st;
     unsigned int* err = device_error_word();
     if (!err) return fail(TDA_ERR_CUDA, "cannot resolve the device error word");
     return cuda_check(launch_attention_backward(a, ws, err, (cudaStream_t)stream), "attention backward");

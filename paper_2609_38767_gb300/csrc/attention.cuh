@@ -57,13 +57,33 @@ __device__ __forceinline__ float distance_bias(const int32_t* bucket, const T* t
     return v;
 }
 
-// Workspace of a call, and its launches. The CUDA-core kernels (k_attention.cu) take every shape; the tensor-core ones
-// (k_attention_tc.cu, k_attention_grad_tc.cu) bf16 with aligned rows.
-size_t attention_ws_bytes(const Attention& a, bool backward);
-bool attention_tc_supported(const Attention& a, bool backward);
+// What a call's first kernel finds for the tensor-core kernels, in the workspace.
+struct AttentionTile {  // of 128 tokens
+    int lo, hi;         // keys that its queries see: all within [lo, hi)
+    int most, least;    // largest start and smallest end of a query's keys: what lies between is seen by all
+    uint32_t unseen[4]; // keys of this tile that no query of the example sees
+    uint32_t idle[4];   // queries that see nothing
+};
+struct AttentionPlan {
+    AttentionTile* tiles;  // [N][tiles], where a range is given
+    float* lut;            // [H][lut_len] bias of a distance, where there is any; distance 0 at lut_mid
+    int lut_len, lut_mid;
+    int reach;             // distances beyond it have the bias of +-reach
+};
+
+// Workspace of a call, and its launches; bound: enough for any range, slope and alignment. The CUDA-core kernels
+// (k_attention.cu) take every shape; the tensor-core ones (k_attention_tc.cu, k_attention_grad_tc.cu) bf16 with aligned rows.
+size_t attention_ws_bytes(const Attention& a, bool backward, bool bound);
 cudaError_t launch_attention_forward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
 cudaError_t launch_attention_backward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
 cudaError_t launch_attention_ranges(int64_t N, int64_t T, const int32_t* doc, const int32_t* prefix, int causal,
                                     int64_t window, int2* range, cudaStream_t s);
+
+bool attention_tc_supported(const Attention& a, bool backward);
+size_t attention_plan_bytes(const Attention& a, bool bound);
+// Fills the plan; *chained: a kernel was launched, the next may be chained to it.
+cudaError_t launch_attention_plan(const Attention& a, void* ws, AttentionPlan* plan, bool* chained, cudaStream_t s);
+bool attention_head_map(void* map, const void* p, int64_t ld, int heads, int hd, int64_t T, int64_t N, int rows);
+cudaError_t launch_attention_forward_tc(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
 
 }  // namespace tda

@@ -1,0 +1,161 @@
+// attention_tc.cuh -- what the tensor-core kernels of the attention share: MMAs with an operand in TMEM, wide TMEM
+// loads and stores, exponentials, pairs of fp32, tensor maps of heads. Included inside namespace tda::{anonymous},
+// after tc_ptx.cuh.
+#pragma once
+
+constexpr int kTileT = 128;                      // tokens of a tile
+constexpr uint32_t kPanel = kTileT * 128;        // 128 tokens x 64 values: 16 KiB
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Shared-memory descriptors, 128-byte swizzle, of `panel` bytes per 64 values of a head. K-major: 8-row groups 1 KiB apart;
+// MN-major: the panels are the 64-value atoms (LBO), 8-row groups of k 1 KiB apart (SBO).
+__device__ __forceinline__ uint64_t k_major(uint32_t saddr) { return sw128_desc(saddr); }
+__device__ __forceinline__ uint64_t mn_major(uint32_t saddr, uint32_t panel) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(panel >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+constexpr uint32_t kBMn = 1u << 16;  // instruction descriptor: B is MN-major
+
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(r));
+    return r;
+}
+// Issued by the elected lane of a converged warp. A and B in shared memory, or A in TMEM (a row per lane, two bf16 a column).
+__device__ __forceinline__ void mma_ss(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t lead, uint32_t bar) {
+    asm volatile(
+        "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+        " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar),
+        "r"(lead)
+        : "memory");
+}
+// D = A B^T over `steps` steps of 16 values of a head: A and B tiles of panels (a_panel, b_panel bytes), K-major.
+__device__ __forceinline__ void mma_heads(uint32_t lead, uint32_t d, uint32_t a, uint32_t a_panel, uint32_t b, uint32_t b_panel,
+                                          uint32_t idesc, int steps) {
+    for (int k = 0; k < steps; ++k)
+        mma_ss(lead, d, k_major(a + (k >> 2) * a_panel + (k & 3) * 32), k_major(b + (k >> 2) * b_panel + (k & 3) * 32), idesc, k > 0);
+}
+// D (+)= A B over K tokens: A in TMEM, B [tokens][head] MN-major in panels.
+template <int K>
+__device__ __forceinline__ void mma_tokens(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t panel, uint32_t idesc, bool first) {
+#pragma unroll
+    for (int k = 0; k < K / 16; ++k) mma_ts(lead, d, a + 8 * k, mn_major(b + k * 2048, panel), idesc, !first || k > 0);
+}
+
+#define TMEM_R32(r)                                                                                                              \
+    (r)[0], (r)[1], (r)[2], (r)[3], (r)[4], (r)[5], (r)[6], (r)[7], (r)[8], (r)[9], (r)[10], (r)[11], (r)[12], (r)[13], (r)[14], \
+        (r)[15], (r)[16], (r)[17], (r)[18], (r)[19], (r)[20], (r)[21], (r)[22], (r)[23], (r)[24], (r)[25], (r)[26], (r)[27],     \
+        (r)[28], (r)[29], (r)[30], (r)[31]
+// 32 lanes x 32 columns into registers; nothing may use them before tmem_wait_ld and tmem_use.
+__device__ __forceinline__ void tmem_ld32(uint32_t t, float* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+          "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]),
+          "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]),
+          "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+        : "r"(t)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Ties 32 loaded registers to what precedes: no use of them moves before it.
+__device__ __forceinline__ void tmem_use(float* r) {
+    asm volatile(""
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]), "+f"(r[8]),
+                   "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]), "+f"(r[16]),
+                   "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]),
+                   "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])::"memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t t, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+        "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(t),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t t, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(t),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 2^x to 2^-22 of its value, 1 / x to 2^-23.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// tanh by 1 - 2 / (1 + e^2x): right at both infinities, its error about 2^-22 absolute.
+__device__ __forceinline__ float tanh_fast(float x) { return fmaf(-2.f, rcp_fast(1.f + exp2_fast(2.f * kLog2e * x)), 1.f); }
+// Two bf16 of a column of TMEM, the first in the low half.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// a b + c of two fp32 pairs in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*(uint64_t*)&d)
+        : "l"(*(uint64_t*)&a), "l"(*(uint64_t*)&b), "l"(*(uint64_t*)&c));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*(uint64_t*)&d) : "l"(*(uint64_t*)&a), "l"(*(uint64_t*)&b));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*(uint64_t*)&d) : "l"(*(uint64_t*)&a), "l"(*(uint64_t*)&b));
+    return d;
+}
+
+// rows of 64 values of one head: {64, 1, rows, 1} boxes of {head_dim, heads, T, N}; values past head_dim and tokens past T
+// arrive as zeros.
+__device__ __forceinline__ void tma_load_head(uint32_t dst, const CUtensorMap* tm, int col, int head, int row, int n, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"((uint64_t)tm), "r"(col), "r"(head), "r"(row), "r"(n), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void chain_prefetch(const CUtensorMap* tm) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)tm) : "memory");
+}
+
+// Waits, up to the time limit, for what is in flight before a CTA may leave.
+__device__ __forceinline__ void wait_settled(uint32_t bar, uint32_t parity, unsigned int* err) {
+    const uint64_t since = global_ns();
+    while (!mbar_try_wait(bar, parity))
+        if (global_ns() - since > kTimeoutNs) {
+            atomicOr(err, kErrTimeout);
+            return;
+        }
+}

@@ -585,14 +585,16 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t attention_ws_bytes(const Attention& a, bool backward) {
-    if (!backward) return 0;
+size_t attention_ws_bytes(const Attention& a, bool backward, bool bound) {
     const size_t tiles = (size_t)((a.T + kTile - 1) / kTile);
-    return up((size_t)a.N * a.T * a.H * 4) + up((size_t)a.N * a.H * tiles * a.n_buckets * 4);
+    size_t n = 0;
+    if (bound ? a.dt == TDA_BF16 && a.hd % 8 == 0 : !backward && attention_tc_supported(a, backward)) n += attention_plan_bytes(a, bound);
+    if (backward) n += up((size_t)a.N * a.T * a.H * 4) + up((size_t)a.N * a.H * tiles * a.n_buckets * 4);
+    return n;
 }
 
 cudaError_t launch_attention_forward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s) {
-    (void)ws, (void)err;
+    if (attention_tc_supported(a, false)) return launch_attention_forward_tc(a, ws, err, s);
     if (a.dt == TDA_BF16) return a.hd <= 64 ? forward_simt<__nv_bfloat16, 64>(a, s) : forward_simt<__nv_bfloat16, 128>(a, s);
     return a.hd <= 64 ? forward_simt<float, 64>(a, s) : forward_simt<float, 128>(a, s);
 }
