@@ -31,7 +31,7 @@ LIBS = {
                   "k_precond.cu", "k_score.cu", "stream_host.cu", "noalloc.cu", "selftest.cu", "k_gemm_tc.cu", "k_gram_tc.cu", "k_kfac.cu", "k_tokens.cu", "k_tokens_tc.cu", "k_materialize_tc.cu",
                   "api_train.cu", "k_embedding.cu", "k_clip.cu", "k_linear.cu", "k_linear_tc.cu",
                   "k_linear_rows.cu", "k_attention.cu", "k_attention_tc.cu",
-                  "k_norm.cu"],
+                  "k_attention_grad_tc.cu", "k_norm.cu"],
     "libtda_synth.so": ["synth.cu"],
 }
 

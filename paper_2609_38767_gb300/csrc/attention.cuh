@@ -85,5 +85,8 @@ size_t attention_plan_bytes(const Attention& a, bool bound);
 cudaError_t launch_attention_plan(const Attention& a, void* ws, AttentionPlan* plan, bool* chained, cudaStream_t s);
 bool attention_head_map(void* map, const void* p, int64_t ld, int heads, int hd, int64_t T, int64_t N, int rows);
 cudaError_t launch_attention_forward_tc(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
+// *part: [H][N * tiles][n_buckets] sums of dS, where a.dtable is wanted.
+size_t attention_grad_tc_bytes(const Attention& a, bool bound);
+cudaError_t launch_attention_backward_tc(const Attention& a, void* ws, unsigned int* err, float** part, cudaStream_t s);
 
 }  // namespace tda

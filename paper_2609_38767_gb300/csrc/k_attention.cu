@@ -560,6 +560,17 @@ cudaError_t forward_simt(const Attention& a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
+cudaError_t join_table(const Attention& a, const float* part, int64_t rows, cudaStream_t s) {
+    if (!a.dtable) return cudaSuccess;
+    note_launches(1);
+    const unsigned grid = (unsigned)((a.n_buckets * a.H + 7) / 8);
+    if (a.gt == TDA_BF16)
+        attention_dtable_kernel<<<grid, 256, 0, s>>>(part, rows, a.n_buckets, a.H, a.beta, (__nv_bfloat16*)a.dtable);
+    else
+        attention_dtable_kernel<<<grid, 256, 0, s>>>(part, rows, a.n_buckets, a.H, a.beta, (float*)a.dtable);
+    return cudaGetLastError();
+}
+
 template <typename T, int HD>
 cudaError_t backward_simt(const Attention& a, float* delta, float* part, cudaStream_t s) {
     constexpr size_t smem_q = smem_of<HD>(4, 1), smem_kv = smem_of<HD>(4, 2);
@@ -570,15 +581,8 @@ cudaError_t backward_simt(const Attention& a, float* delta, float* part, cudaStr
     attention_delta_kernel<T><<<(unsigned)((a.N * a.T * a.H + 7) / 8), 256, 0, s>>>(a, delta);
     attention_dq_kernel<T, HD><<<(unsigned)(tiles * a.N * a.H), kThreads, smem_q, s>>>(a, delta, part);
     attention_dkv_kernel<T, HD><<<(unsigned)(tiles * a.N * a.KV), kThreads, smem_kv, s>>>(a, delta);
-    if (a.dtable) {
-        note_launches(1);
-        const unsigned grid = (unsigned)((a.n_buckets * a.H + 7) / 8);
-        if (a.gt == TDA_BF16)
-            attention_dtable_kernel<<<grid, 256, 0, s>>>(part, a.N * tiles, a.n_buckets, a.H, a.beta, (__nv_bfloat16*)a.dtable);
-        else
-            attention_dtable_kernel<<<grid, 256, 0, s>>>(part, a.N * tiles, a.n_buckets, a.H, a.beta, (float*)a.dtable);
-    }
-    return cudaGetLastError();
+    if (cudaError_t e = cudaGetLastError()) return e;
+    return join_table(a, part, a.N * tiles, s);
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -586,11 +590,12 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
 
 size_t attention_ws_bytes(const Attention& a, bool backward, bool bound) {
+    const bool aligned = bound ? a.dt == TDA_BF16 && a.hd % 8 == 0 : attention_tc_supported(a, backward);
+    if (!backward) return aligned ? attention_plan_bytes(a, bound) : 0;
+    const size_t tc = aligned ? attention_grad_tc_bytes(a, bound) : 0;
+    if (aligned && !bound) return tc;
     const size_t tiles = (size_t)((a.T + kTile - 1) / kTile);
-    size_t n = 0;
-    if (bound ? a.dt == TDA_BF16 && a.hd % 8 == 0 : !backward && attention_tc_supported(a, backward)) n += attention_plan_bytes(a, bound);
-    if (backward) n += up((size_t)a.N * a.T * a.H * 4) + up((size_t)a.N * a.H * tiles * a.n_buckets * 4);
-    return n;
+    return std::max(tc, up((size_t)a.N * a.T * a.H * 4) + up((size_t)a.N * a.H * tiles * a.n_buckets * 4));
 }
 
 cudaError_t launch_attention_forward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s) {
@@ -600,7 +605,11 @@ cudaError_t launch_attention_forward(const Attention& a, void* ws, unsigned int*
 }
 
 cudaError_t launch_attention_backward(const Attention& a, void* ws, unsigned int* err, cudaStream_t s) {
-    (void)err;
+    if (attention_tc_supported(a, true)) {
+        float* part;
+        if (cudaError_t e = launch_attention_backward_tc(a, ws, err, &part, s)) return e;
+        return join_table(a, part, a.N * ((a.T + 127) / 128), s);
+    }
     float* delta = (float*)ws;
     float* part = (float*)((char*)ws + up((size_t)a.N * a.T * a.H * 4));
     if (a.dt == TDA_BF16)
