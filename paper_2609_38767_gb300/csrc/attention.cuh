@@ -33,6 +33,25 @@ struct Attention {
     float beta;
 };
 
+// Division of numbers below 2^31 by a number that a launch knows.
+struct FastDiv {
+    uint32_t d = 1, mul = 0, shift = 0;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t n) : d(n) {
+        uint32_t bits = 0;
+        while ((1ull << bits) < n) ++bits;
+        if (n > 1) mul = (uint32_t)(((1ull << (31 + bits)) + n - 1) / n), shift = bits - 1;
+    }
+    __host__ __device__ __forceinline__ int div(int x) const {
+#ifdef __CUDA_ARCH__
+        return d == 1 ? x : (int)(__umulhi((uint32_t)x, mul) >> shift);
+#else
+        return d == 1 ? x : (int)((((uint64_t)(uint32_t)x * mul) >> 32) >> shift);
+#endif
+    }
+    __host__ __device__ __forceinline__ int mod(int x) const { return x - div(x) * (int)d; }
+};
+
 // Keys [x, y) that row i of an example sees; rows past T see none.
 __device__ __forceinline__ int2 visible(const int2* range, int causal, int T, int64_t row0, int i) {
     if (i >= T) return make_int2(0, 0);

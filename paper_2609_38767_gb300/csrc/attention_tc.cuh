@@ -43,17 +43,21 @@ __device__ __forceinline__ void commit(uint32_t lead, uint32_t bar) {
         "r"(lead)
         : "memory");
 }
-// D = A B^T over `steps` steps of 16 values of a head: A and B tiles of panels (a_panel, b_panel bytes), K-major.
-__device__ __forceinline__ void mma_heads(uint32_t lead, uint32_t d, uint32_t a, uint32_t a_panel, uint32_t b, uint32_t b_panel,
-                                          uint32_t idesc, int steps) {
-    for (int k = 0; k < steps; ++k)
-        mma_ss(lead, d, k_major(a + (k >> 2) * a_panel + (k & 3) * 32), k_major(b + (k >> 2) * b_panel + (k & 3) * 32), idesc, k > 0);
+// D = A B^T over the head: A and B tiles of panels, K-major, `steps` of HD / 16 steps. The descriptors are a base and constants: the
+// issuing warp must keep ahead of the tensor pipe, which takes 64 cycles a step.
+template <int HD>
+__device__ __forceinline__ void mma_heads(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
+    const uint64_t da = k_major(a), db = k_major(b);
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k)
+        if (k < steps) mma_ss(lead, d, da + ((k / 4 * kPanel + k % 4 * 32) >> 4), db + ((k / 4 * kPanel + k % 4 * 32) >> 4), idesc, k > 0);
 }
 // D (+)= A B over K tokens: A in TMEM, B [tokens][head] MN-major in panels.
 template <int K>
-__device__ __forceinline__ void mma_tokens(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t panel, uint32_t idesc, bool first) {
+__device__ __forceinline__ void mma_tokens(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool first) {
+    const uint64_t db = mn_major(b, kPanel);
 #pragma unroll
-    for (int k = 0; k < K / 16; ++k) mma_ts(lead, d, a + 8 * k, mn_major(b + k * 2048, panel), idesc, !first || k > 0);
+    for (int k = 0; k < K / 16; ++k) mma_ts(lead, d, a + 8 * k, db + (k * 2048 >> 4), idesc, !first || k > 0);
 }
 
 #define TMEM_R32(r)                                                                                                              \
@@ -111,8 +115,34 @@ __device__ __forceinline__ float rcp_fast(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// tanh by 1 - 2 / (1 + e^2x): right at both infinities, its error about 2^-22 absolute.
-__device__ __forceinline__ float tanh_fast(float x) { return fmaf(-2.f, rcp_fast(1.f + exp2_fast(2.f * kLog2e * x)), 1.f); }
+// tanh of two values. |x| <= 1: x P(x^2), P fitted to a relative error of 2^-22.6, seven multiply-adds a pair; any x: 1 - 2 / (1 + e^2x),
+// right at both infinities, 2^-22 absolute, three special functions a value with the exponential of its weight, of which the SM has
+// 32 (exp2) and 16 (reciprocal) a cycle.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c);
+__device__ __forceinline__ float2 mul2(float2 a, float2 b);
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 tanh_near(float2 x) {
+    const float2 z = mul2(x, x);
+    float2 p = fma2(z, both(0.0010410186368972063f), both(-0.006203366909176111f));
+    p = fma2(z, p, both(0.020289966836571693f));
+    p = fma2(z, p, both(-0.053457021713256836f));
+    p = fma2(z, p, both(0.13325203955173492f));
+    p = fma2(z, p, both(-0.33332839608192444f));
+    p = fma2(z, p, both(0.9999999403953552f));
+    return mul2(x, p);
+}
+__device__ __forceinline__ float2 tanh_any(float2 x) {
+    const float k = 2.f * kLog2e;
+    return make_float2(fmaf(-2.f, rcp_fast(1.f + exp2_fast(k * x.x)), 1.f), fmaf(-2.f, rcp_fast(1.f + exp2_fast(k * x.y)), 1.f));
+}
+// Whether all of a warp's 32 x N dot products stay within the near range.
+template <int N>
+__device__ __forceinline__ bool all_near(const float* s, float inv_cap) {
+    float m[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < N; ++j) m[j & 3] = fmaxf(m[j & 3], fabsf(s[j]));
+    return __all_sync(0xffffffffu, !(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * inv_cap > 1.f));
+}
 // Two bf16 of a column of TMEM, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
@@ -146,8 +176,47 @@ __device__ __forceinline__ void tma_load_head(uint32_t dst, const CUtensorMap* t
         "l"((uint64_t)tm), "r"(col), "r"(head), "r"(row), "r"(n), "r"(bar)
         : "memory");
 }
-__device__ __forceinline__ void chain_prefetch(const CUtensorMap* tm) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)tm) : "memory");
+__device__ __forceinline__ void tma_store_head(const CUtensorMap* tm, uint32_t src, int col, int head, int row, int n) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"((uint64_t)tm), "r"(col),
+                 "r"(head), "r"(row), "r"(n), "r"(src)
+                 : "memory");
+}
+// Zeros the 128-byte rows of a tile's panels whose bit is set (a warp's work): what no query sees may hold anything, and
+// zero times NaN is NaN.
+__device__ __forceinline__ void clear_rows(uint32_t tile, int panels, const uint32_t* bits) {
+    const int lane = threadIdx.x % 32;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (!(bits[w] >> lane & 1)) continue;
+        for (int p = 0; p < panels; ++p)
+            for (int c = 0; c < 8; ++c)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + p * kPanel + (w * 32 + lane) * 128 + c * 16), "r"(0)
+                             : "memory");
+    }
+    fence_proxy_async();
+    __syncwarp();
+}
+
+// wait_bounded by a whole warp, its outcome the same in all lanes, in few instructions: the many roles of these kernels share the
+// SM's instruction cache, and what runs seldom is fetched again each time (with wait_bounded in their place and loops unrolled
+// over the two tiles 8 x 1024 tokens took 96 us, XX this way).
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, unsigned int* err) {
+    uint32_t tries = 0;
+    uint64_t since = 0;
+    bool ok = true;
+#pragma unroll 1
+    while (!mbar_try_wait(bar, parity)) {
+        if (++tries & 63) continue;
+        const uint64_t now = global_ns();
+        if (!since) since = now;
+        if (*abort || now - since > kTimeoutNs) {
+            atomicOr(err, kErrTimeout);
+            *abort = 1;
+            ok = false;
+            break;
+        }
+    }
+    return __all_sync(0xffffffffu, ok);
 }
 
 // Waits, up to the time limit, for what is in flight before a CTA may leave.

@@ -54,27 +54,6 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* tm, i
 #pragma unroll
     for (int p = 0; p < Tiles<HD>::kPanels; ++p) tma_load_head(dst + p * kPanel, tm, 64 * p, head, row, n, bar);
 }
-__device__ __forceinline__ void tma_store_head(const CUtensorMap* tm, uint32_t src, int col, int head, int row, int n) {
-    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"((uint64_t)tm), "r"(col),
-                 "r"(head), "r"(row), "r"(n), "r"(src)
-                 : "memory");
-}
-
-// Zeros the rows of a tile's panels whose bit is set (a warp's work).
-__device__ __forceinline__ void clear_rows(uint32_t tile, int panels, const uint32_t* bits) {
-    const int lane = threadIdx.x % 32;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if (!(bits[w] >> lane & 1)) continue;
-        for (int p = 0; p < panels; ++p)
-            for (int c = 0; c < 8; ++c)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + p * kPanel + (w * 32 + lane) * 128 + c * 16), "r"(0)
-                             : "memory");
-    }
-    fence_proxy_async();
-    __syncwarp();
-}
-
 // 32 columns of an accumulator from column 32 b on, times `by`, into this thread's row of a bf16 tile in shared memory
 // (128-byte swizzle, as TMA stores it).
 __device__ __forceinline__ void stage_columns(uint32_t t, uint32_t tile, int row, int b, float by, bool any) {
@@ -95,7 +74,7 @@ __device__ __forceinline__ void stage_columns(uint32_t t, uint32_t tile, int row
 
 // From a dot product to x and to its slope by the dot product's scaled value.
 __device__ __forceinline__ float capped(float dot, float cap, float inv_cap, float* bend) {
-    const float t = tanh_fast(dot * inv_cap);
+    const float t = tanh_any(both(dot * inv_cap)).x;
     *bend = fmaf(-t, t, 1.f);
     return cap * t;
 }
@@ -357,7 +336,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
                 if (!ok) return;
                 clear(sq + it % S::kQ * kBytes, it);
                 tc_fence_after();
-                mma_heads(lead, tS, sk, kPanel, sq + it % S::kQ * kBytes, kPanel, kIdS, steps);
+                mma_heads<HD>(lead, tS, sk, sq + it % S::kQ * kBytes, kIdS, steps);
                 commit(lead, smem_u32(&bars.s_full));
             };
             auto gradients = [&](int it) {
@@ -365,13 +344,13 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
                 if (!ok) return;
                 clear(sg + it % S::kG * kBytes, it);
                 tc_fence_after();
-                mma_heads(lead, tP, sv, kPanel, sg + it % S::kG * kBytes, kPanel, kIdS, steps);
+                mma_heads<HD>(lead, tP, sv, sg + it % S::kG * kBytes, kIdS, steps);
                 commit(lead, smem_u32(&bars.dp_full));
             };
             // D += A B, A's halves 64 columns apart
             auto sums = [&](uint32_t d, uint32_t t, uint32_t b, bool first) {
-                mma_tokens<64>(lead, d, t, b, kPanel, kIdO, first);
-                mma_tokens<64>(lead, d, t + 64, b + 64 * 128, kPanel, kIdO, false);
+                mma_tokens<64>(lead, d, t, b, kIdO, first);
+                mma_tokens<64>(lead, d, t + 64, b + 64 * 128, kIdO, false);
             };
             if (total) ok = wait_all(&bars.kv_full, 0, abort, err);
             if (ok && total) scores(0);
@@ -663,14 +642,14 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                     if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(tile_k, kPanels, bits);
                 }
                 tc_fence_after();
-                mma_heads(lead, tmem + (it & 1) * 128, sq, kPanel, tile_k, kPanel, kIdS, steps);
+                mma_heads<HD>(lead, tmem + (it & 1) * 128, sq, tile_k, kIdS, steps);
                 commit(lead, smem_u32(&bars.s_full[it & 1]));
             };
             auto gradients = [&](int it) {
                 ok = wait_all(&bars.v_full[it % S::kV], (it / S::kV) & 1, abort, err);
                 if (!ok) return;
                 tc_fence_after();
-                mma_heads(lead, tP, sg, kPanel, sv + it % S::kV * kBytes, kPanel, kIdS, steps);
+                mma_heads<HD>(lead, tP, sg, sv + it % S::kV * kBytes, kIdS, steps);
                 commit(lead, smem_u32(&bars.dp_full));
                 commit(lead, smem_u32(&bars.v_empty[it % S::kV]));
             };
@@ -687,8 +666,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t t = tmem + (it & 1) * 128, tile_k = sk + it % S::kK * kBytes;
-                mma_tokens<64>(lead, tdQ, t, tile_k, kPanel, kIdO, it == 0);
-                mma_tokens<64>(lead, tdQ, t + 64, tile_k + 64 * 128, kPanel, kIdO, false);
+                mma_tokens<64>(lead, tdQ, t, tile_k, kIdO, it == 0);
+                mma_tokens<64>(lead, tdQ, t + 64, tile_k + 64 * 128, kIdO, false);
                 commit(lead, smem_u32(&bars.k_empty[it % S::kK]));
             }
             commit(lead, smem_u32(&bars.done));

@@ -9,8 +9,9 @@
 // O is rescaled only where a row's maximum has grown by more than 2^8 since the last time; P stays below 2^8 then, which
 // costs bf16 nothing, and sums are fp32.
 //
-// Warps 0-3 and 4-7: rows of the tiles (a row per thread); warp 8 issues the MMAs; warp 9 loads by TMA (10 and 11
-// are there because registers are shared out by warpgroups). Waits are bounded
+// Warps 0-3 and 4-7: rows of the tiles (a row per thread); 8: the MMAs (a warp per tile was slower, the two streams share the
+// pipe so that both end late: 8192 tokens 428 us, 344 with one); 9: keys and values; 10: items and queries; 11: biases by distance;
+// 12-15: outputs of finished tiles. Waits are bounded
 // (about 1 s) and set kErrTimeout on expiry.
 #include <cuda.h>
 #include <math_constants.h>
@@ -28,23 +29,27 @@ namespace {
 
 #include "attention_tc.cuh"
 
-// Three warpgroups, whose registers are shared out anew: 168 each at the launch, then 224 for the two that hold rows of
-// scores and 56 for the third, 64,512 in all either way.
-constexpr int kThreads = 384;
+// Four warpgroups, whose registers are shared out anew: 128 a thread at the launch, then 184 for the two that hold rows of
+// scores and 72 for the one that loads and issues and the one that writes outputs, 65,536 in all either way.
+constexpr int kThreads = 512;
 
-template <int HD>
+template <int HD, bool RICH>
 struct Shape {
     static constexpr int kPanels = HD / 64;
     static constexpr uint32_t kTileBytes = kPanels * kPanel;
-    static constexpr int kStages = HD == 64 ? 6 : 4;
-    static constexpr uint32_t kSmem = (2 + kStages) * kTileBytes + 1024;
+    static constexpr int kStages = HD == 64 ? 6 : RICH ? 3 : 4;
+    static constexpr uint32_t kOut = (2 + kStages) * kTileBytes;  // 32 rows of output for each of 4 warps
+    static constexpr uint32_t kBias = kOut + 4 * 32 * HD * 2;     // RICH: 2 x 2 windows of 256 biases
+    static constexpr uint32_t kSmem = kBias + (RICH ? 4 * 1024 : 0);
 };
 
 struct Bars {
-    uint64_t q_full[2], q_empty[2], s_full[2], p_ready[2], o_done[2], done;
-    uint64_t full[8], empty[8];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_ready[2][2], o_done[2], o_free[2], sum_full[2], done;
+    uint64_t item_full[4], item_empty[4], full[8], empty[8], bias_full[2][2], bias_empty[2][2];
     uint32_t tmem;
     int abort;
+    float2 sums[2][kTileT];  // maximum and sum of a finished row
+    int4 items[4][2];
 };
 
 // Keys that a tile's queries see, and between which all of them see all.
@@ -65,84 +70,80 @@ __device__ __forceinline__ Hull hull_of(const Attention& a, const AttentionPlan&
     return a.causal ? Hull{0, min(q0 + kTileT, T), 0, q0 + 1} : Hull{0, T, 0, T};
 }
 
-// Zeros the 128-byte rows of a tile's panels whose bit is set (a warp's work): what no query sees may hold anything, and
-// zero times NaN is NaN.
-__device__ __forceinline__ void clear_rows(uint32_t tile, int panels, const uint32_t* bits) {
-    const int lane = threadIdx.x % 32;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        if (!(bits[w] >> lane & 1)) continue;
-        for (int p = 0; p < panels; ++p)
-            for (int c = 0; c < 8; ++c)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + p * kPanel + (w * 32 + lane) * 128 + c * 16), "r"(0)
-                             : "memory");
-    }
-    fence_proxy_async();
-    __syncwarp();
-}
-
 // The items (pairs of query tiles of a head) of this CTA, long ones first where the mask is causal; every other round
 // backwards, which evens out what the rounds leave.
 struct Items {
-    int total, pairs, heads, H, tiles;
+    int total, pairs, tiles;
+    FastDiv heads, H, group;  // N H, H, H / KV
     __device__ __forceinline__ int at(int round) const {
         const int g = gridDim.x, b = blockIdx.x;
         return round * g + (round & 1 ? g - 1 - b : b);
     }
-    __device__ __forceinline__ int pair(int item) const { return pairs - 1 - item / heads; }
-    __device__ __forceinline__ int example(int item) const { return item % heads / H; }
-    __device__ __forceinline__ int head(int item) const { return item % heads % H; }
+    __device__ __forceinline__ int pair(int item) const { return pairs - 1 - heads.div(item); }
+    __device__ __forceinline__ int example(int item) const { return H.div(heads.mod(item)); }
+    __device__ __forceinline__ int head(int item) const { return H.mod(heads.mod(item)); }
 };
 
-// A key tile of an item, and which tiles of queries see it; next() goes on to the next item with any.
-struct Walk {
-    int round, item, kt, last, n, first0, last0, first1, last1;
-    bool valid;
-    __device__ __forceinline__ void start(const Attention& a, const AttentionPlan& plan, const Items& items) {
-        round = -1, kt = last = 0;
-        next(a, plan, items);
+// An item as warp 10 leaves it for the others, four at a time: working it out takes longer than a step of the MMAs.
+struct Item {
+    int n, h, pair;  // h < 0: no more
+    int first[2], last[2];  // key tiles that the queries of tile w see
+    __device__ __forceinline__ bool any() const { return min(first[0], first[1]) <= max(last[0], last[1]); }
+};
+struct ItemReader {
+    uint32_t r = 0;
+    // The next item; false after the last one, or where a wait ran out (*ok). Called by whole warps.
+    __device__ __forceinline__ bool next(Item& x, Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
+        const uint32_t bar = smem_u32(&bars.item_full[r % 4]), parity = (r / 4) & 1;
+        *ok = *ok && wait_warp(bar, parity, abort, err);
+        if (!*ok) return false;
+        const int4 a = bars.items[r % 4][0], b = bars.items[r % 4][1];
+        x.n = a.x, x.h = a.y, x.pair = a.z;
+        x.first[0] = b.x, x.last[0] = b.y, x.first[1] = b.z, x.last[1] = b.w;
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(&bars.item_empty[r % 4]));
+        ++r;
+        return x.h >= 0;
     }
-    __device__ __forceinline__ void next(const Attention& a, const AttentionPlan& plan, const Items& items) {
+};
+
+// A key tile of an item; next() goes on to the next item that has any.
+struct Walk {
+    Item item;
+    int kt, last;
+    bool valid = true;
+    ItemReader reader;
+    __device__ __forceinline__ void clear() { kt = last = 0; }  // next() then gives the first
+    __device__ __forceinline__ void next(Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
+        if (!valid) return;
         if (kt < last) {
             ++kt;
             return;
         }
-        while (true) {
-            item = items.at(++round);
-            valid = item < items.total;
-            if (!valid) {
-                if ((round + 1) * (int)gridDim.x >= items.total) return;
-                continue;
-            }
-            n = items.example(item);
-            const int tile = 2 * items.pair(item);
-            const Hull a0 = hull_of(a, plan, n, items.tiles, tile), a1 = hull_of(a, plan, n, items.tiles, tile + 1);
-            first0 = a0.any() ? a0.first() : 1 << 30, last0 = a0.any() ? a0.last() : -1;
-            first1 = a1.any() ? a1.first() : 1 << 30, last1 = a1.any() ? a1.last() : -1;
-            kt = min(first0, first1), last = max(last0, last1);
-            if (kt <= last) return;
-        }
+        do valid = reader.next(item, bars, ok, abort, err);
+        while (valid && !item.any());
+        kt = min(item.first[0], item.first[1]), last = max(item.last[0], item.last[1]);
     }
-    __device__ __forceinline__ int first_of(int w) const { return w ? first1 : first0; }
-    __device__ __forceinline__ int last_of(int w) const { return w ? last1 : last0; }
-    __device__ __forceinline__ bool active(int w) const { return kt >= first_of(w) && kt <= last_of(w); }
+    __device__ __forceinline__ bool active(int w) const { return kt >= item.first[w] && kt <= item.last[w]; }
 };
 
 template <int HD, bool RICH>
 __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                                                                    const __grid_constant__ CUtensorMap tmK,
                                                                    const __grid_constant__ CUtensorMap tmV, const Attention a,
-                                                                   const AttentionPlan plan, unsigned int* err) {
-    using S = Shape<HD>;
-    extern __shared__ uint8_t raw[];
+                                                                   const AttentionPlan plan, const Items items, unsigned int* err) {
+    using S = Shape<HD, RICH>;
+    extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ Bars bars;
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t base = smem_u32(raw);
+    uint8_t* from = raw;
+    if (base & 1023u) {  // the tiles' swizzle needs it
+        if (threadIdx.x == 0) atomicOr(err, kErrBadLaunch);
+        return;
+    }
     const uint32_t sq = base, ring = base + 2 * S::kTileBytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const int T = (int)a.T;
-    Items items;
-    items.tiles = (T + kTileT - 1) / kTileT, items.pairs = (items.tiles + 1) / 2, items.H = a.H, items.heads = (int)(a.N * a.H);
-    items.total = items.pairs * items.heads;
     volatile int* abort = &bars.abort;
 
     if (warp == 8) {
@@ -153,11 +154,18 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                 mbar_init(smem_u32(&bars.q_full[w]), 1);
                 mbar_init(smem_u32(&bars.q_empty[w]), 1);
                 mbar_init(smem_u32(&bars.s_full[w]), 1);
-                mbar_init(smem_u32(&bars.p_ready[w]), 128);
+                mbar_init(smem_u32(&bars.p_ready[w][0]), 4);
+                mbar_init(smem_u32(&bars.p_ready[w][1]), 4);
+                mbar_init(smem_u32(&bars.o_free[w]), 4);
+                mbar_init(smem_u32(&bars.sum_full[w]), 4);
                 mbar_init(smem_u32(&bars.o_done[w]), 1);
             }
             mbar_init(smem_u32(&bars.done), 1);
             for (int s = 0; s < S::kStages; ++s) mbar_init(smem_u32(&bars.full[s]), 1), mbar_init(smem_u32(&bars.empty[s]), 1);
+            for (int r = 0; r < 4; ++r)  // read by the warps of rows and outputs, by the MMAs', the loads' and the biases'
+                mbar_init(smem_u32(&bars.item_full[r]), 1), mbar_init(smem_u32(&bars.item_empty[r]), 14 + (RICH && plan.lut));
+            for (int w = 0; w < 2; ++w)
+                for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&bars.bias_full[w][b]), 32), mbar_init(smem_u32(&bars.bias_empty[w][b]), 4);
             bars.abort = 0;
             fence_mbar_init();
         }
@@ -170,244 +178,449 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
     const uint32_t tmem = bars.tmem;
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         const int w = warp / 4, row = threadIdx.x % 128;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // TMEM lane of the warp's first row
         const uint32_t ts = tmem + lanes + w * 128, to = tmem + lanes + 256 + w * 128;
+        const float* biases = (const float*)(from + S::kBias) + w * 512;
         const float c = RICH ? kLog2e : a.scale * kLog2e;  // s is x (RICH) or the dot product
+        const float2 c2 = both(c);
         const float grow = 8.f / c, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
         bool ok = true;
-        uint32_t turn = 0;  // key tiles so far
-        for (int round = 0; ok && round * (int)gridDim.x < items.total; ++round) {
-            const int item = items.at(round);
-            if (item >= items.total) break;
-            const int n = items.example(item), h = items.head(item), tile = 2 * items.pair(item) + w, q0 = tile * kTileT, i = q0 + row;
-            if (q0 >= T) continue;
-            const Hull my = hull_of(a, plan, n, items.tiles, tile);
-            const int2 see = visible(a.range, a.causal, T, (int64_t)n * T, i);
+        uint32_t turn = 0, outputs = 0;  // key tiles, outputs so far
+        ItemReader reader;
+        Item item, then;
+        int2 see, see_then = make_int2(0, 0);
+        then.h = -2;
+        while (ok) {
+            // the next item and what this thread's row sees in it, one item ahead
+            item = then, see = see_then;
+            if (item.h == -1) break;
+            if (!reader.next(then, bars, &ok, abort, err)) then.h = -1;
+            else see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, (2 * then.pair + w) * kTileT + row);
+            if (item.h < 0) continue;
+            const int first = w ? item.first[1] : item.first[0], last = w ? item.last[1] : item.last[0];
+            if (first > last) continue;
+            const int q0 = (2 * item.pair + w) * kTileT, i = q0 + row;
+            // what the warp's rows see: nothing outside [lo, hi), everything within [most, least)
+            const bool none = see.x >= see.y;
+            const int most = __reduce_max_sync(0xffffffffu, none ? 0 : see.x);
+            const int least = __reduce_min_sync(0xffffffffu, i >= T ? T : none ? 0 : see.y);
+            const int lo = RICH ? __reduce_min_sync(0xffffffffu, none ? T : see.x) : 0;
+            const int hi = RICH ? __reduce_max_sync(0xffffffffu, none ? 0 : see.y) : 0;
             float top = -CUDART_INF_F, sum = 0.f;
-            const int first = my.first(), last = my.any() ? my.last() : -1;
             for (int kt = first; kt <= last; ++kt, ++turn) {
                 const int k0 = kt * kTileT;
-                ok = __all_sync(0xffffffffu, wait_bounded(smem_u32(&bars.s_full[w]), turn & 1, abort, err));
+                ok = wait_warp(smem_u32(&bars.s_full[w]), turn & 1, abort, err);
                 if (!ok) break;
                 tc_fence_after();
-                float s[128];
+                float most_now = top;
+                float s[RICH ? 32 : 128];
+                const bool whole = most <= k0 && least >= k0 + kTileT;
+                auto sees = [&](int b) { return lo < k0 + 32 * b + 32 && hi > k0 + 32 * b; };
+                auto mask = [&](int b, float* x) {
+                    const int at = k0 + 32 * b;
+                    if (most <= at && least >= at + 32) return;
+                    const int from = min(max(see.x - at, 0), 32), to = min(max(see.y - at, 0), 32);
+                    const uint32_t bits = from < to ? (to == 32 ? ~0u : (1u << to) - 1) & (~0u << from) : 0u;
 #pragma unroll
-                for (int b = 0; b < 4; ++b) tmem_ld32(ts + 32 * b, s + 32 * b);
-                tmem_wait_ld();
+                    for (int j = 0; j < 32; ++j)
+                        if (!(bits >> j & 1)) x[j] = -CUDART_INF_F;
+                };
+                auto largest = [&](const float* x) {
+                    float m[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                for (int b = 0; b < 4; ++b) tmem_use(s + 32 * b);
+                    for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], x[j]);
+                    most_now = fmaxf(most_now, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+                };
                 if constexpr (RICH) {
-                    if (a.cap > 0.f) {
-#pragma unroll
-                        for (int j = 0; j < 128; ++j) s[j] = a.cap * tanh_fast(s[j] * inv_cap);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 128; ++j) s[j] *= a.scale;
-                    }
+                    // scores with cap and bias go back to TMEM, 32 columns at a time
+                    const float* bias = nullptr;
+                    bool flat = false;
                     if (plan.lut) {
-                        const int apart = min(max(q0 - k0, -plan.reach - 127), plan.reach + 127);
-                        const float* bias = plan.lut + (int64_t)h * plan.lut_len + plan.lut_mid + apart + row;
-#pragma unroll
-                        for (int j = 0; j < 128; ++j) s[j] += bias[-j];
+                        ok = wait_warp(smem_u32(&bars.bias_full[w][turn & 1]), (turn / 2) & 1, abort, err);
+                        if (!ok) break;
+                        bias = biases + (turn & 1) * 256 + 127 + row;
+                        flat = q0 - k0 >= plan.reach + 127 || q0 - k0 <= -plan.reach - 127;
                     }
-                }
-                if (my.most > k0 || my.least < k0 + kTileT) {
-                    const int lo = see.x - k0;
-                    const uint32_t len = (uint32_t)max(see.y - see.x, 0);
+#pragma unroll 1
+                    for (int b = 0; b < 4; ++b) {
+                        if (!sees(b)) continue;
+                        tmem_ld32(ts + 32 * b, s);
+                        tmem_wait_ld();
+                        tmem_use(s);
+                        if (a.cap > 0.f) {
+                            if (all_near<32>(s, inv_cap)) {
 #pragma unroll
-                    for (int j = 0; j < 128; ++j)
-                        if ((uint32_t)(j - lo) >= len) s[j] = -CUDART_INF_F;
-                }
-                float m4[4] = {s[0], s[1], s[2], s[3]};
+                                for (int j = 0; j < 32; j += 2) {
+                                    const float2 x = mul2(tanh_near(mul2(make_float2(s[j], s[j + 1]), both(inv_cap))), both(a.cap));
+                                    s[j] = x.x, s[j + 1] = x.y;
+                                }
+                            } else {
 #pragma unroll
-                for (int j = 4; j < 128; ++j) m4[j & 3] = fmaxf(m4[j & 3], s[j]);
-                const float most = fmaxf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), top);
+                                for (int j = 0; j < 32; j += 2) {
+                                    const float2 x = mul2(tanh_any(mul2(make_float2(s[j], s[j + 1]), both(inv_cap))), both(a.cap));
+                                    s[j] = x.x, s[j + 1] = x.y;
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) s[j] *= a.scale;
+                        }
+                        if (bias) {
+                            if (flat) {
+                                const float x = *bias;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) s[j] += x;
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) s[j] += bias[-32 * b - j];
+                            }
+                        }
+                        if (!whole) mask(b, s);
+                        largest(s);
+                        tmem_st32(ts + 32 * b, (const uint32_t*)s);
+                    }
+                    tmem_wait_st();
+                    if (bias) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bars.bias_empty[w][turn & 1]));
+                    }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) tmem_ld32(ts + 32 * b, s + 32 * b);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) tmem_use(s + 32 * b);
+                    if (!whole) {
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) mask(b, s + 32 * b);
+                    }
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) largest(s + 32 * b);
+                }
                 if (kt == first) {
-                    top = most;
-                } else if (__any_sync(0xffffffffu, most > top + grow)) {
-                    ok = __all_sync(0xffffffffu, wait_bounded(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err));
+                    top = most_now;
+                } else if (__any_sync(0xffffffffu, most_now > top + grow)) {
+                    ok = wait_warp(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err);
                     if (!ok) break;
                     tc_fence_after();
-                    const float by = most == -CUDART_INF_F ? 1.f : exp2_fast((top - most) * c);
-                    top = most;
+                    const float by = most_now == -CUDART_INF_F ? 1.f : exp2_fast((top - most_now) * c);
+                    top = most_now;
                     sum *= by;
+#pragma unroll 1
+                    for (int b = 0; b < HD / 16; ++b) {
+                        float o[16];
+                        tmem_ld16(to + 16 * b, o);
 #pragma unroll
-                    for (int b = 0; b < HD / 32; ++b) {
-                        float o[32];
-                        tmem_ld32(to + 32 * b, o);
-                        tmem_wait_ld();
-                        tmem_use(o);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] *= by;
-                        tmem_st32(to + 32 * b, (const uint32_t*)o);
+                        for (int j = 0; j < 16; ++j) o[j] *= by;
+                        tmem_st16(to + 16 * b, (const uint32_t*)o);
                     }
                 }
-                const float from = top == -CUDART_INF_F ? 0.f : top;
-                uint32_t p[64];
-                float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                const float2 c2 = make_float2(c, c);
-                const float2 less = RICH ? make_float2(-from, -from) : make_float2(-from * c, -from * c);
+                const float base_of = top == -CUDART_INF_F ? 0.f : top;
+                const float2 less = both(RICH ? -base_of : -base_of * c);
+                float2 part[2] = {both(0.f), both(0.f)};
+                // P of 32 columns of scores
+                auto weigh = [&](const float* x, uint32_t* p) {
 #pragma unroll
-                for (int j = 0; j < 64; ++j) {
-                    float2 x = make_float2(s[2 * j], s[2 * j + 1]);
-                    // the score less the maximum first where a bias may be as large as fp32 goes
-                    x = RICH ? mul2(add2(x, less), c2) : fma2(x, c2, less);
-                    x.x = exp2_fast(x.x), x.y = exp2_fast(x.y);
-                    part[j & 1] = add2(part[j & 1], x);
-                    p[j] = pack_bf16(x.x, x.y);
+                    for (int j = 0; j < 16; ++j) {
+                        float2 v = make_float2(x[2 * j], x[2 * j + 1]);
+                        // the score less the maximum first where a bias may be as large as fp32 goes
+                        v = RICH ? mul2(add2(v, less), c2) : fma2(v, c2, less);
+                        v.x = exp2_fast(v.x), v.y = exp2_fast(v.y);
+                        part[j & 1] = add2(part[j & 1], v);
+                        p[j] = pack_bf16(v.x, v.y);
+                    }
+                };
+                // in two parts of 64 keys, over columns of S that have been read: the MMAs of the first begin while the second is
+                // computed
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int b = 2 * half + e;
+                        if constexpr (RICH) {
+                            if (!sees(b)) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) p[16 * e + j] = 0;
+                                continue;
+                            }
+                            tmem_ld32(ts + 32 * b, s);
+                            tmem_wait_ld();
+                            tmem_use(s);
+                            weigh(s, p + 16 * e);
+                        } else {
+                            weigh(s + 32 * b, p + 16 * e);
+                        }
+                    }
+                    tmem_st32(ts + 32 * half, p);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bars.p_ready[w][half]));
                 }
-                tmem_st32(ts, p);
-                tmem_st32(ts + 32, p + 32);
                 sum += part[0].x + part[0].y + part[1].x + part[1].y;
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(smem_u32(&bars.p_ready[w]));
             }
-            if (ok && first <= last)
-                ok = __all_sync(0xffffffffu, wait_bounded(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err));
+            // an item of one key tile does not wait for the output before it: here it does, as that one's sums may not have been read
+            if (ok && outputs++) ok = wait_warp(smem_u32(&bars.o_free[w]), outputs & 1, abort, err);
             if (!ok) break;
-            tc_fence_after();
-            const float by = sum != 0.f ? 1.f / sum : 0.f;  // NaN sums stay NaN
-            if (a.lse && i < T)
-                a.lse[((int64_t)n * a.H + h) * T + i] = sum != 0.f ? fmaf(top, RICH ? 1.f : a.scale, logf(sum)) : -CUDART_INF_F;
-            __nv_bfloat16* out = (__nv_bfloat16*)a.O + ((int64_t)n * T + i) * a.ld_o + h * a.hd;
+            bars.sums[w][row] = make_float2(top, sum);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.sum_full[w]));
+        }
+        tc_fence_before();
+    } else if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        // outputs of either tile, beside the rows of the next item
+        const int q = warp % 4, row = q * 32 + lane;
+        const uint32_t out = base + S::kOut + q * 64 * HD;
+        uint32_t turns[2] = {0, 0}, done[2] = {0, 0};  // key tiles, outputs so far
+        bool ok = true;
+        ItemReader reader;
+        Item item;
+        while (reader.next(item, bars, &ok, abort, err)) {
+            const int n = item.n, h = item.h;
 #pragma unroll
-            for (int b = 0; b < HD / 32; ++b) {
-                float o[32];
-                tmem_ld32(to + 32 * b, o);
-                tmem_wait_ld();
-                tmem_use(o);
-                if (i < T) {
+            for (int w = 0; w < 2; ++w) {
+                const int q0 = (2 * item.pair + w) * kTileT, i = q0 + row;
+                if (!ok || q0 >= T) continue;
+                const bool any = item.first[w] <= item.last[w];
+                float top = 0.f, sum = 0.f;
+                if (any) {
+                    turns[w] += item.last[w] - item.first[w] + 1;
+                    ok = wait_warp(smem_u32(&bars.sum_full[w]), done[w]++ & 1, abort, err) &&
+                         wait_warp(smem_u32(&bars.o_done[w]), (turns[w] - 1) & 1, abort, err);
+                    if (!ok) continue;
+                    top = bars.sums[w][row].x, sum = bars.sums[w][row].y;
+                    tc_fence_after();
+                }
+                const float by = sum != 0.f ? 1.f / sum : 0.f;  // NaN sums stay NaN
+                const uint32_t to = tmem + ((uint32_t)q << 21) + 256 + w * 128;
+#pragma unroll 1
+                for (int b = 0; b < HD / 32; ++b) {
+                    float o[32];
+                    tmem_ld32(to + 32 * b, o);
+                    tmem_wait_ld();
+                    tmem_use(o);
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        if (32 * b + 8 * g >= a.hd) continue;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (by != 0.f) {  // rows that see nothing: TMEM may hold anything
-                            const float* x = o + 8 * g;
-                            v = make_uint4(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by),
-                                           pack_bf16(x[4] * by, x[5] * by), pack_bf16(x[6] * by, x[7] * by));
-                        }
-                        *(uint4*)(out + 32 * b + 8 * g) = v;
+                        const float* x = o + 8 * g;
+                        uint32_t v[4] = {0, 0, 0, 0};
+                        if (by != 0.f)  // rows that see nothing: TMEM may hold anything
+                            v[0] = pack_bf16(x[0] * by, x[1] * by), v[1] = pack_bf16(x[2] * by, x[3] * by),
+                            v[2] = pack_bf16(x[4] * by, x[5] * by), v[3] = pack_bf16(x[6] * by, x[7] * by);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(out + lane * 2 * HD + ((4 * b + g) ^ (lane & 7)) * 16),
+                                     "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+                                     : "memory");
                     }
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (any && lane == 0) mbar_arrive(smem_u32(&bars.o_free[w]));
+                if (a.lse && i < T)
+                    a.lse[((int64_t)n * a.H + h) * T + i] = sum != 0.f ? fmaf(top, RICH ? 1.f : a.scale, logf(sum)) : -CUDART_INF_F;
+                // whole rows on the way out
+                constexpr int kLanes = HD / 8;  // of a row
+                const int col = lane % kLanes * 8;
+                __nv_bfloat16* dst = (__nv_bfloat16*)a.O + ((int64_t)n * T + q0 + q * 32) * a.ld_o + h * a.hd + col;
+#pragma unroll
+                for (int r = lane / kLanes; r < 32; r += 32 / kLanes) {
+                    uint32_t v[4];
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                                 : "r"(out + r * 2 * HD + ((lane % kLanes) ^ (r & 7)) * 16)
+                                 : "memory");
+                    if (col < a.hd && q0 + q * 32 + r < T) *(uint4*)(dst + r * a.ld_o) = make_uint4(v[0], v[1], v[2], v[3]);
+                }
+                __syncwarp();
             }
         }
         tc_fence_before();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 9) {
-            if (elect_one()) {
-                uint32_t used = 0, queries[2] = {0, 0};  // loads so far
-                Walk at;
-                bool ok = true;
-                auto load = [&](const CUtensorMap* tm, int kv) {
+            const uint32_t lead = elect_one();
+            uint32_t used = 0;  // loads so far
+            bool ok = true;
+            Walk at;
+            at.clear();
+            while (true) {
+                at.next(bars, &ok, abort, err);
+                if (!ok || !at.valid) break;
+                const int kv = items.group.div(at.item.h);
+#pragma unroll 1
+                for (int e = 0; e < 2; ++e) {
                     const uint32_t s = used % S::kStages, turn = used / S::kStages;
-                    if (turn && !wait_bounded(smem_u32(&bars.empty[s]), (turn - 1) & 1, abort, err)) return false;
-                    const uint32_t bar = smem_u32(&bars.full[s]);
-                    mbar_arrive_tx(bar, S::kTileBytes);
-                    for (int p = 0; p < S::kPanels; ++p)
-                        tma_load_head(ring + s * S::kTileBytes + p * kPanel, tm, 64 * p, kv, at.kt * kTileT, at.n, bar);
-                    ++used;
-                    return true;
-                };
-                auto load_q = [&](int w, int h, int pair) {
-                    if (at.first_of(w) > at.last_of(w)) return true;
-                    if (queries[w] && !wait_bounded(smem_u32(&bars.q_empty[w]), (queries[w] - 1) & 1, abort, err)) return false;
-                    const uint32_t bar = smem_u32(&bars.q_full[w]);
-                    mbar_arrive_tx(bar, S::kTileBytes);
-                    for (int p = 0; p < S::kPanels; ++p)
-                        tma_load_head(sq + w * S::kTileBytes + p * kPanel, &tmQ, 64 * p, h, (2 * pair + w) * kTileT, at.n, bar);
-                    ++queries[w];
-                    return true;
-                };
-                for (at.start(a, plan, items); ok && at.valid; at.next(a, plan, items)) {
-                    const int h = items.head(at.item), pair = items.pair(at.item), kv = h / (a.H / a.KV);
-                    const bool first = at.kt == min(at.first0, at.first1);
-                    if (first) ok = load_q(0, h, pair);
-                    ok = ok && load(&tmK, kv);
-                    if (first) ok = ok && load_q(1, h, pair);
-                    ok = ok && load(&tmV, kv);
-                }
+                    if (turn) ok = ok && wait_warp(smem_u32(&bars.empty[s]), (turn - 1) & 1, abort, err);
+                    if (!ok) break;
+                    if (lead) {
+                        const uint32_t bar = smem_u32(&bars.full[s]);
+                        mbar_arrive_tx(bar, S::kTileBytes);
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    if (queries[w]) wait_settled(smem_u32(&bars.q_full[w]), (queries[w] - 1) & 1, err);
-                for (uint32_t s = 0; s < (uint32_t)S::kStages; ++s)
-                    if (used > s) wait_settled(smem_u32(&bars.full[s]), ((used - 1 - s) / S::kStages) & 1, err);
+                        for (int p = 0; p < S::kPanels; ++p)
+                            tma_load_head(ring + s * S::kTileBytes + p * kPanel, e ? &tmV : &tmK, 64 * p, kv, at.kt * kTileT, at.item.n, bar);
+                    }
+                    __syncwarp();
+                    ++used;
+                }
             }
-            __syncwarp();
+            for (uint32_t s = 0; s < (uint32_t)S::kStages; ++s)
+                if (used > s) wait_settled(smem_u32(&bars.full[s]), ((used - 1 - s) / S::kStages) & 1, err);
+        } else if (warp == 10) {
+            // the items, one ahead of their queries, which are loaded as soon as there is room
+            const uint32_t lead = elect_one();
+            uint32_t asked0 = 0, asked1 = 0, made = 0;  // query tiles of either kind, items so far
+            bool ok = true;
+            auto make = [&]() {
+                const uint32_t r = made++;
+                if (r >= 4) ok = ok && wait_warp(smem_u32(&bars.item_empty[r % 4]), (r / 4 - 1) & 1, abort, err);
+                if (!ok) return;
+                const int id = items.at((int)r);
+                int n = 0, h = -1, pair = 0;
+                Hull hull[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                if (id < items.total) {
+                    n = items.example(id), h = items.head(id), pair = items.pair(id);
+                    hull[0] = hull_of(a, plan, n, items.tiles, 2 * pair), hull[1] = hull_of(a, plan, n, items.tiles, 2 * pair + 1);
+                }
+                if (lead) {
+                    const int none = 1 << 30;
+                    bars.items[r % 4][0] = make_int4(n, h, pair, 0);
+                    bars.items[r % 4][1] = make_int4(hull[0].any() ? hull[0].first() : none, hull[0].any() ? hull[0].last() : -1,
+                                                     hull[1].any() ? hull[1].first() : none, hull[1].any() ? hull[1].last() : -1);
+                    mbar_arrive(smem_u32(&bars.item_full[r % 4]));
+                }
+                __syncwarp();
+            };
+            for (uint32_t r = 0; ok; ++r) {  // makes item r, loads the queries of item r - 1
+                if (r && bars.items[(r - 1) % 4][0].y < 0) break;
+                make();
+                if (r == 0) continue;
+                // nobody can have replaced what this warp made: the slot is free for item r + 3 once its readers have passed it
+                const int4 x = bars.items[(r - 1) % 4][0], y = bars.items[(r - 1) % 4][1];
+#pragma unroll 1
+                for (int w = 0; w < 2; ++w) {
+                    if (!ok || (w ? y.z > y.w : y.x > y.y)) continue;
+                    const uint32_t turn = w ? asked1 : asked0;
+                    if (turn) ok = wait_warp(smem_u32(&bars.q_empty[w]), (turn - 1) & 1, abort, err);
+                    if (!ok) continue;
+                    if (lead) {
+                        const uint32_t bar = smem_u32(&bars.q_full[w]);
+                        mbar_arrive_tx(bar, S::kTileBytes);
+#pragma unroll
+                        for (int p = 0; p < S::kPanels; ++p)
+                            tma_load_head(sq + w * S::kTileBytes + p * kPanel, &tmQ, 64 * p, x.y, (2 * x.z + w) * kTileT, x.x, bar);
+                    }
+                    __syncwarp();
+                    w ? ++asked1 : ++asked0;
+                }
+            }
+            if (asked0) wait_settled(smem_u32(&bars.q_full[0]), (asked0 - 1) & 1, err);
+            if (asked1) wait_settled(smem_u32(&bars.q_full[1]), (asked1 - 1) & 1, err);
         } else if (warp == 8) {
             const uint32_t lead = elect_one();
             const int steps = (a.hd + 15) / 16;
             constexpr uint32_t kIdS = idesc_bf16(kTileT, kTileT), kIdO = idesc_bf16(kTileT, HD) | kBMn;
-            uint32_t queries[2] = {0, 0}, weights[2] = {0, 0};  // query tiles, key tiles so far
-            uint32_t used = 0;                                  // stages so far: K, V, K, V ...
-            auto full = [&](uint32_t at) {
-                return __all_sync(0xffffffffu, wait_bounded(smem_u32(&bars.full[at % S::kStages]), (at / S::kStages) & 1, abort, err));
-            };
+            // bit w: parity of the query tiles, of the key tiles, of the outputs of tile w so far; some output; stages (K, V, K ...)
+            uint32_t par_q = 0, par_p = 0, par_o = 0, some_o = 0, used = 0;
+            auto full = [&](uint32_t at) { return wait_warp(smem_u32(&bars.full[at % S::kStages]), (at / S::kStages) & 1, abort, err); };
             auto release = [&](uint32_t at) { commit(lead, smem_u32(&bars.empty[at % S::kStages])); };
             auto stage = [&](uint32_t at) { return ring + (at % S::kStages) * S::kTileBytes; };
             bool ok = true;
-            // scores of tile w with the keys of stage `at`
-            auto scores = [&](const Walk& k, int w, uint32_t at) {
-                if (k.kt == k.first_of(w)) {
-                    ok = __all_sync(0xffffffffu, wait_bounded(smem_u32(&bars.q_full[w]), queries[w] & 1, abort, err));
-                    if (!ok) return;
-                    ++queries[w];
-                }
-                tc_fence_after();
-                mma_heads(lead, tmem + w * 128, sq + w * S::kTileBytes, kPanel, stage(at), kPanel, kIdS, steps);
-                commit(lead, smem_u32(&bars.s_full[w]));
-                if (k.kt == k.last_of(w)) commit(lead, smem_u32(&bars.q_empty[w]));
-            };
-            uint32_t bits[4], next[4];
-            auto unseen = [&](const Walk& k) {
-                if (a.range && k.valid) *(uint4*)next = *(const uint4*)plan.tiles[(int64_t)k.n * items.tiles + k.kt].unseen;
-            };
-            Walk now;
-            now.start(a, plan, items);
-            if (now.valid) {
-                unseen(now);
-                ok = full(0);
-#pragma unroll
-                for (int w = 0; w < 2; ++w)
-                    if (ok && now.active(w)) scores(now, w, 0);
-                if (ok) release(0);
-                used = 1;
-            }
-            while (ok && now.valid) {
-                const uint32_t at_v = used, at_k = used + 1;
-                Walk then = now;
-                then.next(a, plan, items);
-                *(uint4*)bits = *(const uint4*)next;
-                unseen(then);
-                ok = full(at_v);
-                if (!ok) break;
-                if (a.range && (bits[0] | bits[1] | bits[2] | bits[3])) clear_rows(stage(at_v), S::kPanels, bits);
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    if (ok && now.active(w)) {
-                        ok = __all_sync(0xffffffffu, wait_bounded(smem_u32(&bars.p_ready[w]), weights[w] & 1, abort, err));
-                        if (ok) {
-                            tc_fence_after();
-                            mma_tokens<kTileT>(lead, tmem + 256 + w * 128, tmem + w * 128, stage(at_v), kPanel, kIdO,
-                                               now.kt == now.first_of(w));
-                            commit(lead, smem_u32(&bars.o_done[w]));
-                            ++weights[w];
-                        }
+            Walk now, then;
+            then.clear();
+            now.valid = false;
+            // a step: O += P V of the key tile `now`, then S of the one after it, for either tile of queries
+            while (true) {
+                const uint32_t at_v = used, at_k = now.valid ? used + 1 : used;
+                then.next(bars, &ok, abort, err);
+                if (!ok || (!now.valid && !then.valid)) break;
+                uint64_t v = 0;
+                if (now.valid) {
+                    ok = full(at_v);
+                    if (!ok) break;
+                    if (a.range) {
+                        uint32_t bits[4];
+                        *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)now.item.n * items.tiles + now.kt].unseen;
+                        if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(stage(at_v), S::kPanels, bits);
                     }
-                    if (w == 0 && ok && then.valid) ok = full(at_k);
-                    if (ok && then.valid && then.active(w)) scores(then, w, at_k);
+                    v = mn_major(stage(at_v), kPanel);
+                }
+#pragma unroll 1
+                for (int w = 0; w < 2; ++w) {
+                    const uint32_t ts = tmem + w * 128, to = tmem + 256 + w * 128;
+                    const int first = w ? now.item.first[1] : now.item.first[0], last = w ? now.item.last[1] : now.item.last[0];
+                    if (now.valid && now.kt >= first && now.kt <= last) {
+                        if (now.kt == first) {  // the tile's last output has been read
+                            if (some_o >> w & 1) ok = wait_warp(smem_u32(&bars.o_free[w]), ~par_o >> w & 1, abort, err);
+                            some_o |= 1u << w, par_o ^= 1u << w;
+                        }
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {  // 64 keys each
+                            ok = ok && wait_warp(smem_u32(&bars.p_ready[w][b]), par_p >> w & 1, abort, err);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                mma_ts(lead, to, ts + 8 * (4 * b + e), v + ((4 * b + e) * 2048 >> 4), kIdO, now.kt != first || b + e > 0);
+                        }
+                        if (!ok) break;
+                        commit(lead, smem_u32(&bars.o_done[w]));
+                        par_p ^= 1u << w;
+                    }
+                    if (!then.valid) continue;
+                    if (w == 0) ok = full(at_k);
+                    const int first_k = w ? then.item.first[1] : then.item.first[0], last_k = w ? then.item.last[1] : then.item.last[0];
+                    if (ok && then.kt >= first_k && then.kt <= last_k) {
+                        if (then.kt == first_k) {
+                            ok = wait_warp(smem_u32(&bars.q_full[w]), par_q >> w & 1, abort, err);
+                            par_q ^= 1u << w;
+                        }
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_heads<HD>(lead, ts, sq + w * S::kTileBytes, stage(at_k), kIdS, steps);
+                        commit(lead, smem_u32(&bars.s_full[w]));
+                        if (then.kt == last_k) commit(lead, smem_u32(&bars.q_empty[w]));
+                    }
+                    if (!ok) break;
                 }
                 if (!ok) break;
-                release(at_v);
+                if (now.valid) release(at_v);
                 if (then.valid) release(at_k);
-                used += 2;
+                used += (now.valid ? 1 : 0) + (then.valid ? 1 : 0);
                 now = then;
             }
             commit(lead, smem_u32(&bars.done));
             wait_settled(smem_u32(&bars.done), 0, err);
+        } else if (RICH && plan.lut && warp == 11) {
+            // the biases of a tile's 255 distances, ahead of its rows
+            uint32_t turns[2] = {0, 0};
+            bool ok = true;
+            Walk at;
+            at.clear();
+            while (true) {
+                at.next(bars, &ok, abort, err);
+                if (!ok || !at.valid) break;
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const uint32_t turn = turns[w];
+                    if (!at.active(w)) continue;
+                    if (turn >= 2)
+                        ok = wait_warp(smem_u32(&bars.bias_empty[w][turn & 1]), (turn / 2 - 1) & 1, abort, err);
+                    if (!ok) break;
+                    const int q0 = (2 * at.item.pair + w) * kTileT, k0 = at.kt * kTileT;
+                    const int apart = min(max(q0 - k0, -plan.reach - 127), plan.reach + 127);
+                    const float* src = plan.lut + (int64_t)at.item.h * plan.lut_len + plan.lut_mid + apart - 127;
+                    float* dst = (float*)(from + S::kBias) + w * 512 + (turn & 1) * 256;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = src[min(32 * e + lane, 254)];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dst[32 * e + lane] = v[e];
+                    mbar_arrive(smem_u32(&bars.bias_full[w][turn & 1]));
+                    ++turns[w];
+                }
+            }
         }
     }
     __syncthreads();
@@ -511,7 +724,7 @@ bool has_lut(const Attention& a, bool bound) { return a.n_buckets || a.slope || 
 
 template <int HD, bool RICH>
 cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s) {
-    using Sh = Shape<HD>;
+    using Sh = Shape<HD, RICH>;
     if (cudaError_t e = smem_attr_once<attention_tc_kernel<HD, RICH>>(Sh::kSmem)) return e;
     CUtensorMap q, k, v;
     if (!attention_head_map(&q, a.Q, a.ld_q, a.H, a.hd, a.T, a.N, kTileT) ||
@@ -522,9 +735,11 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     bool chained;
     if (cudaError_t e = launch_attention_plan(a, ws, &plan, &chained, s)) return e;
     const int64_t tiles = (a.T + kTileT - 1) / kTileT;
-    const int64_t items = (tiles + 1) / 2 * a.N * a.H;
-    return launch_chained(chained, attention_tc_kernel<HD, RICH>, dim3((unsigned)std::min<int64_t>(items, train_sms())), dim3(kThreads),
-                          Sh::kSmem, s, q, k, v, a, plan, err);
+    Items items;
+    items.tiles = (int)tiles, items.pairs = (int)((tiles + 1) / 2), items.total = (int)(items.pairs * a.N * a.H);
+    items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
+    return launch_chained(chained, attention_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())), dim3(kThreads),
+                          Sh::kSmem, s, q, k, v, a, plan, items, err);
 }
 
 }  // namespace

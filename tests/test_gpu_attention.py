@@ -172,6 +172,7 @@ SHAPES = [
     # (N, T, H, KV, hd)
     (1, 1, 1, 1, 64), (2, 2, 2, 1, 128), (1, 37, 4, 2, 64), (2, 64, 2, 2, 128), (1, 127, 3, 1, 96), (3, 128, 2, 1, 64),
     (1, 129, 2, 2, 128), (1, 255, 4, 1, 80), (2, 257, 2, 2, 128), (1, 300, 2, 1, 8), (1, 513, 2, 1, 64),
+    (30, 140, 16, 2, 64), (9, 600, 16, 4, 128),  # more tiles than SMs
 ]
 
 
