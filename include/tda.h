@@ -715,7 +715,7 @@ tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float ma
  * Sums and statistics are fp32. bf16: products of bf16 values, P rounded to bf16 for the
  * product with V (its sum is of the unrounded values); fp32: fp32 throughout.
  * A bias of -inf hides a pair, and a row whose pairs are all hidden is one that sees
- * nothing. What lies in a token that no token sees, or in the query of one that sees
+ * nothing; a finite bias below -2^127 counts as -2^127. What lies in a token that no token sees, or in the query of one that sees
  * nothing, may be anything, NaN included. A NaN or infinity elsewhere may make other rows of
  * its example and head non-finite.
  * head_dim <= 128 (else TDA_ERR_UNSUPPORTED); any strides and element alignment; bf16 with

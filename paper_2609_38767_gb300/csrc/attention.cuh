@@ -85,7 +85,7 @@ struct AttentionTile {  // of 128 tokens
 };
 struct AttentionPlan {
     AttentionTile* tiles;  // [N][tiles], where a range is given
-    float* lut;            // [H][lut_len] bias of a distance, where there is any; distance 0 at lut_mid
+    float* lut;            // [H][lut_len] bias of a distance times log2 e, where there is any; distance 0 at lut_mid
     int lut_len, lut_mid;
     int reach;             // distances beyond it have the bias of +-reach
 };

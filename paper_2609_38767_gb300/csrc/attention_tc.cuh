@@ -115,33 +115,44 @@ __device__ __forceinline__ float rcp_fast(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// tanh of two values. |x| <= 1: x P(x^2), P fitted to a relative error of 2^-22.6, seven multiply-adds a pair; any x: 1 - 2 / (1 + e^2x),
-// right at both infinities, 2^-22 absolute, three special functions a value with the exponential of its weight, of which the SM has
-// 32 (exp2) and 16 (reciprocal) a cycle.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c);
 __device__ __forceinline__ float2 mul2(float2 a, float2 b);
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+// tanh of two values. |x| <= 1/2: x P(x^2), P fitted to a relative error of 2^-23.1, six instructions a pair; any x:
+// 1 - 2 / (1 + e^2x), right at both infinities, 2^-22 absolute, two special functions a value beside its weight's exponential, of
+// which the SM has 32 (exp2) and 16 (reciprocal) a cycle.
 __device__ __forceinline__ float2 tanh_near(float2 x) {
     const float2 z = mul2(x, x);
-    float2 p = fma2(z, both(0.0010410186368972063f), both(-0.006203366909176111f));
-    p = fma2(z, p, both(0.020289966836571693f));
-    p = fma2(z, p, both(-0.053457021713256836f));
-    p = fma2(z, p, both(0.13325203955173492f));
-    p = fma2(z, p, both(-0.33332839608192444f));
-    p = fma2(z, p, both(0.9999999403953552f));
+    float2 p = fma2(z, both(0.017135003581643105f), both(-0.05298607423901558f));
+    p = fma2(z, p, both(0.13324779272079468f));
+    p = fma2(z, p, both(-0.3333306908607483f));
+    p = fma2(z, p, both(1.f));
     return mul2(x, p);
 }
 __device__ __forceinline__ float2 tanh_any(float2 x) {
     const float k = 2.f * kLog2e;
     return make_float2(fmaf(-2.f, rcp_fast(1.f + exp2_fast(k * x.x)), 1.f), fmaf(-2.f, rcp_fast(1.f + exp2_fast(k * x.y)), 1.f));
 }
+// The largest of three, in one instruction; a NaN gives way to a number.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+template <int N>
+__device__ __forceinline__ float largest(const float* x, float m) {
+    float u = m, v = m;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) u = max3(u, x[j], x[j + 1]), v = max3(v, x[j + 2], x[j + 3]);
+    return fmaxf(u, v);
+}
 // Whether all of a warp's 32 x N dot products stay within the near range.
 template <int N>
-__device__ __forceinline__ bool all_near(const float* s, float inv_cap) {
-    float m[4] = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ bool all_near(const float* x, float inv_cap) {
+    float u = 0.f, v = 0.f;
 #pragma unroll
-    for (int j = 0; j < N; ++j) m[j & 3] = fmaxf(m[j & 3], fabsf(s[j]));
-    return __all_sync(0xffffffffu, !(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * inv_cap > 1.f));
+    for (int j = 0; j < N; j += 4) u = max3(u, fabsf(x[j]), fabsf(x[j + 1])), v = max3(v, fabsf(x[j + 2]), fabsf(x[j + 3]));
+    return __all_sync(0xffffffffu, !(fmaxf(u, v) * inv_cap > 0.5f));
 }
 // Two bf16 of a column of TMEM, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {

@@ -31,7 +31,7 @@ constexpr int kThreads = 384;  // three warpgroups: 168 registers each at the la
 __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
 __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
 
-// A tile's statistics: -lse (times log2 e where scores are not capped or biased) and -dO.O of 128 queries, as delta_kernel
+// A tile's statistics: -lse times log2 e and -dO.O of 128 queries, as delta_kernel
 // writes them; rows that see nothing have -inf and 0.
 constexpr uint32_t kStatBytes = 2 * kTileT * 4;
 
@@ -208,9 +208,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
                 if constexpr (RICH) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float x = a.cap > 0.f ? capped(p[j + e], a.cap, inv_cap, &bend[e]) : p[j + e] * a.scale;
+                        float x = kLog2e * (a.cap > 0.f ? capped(p[j + e], a.cap, inv_cap, &bend[e]) : p[j + e] * a.scale);
                         if (bias) x += bias[j + e];
-                        q[e] = exp2_fast((x + less[e]) * kLog2e);
+                        q[e] = exp2_fast(x + less[e]);
                     }
                 } else {
                     const float2 c2 = make_float2(c, c);
@@ -489,9 +489,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
 #pragma unroll
                 for (int j = 0; j < 64; ++j) {
                     bend[j] = 1.f;
-                    float x = a.cap > 0.f ? capped(p[j], a.cap, inv_cap, &bend[j]) : p[j] * a.scale;
+                    float x = kLog2e * (a.cap > 0.f ? capped(p[j], a.cap, inv_cap, &bend[j]) : p[j] * a.scale);
                     if (bias) x += bias[-j];
-                    p[j] = exp2_fast((x + nl) * kLog2e);
+                    p[j] = exp2_fast(x + nl);
                 }
             } else {
                 const float2 c2 = make_float2(c, c), l2 = make_float2(nl, nl);
@@ -735,7 +735,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
 }
 
 // stats of a tile of 128 queries of a head, 8 lanes per query: -lse and -dO.O.
-__global__ __launch_bounds__(256) void attention_stats_kernel(const Attention a, int rich, float* stats) {
+__global__ __launch_bounds__(256) void attention_stats_kernel(const Attention a, float* stats) {
     const int T = (int)a.T, tiles = (T + kTileT - 1) / kTileT;
     const int64_t at = (int64_t)blockIdx.x * 32 + threadIdx.x / 8;  // over [N][tiles * 128][H]: a token's heads lie together
     const int64_t total = a.N * tiles * kTileT * a.H;
@@ -763,7 +763,7 @@ __global__ __launch_bounds__(256) void attention_stats_kernel(const Attention a,
     if (sub == 0) {
         const bool none = l == -CUDART_INF_F;
         float* out = stats + (((int64_t)n * a.H + h) * tiles + i / kTileT) * 2 * kTileT + i % kTileT;
-        out[0] = none ? -CUDART_INF_F : rich ? -l : -l * kLog2e;
+        out[0] = none ? -CUDART_INF_F : -l * kLog2e;
         out[kTileT] = none ? 0.f : -v;
     }
 }
@@ -790,7 +790,7 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     float* stats = (float*)((char*)ws + attention_plan_bytes(a, false));
     float* part = a.dtable ? (float*)((char*)stats + up((size_t)a.N * a.H * tiles * kStatBytes)) : nullptr;
     note_launches(1);
-    attention_stats_kernel<<<(unsigned)((a.N * tiles * kTileT * a.H + 31) / 32), 256, 0, s>>>(a, RICH, stats);
+    attention_stats_kernel<<<(unsigned)((a.N * tiles * kTileT * a.H + 31) / 32), 256, 0, s>>>(a, stats);
     if (cudaError_t e = cudaGetLastError()) return e;
     if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.H)), dim3(kThreads),
                                        Q::kSmem, s, q, k, v, g, dq, a, plan, (const float*)stats, part, err))

@@ -183,9 +183,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // TMEM lane of the warp's first row
         const uint32_t ts = tmem + lanes + w * 128, to = tmem + lanes + 256 + w * 128;
         const float* biases = (const float*)(from + S::kBias) + w * 512;
-        const float c = RICH ? kLog2e : a.scale * kLog2e;  // s is x (RICH) or the dot product
+        const float c = RICH ? 1.f : a.scale * kLog2e;  // s is the score times log2 e (RICH) or the dot product
         const float2 c2 = both(c);
-        const float grow = 8.f / c, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        const float grow = 8.f / c, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
         bool ok = true;
         uint32_t turn = 0, outputs = 0;  // key tiles, outputs so far
         ItemReader reader;
@@ -227,12 +227,6 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                     for (int j = 0; j < 32; ++j)
                         if (!(bits >> j & 1)) x[j] = -CUDART_INF_F;
                 };
-                auto largest = [&](const float* x) {
-                    float m[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                    for (int j = 4; j < 32; ++j) m[j & 3] = fmaxf(m[j & 3], x[j]);
-                    most_now = fmaxf(most_now, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-                };
                 if constexpr (RICH) {
                     // scores with cap and bias go back to TMEM, 32 columns at a time
                     const float* bias = nullptr;
@@ -249,36 +243,24 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                         tmem_ld32(ts + 32 * b, s);
                         tmem_wait_ld();
                         tmem_use(s);
-                        if (a.cap > 0.f) {
-                            if (all_near<32>(s, inv_cap)) {
+                        // the bias of 32 distances, nothing where they are all beyond the table's reach but the one of the reach
+                        const float beyond = flat ? *bias : 0.f;
+                        const bool add = bias && !flat;
+                        auto score = [&](auto at_pair) {
 #pragma unroll
-                                for (int j = 0; j < 32; j += 2) {
-                                    const float2 x = mul2(tanh_near(mul2(make_float2(s[j], s[j + 1]), both(inv_cap))), both(a.cap));
-                                    s[j] = x.x, s[j + 1] = x.y;
-                                }
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 32; j += 2) {
-                                    const float2 x = mul2(tanh_any(mul2(make_float2(s[j], s[j + 1]), both(inv_cap))), both(a.cap));
-                                    s[j] = x.x, s[j + 1] = x.y;
-                                }
+                            for (int j = 0; j < 32; j += 2) {
+                                float2 x = both(beyond);
+                                if (add) x = make_float2(bias[-32 * b - j], bias[-32 * b - j - 1]);
+                                x = at_pair(make_float2(s[j], s[j + 1]), x);
+                                s[j] = x.x, s[j + 1] = x.y;
                             }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) s[j] *= a.scale;
-                        }
-                        if (bias) {
-                            if (flat) {
-                                const float x = *bias;
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) s[j] += x;
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) s[j] += bias[-32 * b - j];
-                            }
-                        }
+                        };
+                        if (a.cap <= 0.f) score([&](float2 d, float2 x) { return fma2(d, both(a.scale * kLog2e), x); });
+                        else if (all_near<32>(s, inv_cap))
+                            score([&](float2 d, float2 x) { return fma2(tanh_near(mul2(d, both(inv_cap))), both(cap2), x); });
+                        else score([&](float2 d, float2 x) { return fma2(tanh_any(mul2(d, both(inv_cap))), both(cap2), x); });
                         if (!whole) mask(b, s);
-                        largest(s);
+                        most_now = largest<32>(s, most_now);
                         tmem_st32(ts + 32 * b, (const uint32_t*)s);
                     }
                     tmem_wait_st();
@@ -287,17 +269,26 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                         if (lane == 0) mbar_arrive(smem_u32(&bars.bias_empty[w][turn & 1]));
                     }
                 } else {
+                    if (!whole) {
+                        // masked scores go back to TMEM, 32 columns at a time: fewer instructions than masks for all 128 in place
+#pragma unroll 1
+                        for (int b = 0; b < 4; ++b) {
+                            const int at = k0 + 32 * b;
+                            if (most <= at && least >= at + 32) continue;
+                            tmem_ld32(ts + 32 * b, s);
+                            tmem_wait_ld();
+                            tmem_use(s);
+                            mask(b, s);
+                            tmem_st32(ts + 32 * b, (const uint32_t*)s);
+                        }
+                        tmem_wait_st();
+                    }
 #pragma unroll
                     for (int b = 0; b < 4; ++b) tmem_ld32(ts + 32 * b, s + 32 * b);
                     tmem_wait_ld();
 #pragma unroll
                     for (int b = 0; b < 4; ++b) tmem_use(s + 32 * b);
-                    if (!whole) {
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) mask(b, s + 32 * b);
-                    }
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) largest(s + 32 * b);
+                    most_now = largest<128>(s, most_now);
                 }
                 if (kt == first) {
                     top = most_now;
@@ -325,8 +316,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         float2 v = make_float2(x[2 * j], x[2 * j + 1]);
-                        // the score less the maximum first where a bias may be as large as fp32 goes
-                        v = RICH ? mul2(add2(v, less), c2) : fma2(v, c2, less);
+                        v = RICH ? add2(v, less) : fma2(v, c2, less);
                         v.x = exp2_fast(v.x), v.y = exp2_fast(v.y);
                         part[j & 1] = add2(part[j & 1], v);
                         p[j] = pack_bf16(v.x, v.y);
@@ -419,7 +409,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                 __syncwarp();
                 if (any && lane == 0) mbar_arrive(smem_u32(&bars.o_free[w]));
                 if (a.lse && i < T)
-                    a.lse[((int64_t)n * a.H + h) * T + i] = sum != 0.f ? fmaf(top, RICH ? 1.f : a.scale, logf(sum)) : -CUDART_INF_F;
+                    a.lse[((int64_t)n * a.H + h) * T + i] = sum != 0.f ? fmaf(top, RICH ? kLn2 : a.scale, logf(sum)) : -CUDART_INF_F;
                 // whole rows on the way out
                 constexpr int kLanes = HD / 8;  // of a row
                 const int col = lane % kLanes * 8;
@@ -546,7 +536,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                     }
                     v = mn_major(stage(at_v), kPanel);
                 }
-#pragma unroll 1
+#pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     const uint32_t ts = tmem + w * 128, to = tmem + 256 + w * 128;
                     const int first = w ? now.item.first[1] : now.item.first[0], last = w ? now.item.last[1] : now.item.last[0];
@@ -638,8 +628,9 @@ __global__ __launch_bounds__(256) void attention_plan_kernel(const Attention a, 
         const int64_t at = (int64_t)(blockIdx.x - ranged) * 256 + t;
         if (at < (int64_t)a.H * plan.lut_len) {
             const int h = (int)(at / plan.lut_len);
-            plan.lut[at] = distance_bias(a.bucket, (const __nv_bfloat16*)a.table, a.slope, a.n_buckets, a.reach, a.H, h,
-                                         at % plan.lut_len - plan.lut_mid);
+            const float v = distance_bias(a.bucket, (const __nv_bfloat16*)a.table, a.slope, a.n_buckets, a.reach, a.H, h,
+                                          at % plan.lut_len - plan.lut_mid);
+            plan.lut[at] = kLog2e * (v < -0x1p127f && v > -CUDART_INF_F ? -0x1p127f : v);
         }
         return;
     }
