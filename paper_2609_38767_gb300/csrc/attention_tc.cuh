@@ -230,6 +230,17 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, ok);
 }
 
+// A barrier of `threads` threads; whether none of them brings a failure. All come, whatever went wrong before, so that nobody is
+// left alone at it.
+__device__ __forceinline__ bool all_came_well(int id, int threads, bool ok) {
+    uint32_t bad;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n bar.red.or.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(bad)
+                 : "r"(id), "r"(threads), "r"((uint32_t)!ok)
+                 : "memory");
+    return !bad;
+}
+
 // Waits, up to the time limit, for what is in flight before a CTA may leave.
 __device__ __forceinline__ void wait_settled(uint32_t bar, uint32_t parity, unsigned int* err) {
     const uint64_t since = global_ns();

@@ -2,14 +2,14 @@
 // the scores again, so that every sum has a fixed order.
 //
 // attention_dkv_tc_kernel: a CTA has 128 keys of a key/value head and goes over the query tiles that see them, of every head
-// that shares them. S^T = K Q^T and dP^T = V dO^T are in TMEM with a key per lane; eight warps (a lane and half of the queries
-// per thread) turn S^T into P^T over its own columns, and dP^T into dX^T, both bf16, which are the MMAs' operands from TMEM:
+// that shares them. S^T = K Q^T and dP^T = V dO^T are in TMEM with a key per lane; sixteen warps (a lane and a quarter of the
+// queries per thread) turn S^T into P^T over its own columns, and dP^T into dX^T, both bf16, which are the MMAs' operands from TMEM:
 //   dV += P^T dO,  dK += dX^T Q.
 // attention_dq_tc_kernel: a CTA has 128 queries of a head; S = Q K^T and dP = dO V^T with a query per lane, dX over the columns
 // that S had, dQ += dX K; with a learned bias also the sums of dS along the diagonals.
 // The order of MMAs keeps the tensor pipe busy while the warps work: dV(i) S(i+1) | dK(i) dP(i+1), and S(i+1) dP(i+1) | dQ(i).
 //
-// Warps 0-7: rows; 8: MMAs; 9: TMA; 10 (dQ with a learned bias): sums by bucket. Waits are bounded (about 1 s) and set
+// Warps 0-15: rows; 16: MMAs; 17: TMA; 18: biases by distance; 19 (dQ with a learned bias): sums by bucket. Waits are bounded (about 1 s) and set
 // kErrTimeout on expiry.
 #include <cuda.h>
 #include <math_constants.h>
@@ -26,10 +26,13 @@ namespace {
 
 #include "attention_tc.cuh"
 
-constexpr int kThreads = 384;  // three warpgroups: 168 registers each at the launch, then 224, 224 and 56
+// Five warpgroups: 96 registers a thread at the launch, then 104 for the four that hold rows and 64 for the fifth, 61,440 in all
+// either way. A thread has a row of a pair of tiles and a quarter of the columns: with half of them in half as many warps each warp
+// waited for its own instructions (8 x 1024 tokens XX us, XX this way).
+constexpr int kThreads = 640, kRowWarps = 16;
 
-__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
-__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 224;"); }
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 104;"); }
 
 // A tile's statistics: -lse times log2 e and -dO.O of 128 queries, as delta_kernel
 // writes them; rows that see nothing have -inf and 0.
@@ -42,7 +45,67 @@ struct Tiles {
 };
 
 __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatile int* abort, unsigned int* err) {
-    return __all_sync(0xffffffffu, wait_bounded(smem_u32(bar), parity, abort, err));
+    return wait_warp(smem_u32(bar), parity, abort, err);
+}
+__device__ __forceinline__ void arrive_warp(uint64_t* bar) {
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(bar));
+}
+// D (+)= A B over 128 tokens: A in TMEM, 16 columns of every 32 (the quarters that the row warps write), B as mma_tokens'.
+__device__ __forceinline__ void mma_quarters(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool first) {
+    const uint64_t db = mn_major(b, kPanel);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mma_ts(lead, d, a + 32 * (k / 2) + 8 * (k % 2), db + (k * 2048 >> 4), idesc, !first || k > 0);
+}
+// Bits of a 32 x 32 matrix, a row per lane, to its columns.
+__device__ __forceinline__ uint32_t transpose_bits(uint32_t x) {
+    const int lane = threadIdx.x % 32;
+    uint32_t m = 0x0000ffffu;
+#pragma unroll
+    for (int s = 16; s; s >>= 1, m ^= m << s) {
+        const uint32_t y = __shfl_xor_sync(0xffffffffu, x, s);
+        x = lane & s ? (x & ~m) | (y >> s & m) : (x & m) | (y << s & ~m);
+    }
+    return x;
+}
+// Bits [lo, hi) of a word, the bounds cut to [0, 32].
+__device__ __forceinline__ uint32_t bits_of(int lo, int hi) {
+    lo = min(max(lo, 0), 32), hi = min(max(hi, 0), 32);
+    return lo < hi ? (hi == 32 ? ~0u : (1u << hi) - 1) & (~0u << lo) : 0u;
+}
+// Scores times log2 e of a thread's 32 dot products, and in RICH the cap's slope; bias(j): what the pair j's distance adds.
+template <bool RICH, typename F>
+__device__ __forceinline__ void scores_of(const Attention& a, float inv_cap, float* s, float* bend, F&& bias) {
+    const float2 c2 = both(a.scale * kLog2e), cap2 = both(a.cap * kLog2e);
+    if (RICH && a.cap > 0.f) {
+        auto all = [&](auto tanh_of) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                const float2 t = tanh_of(mul2(make_float2(s[j], s[j + 1]), both(inv_cap)));
+                const float2 x = fma2(t, cap2, make_float2(bias(j), bias(j + 1)));
+                const float2 b = fma2(make_float2(-t.x, -t.y), t, both(1.f));
+                s[j] = x.x, s[j + 1] = x.y, bend[j] = b.x, bend[j + 1] = b.y;
+            }
+        };
+        if (all_near<32>(s, inv_cap)) all([](float2 x) { return tanh_near(x); });
+        else all([](float2 x) { return tanh_any(x); });
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float2 x = fma2(make_float2(s[j], s[j + 1]), c2, make_float2(bias(j), bias(j + 1)));
+            s[j] = x.x, s[j + 1] = x.y;
+        }
+    }
+}
+// The window of 255 biases of a pair of tiles q0 - k0 apart (a warp's work).
+__device__ __forceinline__ void load_window(const AttentionPlan& plan, int h, int apart, float* dst) {
+    const int lane = threadIdx.x % 32;
+    const float* src = plan.lut + (int64_t)h * plan.lut_len + plan.lut_mid + min(max(apart, -plan.reach - 127), plan.reach + 127) - 127;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = src[min(32 * e + lane, 254)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dst[32 * e + lane] = v[e];
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
@@ -72,22 +135,16 @@ __device__ __forceinline__ void stage_columns(uint32_t t, uint32_t tile, int row
     }
 }
 
-// From a dot product to x and to its slope by the dot product's scaled value.
-__device__ __forceinline__ float capped(float dot, float cap, float inv_cap, float* bend) {
-    const float t = tanh_any(both(dot * inv_cap)).x;
-    *bend = fmaf(-t, t, 1.f);
-    return cap * t;
-}
-
 // ------------------------------------------------------------------------------------------------ dK, dV
-template <int HD>
+template <int HD, bool RICH>
 struct DkvShape {
-    static constexpr int kQ = HD == 64 ? 5 : 3, kG = HD == 64 ? 4 : 2;
+    static constexpr int kQ = HD == 64 ? 5 : RICH ? 2 : 3, kG = HD == 64 ? 4 : 2;
     static constexpr uint32_t kStats = (2 + kQ + kG) * Tiles<HD>::kBytes;
-    static constexpr uint32_t kBars = kStats + kG * kStatBytes, kSmem = kBars + 512;
+    static constexpr uint32_t kBias = kStats + kG * kStatBytes;  // RICH: 2 windows of 256 biases
+    static constexpr uint32_t kBars = kBias + (RICH ? 2048 : 0), kSmem = kBars + 512;
 };
 struct DkvBars {
-    uint64_t kv_full, q_full[5], q_empty[5], g_full[4], g_empty[4], s_full, p_ready, dp_full, ds_ready, done;
+    uint64_t kv_full, q_full[5], q_empty[5], g_full[4], g_empty[4], s_full, p_ready, dp_full, ds_ready, bias_full[2], bias_empty[2], done;
     uint32_t tmem;
     int abort, first, last;
 };
@@ -98,7 +155,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
     const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
     const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
     const Attention a, const AttentionPlan plan, const float* stats, unsigned int* err) {
-    using S = DkvShape<HD>;
+    using S = DkvShape<HD, RICH>;
     constexpr uint32_t kBytes = Tiles<HD>::kBytes;
     constexpr int kPanels = Tiles<HD>::kPanels;
     extern __shared__ __align__(1024) uint8_t raw[];
@@ -114,14 +171,15 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
         if (threadIdx.x == 0) atomicOr(err, kErrBadLaunch);
         return;
     }
-    if (warp == 8) {
+    if (warp == kRowWarps) {
         tmem_alloc(smem_u32(&bars.tmem), 512);
         tmem_relinquish();
         if (lane == 0) {
             for (uint64_t* b : {&bars.kv_full, &bars.s_full, &bars.dp_full, &bars.done}) mbar_init(smem_u32(b), 1);
-            for (uint64_t* b : {&bars.p_ready, &bars.ds_ready}) mbar_init(smem_u32(b), 256);
+            for (uint64_t* b : {&bars.p_ready, &bars.ds_ready, &bars.bias_empty[0], &bars.bias_empty[1]}) mbar_init(smem_u32(b), kRowWarps);
+            for (uint64_t* b : {&bars.bias_full[0], &bars.bias_full[1]}) mbar_init(smem_u32(b), 32);
             for (int i = 0; i < S::kQ; ++i) mbar_init(smem_u32(&bars.q_full[i]), 1), mbar_init(smem_u32(&bars.q_empty[i]), 1);
-            for (int i = 0; i < S::kG; ++i) mbar_init(smem_u32(&bars.g_full[i]), 1), mbar_init(smem_u32(&bars.g_empty[i]), 1 + 8);
+            for (int i = 0; i < S::kG; ++i) mbar_init(smem_u32(&bars.g_full[i]), 1), mbar_init(smem_u32(&bars.g_empty[i]), 1 + kRowWarps);
             bars.abort = 0, bars.first = tiles, bars.last = -1;
             fence_mbar_init();
         }
@@ -143,238 +201,227 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
     const int q_first = a.range ? bars.first : a.causal ? kt : 0, q_last = a.range ? bars.last : tiles - 1;
     const int each = q_last - q_first + 1, total = each > 0 ? each * group : 0;
     const uint32_t tS = tmem, tP = tmem + 128, tdV = tmem + 256, tdK = tmem + 256 + HD;
+    // step it: query tile qt of head h
+    struct Step {
+        int it = 0, qt, h;
+    };
+    auto begin = [&]() { return Step{0, q_first, kv * group}; };
+    auto next = [&](Step& x) {
+        ++x.it;
+        if (++x.qt > q_last) x.qt = q_first, ++x.h;
+    };
 
-    if (warp < 8) {
+    if (warp < kRowWarps) {
         take_registers();
-        const int half = warp / 4, row = threadIdx.x % 128, key = k0 + row;
+        const int quarter = warp / 4, row = warp % 4 * 32 + lane, key = k0 + row;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const uint32_t ts = tS + lanes + 64 * half, tp = tP + lanes + 64 * half;
-        const float c = a.scale * kLog2e, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        const uint32_t ts = tS + lanes + 32 * quarter, tp = tP + lanes + 32 * quarter;
+        const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
         bool ok = true;
-        for (int it = 0; it < total; ++it) {
-            const int qt = q_first + it % each, h = kv * group + it / each, q0 = qt * kTileT;
-            const int g = it % S::kG;
-            bool masked;
+        int2 range = make_int2(0, 0);  // what query 32 quarter + lane of the step's tile sees
+        auto look = [&](int qt) {
+            if (a.range) range = visible(a.range, 0, T, (int64_t)n * T, qt * kTileT + 32 * quarter + lane);
+        };
+        if (total) look(q_first);
+        for (Step x = begin(); x.it < total; next(x)) {
+            const int q0 = x.qt * kTileT + 32 * quarter, g = x.it % S::kG;
+            // bit j: query q0 + j sees the key; more: and another one
+            uint32_t seen, more;
             if (a.range) {
-                const AttentionTile& t = plan.tiles[(int64_t)n * tiles + qt];
-                masked = t.most > k0 || t.least < k0 + kTileT;
+                const uint32_t many = __ballot_sync(0xffffffffu, range.y - range.x > 1);
+                const int from = k0 + warp % 4 * 32;
+                seen = transpose_bits(bits_of(range.x - from, range.y - from));
+                more = seen & many;
+                look(x.qt < q_last ? x.qt + 1 : q_first);
             } else {
-                masked = (a.causal && q0 < k0 + kTileT) || k0 + kTileT > T;
+                seen = more = a.causal ? bits_of(key - q0, 32) : ~0u;
+                if (q0 == 0 && (a.causal || T == 1)) more &= ~1u;
             }
-            // bit j: query q0 + 64 half + j sees the key; more: and another one
-            uint32_t seen[2] = {~0u, ~0u}, more[2] = {~0u, ~0u};
-            if (masked) {
-                if (a.range) {
-                    seen[0] = seen[1] = more[0] = more[1] = 0;
-                    for (int j = 0; j < 64; ++j) {
-                        const int2 v = visible(a.range, 0, T, (int64_t)n * T, q0 + 64 * half + j);
-                        const uint32_t in = key >= v.x && key < v.y;
-                        seen[j / 32] |= in << (j % 32);
-                        more[j / 32] |= (in & (uint32_t)(v.y - v.x > 1)) << (j % 32);
-                    }
-                } else if (a.causal) {
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int from = key - (q0 + 64 * half + 32 * w);  // the first query that sees the key
-                        seen[w] = more[w] = from <= 0 ? ~0u : from > 31 ? 0u : ~0u << from;
-                        if (q0 + 64 * half + 32 * w == 0) more[w] &= ~1u;
-                    }
-                } else if (T == 1) {
-                    more[0] = more[1] = 0;
-                }
-            }
-            ok = wait_all(&bars.g_full[g], (it / S::kG) & 1, abort, err) && wait_all(&bars.s_full, it & 1, abort, err);
+            const bool whole = __all_sync(0xffffffffu, more == ~0u);
+            ok = wait_all(&bars.g_full[g], (x.it / S::kG) & 1, abort, err) && wait_all(&bars.s_full, x.it & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
-            const float4* nl = (const float4*)(raw + S::kStats + g * kStatBytes + 256 * half);
-            const float4* nd = (const float4*)(raw + S::kStats + g * kStatBytes + 512 + 256 * half);
-            float p[64];
+            const float4* nl = (const float4*)(raw + S::kStats + g * kStatBytes) + 8 * quarter;
+            const float4* nd = nl + kTileT / 4;
+            float p[32], bend[RICH ? 32 : 1];
             tmem_ld32(ts, p);
-            tmem_ld32(ts + 32, p + 32);
-            tmem_wait_ld();
-            tmem_use(p);
-            tmem_use(p + 32);
-            uint32_t w[32];
             const float* bias = nullptr;
             if (RICH && plan.lut) {
-                const int apart = min(max(q0 - k0, -plan.reach - 127), plan.reach + 127);
-                bias = plan.lut + (int64_t)h * plan.lut_len + plan.lut_mid + apart + 64 * half - row;
+                ok = wait_all(&bars.bias_full[x.it & 1], (x.it / 2) & 1, abort, err);
+                if (!ok) break;
+                bias = (const float*)(raw + S::kBias) + (x.it & 1) * 256 + 127 + 32 * quarter - row;
             }
+            tmem_wait_ld();
+            tmem_use(p);
+            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return ((const float*)nl)[j] + bias[j]; });
+            else scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return ((const float*)nl)[j]; });
 #pragma unroll
-            for (int j = 0; j < 64; j += 4) {
-                const float4 l = nl[j / 4];
-                const float less[4] = {l.x, l.y, l.z, l.w};
-                float q[4], bend[4] = {1.f, 1.f, 1.f, 1.f};
-                if constexpr (RICH) {
+            for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
+            if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float x = kLog2e * (a.cap > 0.f ? capped(p[j + e], a.cap, inv_cap, &bend[e]) : p[j + e] * a.scale);
-                        if (bias) x += bias[j + e];
-                        q[e] = exp2_fast(x + less[e]);
-                    }
-                } else {
-                    const float2 c2 = make_float2(c, c);
-                    const float2 u = fma2(make_float2(p[j], p[j + 1]), c2, make_float2(l.x, l.y));
-                    const float2 v = fma2(make_float2(p[j + 2], p[j + 3]), c2, make_float2(l.z, l.w));
-                    q[0] = exp2_fast(u.x), q[1] = exp2_fast(u.y), q[2] = exp2_fast(v.x), q[3] = exp2_fast(v.y);
-                }
-                if (masked) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!(seen[(j + e) / 32] >> ((j + e) % 32) & 1)) q[e] = 0.f;
-                }
-                w[j / 2] = pack_bf16(q[0], q[1]);
-                w[j / 2 + 1] = pack_bf16(q[2], q[3]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) p[j + e] = RICH ? q[e] * bend[e] : q[e];
+                for (int j = 0; j < 32; ++j)
+                    if (!(seen >> j & 1)) p[j] = 0.f;
             }
-            tmem_st32(ts, w);
+            uint32_t w[16];
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(p[j], p[j + 1]);
+            tmem_st16(ts, w);
+            if (RICH && a.cap > 0.f) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) p[j] *= bend[j];
+            }
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(smem_u32(&bars.p_ready));
-            ok = wait_all(&bars.dp_full, it & 1, abort, err);
+            arrive_warp(&bars.p_ready);
+            if (RICH && bias && lane == 0) mbar_arrive(smem_u32(&bars.bias_empty[x.it & 1]));
+            ok = wait_all(&bars.dp_full, x.it & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
+            float d[32];
+            tmem_ld32(tp, d);
+            tmem_wait_ld();
+            tmem_use(d);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                float d[32];
-                tmem_ld32(tp + 32 * b, d);
-                tmem_wait_ld();
-                tmem_use(d);
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    const float4 l = nd[(32 * b + j) / 4];
-                    float2 u = add2(make_float2(d[j], d[j + 1]), make_float2(l.x, l.y));
-                    float2 v = add2(make_float2(d[j + 2], d[j + 3]), make_float2(l.z, l.w));
-                    u = mul2(u, make_float2(p[32 * b + j], p[32 * b + j + 1]));
-                    v = mul2(v, make_float2(p[32 * b + j + 2], p[32 * b + j + 3]));
-                    if (masked) {
-                        const uint32_t m = more[b] >> j;
-                        if (!(m & 1)) u.x = 0.f;
-                        if (!(m & 2)) u.y = 0.f;
-                        if (!(m & 4)) v.x = 0.f;
-                        if (!(m & 8)) v.y = 0.f;
-                    }
-                    w[(32 * b + j) / 2] = pack_bf16(u.x, u.y);
-                    w[(32 * b + j) / 2 + 1] = pack_bf16(v.x, v.y);
-                }
+            for (int j = 0; j < 32; j += 4) {
+                const float4 l = nd[j / 4];
+                const float2 u = mul2(add2(make_float2(d[j], d[j + 1]), make_float2(l.x, l.y)), make_float2(p[j], p[j + 1]));
+                const float2 v = mul2(add2(make_float2(d[j + 2], d[j + 3]), make_float2(l.z, l.w)), make_float2(p[j + 2], p[j + 3]));
+                d[j] = u.x, d[j + 1] = u.y, d[j + 2] = v.x, d[j + 3] = v.y;
             }
-            tmem_st32(tp, w);
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (!(more >> j & 1)) d[j] = 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+            tmem_st16(tp, w);
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(smem_u32(&bars.ds_ready));
-            __syncwarp();
+            arrive_warp(&bars.ds_ready);
             if (lane == 0) mbar_arrive(smem_u32(&bars.g_empty[g]));
         }
-        // warps 0-3: dV, 4-7: dK, through the shared memory of the first query tiles, which nothing reads any more
+        // warps 0-7: dV, 8-15: dK, half of the columns each, through the shared memory of the first query tiles, which nothing reads
+        // any more
         if (ok) ok = wait_all(&bars.done, 0, abort, err);
         if (ok) {
             tc_fence_after();
-            const uint32_t tile = sq + half * kBytes;
-            const float by = half ? a.scale : 1.f;
-#pragma unroll
-            for (int b = 0; b < HD / 32; ++b) stage_columns((half ? tdK : tdV) + lanes, tile, row, b, by, total > 0);
+            const int second = warp / 8, half = quarter & 1;
+            const uint32_t tile = sq + second * kBytes;
+            const float by = second ? a.scale : 1.f;
+#pragma unroll 1
+            for (int b = 0; b < HD / 64; ++b)
+                stage_columns((second ? tdK : tdV) + lanes, tile, row, half * (HD / 64) + b, by, total > 0);
             fence_proxy_async();
-            if (half) asm volatile("bar.sync 2, 128;" ::: "memory");
-            else asm volatile("bar.sync 1, 128;" ::: "memory");
-            if (warp % 4 == 0 && elect_one()) {
-#pragma unroll
-                for (int p = 0; p < kPanels; ++p)
-                    if (64 * p < a.hd) tma_store_head(half ? &tmdK : &tmdV, tile + p * kPanel, 64 * p, kv, k0, n);
-                asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group 0;" ::: "memory");
-            }
-            __syncwarp();
         }
+        const int second = warp / 8;
+        if (all_came_well(1 + second, 256, ok) && warp % 8 == 0 && elect_one()) {
+#pragma unroll
+            for (int p = 0; p < kPanels; ++p)
+                if (64 * p < a.hd) tma_store_head(second ? &tmdK : &tmdV, sq + second * kBytes + p * kPanel, 64 * p, kv, k0, n);
+            asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group 0;" ::: "memory");
+        }
+        __syncwarp();
         tc_fence_before();
     } else {
         give_registers();
-        if (warp == 9) {
-            if (elect_one()) {
-                bool ok = true;
-                int it = 0;
-                if (total) {
-                    mbar_arrive_tx(smem_u32(&bars.kv_full), 2 * kBytes);
-                    load_tile<HD>(sk, &tmK, kv, k0, n, smem_u32(&bars.kv_full));
-                    load_tile<HD>(sv, &tmV, kv, k0, n, smem_u32(&bars.kv_full));
-                }
-                for (; it < total; ++it) {
-                    const int qt = q_first + it % each, h = kv * group + it / each;
-                    const int q = it % S::kQ, g = it % S::kG;
-                    if (it >= S::kQ && !(ok = wait_bounded(smem_u32(&bars.q_empty[q]), (it / S::kQ - 1) & 1, abort, err))) break;
+        if (warp == kRowWarps + 1) {
+            const uint32_t lead = elect_one();
+            bool ok = true;
+            if (total && lead) {
+                mbar_arrive_tx(smem_u32(&bars.kv_full), 2 * kBytes);
+                load_tile<HD>(sk, &tmK, kv, k0, n, smem_u32(&bars.kv_full));
+                load_tile<HD>(sv, &tmV, kv, k0, n, smem_u32(&bars.kv_full));
+            }
+            int loaded_q = 0, loaded_g = 0;
+            for (Step x = begin(); x.it < total; next(x)) {
+                const int q = x.it % S::kQ, g = x.it % S::kG;
+                if (x.it >= S::kQ) ok = wait_all(&bars.q_empty[q], (x.it / S::kQ - 1) & 1, abort, err);
+                if (!ok) break;
+                if (lead) {
                     mbar_arrive_tx(smem_u32(&bars.q_full[q]), kBytes);
-                    load_tile<HD>(sq + q * kBytes, &tmQ, h, qt * kTileT, n, smem_u32(&bars.q_full[q]));
-                    if (it >= S::kG && !(ok = wait_bounded(smem_u32(&bars.g_empty[g]), (it / S::kG - 1) & 1, abort, err))) {
-                        wait_settled(smem_u32(&bars.q_full[q]), (it / S::kQ) & 1, err);
-                        break;
-                    }
+                    load_tile<HD>(sq + q * kBytes, &tmQ, x.h, x.qt * kTileT, n, smem_u32(&bars.q_full[q]));
+                }
+                ++loaded_q;
+                __syncwarp();
+                if (x.it >= S::kG) ok = wait_all(&bars.g_empty[g], (x.it / S::kG - 1) & 1, abort, err);
+                if (!ok) break;
+                if (lead) {
                     mbar_arrive_tx(smem_u32(&bars.g_full[g]), kBytes + kStatBytes);
-                    load_tile<HD>(sg + g * kBytes, &tmG, h, qt * kTileT, n, smem_u32(&bars.g_full[g]));
-                    bulk_load(base + S::kStats + g * kStatBytes, stats + (((int64_t)n * a.H + h) * tiles + qt) * 2 * kTileT, kStatBytes,
+                    load_tile<HD>(sg + g * kBytes, &tmG, x.h, x.qt * kTileT, n, smem_u32(&bars.g_full[g]));
+                    bulk_load(base + S::kStats + g * kStatBytes, stats + (((int64_t)n * a.H + x.h) * tiles + x.qt) * 2 * kTileT, kStatBytes,
                               smem_u32(&bars.g_full[g]));
                 }
-                if (total) wait_settled(smem_u32(&bars.kv_full), 0, err);
-                for (int s = 0; s < S::kQ; ++s)
-                    if (it > s) wait_settled(smem_u32(&bars.q_full[s]), ((it - 1 - s) / S::kQ) & 1, err);
-                for (int s = 0; s < S::kG; ++s)
-                    if (it > s) wait_settled(smem_u32(&bars.g_full[s]), ((it - 1 - s) / S::kG) & 1, err);
+                ++loaded_g;
+                __syncwarp();
             }
-            __syncwarp();
-        } else if (warp == 8) {
+            if (total) wait_settled(smem_u32(&bars.kv_full), 0, err);
+            for (int s = 0; s < S::kQ; ++s)
+                if (loaded_q > s) wait_settled(smem_u32(&bars.q_full[s]), ((loaded_q - 1 - s) / S::kQ) & 1, err);
+            for (int s = 0; s < S::kG; ++s)
+                if (loaded_g > s) wait_settled(smem_u32(&bars.g_full[s]), ((loaded_g - 1 - s) / S::kG) & 1, err);
+        } else if (warp == kRowWarps) {
             const uint32_t lead = elect_one();
             const int steps = (a.hd + 15) / 16;
             constexpr uint32_t kIdS = idesc_bf16(kTileT, kTileT), kIdO = idesc_bf16(kTileT, HD) | kBMn;
-            bool ok = true;
-            auto tile_of = [&](int it) -> const AttentionTile& { return plan.tiles[(int64_t)n * tiles + q_first + it % each]; };
-            auto clear = [&](uint32_t tile, int it) {
+            bool ok = total == 0 || wait_all(&bars.kv_full, 0, abort, err);
+            // what a token holds that sees nothing may be anything
+            auto clear = [&](uint32_t tile, int qt) {
                 if (!a.range) return;
                 uint32_t bits[4];
-                *(uint4*)bits = *(const uint4*)tile_of(it).idle;
+                *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)n * tiles + qt].idle;
                 if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(tile, kPanels, bits);
             };
-            auto scores = [&](int it) {
-                ok = wait_all(&bars.q_full[it % S::kQ], (it / S::kQ) & 1, abort, err);
-                if (!ok) return;
-                clear(sq + it % S::kQ * kBytes, it);
-                tc_fence_after();
-                mma_heads<HD>(lead, tS, sk, sq + it % S::kQ * kBytes, kIdS, steps);
-                commit(lead, smem_u32(&bars.s_full));
-            };
-            auto gradients = [&](int it) {
-                ok = wait_all(&bars.g_full[it % S::kG], (it / S::kG) & 1, abort, err);
-                if (!ok) return;
-                clear(sg + it % S::kG * kBytes, it);
-                tc_fence_after();
-                mma_heads<HD>(lead, tP, sv, sg + it % S::kG * kBytes, kIdS, steps);
-                commit(lead, smem_u32(&bars.dp_full));
-            };
-            // D += A B, A's halves 64 columns apart
-            auto sums = [&](uint32_t d, uint32_t t, uint32_t b, bool first) {
-                mma_tokens<64>(lead, d, t, b, kIdO, first);
-                mma_tokens<64>(lead, d, t + 64, b + 64 * 128, kIdO, false);
-            };
-            if (total) ok = wait_all(&bars.kv_full, 0, abort, err);
-            if (ok && total) scores(0);
-            if (ok && total) gradients(0);
-            for (int it = 0; ok && it < total; ++it) {
-                ok = wait_all(&bars.p_ready, it & 1, abort, err);
-                if (!ok) break;
-                tc_fence_after();
-                sums(tdV, tS, sg + it % S::kG * kBytes, it == 0);
-                commit(lead, smem_u32(&bars.g_empty[it % S::kG]));
-                if (it + 1 < total) scores(it + 1);
-                ok = ok && wait_all(&bars.ds_ready, it & 1, abort, err);
-                if (!ok) break;
-                tc_fence_after();
-                sums(tdK, tP, sq + it % S::kQ * kBytes, it == 0);
-                commit(lead, smem_u32(&bars.q_empty[it % S::kQ]));
-                if (it + 1 < total) gradients(it + 1);
+            // dV(i), S(i + 1), dK(i), dP(i + 1); i = -1 has only the two
+            Step x = begin();
+            for (int it = -1; ok && it < total && total; ++it) {
+                const bool more = it + 1 < total;
+                if (it >= 0) {
+                    ok = wait_all(&bars.p_ready, it & 1, abort, err);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_quarters(lead, tdV, tS, sg + it % S::kG * kBytes, kIdO, it == 0);
+                    commit(lead, smem_u32(&bars.g_empty[it % S::kG]));
+                }
+                if (more) {
+                    const int s = x.it % S::kQ;
+                    ok = wait_all(&bars.q_full[s], (x.it / S::kQ) & 1, abort, err);
+                    if (!ok) break;
+                    clear(sq + s * kBytes, x.qt);
+                    tc_fence_after();
+                    mma_heads<HD>(lead, tS, sk, sq + s * kBytes, kIdS, steps);
+                    commit(lead, smem_u32(&bars.s_full));
+                }
+                if (it >= 0) {
+                    ok = wait_all(&bars.ds_ready, it & 1, abort, err);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_quarters(lead, tdK, tP, sq + it % S::kQ * kBytes, kIdO, it == 0);
+                    commit(lead, smem_u32(&bars.q_empty[it % S::kQ]));
+                }
+                if (more) {
+                    const int s = x.it % S::kG;
+                    ok = wait_all(&bars.g_full[s], (x.it / S::kG) & 1, abort, err);
+                    if (!ok) break;
+                    clear(sg + s * kBytes, x.qt);
+                    tc_fence_after();
+                    mma_heads<HD>(lead, tP, sv, sg + s * kBytes, kIdS, steps);
+                    commit(lead, smem_u32(&bars.dp_full));
+                    next(x);
+                }
             }
             commit(lead, smem_u32(&bars.done));
             wait_settled(smem_u32(&bars.done), 0, err);
+        } else if (RICH && warp == kRowWarps + 2 && plan.lut) {
+            for (Step x = begin(); x.it < total; next(x)) {
+                if (x.it >= 2 && !wait_all(&bars.bias_empty[x.it & 1], (x.it / 2 - 1) & 1, abort, err)) break;
+                load_window(plan, x.h, x.qt * kTileT - k0, (float*)(raw + S::kBias) + (x.it & 1) * 256);
+                mbar_arrive(smem_u32(&bars.bias_full[x.it & 1]));
+            }
         }
     }
     __syncthreads();
-    if (warp == 8) {
+    if (warp == kRowWarps) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -384,14 +431,16 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
 template <int HD, bool RICH>
 struct DqShape {
     static constexpr int kK = HD == 64 ? 4 : RICH ? 2 : 3, kV = HD == 64 ? 3 : 2;
-    static constexpr uint32_t kDiag = (2 + kK + kV) * Tiles<HD>::kBytes;  // RICH: 2 x [8 warps][96] diagonals, then buckets
-    static constexpr uint32_t kHist = kDiag + (RICH ? 2 * 8 * 96 * 4 : 0), kSmem = kHist + (RICH ? 1024 * 4 : 0) + 1024;
+    static constexpr uint32_t kBias = (2 + kK + kV) * Tiles<HD>::kBytes;  // RICH: 2 windows of 256 biases, 2 x [16 warps][64]
+    static constexpr uint32_t kDiag = kBias + (RICH ? 2048 : 0);          // diagonals, the buckets
+    static constexpr uint32_t kHist = kDiag + (RICH ? 2 * kRowWarps * 64 * 4 : 0), kSmem = kHist + (RICH ? 1024 * 4 : 0) + 1024;
 };
 struct DqBars {
-    uint64_t q_full, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free, ds_ready, diag_full[2], diag_empty[2], done;
+    uint64_t q_full, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free, ds_ready, bias_full[2], bias_empty[2],
+        diag_full[2], diag_empty[2], done;
     uint32_t tmem;
     int abort;
-    float flat[8][2];
+    float flat[kRowWarps][2];
 };
 
 template <int HD, bool RICH>
@@ -402,7 +451,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     using S = DqShape<HD, RICH>;
     constexpr uint32_t kBytes = Tiles<HD>::kBytes;
     constexpr int kPanels = Tiles<HD>::kPanels;
-    extern __shared__ uint8_t raw[];
+    extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ DqBars bars;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t* from = raw + (base - smem_u32(raw));
@@ -413,14 +462,17 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     const int n = (int)(blockIdx.x % heads) / a.H, h = (int)(blockIdx.x % heads) % a.H, kv = h / (a.H / a.KV);
     const int q0 = tile * kTileT;
     volatile int* abort = &bars.abort;
-    if (warp == 8) {
+    if (warp == kRowWarps) {
         tmem_alloc(smem_u32(&bars.tmem), 512);
         tmem_relinquish();
         if (lane == 0) {
             for (uint64_t* b : {&bars.q_full, &bars.s_full[0], &bars.s_full[1], &bars.dp_full, &bars.done, &bars.diag_empty[0],
                                 &bars.diag_empty[1]})
                 mbar_init(smem_u32(b), 1);
-            for (uint64_t* b : {&bars.dp_free, &bars.ds_ready, &bars.diag_full[0], &bars.diag_full[1]}) mbar_init(smem_u32(b), 256);
+            for (uint64_t* b : {&bars.dp_free, &bars.ds_ready, &bars.diag_full[0], &bars.diag_full[1], &bars.bias_empty[0],
+                                &bars.bias_empty[1]})
+                mbar_init(smem_u32(b), kRowWarps);
+            for (uint64_t* b : {&bars.bias_full[0], &bars.bias_full[1]}) mbar_init(smem_u32(b), 32);
             for (int i = 0; i < S::kK; ++i) mbar_init(smem_u32(&bars.k_full[i]), 1), mbar_init(smem_u32(&bars.k_empty[i]), 1);
             for (int i = 0; i < S::kV; ++i) mbar_init(smem_u32(&bars.v_full[i]), 1), mbar_init(smem_u32(&bars.v_empty[i]), 1);
             bars.abort = 0;
@@ -449,126 +501,103 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         return apart - 127 >= a.reach ? 1 : apart + 127 <= -a.reach ? -1 : 0;
     };
 
-    if (warp < 8) {
+    if (warp < kRowWarps) {
         take_registers();
-        const int half = warp / 4, row = threadIdx.x % 128, i = q0 + row;
+        const int quarter = warp / 4, row = warp % 4 * 32 + lane, i = q0 + row;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const float c = a.scale * kLog2e, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
         const int2 see = visible(a.range, a.causal, T, (int64_t)n * T, i);
         const float* st = stats + (((int64_t)n * a.H + h) * tiles + tile) * 2 * kTileT;
-        const float nl = st[row], nd = st[kTileT + row];
+        const float nl = st[row];
+        const float2 nd = both(st[kTileT + row]);
         const bool single = see.y - see.x <= 1;
         float flat[2] = {0.f, 0.f};
         uint32_t diags = 0;
         bool ok = true;
         for (int it = 0; it < total; ++it) {
             const int kt = k_first + it, k0 = kt * kTileT;
-            const uint32_t ts = tmem + (it & 1) * 128 + lanes + 64 * half;
-            const bool masked = most > k0 || least < k0 + kTileT;
-            uint32_t seen[2] = {~0u, ~0u};
-            if (masked) {
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int at = k0 + 64 * half + 32 * w;
-                    const int lo = min(max(see.x - at, 0), 32), hi = min(max(see.y - at, 0), 32);
-                    seen[w] = lo < hi && !single ? (hi == 32 ? ~0u : (1u << hi) - 1) & (~0u << lo) : 0u;
-                }
-            }
+            const uint32_t ts = tmem + (it & 1) * 128 + lanes + 32 * quarter;
+            const bool whole = most <= k0 && least >= k0 + kTileT;
+            const int at = k0 + 32 * quarter;
+            const uint32_t seen = whole ? ~0u : single ? 0u : bits_of(see.x - at, see.y - at);
             ok = wait_all(&bars.s_full[it & 1], (it / 2) & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
-            float p[64], bend[RICH ? 64 : 1];
+            float p[32], bend[RICH ? 32 : 1];
             tmem_ld32(ts, p);
-            tmem_ld32(ts + 32, p + 32);
+            const float* bias = nullptr;
+            if (RICH && plan.lut) {
+                ok = wait_all(&bars.bias_full[it & 1], (it / 2) & 1, abort, err);
+                if (!ok) break;
+                bias = (const float*)(from + S::kBias) + (it & 1) * 256 + 127 + row - 32 * quarter;
+            }
             tmem_wait_ld();
             tmem_use(p);
-            tmem_use(p + 32);
-            if constexpr (RICH) {
-                const int apart = min(max(q0 - k0, -plan.reach - 127), plan.reach + 127);
-                const float* bias = plan.lut ? plan.lut + (int64_t)h * plan.lut_len + plan.lut_mid + apart + row - 64 * half : nullptr;
+            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return nl + bias[-j]; });
+            else scores_of<RICH>(a, inv_cap, p, bend, [&](int) { return nl; });
 #pragma unroll
-                for (int j = 0; j < 64; ++j) {
-                    bend[j] = 1.f;
-                    float x = kLog2e * (a.cap > 0.f ? capped(p[j], a.cap, inv_cap, &bend[j]) : p[j] * a.scale);
-                    if (bias) x += bias[-j];
-                    p[j] = exp2_fast(x + nl);
-                }
-            } else {
-                const float2 c2 = make_float2(c, c), l2 = make_float2(nl, nl);
-#pragma unroll
-                for (int j = 0; j < 64; j += 2) {
-                    const float2 x = fma2(make_float2(p[j], p[j + 1]), c2, l2);
-                    p[j] = exp2_fast(x.x), p[j + 1] = exp2_fast(x.y);
-                }
-            }
+            for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
+            if (RICH && bias) arrive_warp(&bars.bias_empty[it & 1]);
             ok = wait_all(&bars.dp_full, it & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
-            uint32_t w[32];
-            float acc = 0.f, sum = 0.f;
-            const int flat_side = learned ? flat_at(kt) : 0;
-            float* diag = nullptr;
-            if (learned && flat_side == 0) {
-                diag = (float*)(from + S::kDiag) + ((diags & 1) * 8 + warp) * 96;
-                if (diags >= 2) {
-                    ok = wait_all(&bars.diag_empty[diags & 1], (diags / 2 - 1) & 1, abort, err);
-                    if (!ok) break;
-                }
+            float d[32];
+            tmem_ld32(tP + lanes + 32 * quarter, d);
+            tmem_wait_ld();
+            tmem_use(d);
+            tc_fence_before();
+            arrive_warp(&bars.dp_free);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                const float2 x = mul2(add2(make_float2(d[j], d[j + 1]), nd), make_float2(p[j], p[j + 1]));
+                d[j] = x.x, d[j + 1] = x.y;
             }
+            if (!whole) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                float d[32];
-                tmem_ld32(tP + lanes + 64 * half + 32 * b, d);
-                tmem_wait_ld();
-                tmem_use(d);
-                if (b == 1) {
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&bars.dp_free));
-                }
-                const float2 d2 = make_float2(nd, nd);
+                for (int j = 0; j < 32; ++j)
+                    if (!(seen >> j & 1)) d[j] = 0.f;
+            }
+            if constexpr (RICH) {
+                if (learned) {
+                    if (const int side = flat_at(kt)) {
+                        float sum = 0.f;
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    float2 x = mul2(add2(make_float2(d[j], d[j + 1]), d2), make_float2(p[32 * b + j], p[32 * b + j + 1]));
-                    if (masked) {
-                        const uint32_t m = seen[b] >> j;
-                        if (!(m & 1)) x.x = 0.f;
-                        if (!(m & 2)) x.y = 0.f;
-                    }
-                    if constexpr (RICH) {
-                        if (diag) {
-                            // a diagonal's sum moves down the lanes with the columns and leaves at lane 31
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                acc += e ? x.y : x.x;
-                                if (lane == 31) diag[31 - (32 * b + j + e) + 63] = acc;
-                                if (32 * b + j + e < 63) {
-                                    acc = __shfl_up_sync(0xffffffffu, acc, 1);
-                                    if (lane == 0) acc = 0.f;
-                                }
-                            }
-                        } else {
-                            sum += x.x + x.y;
+                        for (int j = 0; j < 32; ++j) sum += d[j];
+                        flat[side > 0] += sum;
+                    } else {
+                        float* diag = (float*)(from + S::kDiag) + ((diags & 1) * kRowWarps + warp) * 64;
+                        if (diags >= 2) {
+                            ok = wait_all(&bars.diag_empty[diags & 1], (diags / 2 - 1) & 1, abort, err);
+                            if (!ok) break;
                         }
-                        // masked pairs stay zero whatever their slope is
-                        x.x = masked && x.x == 0.f ? 0.f : x.x * bend[32 * b + j];
-                        x.y = masked && x.y == 0.f ? 0.f : x.y * bend[32 * b + j + 1];
+                        // a diagonal's sum moves down the lanes with the columns and leaves at lane 31
+                        float acc = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            acc += d[j];
+                            if (lane == 31) diag[62 - j] = acc;  // row - column = 31 - j
+                            if (j < 31) {
+                                acc = __shfl_up_sync(0xffffffffu, acc, 1);
+                                if (lane == 0) acc = 0.f;
+                            }
+                        }
+                        if (lane < 31) diag[lane] = acc;  // lane - 31
+                        arrive_warp(&bars.diag_full[diags & 1]);
+                        ++diags;
                     }
-                    w[(32 * b + j) / 2] = pack_bf16(x.x, x.y);
+                }
+                if (a.cap > 0.f) {  // masked pairs stay zero whatever their slope is
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) d[j] = !whole && !(seen >> j & 1) ? 0.f : d[j] * bend[j];
                 }
             }
-            tmem_st32(ts, w);
+            uint32_t w[16];
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+            tmem_st16(ts, w);
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(smem_u32(&bars.ds_ready));
-            if constexpr (RICH) {
-                if (diag) {
-                    diag[lane] = acc;  // diagonals lane - 63
-                    mbar_arrive(smem_u32(&bars.diag_full[diags & 1]));
-                    ++diags;
-                } else if (flat_side) {
-                    flat[flat_side > 0] += sum;
-                }
-            }
+            arrive_warp(&bars.ds_ready);
         }
         if constexpr (RICH) {
             if (learned) {
@@ -583,96 +612,97 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         if (ok) ok = wait_all(&bars.done, 0, abort, err);
         if (ok) {
             tc_fence_after();
-            // half of the columns each
-#pragma unroll
-            for (int b = 0; b < HD / 64; ++b) stage_columns(tdQ + lanes, sq, row, half * (HD / 64) + b, a.scale, total > 0);
+            // 32 columns each: all quarters, or the first two
+            if (quarter < HD / 32) stage_columns(tdQ + lanes, sq, row, quarter, a.scale, total > 0);
             fence_proxy_async();
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (warp == 0 && elect_one()) {
-#pragma unroll
-                for (int p = 0; p < kPanels; ++p)
-                    if (64 * p < a.hd) tma_store_head(&tmdQ, sq + p * kPanel, 64 * p, h, q0, n);
-                asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group 0;" ::: "memory");
-            }
-            __syncwarp();
         }
+        if (all_came_well(1, 32 * kRowWarps, ok) && warp == 0 && elect_one()) {
+#pragma unroll
+            for (int p = 0; p < kPanels; ++p)
+                if (64 * p < a.hd) tma_store_head(&tmdQ, sq + p * kPanel, 64 * p, h, q0, n);
+            asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group 0;" ::: "memory");
+        }
+        __syncwarp();
         tc_fence_before();
     } else {
         give_registers();
-        if (warp == 9) {
-            if (elect_one()) {
-                int it = 0, loaded_v = 0;
-                if (total) {
-                    mbar_arrive_tx(smem_u32(&bars.q_full), 2 * kBytes);
-                    load_tile<HD>(sq, &tmQ, h, q0, n, smem_u32(&bars.q_full));
-                    load_tile<HD>(sg, &tmG, h, q0, n, smem_u32(&bars.q_full));
-                }
-                for (; it < total; ++it) {
-                    const int k = it % S::kK, v = it % S::kV, k0 = (k_first + it) * kTileT;
-                    if (it >= S::kK && !wait_bounded(smem_u32(&bars.k_empty[k]), (it / S::kK - 1) & 1, abort, err)) break;
+        if (warp == kRowWarps + 1) {
+            const uint32_t lead = elect_one();
+            bool ok = true;
+            if (total && lead) {
+                mbar_arrive_tx(smem_u32(&bars.q_full), 2 * kBytes);
+                load_tile<HD>(sq, &tmQ, h, q0, n, smem_u32(&bars.q_full));
+                load_tile<HD>(sg, &tmG, h, q0, n, smem_u32(&bars.q_full));
+            }
+            int loaded_k = 0, loaded_v = 0;
+            for (int it = 0; it < total; ++it) {
+                const int k = it % S::kK, v = it % S::kV, k0 = (k_first + it) * kTileT;
+                if (it >= S::kK) ok = wait_all(&bars.k_empty[k], (it / S::kK - 1) & 1, abort, err);
+                if (!ok) break;
+                if (lead) {
                     mbar_arrive_tx(smem_u32(&bars.k_full[k]), kBytes);
                     load_tile<HD>(sk + k * kBytes, &tmK, kv, k0, n, smem_u32(&bars.k_full[k]));
-                    if (it >= S::kV && !wait_bounded(smem_u32(&bars.v_empty[v]), (it / S::kV - 1) & 1, abort, err)) {
-                        ++it;
-                        break;
-                    }
+                }
+                ++loaded_k;
+                __syncwarp();
+                if (it >= S::kV) ok = wait_all(&bars.v_empty[v], (it / S::kV - 1) & 1, abort, err);
+                if (!ok) break;
+                if (lead) {
                     mbar_arrive_tx(smem_u32(&bars.v_full[v]), kBytes);
                     load_tile<HD>(sv + v * kBytes, &tmV, kv, k0, n, smem_u32(&bars.v_full[v]));
-                    ++loaded_v;
                 }
-                if (total) wait_settled(smem_u32(&bars.q_full), 0, err);
-                for (int s = 0; s < S::kK; ++s)
-                    if (it > s) wait_settled(smem_u32(&bars.k_full[s]), ((it - 1 - s) / S::kK) & 1, err);
-                for (int s = 0; s < S::kV; ++s)
-                    if (loaded_v > s) wait_settled(smem_u32(&bars.v_full[s]), ((loaded_v - 1 - s) / S::kV) & 1, err);
+                ++loaded_v;
+                __syncwarp();
             }
-            __syncwarp();
-        } else if (warp == 8) {
+            if (total) wait_settled(smem_u32(&bars.q_full), 0, err);
+            for (int s = 0; s < S::kK; ++s)
+                if (loaded_k > s) wait_settled(smem_u32(&bars.k_full[s]), ((loaded_k - 1 - s) / S::kK) & 1, err);
+            for (int s = 0; s < S::kV; ++s)
+                if (loaded_v > s) wait_settled(smem_u32(&bars.v_full[s]), ((loaded_v - 1 - s) / S::kV) & 1, err);
+        } else if (warp == kRowWarps) {
             const uint32_t lead = elect_one();
             const int steps = (a.hd + 15) / 16;
             constexpr uint32_t kIdS = idesc_bf16(kTileT, kTileT), kIdO = idesc_bf16(kTileT, HD) | kBMn;
-            bool ok = true;
-            auto scores = [&](int it) {
-                const uint32_t tile_k = sk + it % S::kK * kBytes;
-                ok = wait_all(&bars.k_full[it % S::kK], (it / S::kK) & 1, abort, err);
-                if (!ok) return;
-                if (a.range) {
-                    uint32_t bits[4];
-                    *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)n * tiles + k_first + it].unseen;
-                    if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(tile_k, kPanels, bits);
+            bool ok = total == 0 || wait_all(&bars.q_full, 0, abort, err);
+            // S(i + 1), dP(i + 1), dQ(i); i = -1 has only the two
+            for (int it = -1; ok && it < total && total; ++it) {
+                const int then = it + 1;
+                if (then < total) {
+                    const uint32_t tile_k = sk + then % S::kK * kBytes;
+                    ok = wait_all(&bars.k_full[then % S::kK], (then / S::kK) & 1, abort, err);
+                    if (!ok) break;
+                    if (a.range) {
+                        uint32_t bits[4];
+                        *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)n * tiles + k_first + then].unseen;
+                        if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(tile_k, kPanels, bits);
+                    }
+                    tc_fence_after();
+                    mma_heads<HD>(lead, tmem + (then & 1) * 128, sq, tile_k, kIdS, steps);
+                    commit(lead, smem_u32(&bars.s_full[then & 1]));
+                    if (it >= 0) ok = wait_all(&bars.dp_free, it & 1, abort, err);
+                    ok = ok && wait_all(&bars.v_full[then % S::kV], (then / S::kV) & 1, abort, err);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_heads<HD>(lead, tP, sg, sv + then % S::kV * kBytes, kIdS, steps);
+                    commit(lead, smem_u32(&bars.dp_full));
+                    commit(lead, smem_u32(&bars.v_empty[then % S::kV]));
                 }
-                tc_fence_after();
-                mma_heads<HD>(lead, tmem + (it & 1) * 128, sq, tile_k, kIdS, steps);
-                commit(lead, smem_u32(&bars.s_full[it & 1]));
-            };
-            auto gradients = [&](int it) {
-                ok = wait_all(&bars.v_full[it % S::kV], (it / S::kV) & 1, abort, err);
-                if (!ok) return;
-                tc_fence_after();
-                mma_heads<HD>(lead, tP, sg, sv + it % S::kV * kBytes, kIdS, steps);
-                commit(lead, smem_u32(&bars.dp_full));
-                commit(lead, smem_u32(&bars.v_empty[it % S::kV]));
-            };
-            if (total) ok = wait_all(&bars.q_full, 0, abort, err);
-            if (ok && total) scores(0);
-            if (ok && total) gradients(0);
-            for (int it = 0; ok && it < total; ++it) {
-                if (it + 1 < total) {
-                    scores(it + 1);
-                    ok = ok && wait_all(&bars.dp_free, it & 1, abort, err);
-                    if (ok) gradients(it + 1);
-                }
-                ok = ok && wait_all(&bars.ds_ready, it & 1, abort, err);
+                if (it < 0) continue;
+                ok = wait_all(&bars.ds_ready, it & 1, abort, err);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t t = tmem + (it & 1) * 128, tile_k = sk + it % S::kK * kBytes;
-                mma_tokens<64>(lead, tdQ, t, tile_k, kIdO, it == 0);
-                mma_tokens<64>(lead, tdQ, t + 64, tile_k + 64 * 128, kIdO, false);
+                mma_quarters(lead, tdQ, tmem + (it & 1) * 128, sk + it % S::kK * kBytes, kIdO, it == 0);
                 commit(lead, smem_u32(&bars.k_empty[it % S::kK]));
             }
             commit(lead, smem_u32(&bars.done));
             wait_settled(smem_u32(&bars.done), 0, err);
-        } else if (RICH && warp == 10 && learned) {
+        } else if (RICH && warp == kRowWarps + 2) {
+            for (int it = 0; plan.lut && it < total; ++it) {
+                if (it >= 2 && !wait_all(&bars.bias_empty[it & 1], (it / 2 - 1) & 1, abort, err)) break;
+                load_window(plan, h, q0 - (k_first + it) * kTileT, (float*)(from + S::kBias) + (it & 1) * 256);
+                mbar_arrive(smem_u32(&bars.bias_full[it & 1]));
+            }
+        } else if (RICH && learned) {
             // sums of the diagonals of each pair of tiles by bucket, in the order of the tiles
             float* hist = (float*)(from + S::kHist);
             for (int b = lane; b < a.n_buckets; b += 32) hist[b] = 0.f;
@@ -682,16 +712,17 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 const int kt = k_first + it;
                 if (flat_at(kt)) continue;
                 if (!wait_all(&bars.diag_full[diags & 1], (diags / 2) & 1, abort, err)) break;
-                const float* diag = (const float*)(from + S::kDiag) + (diags & 1) * 8 * 96;
+                const float* diag = (const float*)(from + S::kDiag) + (diags & 1) * kRowWarps * 64;
+#pragma unroll 1
                 for (int x = 0; x < 8; ++x) {
                     const int d = 32 * x + lane - 127;  // of the pair of tiles
                     float v = 0.f;
                     int id = -1;
                     if (d <= 127) {
-#pragma unroll
-                        for (int w = 0; w < 8; ++w) {
-                            const int own = d - 32 * (w % 4) + 64 * (w / 4);
-                            if (own >= -63 && own <= 31) v += diag[w * 96 + own + 63];
+#pragma unroll 4
+                        for (int w = 0; w < kRowWarps; ++w) {
+                            const int own = d - 32 * (w % 4) + 32 * (w / 4);
+                            if (own >= -31 && own <= 31) v += diag[w * 64 + own + 31];
                         }
                         const int64_t far = min(max((int64_t)q0 - (int64_t)kt * kTileT + d, -a.reach), a.reach);
                         id = a.bucket[far + a.reach];
@@ -708,22 +739,21 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                         left &= ~__ballot_sync(0xffffffffu, in);
                     }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars.diag_empty[diags & 1]));
+                arrive_warp(&bars.diag_empty[diags & 1]);
                 ++diags;
             }
         }
     }
     __syncthreads();
-    if (warp == 8) {
+    if (warp == kRowWarps) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
-    } else if (RICH && warp == 10 && learned) {
+    } else if (RICH && warp == kRowWarps + 3 && learned) {
         float* hist = (float*)(from + S::kHist);
         if (lane == 0) {
             for (int e = 0; e < 2; ++e) {
                 float s = 0.f;
-                for (int w = 0; w < 8; ++w) s += bars.flat[w][e];
+                for (int w = 0; w < kRowWarps; ++w) s += bars.flat[w][e];
                 const int id = a.bucket[e ? 2 * a.reach : 0];
                 if (id >= 0 && id < a.n_buckets) hist[id] += s;
             }
@@ -772,7 +802,7 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 template <int HD, bool RICH>
 cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s) {
-    using Kv = DkvShape<HD>;
+    using Kv = DkvShape<HD, RICH>;
     using Q = DqShape<HD, RICH>;
     if (cudaError_t e = smem_attr_once<attention_dkv_tc_kernel<HD, RICH>>(Kv::kSmem)) return e;
     if (cudaError_t e = smem_attr_once<attention_dq_tc_kernel<HD, RICH>>(Q::kSmem)) return e;
