@@ -85,10 +85,22 @@ struct AttentionTile {  // of 128 tokens
 };
 struct AttentionPlan {
     AttentionTile* tiles;  // [N][tiles], where a range is given
+    int* taken;            // the same: items of the forward pass that CTAs have taken
     float* lut;            // [H][lut_len] bias of a distance times log2 e, where there is any; distance 0 at lut_mid
     int lut_len, lut_mid;
     int reach;             // distances beyond it have the bias of +-reach
 };
+
+// The tensor-core kernels sum dS by distance where the distances within the table's reach fit 1024 values (distance 0 at the
+// returned place), else by bucket (-1).
+__host__ __device__ inline int attention_dense_mid(const Attention& a) {
+    const int64_t reach = a.reach < a.T - 1 ? a.reach : a.T - 1;
+    return 2 * reach + 1 <= 1024 ? (int)reach : -1;
+}
+inline int attention_part_width(const Attention& a) {
+    const int mid = attention_dense_mid(a);
+    return a.n_buckets == 0 ? 0 : mid >= 0 ? 2 * mid + 1 : a.n_buckets;
+}
 
 // Workspace of a call, and its launches; bound: enough for any range, slope and alignment. The CUDA-core kernels
 // (k_attention.cu) take every shape; the tensor-core ones (k_attention_tc.cu, k_attention_grad_tc.cu) bf16 with aligned rows.
@@ -104,7 +116,7 @@ size_t attention_plan_bytes(const Attention& a, bool bound);
 cudaError_t launch_attention_plan(const Attention& a, void* ws, AttentionPlan* plan, bool* chained, cudaStream_t s);
 bool attention_head_map(void* map, const void* p, int64_t ld, int heads, int hd, int64_t T, int64_t N, int rows);
 cudaError_t launch_attention_forward_tc(const Attention& a, void* ws, unsigned int* err, cudaStream_t s);
-// *part: [H][N * tiles][n_buckets] sums of dS, where a.dtable is wanted.
+// *part: [H][N * tiles][attention_part_width] sums of dS, where a.dtable is wanted.
 size_t attention_grad_tc_bytes(const Attention& a, bool bound);
 cudaError_t launch_attention_backward_tc(const Attention& a, void* ws, unsigned int* err, float** part, cudaStream_t s);
 

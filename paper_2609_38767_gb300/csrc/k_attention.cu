@@ -436,6 +436,41 @@ __global__ __launch_bounds__(256) void attention_dtable_kernel(const float* part
     if (lane == 0) out[at] = narrow<T>((float)(beta != 0.f ? beta * (double)wide(out[at]) + v : v));
 }
 
+// The same from sums by distance, width = 2 mid + 1 of them: a CTA per head adds up each distance over its rows, then each bucket over
+// its distances, both in order.
+template <typename T>
+__global__ __launch_bounds__(1024) void attention_distances_kernel(const float* part, int64_t rows, int mid, const int32_t* bucket,
+                                                                  int64_t reach, int n_buckets, int H, float beta, T* out) {
+    chain_wait();
+    __shared__ double sums[1024];
+    __shared__ int ids[1024];
+    const int h = blockIdx.x, t = threadIdx.x, width = 2 * mid + 1;
+    // threads in groups of `width` rounded up to warps, each group every `groups`-th row
+    const int span = (width + 31) / 32 * 32, groups = max(1, 1024 / span), g = t / span, d = t % span;
+    double v = 0;
+    if (g < groups && d < width)
+        for (int64_t i = g; i < rows; i += groups) v += part[(h * rows + i) * width + d];
+    sums[t] = v;
+    if (t < width) ids[t] = bucket[t - mid + reach];
+    __syncthreads();
+    if (t < width) {
+        for (int k = 1; k < groups; ++k) v += sums[k * span + t];
+        sums[t] = v;  // other groups' places are past the first
+    }
+    __syncthreads();
+    for (int b = t / 32; b < n_buckets; b += 32) {
+        double s = 0;
+        for (int i = t % 32; i < width; i += 32)
+            if (ids[i] == b) s += sums[i];
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (t % 32 == 0) {
+            T& x = out[(int64_t)b * H + h];
+            x = narrow<T>((float)(beta != 0.f ? beta * (double)wide(x) + s : s));
+        }
+    }
+}
+
 // ------------------------------------------------------------------ ranges
 constexpr int kScan = 1024, kEach = 8;
 
@@ -608,7 +643,13 @@ cudaError_t launch_attention_backward(const Attention& a, void* ws, unsigned int
     if (attention_tc_supported(a, true)) {
         float* part;
         if (cudaError_t e = launch_attention_backward_tc(a, ws, err, &part, s)) return e;
-        return join_table(a, part, a.N * ((a.T + 127) / 128), s);
+        const int64_t rows = a.N * ((a.T + 127) / 128);
+        const int mid = attention_dense_mid(a);
+        if (!a.dtable || mid < 0) return join_table(a, part, rows, s);
+        return a.gt == TDA_BF16 ? launch_chained(true, attention_distances_kernel<__nv_bfloat16>, dim3(a.H), dim3(1024), 0, s, (const float*)part,
+                                                 rows, mid, a.bucket, a.reach, a.n_buckets, a.H, a.beta, (__nv_bfloat16*)a.dtable)
+                                : launch_chained(true, attention_distances_kernel<float>, dim3(a.H), dim3(1024), 0, s, (const float*)part, rows,
+                                                 mid, a.bucket, a.reach, a.n_buckets, a.H, a.beta, (float*)a.dtable);
     }
     float* delta = (float*)ws;
     float* part = (float*)((char*)ws + up((size_t)a.N * a.T * a.H * 4));

@@ -495,6 +495,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     const int total = k_last >= k_first ? k_last - k_first + 1 : 0;
     const uint32_t tP = tmem + 256, tdQ = tmem + 384;
     const bool learned = RICH && part != nullptr;
+    const int dense_mid = attention_dense_mid(a);  // where the sums are by distance, the place of distance 0
+    const bool dense = dense_mid >= 0;
     // every distance of the pair of tiles is beyond the table's reach
     auto flat_at = [&](int kt) {
         const int64_t apart = (int64_t)q0 - (int64_t)kt * kTileT;
@@ -703,9 +705,10 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 mbar_arrive(smem_u32(&bars.bias_full[it & 1]));
             }
         } else if (RICH && learned) {
-            // sums of the diagonals of each pair of tiles by bucket, in the order of the tiles
+            // sums of the diagonals of each pair of tiles, in the order of the tiles: by distance where there is room for all of them,
+            // else by bucket
             float* hist = (float*)(from + S::kHist);
-            for (int b = lane; b < a.n_buckets; b += 32) hist[b] = 0.f;
+            for (int b = lane; b < 1024; b += 32) hist[b] = 0.f;
             __syncwarp();
             uint32_t diags = 0;
             for (int it = 0; it < total; ++it) {
@@ -725,8 +728,27 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                             if (own >= -31 && own <= 31) v += diag[w * 64 + own + 31];
                         }
                         const int64_t far = min(max((int64_t)q0 - (int64_t)kt * kTileT + d, -a.reach), a.reach);
-                        id = a.bucket[far + a.reach];
-                        if (id >= a.n_buckets) id = -1;
+                        if (dense) {
+                            // held within the table's reach the farther ones meet: one lane has them all
+                            const int64_t apart = (int64_t)q0 - (int64_t)kt * kTileT + d;
+                            if (apart > -a.reach && apart < a.reach) hist[far + dense_mid] += v, v = 0.f;
+                        } else {
+                            id = a.bucket[far + a.reach];
+                            if (id >= a.n_buckets) id = -1;
+                        }
+                    }
+                    if (dense) {
+                        const int64_t apart = (int64_t)q0 - (int64_t)kt * kTileT + d;
+                        float ends[2] = {apart <= -a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
+                        if (__any_sync(0xffffffffu, ends[0] != 0.f || ends[1] != 0.f)) {
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                                for (int o = 16; o; o >>= 1) ends[e] += __shfl_xor_sync(0xffffffffu, ends[e], o);
+                                if (lane == 0) hist[e ? dense_mid + (int)min(a.reach, (int64_t)T - 1) : 0] += ends[e];
+                            }
+                        }
+                        __syncwarp();
                     }
                     uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
                     while (left) {
@@ -754,13 +776,14 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             for (int e = 0; e < 2; ++e) {
                 float s = 0.f;
                 for (int w = 0; w < kRowWarps; ++w) s += bars.flat[w][e];
-                const int id = a.bucket[e ? 2 * a.reach : 0];
-                if (id >= 0 && id < a.n_buckets) hist[id] += s;
+                const int id = dense ? (e ? 2 * dense_mid : 0) : a.bucket[e ? 2 * a.reach : 0];
+                if (dense || (id >= 0 && id < a.n_buckets)) hist[id] += s;
             }
         }
         __syncwarp();
-        float* mine = part + ((int64_t)h * a.N * tiles + (int64_t)n * tiles + tile) * a.n_buckets;
-        for (int b = lane; b < a.n_buckets; b += 32) mine[b] = hist[b];
+        const int width = dense ? 2 * dense_mid + 1 : a.n_buckets;
+        float* mine = part + ((int64_t)h * a.N * tiles + (int64_t)n * tiles + tile) * width;
+        for (int b = lane; b < width; b += 32) mine[b] = hist[b];
     }
 }
 
@@ -834,7 +857,7 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
 size_t attention_grad_tc_bytes(const Attention& a, bool bound) {
     const int64_t tiles = (a.T + kTileT - 1) / kTileT;
     return attention_plan_bytes(a, bound) + up((size_t)a.N * a.H * tiles * kStatBytes) +
-           (a.dtable || bound ? up((size_t)a.N * a.H * tiles * a.n_buckets * 4) : 0);
+           (a.dtable || bound ? up((size_t)a.N * a.H * tiles * attention_part_width(a) * 4) : 0);
 }
 
 cudaError_t launch_attention_backward_tc(const Attention& a, void* ws, unsigned int* err, float** part, cudaStream_t s) {

@@ -9,9 +9,9 @@
 // O is rescaled only where a row's maximum has grown by more than 2^8 since the last time; P stays below 2^8 then, which
 // costs bf16 nothing, and sums are fp32.
 //
-// Warps 0-3 and 4-7: rows of the tiles (a row per thread); 8: the MMAs (a warp per tile was slower, the two streams share the
-// pipe so that both end late: 8192 tokens 428 us, 344 with one); 9: keys and values; 10: items and queries; 11: biases by distance;
-// 12-15: outputs of finished tiles. Waits are bounded
+// Warps 0-3 and 4-7: rows of the tiles (a row per thread; of capped or biased scores half a row, 16 warps); then one each for the
+// MMAs (a warp per tile was slower, the two streams share the pipe so that both end late: 8192 tokens 428 us, 344 with one), keys and
+// values, items and queries, biases by distance; four for the outputs of finished tiles. Waits are bounded
 // (about 1 s) and set kErrTimeout on expiry.
 #include <cuda.h>
 #include <math_constants.h>
@@ -29,9 +29,23 @@ namespace {
 
 #include "attention_tc.cuh"
 
-// Four warpgroups, whose registers are shared out anew: 128 a thread at the launch, then 184 for the two that hold rows of
-// scores and 72 for the one that loads and issues and the one that writes outputs, 65,536 in all either way.
-constexpr int kThreads = 512;
+// Registers are shared out anew after the launch, by warpgroup: of 128 a thread 184 for the two that hold rows of scores and 72 for
+// the one that loads and issues and the one that writes outputs, 65,536 in all either way. Scores with cap or bias (RICH) take
+// four times the instructions, and one warp a scheduler and tile waits for its own; there a row's keys are halved over two warps:
+// of 80 a thread 88 for four warpgroups and 64 for two, 61,440 (packed documents XX us with two).
+template <bool RICH>
+struct Warps {
+    static constexpr int kRows = RICH ? 16 : 8, kMma = kRows, kLoad = kRows + 1, kItems = kRows + 2, kBias = kRows + 3,
+                         kOut = kRows + 4, kThreads = 32 * (kRows + 8), kCols = RICH ? 64 : 128;
+    __device__ static __forceinline__ void row_registers() {
+        if constexpr (RICH) asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    }
+    __device__ static __forceinline__ void other_registers() {
+        if constexpr (RICH) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    }
+};
 
 template <int HD, bool RICH>
 struct Shape {
@@ -40,15 +54,17 @@ struct Shape {
     static constexpr int kStages = HD == 64 ? 6 : RICH ? 3 : 4;
     static constexpr uint32_t kOut = (2 + kStages) * kTileBytes;  // 32 rows of output for each of 4 warps
     static constexpr uint32_t kBias = kOut + 4 * 32 * HD * 2;     // RICH: 2 x 2 windows of 256 biases
-    static constexpr uint32_t kSmem = kBias + (RICH ? 4 * 1024 : 0);
+    static constexpr uint32_t kSwap = kBias + (RICH ? 4096 : 0);  // RICH: 16 warps' maxima, at two places in turn
+    static constexpr uint32_t kSmem = kSwap + (RICH ? 16 * 256 : 0);
 };
 
-struct Bars {
+template <bool RICH>
+struct BarsOf {
     uint64_t q_full[2], q_empty[2], s_full[2], p_ready[2][2], o_done[2], o_free[2], sum_full[2], done;
     uint64_t item_full[4], item_empty[4], full[8], empty[8], bias_full[2][2], bias_empty[2][2];
     uint32_t tmem;
     int abort;
-    float2 sums[2][kTileT];  // maximum and sum of a finished row
+    float2 sums[2][RICH ? 2 : 1][kTileT];  // maximum and sum of a finished row
     int4 items[4][2];
 };
 
@@ -71,7 +87,7 @@ __device__ __forceinline__ Hull hull_of(const Attention& a, const AttentionPlan&
 }
 
 // The items (pairs of query tiles of a head) of this CTA, long ones first where the mask is causal; every other round
-// backwards, which evens out what the rounds leave.
+// backwards, which evens out what the rounds leave. With ranges CTAs take items as they are done (packed documents XX us, XX so).
 struct Items {
     int total, pairs, tiles;
     FastDiv heads, H, group;  // N H, H, H / KV
@@ -93,6 +109,7 @@ struct Item {
 struct ItemReader {
     uint32_t r = 0;
     // The next item; false after the last one, or where a wait ran out (*ok). Called by whole warps.
+    template <typename Bars>
     __device__ __forceinline__ bool next(Item& x, Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
         const uint32_t bar = smem_u32(&bars.item_full[r % 4]), parity = (r / 4) & 1;
         *ok = *ok && wait_warp(bar, parity, abort, err);
@@ -114,6 +131,7 @@ struct Walk {
     bool valid = true;
     ItemReader reader;
     __device__ __forceinline__ void clear() { kt = last = 0; }  // next() then gives the first
+    template <typename Bars>
     __device__ __forceinline__ void next(Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
         if (!valid) return;
         if (kt < last) {
@@ -128,13 +146,14 @@ struct Walk {
 };
 
 template <int HD, bool RICH>
-__global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
+__global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                                                                    const __grid_constant__ CUtensorMap tmK,
                                                                    const __grid_constant__ CUtensorMap tmV, const Attention a,
                                                                    const AttentionPlan plan, const Items items, unsigned int* err) {
     using S = Shape<HD, RICH>;
+    using W = Warps<RICH>;
     extern __shared__ __align__(1024) uint8_t raw[];
-    __shared__ Bars bars;
+    __shared__ BarsOf<RICH> bars;
     const uint32_t base = smem_u32(raw);
     uint8_t* from = raw;
     if (base & 1023u) {  // the tiles' swizzle needs it
@@ -146,7 +165,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
     const int T = (int)a.T;
     volatile int* abort = &bars.abort;
 
-    if (warp == 8) {
+    if (warp == W::kMma) {
         tmem_alloc(smem_u32(&bars.tmem), 512);
         tmem_relinquish();
         if (lane == 0) {
@@ -157,15 +176,15 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                 mbar_init(smem_u32(&bars.p_ready[w][0]), 4);
                 mbar_init(smem_u32(&bars.p_ready[w][1]), 4);
                 mbar_init(smem_u32(&bars.o_free[w]), 4);
-                mbar_init(smem_u32(&bars.sum_full[w]), 4);
+                mbar_init(smem_u32(&bars.sum_full[w]), W::kRows / 2);
                 mbar_init(smem_u32(&bars.o_done[w]), 1);
             }
             mbar_init(smem_u32(&bars.done), 1);
             for (int s = 0; s < S::kStages; ++s) mbar_init(smem_u32(&bars.full[s]), 1), mbar_init(smem_u32(&bars.empty[s]), 1);
             for (int r = 0; r < 4; ++r)  // read by the warps of rows and outputs, by the MMAs', the loads' and the biases'
-                mbar_init(smem_u32(&bars.item_full[r]), 1), mbar_init(smem_u32(&bars.item_empty[r]), 14 + (RICH && plan.lut));
+                mbar_init(smem_u32(&bars.item_full[r]), 1), mbar_init(smem_u32(&bars.item_empty[r]), W::kRows + 6 + (RICH && plan.lut));
             for (int w = 0; w < 2; ++w)
-                for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&bars.bias_full[w][b]), 32), mbar_init(smem_u32(&bars.bias_empty[w][b]), 4);
+                for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&bars.bias_full[w][b]), 32), mbar_init(smem_u32(&bars.bias_empty[w][b]), W::kRows / 2);
             bars.abort = 0;
             fence_mbar_init();
         }
@@ -177,16 +196,25 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
     tc_fence_after();
     const uint32_t tmem = bars.tmem;
 
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-        const int w = warp / 4, row = threadIdx.x % 128;
+    if (warp < W::kRows) {
+        W::row_registers();
+        // tile w; RICH: columns 64 half + [0, 64) of its scores
+        const int w = warp / (W::kRows / 2), half = RICH ? warp / 4 % 2 : 0, row = warp % 4 * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // TMEM lane of the warp's first row
-        const uint32_t ts = tmem + lanes + w * 128, to = tmem + lanes + 256 + w * 128;
+        const uint32_t ts = tmem + lanes + w * 128, to = tmem + lanes + 256 + w * 128 + half * (HD / 2);
         const float* biases = (const float*)(from + S::kBias) + w * 512;
         const float c = RICH ? 1.f : a.scale * kLog2e;  // s is the score times log2 e (RICH) or the dot product
         const float2 c2 = both(c);
         const float grow = 8.f / c, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
         bool ok = true;
+        // RICH: a barrier of the two warps that share rows, and the larger of their maxima. A wait that ran out in one of them ends
+        // both here: until then either goes on, so that the other is not left alone.
+        auto join = [&](float mine, uint32_t turn) {
+            float* at = (float*)(from + S::kSwap) + (turn & 1) * 32 + lane;
+            at[warp * 64] = mine;
+            ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
+            return fmaxf(mine, at[(warp ^ 4) * 64]);
+        };
         uint32_t turn = 0, outputs = 0;  // key tiles, outputs so far
         ItemReader reader;
         Item item, then;
@@ -196,7 +224,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
             // the next item and what this thread's row sees in it, one item ahead
             item = then, see = see_then;
             if (item.h == -1) break;
-            if (!reader.next(then, bars, &ok, abort, err)) then.h = -1;
+            bool there = reader.next(then, bars, &ok, abort, err);
+            if (RICH) there = (ok = all_came_well(1 + w * 4 + warp % 4, 64, ok)) && there;
+            if (!there) then.h = -1;
             else see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, (2 * then.pair + w) * kTileT + row);
             if (item.h < 0) continue;
             const int first = w ? item.first[1] : item.first[0], last = w ? item.last[1] : item.last[0];
@@ -210,13 +240,13 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
             const int hi = RICH ? __reduce_max_sync(0xffffffffu, none ? 0 : see.y) : 0;
             float top = -CUDART_INF_F, sum = 0.f;
             for (int kt = first; kt <= last; ++kt, ++turn) {
-                const int k0 = kt * kTileT;
-                ok = wait_warp(smem_u32(&bars.s_full[w]), turn & 1, abort, err);
-                if (!ok) break;
+                const int k0 = kt * kTileT + 64 * half;
+                ok = ok && wait_warp(smem_u32(&bars.s_full[w]), turn & 1, abort, err);
+                if (!RICH && !ok) break;
                 tc_fence_after();
                 float most_now = top;
                 float s[RICH ? 32 : 128];
-                const bool whole = most <= k0 && least >= k0 + kTileT;
+                const bool whole = most <= k0 && least >= k0 + W::kCols;
                 auto sees = [&](int b) { return lo < k0 + 32 * b + 32 && hi > k0 + 32 * b; };
                 auto mask = [&](int b, float* x) {
                     const int at = k0 + 32 * b;
@@ -232,15 +262,15 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                     const float* bias = nullptr;
                     bool flat = false;
                     if (plan.lut) {
-                        ok = wait_warp(smem_u32(&bars.bias_full[w][turn & 1]), (turn / 2) & 1, abort, err);
-                        if (!ok) break;
-                        bias = biases + (turn & 1) * 256 + 127 + row;
-                        flat = q0 - k0 >= plan.reach + 127 || q0 - k0 <= -plan.reach - 127;
+                        ok = ok && wait_warp(smem_u32(&bars.bias_full[w][turn & 1]), (turn / 2) & 1, abort, err);
+                        bias = biases + (turn & 1) * 256 + 127 + row - 64 * half;
+                        const int apart = q0 - kt * kTileT;
+                        flat = apart >= plan.reach + 127 || apart <= -plan.reach - 127;
                     }
 #pragma unroll 1
-                    for (int b = 0; b < 4; ++b) {
+                    for (int b = 0; b < 2; ++b) {
                         if (!sees(b)) continue;
-                        tmem_ld32(ts + 32 * b, s);
+                        tmem_ld32(ts + 64 * half + 32 * b, s);
                         tmem_wait_ld();
                         tmem_use(s);
                         // the bias of 32 distances, nothing where they are all beyond the table's reach but the one of the reach
@@ -261,13 +291,15 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                         else score([&](float2 d, float2 x) { return fma2(tanh_any(mul2(d, both(inv_cap))), both(cap2), x); });
                         if (!whole) mask(b, s);
                         most_now = largest<32>(s, most_now);
-                        tmem_st32(ts + 32 * b, (const uint32_t*)s);
+                        tmem_st32(ts + 64 * half + 32 * b, (const uint32_t*)s);
                     }
                     tmem_wait_st();
                     if (bias) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem_u32(&bars.bias_empty[w][turn & 1]));
                     }
+                    most_now = join(most_now, turn);
+                    if (!ok) break;
                 } else {
                     if (!whole) {
                         // masked scores go back to TMEM, 32 columns at a time: fewer instructions than masks for all 128 in place
@@ -294,13 +326,13 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                     top = most_now;
                 } else if (__any_sync(0xffffffffu, most_now > top + grow)) {
                     ok = wait_warp(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err);
-                    if (!ok) break;
+                    if (!RICH && !ok) break;
                     tc_fence_after();
                     const float by = most_now == -CUDART_INF_F ? 1.f : exp2_fast((top - most_now) * c);
                     top = most_now;
                     sum *= by;
 #pragma unroll 1
-                    for (int b = 0; b < HD / 16; ++b) {
+                    for (int b = 0; b < HD / 16 / (RICH ? 2 : 1); ++b) {
                         float o[16];
                         tmem_ld16(to + 16 * b, o);
 #pragma unroll
@@ -322,46 +354,53 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                         p[j] = pack_bf16(v.x, v.y);
                     }
                 };
-                // in two parts of 64 keys, over columns of S that have been read: the MMAs of the first begin while the second is
-                // computed
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int b = 2 * half + e;
-                        if constexpr (RICH) {
-                            if (!sees(b)) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) p[16 * e + j] = 0;
-                                continue;
-                            }
-                            tmem_ld32(ts + 32 * b, s);
+                // over columns of S that have been read (RICH: the chunks of one's own half, whose first column their P begins at), in
+                // two parts of 64 keys: the MMAs of the first begin while the second is computed, or the other warp's is
+                if constexpr (RICH) {
+#pragma unroll 1
+                    for (int b = 0; b < 2; ++b) {
+                        uint32_t p[16];
+                        if (sees(b)) {
+                            tmem_ld32(ts + 64 * half + 32 * b, s);
                             tmem_wait_ld();
                             tmem_use(s);
-                            weigh(s, p + 16 * e);
+                            weigh(s, p);
                         } else {
-                            weigh(s + 32 * b, p + 16 * e);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) p[j] = 0;
                         }
+                        tmem_st16(ts + 64 * half + 16 * b, p);
                     }
-                    tmem_st32(ts + 32 * half, p);
                     tmem_wait_st();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&bars.p_ready[w][half]));
+                } else {
+#pragma unroll
+                    for (int part_of = 0; part_of < 2; ++part_of) {
+                        uint32_t p[32];
+                        weigh(s + 64 * part_of, p);
+                        weigh(s + 64 * part_of + 32, p + 16);
+                        tmem_st32(ts + 32 * part_of, p);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bars.p_ready[w][part_of]));
+                    }
                 }
                 sum += part[0].x + part[0].y + part[1].x + part[1].y;
             }
             // an item of one key tile does not wait for the output before it: here it does, as that one's sums may not have been read
-            if (ok && outputs++) ok = wait_warp(smem_u32(&bars.o_free[w]), outputs & 1, abort, err);
+            if (outputs++) ok = ok && wait_warp(smem_u32(&bars.o_free[w]), outputs & 1, abort, err);
+            if (RICH) ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
             if (!ok) break;
-            bars.sums[w][row] = make_float2(top, sum);
+            bars.sums[w][half][row] = make_float2(top, sum);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.sum_full[w]));
         }
         tc_fence_before();
-    } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    } else if (warp >= W::kOut) {
+        W::other_registers();
         // outputs of either tile, beside the rows of the next item
         const int q = warp % 4, row = q * 32 + lane;
         const uint32_t out = base + S::kOut + q * 64 * HD;
@@ -382,7 +421,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                     ok = wait_warp(smem_u32(&bars.sum_full[w]), done[w]++ & 1, abort, err) &&
                          wait_warp(smem_u32(&bars.o_done[w]), (turns[w] - 1) & 1, abort, err);
                     if (!ok) continue;
-                    top = bars.sums[w][row].x, sum = bars.sums[w][row].y;
+                    top = bars.sums[w][0][row].x, sum = bars.sums[w][0][row].y;
+                    if (RICH) sum += bars.sums[w][RICH][row].y;
                     tc_fence_after();
                 }
                 const float by = sum != 0.f ? 1.f / sum : 0.f;  // NaN sums stay NaN
@@ -428,8 +468,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
         }
         tc_fence_before();
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 9) {
+        W::other_registers();
+        if (warp == W::kLoad) {
             const uint32_t lead = elect_one();
             uint32_t used = 0;  // loads so far
             bool ok = true;
@@ -457,7 +497,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
             }
             for (uint32_t s = 0; s < (uint32_t)S::kStages; ++s)
                 if (used > s) wait_settled(smem_u32(&bars.full[s]), ((used - 1 - s) / S::kStages) & 1, err);
-        } else if (warp == 10) {
+        } else if (warp == W::kItems) {
             // the items, one ahead of their queries, which are loaded as soon as there is room
             const uint32_t lead = elect_one();
             uint32_t asked0 = 0, asked1 = 0, made = 0;  // query tiles of either kind, items so far
@@ -466,7 +506,11 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                 const uint32_t r = made++;
                 if (r >= 4) ok = ok && wait_warp(smem_u32(&bars.item_empty[r % 4]), (r / 4 - 1) & 1, abort, err);
                 if (!ok) return;
-                const int id = items.at((int)r);
+                int id = items.at((int)r);
+                if (a.range) {  // their lengths are known here only: whoever is done takes the next
+                    if (lane == 0) id = atomicAdd(plan.taken, 1);
+                    id = __shfl_sync(0xffffffffu, id, 0);
+                }
                 int n = 0, h = -1, pair = 0;
                 Hull hull[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
                 if (id < items.total) {
@@ -507,7 +551,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
             }
             if (asked0) wait_settled(smem_u32(&bars.q_full[0]), (asked0 - 1) & 1, err);
             if (asked1) wait_settled(smem_u32(&bars.q_full[1]), (asked1 - 1) & 1, err);
-        } else if (warp == 8) {
+        } else if (warp == W::kMma) {
             const uint32_t lead = elect_one();
             const int steps = (a.hd + 15) / 16;
             constexpr uint32_t kIdS = idesc_bf16(kTileT, kTileT), kIdO = idesc_bf16(kTileT, HD) | kBMn;
@@ -552,7 +596,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
                             tc_fence_after();
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                mma_ts(lead, to, ts + 8 * (4 * b + e), v + ((4 * b + e) * 2048 >> 4), kIdO, now.kt != first || b + e > 0);
+                                mma_ts(lead, to, ts + (RICH ? 64 : 32) * b + 8 * e, v + ((4 * b + e) * 2048 >> 4), kIdO, now.kt != first || b + e > 0);
                         }
                         if (!ok) break;
                         commit(lead, smem_u32(&bars.o_done[w]));
@@ -582,7 +626,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
             }
             commit(lead, smem_u32(&bars.done));
             wait_settled(smem_u32(&bars.done), 0, err);
-        } else if (RICH && plan.lut && warp == 11) {
+        } else if (RICH && plan.lut) {
             // the biases of a tile's 255 distances, ahead of its rows
             uint32_t turns[2] = {0, 0};
             bool ok = true;
@@ -614,7 +658,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_tc_kernel(const __grid_
         }
     }
     __syncthreads();
-    if (warp == 8) {
+    if (warp == W::kMma) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -635,6 +679,7 @@ __global__ __launch_bounds__(256) void attention_plan_kernel(const Attention a, 
         return;
     }
     __shared__ AttentionTile tile;
+    if (blockIdx.x == 0 && t == 0) *plan.taken = 0;
     const int T = (int)a.T, tiles = (T + kTileT - 1) / kTileT, n = blockIdx.x / tiles, k0 = (int)(blockIdx.x % tiles) * kTileT;
     const int2* range = a.range + (int64_t)n * T;
     if (t == 0) {
@@ -729,7 +774,7 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     Items items;
     items.tiles = (int)tiles, items.pairs = (int)((tiles + 1) / 2), items.total = (int)(items.pairs * a.N * a.H);
     items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
-    return launch_chained(chained, attention_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())), dim3(kThreads),
+    return launch_chained(chained, attention_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())), dim3(Warps<RICH>::kThreads),
                           Sh::kSmem, s, q, k, v, a, plan, items, err);
 }
 
@@ -746,7 +791,7 @@ bool attention_tc_supported(const Attention& a, bool backward) {
 
 size_t attention_plan_bytes(const Attention& a, bool bound) {
     size_t n = 0;
-    if (a.range || bound) n += up((size_t)a.N * ((a.T + kTileT - 1) / kTileT) * sizeof(AttentionTile));
+    if (a.range || bound) n += up((size_t)a.N * ((a.T + kTileT - 1) / kTileT) * sizeof(AttentionTile) + 4);
     if (has_lut(a, bound)) n += up((size_t)a.H * (2 * lut_reach(a, bound) + 513) * 4);
     return n;
 }
@@ -758,7 +803,8 @@ cudaError_t launch_attention_plan(const Attention& a, void* ws, AttentionPlan* p
     char* at = (char*)ws;
     if (a.range) {
         plan->tiles = (AttentionTile*)at;
-        at += up((size_t)a.N * tiles * sizeof(AttentionTile));
+        plan->taken = (int*)(plan->tiles + a.N * tiles);
+        at += up((size_t)a.N * tiles * sizeof(AttentionTile) + 4);
         ranged = a.N * tiles;
     }
     if (has_lut(a, false)) {
