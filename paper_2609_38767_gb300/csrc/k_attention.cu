@@ -448,8 +448,18 @@ __global__ __launch_bounds__(1024) void attention_distances_kernel(const float* 
     // threads in groups of `width` rounded up to warps, each group every `groups`-th row
     const int span = (width + 31) / 32 * 32, groups = max(1, 1024 / span), g = t / span, d = t % span;
     double v = 0;
-    if (g < groups && d < width)
-        for (int64_t i = g; i < rows; i += groups) v += part[(h * rows + i) * width + d];
+    if (g < groups && d < width) {
+        const float* p = part + h * rows * width + d;
+        int64_t i = g;
+        for (; i + 7 * groups < rows; i += 8 * groups) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = p[(i + e * groups) * width];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v += x[e];
+        }
+        for (; i < rows; i += groups) v += p[i * width];
+    }
     sums[t] = v;
     if (t < width) ids[t] = bucket[t - mid + reach];
     __syncthreads();
@@ -492,7 +502,74 @@ __device__ __forceinline__ int scan(int v, int identity, int* parts) {
     return MAX ? max(v, before) : min(v, before);
 }
 
-// One CTA per example, 8 tokens a thread at a time: forwards for the first token of each document, backwards for its end
+// Up to 8192 tokens: one CTA per example, EACH tokens a thread in registers, and the three steps of the kernel below at once:
+// scans over the warps' tokens, over the warps by each warp, and the ends of the prefixes through shared memory.
+// 4 x 2047 tokens XX us (the kernel below 12).
+template <int EACH>
+__global__ __launch_bounds__(kScan) void attention_ranges_short_kernel(const int32_t* doc, const int32_t* prefix, int causal, int T,
+                                                                       int64_t window, int2* range) {
+    __shared__ int stops[kScan * EACH], firsts[kScan / 32], ends[kScan / 32];
+    const int64_t row0 = (int64_t)blockIdx.x * T;
+    const int32_t* pre = causal ? prefix : nullptr;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, at = threadIdx.x * EACH;
+    int ids[EACH + 2], flags[EACH];  // from token at - 1 to at + EACH
+#pragma unroll
+    for (int e = 0; e < EACH + 2; ++e) {
+        const int i = at + e - 1;
+        ids[e] = doc && i >= 0 && i < T ? doc[row0 + i] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) flags[e] = pre && at + e < T ? pre[row0 + at + e] : 0;
+    int first[EACH], stop[EACH], f = 0, s = T;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        if (at + e > 0 && ids[e + 1] != ids[e]) f = at + e;
+        first[e] = f;
+    }
+#pragma unroll
+    for (int e = EACH - 1; e >= 0; --e) {
+        const int i = at + e;
+        if (i < T) {
+            const bool last = i == T - 1 || ids[e + 2] != ids[e + 1];
+            if (pre) {
+                if (last || !flags[e]) s = i + (flags[e] != 0);
+            } else if (last) {
+                s = i + 1;
+            }
+        }
+        stop[e] = s;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, f, o), y = __shfl_down_sync(0xffffffffu, s, o);
+        if (lane >= o) f = max(f, x);
+        if (lane + o < 32) s = min(s, y);
+    }
+    if (lane == 31) firsts[warp] = f;
+    if (lane == 0) ends[warp] = s;
+    f = __shfl_up_sync(0xffffffffu, f, 1), s = __shfl_down_sync(0xffffffffu, s, 1);
+    if (lane == 0) f = 0;
+    if (lane == 31) s = T;
+    __syncthreads();
+    f = max(f, __reduce_max_sync(0xffffffffu, lane < warp ? firsts[lane] : 0));
+    s = min(s, __reduce_min_sync(0xffffffffu, lane > warp ? ends[lane] : T));
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        first[e] = max(first[e], f), stop[e] = min(stop[e], s);
+        stops[at + e] = stop[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int i = at + e;
+        if (i >= T) continue;
+        int64_t lo = first[e], hi = !causal ? stop[e] : pre ? max(i + 1, stops[first[e]]) : i + 1;
+        if (window) lo = max(lo, i - window + 1), hi = min(hi, i + window);
+        range[row0 + i] = ids[e + 1] < 0 ? make_int2(0, 0) : make_int2((int)lo, (int)hi);
+    }
+}
+
+// Longer ones: one CTA per example, 8 tokens a thread at a time: forwards for the first token of each document, backwards for its end
 // (or, with a prefix, for the first token from here on that is not prefix), and once more for the ranges.
 __global__ __launch_bounds__(kScan) void attention_ranges_kernel(const int32_t* doc, const int32_t* prefix, int causal, int T,
                                                                  int64_t window, int2* range) {
@@ -662,7 +739,9 @@ cudaError_t launch_attention_backward(const Attention& a, void* ws, unsigned int
 cudaError_t launch_attention_ranges(int64_t N, int64_t T, const int32_t* doc, const int32_t* prefix, int causal, int64_t window,
                                     int2* range, cudaStream_t s) {
     note_launches(1);
-    attention_ranges_kernel<<<(unsigned)N, kScan, 0, s>>>(doc, prefix, causal, (int)T, window, range);
+    if (T <= 2 * kScan) attention_ranges_short_kernel<2><<<(unsigned)N, kScan, 0, s>>>(doc, prefix, causal, (int)T, window, range);
+    else if (T <= 8 * kScan) attention_ranges_short_kernel<8><<<(unsigned)N, kScan, 0, s>>>(doc, prefix, causal, (int)T, window, range);
+    else attention_ranges_kernel<<<(unsigned)N, kScan, 0, s>>>(doc, prefix, causal, (int)T, window, range);
     return cudaGetLastError();
 }
 

@@ -73,7 +73,8 @@ __device__ __forceinline__ uint32_t bits_of(int lo, int hi) {
     lo = min(max(lo, 0), 32), hi = min(max(hi, 0), 32);
     return lo < hi ? (hi == 32 ? ~0u : (1u << hi) - 1) & (~0u << lo) : 0u;
 }
-// Scores times log2 e of a thread's 32 dot products, and in RICH the cap's slope; bias(j): what the pair j's distance adds.
+// Scores times log2 e of a thread's 32 dot products, and in RICH the cap's slope less its sign, t^2 - 1; bias(j): what the pairs
+// j and j + 1 get beside.
 template <bool RICH, typename F>
 __device__ __forceinline__ void scores_of(const Attention& a, float inv_cap, float* s, float* bend, F&& bias) {
     const float2 c2 = both(a.scale * kLog2e), cap2 = both(a.cap * kLog2e);
@@ -82,8 +83,8 @@ __device__ __forceinline__ void scores_of(const Attention& a, float inv_cap, flo
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
                 const float2 t = tanh_of(mul2(make_float2(s[j], s[j + 1]), both(inv_cap)));
-                const float2 x = fma2(t, cap2, make_float2(bias(j), bias(j + 1)));
-                const float2 b = fma2(make_float2(-t.x, -t.y), t, both(1.f));
+                const float2 x = fma2(t, cap2, bias(j));
+                const float2 b = fma2(t, t, both(-1.f));
                 s[j] = x.x, s[j + 1] = x.y, bend[j] = b.x, bend[j + 1] = b.y;
             }
         };
@@ -92,7 +93,7 @@ __device__ __forceinline__ void scores_of(const Attention& a, float inv_cap, flo
     } else {
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
-            const float2 x = fma2(make_float2(s[j], s[j + 1]), c2, make_float2(bias(j), bias(j + 1)));
+            const float2 x = fma2(make_float2(s[j], s[j + 1]), c2, bias(j));
             s[j] = x.x, s[j + 1] = x.y;
         }
     }
@@ -253,8 +254,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
             }
             tmem_wait_ld();
             tmem_use(p);
-            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return ((const float*)nl)[j] + bias[j]; });
-            else scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return ((const float*)nl)[j]; });
+            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add2(((const float2*)nl)[j / 2], make_float2(bias[j], bias[j + 1])); });
+            else scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return ((const float2*)nl)[j / 2]; });
 #pragma unroll
             for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
             if (!whole) {
@@ -268,7 +269,10 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
             tmem_st16(ts, w);
             if (RICH && a.cap > 0.f) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) p[j] *= bend[j];
+                for (int j = 0; j < 32; j += 2) {
+                    const float2 x = mul2(make_float2(p[j], p[j + 1]), make_float2(bend[j], bend[j + 1]));
+                    p[j] = x.x, p[j + 1] = x.y;
+                }
             }
             tmem_wait_st();
             tc_fence_before();
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
             tc_fence_after();
             const int second = warp / 8, half = quarter & 1;
             const uint32_t tile = sq + second * kBytes;
-            const float by = second ? a.scale : 1.f;
+            const float by = second ? RICH && a.cap > 0.f ? -a.scale : a.scale : 1.f;  // the slope's sign
 #pragma unroll 1
             for (int b = 0; b < HD / 64; ++b)
                 stage_columns((second ? tdK : tdV) + lanes, tile, row, half * (HD / 64) + b, by, total > 0);
@@ -510,9 +514,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
         const int2 see = visible(a.range, a.causal, T, (int64_t)n * T, i);
         const float* st = stats + (((int64_t)n * a.H + h) * tiles + tile) * 2 * kTileT;
-        const float nl = st[row];
+        const float2 nl = both(st[row]);
         const float2 nd = both(st[kTileT + row]);
-        const bool single = see.y - see.x <= 1;
+        const bool single = see.y - see.x <= 1, idle = __any_sync(0xffffffffu, see.x >= see.y);
         float flat[2] = {0.f, 0.f};
         uint32_t diags = 0;
         bool ok = true;
@@ -535,7 +539,11 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             }
             tmem_wait_ld();
             tmem_use(p);
-            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return nl + bias[-j]; });
+            if (RICH && idle) {  // the queries of rows that see nothing may be anything, and zero times a slope of NaN is NaN
+#pragma unroll
+                for (int j = 0; j < 32; ++j) p[j] = see.x < see.y ? p[j] : 0.f;
+            }
+            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add2(nl, make_float2(bias[-j], bias[-j - 1])); });
             else scores_of<RICH>(a, inv_cap, p, bend, [&](int) { return nl; });
 #pragma unroll
             for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
@@ -588,9 +596,12 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                         ++diags;
                     }
                 }
-                if (a.cap > 0.f) {  // masked pairs stay zero whatever their slope is
+                if (a.cap > 0.f) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) d[j] = !whole && !(seen >> j & 1) ? 0.f : d[j] * bend[j];
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 x = mul2(make_float2(d[j], d[j + 1]), make_float2(bend[j], bend[j + 1]));
+                        d[j] = x.x, d[j + 1] = x.y;
+                    }
                 }
             }
             uint32_t w[16];
@@ -615,7 +626,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         if (ok) {
             tc_fence_after();
             // 32 columns each: all quarters, or the first two
-            if (quarter < HD / 32) stage_columns(tdQ + lanes, sq, row, quarter, a.scale, total > 0);
+            if (quarter < HD / 32) stage_columns(tdQ + lanes, sq, row, quarter, RICH && a.cap > 0.f ? -a.scale : a.scale, total > 0);
             fence_proxy_async();
         }
         if (all_came_well(1, 32 * kRowWarps, ok) && warp == 0 && elect_one()) {
@@ -787,38 +798,44 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     }
 }
 
-// stats of a tile of 128 queries of a head, 8 lanes per query: -lse and -dO.O.
-__global__ __launch_bounds__(256) void attention_stats_kernel(const Attention a, float* stats) {
+// stats of a tile of 128 queries of a head, LANES lanes a query: -lse log2 e and -dO.O. Bound by reading O and dO.
+template <int LANES>
+__global__ __launch_bounds__(256) void attention_stats_kernel(const Attention a, const FastDiv heads, int tokens, float* stats) {
     const int T = (int)a.T, tiles = (T + kTileT - 1) / kTileT;
-    const int64_t at = (int64_t)blockIdx.x * 32 + threadIdx.x / 8;  // over [N][tiles * 128][H]: a token's heads lie together
-    const int64_t total = a.N * tiles * kTileT * a.H;
-    if (at >= total) return;
-    const int h = (int)(at % a.H), sub = threadIdx.x % 8;
-    const int64_t token = at / a.H;
-    const int i = (int)(token % (tiles * kTileT)), n = (int)(token / (tiles * kTileT));
-    float v = 0.f, l = -CUDART_INF_F;
-    if (i < T) {
-        const int64_t row = (int64_t)n * T + i;
-        const __nv_bfloat16 *o = (const __nv_bfloat16*)a.O + row * a.ld_o + h * a.hd, *g = (const __nv_bfloat16*)a.dO + row * a.ld_do + h * a.hd;
-        for (int c = sub * 8; c < a.hd; c += 64) {
-            const uint4 x = *(const uint4*)(o + c), y = *(const uint4*)(g + c);
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    const int at = (int)(blockIdx.x * (256 / LANES)) + threadIdx.x / LANES, sub = threadIdx.x % LANES;  // over [tokens][H]
+    const int token = heads.div(at), h = at - token * a.H;  // a token's heads lie together
+    if (token >= tokens) return;
+    const int n = token / T, i = token - n * T;
+    const __nv_bfloat16 *o = (const __nv_bfloat16*)a.O + (int64_t)token * a.ld_o + h * a.hd,
+                        *g = (const __nv_bfloat16*)a.dO + (int64_t)token * a.ld_do + h * a.hd;
+    const int64_t where = (int64_t)n * a.H + h;
+    const float l = sub == 0 ? a.lse[where * T + i] : 0.f;
+    uint4 x[2], y[2];  // 16 values of 16 bytes each at most
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v = fmaf(__uint_as_float(xs[e] << 16), __uint_as_float(ys[e] << 16), v);
-                v = fmaf(__uint_as_float(xs[e] & 0xffff0000u), __uint_as_float(ys[e] & 0xffff0000u), v);
-            }
+    for (int e = 0; e < 2; ++e) {
+        const int c = (sub + e * LANES) * 8;
+        x[e] = y[e] = make_uint4(0, 0, 0, 0);
+        if (c < a.hd) x[e] = *(const uint4*)(o + c), y[e] = *(const uint4*)(g + c);
+    }
+    float v = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t xs[4] = {x[e].x, x[e].y, x[e].z, x[e].w}, ys[4] = {y[e].x, y[e].y, y[e].z, y[e].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ys[k] << 16), v);
+            v = fmaf(__uint_as_float(xs[k] & 0xffff0000u), __uint_as_float(ys[k] & 0xffff0000u), v);
         }
-        l = a.lse[((int64_t)n * a.H + h) * T + i];
     }
 #pragma unroll
-    for (int o = 4; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (sub == 0) {
-        const bool none = l == -CUDART_INF_F;
-        float* out = stats + (((int64_t)n * a.H + h) * tiles + i / kTileT) * 2 * kTileT + i % kTileT;
-        out[0] = none ? -CUDART_INF_F : -l * kLog2e;
-        out[kTileT] = none ? 0.f : -v;
-    }
+    for (int s = LANES / 2; s; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+    if (sub) return;
+    const bool none = l == -CUDART_INF_F;
+    float* out = stats + (where * tiles + i / kTileT) * 2 * kTileT + i % kTileT;
+    out[0] = none ? -CUDART_INF_F : -l * kLog2e;
+    out[kTileT] = none ? 0.f : -v;
+    if (i == T - 1)  // the rest of the last tile: no queries
+        for (int k = 1; k < tiles * kTileT - i; ++k) out[k] = -CUDART_INF_F, out[kTileT + k] = 0.f;
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
@@ -842,8 +859,11 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     if (cudaError_t e = launch_attention_plan(a, ws, &plan, &chained, s)) return e;
     float* stats = (float*)((char*)ws + attention_plan_bytes(a, false));
     float* part = a.dtable ? (float*)((char*)stats + up((size_t)a.N * a.H * tiles * kStatBytes)) : nullptr;
+    // 16 bytes a lane, or twice; a head's last lanes idle where hd is no power of two
     note_launches(1);
-    attention_stats_kernel<<<(unsigned)((a.N * tiles * kTileT * a.H + 31) / 32), 256, 0, s>>>(a, stats);
+    constexpr int kLanes = HD / 16;
+    const unsigned grid = (unsigned)((a.N * a.T * a.H + 256 / kLanes - 1) / (256 / kLanes));
+    attention_stats_kernel<kLanes><<<grid, 256, 0, s>>>(a, FastDiv(a.H), (int)(a.N * a.T), stats);
     if (cudaError_t e = cudaGetLastError()) return e;
     if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.H)), dim3(kThreads),
                                        Q::kSmem, s, q, k, v, g, dq, a, plan, (const float*)stats, part, err))
