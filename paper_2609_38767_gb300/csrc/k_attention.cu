@@ -442,12 +442,16 @@ template <typename T>
 __global__ __launch_bounds__(1024) void attention_distances_kernel(const float* part, int64_t rows, int mid, const int32_t* bucket,
                                                                   int64_t reach, int n_buckets, int H, float beta, T* out) {
     chain_wait();
-    __shared__ double sums[1024];
+    __shared__ float sums[1024];
     __shared__ int ids[1024];
     const int h = blockIdx.x, t = threadIdx.x, width = 2 * mid + 1;
     // threads in groups of `width` rounded up to warps, each group every `groups`-th row
     const int span = (width + 31) / 32 * 32, groups = max(1, 1024 / span), g = t / span, d = t % span;
-    double v = 0;
+    float v = 0.f, low = 0.f;  // the sum and what its roundings lost: the SM has 64-bit adders for two lanes
+    auto add = [&](float x) {
+        const float y = x - low, s = v + y;
+        low = (s - v) - y, v = s;
+    };
     if (g < groups && d < width) {
         const float* p = part + h * rows * width + d;
         int64_t i = g;
@@ -456,9 +460,9 @@ __global__ __launch_bounds__(1024) void attention_distances_kernel(const float* 
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = p[(i + e * groups) * width];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v += x[e];
+            for (int e = 0; e < 8; ++e) add(x[e]);
         }
-        for (; i < rows; i += groups) v += p[i * width];
+        for (; i < rows; i += groups) add(p[i * width]);
     }
     sums[t] = v;
     if (t < width) ids[t] = bucket[t - mid + reach];
@@ -469,14 +473,14 @@ __global__ __launch_bounds__(1024) void attention_distances_kernel(const float* 
     }
     __syncthreads();
     for (int b = t / 32; b < n_buckets; b += 32) {
-        double s = 0;
+        float s = 0.f;
         for (int i = t % 32; i < width; i += 32)
             if (ids[i] == b) s += sums[i];
 #pragma unroll
         for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (t % 32 == 0) {
             T& x = out[(int64_t)b * H + h];
-            x = narrow<T>((float)(beta != 0.f ? beta * (double)wide(x) + s : s));
+            x = narrow<T>(beta != 0.f ? fmaf(beta, wide(x), s) : s);
         }
     }
 }

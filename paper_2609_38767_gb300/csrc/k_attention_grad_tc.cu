@@ -5,11 +5,12 @@
 // that shares them. S^T = K Q^T and dP^T = V dO^T are in TMEM with a key per lane; sixteen warps (a lane and a quarter of the
 // queries per thread) turn S^T into P^T over its own columns, and dP^T into dX^T, both bf16, which are the MMAs' operands from TMEM:
 //   dV += P^T dO,  dK += dX^T Q.
-// attention_dq_tc_kernel: a CTA has 128 queries of a head; S = Q K^T and dP = dO V^T with a query per lane, dX over the columns
+// attention_dq_tc_kernel: an item is 128 queries of a head, a CTA per SM takes them in turn; S = Q K^T and dP = dO V^T with a query per lane, dX over the columns
 // that S had, dQ += dX K; with a learned bias also the sums of dS along the diagonals.
 // The order of MMAs keeps the tensor pipe busy while the warps work: dV(i) S(i+1) | dK(i) dP(i+1), and S(i+1) dP(i+1) | dQ(i).
 //
-// Warps 0-15: rows; 16: MMAs; 17: TMA; 18: biases by distance; 19 (dQ with a learned bias): sums by bucket. Waits are bounded (about 1 s) and set
+// Warps 0-15: rows; 16: MMAs; 17: TMA; 18: biases by distance, in dQ also items and their queries; 19 (dQ with a learned bias): sums by
+// distance or bucket. Waits are bounded (about 1 s) and set
 // kErrTimeout on expiry.
 #include <cuda.h>
 #include <math_constants.h>
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
 #pragma unroll
             for (int p = 0; p < kPanels; ++p)
                 if (64 * p < a.hd) tma_store_head(second ? &tmdK : &tmdV, sq + second * kBytes + p * kPanel, 64 * p, kv, k0, n);
-            asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group 0;" ::: "memory");
+            asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group.read 0;" ::: "memory");
         }
         __syncwarp();
         tc_fence_before();
@@ -436,45 +437,103 @@ template <int HD, bool RICH>
 struct DqShape {
     static constexpr int kK = HD == 64 ? 4 : RICH ? 2 : 3, kV = HD == 64 ? 3 : 2;
     static constexpr uint32_t kBias = (2 + kK + kV) * Tiles<HD>::kBytes;  // RICH: 2 windows of 256 biases, 2 x [16 warps][64]
-    static constexpr uint32_t kDiag = kBias + (RICH ? 2048 : 0);          // diagonals, the buckets
-    static constexpr uint32_t kHist = kDiag + (RICH ? 2 * kRowWarps * 64 * 4 : 0), kSmem = kHist + (RICH ? 1024 * 4 : 0) + 1024;
+    static constexpr uint32_t kDiag = kBias + (RICH ? 2048 : 0);          // diagonals, the sums of an item
+    static constexpr uint32_t kHist = kDiag + (RICH ? 2 * kRowWarps * 64 * 4 : 0), kSmem = kHist + (RICH ? 1024 * 4 : 0);
 };
 struct DqBars {
-    uint64_t q_full, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free, ds_ready, bias_full[2], bias_empty[2],
-        diag_full[2], diag_empty[2], done;
+    uint64_t item_full[4], item_empty[4], q_full, q_empty, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free,
+        ds_ready, dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, done;
+    int4 items[4][2];
+    float flat[kRowWarps][2];
     uint32_t tmem;
     int abort;
-    float flat[kRowWarps][2];
 };
+// The query tiles of all heads, long ones first where the mask is causal, and how CTAs take them (see the forward pass).
+struct DqItems {
+    int total, tiles;
+    FastDiv heads, H, group;
+};
+// An item as warp 18 leaves it for the others, four at a time.
+struct DqItem {
+    int n, h, tile;  // h < 0: no more
+    int first, last, most, least;
+};
+struct DqReader {
+    uint32_t r = 0;
+    __device__ __forceinline__ bool next(DqItem& x, DqBars& bars, bool* ok, volatile int* abort, unsigned int* err) {
+        *ok = *ok && wait_all(&bars.item_full[r % 4], (r / 4) & 1, abort, err);
+        if (!*ok) return false;
+        const int4 a = bars.items[r % 4][0], b = bars.items[r % 4][1];
+        x.n = a.x, x.h = a.y, x.tile = a.z;
+        x.first = b.x, x.last = b.y, x.most = b.z, x.least = b.w;
+        arrive_warp(&bars.item_empty[r % 4]);
+        ++r;
+        return x.h >= 0;
+    }
+};
+struct DqWalk {
+    DqItem item;
+    int kt = 0, last = 0;
+    bool valid = true;
+    DqReader reader;
+    __device__ __forceinline__ void next(DqBars& bars, bool* ok, volatile int* abort, unsigned int* err) {
+        if (!valid) return;
+        if (kt < last) {
+            ++kt;
+            return;
+        }
+        do valid = reader.next(item, bars, ok, abort, err);
+        while (valid && item.first > item.last);
+        kt = item.first, last = item.last;
+    }
+};
+// Lane l of four gets the l-th 16 bytes of each of the four lanes' 64.
+__device__ __forceinline__ void transpose_quads(uint4 (&v)[4]) {
+    const int lane = threadIdx.x % 32;
+    auto swap = [&](uint4& low, uint4& high, int by) {  // the lane without the bit gives its high, the other its low
+        const bool up = lane & by;
+        uint4 out = up ? low : high;
+        out.x = __shfl_xor_sync(0xffffffffu, out.x, by), out.y = __shfl_xor_sync(0xffffffffu, out.y, by);
+        out.z = __shfl_xor_sync(0xffffffffu, out.z, by), out.w = __shfl_xor_sync(0xffffffffu, out.w, by);
+        if (up) low = out;
+        else high = out;
+    };
+    swap(v[0], v[1], 1), swap(v[2], v[3], 1);
+    swap(v[0], v[2], 2), swap(v[1], v[3], 2);
+}
 
 template <int HD, bool RICH>
 __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-    const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmdQ, const Attention a, const AttentionPlan plan,
-    const float* stats, float* part, unsigned int* err) {
+    const __grid_constant__ CUtensorMap tmG, const Attention a, const AttentionPlan plan, const DqItems items, const float* stats,
+    float* part, unsigned int* err) {
     using S = DqShape<HD, RICH>;
     constexpr uint32_t kBytes = Tiles<HD>::kBytes;
     constexpr int kPanels = Tiles<HD>::kPanels;
     extern __shared__ __align__(1024) uint8_t raw[];
     __shared__ DqBars bars;
-    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    uint8_t* from = raw + (base - smem_u32(raw));
+    const uint32_t base = smem_u32(raw);
     const uint32_t sq = base, sg = base + kBytes, sk = base + 2 * kBytes, sv = sk + S::kK * kBytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
-    const int T = (int)a.T, tiles = (T + kTileT - 1) / kTileT, heads = (int)(a.N * a.H);
-    const int tile = tiles - 1 - (int)(blockIdx.x / heads);  // long rows first
-    const int n = (int)(blockIdx.x % heads) / a.H, h = (int)(blockIdx.x % heads) % a.H, kv = h / (a.H / a.KV);
-    const int q0 = tile * kTileT;
+    const int T = (int)a.T, tiles = items.tiles;
     volatile int* abort = &bars.abort;
+    const bool learned = RICH && part != nullptr;
+    const int dense_mid = attention_dense_mid(a);  // where the sums are by distance, the place of distance 0
+    const bool dense = dense_mid >= 0;
+    if (base & 1023u) {
+        if (threadIdx.x == 0) atomicOr(err, kErrBadLaunch);
+        return;
+    }
     if (warp == kRowWarps) {
         tmem_alloc(smem_u32(&bars.tmem), 512);
         tmem_relinquish();
         if (lane == 0) {
-            for (uint64_t* b : {&bars.q_full, &bars.s_full[0], &bars.s_full[1], &bars.dp_full, &bars.done, &bars.diag_empty[0],
-                                &bars.diag_empty[1]})
+            for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bars.item_full[i]), 1), mbar_init(smem_u32(&bars.item_empty[i]), kRowWarps + 2 + learned);
+            for (uint64_t* b : {&bars.q_full, &bars.q_empty, &bars.s_full[0], &bars.s_full[1], &bars.dp_full, &bars.dq_done, &bars.done,
+                                &bars.diag_empty[0], &bars.diag_empty[1], &bars.flat_empty})
                 mbar_init(smem_u32(b), 1);
             for (uint64_t* b : {&bars.dp_free, &bars.ds_ready, &bars.diag_full[0], &bars.diag_full[1], &bars.bias_empty[0],
-                                &bars.bias_empty[1]})
+                                &bars.bias_empty[1], &bars.flat_full})
                 mbar_init(smem_u32(b), kRowWarps);
             for (uint64_t* b : {&bars.bias_full[0], &bars.bias_full[1]}) mbar_init(smem_u32(b), 32);
             for (int i = 0; i < S::kK; ++i) mbar_init(smem_u32(&bars.k_full[i]), 1), mbar_init(smem_u32(&bars.k_empty[i]), 1);
@@ -489,291 +548,388 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars.tmem;
-    int k_first = 0, k_last, most = 0, least;
-    if (a.range) {
-        const AttentionTile& t = plan.tiles[(int64_t)n * tiles + tile];
-        k_first = t.lo / kTileT, k_last = t.lo < t.hi ? (t.hi - 1) / kTileT : -1, most = t.most, least = t.least;
-    } else {
-        k_last = (a.causal ? min(q0 + kTileT, T) - 1 : T - 1) / kTileT, least = a.causal ? q0 + 1 : T;
-    }
-    const int total = k_last >= k_first ? k_last - k_first + 1 : 0;
     const uint32_t tP = tmem + 256, tdQ = tmem + 384;
-    const bool learned = RICH && part != nullptr;
-    const int dense_mid = attention_dense_mid(a);  // where the sums are by distance, the place of distance 0
-    const bool dense = dense_mid >= 0;
-    // every distance of the pair of tiles is beyond the table's reach
-    auto flat_at = [&](int kt) {
-        const int64_t apart = (int64_t)q0 - (int64_t)kt * kTileT;
+    // every distance of a pair of tiles is beyond the table's reach
+    auto flat_at = [&](int tile, int kt) {
+        const int64_t apart = ((int64_t)tile - kt) * kTileT;
         return apart - 127 >= a.reach ? 1 : apart + 127 <= -a.reach ? -1 : 0;
     };
 
     if (warp < kRowWarps) {
         take_registers();
-        const int quarter = warp / 4, row = warp % 4 * 32 + lane, i = q0 + row;
+        const int quarter = warp / 4, row = warp % 4 * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
-        const int2 see = visible(a.range, a.causal, T, (int64_t)n * T, i);
-        const float* st = stats + (((int64_t)n * a.H + h) * tiles + tile) * 2 * kTileT;
-        const float2 nl = both(st[row]);
-        const float2 nd = both(st[kTileT + row]);
-        const bool single = see.y - see.x <= 1, idle = __any_sync(0xffffffffu, see.x >= see.y);
-        float flat[2] = {0.f, 0.f};
-        uint32_t diags = 0;
+        const float by = RICH && a.cap > 0.f ? -a.scale : a.scale;  // the slope's sign
+        uint32_t it = 0, diags = 0, done = 0, written = 0;  // key tiles, diagonals, outputs, items' sums so far
         bool ok = true;
-        for (int it = 0; it < total; ++it) {
-            const int kt = k_first + it, k0 = kt * kTileT;
-            const uint32_t ts = tmem + (it & 1) * 128 + lanes + 32 * quarter;
-            const bool whole = most <= k0 && least >= k0 + kTileT;
-            const int at = k0 + 32 * quarter;
-            const uint32_t seen = whole ? ~0u : single ? 0u : bits_of(see.x - at, see.y - at);
-            ok = wait_all(&bars.s_full[it & 1], (it / 2) & 1, abort, err);
-            if (!ok) break;
-            tc_fence_after();
-            float p[32], bend[RICH ? 32 : 1];
-            tmem_ld32(ts, p);
-            const float* bias = nullptr;
-            if (RICH && plan.lut) {
-                ok = wait_all(&bars.bias_full[it & 1], (it / 2) & 1, abort, err);
+        DqReader reader;
+        DqItem item, then;
+        then.h = -2;
+        int2 see, see_then = make_int2(0, 0);
+        float2 stat, stat_then = make_float2(0.f, 0.f);
+        while (ok) {
+            // the next item and what this thread's row sees and has in it, one item ahead
+            item = then, see = see_then, stat = stat_then;
+            if (item.h == -1) break;
+            if (!reader.next(then, bars, &ok, abort, err)) {
+                then.h = -1;
+            } else {
+                see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, then.tile * kTileT + row);
+                const float* st = stats + (((int64_t)then.n * a.H + then.h) * tiles + then.tile) * 2 * kTileT;
+                stat_then = make_float2(st[row], st[kTileT + row]);
+            }
+            if (item.h < 0) continue;
+            const int q0 = item.tile * kTileT;
+            const float2 nl = both(stat.x), nd = both(stat.y);
+            const bool single = see.y - see.x <= 1, idle = __any_sync(0xffffffffu, see.x >= see.y);
+            float flat[2] = {0.f, 0.f};
+            for (int kt = item.first; kt <= item.last; ++kt, ++it) {
+                const int k0 = kt * kTileT;
+                const uint32_t ts = tmem + (it & 1) * 128 + lanes + 32 * quarter;
+                const bool whole = item.most <= k0 && item.least >= k0 + kTileT;
+                const int at = k0 + 32 * quarter;
+                const uint32_t seen = whole ? ~0u : single ? 0u : bits_of(see.x - at, see.y - at);
+                ok = wait_all(&bars.s_full[it & 1], (it / 2) & 1, abort, err);
                 if (!ok) break;
-                bias = (const float*)(from + S::kBias) + (it & 1) * 256 + 127 + row - 32 * quarter;
-            }
-            tmem_wait_ld();
-            tmem_use(p);
-            if (RICH && idle) {  // the queries of rows that see nothing may be anything, and zero times a slope of NaN is NaN
+                tc_fence_after();
+                float p[32], bend[RICH ? 32 : 1];
+                tmem_ld32(ts, p);
+                const float* bias = nullptr;
+                if (RICH && plan.lut) {
+                    ok = wait_all(&bars.bias_full[it & 1], (it / 2) & 1, abort, err);
+                    if (!ok) break;
+                    bias = (const float*)(raw + S::kBias) + (it & 1) * 256 + 127 + row - 32 * quarter;
+                }
+                tmem_wait_ld();
+                tmem_use(p);
+                if (RICH && idle) {  // the queries of rows that see nothing may be anything, and zero times a slope of NaN is NaN
 #pragma unroll
-                for (int j = 0; j < 32; ++j) p[j] = see.x < see.y ? p[j] : 0.f;
-            }
-            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add2(nl, make_float2(bias[-j], bias[-j - 1])); });
-            else scores_of<RICH>(a, inv_cap, p, bend, [&](int) { return nl; });
+                    for (int j = 0; j < 32; ++j) p[j] = see.x < see.y ? p[j] : 0.f;
+                }
+                if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add2(nl, make_float2(bias[-j], bias[-j - 1])); });
+                else scores_of<RICH>(a, inv_cap, p, bend, [&](int) { return nl; });
 #pragma unroll
-            for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
-            if (RICH && bias) arrive_warp(&bars.bias_empty[it & 1]);
-            ok = wait_all(&bars.dp_full, it & 1, abort, err);
+                for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
+                if (RICH && bias) arrive_warp(&bars.bias_empty[it & 1]);
+                ok = wait_all(&bars.dp_full, it & 1, abort, err);
+                if (!ok) break;
+                tc_fence_after();
+                float d[32];
+                tmem_ld32(tP + lanes + 32 * quarter, d);
+                tmem_wait_ld();
+                tmem_use(d);
+                tc_fence_before();
+                arrive_warp(&bars.dp_free);
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    const float2 x = mul2(add2(make_float2(d[j], d[j + 1]), nd), make_float2(p[j], p[j + 1]));
+                    d[j] = x.x, d[j + 1] = x.y;
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (!(seen >> j & 1)) d[j] = 0.f;
+                }
+                if constexpr (RICH) {
+                    if (learned) {
+                        if (const int side = flat_at(item.tile, kt)) {
+                            float sum = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum += d[j];
+                            flat[side > 0] += sum;
+                        } else {
+                            float* diag = (float*)(raw + S::kDiag) + ((diags & 1) * kRowWarps + warp) * 64;
+                            if (diags >= 2) {
+                                ok = wait_all(&bars.diag_empty[diags & 1], (diags / 2 - 1) & 1, abort, err);
+                                if (!ok) break;
+                            }
+                            // a diagonal's sum moves down the lanes with the columns and leaves at lane 31
+                            float acc = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                acc += d[j];
+                                if (lane == 31) diag[62 - j] = acc;  // row - column = 31 - j
+                                if (j < 31) {
+                                    acc = __shfl_up_sync(0xffffffffu, acc, 1);
+                                    if (lane == 0) acc = 0.f;
+                                }
+                            }
+                            if (lane < 31) diag[lane] = acc;  // lane - 31
+                            arrive_warp(&bars.diag_full[diags & 1]);
+                            ++diags;
+                        }
+                    }
+                    if (a.cap > 0.f) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 x = mul2(make_float2(d[j], d[j + 1]), make_float2(bend[j], bend[j + 1]));
+                            d[j] = x.x, d[j + 1] = x.y;
+                        }
+                    }
+                }
+                uint32_t w[16];
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+                tmem_st16(ts, w);
+                tmem_wait_st();
+                tc_fence_before();
+                arrive_warp(&bars.ds_ready);
+            }
             if (!ok) break;
-            tc_fence_after();
-            float d[32];
-            tmem_ld32(tP + lanes + 32 * quarter, d);
-            tmem_wait_ld();
-            tmem_use(d);
-            tc_fence_before();
-            arrive_warp(&bars.dp_free);
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                const float2 x = mul2(add2(make_float2(d[j], d[j + 1]), nd), make_float2(p[j], p[j + 1]));
-                d[j] = x.x, d[j + 1] = x.y;
-            }
-            if (!whole) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (!(seen >> j & 1)) d[j] = 0.f;
-            }
             if constexpr (RICH) {
                 if (learned) {
-                    if (const int side = flat_at(kt)) {
-                        float sum = 0.f;
+                    if (written++) ok = wait_all(&bars.flat_empty, written & 1, abort, err);
+                    if (!ok) break;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) sum += d[j];
-                        flat[side > 0] += sum;
-                    } else {
-                        float* diag = (float*)(from + S::kDiag) + ((diags & 1) * kRowWarps + warp) * 64;
-                        if (diags >= 2) {
-                            ok = wait_all(&bars.diag_empty[diags & 1], (diags / 2 - 1) & 1, abort, err);
-                            if (!ok) break;
-                        }
-                        // a diagonal's sum moves down the lanes with the columns and leaves at lane 31
-                        float acc = 0.f;
+                    for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            acc += d[j];
-                            if (lane == 31) diag[62 - j] = acc;  // row - column = 31 - j
-                            if (j < 31) {
-                                acc = __shfl_up_sync(0xffffffffu, acc, 1);
-                                if (lane == 0) acc = 0.f;
-                            }
-                        }
-                        if (lane < 31) diag[lane] = acc;  // lane - 31
-                        arrive_warp(&bars.diag_full[diags & 1]);
-                        ++diags;
+                        for (int o = 16; o; o >>= 1) flat[e] += __shfl_xor_sync(0xffffffffu, flat[e], o);
+                        if (lane == 0) bars.flat[warp][e] = flat[e];
                     }
-                }
-                if (a.cap > 0.f) {
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const float2 x = mul2(make_float2(d[j], d[j + 1]), make_float2(bend[j], bend[j + 1]));
-                        d[j] = x.x, d[j + 1] = x.y;
-                    }
+                    arrive_warp(&bars.flat_full);
                 }
             }
-            uint32_t w[16];
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
-            tmem_st16(ts, w);
-            tmem_wait_st();
-            tc_fence_before();
-            arrive_warp(&bars.ds_ready);
-        }
-        if constexpr (RICH) {
-            if (learned) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int o = 16; o; o >>= 1) flat[e] += __shfl_xor_sync(0xffffffffu, flat[e], o);
-                    if (lane == 0) bars.flat[warp][e] = flat[e];
-                }
-            }
-        }
-        if (ok) ok = wait_all(&bars.done, 0, abort, err);
-        if (ok) {
+            const bool any = item.first <= item.last;
+            if (any) ok = wait_all(&bars.dq_done, done++ & 1, abort, err);
+            if (!ok) break;
             tc_fence_after();
-            // 32 columns each: all quarters, or the first two
-            if (quarter < HD / 32) stage_columns(tdQ + lanes, sq, row, quarter, RICH && a.cap > 0.f ? -a.scale : a.scale, total > 0);
-            fence_proxy_async();
-        }
-        if (all_came_well(1, 32 * kRowWarps, ok) && warp == 0 && elect_one()) {
+            // 32 columns each (all quarters, or the first two), four lanes to 64 bytes of a row on the way out
+            if (quarter < HD / 32 && 32 * quarter < a.hd) {
+                float o[32];
+                uint4 v[4];
+                tmem_ld32(tdQ + lanes + 32 * quarter, o);
+                tmem_wait_ld();
+                tmem_use(o);
 #pragma unroll
-            for (int p = 0; p < kPanels; ++p)
-                if (64 * p < a.hd) tma_store_head(&tmdQ, sq + p * kPanel, 64 * p, h, q0, n);
-            asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group 0;" ::: "memory");
+                for (int g = 0; g < 4; ++g) {
+                    const float* x = o + 8 * g;
+                    v[g] = any ? make_uint4(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by), pack_bf16(x[4] * by, x[5] * by),
+                                            pack_bf16(x[6] * by, x[7] * by))
+                               : make_uint4(0, 0, 0, 0);
+                }
+                transpose_quads(v);
+                const int col = 32 * quarter + lane % 4 * 8, first_row = q0 + warp % 4 * 32 + lane / 4 * 4;
+                __nv_bfloat16* out = (__nv_bfloat16*)a.dQ + ((int64_t)item.n * T + first_row) * a.ld_dq + item.h * a.hd + col;
+                if (col < a.hd) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (first_row + k < T) *(uint4*)(out + k * a.ld_dq) = v[k];
+                }
+            }
+            tc_fence_before();
         }
-        __syncwarp();
-        tc_fence_before();
     } else {
         give_registers();
+        bool ok = true;
         if (warp == kRowWarps + 1) {
             const uint32_t lead = elect_one();
-            bool ok = true;
-            if (total && lead) {
-                mbar_arrive_tx(smem_u32(&bars.q_full), 2 * kBytes);
-                load_tile<HD>(sq, &tmQ, h, q0, n, smem_u32(&bars.q_full));
-                load_tile<HD>(sg, &tmG, h, q0, n, smem_u32(&bars.q_full));
-            }
-            int loaded_k = 0, loaded_v = 0;
-            for (int it = 0; it < total; ++it) {
-                const int k = it % S::kK, v = it % S::kV, k0 = (k_first + it) * kTileT;
-                if (it >= S::kK) ok = wait_all(&bars.k_empty[k], (it / S::kK - 1) & 1, abort, err);
+            uint32_t used = 0;  // key tiles so far
+            uint32_t loaded_v = 0;
+            DqWalk x;
+            while (true) {
+                x.next(bars, &ok, abort, err);
+                if (!ok || !x.valid) break;
+                const uint32_t k = used % S::kK, v = used % S::kV;
+                const int kv = items.group.div(x.item.h), k0 = x.kt * kTileT;
+                if (used >= S::kK) ok = wait_all(&bars.k_empty[k], (used / S::kK - 1) & 1, abort, err);
                 if (!ok) break;
                 if (lead) {
                     mbar_arrive_tx(smem_u32(&bars.k_full[k]), kBytes);
-                    load_tile<HD>(sk + k * kBytes, &tmK, kv, k0, n, smem_u32(&bars.k_full[k]));
+                    load_tile<HD>(sk + k * kBytes, &tmK, kv, k0, x.item.n, smem_u32(&bars.k_full[k]));
                 }
-                ++loaded_k;
+                ++used;
                 __syncwarp();
-                if (it >= S::kV) ok = wait_all(&bars.v_empty[v], (it / S::kV - 1) & 1, abort, err);
+                if (loaded_v >= S::kV) ok = wait_all(&bars.v_empty[v], (loaded_v / S::kV - 1) & 1, abort, err);
                 if (!ok) break;
                 if (lead) {
                     mbar_arrive_tx(smem_u32(&bars.v_full[v]), kBytes);
-                    load_tile<HD>(sv + v * kBytes, &tmV, kv, k0, n, smem_u32(&bars.v_full[v]));
+                    load_tile<HD>(sv + v * kBytes, &tmV, kv, k0, x.item.n, smem_u32(&bars.v_full[v]));
                 }
                 ++loaded_v;
                 __syncwarp();
             }
-            if (total) wait_settled(smem_u32(&bars.q_full), 0, err);
-            for (int s = 0; s < S::kK; ++s)
-                if (loaded_k > s) wait_settled(smem_u32(&bars.k_full[s]), ((loaded_k - 1 - s) / S::kK) & 1, err);
-            for (int s = 0; s < S::kV; ++s)
+            for (uint32_t s = 0; s < (uint32_t)S::kK; ++s)
+                if (used > s) wait_settled(smem_u32(&bars.k_full[s]), ((used - 1 - s) / S::kK) & 1, err);
+            for (uint32_t s = 0; s < (uint32_t)S::kV; ++s)
                 if (loaded_v > s) wait_settled(smem_u32(&bars.v_full[s]), ((loaded_v - 1 - s) / S::kV) & 1, err);
         } else if (warp == kRowWarps) {
             const uint32_t lead = elect_one();
             const int steps = (a.hd + 15) / 16;
             constexpr uint32_t kIdS = idesc_bf16(kTileT, kTileT), kIdO = idesc_bf16(kTileT, HD) | kBMn;
-            bool ok = total == 0 || wait_all(&bars.q_full, 0, abort, err);
-            // S(i + 1), dP(i + 1), dQ(i); i = -1 has only the two
-            for (int it = -1; ok && it < total && total; ++it) {
-                const int then = it + 1;
-                if (then < total) {
-                    const uint32_t tile_k = sk + then % S::kK * kBytes;
-                    ok = wait_all(&bars.k_full[then % S::kK], (then / S::kK) & 1, abort, err);
+            uint32_t it = 0, queries = 0;  // key tiles (`now`), query tiles so far
+            DqWalk now, then;
+            now.valid = false;
+            // S, dP of the key tile after `now`, then dQ of `now`
+            while (true) {
+                const uint32_t at = now.valid ? it + 1 : it;
+                then.next(bars, &ok, abort, err);
+                if (!ok || (!now.valid && !then.valid)) break;
+                if (then.valid) {
+                    const uint32_t tile_k = sk + at % S::kK * kBytes;
+                    if (then.kt == then.item.first) ok = wait_all(&bars.q_full, queries++ & 1, abort, err);
+                    ok = ok && wait_all(&bars.k_full[at % S::kK], (at / S::kK) & 1, abort, err);
                     if (!ok) break;
                     if (a.range) {
                         uint32_t bits[4];
-                        *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)n * tiles + k_first + then].unseen;
+                        *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)then.item.n * tiles + then.kt].unseen;
                         if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(tile_k, kPanels, bits);
                     }
                     tc_fence_after();
-                    mma_heads<HD>(lead, tmem + (then & 1) * 128, sq, tile_k, kIdS, steps);
-                    commit(lead, smem_u32(&bars.s_full[then & 1]));
-                    if (it >= 0) ok = wait_all(&bars.dp_free, it & 1, abort, err);
-                    ok = ok && wait_all(&bars.v_full[then % S::kV], (then / S::kV) & 1, abort, err);
+                    mma_heads<HD>(lead, tmem + (at & 1) * 128, sq, tile_k, kIdS, steps);
+                    commit(lead, smem_u32(&bars.s_full[at & 1]));
+                    if (at) ok = wait_all(&bars.dp_free, (at - 1) & 1, abort, err);
+                    ok = ok && wait_all(&bars.v_full[at % S::kV], (at / S::kV) & 1, abort, err);
                     if (!ok) break;
                     tc_fence_after();
-                    mma_heads<HD>(lead, tP, sg, sv + then % S::kV * kBytes, kIdS, steps);
+                    mma_heads<HD>(lead, tP, sg, sv + at % S::kV * kBytes, kIdS, steps);
                     commit(lead, smem_u32(&bars.dp_full));
-                    commit(lead, smem_u32(&bars.v_empty[then % S::kV]));
+                    commit(lead, smem_u32(&bars.v_empty[at % S::kV]));
+                    if (then.kt == then.last) commit(lead, smem_u32(&bars.q_empty));
                 }
-                if (it < 0) continue;
-                ok = wait_all(&bars.ds_ready, it & 1, abort, err);
-                if (!ok) break;
-                tc_fence_after();
-                mma_quarters(lead, tdQ, tmem + (it & 1) * 128, sk + it % S::kK * kBytes, kIdO, it == 0);
-                commit(lead, smem_u32(&bars.k_empty[it % S::kK]));
+                if (now.valid) {
+                    ok = wait_all(&bars.ds_ready, it & 1, abort, err);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_quarters(lead, tdQ, tmem + (it & 1) * 128, sk + it % S::kK * kBytes, kIdO, now.kt == now.item.first);
+                    commit(lead, smem_u32(&bars.k_empty[it % S::kK]));
+                    if (now.kt == now.last) commit(lead, smem_u32(&bars.dq_done));
+                    ++it;
+                }
+                now = then;
             }
             commit(lead, smem_u32(&bars.done));
             wait_settled(smem_u32(&bars.done), 0, err);
-        } else if (RICH && warp == kRowWarps + 2) {
-            for (int it = 0; plan.lut && it < total; ++it) {
-                if (it >= 2 && !wait_all(&bars.bias_empty[it & 1], (it / 2 - 1) & 1, abort, err)) break;
-                load_window(plan, h, q0 - (k_first + it) * kTileT, (float*)(from + S::kBias) + (it & 1) * 256);
-                mbar_arrive(smem_u32(&bars.bias_full[it & 1]));
+        } else if (warp == kRowWarps + 2) {
+            // the items, one ahead; the queries and gradients of an item as soon as there is room; its biases
+            const uint32_t lead = elect_one();
+            uint32_t queries = 0, windows = 0;
+            for (uint32_t r = 0;; ++r) {  // makes item r, loads for item r - 1
+                if (r && bars.items[(r - 1) % 4][0].y < 0) break;
+                if (r >= 4) ok = wait_all(&bars.item_empty[r % 4], (r / 4 - 1) & 1, abort, err);
+                if (!ok) break;
+                const int g = gridDim.x;
+                int id = (int)r * g + (r & 1 ? g - 1 - (int)blockIdx.x : (int)blockIdx.x);
+                if (a.range) {
+                    if (lane == 0) id = atomicAdd(plan.taken, 1);
+                    id = __shfl_sync(0xffffffffu, id, 0);
+                }
+                int4 x = make_int4(0, -1, 0, 0), y = make_int4(0, -1, 0, 0);
+                if (id < items.total) {
+                    const int tile = tiles - 1 - items.heads.div(id), of = items.heads.mod(id), q0 = tile * kTileT;
+                    x = make_int4(items.H.div(of), items.H.mod(of), tile, 0);
+                    if (a.range) {
+                        const AttentionTile& t = plan.tiles[(int64_t)x.x * tiles + tile];
+                        y = make_int4(t.lo / kTileT, t.lo < t.hi ? (t.hi - 1) / kTileT : -1, t.most, t.least);
+                    } else {
+                        y = make_int4(0, (a.causal ? min(q0 + kTileT, T) - 1 : T - 1) / kTileT, 0, a.causal ? q0 + 1 : T);
+                    }
+                }
+                if (lead) {
+                    bars.items[r % 4][0] = x, bars.items[r % 4][1] = y;
+                    mbar_arrive(smem_u32(&bars.item_full[r % 4]));
+                }
+                __syncwarp();
+                if (r == 0) continue;
+                // nobody can have replaced what this warp made: the slot is free for item r + 3 once its readers have passed it
+                x = bars.items[(r - 1) % 4][0], y = bars.items[(r - 1) % 4][1];
+                if (y.x > y.y) continue;
+                if (queries) ok = wait_all(&bars.q_empty, (queries - 1) & 1, abort, err);
+                if (!ok) break;
+                if (lead) {
+                    mbar_arrive_tx(smem_u32(&bars.q_full), 2 * kBytes);
+                    load_tile<HD>(sq, &tmQ, x.y, x.z * kTileT, x.x, smem_u32(&bars.q_full));
+                    load_tile<HD>(sg, &tmG, x.y, x.z * kTileT, x.x, smem_u32(&bars.q_full));
+                }
+                ++queries;
+                __syncwarp();
+                if (RICH && plan.lut) {
+                    for (int kt = y.x; kt <= y.y; ++kt, ++windows) {
+                        if (windows >= 2) ok = wait_all(&bars.bias_empty[windows & 1], (windows / 2 - 1) & 1, abort, err);
+                        if (!ok) break;
+                        load_window(plan, x.y, (x.z - kt) * kTileT, (float*)(raw + S::kBias) + (windows & 1) * 256);
+                        mbar_arrive(smem_u32(&bars.bias_full[windows & 1]));
+                    }
+                    if (!ok) break;
+                }
             }
+            if (queries) wait_settled(smem_u32(&bars.q_full), (queries - 1) & 1, err);
         } else if (RICH && learned) {
             // sums of the diagonals of each pair of tiles, in the order of the tiles: by distance where there is room for all of them,
             // else by bucket
-            float* hist = (float*)(from + S::kHist);
-            for (int b = lane; b < 1024; b += 32) hist[b] = 0.f;
-            __syncwarp();
-            uint32_t diags = 0;
-            for (int it = 0; it < total; ++it) {
-                const int kt = k_first + it;
-                if (flat_at(kt)) continue;
-                if (!wait_all(&bars.diag_full[diags & 1], (diags / 2) & 1, abort, err)) break;
-                const float* diag = (const float*)(from + S::kDiag) + (diags & 1) * kRowWarps * 64;
+            float* hist = (float*)(raw + S::kHist);
+            const int width = dense ? 2 * dense_mid + 1 : a.n_buckets;
+            for (int i = lane; i < 2 * kRowWarps; i += 32) ((float*)(raw + S::kDiag))[i * 64 + 63] = 0.f;  // read below, never written
+            uint32_t diags = 0, read = 0;
+            DqReader reader;
+            DqItem item;
+            while (reader.next(item, bars, &ok, abort, err)) {
+                for (int b = lane; b < width; b += 32) hist[b] = 0.f;
+                __syncwarp();
+                for (int kt = item.first; ok && kt <= item.last; ++kt) {
+                    if (flat_at(item.tile, kt)) continue;
+                    ok = wait_all(&bars.diag_full[diags & 1], (diags / 2) & 1, abort, err);
+                    if (!ok) break;
+                    const float* diag = (const float*)(raw + S::kDiag) + (diags & 1) * kRowWarps * 64;
 #pragma unroll 1
-                for (int x = 0; x < 8; ++x) {
-                    const int d = 32 * x + lane - 127;  // of the pair of tiles
-                    float v = 0.f;
-                    int id = -1;
-                    if (d <= 127) {
-#pragma unroll 4
-                        for (int w = 0; w < kRowWarps; ++w) {
-                            const int own = d - 32 * (w % 4) + 32 * (w / 4);
-                            if (own >= -31 && own <= 31) v += diag[w * 64 + own + 31];
-                        }
-                        const int64_t far = min(max((int64_t)q0 - (int64_t)kt * kTileT + d, -a.reach), a.reach);
-                        if (dense) {
-                            // held within the table's reach the farther ones meet: one lane has them all
-                            const int64_t apart = (int64_t)q0 - (int64_t)kt * kTileT + d;
-                            if (apart > -a.reach && apart < a.reach) hist[far + dense_mid] += v, v = 0.f;
-                        } else {
-                            id = a.bucket[far + a.reach];
-                            if (id >= a.n_buckets) id = -1;
-                        }
-                    }
-                    if (dense) {
-                        const int64_t apart = (int64_t)q0 - (int64_t)kt * kTileT + d;
-                        float ends[2] = {apart <= -a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
-                        if (__any_sync(0xffffffffu, ends[0] != 0.f || ends[1] != 0.f)) {
+                    for (int x = 0; x < 8; ++x) {
+                        // row - column = 32 x - 127 + lane in the pair of tiles; 32 (row quarter - column quarter) is 32 (x - 3) with
+                        // lane - 31 left, or 32 (x - 4) with lane + 1
+                        float v = 0.f;
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
+                        for (int e = 0; e < 2; ++e)
 #pragma unroll
-                                for (int o = 16; o; o >>= 1) ends[e] += __shfl_xor_sync(0xffffffffu, ends[e], o);
-                                if (lane == 0) hist[e ? dense_mid + (int)min(a.reach, (int64_t)T - 1) : 0] += ends[e];
+                            for (int c = 0; c < 4; ++c) {
+                                const int r = c + x - 3 - e;
+                                if (r >= 0 && r < 4) v += diag[(c * 4 + r) * 64 + lane + 32 * e];
                             }
-                        }
-                        __syncwarp();
-                    }
-                    uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
-                    while (left) {
-                        const int who = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
-                        const bool in = id == who;
-                        float s = in ? v : 0.f;
+                        const int64_t apart = ((int64_t)item.tile - kt) * kTileT + 32 * x + lane - 127;
+                        const int64_t far = min(max(apart, -a.reach), a.reach);
+                        if (dense) {
+                            // the distances beyond the table's reach meet
+                            float ends[2] = {apart <= -a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
+                            if (apart > -a.reach && apart < a.reach && apart >= -dense_mid && apart <= dense_mid) hist[apart + dense_mid] += v;
+                            if (__any_sync(0xffffffffu, ends[0] != 0.f || ends[1] != 0.f)) {
 #pragma unroll
-                        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                        if (lane == 0) hist[who] += s;
-                        left &= ~__ballot_sync(0xffffffffu, in);
+                                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                                    for (int o = 16; o; o >>= 1) ends[e] += __shfl_xor_sync(0xffffffffu, ends[e], o);
+                                    if (lane == 0) hist[e ? 2 * dense_mid : 0] += ends[e];
+                                }
+                            }
+                            __syncwarp();
+                            continue;
+                        }
+                        int id = a.bucket[far + a.reach];
+                        if (id >= a.n_buckets) id = -1;
+                        uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
+                        while (left) {
+                            const int who = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
+                            const bool in = id == who;
+                            float s = in ? v : 0.f;
+#pragma unroll
+                            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                            if (lane == 0) hist[who] += s;
+                            left &= ~__ballot_sync(0xffffffffu, in);
+                        }
+                    }
+                    arrive_warp(&bars.diag_empty[diags & 1]);
+                    ++diags;
+                }
+                ok = ok && wait_all(&bars.flat_full, read++ & 1, abort, err);
+                if (!ok) break;
+                if (lane == 0) {
+                    for (int e = 0; e < 2; ++e) {
+                        float s = 0.f;
+                        for (int w = 0; w < kRowWarps; ++w) s += bars.flat[w][e];
+                        const int id = dense ? (e ? 2 * dense_mid : 0) : a.bucket[e ? 2 * a.reach : 0];
+                        if (dense || (id >= 0 && id < a.n_buckets)) hist[id] += s;
                     }
                 }
-                arrive_warp(&bars.diag_empty[diags & 1]);
-                ++diags;
+                arrive_warp(&bars.flat_empty);
+                float* mine = part + ((int64_t)item.h * a.N * tiles + (int64_t)item.n * tiles + item.tile) * width;
+                for (int b = lane; b < width; b += 32) mine[b] = hist[b];
+                __syncwarp();
             }
         }
     }
@@ -781,20 +937,6 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     if (warp == kRowWarps) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
-    } else if (RICH && warp == kRowWarps + 3 && learned) {
-        float* hist = (float*)(from + S::kHist);
-        if (lane == 0) {
-            for (int e = 0; e < 2; ++e) {
-                float s = 0.f;
-                for (int w = 0; w < kRowWarps; ++w) s += bars.flat[w][e];
-                const int id = dense ? (e ? 2 * dense_mid : 0) : a.bucket[e ? 2 * a.reach : 0];
-                if (dense || (id >= 0 && id < a.n_buckets)) hist[id] += s;
-            }
-        }
-        __syncwarp();
-        const int width = dense ? 2 * dense_mid + 1 : a.n_buckets;
-        float* mine = part + ((int64_t)h * a.N * tiles + (int64_t)n * tiles + tile) * width;
-        for (int b = lane; b < width; b += 32) mine[b] = hist[b];
     }
 }
 
@@ -846,12 +988,12 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     using Q = DqShape<HD, RICH>;
     if (cudaError_t e = smem_attr_once<attention_dkv_tc_kernel<HD, RICH>>(Kv::kSmem)) return e;
     if (cudaError_t e = smem_attr_once<attention_dq_tc_kernel<HD, RICH>>(Q::kSmem)) return e;
-    CUtensorMap q, k, v, g, dq, dk, dv;
+    CUtensorMap q, k, v, g, dk, dv;
     auto map = [&](CUtensorMap* m, const void* p, int64_t ld, int heads) {
         return attention_head_map(m, p, ld, heads, a.hd, a.T, a.N, kTileT);
     };
     if (!map(&q, a.Q, a.ld_q, a.H) || !map(&k, a.K, a.ld_k, a.KV) || !map(&v, a.V, a.ld_v, a.KV) || !map(&g, a.dO, a.ld_do, a.H) ||
-        !map(&dq, a.dQ, a.ld_dq, a.H) || !map(&dk, a.dK, a.ld_dk, a.KV) || !map(&dv, a.dV, a.ld_dv, a.KV))
+        !map(&dk, a.dK, a.ld_dk, a.KV) || !map(&dv, a.dV, a.ld_dv, a.KV))
         return cudaErrorInvalidValue;
     const int64_t tiles = (a.T + kTileT - 1) / kTileT;
     AttentionPlan plan;
@@ -865,8 +1007,11 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     const unsigned grid = (unsigned)((a.N * a.T * a.H + 256 / kLanes - 1) / (256 / kLanes));
     attention_stats_kernel<kLanes><<<grid, 256, 0, s>>>(a, FastDiv(a.H), (int)(a.N * a.T), stats);
     if (cudaError_t e = cudaGetLastError()) return e;
-    if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.H)), dim3(kThreads),
-                                       Q::kSmem, s, q, k, v, g, dq, a, plan, (const float*)stats, part, err))
+    DqItems items;
+    items.tiles = (int)tiles, items.total = (int)(tiles * a.N * a.H);
+    items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
+    if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())),
+                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, a, plan, items, (const float*)stats, part, err))
         return e;
     return launch_chained(true, attention_dkv_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.KV)), dim3(kThreads), Kv::kSmem, s, q,
                           k, v, g, dk, dv, a, plan, (const float*)stats, err);
