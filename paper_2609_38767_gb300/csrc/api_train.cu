@@ -79,8 +79,8 @@ tda_status check_attention(const tda_attention_desc* L, const char* who) {
     if (L->heads % L->kv_heads)
         return fail(TDA_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, L->kv_heads, L->heads);
     if (L->head_dim > kMaxHeadDim) return fail(TDA_ERR_UNSUPPORTED, "%s: head_dim %d > %d", who, L->head_dim, kMaxHeadDim);
-    // one CTA per 64 queries of a head
-    if (L->N * L->T > kMaxCount || L->N * ((L->T + 63) / 64) > (kMaxCount - 65536) / L->heads || L->N * L->T > (kMaxCount - 65536) / L->heads)
+    // one CTA per 64 queries of a head, and per 64 keys
+    if (L->N * L->T > kMaxCount || L->N * ((L->T + 63) / 64) > (kMaxCount - 65536) / 2 / L->heads || L->N * L->T > (kMaxCount - 65536) / L->heads)
         return fail(TDA_ERR_INVALID_ARG, "%s: too many tokens or heads (N=%lld T=%lld heads=%d)", who, (long long)L->N,
                     (long long)L->T, L->heads);
     if (!float_type(L->dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);

@@ -40,15 +40,37 @@ __device__ __forceinline__ float row_max(float v) {
 }
 
 // Rows [first, first + 64) of one head into shared memory as fp32, zeros past the example, past hd, and for rows
-// that `live` leaves out (a token that nothing sees may hold anything, and zero times NaN is NaN).
+// that `live` leaves out (a token that nothing sees may hold anything, and zero times NaN is NaN). vec: fp32 rows on 16 bytes.
 template <typename T, int HD>
 __device__ __forceinline__ void load_tile(float* dst, const void* src, int64_t ld, int64_t row0, int first, int rows, int col,
-                                          int hd, const uint8_t* live) {
+                                          int hd, const uint8_t* live, bool vec) {
     const T* p = (const T*)src + (row0 + first) * ld + col;
+    if (sizeof(T) == 4 && vec) {
+        constexpr int kQuads = HD / 4, kTimes = kTile * kQuads / kThreads;
+        float4 v[kTimes];
+#pragma unroll
+        for (int k = 0; k < kTimes; ++k) {
+            const int i = threadIdx.x + k * kThreads, r = i / kQuads, c = i % kQuads * 4;
+            v[k] = first + r < rows && c < hd && (!live || live[r]) ? *(const float4*)((const float*)p + r * ld + c)
+                                                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < kTimes; ++k) {
+            const int i = threadIdx.x + k * kThreads, r = i / kQuads, c = i % kQuads * 4;
+            *(float4*)&dst[r * (HD + 4) + c] = v[k];
+        }
+        return;
+    }
+#pragma unroll 4
     for (int i = threadIdx.x; i < kTile * HD; i += kThreads) {
         const int r = i / HD, c = i % HD;
         dst[r * (HD + 4) + c] = first + r < rows && c < hd && (!live || live[r]) ? wide(p[r * ld + c]) : 0.f;
     }
+}
+// Whether an fp32 tensor's rows and heads start on 16 bytes.
+template <typename T>
+__device__ __forceinline__ bool vectors(const void* p, int64_t ld, int hd) {
+    return sizeof(T) == 4 && (((uint64_t)p | (uint64_t)(ld * 4)) & 15) == 0 && hd % 4 == 0;
 }
 
 // s[r][c] = a_row . b_row for rows ty + 16 r of A and tx + 16 c of B.
@@ -184,7 +206,7 @@ __device__ __forceinline__ void mark_keys(Small& m, int k0) {
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void attention_kernel(const Attention a) {
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(const Attention a) {
     extern __shared__ __align__(16) float sm[];
     float *Q = sm, *K = Q + kTile * (HD + 4), *V = K + kTile * (HD + 4), *P = V + kTile * (HD + 4);
     Small& m = *(Small*)(P + kTile * (kTile + 4));
@@ -193,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const Attention a) 
     const int n = (int)(blockIdx.x % heads) / a.H, h = (int)(blockIdx.x % heads) % a.H, kv = h / (a.H / a.KV);
     const int64_t row0 = n * a.T;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16, rows = (int)a.T;
-    load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, nullptr);
+    load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, nullptr, vectors<T>(a.Q, a.ld_q, a.hd));
     load_rows(a, m, row0, q0);
     float acc[4][HD / 16], top[4], sum[4];
 #pragma unroll
@@ -202,10 +224,11 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const Attention a) 
 #pragma unroll
         for (int c = 0; c < HD / 16; ++c) acc[r][c] = 0.f;
     }
+    const uint8_t* live = a.range ? m.live : nullptr;
     for (int k0 = m.lo / kTile * kTile; k0 < m.hi; k0 += kTile) {
-        mark_keys(m, k0);
-        load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, m.live);
-        load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, m.live);
+        if (live) mark_keys(m, k0);
+        load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.K, a.ld_k, a.hd));
+        load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.V, a.ld_v, a.hd));
         load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
         __syncthreads();
         float s[4][4];
@@ -292,18 +315,17 @@ __device__ __forceinline__ void gradient(const Attention& a, const Small& m, int
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void attention_dq_kernel(const Attention a, const float* delta, float* part) {
-    extern __shared__ __align__(16) float sm[];
+__device__ __forceinline__ void dq_tile(const Attention& a, const float* delta, float* part, int block, float* sm) {
     float *Q = sm, *K = Q + kTile * (HD + 4), *V = K + kTile * (HD + 4), *G = V + kTile * (HD + 4);
     float* S = G + kTile * (HD + 4);
     Small& m = *(Small*)(S + kTile * (kTile + 4));
     const int tiles = (int)((a.T + kTile - 1) / kTile), heads = (int)(a.N * a.H);
-    const int q0 = (tiles - 1 - (int)(blockIdx.x / heads)) * kTile;
-    const int n = (int)(blockIdx.x % heads) / a.H, h = (int)(blockIdx.x % heads) % a.H, kv = h / (a.H / a.KV);
+    const int q0 = (tiles - 1 - (int)(block / heads)) * kTile;
+    const int n = (int)(block % heads) / a.H, h = (int)(block % heads) % a.H, kv = h / (a.H / a.KV);
     const int64_t row0 = n * a.T;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16, rows = (int)a.T;
-    load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, nullptr);
-    load_tile<T, HD>(G, a.dO, a.ld_do, row0, q0, rows, h * a.hd, a.hd, nullptr);
+    load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, nullptr, vectors<T>(a.Q, a.ld_q, a.hd));
+    load_tile<T, HD>(G, a.dO, a.ld_do, row0, q0, rows, h * a.hd, a.hd, nullptr, vectors<T>(a.dO, a.ld_do, a.hd));
     load_rows(a, m, row0, q0);
     load_stats(a, m, delta, n, h, q0);
     const bool learned = a.dtable != nullptr;
@@ -316,10 +338,11 @@ __global__ __launch_bounds__(kThreads) void attention_dq_kernel(const Attention 
     float* mine = part + ((int64_t)h * a.N * tiles + (int64_t)n * tiles + q0 / kTile) * a.n_buckets;
     if (learned)
         for (int b = threadIdx.x; b < a.n_buckets; b += kThreads) mine[b] = 0.f;
+    const uint8_t* live = a.range ? m.live : nullptr;
     for (int k0 = m.lo / kTile * kTile; k0 < m.hi; k0 += kTile) {
-        mark_keys(m, k0);
-        load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, m.live);
-        load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, m.live);
+        if (live) mark_keys(m, k0);
+        load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.K, a.ld_k, a.hd));
+        load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.V, a.ld_v, a.hd));
         load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
         __syncthreads();
         float s[4][4], dp[4][4], ds[4][4], p;
@@ -367,17 +390,16 @@ __global__ __launch_bounds__(kThreads) void attention_dq_kernel(const Attention 
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void attention_dkv_kernel(const Attention a, const float* delta) {
-    extern __shared__ __align__(16) float sm[];
+__device__ __forceinline__ void dkv_tile(const Attention& a, const float* delta, int block, float* sm) {
     float *Q = sm, *K = Q + kTile * (HD + 4), *V = K + kTile * (HD + 4), *G = V + kTile * (HD + 4);
     float *P = G + kTile * (HD + 4), *S = P + kTile * (kTile + 4);
     Small& m = *(Small*)(S + kTile * (kTile + 4));
     const int heads = (int)(a.N * a.KV), group = a.H / a.KV;
-    const int k0 = (int)(blockIdx.x / heads) * kTile, n = (int)(blockIdx.x % heads) / a.KV, kv = (int)(blockIdx.x % heads) % a.KV;
+    const int k0 = (int)(block / heads) * kTile, n = (int)(block % heads) / a.KV, kv = (int)(block % heads) % a.KV;
     const int64_t row0 = n * a.T;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16, rows = (int)a.T;
-    load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, nullptr);
-    load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, nullptr);
+    load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, nullptr, vectors<T>(a.K, a.ld_k, a.hd));
+    load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, nullptr, vectors<T>(a.V, a.ld_v, a.hd));
     float dk[4][HD / 16], dv[4][HD / 16];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -393,8 +415,8 @@ __global__ __launch_bounds__(kThreads) void attention_dkv_kernel(const Attention
         }
         if (!__syncthreads_or(any)) continue;
         for (int h = kv * group; h < (kv + 1) * group; ++h) {
-            load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, m.live);
-            load_tile<T, HD>(G, a.dO, a.ld_do, row0, q0, rows, h * a.hd, a.hd, m.live);
+            load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, a.range ? m.live : nullptr, vectors<T>(a.Q, a.ld_q, a.hd));
+            load_tile<T, HD>(G, a.dO, a.ld_do, row0, q0, rows, h * a.hd, a.hd, a.range ? m.live : nullptr, vectors<T>(a.dO, a.ld_do, a.hd));
             load_stats(a, m, delta, n, h, q0);
             load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
             __syncthreads();
@@ -419,6 +441,16 @@ __global__ __launch_bounds__(kThreads) void attention_dkv_kernel(const Attention
     const float by[4] = {a.scale, a.scale, a.scale, a.scale}, one[4] = {1.f, 1.f, 1.f, 1.f};
     store_tile<T, HD>(a.dK, a.ld_dk, row0, k0, rows, kv * a.hd, a.hd, dk, by);
     store_tile<T, HD>(a.dV, a.ld_dv, row0, k0, rows, kv * a.hd, a.hd, dv, one);
+}
+
+// dK, dV of a tile of keys, or dQ of a tile of queries: the two kinds of CTAs in one launch, so that an SM has one of either (2 x 515
+// tokens of 8 heads fp32 one after the other 202 + 175 us).
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads, HD == 64 ? 2 : 1) void attention_grad_kernel(const Attention a, const float* delta, float* part,
+                                                                                   int kv_tiles) {
+    extern __shared__ __align__(16) float sm[];
+    if ((int)blockIdx.x < kv_tiles) dkv_tile<T, HD>(a, delta, blockIdx.x, sm);
+    else dq_tile<T, HD>(a, delta, part, blockIdx.x - kv_tiles, sm);
 }
 
 // dtable[b][h] = beta dtable[b][h] + the sum of head h's partial sums, in order: a warp per entry, 32 running sums joined
@@ -689,14 +721,12 @@ cudaError_t join_table(const Attention& a, const float* part, int64_t rows, cuda
 
 template <typename T, int HD>
 cudaError_t backward_simt(const Attention& a, float* delta, float* part, cudaStream_t s) {
-    constexpr size_t smem_q = smem_of<HD>(4, 1), smem_kv = smem_of<HD>(4, 2);
-    if (cudaError_t e = smem_attr_once<attention_dq_kernel<T, HD>>(smem_q)) return e;
-    if (cudaError_t e = smem_attr_once<attention_dkv_kernel<T, HD>>(smem_kv)) return e;
+    constexpr size_t smem = smem_of<HD>(4, 2);
+    if (cudaError_t e = smem_attr_once<attention_grad_kernel<T, HD>>(smem)) return e;
     const int64_t tiles = (a.T + kTile - 1) / kTile;
-    note_launches(3);
+    note_launches(2);
     attention_delta_kernel<T><<<(unsigned)((a.N * a.T * a.H + 7) / 8), 256, 0, s>>>(a, delta);
-    attention_dq_kernel<T, HD><<<(unsigned)(tiles * a.N * a.H), kThreads, smem_q, s>>>(a, delta, part);
-    attention_dkv_kernel<T, HD><<<(unsigned)(tiles * a.N * a.KV), kThreads, smem_kv, s>>>(a, delta);
+    attention_grad_kernel<T, HD><<<(unsigned)(tiles * a.N * (a.KV + a.H)), kThreads, smem, s>>>(a, delta, part, (int)(tiles * a.N * a.KV));
     if (cudaError_t e = cudaGetLastError()) return e;
     return join_table(a, part, a.N * tiles, s);
 }
