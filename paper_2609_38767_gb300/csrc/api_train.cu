@@ -68,11 +68,11 @@ tda_status check_ws(const void* ws, size_t ws_bytes, size_t need, const char* wh
 }
 
 constexpr int kMaxHeadDim = 128;
-constexpr int64_t kMaxReach = 1 << 20, kMaxBuckets = 1024;
+constexpr int64_t kMaxReach = 1 << 20, kMaxBuckets = 1024, kMaxTokens = 1 << 29;  // a window of distances is 2 T + 513 long
 
 tda_status check_attention(const tda_attention_desc* L, const char* who) {
     if (!L) return fail(TDA_ERR_INVALID_ARG, "%s: attention descriptor is NULL", who);
-    if (L->N < 0 || L->T < 0 || L->N > kMaxCount || L->T > kMaxCount || L->heads < 1 || L->heads > 65535 || L->kv_heads < 1 ||
+    if (L->N < 0 || L->T < 0 || L->N > kMaxCount || L->T > kMaxTokens || L->heads < 1 || L->heads > 65535 || L->kv_heads < 1 ||
         L->head_dim < 1)
         return fail(TDA_ERR_INVALID_ARG, "%s: bad sizes N=%lld T=%lld heads=%d kv_heads=%d head_dim=%d", who, (long long)L->N,
                     (long long)L->T, L->heads, L->kv_heads, L->head_dim);
@@ -80,7 +80,7 @@ tda_status check_attention(const tda_attention_desc* L, const char* who) {
         return fail(TDA_ERR_INVALID_ARG, "%s: kv_heads=%d does not divide heads=%d", who, L->kv_heads, L->heads);
     if (L->head_dim > kMaxHeadDim) return fail(TDA_ERR_UNSUPPORTED, "%s: head_dim %d > %d", who, L->head_dim, kMaxHeadDim);
     // one CTA per 64 queries of a head, and per 64 keys
-    if (L->N * L->T > kMaxCount || L->N * ((L->T + 63) / 64) > (kMaxCount - 65536) / 2 / L->heads || L->N * L->T > (kMaxCount - 65536) / L->heads)
+    if ((L->T && L->N > (kMaxCount - 65536) / L->heads / L->T) || L->N * ((L->T + 63) / 64) > (kMaxCount - 65536) / 2 / L->heads)
         return fail(TDA_ERR_INVALID_ARG, "%s: too many tokens or heads (N=%lld T=%lld heads=%d)", who, (long long)L->N,
                     (long long)L->T, L->heads);
     if (!float_type(L->dtype)) return fail(TDA_ERR_INVALID_ARG, "%s: dtype must be TDA_F32 or TDA_BF16", who);

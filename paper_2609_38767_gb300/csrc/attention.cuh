@@ -57,7 +57,7 @@ __device__ __forceinline__ int2 visible(const int2* range, int causal, int T, in
     if (i >= T) return make_int2(0, 0);
     if (range) {
         const int2 r = range[row0 + i];
-        return make_int2(max(r.x, 0), min(r.y, T));
+        return make_int2(min(max(r.x, 0), T), min(max(r.y, 0), T));  // both ways: differences of the ends fit an int then
     }
     return make_int2(0, causal ? i + 1 : T);
 }

@@ -540,7 +540,7 @@ __device__ __forceinline__ int scan(int v, int identity, int* parts) {
 
 // Up to 8192 tokens: one CTA per example, EACH tokens a thread in registers, and the three steps of the kernel below at once:
 // scans over the warps' tokens, over the warps by each warp, and the ends of the prefixes through shared memory.
-// 4 x 2047 tokens XX us (the kernel below 12).
+// 4 x 2047 tokens 5 us (the kernel below 12).
 template <int EACH>
 __global__ __launch_bounds__(kScan) void attention_ranges_short_kernel(const int32_t* doc, const int32_t* prefix, int causal, int T,
                                                                        int64_t window, int2* range) {

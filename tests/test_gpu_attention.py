@@ -248,6 +248,96 @@ def test_equal_calls_give_equal_bits(dev):
             assert all(torch.equal(x, y) for x, y in zip(got[0], other))
 
 
+MORE = [
+    ((12, 300, 16, 4, 128), "docs", 20.0, 32, 128, True),   # items over several rounds, a row of scores over two warps
+    ((40, 129, 8, 8, 64), "any", 5.0, 300, 60, False),
+    ((1, 1300, 2, 1, 64), "causal", 0.0, 1024, 2000, False),  # distances that are summed by bucket
+    ((2, 700, 4, 2, 128), "docs", 30.0, 600, 699, True),
+    ((1, 600, 2, 2, 40), "full", 0.0, 33, 560, False),
+    ((1, 1500, 3, 3, 64), "window", 50.0, 2, 0, False),       # one distance for all
+]
+
+
+@pytest.mark.parametrize("shape,mask,cap,buckets,reach,slope", MORE)
+def test_many_items_and_wide_tables(dev, shape, mask, cap, buckets, reach, slope):
+    p = Problem(dev, *shape, BF, mask, cap, buckets, reach, slope)
+    f, b = check_forward(p)
+    check_backward(p, f, b, beta=0.5, grad=F32)
+
+
+@pytest.mark.parametrize("mask", ["causal", "any"])
+def test_long(dev, mask):
+    p = Problem(dev, 1, 6001, 2, 1, 64, BF, mask)
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+
+
+@pytest.mark.parametrize("dtype,hd", [(BF, 64), (BF, 28), (F32, 64)])
+def test_offsets_past_32_bits(dev, dtype, hd):
+    """Rows 2^25 bytes and more apart: the last ones lie past 2^32 bytes, with 130 rows past 2^31 values."""
+    p = Problem(dev, 2, 65, 1, 1, hd, dtype, "docs", layout=((1 << 24) + 64 - hd, 8))
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_wild_ranges(dev, dtype):
+    """Ranges with ends anywhere in 32 bits are clamped."""
+    p = Problem(dev, 2, 200, 2, 1, 64, dtype, "full")
+    g = torch.Generator().manual_seed(3)
+    ends = torch.tensor([-2 ** 31, -2 ** 31 + 1, -1, 0, 1, 63, 64, 128, 199, 200, 201, 2 ** 31 - 2, 2 ** 31 - 1])
+    p.range = ends[torch.randint(0, len(ends), (2, 200, 2), generator=g)].int().to(dev)
+    p.L.causal = 1  # not read
+    at = torch.arange(200, device=dev)
+    p.seen = (at >= p.range[..., :1]) & (at < p.range[..., 1:])
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_one_tensor_for_all(dev, dtype):
+    p = Problem(dev, 2, 150, 2, 2, 64, dtype, "causal")
+    p.K = p.V = p.Q
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+
+
+def test_two_calls_at_once(dev):
+    """Two batches on two streams, each with its workspace, as calls and as graphs, many times over each other."""
+    ps = [Problem(dev, 3, 700, 8, 2, 64, BF, "docs", 20.0, 16, 64, seed=s) for s in (1, 2)]
+    names = ("O", "lse", "dQ", "dK", "dV", "dtable")
+    want = []
+    for p in ps:
+        p.forward()
+        p.backward()
+        want.append([getattr(p, x).clone() for x in names])
+    streams = [torch.cuda.Stream() for _ in ps]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, s in zip(ps, streams):
+            with torch.cuda.stream(s):
+                p.forward()
+                p.backward()
+    torch.cuda.synchronize()
+    for p, w in zip(ps, want):
+        assert all(torch.equal(getattr(p, x), y) for x, y in zip(names, w))
+    graphs = []
+    for p in ps:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            p.forward()
+            p.backward()
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    tda.tda_device_status()
+    torch.cuda.synchronize()
+    for p, w in zip(ps, want):
+        assert all(torch.equal(getattr(p, x), y) for x, y in zip(names, w))
+
+
 def test_no_lse_and_empty_batches(dev):
     p = Problem(dev, 1, 90, 2, 1, 64, BF, "causal")
     p.forward()

@@ -160,3 +160,31 @@ def test_nan_stays_in_its_row(dev):
     tda.tda_rmsnorm_forward(tda.TDA_F32, x, 600, None, 0, 40, 600, w, EPS, None, 0, y, 600)
     bad = ~torch.isfinite(y).all(1)
     assert bad[3] and bad[7] and bad.sum() == 2
+
+
+@pytest.mark.parametrize("M,d", [(263000, 8192), (5000000, 8)])
+def test_many_rows(dev, M, d):
+    """Rows past 2^31 values, and millions of short ones; the last rows and the weight's gradient against 64 bits."""
+    g = torch.Generator(device=dev).manual_seed(1)
+    x = torch.randn((1000, d), generator=g, device=dev).bfloat16().repeat(M // 1000, 1)  # a thousand rows over and over
+    dy, w = x.roll(1, 0), torch.randn(d, generator=g, device=dev).bfloat16()
+    y, dx = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    rstd, dw = torch.empty(M, device=dev), torch.empty(d, device=dev)
+    tda.tda_rmsnorm_forward(tda.TDA_BF16, x, d, None, 0, M, d, w, EPS, None, 0, y, d, rstd)
+    wsb = tda.tda_rmsnorm_workspace_size(M, d)
+    ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
+    tda.tda_rmsnorm_backward(tda.TDA_BF16, x, d, rstd, w, dy, d, None, 0, M, d, dx, d, dw, tda.TDA_F32, 0.0, ws, wsb)
+    for out in (y, dx):  # equal rows give equal bits
+        blocks = out.view(M // 1000, 1000, d)
+        assert torch.equal(blocks[1:-1], blocks[1:2].expand(M // 1000 - 2, 1000, d)) and torch.equal(blocks[-1, 1:], blocks[1, 1:])
+    a, b = x[-1000:].to(D), dy[-1000:].to(D)
+    by = 1 / (a.square().mean(1, keepdim=True) + EPS).sqrt()
+    n, gr = a * by, b * w.to(D)
+    want = n * w.to(D)
+    assert ((y[-1000:].to(D) - want).abs() <= (2.0 ** -8 + 8 * 2.0 ** -24) * want.abs()).all()
+    s = (gr * n).mean(1, keepdim=True)
+    want, size = by * (gr - n * s), by * (gr.abs() + n.abs() * (gr * n).abs().mean(1, keepdim=True))
+    assert ((dx[-1000:].to(D) - want).abs() <= 2.0 ** -8 * want.abs() + 64 * 2.0 ** -24 * size).all()
+    # every row has all others' terms in its column; a CTA adds up to M / 152 rows one after the other, then 608 shares
+    total, size = (b * n).sum(0) * (M // 1000), (b * n).abs().sum(0) * (M // 1000)
+    assert ((dw.to(D) - total).abs() <= (M / 152 + 608) * 2.0 ** -24 * size).all()
