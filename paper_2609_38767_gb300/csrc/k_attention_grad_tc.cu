@@ -442,7 +442,7 @@ struct DqShape {
 };
 struct DqBars {
     uint64_t item_full[4], item_empty[4], q_full, q_empty, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free,
-        ds_ready, dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, done;
+        ds_ready[2], dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, done;
     int4 items[4][2];
     float flat[kRowWarps][2];
     uint32_t tmem;
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             for (uint64_t* b : {&bars.q_full, &bars.q_empty, &bars.s_full[0], &bars.s_full[1], &bars.dp_full, &bars.dq_done, &bars.done,
                                 &bars.diag_empty[0], &bars.diag_empty[1], &bars.flat_empty})
                 mbar_init(smem_u32(b), 1);
-            for (uint64_t* b : {&bars.dp_free, &bars.ds_ready, &bars.diag_full[0], &bars.diag_full[1], &bars.bias_empty[0],
+            for (uint64_t* b : {&bars.dp_free, &bars.ds_ready[0], &bars.ds_ready[1], &bars.diag_full[0], &bars.diag_full[1], &bars.bias_empty[0],
                                 &bars.bias_empty[1], &bars.flat_full})
                 mbar_init(smem_u32(b), kRowWarps);
             for (uint64_t* b : {&bars.bias_full[0], &bars.bias_full[1]}) mbar_init(smem_u32(b), 32);
@@ -674,7 +674,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 tmem_st16(ts, w);
                 tmem_wait_st();
                 tc_fence_before();
-                arrive_warp(&bars.ds_ready);
+                // two barriers in turn: a warp may be done with the next pair of tiles (dP is free as soon as all have read it) before another,
+                // which has diagonals to sum, is with this one
+                arrive_warp(&bars.ds_ready[it & 1]);
             }
             if (!ok) break;
             if constexpr (RICH) {
@@ -788,7 +790,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                     if (then.kt == then.last) commit(lead, smem_u32(&bars.q_empty));
                 }
                 if (now.valid) {
-                    ok = wait_all(&bars.ds_ready, it & 1, abort, err);
+                    ok = wait_all(&bars.ds_ready[it & 1], (it / 2) & 1, abort, err);
                     if (!ok) break;
                     tc_fence_after();
                     mma_quarters(lead, tdQ, tmem + (it & 1) * 128, sk + it % S::kK * kBytes, kIdO, now.kt == now.item.first);

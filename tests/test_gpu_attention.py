@@ -338,6 +338,14 @@ def test_two_calls_at_once(dev):
         assert all(torch.equal(getattr(p, x), y) for x, y in zip(names, w))
 
 
+def test_warps_that_run_ahead(dev):
+    """Pairs of tiles with diagonals to sum beside pairs without: the fast warps' weights never stand in for the slow ones'."""
+    p = Problem(dev, 1, 700, 4, 1, 64, BF, "full", 30.0, 5, 40, sigma=4.0)
+    f, b = check_forward(p)
+    for _ in range(40):
+        check_backward(p, f, b)
+
+
 def test_no_lse_and_empty_batches(dev):
     p = Problem(dev, 1, 90, 2, 1, 64, BF, "causal")
     p.forward()
