@@ -31,6 +31,9 @@ struct Attention {
     int64_t ld_do, ld_dq, ld_dk, ld_dv;
     tda_dtype gt;
     float beta;
+    // tensor-core kernels with a cap: tanh(x / cap) of a dot product d up to near_limit is d P(d^2), times what the kernel wants
+    float near_limit;
+    float2 near[5];  // P's coefficients, the highest first, in pairs as the instructions take them
 };
 
 // Division of numbers below 2^31 by a number that a launch knows.
@@ -111,6 +114,8 @@ cudaError_t launch_attention_ranges(int64_t N, int64_t T, const int32_t* doc, co
                                     int64_t window, int2* range, cudaStream_t s);
 
 bool attention_tc_supported(const Attention& a, bool backward);
+// a.near_limit and a.near for d P(d^2) = by * tanh(d scale / cap).
+void attention_near(Attention& a, float by);
 size_t attention_plan_bytes(const Attention& a, bool bound);
 // Fills the plan; *chained: a kernel was launched, the next may be chained to it.
 cudaError_t launch_attention_plan(const Attention& a, void* ws, AttentionPlan* plan, bool* chained, cudaStream_t s);

@@ -118,16 +118,16 @@ __device__ __forceinline__ float rcp_fast(float x) {
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c);
 __device__ __forceinline__ float2 mul2(float2 a, float2 b);
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-// tanh of two values. |x| <= 1/2: x P(x^2), P fitted to a relative error of 2^-23.1, six instructions a pair; any x:
-// 1 - 2 / (1 + e^2x), right at both infinities, 2^-22 absolute, two special functions a value beside its weight's exponential, of
-// which the SM has 32 (exp2) and 16 (reciprocal) a cycle.
-__device__ __forceinline__ float2 tanh_near(float2 x) {
-    const float2 z = mul2(x, x);
-    float2 p = fma2(z, both(0.017135003581643105f), both(-0.05298607423901558f));
-    p = fma2(z, p, both(0.13324779272079468f));
-    p = fma2(z, p, both(-0.3333306908607483f));
-    p = fma2(z, p, both(1.f));
-    return mul2(x, p);
+// d P(d^2) for two dot products within a.near_limit, |x| <= 1/2: tanh to a relative error of 2^-23.1 (the fit is in
+// attention_near), five instructions a pair and the caller's product with d. Any x: 1 - 2 / (1 + e^2x), right at both
+// infinities, 2^-22 absolute, two special functions a value beside its weight's exponential, of which the SM has 32 (exp2) and
+// 16 (reciprocal) a cycle.
+__device__ __forceinline__ float2 tanh_near(const Attention& a, float2 d) {
+    const float2 z = mul2(d, d);
+    float2 p = fma2(z, a.near[0], a.near[1]);
+    p = fma2(z, p, a.near[2]);
+    p = fma2(z, p, a.near[3]);
+    return fma2(z, p, a.near[4]);
 }
 __device__ __forceinline__ float2 tanh_any(float2 x) {
     const float k = 2.f * kLog2e;
@@ -146,13 +146,13 @@ __device__ __forceinline__ float largest(const float* x, float m) {
     for (int j = 0; j < N; j += 4) u = max3(u, x[j], x[j + 1]), v = max3(v, x[j + 2], x[j + 3]);
     return fmaxf(u, v);
 }
-// Whether all of a warp's 32 x N dot products stay within the near range.
+// Whether all of a warp's 32 x N dot products stay within a limit.
 template <int N>
-__device__ __forceinline__ bool all_near(const float* x, float inv_cap) {
+__device__ __forceinline__ bool all_near(const float* x, float limit) {
     float u = 0.f, v = 0.f;
 #pragma unroll
     for (int j = 0; j < N; j += 4) u = max3(u, fabsf(x[j]), fabsf(x[j + 1])), v = max3(v, fabsf(x[j + 2]), fabsf(x[j + 3]));
-    return __all_sync(0xffffffffu, !(fmaxf(u, v) * inv_cap > 0.5f));
+    return __all_sync(0xffffffffu, fmaxf(u, v) <= limit);
 }
 // Two bf16 of a column of TMEM, the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -206,6 +206,29 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int panels, const uint
     }
     fence_proxy_async();
     __syncwarp();
+}
+
+// A window has the biases of a pair of tiles by distance, so that what row r reads for column j is V[128 - r + j]. Four copies, each
+// one value behind the other: 4 columns are a 16-byte load for every row, and the copies lie on banks such that 8 rows, which read
+// two pieces of a copy each, find 8 pieces beside one another.
+constexpr int kWindow = 4 * 288;
+__device__ __forceinline__ int copy_of(int c) { return c * 256 + (c == 0 ? 0 : 4 + 8 * c); }
+__device__ __forceinline__ int window_row(int row) { return copy_of(-row & 3) + (128 - row & ~3); }
+// The window of a pair of tiles q0 - k0 apart (a warp's work); BY_QUERY: rows are queries, else keys.
+template <bool BY_QUERY>
+__device__ __forceinline__ void load_window(const AttentionPlan& plan, int h, int apart, float* dst) {
+    const int lane = threadIdx.x % 32;
+    const float* src = plan.lut + (int64_t)h * plan.lut_len + plan.lut_mid + min(max(apart, -plan.reach - 127), plan.reach + 127) - 127;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = src[min(32 * e + lane, 254)];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int at = BY_QUERY ? 255 - 32 * e - lane : 32 * e + lane + 1;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (at >= c && at < 256) dst[copy_of(c) + at - c] = v[e];
+    }
 }
 
 // wait_bounded by a whole warp, its outcome the same in all lanes, in few instructions: the many roles of these kernels share the

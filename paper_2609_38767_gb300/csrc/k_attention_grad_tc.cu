@@ -74,40 +74,38 @@ __device__ __forceinline__ uint32_t bits_of(int lo, int hi) {
     lo = min(max(lo, 0), 32), hi = min(max(hi, 0), 32);
     return lo < hi ? (hi == 32 ? ~0u : (1u << hi) - 1) & (~0u << lo) : 0u;
 }
-// Scores times log2 e of a thread's 32 dot products, and in RICH the cap's slope less its sign, t^2 - 1; bias(j): what the pairs
-// j and j + 1 get beside.
+__device__ __forceinline__ float4 add4(float4 a, float4 b) {
+    const float2 x = add2(make_float2(a.x, a.y), make_float2(b.x, b.y)), y = add2(make_float2(a.z, a.w), make_float2(b.z, b.w));
+    return make_float4(x.x, x.y, y.x, y.y);
+}
+// Scores times log2 e of a thread's 32 dot products, and in RICH the cap's slope less its sign, t^2 - 1; bias(j): what columns
+// j to j + 3 get beside.
 template <bool RICH, typename F>
 __device__ __forceinline__ void scores_of(const Attention& a, float inv_cap, float* s, float* bend, F&& bias) {
     const float2 c2 = both(a.scale * kLog2e), cap2 = both(a.cap * kLog2e);
     if (RICH && a.cap > 0.f) {
         auto all = [&](auto tanh_of) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                const float2 t = tanh_of(mul2(make_float2(s[j], s[j + 1]), both(inv_cap)));
-                const float2 x = fma2(t, cap2, bias(j));
-                const float2 b = fma2(t, t, both(-1.f));
-                s[j] = x.x, s[j + 1] = x.y, bend[j] = b.x, bend[j + 1] = b.y;
+            for (int j = 0; j < 32; j += 4) {
+                const float4 more = bias(j);
+                const float2 t = tanh_of(make_float2(s[j], s[j + 1])), u = tanh_of(make_float2(s[j + 2], s[j + 3]));
+                const float2 x = fma2(t, cap2, make_float2(more.x, more.y)), y = fma2(u, cap2, make_float2(more.z, more.w));
+                const float2 b = fma2(t, t, both(-1.f)), c = fma2(u, u, both(-1.f));
+                s[j] = x.x, s[j + 1] = x.y, s[j + 2] = y.x, s[j + 3] = y.y;
+                bend[j] = b.x, bend[j + 1] = b.y, bend[j + 2] = c.x, bend[j + 3] = c.y;
             }
         };
-        if (all_near<32>(s, inv_cap)) all([](float2 x) { return tanh_near(x); });
-        else all([](float2 x) { return tanh_any(x); });
+        if (all_near<32>(s, a.near_limit)) all([&](float2 d) { return mul2(d, tanh_near(a, d)); });
+        else all([&](float2 d) { return tanh_any(mul2(d, both(inv_cap))); });
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const float2 x = fma2(make_float2(s[j], s[j + 1]), c2, bias(j));
-            s[j] = x.x, s[j + 1] = x.y;
+        for (int j = 0; j < 32; j += 4) {
+            const float4 more = bias(j);
+            const float2 x = fma2(make_float2(s[j], s[j + 1]), c2, make_float2(more.x, more.y));
+            const float2 y = fma2(make_float2(s[j + 2], s[j + 3]), c2, make_float2(more.z, more.w));
+            s[j] = x.x, s[j + 1] = x.y, s[j + 2] = y.x, s[j + 3] = y.y;
         }
     }
-}
-// The window of 255 biases of a pair of tiles q0 - k0 apart (a warp's work).
-__device__ __forceinline__ void load_window(const AttentionPlan& plan, int h, int apart, float* dst) {
-    const int lane = threadIdx.x % 32;
-    const float* src = plan.lut + (int64_t)h * plan.lut_len + plan.lut_mid + min(max(apart, -plan.reach - 127), plan.reach + 127) - 127;
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = src[min(32 * e + lane, 254)];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) dst[32 * e + lane] = v[e];
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
@@ -142,8 +140,8 @@ template <int HD, bool RICH>
 struct DkvShape {
     static constexpr int kQ = HD == 64 ? 5 : RICH ? 2 : 3, kG = HD == 64 ? 4 : 2;
     static constexpr uint32_t kStats = (2 + kQ + kG) * Tiles<HD>::kBytes;
-    static constexpr uint32_t kBias = kStats + kG * kStatBytes;  // RICH: 2 windows of 256 biases
-    static constexpr uint32_t kBars = kBias + (RICH ? 2048 : 0), kSmem = kBars + 512;
+    static constexpr uint32_t kBias = kStats + kG * kStatBytes;  // RICH: 2 windows of biases
+    static constexpr uint32_t kBars = kBias + (RICH ? 8 * kWindow : 0), kSmem = kBars + 512;
 };
 struct DkvBars {
     uint64_t kv_full, q_full[5], q_empty[5], g_full[4], g_empty[4], s_full, p_ready, dp_full, ds_ready, bias_full[2], bias_empty[2], done;
@@ -239,7 +237,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
                 seen = more = a.causal ? bits_of(key - q0, 32) : ~0u;
                 if (q0 == 0 && (a.causal || T == 1)) more &= ~1u;
             }
-            const bool whole = __all_sync(0xffffffffu, more == ~0u);
+            const bool whole = __all_sync(0xffffffffu, more == ~0u), some = __any_sync(0xffffffffu, seen != 0);
             ok = wait_all(&bars.g_full[g], (x.it / S::kG) & 1, abort, err) && wait_all(&bars.s_full, x.it & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
@@ -251,30 +249,35 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
             if (RICH && plan.lut) {
                 ok = wait_all(&bars.bias_full[x.it & 1], (x.it / 2) & 1, abort, err);
                 if (!ok) break;
-                bias = (const float*)(raw + S::kBias) + (x.it & 1) * 256 + 127 + 32 * quarter - row;
+                bias = (const float*)(raw + S::kBias) + (x.it & 1) * kWindow + window_row(row) + 32 * quarter;
             }
             tmem_wait_ld();
             tmem_use(p);
-            if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add2(((const float2*)nl)[j / 2], make_float2(bias[j], bias[j + 1])); });
-            else scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return ((const float2*)nl)[j / 2]; });
-#pragma unroll
-            for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
-            if (!whole) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (!(seen >> j & 1)) p[j] = 0.f;
-            }
             uint32_t w[16];
+            if (some) {
+                if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add4(nl[j / 4], *(const float4*)(bias + j)); });
+                else scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return nl[j / 4]; });
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(p[j], p[j + 1]);
-            tmem_st16(ts, w);
-            if (RICH && a.cap > 0.f) {
+                for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
+                if (!whole) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    const float2 x = mul2(make_float2(p[j], p[j + 1]), make_float2(bend[j], bend[j + 1]));
-                    p[j] = x.x, p[j + 1] = x.y;
+                    for (int j = 0; j < 32; ++j)
+                        if (!(seen >> j & 1)) p[j] = 0.f;
                 }
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(p[j], p[j + 1]);
+                if (RICH && a.cap > 0.f) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 x = mul2(make_float2(p[j], p[j + 1]), make_float2(bend[j], bend[j + 1]));
+                        p[j] = x.x, p[j + 1] = x.y;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) w[j] = 0;
             }
+            tmem_st16(ts, w);
             tmem_wait_st();
             tc_fence_before();
             arrive_warp(&bars.p_ready);
@@ -282,24 +285,26 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
             ok = wait_all(&bars.dp_full, x.it & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
-            float d[32];
-            tmem_ld32(tp, d);
-            tmem_wait_ld();
-            tmem_use(d);
+            if (some) {
+                float d[32];
+                tmem_ld32(tp, d);
+                tmem_wait_ld();
+                tmem_use(d);
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                const float4 l = nd[j / 4];
-                const float2 u = mul2(add2(make_float2(d[j], d[j + 1]), make_float2(l.x, l.y)), make_float2(p[j], p[j + 1]));
-                const float2 v = mul2(add2(make_float2(d[j + 2], d[j + 3]), make_float2(l.z, l.w)), make_float2(p[j + 2], p[j + 3]));
-                d[j] = u.x, d[j + 1] = u.y, d[j + 2] = v.x, d[j + 3] = v.y;
-            }
-            if (!whole) {
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 l = nd[j / 4];
+                    const float2 u = mul2(add2(make_float2(d[j], d[j + 1]), make_float2(l.x, l.y)), make_float2(p[j], p[j + 1]));
+                    const float2 v = mul2(add2(make_float2(d[j + 2], d[j + 3]), make_float2(l.z, l.w)), make_float2(p[j + 2], p[j + 3]));
+                    d[j] = u.x, d[j + 1] = u.y, d[j + 2] = v.x, d[j + 3] = v.y;
+                }
+                if (!whole) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (!(more >> j & 1)) d[j] = 0.f;
-            }
+                    for (int j = 0; j < 32; ++j)
+                        if (!(more >> j & 1)) d[j] = 0.f;
+                }
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+                for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+            }  // else w is zeros still
             tmem_st16(tp, w);
             tmem_wait_st();
             tc_fence_before();
@@ -420,7 +425,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
         } else if (RICH && warp == kRowWarps + 2 && plan.lut) {
             for (Step x = begin(); x.it < total; next(x)) {
                 if (x.it >= 2 && !wait_all(&bars.bias_empty[x.it & 1], (x.it / 2 - 1) & 1, abort, err)) break;
-                load_window(plan, x.h, x.qt * kTileT - k0, (float*)(raw + S::kBias) + (x.it & 1) * 256);
+                load_window<false>(plan, x.h, x.qt * kTileT - k0, (float*)(raw + S::kBias) + (x.it & 1) * kWindow);
                 mbar_arrive(smem_u32(&bars.bias_full[x.it & 1]));
             }
         }
@@ -436,9 +441,10 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
 template <int HD, bool RICH>
 struct DqShape {
     static constexpr int kK = HD == 64 ? 4 : RICH ? 2 : 3, kV = HD == 64 ? 3 : 2;
-    static constexpr uint32_t kBias = (2 + kK + kV) * Tiles<HD>::kBytes;  // RICH: 2 windows of 256 biases, 2 x [16 warps][64]
-    static constexpr uint32_t kDiag = kBias + (RICH ? 2048 : 0);          // diagonals, the sums of an item
-    static constexpr uint32_t kHist = kDiag + (RICH ? 2 * kRowWarps * 64 * 4 : 0), kSmem = kHist + (RICH ? 1024 * 4 : 0);
+    static constexpr uint32_t kBias = (2 + kK + kV) * Tiles<HD>::kBytes;  // RICH: 2 windows of biases, 2 x [16 warps][64]
+    static constexpr uint32_t kDiag = kBias + (RICH ? 8 * kWindow : 0);  // diagonals, the sums of an item
+    static constexpr uint32_t kHalves = kDiag + (RICH ? 2 * kRowWarps * 64 * 4 : 0);  // a warp's diagonals of 16 columns each
+    static constexpr uint32_t kHist = kHalves + (RICH ? kRowWarps * 128 * 4 : 0), kSmem = kHist + (RICH ? 1024 * 4 : 0);
 };
 struct DqBars {
     uint64_t item_full[4], item_empty[4], q_full, q_empty, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free,
@@ -562,6 +568,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
         const float by = RICH && a.cap > 0.f ? -a.scale : a.scale;  // the slope's sign
         uint32_t it = 0, diags = 0, done = 0, written = 0;  // key tiles, diagonals, outputs, items' sums so far
+        float* halves = (float*)(raw + S::kHalves) + warp * 128;
+        if (learned)
+            for (int i = lane; i < 128; i += 32) halves[i] = 0.f;  // some are never written
         bool ok = true;
         DqReader reader;
         DqItem item, then;
@@ -590,6 +599,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 const bool whole = item.most <= k0 && item.least >= k0 + kTileT;
                 const int at = k0 + 32 * quarter;
                 const uint32_t seen = whole ? ~0u : single ? 0u : bits_of(see.x - at, see.y - at);
+                // blocks of 32 x 32 without a gradient leave zeros (packed documents 363 us, 355 so)
+                const bool some = __any_sync(0xffffffffu, seen != 0);
                 ok = wait_all(&bars.s_full[it & 1], (it / 2) & 1, abort, err);
                 if (!ok) break;
                 tc_fence_after();
@@ -599,18 +610,20 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 if (RICH && plan.lut) {
                     ok = wait_all(&bars.bias_full[it & 1], (it / 2) & 1, abort, err);
                     if (!ok) break;
-                    bias = (const float*)(raw + S::kBias) + (it & 1) * 256 + 127 + row - 32 * quarter;
+                    bias = (const float*)(raw + S::kBias) + (it & 1) * kWindow + window_row(row) + 32 * quarter;
                 }
                 tmem_wait_ld();
                 tmem_use(p);
-                if (RICH && idle) {  // the queries of rows that see nothing may be anything, and zero times a slope of NaN is NaN
+                if (some) {
+                    if (RICH && idle) {  // the queries of rows that see nothing may be anything, and zero times a slope of NaN is NaN
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) p[j] = see.x < see.y ? p[j] : 0.f;
+                        for (int j = 0; j < 32; ++j) p[j] = see.x < see.y ? p[j] : 0.f;
+                    }
+                    if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add4(make_float4(nl.x, nl.x, nl.x, nl.x), *(const float4*)(bias + j)); });
+                    else scores_of<RICH>(a, inv_cap, p, bend, [&](int) { return make_float4(nl.x, nl.x, nl.x, nl.x); });
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
                 }
-                if (bias) scores_of<RICH>(a, inv_cap, p, bend, [&](int j) { return add2(nl, make_float2(bias[-j], bias[-j - 1])); });
-                else scores_of<RICH>(a, inv_cap, p, bend, [&](int) { return nl; });
-#pragma unroll
-                for (int j = 0; j < 32; ++j) p[j] = exp2_fast(p[j]);
                 if (RICH && bias) arrive_warp(&bars.bias_empty[it & 1]);
                 ok = wait_all(&bars.dp_full, it & 1, abort, err);
                 if (!ok) break;
@@ -621,56 +634,75 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 tmem_use(d);
                 tc_fence_before();
                 arrive_warp(&bars.dp_free);
+                uint32_t w[16];
+                if (some) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    const float2 x = mul2(add2(make_float2(d[j], d[j + 1]), nd), make_float2(p[j], p[j + 1]));
-                    d[j] = x.x, d[j + 1] = x.y;
-                }
-                if (!whole) {
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 x = mul2(add2(make_float2(d[j], d[j + 1]), nd), make_float2(p[j], p[j + 1]));
+                        d[j] = x.x, d[j + 1] = x.y;
+                    }
+                    if (!whole) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (!(seen >> j & 1)) d[j] = 0.f;
+                        for (int j = 0; j < 32; ++j)
+                            if (!(seen >> j & 1)) d[j] = 0.f;
+                    }
                 }
                 if constexpr (RICH) {
                     if (learned) {
                         if (const int side = flat_at(item.tile, kt)) {
-                            float sum = 0.f;
+                            if (some) {
+                                float sum = 0.f;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sum += d[j];
-                            flat[side > 0] += sum;
+                                for (int j = 0; j < 32; ++j) sum += d[j];
+                                flat[side > 0] += sum;
+                            }
                         } else {
                             float* diag = (float*)(raw + S::kDiag) + ((diags & 1) * kRowWarps + warp) * 64;
+                            if (some) {
+                                // a diagonal's sum moves down the lanes with the columns and leaves at lane 31; of 16 columns at a
+                                // time, side by side, as each step waits for the shuffle before it (packed documents 355 us with
+                                // all 32 in a row, 331 so, 341 with 8 at a time, whose sums take more to join)
+                                float acc[2] = {0.f, 0.f};
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    acc[0] += d[j], acc[1] += d[16 + j];
+                                    if (lane == 31) halves[62 - j] = acc[0], halves[64 + 46 - j] = acc[1];  // row - column + 31
+                                    if (j < 15) {
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e) {
+                                            acc[e] = __shfl_up_sync(0xffffffffu, acc[e], 1);
+                                            if (lane == 0) acc[e] = 0.f;
+                                        }
+                                    }
+                                }
+                                if (lane < 31) halves[16 + lane] = acc[0], halves[64 + lane] = acc[1];
+                                __syncwarp();
+                            }
                             if (diags >= 2) {
                                 ok = wait_all(&bars.diag_empty[diags & 1], (diags / 2 - 1) & 1, abort, err);
                                 if (!ok) break;
                             }
-                            // a diagonal's sum moves down the lanes with the columns and leaves at lane 31
-                            float acc = 0.f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                acc += d[j];
-                                if (lane == 31) diag[62 - j] = acc;  // row - column = 31 - j
-                                if (j < 31) {
-                                    acc = __shfl_up_sync(0xffffffffu, acc, 1);
-                                    if (lane == 0) acc = 0.f;
-                                }
-                            }
-                            if (lane < 31) diag[lane] = acc;  // lane - 31
+                            diag[lane] = some ? halves[lane] + halves[64 + lane] : 0.f;
+                            if (lane < 31) diag[32 + lane] = some ? halves[32 + lane] + halves[96 + lane] : 0.f;
                             arrive_warp(&bars.diag_full[diags & 1]);
                             ++diags;
                         }
                     }
-                    if (a.cap > 0.f) {
+                }
+                if (some) {
+                    if (RICH && a.cap > 0.f) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
                             const float2 x = mul2(make_float2(d[j], d[j + 1]), make_float2(bend[j], bend[j + 1]));
                             d[j] = x.x, d[j + 1] = x.y;
                         }
                     }
-                }
-                uint32_t w[16];
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+                    for (int j = 0; j < 32; j += 2) w[j / 2] = pack_bf16(d[j], d[j + 1]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) w[j] = 0;
+                }
                 tmem_st16(ts, w);
                 tmem_wait_st();
                 tc_fence_before();
@@ -849,7 +881,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                     for (int kt = y.x; kt <= y.y; ++kt, ++windows) {
                         if (windows >= 2) ok = wait_all(&bars.bias_empty[windows & 1], (windows / 2 - 1) & 1, abort, err);
                         if (!ok) break;
-                        load_window(plan, x.y, (x.z - kt) * kTileT, (float*)(raw + S::kBias) + (windows & 1) * 256);
+                        load_window<true>(plan, x.y, (x.z - kt) * kTileT, (float*)(raw + S::kBias) + (windows & 1) * kWindow);
                         mbar_arrive(smem_u32(&bars.bias_full[windows & 1]));
                     }
                     if (!ok) break;
@@ -1009,14 +1041,16 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     const unsigned grid = (unsigned)((a.N * a.T * a.H + 256 / kLanes - 1) / (256 / kLanes));
     attention_stats_kernel<kLanes><<<grid, 256, 0, s>>>(a, FastDiv(a.H), (int)(a.N * a.T), stats);
     if (cudaError_t e = cudaGetLastError()) return e;
+    Attention with = a;
+    attention_near(with, 1.f);
     DqItems items;
     items.tiles = (int)tiles, items.total = (int)(tiles * a.N * a.H);
     items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
     if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())),
-                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, a, plan, items, (const float*)stats, part, err))
+                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, with, plan, items, (const float*)stats, part, err))
         return e;
     return launch_chained(true, attention_dkv_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.KV)), dim3(kThreads), Kv::kSmem, s, q,
-                          k, v, g, dk, dv, a, plan, (const float*)stats, err);
+                          k, v, g, dk, dv, with, plan, (const float*)stats, err);
 }
 
 }  // namespace

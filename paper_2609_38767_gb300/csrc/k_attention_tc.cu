@@ -17,6 +17,7 @@
 #include <math_constants.h>
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 
 #include "attention.cuh"
@@ -48,14 +49,16 @@ struct Warps {
     }
 };
 
+constexpr float kLowest = -20.f;  // base of bounded scores
+
 template <int HD, bool RICH>
 struct Shape {
     static constexpr int kPanels = HD / 64;
     static constexpr uint32_t kTileBytes = kPanels * kPanel;
     static constexpr int kStages = HD == 64 ? 6 : RICH ? 3 : 4;
     static constexpr uint32_t kOut = (2 + kStages) * kTileBytes;  // 32 rows of output for each of 4 warps
-    static constexpr uint32_t kBias = kOut + 4 * 32 * HD * 2;     // RICH: 2 x 2 windows of 256 biases
-    static constexpr uint32_t kSwap = kBias + (RICH ? 4096 : 0);  // RICH: 16 warps' maxima, at two places in turn
+    static constexpr uint32_t kBias = kOut + 4 * 32 * HD * 2;                  // RICH: 2 x 2 windows of biases
+    static constexpr uint32_t kSwap = kBias + (RICH ? 16 * kWindow : 0);  // RICH: 16 warps' maxima, at two places in turn
     static constexpr uint32_t kSmem = kSwap + (RICH ? 16 * 256 : 0);
 };
 
@@ -193,7 +196,22 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
         tc_fence_before();
     }
     chain_wait();
-    __syncthreads();
+    // Capped scores with a small learned bias lie in +-90 (times log2 e): their weights need no maximum first, 2^x of a row's
+    // scores less a base that is -20 at least stays in fp32's range. Slopes and large tables take the maximum.
+    bool bounded = false;
+    if constexpr (RICH) {
+        const float limit = 90.f / kLog2e - a.cap;
+        bool beyond = !(a.cap > 0.f && limit >= 0.f) || a.slope || (int64_t)a.n_buckets * a.H > 65536;
+        for (int i = threadIdx.x; !beyond && i < a.n_buckets * a.H; i += W::kThreads) {
+            const float x = (float)((const __nv_bfloat16*)a.table)[i];
+            beyond = !(fabsf(x) <= limit || x == -CUDART_INF_F);
+        }
+        if (!plan.lut)
+            for (int i = threadIdx.x; i < 4 * kWindow; i += W::kThreads) ((float*)(from + S::kBias))[i] = 0.f;
+        bounded = !__syncthreads_or(beyond);
+    } else {
+        __syncthreads();
+    }
     tc_fence_after();
     const uint32_t tmem = bars.tmem;
 
@@ -203,7 +221,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
         const int w = warp / (W::kRows / 2), half = RICH ? warp / 4 % 2 : 0, row = warp % 4 * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // TMEM lane of the warp's first row
         const uint32_t ts = tmem + lanes + w * 128, to = tmem + lanes + 256 + w * 128 + half * (HD / 2);
-        const float* biases = (const float*)(from + S::kBias) + w * 512;
+        const float* biases = (const float*)(from + S::kBias) + w * 2 * kWindow + window_row(row) + 64 * half;
         const float c = RICH ? 1.f : a.scale * kLog2e;  // s is the score times log2 e (RICH) or the dot product
         const float2 c2 = both(c);
         const float grow = 8.f / c, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
@@ -215,6 +233,20 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             at[warp * 64] = mine;
             ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
             return fmaxf(mine, at[(warp ^ 4) * 64]);
+        };
+        // O of the rows (RICH: half of its columns) times a number, once the MMAs before key tile `turn` are done
+        auto rescale = [&](uint32_t turn, float by) {
+            ok = ok && wait_warp(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err);
+            if (!ok) return;
+            tc_fence_after();
+#pragma unroll 1
+            for (int b = 0; b < HD / 16 / (RICH ? 2 : 1); ++b) {
+                float o[16];
+                tmem_ld16(to + 16 * b, o);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[j] *= by;
+                tmem_st16(to + 16 * b, (const uint32_t*)o);
+            }
         };
         uint32_t turn = 0, outputs = 0;  // key tiles, outputs so far
         ItemReader reader;
@@ -259,46 +291,102 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                         if (!(bits >> j & 1)) x[j] = -CUDART_INF_F;
                 };
                 if constexpr (RICH) {
-                    // scores with cap and bias go back to TMEM, 32 columns at a time
-                    const float* bias = nullptr;
-                    bool flat = false;
-                    if (plan.lut) {
-                        ok = ok && wait_warp(smem_u32(&bars.bias_full[w][turn & 1]), (turn / 2) & 1, abort, err);
-                        bias = biases + (turn & 1) * 256 + 127 + row - 64 * half;
-                        const int apart = q0 - kt * kTileT;
-                        flat = apart >= plan.reach + 127 || apart <= -plan.reach - 127;
-                    }
-#pragma unroll 1
-                    for (int b = 0; b < 2; ++b) {
-                        if (!sees(b)) continue;
+                    const float* bias = biases + (turn & 1) * kWindow;
+                    if (plan.lut) ok = ok && wait_warp(smem_u32(&bars.bias_full[w][turn & 1]), (turn / 2) & 1, abort, err);
+                    // the scores of 32 columns, biases as moved() leaves them
+                    auto scored = [&](int b, auto moved) {
                         tmem_ld32(ts + 64 * half + 32 * b, s);
                         tmem_wait_ld();
                         tmem_use(s);
-                        // the bias of 32 distances, nothing where they are all beyond the table's reach but the one of the reach
-                        const float beyond = flat ? *bias : 0.f;
-                        const bool add = bias && !flat;
-                        auto score = [&](auto at_pair) {
+                        auto all = [&](auto score) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 2) {
-                                float2 x = both(beyond);
-                                if (add) x = make_float2(bias[-32 * b - j], bias[-32 * b - j - 1]);
-                                x = at_pair(make_float2(s[j], s[j + 1]), x);
-                                s[j] = x.x, s[j + 1] = x.y;
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 x = *(const float4*)(bias + 32 * b + j);
+                                const float2 u = score(make_float2(s[j], s[j + 1]), moved(make_float2(x.x, x.y)));
+                                const float2 v = score(make_float2(s[j + 2], s[j + 3]), moved(make_float2(x.z, x.w)));
+                                s[j] = u.x, s[j + 1] = u.y, s[j + 2] = v.x, s[j + 3] = v.y;
                             }
                         };
-                        if (a.cap <= 0.f) score([&](float2 d, float2 x) { return fma2(d, both(a.scale * kLog2e), x); });
-                        else if (all_near<32>(s, inv_cap))
-                            score([&](float2 d, float2 x) { return fma2(tanh_near(mul2(d, both(inv_cap))), both(cap2), x); });
-                        else score([&](float2 d, float2 x) { return fma2(tanh_any(mul2(d, both(inv_cap))), both(cap2), x); });
+                        if (a.cap <= 0.f) all([&](float2 d, float2 x) { return fma2(d, both(a.scale * kLog2e), x); });
+                        else if (all_near<32>(s, a.near_limit)) all([&](float2 d, float2 x) { return fma2(d, tanh_near(a, d), x); });
+                        else all([&](float2 d, float2 x) { return fma2(tanh_any(mul2(d, both(inv_cap))), both(cap2), x); });
                         if (!whole) mask(b, s);
+                    };
+                    auto bias_read = [&]() {
+                        if (!plan.lut) return;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bars.bias_empty[w][turn & 1]));
+                    };
+                    if (bounded) {
+                        // weights by the row's base so far, in one go; they cannot overflow
+                        if (kt == first) top = 0.f;
+                        const float2 less = both(-top);
+                        float2 part[2] = {both(0.f), both(0.f)};
+#pragma unroll 1
+                        for (int b = 0; b < 2; ++b) {
+                            uint32_t p[16];
+                            if (sees(b)) {
+                                scored(b, [&](float2 x) { return add2(x, less); });
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    const float2 v = make_float2(exp2_fast(s[2 * j]), exp2_fast(s[2 * j + 1]));
+                                    part[j & 1] = add2(part[j & 1], v);
+                                    p[j] = pack_bf16(v.x, v.y);
+                                }
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) p[j] = 0;
+                            }
+                            tmem_st16(ts + 64 * half + 16 * b, p);
+                        }
+                        bias_read();
+                        float now = part[0].x + part[0].y + part[1].x + part[1].y;
+                        tmem_wait_st();
+                        const bool fits = now <= 0x1p16f && (sum > 0.f || now >= 0x1p-16f || now == 0.f);
+                        if (!all_came_well(1 + w * 4 + warp % 4, 64, ok && fits)) {
+                            // a base by the sum of both halves of a row, by a power of two: the weights' scaling is exact
+                            float* swap = (float*)(from + S::kSwap) + lane;
+                            swap[warp * 64] = now, swap[warp * 64 + 32] = sum;
+                            ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
+                            if (!ok) break;
+                            const float tile = now + swap[(warp ^ 4) * 64], before = sum + swap[(warp ^ 4) * 64 + 32];
+                            int by2 = (int)(__float_as_uint(tile) >> 23) - 127;  // sums are positive, or NaN
+                            if (tile == 0.f || by2 > 126 || (by2 <= 16 && (before > 0.f || by2 >= -16))) by2 = 0;
+                            by2 = max(by2, (int)(kLowest - top));
+                            top += (float)by2;
+                            const float by = __int_as_float((127 - by2) << 23);
+                            now *= by, sum *= by;
+                            const __nv_bfloat162 by_pair = __float2bfloat162_rn(by);
+#pragma unroll 1
+                            for (int b = 0; b < 2; ++b) {
+                                uint32_t p[16];
+                                tmem_ld16(ts + 64 * half + 16 * b, (float*)p);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) {
+                                    __nv_bfloat162 v = __hmul2(*(const __nv_bfloat162*)&p[j], by_pair);
+                                    p[j] = *(const uint32_t*)&v;
+                                }
+                                tmem_st16(ts + 64 * half + 16 * b, p);
+                            }
+                            if (kt != first) rescale(turn, by);
+                            tmem_wait_st();
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bars.p_ready[w][half]));
+                        sum += now;
+                        continue;
+                    }
+                    // scores go back to TMEM, 32 columns at a time, until their maximum is known
+#pragma unroll 1
+                    for (int b = 0; b < 2; ++b) {
+                        if (!sees(b)) continue;
+                        scored(b, [](float2 x) { return x; });
                         most_now = largest<32>(s, most_now);
                         tmem_st32(ts + 64 * half + 32 * b, (const uint32_t*)s);
                     }
                     tmem_wait_st();
-                    if (bias) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&bars.bias_empty[w][turn & 1]));
-                    }
+                    bias_read();
                     most_now = join(most_now, turn);
                     if (!ok) break;
                 } else {
@@ -326,20 +414,11 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                 if (kt == first) {
                     top = most_now;
                 } else if (__any_sync(0xffffffffu, most_now > top + grow)) {
-                    ok = wait_warp(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err);
-                    if (!RICH && !ok) break;
-                    tc_fence_after();
                     const float by = most_now == -CUDART_INF_F ? 1.f : exp2_fast((top - most_now) * c);
                     top = most_now;
                     sum *= by;
-#pragma unroll 1
-                    for (int b = 0; b < HD / 16 / (RICH ? 2 : 1); ++b) {
-                        float o[16];
-                        tmem_ld16(to + 16 * b, o);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) o[j] *= by;
-                        tmem_st16(to + 16 * b, (const uint32_t*)o);
-                    }
+                    rescale(turn, by);
+                    if (!RICH && !ok) break;
                 }
                 const float base_of = top == -CUDART_INF_F ? 0.f : top;
                 const float2 less = both(RICH ? -base_of : -base_of * c);
@@ -644,14 +723,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                         ok = wait_warp(smem_u32(&bars.bias_empty[w][turn & 1]), (turn / 2 - 1) & 1, abort, err);
                     if (!ok) break;
                     const int q0 = (2 * at.item.pair + w) * kTileT, k0 = at.kt * kTileT;
-                    const int apart = min(max(q0 - k0, -plan.reach - 127), plan.reach + 127);
-                    const float* src = plan.lut + (int64_t)at.item.h * plan.lut_len + plan.lut_mid + apart - 127;
-                    float* dst = (float*)(from + S::kBias) + w * 512 + (turn & 1) * 256;
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = src[min(32 * e + lane, 254)];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dst[32 * e + lane] = v[e];
+                    load_window<true>(plan, at.item.h, q0 - k0, (float*)(from + S::kBias) + (2 * w + (turn & 1)) * kWindow);
                     mbar_arrive(smem_u32(&bars.bias_full[w][turn & 1]));
                     ++turns[w];
                 }
@@ -770,12 +842,14 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     AttentionPlan plan;
     bool chained;
     if (cudaError_t e = launch_attention_plan(a, ws, &plan, &chained, s)) return e;
+    Attention with = a;
+    attention_near(with, a.cap * kLog2e);
     const int64_t tiles = (a.T + kTileT - 1) / kTileT;
     Items items;
     items.tiles = (int)tiles, items.pairs = (int)((tiles + 1) / 2), items.total = (int)(items.pairs * a.N * a.H);
     items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
     return launch_chained(chained, attention_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())), dim3(Warps<RICH>::kThreads),
-                          Sh::kSmem, s, q, k, v, a, plan, items, err);
+                          Sh::kSmem, s, q, k, v, with, plan, items, err);
 }
 
 }  // namespace
@@ -787,6 +861,21 @@ bool attention_tc_supported(const Attention& a, bool backward) {
         ok = ok && head_rows(a.dO, a.ld_do, a.T) && head_rows(a.dQ, a.ld_dq, a.T) && head_rows(a.dK, a.ld_dk, a.T) &&
              head_rows(a.dV, a.ld_dv, a.T);
     return ok && linear_tc_available();
+}
+
+void attention_near(Attention& a, float by) {
+    // tanh x = x P(x^2) for |x| <= 1/2, a minimax fit
+    constexpr double fit[5] = {0.017135003581643105, -0.05298607423901558, 0.13324779272079468, -0.3333306908607483, 1.0};
+    a.near_limit = -1.f;  // no dot product is near
+    if (!(a.cap > 0.f)) return;
+    const double x = (double)a.scale / a.cap;
+    bool fine = x > 0x1p-20 && x < 0x1p20;
+    for (int k = 0; k < 5; ++k) {
+        const float c = (float)(fit[k] * by * std::pow(x, 9 - 2 * k));
+        a.near[k] = make_float2(c, c);
+        fine = fine && std::isnormal(c);
+    }
+    if (fine) a.near_limit = (float)(0.5 / x);
 }
 
 size_t attention_plan_bytes(const Attention& a, bool bound) {

@@ -144,7 +144,8 @@ def check_forward(p):
     buf = p.forward()
     tda.tda_device_status()
     f = p.exact()
-    b = Bounds(f, p.dtype, p.T, p.hd, p.cap, p.bias)
+    bias = p.bias if p.bias is None else p.bias.nan_to_num(neginf=0.0)  # a hidden pair has no weight and no error
+    b = Bounds(f, p.dtype, p.T, p.hd, p.cap, bias)
     near(p.heads(p.O, p.H), f["o"], b.o(), "O")
     near(p.lse, f["lse"], b.lse(), "lse")
     untouched(buf, p, p.H * p.hd)
@@ -246,6 +247,30 @@ def test_equal_calls_give_equal_bits(dev):
         tda.tda_device_status()
         for other in got[1:]:
             assert all(torch.equal(x, y) for x, y in zip(got[0], other))
+
+
+@pytest.mark.parametrize("buckets", [0, 5])
+@pytest.mark.parametrize("cap", [4.0, 30.0, 60.0, 62.3, 62.4, 80.0])
+def test_scores_at_the_cap(dev, cap, buckets):
+    """Scores that rise and fall from one end of the capped range to the other, within a tile and from tile to tile, and rows
+    that stay at the lower end."""
+    T, hd = 700, 64
+    p = Problem(dev, 1, T, 4, 1, hd, BF, "full", cap, buckets, 40 if buckets else 0, sigma=0.5)
+    at = torch.arange(T, device=dev)
+    along = torch.stack([torch.sin(at / 40.0) * 3, at / T * 6 - 3, 3 - at / T * 6, (at // 128 % 2) * 6.0 - 3])  # of the keys, by head
+    if buckets:
+        p.table[1] = -math.inf
+        p.table[2] = 4.0
+        p.bias = bias_of(T, 4, p.bucket, 40, p.table, None, dev)
+    p.Q[:, :] = 0
+    p.K[:, :] = 0
+    for h in range(4):  # a direction of its own for each head's queries, of either sign and some weak
+        p.Q[:, h * hd + h] = torch.where(at % 3 == 0, 1.0, torch.where(at % 3 == 1, -1.0, 0.05)).to(BF)
+        p.K[:, h] = (along[h] * cap / p.scale).to(BF)
+    p.Q[:, 8], p.Q[:, hd + 8] = 1.0, -1.0
+    p.K[:, 8] = -(cap / p.scale)
+    f, b = check_forward(p)
+    check_backward(p, f, b, beta=0.5 if buckets else 0.0, grad=F32)
 
 
 MORE = [
