@@ -70,6 +70,7 @@ struct BarsOf {
     int abort;
     float2 sums[2][RICH ? 2 : 1][kTileT];  // maximum and sum of a finished row
     int4 items[4][2];
+    int example[4];
 };
 
 // Keys that a tile's queries see, and between which all of them see all.
@@ -90,41 +91,60 @@ __device__ __forceinline__ Hull hull_of(const Attention& a, const AttentionPlan&
     return a.causal ? Hull{0, min(q0 + kTileT, T), 0, q0 + 1} : Hull{0, T, 0, T};
 }
 
-// The items (pairs of query tiles of a head) of this CTA, long ones first where the mask is causal; every other round
-// backwards, which evens out what the rounds leave. With ranges, which rounds do not even out, CTAs take items as they come free.
+// The items of this CTA, long ones first where the mask is causal; every other round backwards, which evens out what the rounds
+// leave. With ranges, which rounds do not even out, CTAs take items as they come free. An item's two tiles are the same queries of two
+// heads that share their keys, where there are such heads and enough items for the SMs: they are equally long then (neighbours of
+// one head are not where the mask is causal, and the longer one's last key tile has the CTA to itself: 8 x 1024 tokens 72 us, 65 so).
 struct Items {
-    int total, pairs, tiles;
-    FastDiv heads, H, group;  // N H, H, H / KV
+    int total, tiles, groups, by_head;  // groups of tiles
+    FastDiv heads, H, group;            // N heads, heads (or pairs of heads), query heads per key head
     __device__ __forceinline__ int at(int round) const {
         const int g = gridDim.x, b = blockIdx.x;
         return round * g + (round & 1 ? g - 1 - b : b);
     }
-    __device__ __forceinline__ int pair(int item) const { return pairs - 1 - heads.div(item); }
+    __device__ __forceinline__ int tile(int item) const { return (groups - 1 - heads.div(item)) << !by_head; }
     __device__ __forceinline__ int example(int item) const { return H.div(heads.mod(item)); }
-    __device__ __forceinline__ int head(int item) const { return H.mod(heads.mod(item)); }
+    __device__ __forceinline__ int head(int item) const { return H.mod(heads.mod(item)) << by_head; }
 };
 
-// An item as warp 10 leaves it for the others, four at a time: working it out takes longer than a step of the MMAs.
+// An item as the warp that makes them leaves it for the others, four at a time: working it out takes longer than a step of the MMAs.
+struct Part {  // of an item: a tile of queries
+    int n, h, tile, first, last;  // h < 0: no more items; first > last: no keys
+    __device__ __forceinline__ int q0() const { return tile * kTileT; }
+};
 struct Item {
-    int n, h, pair;  // h < 0: no more
-    int first[2], last[2];  // key tiles that the queries of tile w see
-    __device__ __forceinline__ bool any() const { return min(first[0], first[1]) <= max(last[0], last[1]); }
+    Part of[2];
+    __device__ __forceinline__ bool any() const { return min(of[0].first, of[1].first) <= max(of[0].last, of[1].last); }
 };
 struct ItemReader {
     uint32_t r = 0;
-    // The next item; false after the last one, or where a wait ran out (*ok). Called by whole warps.
+    // The next item, or one of its parts; false after the last one, or where a wait ran out (*ok). Called by whole warps.
+    template <typename Bars>
+    __device__ __forceinline__ bool next(Part& x, int w, Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
+        *ok = *ok && wait_warp(smem_u32(&bars.item_full[r % 4]), (r / 4) & 1, abort, err);
+        if (!*ok) return false;
+        read(x, w, bars);
+        done(bars);
+        return x.h >= 0;
+    }
     template <typename Bars>
     __device__ __forceinline__ bool next(Item& x, Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
-        const uint32_t bar = smem_u32(&bars.item_full[r % 4]), parity = (r / 4) & 1;
-        *ok = *ok && wait_warp(bar, parity, abort, err);
+        *ok = *ok && wait_warp(smem_u32(&bars.item_full[r % 4]), (r / 4) & 1, abort, err);
         if (!*ok) return false;
-        const int4 a = bars.items[r % 4][0], b = bars.items[r % 4][1];
-        x.n = a.x, x.h = a.y, x.pair = a.z;
-        x.first[0] = b.x, x.last[0] = b.y, x.first[1] = b.z, x.last[1] = b.w;
+        read(x.of[0], 0, bars), read(x.of[1], 1, bars);
+        done(bars);
+        return x.of[0].h >= 0;
+    }
+    template <typename Bars>
+    __device__ __forceinline__ void read(Part& x, int w, Bars& bars) const {
+        const int4 a = bars.items[r % 4][w];
+        x.n = bars.example[r % 4], x.h = a.x, x.tile = a.y, x.first = a.z, x.last = a.w;
+    }
+    template <typename Bars>
+    __device__ __forceinline__ void done(Bars& bars) {
         __syncwarp();
         if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(&bars.item_empty[r % 4]));
         ++r;
-        return x.h >= 0;
     }
 };
 
@@ -144,9 +164,9 @@ struct Walk {
         }
         do valid = reader.next(item, bars, ok, abort, err);
         while (valid && !item.any());
-        kt = min(item.first[0], item.first[1]), last = max(item.last[0], item.last[1]);
+        kt = min(item.of[0].first, item.of[1].first), last = max(item.of[0].last, item.of[1].last);
     }
-    __device__ __forceinline__ bool active(int w) const { return kt >= item.first[w] && kt <= item.last[w]; }
+    __device__ __forceinline__ bool active(int w) const { return kt >= item.of[w].first && kt <= item.of[w].last; }
 };
 
 template <int HD, bool RICH>
@@ -250,21 +270,21 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
         };
         uint32_t turn = 0, outputs = 0;  // key tiles, outputs so far
         ItemReader reader;
-        Item item, then;
+        Part item, then;
         int2 see, see_then = make_int2(0, 0);
         then.h = -2;
         while (ok) {
             // the next item and what this thread's row sees in it, one item ahead
             item = then, see = see_then;
             if (item.h == -1) break;
-            bool there = reader.next(then, bars, &ok, abort, err);
+            bool there = reader.next(then, w, bars, &ok, abort, err);
             if (RICH) there = (ok = all_came_well(1 + w * 4 + warp % 4, 64, ok)) && there;
             if (!there) then.h = -1;
-            else see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, (2 * then.pair + w) * kTileT + row);
+            else see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, then.q0() + row);
             if (item.h < 0) continue;
-            const int first = w ? item.first[1] : item.first[0], last = w ? item.last[1] : item.last[0];
+            const int first = item.first, last = item.last;
             if (first > last) continue;
-            const int q0 = (2 * item.pair + w) * kTileT, i = q0 + row;
+            const int i = item.q0() + row;
             // what the warp's rows see: nothing outside [lo, hi), everything within [most, least)
             const bool none = see.x >= see.y;
             const int most = __reduce_max_sync(0xffffffffu, none ? 0 : see.x);
@@ -489,15 +509,15 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
         ItemReader reader;
         Item item;
         while (reader.next(item, bars, &ok, abort, err)) {
-            const int n = item.n, h = item.h;
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-                const int q0 = (2 * item.pair + w) * kTileT, i = q0 + row;
+                const Part& x = item.of[w];
+                const int n = x.n, h = x.h, q0 = x.q0(), i = q0 + row;
                 if (!ok || q0 >= T) continue;
-                const bool any = item.first[w] <= item.last[w];
+                const bool any = x.first <= x.last;
                 float top = 0.f, sum = 0.f;
                 if (any) {
-                    turns[w] += item.last[w] - item.first[w] + 1;
+                    turns[w] += x.last - x.first + 1;
                     ok = wait_warp(smem_u32(&bars.sum_full[w]), done[w]++ & 1, abort, err) &&
                          wait_warp(smem_u32(&bars.o_done[w]), (turns[w] - 1) & 1, abort, err);
                     if (!ok) continue;
@@ -558,7 +578,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             while (true) {
                 at.next(bars, &ok, abort, err);
                 if (!ok || !at.valid) break;
-                const int kv = items.group.div(at.item.h);
+                const int kv = items.group.div(at.item.of[0].h);
 #pragma unroll 1
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t s = used % S::kStages, turn = used / S::kStages;
@@ -569,7 +589,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                         mbar_arrive_tx(bar, S::kTileBytes);
 #pragma unroll
                         for (int p = 0; p < S::kPanels; ++p)
-                            tma_load_head(ring + s * S::kTileBytes + p * kPanel, e ? &tmV : &tmK, 64 * p, kv, at.kt * kTileT, at.item.n, bar);
+                            tma_load_head(ring + s * S::kTileBytes + p * kPanel, e ? &tmV : &tmK, 64 * p, kv, at.kt * kTileT, at.item.of[0].n, bar);
                     }
                     __syncwarp();
                     ++used;
@@ -591,30 +611,32 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     if (lane == 0) id = atomicAdd(plan.taken, 1);
                     id = __shfl_sync(0xffffffffu, id, 0);
                 }
-                int n = 0, h = -1, pair = 0;
+                int n = 0, h = -2, tile = 0;
                 Hull hull[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
                 if (id < items.total) {
-                    n = items.example(id), h = items.head(id), pair = items.pair(id);
-                    hull[0] = hull_of(a, plan, n, items.tiles, 2 * pair), hull[1] = hull_of(a, plan, n, items.tiles, 2 * pair + 1);
+                    n = items.example(id), h = items.head(id), tile = items.tile(id);
+                    hull[0] = hull_of(a, plan, n, items.tiles, tile), hull[1] = hull_of(a, plan, n, items.tiles, tile + !items.by_head);
                 }
                 if (lead) {
-                    const int none = 1 << 30;
-                    bars.items[r % 4][0] = make_int4(n, h, pair, 0);
-                    bars.items[r % 4][1] = make_int4(hull[0].any() ? hull[0].first() : none, hull[0].any() ? hull[0].last() : -1,
-                                                     hull[1].any() ? hull[1].first() : none, hull[1].any() ? hull[1].last() : -1);
+                    bars.example[r % 4] = n;
+#pragma unroll
+                    for (int w = 0; w < 2; ++w)
+                        bars.items[r % 4][w] = make_int4(h + (w & items.by_head), tile + (w & ~items.by_head), hull[w].any() ? hull[w].first() : 1 << 30,
+                                                         hull[w].any() ? hull[w].last() : -1);
                     mbar_arrive(smem_u32(&bars.item_full[r % 4]));
                 }
                 __syncwarp();
             };
             for (uint32_t r = 0; ok; ++r) {  // makes item r, loads the queries of item r - 1
-                if (r && bars.items[(r - 1) % 4][0].y < 0) break;
+                if (r && bars.items[(r - 1) % 4][0].x < 0) break;
                 make();
                 if (r == 0) continue;
                 // nobody can have replaced what this warp made: the slot is free for item r + 3 once its readers have passed it
-                const int4 x = bars.items[(r - 1) % 4][0], y = bars.items[(r - 1) % 4][1];
+                const int example = bars.example[(r - 1) % 4];
 #pragma unroll 1
                 for (int w = 0; w < 2; ++w) {
-                    if (!ok || (w ? y.z > y.w : y.x > y.y)) continue;
+                    const int4 x = bars.items[(r - 1) % 4][w];
+                    if (!ok || x.z > x.w) continue;
                     const uint32_t turn = w ? asked1 : asked0;
                     if (turn) ok = wait_warp(smem_u32(&bars.q_empty[w]), (turn - 1) & 1, abort, err);
                     if (!ok) continue;
@@ -623,7 +645,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                         mbar_arrive_tx(bar, S::kTileBytes);
 #pragma unroll
                         for (int p = 0; p < S::kPanels; ++p)
-                            tma_load_head(sq + w * S::kTileBytes + p * kPanel, &tmQ, 64 * p, x.y, (2 * x.z + w) * kTileT, x.x, bar);
+                            tma_load_head(sq + w * S::kTileBytes + p * kPanel, &tmQ, 64 * p, x.x, x.y * kTileT, example, bar);
                     }
                     __syncwarp();
                     w ? ++asked1 : ++asked0;
@@ -655,7 +677,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     if (!ok) break;
                     if (a.range) {
                         uint32_t bits[4];
-                        *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)now.item.n * items.tiles + now.kt].unseen;
+                        *(uint4*)bits = *(const uint4*)plan.tiles[(int64_t)now.item.of[0].n * items.tiles + now.kt].unseen;
                         if (bits[0] | bits[1] | bits[2] | bits[3]) clear_rows(stage(at_v), S::kPanels, bits);
                     }
                     v = mn_major(stage(at_v), kPanel);
@@ -663,7 +685,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     const uint32_t ts = tmem + w * 128, to = tmem + 256 + w * 128;
-                    const int first = w ? now.item.first[1] : now.item.first[0], last = w ? now.item.last[1] : now.item.last[0];
+                    const int first = now.item.of[w].first, last = now.item.of[w].last;
                     if (now.valid && now.kt >= first && now.kt <= last) {
                         if (now.kt == first) {  // the tile's last output has been read
                             if (some_o >> w & 1) ok = wait_warp(smem_u32(&bars.o_free[w]), ~par_o >> w & 1, abort, err);
@@ -684,7 +706,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     }
                     if (!then.valid) continue;
                     if (w == 0) ok = full(at_k);
-                    const int first_k = w ? then.item.first[1] : then.item.first[0], last_k = w ? then.item.last[1] : then.item.last[0];
+                    const int first_k = then.item.of[w].first, last_k = then.item.of[w].last;
                     if (ok && then.kt >= first_k && then.kt <= last_k) {
                         if (then.kt == first_k) {
                             ok = wait_warp(smem_u32(&bars.q_full[w]), par_q >> w & 1, abort, err);
@@ -722,8 +744,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     if (turn >= 2)
                         ok = wait_warp(smem_u32(&bars.bias_empty[w][turn & 1]), (turn / 2 - 1) & 1, abort, err);
                     if (!ok) break;
-                    const int q0 = (2 * at.item.pair + w) * kTileT, k0 = at.kt * kTileT;
-                    load_window<true>(plan, at.item.h, q0 - k0, (float*)(from + S::kBias) + (2 * w + (turn & 1)) * kWindow);
+                    load_window<true>(plan, at.item.of[w].h, at.item.of[w].q0() - at.kt * kTileT, (float*)(from + S::kBias) + (2 * w + (turn & 1)) * kWindow);
                     mbar_arrive(smem_u32(&bars.bias_full[w][turn & 1]));
                     ++turns[w];
                 }
@@ -846,8 +867,10 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     attention_near(with, a.cap * kLog2e);
     const int64_t tiles = (a.T + kTileT - 1) / kTileT;
     Items items;
-    items.tiles = (int)tiles, items.pairs = (int)((tiles + 1) / 2), items.total = (int)(items.pairs * a.N * a.H);
-    items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
+    const int64_t group = a.H / a.KV, by_head = group % 2 == 0 && tiles * a.N * a.H / 2 >= train_sms(), heads = a.H >> by_head;
+    items.tiles = (int)tiles, items.by_head = (int)by_head, items.groups = (int)(by_head ? tiles : (tiles + 1) / 2);
+    items.total = (int)(items.groups * a.N * heads);
+    items.heads = FastDiv((uint32_t)(a.N * heads)), items.H = FastDiv((uint32_t)heads), items.group = FastDiv((uint32_t)group);
     return launch_chained(chained, attention_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())), dim3(Warps<RICH>::kThreads),
                           Sh::kSmem, s, q, k, v, with, plan, items, err);
 }
