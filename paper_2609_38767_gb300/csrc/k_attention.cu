@@ -10,6 +10,7 @@
 #include <math_constants.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attention.cuh"
 
@@ -73,49 +74,61 @@ __device__ __forceinline__ bool vectors(const void* p, int64_t ld, int hd) {
     return sizeof(T) == 4 && (((uint64_t)p | (uint64_t)(ld * 4)) & 15) == 0 && hd % 4 == 0;
 }
 
-// s[r][c] = a_row . b_row for rows ty + 16 r of A and tx + 16 c of B.
-template <int HD>
+// a b + c of two fp32 pairs in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*(uint64_t*)&d)
+        : "l"(*(uint64_t*)&a), "l"(*(uint64_t*)&b), "l"(*(uint64_t*)&c));
+    return d;
+}
+
+// s[r][c] = a_row . b_row for rows ty + 16 r of A, r < R, and tx + 16 c of B: even and odd terms beside one another.
+template <int HD, int R>
 __device__ __forceinline__ void dots(const float* A, const float* B, float (&s)[4][4]) {
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+    float2 sum[R][4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[r][c] = 0.f;
+        for (int c = 0; c < 4; ++c) sum[r][c] = make_float2(0.f, 0.f);
 #pragma unroll 4
     for (int d = 0; d < HD; d += 4) {
-        float4 a[4], b[4];
+        float4 a[R], b[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) a[r] = *(const float4*)&A[(ty + 16 * r) * (HD + 4) + d];
+        for (int r = 0; r < R; ++r) a[r] = *(const float4*)&A[(ty + 16 * r) * (HD + 4) + d];
 #pragma unroll
         for (int c = 0; c < 4; ++c) b[c] = *(const float4*)&B[(tx + 16 * c) * (HD + 4) + d];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                s[r][c] = fmaf(a[r].x, b[c].x, s[r][c]);
-                s[r][c] = fmaf(a[r].y, b[c].y, s[r][c]);
-                s[r][c] = fmaf(a[r].z, b[c].z, s[r][c]);
-                s[r][c] = fmaf(a[r].w, b[c].w, s[r][c]);
+                sum[r][c] = fma2(make_float2(a[r].x, a[r].y), make_float2(b[c].x, b[c].y), sum[r][c]);
+                sum[r][c] = fma2(make_float2(a[r].z, a[r].w), make_float2(b[c].z, b[c].w), sum[r][c]);
             }
     }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[r][c] = sum[r][c].x + sum[r][c].y;
 }
 
-// acc[r][c] += sum_k W[ty + 16 r][k] V[k][c'], c' = 4 tx + 64 (c / 4) + c % 4: 64 rows of W with stride 68.
-template <int HD>
-__device__ __forceinline__ void weigh(const float* W, const float* V, float (&acc)[4][HD / 16]) {
+// acc[r][c] += sum over k < n of W[ty + 16 r][k] V[k][c'], c' = 4 tx + 64 (c / 4) + c % 4, r < R: 64 rows of W with stride 68.
+template <int HD, int R>
+__device__ __forceinline__ void weigh(const float* W, const float* V, float (&acc)[4][HD / 16], int n) {
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
 #pragma unroll 2
-    for (int k = 0; k < kTile; k += 4) {
-        float4 w[4];
+    for (int k = 0; k < n; k += 4) {
+        float4 w[R];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) w[r] = *(const float4*)&W[(ty + 16 * r) * (kTile + 4) + k];
+        for (int r = 0; r < R; ++r) w[r] = *(const float4*)&W[(ty + 16 * r) * (kTile + 4) + k];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int b = 0; b < HD / 64; ++b) {
                 const float4 v = *(const float4*)&V[(k + j) * (HD + 4) + 4 * tx + 64 * b];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < R; ++r) {
                     const float x = j == 0 ? w[r].x : j == 1 ? w[r].y : j == 2 ? w[r].z : w[r].w;
                     acc[r][4 * b + 0] = fmaf(x, v.x, acc[r][4 * b + 0]);
                     acc[r][4 * b + 1] = fmaf(x, v.y, acc[r][4 * b + 1]);
@@ -124,6 +137,14 @@ __device__ __forceinline__ void weigh(const float* W, const float* V, float (&ac
                 }
             }
     }
+}
+// f with the number of 16-row groups that a tile with `rows` rows left has, 1, 2 or 4: the last tile of an example is not paid for in
+// full (with fma2 in dots, 4 x 515 tokens of 8 heads 69 -> 59 us, the backward pass of 2 x 515 140 -> 133).
+template <typename F>
+__device__ __forceinline__ void by_rows(int rows, F&& f) {
+    if (rows <= 16) f(std::integral_constant<int, 1>());
+    else if (rows <= 32) f(std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 4>());
 }
 
 template <typename T, int HD>
@@ -225,46 +246,49 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(const Attention 
         for (int c = 0; c < HD / 16; ++c) acc[r][c] = 0.f;
     }
     const uint8_t* live = a.range ? m.live : nullptr;
-    for (int k0 = m.lo / kTile * kTile; k0 < m.hi; k0 += kTile) {
-        if (live) mark_keys(m, k0);
-        load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.K, a.ld_k, a.hd));
-        load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.V, a.ld_v, a.hd));
-        load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
-        __syncthreads();
-        float s[4][4];
-        dots<HD>(Q, K, s);
+    by_rows(rows - q0, [&](auto groups) {
+        constexpr int R = decltype(groups)::value;
+        for (int k0 = m.lo / kTile * kTile; k0 < m.hi; k0 += kTile) {
+            if (live) mark_keys(m, k0);
+            load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.K, a.ld_k, a.hd));
+            load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.V, a.ld_v, a.hd));
+            load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
+            __syncthreads();
+            float s[4][4];
+            dots<HD, R>(Q, K, s);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = ty + 16 * r;
-            const int2 see = m.see[i];
-            float most = -CUDART_INF_F;
+            for (int r = 0; r < R; ++r) {
+                const int i = ty + 16 * r;
+                const int2 see = m.see[i];
+                float most = -CUDART_INF_F;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int j = tx + 16 * c;
-                float bend;
-                const float x = score(s[r][c], a.scale, a.cap, m.biases[kTile + i - j], &bend);
-                s[r][c] = k0 + j >= see.x && k0 + j < see.y ? x : -CUDART_INF_F;
-                most = fmaxf(most, s[r][c]);
+                for (int c = 0; c < 4; ++c) {
+                    const int j = tx + 16 * c;
+                    float bend;
+                    const float x = score(s[r][c], a.scale, a.cap, m.biases[kTile + i - j], &bend);
+                    s[r][c] = k0 + j >= see.x && k0 + j < see.y ? x : -CUDART_INF_F;
+                    most = fmaxf(most, s[r][c]);
+                }
+                const float now = fmaxf(top[r], row_max(most));
+                const float base = now == -CUDART_INF_F ? 0.f : now;
+                const float by = expf(top[r] - base);
+                float part = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float p = expf(s[r][c] - base);
+                    part += p;
+                    P[i * (kTile + 4) + tx + 16 * c] = p;
+                }
+                sum[r] = sum[r] * by + row_sum(part);
+                top[r] = now;
+#pragma unroll
+                for (int c = 0; c < HD / 16; ++c) acc[r][c] *= by;
             }
-            const float now = fmaxf(top[r], row_max(most));
-            const float base = now == -CUDART_INF_F ? 0.f : now;
-            const float by = expf(top[r] - base);
-            float part = 0.f;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float p = expf(s[r][c] - base);
-                part += p;
-                P[i * (kTile + 4) + tx + 16 * c] = p;
-            }
-            sum[r] = sum[r] * by + row_sum(part);
-            top[r] = now;
-#pragma unroll
-            for (int c = 0; c < HD / 16; ++c) acc[r][c] *= by;
+            __syncthreads();
+            weigh<HD, R>(P, V, acc, min(rows - k0, kTile));
+            __syncthreads();
         }
-        __syncthreads();
-        weigh<HD>(P, V, acc);
-        __syncthreads();
-    }
+    });
     float by[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -339,52 +363,55 @@ __device__ __forceinline__ void dq_tile(const Attention& a, const float* delta, 
     if (learned)
         for (int b = threadIdx.x; b < a.n_buckets; b += kThreads) mine[b] = 0.f;
     const uint8_t* live = a.range ? m.live : nullptr;
-    for (int k0 = m.lo / kTile * kTile; k0 < m.hi; k0 += kTile) {
-        if (live) mark_keys(m, k0);
-        load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.K, a.ld_k, a.hd));
-        load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.V, a.ld_v, a.hd));
-        load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
-        __syncthreads();
-        float s[4][4], dp[4][4], ds[4][4], p;
-        dots<HD>(Q, K, s);
-        dots<HD>(G, V, dp);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float dx;
-                gradient(a, m, ty + 16 * r, tx + 16 * c, k0, s[r][c], dp[r][c], &p, &ds[r][c], &dx);
-                s[r][c] = dx;
-                if (learned) S[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = ds[r][c];
-            }
-        if (learned) {
+    by_rows(learned ? kTile : rows - q0, [&](auto groups) {  // the diagonals' sums read every row
+        constexpr int R = decltype(groups)::value;
+        for (int k0 = m.lo / kTile * kTile; k0 < m.hi; k0 += kTile) {
+            if (live) mark_keys(m, k0);
+            load_tile<T, HD>(K, a.K, a.ld_k, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.K, a.ld_k, a.hd));
+            load_tile<T, HD>(V, a.V, a.ld_v, row0, k0, rows, kv * a.hd, a.hd, live, vectors<T>(a.V, a.ld_v, a.hd));
+            load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
             __syncthreads();
-            const int t = threadIdx.x;
-            if (t > 0 && t < 2 * kTile) {  // diagonal i - j = t - 64, top to bottom
-                const int d = t - kTile;
-                float v = 0.f;
-                for (int i = max(d, 0); i < min(kTile, kTile + d); ++i) v += S[i * (kTile + 4) + i - d];
-                m.diag[t] = v;
-                const int64_t far = min(max((int64_t)q0 - k0 + d, -a.reach), a.reach);
-                m.ids[t] = a.bucket[far + a.reach];
+            float s[4][4], dp[4][4], ds[4][4], p;
+            dots<HD, R>(Q, K, s);
+            dots<HD, R>(G, V, dp);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float dx;
+                    gradient(a, m, ty + 16 * r, tx + 16 * c, k0, s[r][c], dp[r][c], &p, &ds[r][c], &dx);
+                    s[r][c] = dx;
+                    if (learned) S[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = ds[r][c];
+                }
+            if (learned) {
+                __syncthreads();
+                const int t = threadIdx.x;
+                if (t > 0 && t < 2 * kTile) {  // diagonal i - j = t - 64, top to bottom
+                    const int d = t - kTile;
+                    float v = 0.f;
+                    for (int i = max(d, 0); i < min(kTile, kTile + d); ++i) v += S[i * (kTile + 4) + i - d];
+                    m.diag[t] = v;
+                    const int64_t far = min(max((int64_t)q0 - k0 + d, -a.reach), a.reach);
+                    m.ids[t] = a.bucket[far + a.reach];
+                }
+                __syncthreads();
+                for (int b = t; b < a.n_buckets; b += kThreads) {
+                    float v = mine[b];
+                    for (int i = 1; i < 2 * kTile; ++i)
+                        if (m.ids[i] == b) v += m.diag[i];
+                    mine[b] = v;
+                }
+                __syncthreads();
             }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) S[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = s[r][c];
             __syncthreads();
-            for (int b = t; b < a.n_buckets; b += kThreads) {
-                float v = mine[b];
-                for (int i = 1; i < 2 * kTile; ++i)
-                    if (m.ids[i] == b) v += m.diag[i];
-                mine[b] = v;
-            }
+            weigh<HD, R>(S, K, acc, min(rows - k0, kTile));
             __syncthreads();
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) S[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = s[r][c];
-        __syncthreads();
-        weigh<HD>(S, K, acc);
-        __syncthreads();
-    }
+    });
     const float by[4] = {a.scale, a.scale, a.scale, a.scale};
     store_tile<T, HD>(a.dQ, a.ld_dq, row0, q0, rows, h * a.hd, a.hd, acc, by);
 }
@@ -405,39 +432,42 @@ __device__ __forceinline__ void dkv_tile(const Attention& a, const float* delta,
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < HD / 16; ++c) dk[r][c] = dv[r][c] = 0.f;
-    for (int q0 = !a.range && a.causal ? k0 : 0; q0 < rows; q0 += kTile) {
-        bool any = false;
-        if (threadIdx.x < kTile) {
-            const int2 v = visible(a.range, a.causal, rows, row0, q0 + threadIdx.x);
-            m.see[threadIdx.x] = v;
-            any = max(v.x, k0) < min(v.y, k0 + kTile);
-            m.live[threadIdx.x] = any;
-        }
-        if (!__syncthreads_or(any)) continue;
-        for (int h = kv * group; h < (kv + 1) * group; ++h) {
-            load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, a.range ? m.live : nullptr, vectors<T>(a.Q, a.ld_q, a.hd));
-            load_tile<T, HD>(G, a.dO, a.ld_do, row0, q0, rows, h * a.hd, a.hd, a.range ? m.live : nullptr, vectors<T>(a.dO, a.ld_do, a.hd));
-            load_stats(a, m, delta, n, h, q0);
-            load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
-            __syncthreads();
-            float s[4][4], dp[4][4];
-            dots<HD>(K, Q, s);  // rows are keys
-            dots<HD>(V, G, dp);
+    by_rows(rows - k0, [&](auto groups) {
+        constexpr int R = decltype(groups)::value;
+        for (int q0 = !a.range && a.causal ? k0 : 0; q0 < rows; q0 += kTile) {
+            bool any = false;
+            if (threadIdx.x < kTile) {
+                const int2 v = visible(a.range, a.causal, rows, row0, q0 + threadIdx.x);
+                m.see[threadIdx.x] = v;
+                any = max(v.x, k0) < min(v.y, k0 + kTile);
+                m.live[threadIdx.x] = any;
+            }
+            if (!__syncthreads_or(any)) continue;
+            for (int h = kv * group; h < (kv + 1) * group; ++h) {
+                load_tile<T, HD>(Q, a.Q, a.ld_q, row0, q0, rows, h * a.hd, a.hd, a.range ? m.live : nullptr, vectors<T>(a.Q, a.ld_q, a.hd));
+                load_tile<T, HD>(G, a.dO, a.ld_do, row0, q0, rows, h * a.hd, a.hd, a.range ? m.live : nullptr, vectors<T>(a.dO, a.ld_do, a.hd));
+                load_stats(a, m, delta, n, h, q0);
+                load_biases<T>(a, m.biases, h, (int64_t)q0 - k0);
+                __syncthreads();
+                float s[4][4], dp[4][4];
+                dots<HD, R>(K, Q, s);  // rows are keys
+                dots<HD, R>(V, G, dp);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float p, ds, dx;
-                    gradient(a, m, tx + 16 * c, ty + 16 * r, k0, s[r][c], dp[r][c], &p, &ds, &dx);
-                    P[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = p;
-                    S[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = dx;
-                }
-            __syncthreads();
-            weigh<HD>(P, G, dv);
-            weigh<HD>(S, Q, dk);
-            __syncthreads();
+                    for (int c = 0; c < 4; ++c) {
+                        float p, ds, dx;
+                        gradient(a, m, tx + 16 * c, ty + 16 * r, k0, s[r][c], dp[r][c], &p, &ds, &dx);
+                        P[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = p;
+                        S[(ty + 16 * r) * (kTile + 4) + tx + 16 * c] = dx;
+                    }
+                __syncthreads();
+                weigh<HD, R>(P, G, dv, min(rows - q0, kTile));
+                weigh<HD, R>(S, Q, dk, min(rows - q0, kTile));
+                __syncthreads();
+            }
         }
-    }
+    });
     const float by[4] = {a.scale, a.scale, a.scale, a.scale}, one[4] = {1.f, 1.f, 1.f, 1.f};
     store_tile<T, HD>(a.dK, a.ld_dk, row0, k0, rows, kv * a.hd, a.hd, dk, by);
     store_tile<T, HD>(a.dV, a.ld_dv, row0, k0, rows, kv * a.hd, a.hd, dv, one);
