@@ -887,18 +887,21 @@ bool attention_tc_supported(const Attention& a, bool backward) {
 }
 
 void attention_near(Attention& a, float by) {
-    // tanh x = x P(x^2) for |x| <= 1/2, a minimax fit
+    // tanh x = x P(x^2) for |x| <= 1/2, a minimax fit. Where the cap is so large that a coefficient leaves fp32's range, it and
+    // those above it are left out, and what is near ends where they would be 2^-24 of the value.
     constexpr double fit[5] = {0.017135003581643105, -0.05298607423901558, 0.13324779272079468, -0.3333306908607483, 1.0};
-    a.near_limit = -1.f;  // no dot product is near
+    constexpr double near[5] = {0.21, 0.1, 0.026, 0.0004, 0.0};  // without a term and those above it
+    a.near_limit = -1.f;                                         // no dot product is near
     if (!(a.cap > 0.f)) return;
     const double x = (double)a.scale / a.cap;
-    bool fine = x > 0x1p-20 && x < 0x1p20;
+    double most = 0.5;
     for (int k = 0; k < 5; ++k) {
-        const float c = (float)(fit[k] * by * std::pow(x, 9 - 2 * k));
+        float c = (float)(fit[k] * by * std::pow(x, 9 - 2 * k));
+        if (!std::isfinite(c)) return;
+        if (!std::isnormal(c)) c = 0.f, most = near[k];
         a.near[k] = make_float2(c, c);
-        fine = fine && std::isnormal(c);
     }
-    if (fine) a.near_limit = (float)(0.5 / x);
+    if (most > 0) a.near_limit = (float)std::min(most / x, 0x1p60);  // its square is finite
 }
 
 size_t attention_plan_bytes(const Attention& a, bool bound) {

@@ -273,6 +273,19 @@ def test_scores_at_the_cap(dev, cap, buckets):
     check_backward(p, f, b, beta=0.5 if buckets else 0.0, grad=F32)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cap", [1e3, 3e3, 2e4, 1e6, 1e9, 1e30])
+def test_large_caps(dev, cap, dtype):
+    """Caps that hardly bend the scores cost them no digits: the bounds are those of scores without a cap."""
+    p = Problem(dev, 1, 200, 2, 1, 64, dtype, "causal", cap, sigma=2.0)
+    check_forward(p)
+    f = p.exact()
+    b = Bounds(f, dtype, p.T, p.hd, 0.0, None)
+    near(p.heads(p.O, p.H), f["o"], b.o(), "O")
+    near(p.lse, f["lse"], b.lse(), "lse")
+    check_backward(p, f, b)
+
+
 MORE = [
     ((12, 300, 16, 4, 128), "docs", 20.0, 32, 128, True),   # items over several rounds, a row of scores over two warps
     ((40, 129, 8, 8, 64), "any", 5.0, 300, 60, False),
