@@ -448,9 +448,9 @@ struct DqShape {
 };
 struct DqBars {
     uint64_t item_full[4], item_empty[4], q_full, q_empty, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free,
-        ds_ready[2], dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, done;
+        ds_ready[2], dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, delta_full[4], done;
     int4 items[4][2];
-    float flat[kRowWarps][2];
+    float flat[kRowWarps][2], delta[4][kTileT];
     uint32_t tmem;
     int abort;
 };
@@ -511,7 +511,7 @@ __device__ __forceinline__ void transpose_quads(uint4 (&v)[4]) {
 template <int HD, bool RICH>
 __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-    const __grid_constant__ CUtensorMap tmG, const Attention a, const AttentionPlan plan, const DqItems items, const float* stats,
+    const __grid_constant__ CUtensorMap tmG, const Attention a, const AttentionPlan plan, const DqItems items, float* stats,
     float* part, unsigned int* err) {
     using S = DqShape<HD, RICH>;
     constexpr uint32_t kBytes = Tiles<HD>::kBytes;
@@ -542,6 +542,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                                 &bars.bias_empty[1], &bars.flat_full})
                 mbar_init(smem_u32(b), kRowWarps);
             for (uint64_t* b : {&bars.bias_full[0], &bars.bias_full[1]}) mbar_init(smem_u32(b), 32);
+            for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bars.delta_full[i]), 4);
             for (int i = 0; i < S::kK; ++i) mbar_init(smem_u32(&bars.k_full[i]), 1), mbar_init(smem_u32(&bars.k_empty[i]), 1);
             for (int i = 0; i < S::kV; ++i) mbar_init(smem_u32(&bars.v_full[i]), 1), mbar_init(smem_u32(&bars.v_empty[i]), 1);
             bars.abort = 0;
@@ -567,7 +568,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
         const float by = RICH && a.cap > 0.f ? -a.scale : a.scale;  // the slope's sign
-        uint32_t it = 0, diags = 0, done = 0, written = 0;  // key tiles, diagonals, outputs, items' sums so far
+        uint32_t it = 0, diags = 0, done = 0, written = 0, alone = 0;  // key tiles, diagonals, outputs, items' sums, items of one tile so far
         float* halves = (float*)(raw + S::kHalves) + warp * 128;
         if (learned)
             for (int i = lane; i < 128; i += 32) halves[i] = 0.f;  // some are never written
@@ -590,7 +591,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             }
             if (item.h < 0) continue;
             const int q0 = item.tile * kTileT;
-            const float2 nl = both(stat.x), nd = both(stat.y);
+            const float2 nl = both(stat.x);
+            float2 nd = both(stat.y);
             const bool single = see.y - see.x <= 1, idle = __any_sync(0xffffffffu, see.x >= see.y);
             float flat[2] = {0.f, 0.f};
             for (int kt = item.first; kt <= item.last; ++kt, ++it) {
@@ -632,8 +634,24 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 tmem_ld32(tP + lanes + 32 * quarter, d);
                 tmem_wait_ld();
                 tmem_use(d);
+                if (item.first == item.last) {
+                    // All keys of the rows are here, so dO.O is the sum of P dP, without the rounding that O was stored with: few
+                    // keys leave little of dP - dO.O (6 tokens of 2 heads: gradients 0.0046 off, 0.0023 so, both of the values' norm). For dK and dV too.
+                    float sum = 0.f;
+                    if (some) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum = seen >> j & 1 ? fmaf(p[j], d[j], sum) : sum;
+                    }
+                    bars.delta[quarter][row] = sum;
+                    arrive_warp(&bars.delta_full[warp % 4]);
+                    ok = wait_all(&bars.delta_full[warp % 4], alone++ & 1, abort, err);
+                    if (!ok) break;
+                    sum = bars.delta[0][row] + bars.delta[1][row] + bars.delta[2][row] + bars.delta[3][row];
+                    nd = both(-sum);
+                    if (quarter == 0) stats[(((int64_t)item.n * a.H + item.h) * tiles + item.tile) * 2 * kTileT + kTileT + row] = -sum;
+                }
                 tc_fence_before();
-                arrive_warp(&bars.dp_free);
+                arrive_warp(&bars.dp_free);  // nobody writes to delta again before all have read it
                 uint32_t w[16];
                 if (some) {
 #pragma unroll
@@ -1047,7 +1065,7 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     items.tiles = (int)tiles, items.total = (int)(tiles * a.N * a.H);
     items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
     if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())),
-                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, with, plan, items, (const float*)stats, part, err))
+                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, with, plan, items, stats, part, err))
         return e;
     return launch_chained(true, attention_dkv_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.KV)), dim3(kThreads), Kv::kSmem, s, q,
                           k, v, g, dk, dv, with, plan, (const float*)stats, err);

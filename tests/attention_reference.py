@@ -104,12 +104,15 @@ class Bounds:
         off = f["p"] * (2 * self.e + 2 * (f["p"] * self.e).sum(3, keepdim=True) + self.up + 2 * self.g)
         return off @ f["v"].abs() + self.u * f["o"].abs() + 1e-37
 
-    def grads(self, r, scale, KV, bucket=None, reach=0, n_buckets=0, grad_u=None):
+    def grads(self, r, scale, KV, bucket=None, reach=0, n_buckets=0, grad_u=None, summed=False):
+        """summed: dO . O is the sum of P dP in fp32, not taken from the stored O."""
         f = self.f
         N, H, T, d = r["do"].shape
         dp_mag = r["do"].abs() @ f["v"].abs().transpose(2, 3)
         delta_off = (r["do"].abs() * (self.o() + self.g * f["o"].abs())).sum(3, keepdim=True)
         p_off = 2 * self.e + 2 * (f["p"] * self.e).sum(3, keepdim=True) + 2.0 ** -20
+        if summed:
+            delta_off = (f["p"] * (p_off * r["dp"].abs() + self.g * dp_mag + 2.0 ** -24 * T * r["dp"].abs())).sum(3, keepdim=True)
         many = f["seen"].sum(3, keepdim=True) > 1
         ds_off = many * f["p"] * (p_off * (r["dp"] - r["delta"]).abs() + self.g * dp_mag + delta_off
                                   + 2.0 ** -22 * (r["dp"].abs() + r["delta"].abs()))

@@ -152,13 +152,13 @@ def check_forward(p):
     return f, b
 
 
-def check_backward(p, f, b, beta=0.0, grad=None):
+def check_backward(p, f, b, beta=0.0, grad=None, summed=False):
     bufs = p.backward(beta, grad)
     tda.tda_device_status()
     r = gradients(f, p.heads(p.dO, p.H), p.scale, p.KV, p.bucket, p.reach, p.buckets)
     if p.buckets:
         r["dtable"] = r["dtable"] + beta * 0.5
-    tol = b.grads(r, p.scale, p.KV, p.bucket, p.reach, p.buckets, {BF: 2.0 ** -8, F32: 2.0 ** -24}[grad or p.dtype])
+    tol = b.grads(r, p.scale, p.KV, p.bucket, p.reach, p.buckets, {BF: 2.0 ** -8, F32: 2.0 ** -24}[grad or p.dtype], summed)
     near(p.heads(p.dQ, p.H), r["dQ"], tol["dQ"], "dQ")
     near(p.heads(p.dK, p.KV), r["dK"], tol["dK"], "dK")
     near(p.heads(p.dV, p.KV), r["dV"], tol["dV"], "dV")
@@ -271,6 +271,15 @@ def test_scores_at_the_cap(dev, cap, buckets):
     p.K[:, 8] = -(cap / p.scale)
     f, b = check_forward(p)
     check_backward(p, f, b, beta=0.5 if buckets else 0.0, grad=F32)
+
+
+@pytest.mark.parametrize("mask", ["causal", "docs", "any"])
+@pytest.mark.parametrize("T,hd", [(2, 64), (6, 96), (17, 128), (40, 64), (100, 80), (128, 128)])
+def test_gradients_of_few_keys(dev, T, hd, mask):
+    """Keys of one tile: the gradients do without the stored O and the errors that its rounding has left in it."""
+    p = Problem(dev, 3, T, 4, 2, hd, BF, mask, 0.0 if T % 4 else 30.0, 7, 9, sigma=1.3)
+    f, b = check_forward(p)
+    check_backward(p, f, b, grad=F32, summed=True)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
