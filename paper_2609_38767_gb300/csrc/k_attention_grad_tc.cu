@@ -636,7 +636,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 tmem_use(d);
                 if (item.first == item.last) {
                     // All keys of the rows are here, so dO.O is the sum of P dP, without the rounding that O was stored with: few
-                    // keys leave little of dP - dO.O (6 tokens of 2 heads: gradients 0.0046 off, 0.0023 so, both of the values' norm). For dK and dV too.
+                    // keys leave little of dP - dO.O (6 tokens of 2 heads: gradients 0.0046 of their norm off, 0.0023 so). For dK and dV too.
                     float sum = 0.f;
                     if (some) {
 #pragma unroll
