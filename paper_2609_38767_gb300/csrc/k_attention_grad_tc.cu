@@ -575,21 +575,21 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         bool ok = true;
         DqReader reader;
         DqItem item, then;
-        then.h = -2;
         int2 see, see_then = make_int2(0, 0);
         float2 stat, stat_then = make_float2(0.f, 0.f);
-        while (ok) {
-            // the next item and what this thread's row sees and has in it, one item ahead
-            item = then, see = see_then, stat = stat_then;
-            if (item.h == -1) break;
+        // the next item and what this thread's row sees and has in it
+        auto look = [&]() {
             if (!reader.next(then, bars, &ok, abort, err)) {
                 then.h = -1;
-            } else {
-                see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, then.tile * kTileT + row);
-                const float* st = stats + (((int64_t)then.n * a.H + then.h) * tiles + then.tile) * 2 * kTileT;
-                stat_then = make_float2(st[row], st[kTileT + row]);
+                return;
             }
-            if (item.h < 0) continue;
+            see_then = visible(a.range, a.causal, T, (int64_t)then.n * T, then.tile * kTileT + row);
+            const float* st = stats + (((int64_t)then.n * a.H + then.h) * tiles + then.tile) * 2 * kTileT;
+            stat_then = make_float2(st[row], st[kTileT + row]);
+        };
+        look();
+        while (ok && then.h >= 0) {
+            item = then, see = see_then, stat = stat_then;
             const int q0 = item.tile * kTileT;
             const float2 nl = both(stat.x);
             float2 nd = both(stat.y);
@@ -743,7 +743,8 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 }
             }
             const bool any = item.first <= item.last;
-            if (any) ok = wait_all(&bars.dq_done, done++ & 1, abort, err);
+            look();  // while the last MMAs are under way
+            if (any) ok = ok && wait_all(&bars.dq_done, done++ & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
             // 32 columns each (all quarters, or the first two), four lanes to 64 bytes of a row on the way out
