@@ -448,7 +448,7 @@ struct DqShape {
 };
 struct DqBars {
     uint64_t item_full[4], item_empty[4], q_full, q_empty, k_full[4], k_empty[4], v_full[3], v_empty[3], s_full[2], dp_full, dp_free,
-        ds_ready[2], dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, delta_full[4], done;
+        ds_ready[2], dq_done, bias_full[2], bias_empty[2], diag_full[2], diag_empty[2], flat_full, flat_empty, delta_full[4], out_full, done;
     int4 items[4][2];
     float flat[kRowWarps][2], delta[4][kTileT];
     uint32_t tmem;
@@ -511,7 +511,8 @@ __device__ __forceinline__ void transpose_quads(uint4 (&v)[4]) {
 template <int HD, bool RICH>
 __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
     const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-    const __grid_constant__ CUtensorMap tmG, const Attention a, const AttentionPlan plan, const DqItems items, float* stats,
+    const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmdQ, const Attention a, const AttentionPlan plan,
+    const DqItems items, float* stats,
     float* part, unsigned int* err) {
     using S = DqShape<HD, RICH>;
     constexpr uint32_t kBytes = Tiles<HD>::kBytes;
@@ -534,12 +535,12 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         tmem_alloc(smem_u32(&bars.tmem), 512);
         tmem_relinquish();
         if (lane == 0) {
-            for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bars.item_full[i]), 1), mbar_init(smem_u32(&bars.item_empty[i]), kRowWarps + 2 + learned);
+            for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bars.item_full[i]), 1), mbar_init(smem_u32(&bars.item_empty[i]), kRowWarps + 2 + (!RICH || learned));
             for (uint64_t* b : {&bars.q_full, &bars.q_empty, &bars.s_full[0], &bars.s_full[1], &bars.dp_full, &bars.dq_done, &bars.done,
                                 &bars.diag_empty[0], &bars.diag_empty[1], &bars.flat_empty})
                 mbar_init(smem_u32(b), 1);
             for (uint64_t* b : {&bars.dp_free, &bars.ds_ready[0], &bars.ds_ready[1], &bars.diag_full[0], &bars.diag_full[1], &bars.bias_empty[0],
-                                &bars.bias_empty[1], &bars.flat_full})
+                                &bars.bias_empty[1], &bars.flat_full, &bars.out_full})
                 mbar_init(smem_u32(b), kRowWarps);
             for (uint64_t* b : {&bars.bias_full[0], &bars.bias_full[1]}) mbar_init(smem_u32(b), 32);
             for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&bars.delta_full[i]), 4);
@@ -747,28 +748,39 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             if (any) ok = ok && wait_all(&bars.dq_done, done++ & 1, abort, err);
             if (!ok) break;
             tc_fence_after();
-            // 32 columns each (all quarters, or the first two), four lanes to 64 bytes of a row on the way out
-            if (quarter < HD / 32 && 32 * quarter < a.hd) {
-                float o[32];
-                uint4 v[4];
-                tmem_ld32(tdQ + lanes + 32 * quarter, o);
-                tmem_wait_ld();
-                tmem_use(o);
+            if constexpr (RICH) {
+                // 32 columns each (all quarters, or the first two), four lanes to 64 bytes of a row on the way out: warp 19 would be
+                // late with them here, busy with diagonals (packed documents 330 us, 334 with it)
+                if (quarter < HD / 32 && 32 * quarter < a.hd) {
+                    float o[32];
+                    uint4 v[4];
+                    tmem_ld32(tdQ + lanes + 32 * quarter, o);
+                    tmem_wait_ld();
+                    tmem_use(o);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float* x = o + 8 * g;
-                    v[g] = any ? make_uint4(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by), pack_bf16(x[4] * by, x[5] * by),
-                                            pack_bf16(x[6] * by, x[7] * by))
-                               : make_uint4(0, 0, 0, 0);
-                }
-                transpose_quads(v);
-                const int col = 32 * quarter + lane % 4 * 8, first_row = q0 + warp % 4 * 32 + lane / 4 * 4;
-                __nv_bfloat16* out = (__nv_bfloat16*)a.dQ + ((int64_t)item.n * T + first_row) * a.ld_dq + item.h * a.hd + col;
-                if (col < a.hd) {
+                    for (int g = 0; g < 4; ++g) {
+                        const float* x = o + 8 * g;
+                        v[g] = any ? make_uint4(pack_bf16(x[0] * by, x[1] * by), pack_bf16(x[2] * by, x[3] * by), pack_bf16(x[4] * by, x[5] * by),
+                                                pack_bf16(x[6] * by, x[7] * by))
+                                   : make_uint4(0, 0, 0, 0);
+                    }
+                    transpose_quads(v);
+                    const int col = 32 * quarter + lane % 4 * 8, first_row = q0 + warp % 4 * 32 + lane / 4 * 4;
+                    __nv_bfloat16* out = (__nv_bfloat16*)a.dQ + ((int64_t)item.n * T + first_row) * a.ld_dq + item.h * a.hd + col;
+                    if (col < a.hd) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (first_row + k < T) *(uint4*)(out + k * a.ld_dq) = v[k];
+                        for (int k = 0; k < 4; ++k)
+                            if (first_row + k < T) *(uint4*)(out + k * a.ld_dq) = v[k];
+                    }
                 }
+            } else if (any) {
+                // to where the last tile of keys was; warp 19 sends them on (8 x 1024 tokens 232 us with the stores above, 227 so)
+                if (quarter < HD / 32) stage_columns(tdQ + lanes, sk + (it - 1) % S::kK * kBytes, row, quarter, by, true);
+                fence_proxy_async();
+                arrive_warp(&bars.out_full);
+            } else if (q0 + row < T) {
+                uint4* out = (uint4*)((__nv_bfloat16*)a.dQ + ((int64_t)item.n * T + q0 + row) * a.ld_dq + item.h * a.hd);
+                for (int c = quarter; c < a.hd / 8; c += 4) out[c] = make_uint4(0, 0, 0, 0);
             }
             tc_fence_before();
         }
@@ -845,7 +857,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                     if (!ok) break;
                     tc_fence_after();
                     mma_quarters(lead, tdQ, tmem + (it & 1) * 128, sk + it % S::kK * kBytes, kIdO, now.kt == now.item.first);
-                    commit(lead, smem_u32(&bars.k_empty[it % S::kK]));
+                    if (RICH || now.kt != now.last) commit(lead, smem_u32(&bars.k_empty[it % S::kK]));
                     if (now.kt == now.last) commit(lead, smem_u32(&bars.dq_done));
                     ++it;
                 }
@@ -907,81 +919,97 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                 }
             }
             if (queries) wait_settled(smem_u32(&bars.q_full), (queries - 1) & 1, err);
-        } else if (RICH && learned) {
-            // sums of the diagonals of each pair of tiles, in the order of the tiles: by distance where there is room for all of them,
-            // else by bucket
+        } else if (!RICH || learned) {
+            // the outputs, or the sums of the diagonals of each pair of tiles, in the order of the tiles: by distance where there is
+            // room for all of them, else by bucket
             float* hist = (float*)(raw + S::kHist);
             const int width = dense ? 2 * dense_mid + 1 : a.n_buckets;
-            for (int i = lane; i < 2 * kRowWarps; i += 32) ((float*)(raw + S::kDiag))[i * 64 + 63] = 0.f;  // read below, never written
-            uint32_t diags = 0, read = 0;
+            for (int i = lane; RICH && i < 2 * kRowWarps; i += 32) ((float*)(raw + S::kDiag))[i * 64 + 63] = 0.f;  // read below, never written
+            const uint32_t lead = elect_one();
+            uint32_t diags = 0, read = 0, used = 0, outs = 0;
             DqReader reader;
             DqItem item;
             while (reader.next(item, bars, &ok, abort, err)) {
-                for (int b = lane; b < width; b += 32) hist[b] = 0.f;
-                __syncwarp();
-                for (int kt = item.first; ok && kt <= item.last; ++kt) {
-                    if (flat_at(item.tile, kt)) continue;
-                    ok = wait_all(&bars.diag_full[diags & 1], (diags / 2) & 1, abort, err);
-                    if (!ok) break;
-                    const float* diag = (const float*)(raw + S::kDiag) + (diags & 1) * kRowWarps * 64;
+                if constexpr (RICH) {
+                    for (int b = lane; b < width; b += 32) hist[b] = 0.f;
+                    __syncwarp();
+                    for (int kt = item.first; ok && kt <= item.last; ++kt) {
+                        if (flat_at(item.tile, kt)) continue;
+                        ok = wait_all(&bars.diag_full[diags & 1], (diags / 2) & 1, abort, err);
+                        if (!ok) break;
+                        const float* diag = (const float*)(raw + S::kDiag) + (diags & 1) * kRowWarps * 64;
 #pragma unroll 1
-                    for (int x = 0; x < 8; ++x) {
-                        // row - column = 32 x - 127 + lane in the pair of tiles; 32 (row quarter - column quarter) is 32 (x - 3) with
-                        // lane - 31 left, or 32 (x - 4) with lane + 1
-                        float v = 0.f;
+                        for (int x = 0; x < 8; ++x) {
+                            // row - column = 32 x - 127 + lane in the pair of tiles; 32 (row quarter - column quarter) is 32 (x - 3) with
+                            // lane - 31 left, or 32 (x - 4) with lane + 1
+                            float v = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
+                            for (int e = 0; e < 2; ++e)
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                const int r = c + x - 3 - e;
-                                if (r >= 0 && r < 4) v += diag[(c * 4 + r) * 64 + lane + 32 * e];
-                            }
-                        const int64_t apart = ((int64_t)item.tile - kt) * kTileT + 32 * x + lane - 127;
-                        const int64_t far = min(max(apart, -a.reach), a.reach);
-                        if (dense) {
-                            // the distances beyond the table's reach meet
-                            float ends[2] = {apart <= -a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
-                            if (apart > -a.reach && apart < a.reach && apart >= -dense_mid && apart <= dense_mid) hist[apart + dense_mid] += v;
-                            if (__any_sync(0xffffffffu, ends[0] != 0.f || ends[1] != 0.f)) {
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                                    for (int o = 16; o; o >>= 1) ends[e] += __shfl_xor_sync(0xffffffffu, ends[e], o);
-                                    if (lane == 0) hist[e ? 2 * dense_mid : 0] += ends[e];
+                                for (int c = 0; c < 4; ++c) {
+                                    const int r = c + x - 3 - e;
+                                    if (r >= 0 && r < 4) v += diag[(c * 4 + r) * 64 + lane + 32 * e];
                                 }
-                            }
-                            __syncwarp();
-                            continue;
-                        }
-                        int id = a.bucket[far + a.reach];
-                        if (id >= a.n_buckets) id = -1;
-                        uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
-                        while (left) {
-                            const int who = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
-                            const bool in = id == who;
-                            float s = in ? v : 0.f;
+                            const int64_t apart = ((int64_t)item.tile - kt) * kTileT + 32 * x + lane - 127;
+                            const int64_t far = min(max(apart, -a.reach), a.reach);
+                            if (dense) {
+                                // the distances beyond the table's reach meet
+                                float ends[2] = {apart <= -a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
+                                if (apart > -a.reach && apart < a.reach && apart >= -dense_mid && apart <= dense_mid) hist[apart + dense_mid] += v;
+                                if (__any_sync(0xffffffffu, ends[0] != 0.f || ends[1] != 0.f)) {
 #pragma unroll
-                            for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                            if (lane == 0) hist[who] += s;
-                            left &= ~__ballot_sync(0xffffffffu, in);
+                                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                                        for (int o = 16; o; o >>= 1) ends[e] += __shfl_xor_sync(0xffffffffu, ends[e], o);
+                                        if (lane == 0) hist[e ? 2 * dense_mid : 0] += ends[e];
+                                    }
+                                }
+                                __syncwarp();
+                                continue;
+                            }
+                            int id = a.bucket[far + a.reach];
+                            if (id >= a.n_buckets) id = -1;
+                            uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
+                            while (left) {
+                                const int who = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
+                                const bool in = id == who;
+                                float s = in ? v : 0.f;
+#pragma unroll
+                                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                                if (lane == 0) hist[who] += s;
+                                left &= ~__ballot_sync(0xffffffffu, in);
+                            }
+                        }
+                        arrive_warp(&bars.diag_empty[diags & 1]);
+                        ++diags;
+                    }
+                    ok = ok && wait_all(&bars.flat_full, read++ & 1, abort, err);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        for (int e = 0; e < 2; ++e) {
+                            float s = 0.f;
+                            for (int w = 0; w < kRowWarps; ++w) s += bars.flat[w][e];
+                            const int id = dense ? (e ? 2 * dense_mid : 0) : a.bucket[e ? 2 * a.reach : 0];
+                            if (dense || (id >= 0 && id < a.n_buckets)) hist[id] += s;
                         }
                     }
-                    arrive_warp(&bars.diag_empty[diags & 1]);
-                    ++diags;
+                    arrive_warp(&bars.flat_empty);
+                    float* mine = part + ((int64_t)item.h * a.N * tiles + (int64_t)item.n * tiles + item.tile) * width;
+                    for (int b = lane; b < width; b += 32) mine[b] = hist[b];
+                    __syncwarp();
                 }
-                ok = ok && wait_all(&bars.flat_full, read++ & 1, abort, err);
+                if (RICH || item.first > item.last) continue;
+                used += item.last - item.first + 1;
+                ok = wait_all(&bars.out_full, outs++ & 1, abort, err);
                 if (!ok) break;
-                if (lane == 0) {
-                    for (int e = 0; e < 2; ++e) {
-                        float s = 0.f;
-                        for (int w = 0; w < kRowWarps; ++w) s += bars.flat[w][e];
-                        const int id = dense ? (e ? 2 * dense_mid : 0) : a.bucket[e ? 2 * a.reach : 0];
-                        if (dense || (id >= 0 && id < a.n_buckets)) hist[id] += s;
-                    }
+                const uint32_t at = (used - 1) % S::kK;
+                if (lead) {
+#pragma unroll
+                    for (int p = 0; p < kPanels; ++p)
+                        if (64 * p < a.hd) tma_store_head(&tmdQ, sk + at * kBytes + p * kPanel, 64 * p, item.h, item.tile * kTileT, item.n);
+                    asm volatile("cp.async.bulk.commit_group;\n cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    mbar_arrive(smem_u32(&bars.k_empty[at]));
                 }
-                arrive_warp(&bars.flat_empty);
-                float* mine = part + ((int64_t)item.h * a.N * tiles + (int64_t)item.n * tiles + item.tile) * width;
-                for (int b = lane; b < width; b += 32) mine[b] = hist[b];
                 __syncwarp();
             }
         }
@@ -1041,12 +1069,12 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     using Q = DqShape<HD, RICH>;
     if (cudaError_t e = smem_attr_once<attention_dkv_tc_kernel<HD, RICH>>(Kv::kSmem)) return e;
     if (cudaError_t e = smem_attr_once<attention_dq_tc_kernel<HD, RICH>>(Q::kSmem)) return e;
-    CUtensorMap q, k, v, g, dk, dv;
+    CUtensorMap q, k, v, g, dq, dk, dv;
     auto map = [&](CUtensorMap* m, const void* p, int64_t ld, int heads) {
         return attention_head_map(m, p, ld, heads, a.hd, a.T, a.N, kTileT);
     };
     if (!map(&q, a.Q, a.ld_q, a.H) || !map(&k, a.K, a.ld_k, a.KV) || !map(&v, a.V, a.ld_v, a.KV) || !map(&g, a.dO, a.ld_do, a.H) ||
-        !map(&dk, a.dK, a.ld_dk, a.KV) || !map(&dv, a.dV, a.ld_dv, a.KV))
+        !map(&dq, a.dQ, a.ld_dq, a.H) || !map(&dk, a.dK, a.ld_dk, a.KV) || !map(&dv, a.dV, a.ld_dv, a.KV))
         return cudaErrorInvalidValue;
     const int64_t tiles = (a.T + kTileT - 1) / kTileT;
     AttentionPlan plan;
@@ -1066,7 +1094,7 @@ cudaError_t run(const Attention& a, void* ws, unsigned int* err, cudaStream_t s)
     items.tiles = (int)tiles, items.total = (int)(tiles * a.N * a.H);
     items.heads = FastDiv((uint32_t)(a.N * a.H)), items.H = FastDiv(a.H), items.group = FastDiv(a.H / a.KV);
     if (cudaError_t e = launch_chained(true, attention_dq_tc_kernel<HD, RICH>, dim3((unsigned)std::min(items.total, train_sms())),
-                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, with, plan, items, stats, part, err))
+                                       dim3(kThreads), Q::kSmem, s, q, k, v, g, dq, with, plan, items, stats, part, err))
         return e;
     return launch_chained(true, attention_dkv_tc_kernel<HD, RICH>, dim3((unsigned)(tiles * a.N * a.KV)), dim3(kThreads), Kv::kSmem, s, q,
                           k, v, g, dk, dv, with, plan, (const float*)stats, err);
