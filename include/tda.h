@@ -731,7 +731,7 @@ tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float ma
  * dK and dV summed over the query heads that share them. dS of a token that sees a single
  * key is 0. P and dX are rounded to bf16 for bf16 products; dO . O takes O as it was stored
  * (bf16: an error of up to 2^-8 of |dO||O| in every dS of a row, in dtable too; on the tensor
- * cores only where the keys of a tile of 128 queries lie in more than one tile of 128 keys).
+ * cores only where a row's keys lie in more than one tile of 128).
  *   dQ, dK, dV  of L->dtype, overwritten; strides as Q, K, V. They overlap nothing else.
  *   dtable      [n_buckets][heads] of grad_dtype (TDA_F32, or TDA_BF16 for bf16 inputs), or
  *               NULL. slope has no gradient.

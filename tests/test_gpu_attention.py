@@ -282,6 +282,24 @@ def test_gradients_of_few_keys(dev, T, hd, mask):
     check_backward(p, f, b, grad=F32, summed=True)
 
 
+def test_gradients_of_narrow_windows(dev):
+    """The same for four keys a row in long examples, but where they lie in two tiles."""
+    T = 300
+    p = Problem(dev, 2, T, 4, 2, 64, BF, "full", 0.0, 5, 9, sigma=1.3)
+    at = torch.arange(T, device=dev)
+    p.range = torch.stack([(at - 3).clamp(min=0), at + 1], 1).int().expand(2, T, 2).contiguous()
+    p.seen = (at >= p.range[..., :1]) & (at < p.range[..., 1:])
+    f, b = check_forward(p)
+    p.backward(grad=F32)
+    tda.tda_device_status()
+    r = gradients(f, p.heads(p.dO, 4), p.scale, 2, p.bucket, p.reach, p.buckets)
+    tight, wide = (b.grads(r, p.scale, 2, p.bucket, p.reach, p.buckets, 2.0 ** -24, x) for x in (True, False))
+    q, k = (at % 128 < 3)[:, None], ((at % 128 < 3) | (at % 128 >= 125))[:, None]
+    near(p.heads(p.dQ, 4), r["dQ"], torch.where(q, wide["dQ"], tight["dQ"]), "dQ")
+    near(p.heads(p.dK, 2), r["dK"], torch.where(k, wide["dK"], tight["dK"]), "dK")
+    near(p.dtable, r["dtable"], wide["dtable"], "dtable")
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("cap", [1e3, 3e3, 2e4, 1e6, 1e9, 1e30])
 def test_large_caps(dev, cap, dtype):
