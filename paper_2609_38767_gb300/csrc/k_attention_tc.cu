@@ -795,14 +795,19 @@ __global__ __launch_bounds__(256) void attention_plan_kernel(const Attention a, 
         if (t % 32 == 0) tile.idle[t / 32] = idle;
     }
     uint32_t seen[4] = {0, 0, 0, 0};
-    for (int i = t; i < T; i += 256) {
-        const int2 r = visible(a.range, 0, T, (int64_t)n * T, i);
-        const int lo = r.x - k0, hi = r.y - k0;
-        if (hi <= 0 || lo >= kTileT || lo >= hi) continue;
+    for (int at = t; at < T; at += 8 * 256) {  // eight loads on their way at a time
+        int2 r[8];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int x = min(max(lo - 32 * w, 0), 32), y = min(max(hi - 32 * w, 0), 32);
-            if (x < y) seen[w] |= (y == 32 ? ~0u : (1u << y) - 1) & (~0u << x);
+        for (int e = 0; e < 8; ++e) r[e] = visible(a.range, 0, T, (int64_t)n * T, at + 256 * e);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int lo = r[e].x - k0, hi = r[e].y - k0;
+            if (hi <= 0 || lo >= kTileT || lo >= hi) continue;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int x = min(max(lo - 32 * w, 0), 32), y = min(max(hi - 32 * w, 0), 32);
+                if (x < y) seen[w] |= (y == 32 ? ~0u : (1u << y) - 1) & (~0u << x);
+            }
         }
     }
     __shared__ uint32_t all[4];
