@@ -222,10 +222,13 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
     bool bounded = false;
     if constexpr (RICH) {
         const float limit = 90.f / kLog2e - a.cap;
-        bool beyond = !(a.cap > 0.f && limit >= 0.f) || a.slope || (int64_t)a.n_buckets * a.H > 65536;
-        for (int i = threadIdx.x; !beyond && i < a.n_buckets * a.H; i += W::kThreads) {
+        const int64_t entries = (int64_t)a.n_buckets * a.H;  // read by every CTA
+        bool beyond = !(a.cap > 0.f && limit >= 0.f) || a.slope || entries > 16384;
+        const int read = beyond ? 0 : (int)entries;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < read; i += W::kThreads) {
             const float x = (float)((const __nv_bfloat16*)a.table)[i];
-            beyond = !(fabsf(x) <= limit || x == -CUDART_INF_F);
+            beyond |= !(fabsf(x) <= limit || x == -CUDART_INF_F);
         }
         if (!plan.lut)
             for (int i = threadIdx.x; i < 4 * kWindow; i += W::kThreads) ((float*)(from + S::kBias))[i] = 0.f;
@@ -495,7 +498,8 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             if (outputs++) ok = ok && wait_warp(smem_u32(&bars.o_free[w]), outputs & 1, abort, err);
             if (RICH) ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
             if (!ok) break;
-            bars.sums[w][half][row] = make_float2(top, sum);
+            // negative: of one key, whose weight is no power of two
+            bars.sums[w][half][row] = make_float2(top, RICH && bounded && see.y - see.x == 1 ? -sum : sum);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars.sum_full[w]));
         }
@@ -526,7 +530,10 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     if (RICH) sum += bars.sums[w][RICH][row].y;
                     tc_fence_after();
                 }
-                const float by = sum != 0.f ? 1.f / sum : 0.f;  // NaN sums stay NaN
+                // one key's value is divided by its weight as that was rounded; NaN sums stay NaN
+                const float over = RICH && sum < 0.f ? __bfloat162float(__float2bfloat16(sum)) : sum;
+                const float by = sum != 0.f ? 1.f / fabsf(over) : 0.f;
+                sum = fabsf(sum);
                 const uint32_t to = tmem + ((uint32_t)q << 21) + 256 + w * 128;
 #pragma unroll 1
                 for (int b = 0; b < HD / 32; ++b) {

@@ -313,6 +313,21 @@ def test_large_caps(dev, cap, dtype):
     check_backward(p, f, b)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("cap,buckets,slope", [(0.0, 0, False), (30.0, 6, False), (50.0, 0, False), (90.0, 6, False), (20.0, 0, True)])
+def test_single_keys(dev, cap, buckets, slope, dtype):
+    """A token that sees one key has that key's value, to the last bit; one key of the other half of a tile of keys among them."""
+    p = Problem(dev, 2, 200, 4, 2, 64, dtype, "full", cap, buckets, 30 if buckets else 0, slope, sigma=2.0)
+    key = torch.randint(0, 200, (2, 200), generator=torch.Generator().manual_seed(4)).to(dev)
+    p.range = torch.stack([key, key + 1], 2).int().contiguous()
+    p.seen = torch.arange(200, device=dev) == key[..., None]
+    f, b = check_forward(p)
+    v = p.heads(p.V, 2).repeat_interleave(2, 1).gather(2, key[:, None, :, None].expand(2, 4, 200, 64))
+    assert torch.equal(p.heads(p.O, 4), v)
+    check_backward(p, f, b)
+    assert (p.dQ == 0).all() and (p.dK == 0).all()
+
+
 MORE = [
     ((12, 300, 16, 4, 128), "docs", 20.0, 32, 128, True),   # items over several rounds, a row of scores over two warps
     ((40, 129, 8, 8, 64), "any", 5.0, 300, 60, False),
@@ -320,6 +335,7 @@ MORE = [
     ((2, 700, 4, 2, 128), "docs", 30.0, 600, 699, True),
     ((1, 600, 2, 2, 40), "full", 0.0, 33, 560, False),
     ((1, 1500, 3, 3, 64), "window", 50.0, 2, 0, False),       # one distance for all
+    ((1, 150, 32, 4, 64), "causal", 20.0, 1024, 140, False),  # a table that no CTA reads beforehand
 ]
 
 
