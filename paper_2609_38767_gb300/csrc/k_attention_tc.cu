@@ -258,18 +258,26 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
             return fmaxf(mine, at[(warp ^ 4) * 64]);
         };
-        // O of the rows (RICH: half of its columns) times a number, once the MMAs before key tile `turn` are done
+        // O of the rows (RICH: half of its columns) times a number, once the MMAs before key tile `turn` are done. RICH: the weights of
+        // one half of the keys are added to all columns as soon as their warps are ready, so both warps of a row have its O rescaled
+        // before either goes on. Whether `by` is asked for is the same in both.
         auto rescale = [&](uint32_t turn, float by) {
             ok = ok && wait_warp(smem_u32(&bars.o_done[w]), (turn - 1) & 1, abort, err);
-            if (!ok) return;
-            tc_fence_after();
+            if (ok) {
+                tc_fence_after();
 #pragma unroll 1
-            for (int b = 0; b < HD / 16 / (RICH ? 2 : 1); ++b) {
-                float o[16];
-                tmem_ld16(to + 16 * b, o);
+                for (int b = 0; b < HD / 16 / (RICH ? 2 : 1); ++b) {
+                    float o[16];
+                    tmem_ld16(to + 16 * b, o);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) o[j] *= by;
-                tmem_st16(to + 16 * b, (const uint32_t*)o);
+                    for (int j = 0; j < 16; ++j) o[j] *= by;
+                    tmem_st16(to + 16 * b, (const uint32_t*)o);
+                }
+                if (RICH) tmem_wait_st();
+            }
+            if (RICH) {
+                tc_fence_before();
+                ok = all_came_well(1 + w * 4 + warp % 4, 64, ok);
             }
         };
         uint32_t turn = 0, outputs = 0;  // key tiles, outputs so far
@@ -392,8 +400,9 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                                 }
                                 tmem_st16(ts + 64 * half + 16 * b, p);
                             }
-                            if (kt != first) rescale(turn, by);
                             tmem_wait_st();
+                            if (kt != first) rescale(turn, by);
+                            if (!ok) break;
                         }
                         tc_fence_before();
                         __syncwarp();
@@ -442,7 +451,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     top = most_now;
                     sum *= by;
                     rescale(turn, by);
-                    if (!RICH && !ok) break;
+                    if (!ok) break;
                 }
                 const float base_of = top == -CUDART_INF_F ? 0.f : top;
                 const float2 less = both(RICH ? -base_of : -base_of * c);
