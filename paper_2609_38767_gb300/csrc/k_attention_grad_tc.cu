@@ -954,8 +954,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                             const int64_t apart = ((int64_t)item.tile - kt) * kTileT + 32 * x + lane - 127;
                             const int64_t far = min(max(apart, -a.reach), a.reach);
                             if (dense) {
-                                // the distances beyond the table's reach meet
-                                float ends[2] = {apart <= -a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
+                                // the distances beyond the table's reach meet, at either end once: with a reach of 0 all are beyond
+                                // it, and distance 0 is both ends'
+                                float ends[2] = {apart <= -a.reach && apart < a.reach ? v : 0.f, apart >= a.reach ? v : 0.f};
                                 if (apart > -a.reach && apart < a.reach && apart >= -dense_mid && apart <= dense_mid) hist[apart + dense_mid] += v;
                                 if (__any_sync(0xffffffffu, ends[0] != 0.f || ends[1] != 0.f)) {
 #pragma unroll
