@@ -881,12 +881,14 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
                     id = __shfl_sync(0xffffffffu, id, 0);
                 }
                 int4 x = make_int4(0, -1, 0, 0), y = make_int4(0, -1, 0, 0);
-                if (id < items.total) {
+                if ((uint32_t)id < (uint32_t)items.total) {
                     const int tile = tiles - 1 - items.heads.div(id), of = items.heads.mod(id), q0 = tile * kTileT;
                     x = make_int4(items.H.div(of), items.H.mod(of), tile, 0);
                     if (a.range) {
                         const AttentionTile& t = plan.tiles[(int64_t)x.x * tiles + tile];
-                        y = make_int4(t.lo / kTileT, t.lo < t.hi ? (t.hi - 1) / kTileT : -1, t.most, t.least);
+                        // in range whatever a workspace in other use by now holds
+                        const int lo = max(t.lo, 0), hi = min(t.hi, T);
+                        y = make_int4(lo / kTileT, lo < hi ? (hi - 1) / kTileT : -1, t.most, t.least);
                     } else {
                         y = make_int4(0, (a.causal ? min(q0 + kTileT, T) - 1 : T - 1) / kTileT, 0, a.causal ? q0 + 1 : T);
                     }

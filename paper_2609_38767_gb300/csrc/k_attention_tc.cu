@@ -86,7 +86,7 @@ __device__ __forceinline__ Hull hull_of(const Attention& a, const AttentionPlan&
     if (q0 >= a.T) return {0, 0, 0, 0};
     if (a.range) {
         const AttentionTile& t = plan.tiles[(int64_t)n * tiles + tile];
-        return {t.lo, t.hi, t.most, t.least};
+        return {max(t.lo, 0), min(t.hi, (int)a.T), t.most, t.least};  // in range whatever a workspace in other use by now holds
     }
     const int T = (int)a.T;
     return a.causal ? Hull{0, min(q0 + kTileT, T), 0, q0 + 1} : Hull{0, T, 0, T};
@@ -630,7 +630,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                 }
                 int n = 0, h = -2, tile = 0;
                 Hull hull[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-                if (id < items.total) {
+                if ((uint32_t)id < (uint32_t)items.total) {
                     n = items.example(id), h = items.head(id), tile = items.tile(id);
                     hull[0] = hull_of(a, plan, n, items.tiles, tile), hull[1] = hull_of(a, plan, n, items.tiles, tile + !items.by_head);
                 }
