@@ -6,7 +6,7 @@ import paper_2609_38767_gb300 as tda
 from attention_reference import Bounds, bias_of, gradients
 from attention_table import table_bound
 from paper_2609_38767_gb300 import build as tbuild
-from test_gpu_attention import BF, F32, Problem, near
+from test_gpu_attention import BF, F32, MORE, Problem, check_backward, check_forward, near
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +54,30 @@ def test_one_bucket_for_all_distances(dev, N, T, H, KV, hd, mask, cap, buckets, 
         assert (diagonal > 4 * tol[bucket]).all()  # what a diagonal counted twice or not at all leaves
         p.dtable[bucket] = 0
     assert (p.dtable == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("shape,mask,cap,buckets,reach,slope", MORE + [
+    ((2, 1030, 4, 1, 64), "docs", 30.0, 32, 128, False), ((1, 2000, 2, 2, 128), "full", 0.0, 40, 511, False),
+    ((1, 1100, 4, 2, 64), "any", 50.0, 12, 300, True)])
+def test_long_examples(dev, shape, mask, cap, buckets, reach, slope, dtype):
+    p = Problem(dev, *shape, dtype, mask, cap, buckets, reach, slope)
+    toward_values(p)
+    idle = ~p.seen.any(2).reshape(-1)
+    p.dO[idle] = float("nan")
+    check_table(p)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hd,cap,buckets", [(64, 0.0, 0), (128, 30.0, 16), (64, 0.0, 16)])
+def test_causal_order_as_ranges(dev, hd, cap, buckets, dtype):
+    """Keys up to the token itself, said by ranges."""
+    p = Problem(dev, 2, 450, 4, 2, hd, dtype, "causal_range", cap, buckets, 60 if buckets else 0)
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+    got = [x.clone() for x in (p.O, p.lse, p.dQ, p.dK, p.dV)]
+    p.range, p.L.causal = None, 1
+    f, b = check_forward(p)
+    check_backward(p, f, b)
+    for x, y in zip(got, (p.O, p.lse, p.dQ, p.dK, p.dV)):
+        assert torch.equal(x, y)  # the same tiles in the same order
