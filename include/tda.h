@@ -760,7 +760,7 @@ typedef struct {
     int32_t head_dim;
     int32_t dtype;        /* tda_dtype: TDA_BF16 or TDA_F32 */
     float scale;          /* > 0 */
-    float cap;            /* >= 0 */
+    float cap;            /* >= 0; 2^100 and more bends nothing: as 0 */
     int32_t causal;       /* 0 or 1 */
     int32_t n_buckets;    /* 0 ... 1024 */
     int64_t max_distance; /* 0 ... 2^20 */

@@ -114,7 +114,8 @@ tda_status check_attention_inputs(const tda_attention_desc* L, const void* Q, in
 Attention attention_of(const tda_attention_desc* L) {
     Attention a = {};
     a.N = L->N, a.T = L->T, a.H = L->heads, a.KV = L->kv_heads, a.hd = L->head_dim, a.dt = (tda_dtype)L->dtype;
-    a.scale = L->scale, a.cap = L->cap, a.causal = L->causal, a.n_buckets = L->n_buckets, a.reach = L->max_distance;
+    // cap tanh(x / cap) is x in fp32 for any |x| < 2^88 then; x / cap would lose its digits below fp32's smallest normal number
+    a.scale = L->scale, a.cap = L->cap < 0x1p100f ? L->cap : 0.f, a.causal = L->causal, a.n_buckets = L->n_buckets, a.reach = L->max_distance;
     return a;
 }
 

@@ -2,6 +2,8 @@
 // pass, a row's visible keys, the scores' cap and biases. Internal.
 #pragma once
 
+#include <cfloat>
+
 #include <cuda_bf16.h>
 
 #include "tda_internal.cuh"

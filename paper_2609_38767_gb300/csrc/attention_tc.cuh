@@ -118,6 +118,8 @@ __device__ __forceinline__ float rcp_fast(float x) {
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c);
 __device__ __forceinline__ float2 mul2(float2 a, float2 b);
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+// What a dot product is of the cap; held finite, as 0 times it is 0 however small the cap.
+__device__ __forceinline__ float over_cap(const Attention& a) { return a.cap > 0.f ? fminf(a.scale / a.cap, FLT_MAX) : 0.f; }
 // d P(d^2) for two dot products within a.near_limit, |x| <= 1/2: tanh to a relative error of 2^-23.1 (the fit is in
 // attention_near), five instructions a pair and the caller's product with d. Any x: 1 - 2 / (1 + e^2x), right at both
 // infinities, 2^-22 absolute, two special functions a value beside its weight's exponential, of which the SM has 32 (exp2) and

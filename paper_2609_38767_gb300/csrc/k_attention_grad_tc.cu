@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_tc_kernel(
         const int quarter = warp / 4, row = warp % 4 * 32 + lane, key = k0 + row;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
         const uint32_t ts = tS + lanes + 32 * quarter, tp = tP + lanes + 32 * quarter;
-        const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        const float inv_cap = RICH ? over_cap(a) : 0.f;
         bool ok = true;
         int2 range = make_int2(0, 0);  // what query 32 quarter + lane of the step's tile sees
         auto look = [&](int qt) {
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
         take_registers();
         const int quarter = warp / 4, row = warp % 4 * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4) << 21;
-        const float inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f;
+        const float inv_cap = RICH ? over_cap(a) : 0.f;
         const float by = RICH && a.cap > 0.f ? -a.scale : a.scale;  // the slope's sign
         uint32_t it = 0, diags = 0, done = 0, written = 0, sums = 0;  // key tiles, diagonals, outputs, items' sums, rows' sums so far
         float* halves = (float*)(raw + S::kHalves) + warp * 128;

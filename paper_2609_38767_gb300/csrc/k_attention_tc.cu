@@ -248,7 +248,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
         const float* biases = (const float*)(from + S::kBias) + w * 2 * kWindow + window_row(row) + 64 * half;
         const float c = RICH ? 1.f : a.scale * kLog2e;  // s is the score times log2 e (RICH) or the dot product
         const float2 c2 = both(c);
-        const float grow = 8.f / c, inv_cap = RICH && a.cap > 0.f ? a.scale / a.cap : 0.f, cap2 = a.cap * kLog2e;
+        const float grow = 8.f / c, inv_cap = RICH ? over_cap(a) : 0.f, cap2 = a.cap * kLog2e;
         bool ok = true;
         // RICH: a barrier of the two warps that share rows, and the larger of their maxima. A wait that ran out in one of them ends
         // both here: until then either goes on, so that the other is not left alone.
