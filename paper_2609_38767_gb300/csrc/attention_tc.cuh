@@ -52,18 +52,6 @@ __device__ __forceinline__ void mma_heads(uint32_t lead, uint32_t d, uint32_t a,
     for (int k = 0; k < HD / 16; ++k)
         if (k < steps) mma_ss(lead, d, da + ((k / 4 * kPanel + k % 4 * 32) >> 4), db + ((k / 4 * kPanel + k % 4 * 32) >> 4), idesc, k > 0);
 }
-// D (+)= A B over K tokens: A in TMEM, B [tokens][head] MN-major in panels.
-template <int K>
-__device__ __forceinline__ void mma_tokens(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool first) {
-    const uint64_t db = mn_major(b, kPanel);
-#pragma unroll
-    for (int k = 0; k < K / 16; ++k) mma_ts(lead, d, a + 8 * k, db + (k * 2048 >> 4), idesc, !first || k > 0);
-}
-
-#define TMEM_R32(r)                                                                                                              \
-    (r)[0], (r)[1], (r)[2], (r)[3], (r)[4], (r)[5], (r)[6], (r)[7], (r)[8], (r)[9], (r)[10], (r)[11], (r)[12], (r)[13], (r)[14], \
-        (r)[15], (r)[16], (r)[17], (r)[18], (r)[19], (r)[20], (r)[21], (r)[22], (r)[23], (r)[24], (r)[25], (r)[26], (r)[27],     \
-        (r)[28], (r)[29], (r)[30], (r)[31]
 // 32 lanes x 32 columns into registers; nothing may use them before tmem_wait_ld and tmem_use.
 __device__ __forceinline__ void tmem_ld32(uint32_t t, float* r) {
     asm volatile(

@@ -52,7 +52,8 @@ __device__ __forceinline__ void arrive_warp(uint64_t* bar) {
     __syncwarp();
     if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(bar));
 }
-// D (+)= A B over 128 tokens: A in TMEM, 16 columns of every 32 (the quarters that the row warps write), B as mma_tokens'.
+// D (+)= A B over 128 tokens: A in TMEM, 16 columns of every 32 (the quarters that the row warps write), B [tokens][head] MN-major in
+// panels.
 __device__ __forceinline__ void mma_quarters(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool first) {
     const uint64_t db = mn_major(b, kPanel);
 #pragma unroll

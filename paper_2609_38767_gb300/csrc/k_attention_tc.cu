@@ -74,22 +74,21 @@ struct BarsOf {
     int example[4];
 };
 
-// Keys that a tile's queries see, and between which all of them see all.
+// Keys that a tile's queries see.
 struct Hull {
-    int lo, hi, most, least;
+    int lo, hi;
     __device__ __forceinline__ bool any() const { return lo < hi; }
     __device__ __forceinline__ int first() const { return lo / kTileT; }
     __device__ __forceinline__ int last() const { return (hi - 1) / kTileT; }
 };
 __device__ __forceinline__ Hull hull_of(const Attention& a, const AttentionPlan& plan, int n, int tiles, int tile) {
-    const int q0 = tile * kTileT;
-    if (q0 >= a.T) return {0, 0, 0, 0};
+    const int q0 = tile * kTileT, T = (int)a.T;
+    if (q0 >= T) return {0, 0};
     if (a.range) {
         const AttentionTile& t = plan.tiles[(int64_t)n * tiles + tile];
-        return {max(t.lo, 0), min(t.hi, (int)a.T), t.most, t.least};  // in range whatever a workspace in other use by now holds
+        return {max(t.lo, 0), min(t.hi, T)};  // in range whatever a workspace in other use by now holds
     }
-    const int T = (int)a.T;
-    return a.causal ? Hull{0, min(q0 + kTileT, T), 0, q0 + 1} : Hull{0, T, 0, T};
+    return {0, a.causal ? min(q0 + kTileT, T) : T};
 }
 
 // The items of this CTA, long ones first where the mask is causal; every other round backwards, which evens out what the rounds
@@ -629,7 +628,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
                     id = __shfl_sync(0xffffffffu, id, 0);
                 }
                 int n = 0, h = -2, tile = 0;
-                Hull hull[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                Hull hull[2] = {{0, 0}, {0, 0}};
                 if ((uint32_t)id < (uint32_t)items.total) {
                     n = items.example(id), h = items.head(id), tile = items.tile(id);
                     hull[0] = hull_of(a, plan, n, items.tiles, tile), hull[1] = hull_of(a, plan, n, items.tiles, tile + !items.by_head);
