@@ -478,19 +478,23 @@ struct DqReader {
         return x.h >= 0;
     }
 };
+// The key tiles of one item after the other. busy: see the forward pass; here the rows' warps wait for dQ's products before they read on.
 struct DqWalk {
     DqItem item;
     int kt = 0, last = 0;
-    bool valid = true;
+    bool valid = true, ended = false;
     DqReader reader;
-    __device__ __forceinline__ void next(DqBars& bars, bool* ok, volatile int* abort, unsigned int* err) {
-        if (!valid) return;
+    __device__ __forceinline__ void next(bool busy, DqBars& bars, bool* ok, volatile int* abort, unsigned int* err) {
         if (kt < last) {
             ++kt;
             return;
         }
-        do valid = reader.next(item, bars, ok, abort, err);
-        while (valid && item.first > item.last);
+        valid = false;
+        while (!ended && !valid) {
+            ended = !reader.next(item, bars, ok, abort, err);
+            valid = !ended && item.first <= item.last;
+            if (busy) break;
+        }
         kt = item.first, last = item.last;
     }
 };
@@ -795,7 +799,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             uint32_t loaded_v = 0;
             DqWalk x;
             while (true) {
-                x.next(bars, &ok, abort, err);
+                x.next(false, bars, &ok, abort, err);
                 if (!ok || !x.valid) break;
                 const uint32_t k = used % S::kK, v = used % S::kV;
                 const int kv = items.group.div(x.item.h), k0 = x.kt * kTileT;
@@ -830,7 +834,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_tc_kernel(
             // S, dP of the key tile after `now`, then dQ of `now`
             while (true) {
                 const uint32_t at = now.valid ? it + 1 : it;
-                then.next(bars, &ok, abort, err);
+                then.next(now.valid, bars, &ok, abort, err);
                 if (!ok || (!now.valid && !then.valid)) break;
                 if (then.valid) {
                     const uint32_t tile_k = sk + at % S::kK * kBytes;

@@ -148,22 +148,27 @@ struct ItemReader {
     }
 };
 
-// A key tile of an item; next() goes on to the next item that has any.
+// A key tile of an item; next() goes on to the next item that has any, whose first one it gives. busy: products of the tile before
+// are still to be issued, so only the item right behind is looked at, and where it has no keys there is no tile for now (!valid): items
+// come four at a time, the outputs' warps do not pass theirs before its products, and the one wanted may not be made until they do.
 struct Walk {
     Item item;
     int kt, last;
-    bool valid = true;
+    bool valid = true, ended = false;
     ItemReader reader;
     __device__ __forceinline__ void clear() { kt = last = 0; }  // next() then gives the first
     template <typename Bars>
-    __device__ __forceinline__ void next(Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
-        if (!valid) return;
+    __device__ __forceinline__ void next(bool busy, Bars& bars, bool* ok, volatile int* abort, unsigned int* err) {
         if (kt < last) {
             ++kt;
             return;
         }
-        do valid = reader.next(item, bars, ok, abort, err);
-        while (valid && !item.any());
+        valid = false;
+        while (!ended && !valid) {
+            ended = !reader.next(item, bars, ok, abort, err);
+            valid = !ended && item.any();
+            if (busy) break;
+        }
         kt = min(item.of[0].first, item.of[1].first), last = max(item.of[0].last, item.of[1].last);
     }
     __device__ __forceinline__ bool active(int w) const { return kt >= item.of[w].first && kt <= item.of[w].last; }
@@ -592,7 +597,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             Walk at;
             at.clear();
             while (true) {
-                at.next(bars, &ok, abort, err);
+                at.next(false, bars, &ok, abort, err);
                 if (!ok || !at.valid) break;
                 const int kv = items.group.div(at.item.of[0].h);
 #pragma unroll 1
@@ -685,7 +690,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             // a step: O += P V of the key tile `now`, then S of the one after it, for either tile of queries
             while (true) {
                 const uint32_t at_v = used, at_k = now.valid ? used + 1 : used;
-                then.next(bars, &ok, abort, err);
+                then.next(now.valid, bars, &ok, abort, err);
                 if (!ok || (!now.valid && !then.valid)) break;
                 uint64_t v = 0;
                 if (now.valid) {
@@ -751,7 +756,7 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
             Walk at;
             at.clear();
             while (true) {
-                at.next(bars, &ok, abort, err);
+                at.next(false, bars, &ok, abort, err);
                 if (!ok || !at.valid) break;
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
