@@ -714,14 +714,19 @@ tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float ma
  *   lse    [N][heads][T] fp32, natural logarithm, or NULL.
  * Sums and statistics are fp32. bf16: products of bf16 values, P rounded to bf16 for the
  * product with V (its sum is of the unrounded values); fp32: fp32 throughout.
- * A bias of -inf hides a pair, and a row whose pairs are all hidden is one that sees
- * nothing; a finite bias below -2^127 counts as -2^127. What lies in a token that no token
- * sees, or in the query of one that sees nothing, may be anything, NaN included. A NaN or
- * infinity elsewhere may make other rows of its example and head non-finite.
+ * A bias of -inf hides a pair, and a row whose pairs are all hidden has O 0 and lse -inf; a
+ * finite bias below -2^127 counts as -2^127. lse is fp32 and the backward pass takes P from it:
+ * where all keys of a row have biases of size B, P is off by 2^-24 B of itself there (-inf hides
+ * without that; the type's lowest value only where another key is seen). What lies in a token
+ * that is in no token's range, or in the query and dO of one whose range is empty, may be
+ * anything, NaN included; pairs that a bias hides are computed. A NaN or infinity elsewhere may
+ * make other rows of its example and head non-finite.
  * head_dim <= 128 (else TDA_ERR_UNSUPPORTED); any strides and element alignment; bf16 with
  * head_dim a multiple of 8 and rows on 16 bytes runs on the tensor cores (sm_103), anything
  * else on the CUDA cores. N or T may be 0; T <= 2^29, N * T * heads <= 2^31 - 2^16 - 2 and
- * N * ceil(T / 64) * heads <= 2^30 - 2^15 - 1. ws: tda_attention_workspace_size(op, L)
+ * N * ceil(T / 64) * heads <= 2^30 - 2^15 - 1. On the tensor cores a tile of 128 queries has a
+ * second for its keys (some 10^8), then the call ends in TDA_ERR_TIMEOUT; with a range there is
+ * a part that grows as N * T^2 / 128 (half the time of 2^20 tokens in windows of 511). ws: tda_attention_workspace_size(op, L)
  * bytes, 256-byte aligned. O overlaps no input.
  *
  * tda_attention_backward -- its gradients, given O and lse of the forward pass and dO:

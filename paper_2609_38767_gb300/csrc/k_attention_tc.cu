@@ -780,7 +780,8 @@ __global__ __launch_bounds__(Warps<RICH>::kThreads, 1) void attention_tc_kernel(
 }
 
 // One CTA per tile of 128 tokens and example: what its queries see, and which of its tokens nothing sees; the CTAs
-// behind them fill the biases by distance.
+// behind them fill the biases by distance. Every CTA reads all ranges of its example, T^2 / 128 in all: simple, and 10 us with the
+// ranges' own kernel at 4 x 2047 tokens, but where the attention is linear in T (windows of 511) half of the 7.7 ms of 1,048,576 tokens.
 __global__ __launch_bounds__(256) void attention_plan_kernel(const Attention a, const AttentionPlan plan, int ranged) {
     const int t = threadIdx.x;
     if ((int)blockIdx.x >= ranged) {
