@@ -726,8 +726,8 @@ tda_status tda_grad_clip(const tda_tensor_ref* list, int64_t n_tensors, float ma
  * else on the CUDA cores. N or T may be 0; T <= 2^29, N * T * heads <= 2^31 - 2^16 - 2 and
  * N * ceil(T / 64) * heads <= 2^30 - 2^15 - 1. On the tensor cores a tile of 128 queries has a
  * second for its keys (some 10^8), then the call ends in TDA_ERR_TIMEOUT; with a range there is
- * a part that grows as N * T^2 / 128 (half the time of 2^20 tokens in windows of 511). ws: tda_attention_workspace_size(op, L)
- * bytes, 256-byte aligned. O overlaps no input.
+ * a part that grows as N * T^2 / 128 (half the time of 2^20 tokens in windows of 511).
+ * ws: tda_attention_workspace_size(op, L) bytes, 256-byte aligned. O overlaps no input.
  *
  * tda_attention_backward -- its gradients, given O and lse of the forward pass and dO:
  *   dV_j = sum P_ij dO_i,   dP_ij = dO_i . v_j,   dS_ij = P_ij (dP_ij - dO_i . O_i),
